@@ -441,6 +441,110 @@ size_t gbdt_grow_tree_depthwise_scratch_bytes(int64_t n_rows, int32_t n_features
                                               int32_t max_depth);
 
 /*
+ * ---- Linear leaves ----------------------------------------------------------------------
+ *
+ * A tree routes every row to one leaf, and its growers leave the rows of the leaves side by
+ * side on the device (row_order_out, row_begin, count).  A constant leaf answers with one
+ * number; a linear leaf answers with a linear map of the row's features:
+ *
+ *   y[d] = W_l x[d] + b_l   for the rows d = row_idx[p], leaf_offsets[l] <= p < leaf_offsets[l + 1]
+ *
+ * Matrices here are row-major in one of two element types; ld_* is the distance of rows in
+ * elements, at least the row's length; pointers need only their element's alignment, but
+ * rows of whole 16-byte chunks (16-byte aligned, lengths and distances a multiple of 8 bf16 or
+ * 4 f32) take a faster path.  bf16 products are exact in f32, sums are kept in f32, results are
+ * rounded once to the element type, to nearest even.
+ */
+typedef enum { GBDT_F32 = 0, GBDT_BF16 = 1 } gbdt_dtype;
+
+/*
+ *   x             DEVICE [n_rows][d_in], by ROW ID (rows of no leaf are not read)
+ *   weight        DEVICE [n_leaves][d_out][d_in], dense
+ *   bias          DEVICE [n_leaves][d_out] or NULL
+ *   row_idx       DEVICE int32 [n_positions], or NULL: position p is row p (n_positions <= n_rows).
+ *                 A row belongs to one leaf at most; entries outside [0, n_rows) are passed over
+ *   leaf_offsets  DEVICE int64 [n_leaves + 1], not decreasing; leaves may be empty, positions
+ *                 before the first and from the last offset on belong to no leaf, offsets
+ *                 outside [0, n_positions] are taken as its ends.  They are on the device so that a
+ *                 caller that routes rows there need not wait for their numbers
+ *   y_out         DEVICE [n_rows][d_out], by ROW ID; rows of no leaf are left as they are
+ * n_rows and n_positions < 2^30, n_leaves, d_in and d_out < 2^24 (GBDT_EUNSUPPORTED beyond).
+ */
+int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const void* bias,
+                      const int32_t* row_idx, const int64_t* leaf_offsets, int64_t n_positions,
+                      int32_t n_leaves, int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype,
+                      void* y_out, int64_t ld_y, void* stream);
+
+/*
+ * Its gradients, of which any may be NULL:
+ *   dx_out[d]        = W_l^T dy[d]                 DEVICE [n_rows][d_in]; rows of no leaf are left as they are
+ *   dweight_out[l]   = sum over leaf l of dy[d] x[d]^T   DEVICE [n_leaves][d_out][d_in], zeros for an empty leaf
+ *   dbias_out[l]     = sum over leaf l of dy[d]    DEVICE [n_leaves][d_out], zeros for an empty leaf
+ * weight is read for dx only, x for dweight only.  Long leaves are summed in parts, whose f32
+ * sums lie in the library's scratch and are added in the order of the list: the same call gives
+ * the same bits.  gbdt_leaf_product_grad_workspace_bytes: the size of a registered workspace
+ * (gbdt_set_workspace) that suffices (0 on invalid arguments).
+ */
+int gbdt_leaf_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
+                           const void* weight, const int32_t* row_idx, const int64_t* leaf_offsets,
+                           int64_t n_positions, int32_t n_leaves, int64_t n_rows, int32_t d_in,
+                           int32_t d_out, int32_t dtype, void* dx_out, int64_t ld_dx,
+                           void* dweight_out, void* dbias_out, void* stream);
+size_t gbdt_leaf_product_grad_workspace_bytes(int64_t n_positions, int32_t d_in, int32_t d_out);
+
+/*
+ * ---- Softmax over many classes ------------------------------------------------------------
+ *
+ * What the rows' answers are trained by, and where the gradients and hessians of a tree with
+ * many classes come from.  A row's answer h_d (an embedding) meets a matrix of classes:
+ *
+ *   s_v = <h_d, c_v>   lse_d = log sum_v exp(s_v)   loss_d = lse_d - s_{y_d}   p_v = exp(s_v - lse_d)
+ *
+ * The n_rows x n_classes scores are never stored.
+ *   h        DEVICE [n_rows][dim]
+ *   classes  DEVICE [n_classes][dim]
+ *   labels   DEVICE int32 [n_rows].  A row whose label is outside [0, n_classes) is ignored: its
+ *            loss, lse, gradients and hessians are 0 and it takes no part in any sum, whatever
+ *            its h holds.  NULL (loss_out NULL as well): every row counts and none has a label
+ *   loss_out, lse_out   DEVICE float [n_rows]
+ * n_rows and n_classes < 2^30, dim < 2^24 (GBDT_EUNSUPPORTED beyond).  An infinite or NaN score
+ * goes where the formula takes it.
+ */
+int gbdt_softmax_loss(const void* h, int64_t ld_h, const void* classes, int64_t ld_c,
+                      const int32_t* labels, int64_t n_rows, int64_t n_classes, int32_t dim,
+                      int32_t dtype, float* loss_out, float* lse_out, void* stream);
+
+/*
+ * Gradients of scale * sum_d row_weight[d] * loss_d, either of which may be NULL:
+ *   dh_out        DEVICE [n_rows][dim]
+ *   dclasses_out  DEVICE [n_classes][dim]
+ *   lse           DEVICE float [n_rows], as gbdt_softmax_loss left it
+ *   row_weight    DEVICE float [n_rows] or NULL (all 1)
+ * The classes are taken in pieces, whose row_weight * (p - [v = y]) lies in the library's scratch
+ * in the element type (about 256 MiB, or 256 classes for all rows if that is more), beside f32 sums
+ * of dh.  gbdt_softmax_workspace_bytes: the size of a registered workspace that suffices for
+ * this call and gbdt_softmax_loss (0 on invalid arguments).  The same call gives the same bits.
+ */
+int gbdt_softmax_grad(const void* h, int64_t ld_h, const void* classes, int64_t ld_c,
+                      const int32_t* labels, const float* lse, const float* row_weight, float scale,
+                      int64_t n_rows, int64_t n_classes, int32_t dim, int32_t dtype, void* dh_out,
+                      int64_t ld_dh, void* dclasses_out, int64_t ld_dc, void* stream);
+size_t gbdt_softmax_workspace_bytes(int64_t n_rows, int64_t n_classes, int32_t dim, int32_t dtype);
+
+/*
+ * First and second derivative of the loss by the scores of classes class_begin .. class_end - 1,
+ * a column of n_rows floats a class, as gbdt_hist_build takes its grad and hess:
+ *   grad_out[v - class_begin][d] = p_v - [v = y_d]     hess_out[..][d] = p_v (1 - p_v)
+ *   lse      DEVICE float [n_rows], as gbdt_softmax_loss left it
+ *   labels   NULL: grad_out holds p_v itself (what a trained model answers with)
+ *   ld_out   distance of the columns, >= n_rows
+ */
+int gbdt_softmax_stats(const void* h, int64_t ld_h, const void* classes, int64_t ld_c,
+                       const int32_t* labels, const float* lse, int64_t n_rows, int64_t n_classes,
+                       int32_t dim, int32_t dtype, int64_t class_begin, int64_t class_end,
+                       float* grad_out, float* hess_out, int64_t ld_out, void* stream);
+
+/*
  * Scratch workspace.  By default the library allocates device scratch itself
  * on first use and grows it when a larger problem arrives (hipMalloc inside
  * gbdt_hist_build / gbdt_best_split / gbdt_partition_rows).  A caller that wants no allocation in

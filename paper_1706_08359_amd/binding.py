@@ -33,6 +33,8 @@ EXPORTS = [
     "gbdt_set_wide_accumulation", "gbdt_profile_durations", "gbdt_reset",
     "gbdt_hist_build_noalloc", "gbdt_hist_build_noalloc_max_partial_bytes",
     "gbdt_bins_fused_bytes", "gbdt_bins_fuse", "gbdt_bins_unfuse", "gbdt_debug_fusion_plan",
+    "gbdt_leaf_product", "gbdt_leaf_product_grad", "gbdt_leaf_product_grad_workspace_bytes",
+    "gbdt_softmax_loss", "gbdt_softmax_grad", "gbdt_softmax_stats", "gbdt_softmax_workspace_bytes",
 ]
 
 # numpy views of the two C structs
@@ -140,6 +142,29 @@ def load():
     lib.gbdt_set_wide_accumulation.argtypes = [c.c_int]
     lib.gbdt_calibration_copy.restype = c.c_int
     lib.gbdt_calibration_copy.argtypes = [c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+    lib.gbdt_leaf_product.restype = c.c_int
+    lib.gbdt_leaf_product.argtypes = [c.c_void_p, c.c_int64, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p,
+                                      c.c_int64, c.c_int32, c.c_int64, c.c_int32, c.c_int32, c.c_int32,
+                                      c.c_void_p, c.c_int64, c.c_void_p]
+    lib.gbdt_leaf_product_grad.restype = c.c_int
+    lib.gbdt_leaf_product_grad.argtypes = [c.c_void_p, c.c_int64, c.c_void_p, c.c_int64, c.c_void_p, c.c_void_p,
+                                           c.c_void_p, c.c_int64, c.c_int32, c.c_int64, c.c_int32, c.c_int32,
+                                           c.c_int32, c.c_void_p, c.c_int64, c.c_void_p, c.c_void_p, c.c_void_p]
+    lib.gbdt_leaf_product_grad_workspace_bytes.restype = c.c_size_t
+    lib.gbdt_leaf_product_grad_workspace_bytes.argtypes = [c.c_int64, c.c_int32, c.c_int32]
+    lib.gbdt_softmax_loss.restype = c.c_int
+    lib.gbdt_softmax_loss.argtypes = [c.c_void_p, c.c_int64, c.c_void_p, c.c_int64, c.c_void_p, c.c_int64,
+                                      c.c_int64, c.c_int32, c.c_int32, c.c_void_p, c.c_void_p, c.c_void_p]
+    lib.gbdt_softmax_grad.restype = c.c_int
+    lib.gbdt_softmax_grad.argtypes = [c.c_void_p, c.c_int64, c.c_void_p, c.c_int64, c.c_void_p, c.c_void_p,
+                                      c.c_void_p, c.c_float, c.c_int64, c.c_int64, c.c_int32, c.c_int32,
+                                      c.c_void_p, c.c_int64, c.c_void_p, c.c_int64, c.c_void_p]
+    lib.gbdt_softmax_stats.restype = c.c_int
+    lib.gbdt_softmax_stats.argtypes = [c.c_void_p, c.c_int64, c.c_void_p, c.c_int64, c.c_void_p, c.c_void_p,
+                                       c.c_int64, c.c_int64, c.c_int32, c.c_int32, c.c_int64, c.c_int64,
+                                       c.c_void_p, c.c_void_p, c.c_int64, c.c_void_p]
+    lib.gbdt_softmax_workspace_bytes.restype = c.c_size_t
+    lib.gbdt_softmax_workspace_bytes.argtypes = [c.c_int64, c.c_int64, c.c_int32, c.c_int32]
     _lib = lib
     return lib
 
@@ -669,6 +694,178 @@ def gbdt_debug_wide_pair(first, second):
     lib.gbdt_debug_wide_pair.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p]
     _check(lib.gbdt_debug_wide_pair(a.ctypes.data, b.ctypes.data, a.size, out), "gbdt_debug_wide_pair")
     return tuple(int(v) for v in out)
+
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1}   # gbdt_dtype
+
+
+def _mat(t: torch.Tensor, dtype, rows, cols: int, name: str):
+    """(address, distance of rows in elements) of a 2-D tensor whose rows are dense; they may lie apart."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[1] == cols
+            and (rows is None or t.shape[0] == rows)):
+        raise TypeError(f"{name}: expected a CUDA tensor of dtype {dtype} and shape [{'n' if rows is None else rows}, {cols}]")
+    ld = t.stride(0) if t.shape[0] > 1 else cols
+    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        raise TypeError(f"{name}: the elements of a row must lie side by side and rows must not overlap")
+    return t.data_ptr(), ld
+
+
+def _dense(t: torch.Tensor, dtype, shape, name: str) -> int:
+    if tuple(t.shape) != tuple(shape):
+        raise TypeError(f"{name}: expected shape {tuple(shape)}")
+    return _dev(t, dtype, name)
+
+
+def _element_type(t: torch.Tensor, name: str) -> int:
+    if not isinstance(t, torch.Tensor) or t.dtype not in DTYPES:
+        raise TypeError(f"{name}: expected a float32 or bfloat16 tensor")
+    return DTYPES[t.dtype]
+
+
+def _leaf_lists(leaf_offsets, row_idx, n_leaves: int, n_rows: int):
+    if not isinstance(leaf_offsets, torch.Tensor) or leaf_offsets.numel() != n_leaves + 1:
+        raise GbdtError("leaf_offsets: need n_leaves + 1 entries")
+    if row_idx is None:
+        return None, _dev(leaf_offsets, torch.int64, "leaf_offsets"), n_rows
+    return _dev(row_idx, torch.int32, "row_idx"), _dev(leaf_offsets, torch.int64, "leaf_offsets"), row_idx.numel()
+
+
+def gbdt_leaf_product(x, weight, leaf_offsets, row_idx=None, bias=None, y_out=None, stream=None):
+    """y[d] = weight[l] x[d] + bias[l] for every row d of leaf l.  x: [n_rows, d_in]; weight: [n_leaves, d_out, d_in];
+    bias: [n_leaves, d_out]; all float32 or all bfloat16.  leaf_offsets: int64 CUDA tensor [n_leaves + 1] into row_idx
+    (int32 CUDA tensor; None: position p is row p).  Returns y_out [n_rows, d_out]; rows of no leaf keep what y_out
+    holds (zeros if it is made here)."""
+    code = _element_type(x, "x")
+    if weight.dim() != 3 or x.dim() != 2:
+        raise TypeError("expected x [n_rows, d_in] and weight [n_leaves, d_out, d_in]")
+    n_rows, (n_leaves, d_out, d_in) = x.shape[0], weight.shape
+    x_p, ld_x = _mat(x, x.dtype, n_rows, d_in, "x")
+    w_p = _dev(weight, x.dtype, "weight")
+    b_p = None if bias is None else _dense(bias, x.dtype, (n_leaves, d_out), "bias")
+    idx_p, off_p, n_positions = _leaf_lists(leaf_offsets, row_idx, n_leaves, n_rows)
+    if y_out is None:
+        y_out = torch.zeros((n_rows, d_out), dtype=x.dtype, device=x.device)
+    y_p, ld_y = _mat(y_out, x.dtype, n_rows, d_out, "y_out")
+    _check(load().gbdt_leaf_product(x_p, ld_x, w_p, b_p, idx_p, off_p, n_positions, n_leaves, n_rows, d_in, d_out, code,
+                                    y_p, ld_y, _stream(stream)), "gbdt_leaf_product")
+    return y_out
+
+
+def gbdt_leaf_product_grad(dy, x, weight, leaf_offsets, row_idx=None, dx_out=None, dweight_out=None, dbias_out=None,
+                           want=("x", "weight", "bias"), stream=None):
+    """Gradients of gbdt_leaf_product by what `want` names.  dy: [n_rows, d_out].  Returns (dx [n_rows, d_in],
+    dweight [n_leaves, d_out, d_in], dbias [n_leaves, d_out]), None for what is not wanted; rows of no leaf keep what
+    dx_out holds (zeros if it is made here)."""
+    code = _element_type(x, "x")
+    if weight.dim() != 3 or x.dim() != 2:
+        raise TypeError("expected x [n_rows, d_in] and weight [n_leaves, d_out, d_in]")
+    if not set(want) <= {"x", "weight", "bias"}:
+        raise GbdtError("want: any of 'x', 'weight', 'bias'")
+    n_rows, (n_leaves, d_out, d_in) = x.shape[0], weight.shape
+    x_p, ld_x = _mat(x, x.dtype, n_rows, d_in, "x")
+    dy_p, ld_dy = _mat(dy, x.dtype, n_rows, d_out, "dy")
+    w_p = _dev(weight, x.dtype, "weight")
+    idx_p, off_p, n_positions = _leaf_lists(leaf_offsets, row_idx, n_leaves, n_rows)
+    dx_p = dw_p = db_p = None
+    ld_dx = d_in
+    if "x" in want:
+        if dx_out is None:
+            dx_out = torch.zeros((n_rows, d_in), dtype=x.dtype, device=x.device)
+        dx_p, ld_dx = _mat(dx_out, x.dtype, n_rows, d_in, "dx_out")
+    if "weight" in want:
+        if dweight_out is None:
+            dweight_out = torch.empty((n_leaves, d_out, d_in), dtype=x.dtype, device=x.device)
+        dw_p = _dense(dweight_out, x.dtype, (n_leaves, d_out, d_in), "dweight_out")
+    if "bias" in want:
+        if dbias_out is None:
+            dbias_out = torch.empty((n_leaves, d_out), dtype=x.dtype, device=x.device)
+        db_p = _dense(dbias_out, x.dtype, (n_leaves, d_out), "dbias_out")
+    _check(load().gbdt_leaf_product_grad(dy_p, ld_dy, x_p, ld_x, w_p, idx_p, off_p, n_positions, n_leaves, n_rows, d_in,
+                                         d_out, code, dx_p, ld_dx, dw_p, db_p, _stream(stream)),
+           "gbdt_leaf_product_grad")
+    return (dx_out if dx_p is not None else None, dweight_out if dw_p is not None else None,
+            dbias_out if db_p is not None else None)
+
+
+def gbdt_leaf_product_grad_workspace_bytes(n_positions: int, d_in: int, d_out: int) -> int:
+    return int(load().gbdt_leaf_product_grad_workspace_bytes(n_positions, d_in, d_out))
+
+
+def _softmax_operands(h, classes, labels):
+    code = _element_type(h, "h")
+    if h.dim() != 2:
+        raise TypeError("h: expected [n_rows, dim]")
+    n_rows, dim = h.shape
+    h_p, ld_h = _mat(h, h.dtype, n_rows, dim, "h")
+    c_p, ld_c = _mat(classes, h.dtype, None, dim, "classes")
+    y_p = None if labels is None else _dense(labels, torch.int32, (n_rows,), "labels")
+    return code, n_rows, classes.shape[0], dim, h_p, ld_h, c_p, ld_c, y_p
+
+
+def gbdt_softmax_loss(h, classes, labels=None, loss_out=None, lse_out=None, stream=None):
+    """h: [n_rows, dim], classes: [n_classes, dim], both float32 or both bfloat16; labels: int32 [n_rows].  Returns
+    (loss, lse), float32 [n_rows]; loss is None without labels."""
+    code, n_rows, n_classes, dim, h_p, ld_h, c_p, ld_c, y_p = _softmax_operands(h, classes, labels)
+    if labels is not None and loss_out is None:
+        loss_out = torch.empty(n_rows, dtype=torch.float32, device=h.device)
+    if lse_out is None:
+        lse_out = torch.empty(n_rows, dtype=torch.float32, device=h.device)
+    loss_p = None if loss_out is None else _dense(loss_out, torch.float32, (n_rows,), "loss_out")
+    _check(load().gbdt_softmax_loss(h_p, ld_h, c_p, ld_c, y_p, n_rows, n_classes, dim, code, loss_p,
+                                    _dense(lse_out, torch.float32, (n_rows,), "lse_out"), _stream(stream)),
+           "gbdt_softmax_loss")
+    return loss_out, lse_out
+
+
+def gbdt_softmax_grad(h, classes, labels, lse, row_weight=None, scale=1.0, dh_out=None, dclasses_out=None,
+                      want=("h", "classes"), stream=None):
+    """Gradients of scale * sum(row_weight * loss) by what `want` names.  Returns (dh [n_rows, dim],
+    dclasses [n_classes, dim]), None for what is not wanted."""
+    if labels is None:
+        raise TypeError("labels: expected an int32 CUDA tensor")
+    if not set(want) <= {"h", "classes"}:
+        raise GbdtError("want: any of 'h', 'classes'")
+    code, n_rows, n_classes, dim, h_p, ld_h, c_p, ld_c, y_p = _softmax_operands(h, classes, labels)
+    w_p = None if row_weight is None else _dense(row_weight, torch.float32, (n_rows,), "row_weight")
+    dh_p = dc_p = None
+    ld_dh = ld_dc = dim
+    if "h" in want:
+        if dh_out is None:
+            dh_out = torch.empty((n_rows, dim), dtype=h.dtype, device=h.device)
+        dh_p, ld_dh = _mat(dh_out, h.dtype, n_rows, dim, "dh_out")
+    if "classes" in want:
+        if dclasses_out is None:
+            dclasses_out = torch.empty((n_classes, dim), dtype=h.dtype, device=h.device)
+        dc_p, ld_dc = _mat(dclasses_out, h.dtype, n_classes, dim, "dclasses_out")
+    _check(load().gbdt_softmax_grad(h_p, ld_h, c_p, ld_c, y_p, _dense(lse, torch.float32, (n_rows,), "lse"), w_p,
+                                    float(scale), n_rows, n_classes, dim, code, dh_p, ld_dh, dc_p, ld_dc,
+                                    _stream(stream)), "gbdt_softmax_grad")
+    return dh_out if dh_p is not None else None, dclasses_out if dc_p is not None else None
+
+
+def gbdt_softmax_stats(h, classes, labels, lse, class_begin, class_end, grad_out=None, hess_out=None, stream=None):
+    """Gradient and hessian columns of classes class_begin .. class_end - 1, float32 [class_end - class_begin, n_rows]
+    each: grad[i], hess[i] are what gbdt_hist_build takes.  labels None: grad holds the probabilities."""
+    code, n_rows, n_classes, dim, h_p, ld_h, c_p, ld_c, y_p = _softmax_operands(h, classes, labels)
+    count = class_end - class_begin
+    if class_begin < 0 or count < 0 or class_end > n_classes:
+        raise GbdtError("class_begin, class_end: outside the classes")
+    if grad_out is None:
+        grad_out = torch.empty((count, n_rows), dtype=torch.float32, device=h.device)
+    if hess_out is None:
+        hess_out = torch.empty((count, n_rows), dtype=torch.float32, device=h.device)
+    g_p, ld_g = _mat(grad_out, torch.float32, count, n_rows, "grad_out")
+    k_p, ld_k = _mat(hess_out, torch.float32, count, n_rows, "hess_out")
+    if ld_g != ld_k:
+        raise GbdtError("grad_out, hess_out: columns must lie the same distance apart")
+    _check(load().gbdt_softmax_stats(h_p, ld_h, c_p, ld_c, y_p, _dense(lse, torch.float32, (n_rows,), "lse"), n_rows,
+                                     n_classes, dim, code, class_begin, class_end, g_p, k_p, ld_g, _stream(stream)),
+           "gbdt_softmax_stats")
+    return grad_out, hess_out
+
+
+def gbdt_softmax_workspace_bytes(n_rows: int, n_classes: int, dim: int, dtype=torch.float32) -> int:
+    return int(load().gbdt_softmax_workspace_bytes(n_rows, n_classes, dim, DTYPES[dtype]))
 
 
 def gbdt_set_deterministic(enable: bool) -> None:

@@ -1,0 +1,268 @@
+// Products grouped by leaf: y[d] = W_l x[d] + b_l for the rows d of leaf l, and its gradients.
+//
+// Positions p of the row list are grouped by leaf: leaf l holds offsets[l] <= p < offsets[l + 1], p's row is row_idx[p].
+// offsets are read on the device, so nothing waits for the host between routing rows and using them; the host knows only
+// the number of positions and of leaves.  Tiles of BM positions never cross a leaf: leaf l owns the tiles from
+// T(l) = offsets[l] / BM + l on.  T rises by at least the number of tiles that the leaf needs, because
+// ceil((b - a) / BM) <= floor(b / BM) - floor(a / BM) + 1, so positions / BM + leaves workgroups hold every tile whatever the
+// lengths are, no sum over the leaves before a leaf is needed, and a tile finds its leaf by a search over T.
+#pragma once
+
+#include "tile_product.h"
+
+namespace gbdt_leaf {
+
+using namespace gbdt_tile;
+
+template <typename T>
+struct LeafArgs {
+  const T* x;         // [n_rows][d_in]
+  const T* dy;        // [n_rows][d_out]
+  const T* w;         // [n_leaves][d_out][d_in]
+  const T* bias;      // [n_leaves][d_out] or null
+  T* y;               // [n_rows][d_out]
+  T* dx;              // [n_rows][d_in]
+  T* dw;              // [n_leaves][d_out][d_in] or null
+  T* dbias;           // [n_leaves][d_out] or null
+  float* partial;     // 2 slots a cut of the position axis, of (d_in + 1) * d_out sums each
+  const int32_t* row_idx;  // or null: row = position
+  const int64_t* offsets;  // [n_leaves + 1]
+  int64_t ld_x, ld_dy, ld_y, ld_dx;
+  int32_t n_positions, n_leaves, n_rows, d_in, d_out;
+  int32_t cut;        // gradient of the weights: positions between cuts
+  uint32_t col_tiles, row_tiles;
+};
+
+// An offset as the kernels take it: inside the list, whatever the array holds.
+__device__ __forceinline__ int offset_at(const int64_t* offsets, int l, int n_positions) {
+  const int64_t o = offsets[l];
+  return o < 0 ? 0 : o > n_positions ? n_positions : (int)o;
+}
+
+// The largest leaf l with offset(l) / unit + l <= tile, by 64 probes at a time; -1 if there is none.
+__device__ __forceinline__ int find_leaf(const int64_t* offsets, int n_leaves, int n_positions, int unit, int tile) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n_leaves;
+  bool any = false;
+  while (hi - lo > 1 || !any) {
+    const int step = (hi - lo + 63) / 64;
+    const int i = lo + lane * step;
+    const bool ok = i < hi && offset_at(offsets, i, n_positions) / unit + i <= tile;
+    const int n = __popcll(__ballot(ok));
+    if (n == 0) return -1;
+    any = true;
+    lo += (n - 1) * step;
+    hi = lo + step < hi ? lo + step : hi;
+  }
+  return lo;
+}
+
+// Rows of a matrix by position in the list.
+template <typename T>
+struct ListRows {
+  const T* base;
+  int64_t ld;
+  const int32_t* row_idx;
+  int32_t end, n_rows;
+  __device__ __forceinline__ const T* operator()(int p) const {
+    if (p >= end) return nullptr;
+    const int d = row_idx ? row_idx[p] : p;
+    return (uint32_t)d < (uint32_t)n_rows ? base + (int64_t)d * ld : nullptr;
+  }
+};
+
+// Rows of a matrix in order.
+template <typename T>
+struct PlainRows {
+  const T* base;
+  int64_t ld;
+  int32_t n;
+  __device__ __forceinline__ const T* operator()(int r) const { return r < n ? base + (int64_t)r * ld : nullptr; }
+};
+
+// Writes the tile's values (N_INNER) to the rows of the list, adding bias if there is one.
+template <class S, typename T>
+__device__ __forceinline__ void scatter_rows(const f32x4 (&acc)[S::TM][S::TN], const T* bias, T* out, int64_t ld, const int32_t* row_idx,
+                                             int p0, int p1, int n_rows, int col0, int cols) {
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int m0 = (w / S::WN) * (S::TM * 16), n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int p = p0 + m0 + 16 * i + (l & 15);
+    if (p >= p1) continue;
+    const int d = row_idx ? row_idx[p] : p;
+    if ((uint32_t)d >= (uint32_t)n_rows) continue;
+    T* to = out + (int64_t)d * ld;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      const int n = n0 + 16 * j;
+      f32x4 v = acc[i][j];
+      if (bias) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (n + r < cols) v[r] += (float)bias[n + r];
+      }
+      if (n < cols) store4(to + n, v, cols - n);
+    }
+  }
+}
+
+// y: rows of x times the leaf's rows of w, both with k = input along memory.
+template <class S>
+__global__ void __launch_bounds__(S::NT) leaf_product_kernel(const LeafArgs<typename S::T> g) {
+  typedef typename S::T T;
+  __shared__ __align__(16) char lds[S::kLdsBytes];
+  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
+  const int tile = (int)(t / g.col_tiles), col0 = (int)(t % g.col_tiles) * S::BN;
+  const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, S::BM, tile);
+  if (leaf < 0) return;
+  const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
+  const int p0 = begin + (tile - (begin / S::BM + leaf)) * S::BM;
+  if (p0 >= end || p0 < begin) return;
+  const ListRows<T> rows_a = {g.x, g.ld_x, g.row_idx, end, g.n_rows};
+  const PlainRows<T> rows_b = {g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out};
+  RowOperand<T, S::BM, S::NT, S::DIRECT> a;
+  RowOperand<T, S::BN, S::NT, S::DIRECT> b;
+  a.init(rows_a, p0, 0, 0, g.d_in);
+  b.init(rows_b, col0, 0, 0, g.d_in);
+  f32x4 acc[S::TM][S::TN];
+  tile_product<S, true>(lds, a, b, rows_a, rows_b, 0, g.d_in, acc, Nothing{});
+  scatter_rows<S>(acc, g.bias ? g.bias + (int64_t)leaf * g.d_out : nullptr, g.y, g.ld_y, g.row_idx, p0,
+                  end < p0 + S::BM ? end : p0 + S::BM, g.n_rows, col0, g.d_out);
+}
+
+// dx: rows of dy (k = output along memory) times w, whose rows are k.
+template <class S>
+__global__ void __launch_bounds__(S::NT) leaf_grad_input_kernel(const LeafArgs<typename S::T> g) {
+  typedef typename S::T T;
+  __shared__ __align__(16) char lds[S::kLdsBytes];
+  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
+  const int tile = (int)(t / g.col_tiles), col0 = (int)(t % g.col_tiles) * S::BN;
+  const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, S::BM, tile);
+  if (leaf < 0) return;
+  const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
+  const int p0 = begin + (tile - (begin / S::BM + leaf)) * S::BM;
+  if (p0 >= end || p0 < begin) return;
+  const ListRows<T> rows_a = {g.dy, g.ld_dy, g.row_idx, end, g.n_rows};
+  const PlainRows<T> rows_b = {g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out};
+  RowOperand<T, S::BM, S::NT, S::DIRECT> a;
+  ColumnOperand<T, S::BN, S::NT, S::DIRECT> b;
+  a.init(rows_a, p0, 0, 0, g.d_out);
+  b.init(rows_b, col0, g.d_in, 0, g.d_out);
+  f32x4 acc[S::TM][S::TN];
+  tile_product<S, true>(lds, a, b, rows_a, rows_b, 0, g.d_out, acc, Nothing{});
+  scatter_rows<S>(acc, (const T*)nullptr, g.dx, g.ld_dx, g.row_idx, p0, end < p0 + S::BM ? end : p0 + S::BM, g.n_rows, col0, g.d_in);
+}
+
+// Sums over k of operand a's rows, by a product with ones: every n of the block holds the sum for its m.
+template <class S>
+struct RowSums {
+  f32x4 (&sum)[S::TM];
+  bool on;
+  template <class FA, class FB>
+  __device__ __forceinline__ void operator()(const FA& fa, const FB&) const {
+    if (!on) return;
+    typename Traits<typename S::T>::Frag ones;
+#pragma unroll
+    for (int i = 0; i < kChunk<typename S::T>; ++i) ones[i] = (typename S::T)1.0f;
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) sum[i] = mma(ones, fa[i], sum[i]);
+  }
+};
+
+// dW_l and db_l: both operands' rows are k = the leaf's positions.  The position axis is cut at multiples of g.cut, so that
+// one long leaf is the work of many workgroups: a piece is what a leaf has between two cuts, and leaf l owns the pieces from
+// offsets[l] / cut + l on (as above).  A leaf of one piece writes its result; the pieces of others leave f32 sums in slots: of
+// the pieces between two cuts only the first can have begun before (slot 2 b) and only the last can end behind (2 b + 1).
+// leaf_grad_join_kernel adds a leaf's slots in order, so the sums do not depend on which workgroup ran first.
+template <class S>
+__global__ void __launch_bounds__(S::NT) leaf_grad_weight_kernel(const LeafArgs<typename S::T> g) {
+  typedef typename S::T T;
+  __shared__ __align__(16) char lds[S::kLdsBytes];
+  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
+  const uint32_t tiles = g.col_tiles * g.row_tiles;
+  const int piece = (int)(t / tiles), r = (int)(t % tiles);
+  const int row0 = r / (int)g.col_tiles * S::BM, col0 = r % (int)g.col_tiles * S::BN;
+  const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, g.cut, piece);
+  if (leaf < 0) return;
+  const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
+  const int64_t block = piece - leaf;
+  const int64_t b0 = block * g.cut, b1 = b0 + g.cut;
+  const int p0 = begin > b0 ? begin : (int)(b0 < end ? b0 : end), p1 = end < b1 ? end : (int)b1;
+  if (p0 >= p1 && (end > begin || block != begin / g.cut)) return;  // only an empty leaf's one piece is empty: zeros
+  const ListRows<T> rows_a = {g.dy, g.ld_dy, g.row_idx, p1, g.n_rows};
+  const ListRows<T> rows_b = {g.x, g.ld_x, g.row_idx, p1, g.n_rows};
+  ColumnOperand<T, S::BM, S::NT, S::DIRECT> a;
+  ColumnOperand<T, S::BN, S::NT, S::DIRECT> b;
+  a.init(rows_a, row0, g.d_out, p0, p1);
+  b.init(rows_b, col0, g.d_in, p0, p1);
+  f32x4 acc[S::TM][S::TN];
+  f32x4 sum[S::TM];
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) sum[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+  const bool sums = g.dbias != nullptr && col0 == 0 && w % S::WN == 0;
+  tile_product<S, true>(lds, a, b, rows_a, rows_b, p0, p1, acc, RowSums<S>{sum, sums});
+
+  const bool whole = begin >= b0 && end <= b1;
+  const int64_t slot = 2 * block + (begin < b0 ? 0 : 1);
+  float* part = g.partial + slot * ((int64_t)(g.d_in + 1) * g.d_out);
+  const int m0 = row0 + (w / S::WN) * (S::TM * 16), n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int o = m0 + 16 * i + (l & 15);
+    if (o >= g.d_out) continue;
+    if (g.dw) {
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) {
+        const int n = n0 + 16 * j;
+        if (n >= g.d_in) continue;
+        if (whole) {
+          store4(g.dw + ((int64_t)leaf * g.d_out + o) * g.d_in + n, acc[i][j], g.d_in - n);
+        } else {
+          store4(part + (int64_t)o * g.d_in + n, acc[i][j], g.d_in - n);
+        }
+      }
+    }
+    if (sums && l < 16) {
+      if (whole) {
+        g.dbias[(int64_t)leaf * g.d_out + o] = (T)sum[i][0];
+      } else {
+        part[(int64_t)g.d_out * g.d_in + o] = sum[i][0];
+      }
+    }
+  }
+}
+
+// One row of workgroups for each cut but the first position: the cut's leaf, if it crosses a cut here for the first time.
+template <typename T>
+__global__ void __launch_bounds__(256) leaf_grad_join_kernel(const LeafArgs<T> g) {
+  const int64_t block = (int64_t)blockIdx.y + 1;
+  const int64_t at = block * g.cut;
+  // the leaf that holds position at - 1 and position at
+  int lo = 0, hi = g.n_leaves;  // the largest leaf whose offset is < at
+  while (hi - lo > 1) {
+    const int mid = lo + (hi - lo) / 2;
+    if (offset_at(g.offsets, mid, g.n_positions) < at) {
+      lo = mid;
+    } else {
+      hi = mid;
+    }
+  }
+  const int begin = offset_at(g.offsets, lo, g.n_positions), end = offset_at(g.offsets, lo + 1, g.n_positions);
+  if (begin >= at || end <= at || begin < at - g.cut) return;
+  const int64_t last = ((int64_t)end - 1) / g.cut;
+  const int64_t per = (int64_t)(g.d_in + 1) * g.d_out, n_w = (int64_t)g.d_in * g.d_out;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < per; e += (int64_t)gridDim.x * 256) {
+    if (e < n_w ? g.dw == nullptr : g.dbias == nullptr) continue;
+    float s = g.partial[(2 * (block - 1) + 1) * per + e];
+    for (int64_t b = block; b <= last; ++b) s += g.partial[2 * b * per + e];
+    if (e < n_w) {
+      g.dw[lo * n_w + e] = (T)s;
+    } else {
+      g.dbias[(int64_t)lo * g.d_out + (e - n_w)] = (T)s;
+    }
+  }
+}
+
+}  // namespace gbdt_leaf

@@ -1,0 +1,567 @@
+// Linear leaves and the softmax over many classes: host side of gbdt_leaf_product, gbdt_leaf_product_grad,
+// gbdt_softmax_loss, gbdt_softmax_grad and gbdt_softmax_stats (checks, choice of tile, scratch, launches).  The kernels are
+// in leaf_product_kernels.h and softmax_kernels.h, the tile that all of them share in tile_product.h.
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+#include <stdio.h>
+
+#include <algorithm>
+
+#include "../../include/gbdt_hist.h"
+#include "library_state.h"
+
+#include "leaf_product_kernels.h"
+#include "softmax_kernels.h"
+
+namespace {
+
+using gbdt_internal::hip_failed;
+using gbdt_tile::bf16;
+using gbdt_tile::kChunk;
+using gbdt_tile::kStep;
+using gbdt_tile::Shape;
+
+#define LAUNCHED(what)                                    \
+  do {                                                    \
+    hipError_t e_ = hipGetLastError();                    \
+    if (e_ != hipSuccess) return hip_failed(e_, what);    \
+  } while (0)
+
+constexpr int64_t kMaxRows = (int64_t)1 << 30;     // rows, positions, classes
+constexpr int64_t kMaxWidth = (int64_t)1 << 24;    // d_in, d_out, dim, leaves
+constexpr int64_t kMaxBlocks = ((int64_t)1 << 31) - 1;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+size_t pad256(size_t b) { return (b + 255) / 256 * 256; }
+
+// Rows of whole 16-byte chunks: every row 16-byte aligned and `cols` whole chunks.
+template <typename T>
+bool whole_chunks(const void* p, int64_t ld, int64_t cols) {
+  return ((uintptr_t)p & 15) == 0 && ld % kChunk<T> == 0 && cols % kChunk<T> == 0;
+}
+
+// ---------------------------------------------------------------- leaves
+
+int leaf_check(int64_t n_positions, int32_t n_leaves, int64_t n_rows, int32_t d_in, int32_t d_out, const void* row_idx,
+               const void* offsets, int32_t dtype) {
+  if (n_positions < 0 || n_leaves <= 0 || n_rows < 0 || d_in <= 0 || d_out <= 0 || !offsets) return GBDT_EINVAL;
+  if (((uintptr_t)offsets & 7) != 0 || ((uintptr_t)row_idx & 3) != 0) return GBDT_EINVAL;
+  if (dtype != GBDT_F32 && dtype != GBDT_BF16) return GBDT_EINVAL;
+  if (!row_idx && n_positions > n_rows) return GBDT_EINVAL;
+  if (n_positions >= kMaxRows || n_rows >= kMaxRows || n_leaves >= kMaxWidth || d_in >= kMaxWidth || d_out >= kMaxWidth)
+    return GBDT_EUNSUPPORTED;
+  return GBDT_OK;
+}
+
+// A pointer that no element can lie at.
+bool off_element(const void* p, int32_t dtype) { return ((uintptr_t)p & (dtype == GBDT_F32 ? 3 : 1)) != 0; }
+
+template <class S, typename T>
+int launch_leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
+  g.col_tiles = (uint32_t)ceil_div(g.d_out, S::BN);
+  const int64_t blocks = ((int64_t)g.n_positions / S::BM + g.n_leaves) * g.col_tiles;
+  if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
+  gbdt_leaf::leaf_product_kernel<S><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+  LAUNCHED("leaf_product_kernel");
+  return GBDT_OK;
+}
+
+template <typename T>
+int leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
+  const bool direct = whole_chunks<T>(g.x, g.ld_x, g.d_in) && whole_chunks<T>(g.w, g.d_in, g.d_in);
+  if (g.d_out <= 16)
+    return direct ? launch_leaf_product<Shape<T, 128, 16, 4, 1, true>>(g, s) : launch_leaf_product<Shape<T, 128, 16, 4, 1, false>>(g, s);
+  return direct ? launch_leaf_product<Shape<T, 128, 128, 2, 2, true>>(g, s) : launch_leaf_product<Shape<T, 128, 128, 2, 2, false>>(g, s);
+}
+
+template <class S, typename T>
+int launch_leaf_grad_input(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
+  g.col_tiles = (uint32_t)ceil_div(g.d_in, S::BN);
+  const int64_t blocks = ((int64_t)g.n_positions / S::BM + g.n_leaves) * g.col_tiles;
+  if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
+  gbdt_leaf::leaf_grad_input_kernel<S><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+  LAUNCHED("leaf_grad_input_kernel");
+  return GBDT_OK;
+}
+
+constexpr int kGradBM = 128, kGradBN = 128;  // the weights' gradient: outputs x inputs a tile
+
+// Positions between cuts: twice as many whole pieces of work as compute units, from 512 positions on.  Then the sums that
+// pieces leave behind are at most 2 x 2 x units tiles of f32 (64 MiB on 256 units) whatever the sizes are.
+int64_t leaf_cut(int64_t n_positions, int64_t tiles, int64_t units) {
+  return std::max<int64_t>(512, round_up(ceil_div(n_positions * tiles, 2 * units), 64));
+}
+int64_t leaf_tiles(int64_t d_in, int64_t d_out) { return ceil_div(d_out, kGradBM) * ceil_div(d_in, kGradBN); }
+size_t leaf_partial_bytes(int64_t n_positions, int64_t d_in, int64_t d_out, int64_t units) {
+  const int64_t blocks = ceil_div(n_positions, leaf_cut(n_positions, leaf_tiles(d_in, d_out), units));
+  return blocks < 2 ? 0 : pad256((size_t)(2 * blocks * (d_in + 1) * d_out) * sizeof(float));
+}
+
+template <class S, typename T>
+int launch_leaf_grad_weight(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
+  static_assert(S::BM == kGradBM && S::BN == kGradBN, "leaf_tiles counts these");
+  g.col_tiles = (uint32_t)(g.dw ? ceil_div(g.d_in, S::BN) : 1);
+  g.row_tiles = (uint32_t)ceil_div(g.d_out, S::BM);
+  const int64_t blocks = ((int64_t)g.n_positions / g.cut + g.n_leaves) * g.col_tiles * g.row_tiles;
+  if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
+  gbdt_leaf::leaf_grad_weight_kernel<S><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+  LAUNCHED("leaf_grad_weight_kernel");
+  return GBDT_OK;
+}
+
+template <typename T>
+int leaf_product_grad(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
+  if (g.dx && g.n_positions > 0) {
+    const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.w, g.d_in, g.d_in);
+    const int rc = direct ? launch_leaf_grad_input<Shape<T, 128, 128, 2, 2, true>>(g, s)
+                          : launch_leaf_grad_input<Shape<T, 128, 128, 2, 2, false>>(g, s);
+    if (rc != GBDT_OK) return rc;
+  }
+  if (!g.dw && !g.dbias) return GBDT_OK;
+  const int64_t units = gbdt_internal::cu_count();
+  g.cut = (int32_t)leaf_cut(g.n_positions, leaf_tiles(g.d_in, g.d_out), units);
+  const size_t bytes = leaf_partial_bytes(g.n_positions, g.d_in, g.d_out, units);
+  if (bytes) {
+    void* ws = nullptr;
+    const int rc = gbdt_internal::workspace(bytes, s, &ws);
+    if (rc != GBDT_OK) return rc;
+    g.partial = (float*)ws;
+  }
+  const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.x, g.ld_x, g.d_in);
+  const int rc = direct ? launch_leaf_grad_weight<Shape<T, 128, 128, 2, 2, true>>(g, s)
+                        : launch_leaf_grad_weight<Shape<T, 128, 128, 2, 2, false>>(g, s);
+  if (rc != GBDT_OK) return rc;
+  const int64_t cuts = ceil_div(g.n_positions, g.cut) - 1;
+  if (cuts > 0) {
+    const int64_t per = ceil_div((int64_t)(g.d_in + 1) * g.d_out, 256);
+    gbdt_leaf::leaf_grad_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(per, 2048), (unsigned)cuts), dim3(256), 0, s>>>(g);
+    LAUNCHED("leaf_grad_join_kernel");
+  }
+  return GBDT_OK;
+}
+
+// ---------------------------------------------------------------- softmax
+
+constexpr int kScoreBM = 128, kScoreBN = 128;
+constexpr int64_t kPieceAlign = 256;                    // classes: whole tiles of every shape
+constexpr int64_t kPieceBytes = (int64_t)256 << 20;     // G of a piece, as long as it is kPieceAlign classes wide at least
+constexpr int64_t kPartsBytes = (int64_t)256 << 20;     // maxima and sums of a launch's tiles
+
+int softmax_check(const void* h, int64_t ld_h, const void* c, int64_t ld_c, int64_t n_rows, int64_t n_classes, int32_t dim,
+                  int32_t dtype) {
+  if (n_rows < 0 || n_classes <= 0 || dim <= 0 || !c || (!h && n_rows > 0) || ld_h < dim || ld_c < dim) return GBDT_EINVAL;
+  if (dtype != GBDT_F32 && dtype != GBDT_BF16) return GBDT_EINVAL;
+  if (off_element(h, dtype) || off_element(c, dtype)) return GBDT_EINVAL;
+  if (n_rows >= kMaxRows || n_classes >= kMaxRows || dim >= kMaxWidth) return GBDT_EUNSUPPORTED;
+  return GBDT_OK;
+}
+
+// Row tiles that go through the classes together: 2 MiB of rows, half of an XCD's L2.
+uint32_t group_of(int64_t tile_rows, int64_t dim, int64_t bytes) {
+  return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(64, ((int64_t)2 << 20) / (tile_rows * dim * bytes)));
+}
+
+template <class S, typename T>
+int score_grid(gbdt_softmax::ScoreArgs<T>& g, unsigned* blocks) {
+  g.row_tiles = (uint32_t)ceil_div(g.n_rows, S::BM);
+  g.col_tiles = (uint32_t)ceil_div(g.end - g.begin, S::BN);
+  g.group = group_of(S::BM, g.dim, sizeof(T));
+  const int64_t n = (int64_t)g.row_tiles * g.col_tiles;
+  if (n > kMaxBlocks || (int64_t)g.group * g.col_tiles > kMaxBlocks) return GBDT_EUNSUPPORTED;
+  *blocks = (unsigned)n;
+  return GBDT_OK;
+}
+
+struct LossPlan {
+  int64_t rows;  // of a launch
+  int64_t tiles;
+  size_t parts_bytes, bytes;
+};
+LossPlan loss_plan(int64_t n_rows, int64_t n_classes) {
+  LossPlan p;
+  p.tiles = ceil_div(n_classes, kScoreBN);
+  p.rows = std::min(n_rows, std::max<int64_t>(4096, kPartsBytes / (8 * p.tiles) / 4096 * 4096));
+  p.parts_bytes = pad256((size_t)(p.rows * p.tiles) * 8);
+  p.bytes = p.parts_bytes + pad256((size_t)p.rows * 4);
+  return p;
+}
+
+template <class S, typename T>
+int launch_scores(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
+  static_assert(S::BN == kScoreBN, "loss_plan counts these");
+  unsigned blocks = 0;
+  const int rc = score_grid<S>(g, &blocks);
+  if (rc != GBDT_OK) return rc;
+  gbdt_softmax::softmax_scores_kernel<S><<<dim3(blocks), dim3(S::NT), 0, s>>>(g);
+  LAUNCHED("softmax_scores_kernel");
+  return GBDT_OK;
+}
+
+template <typename T>
+int softmax_loss(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32_t* labels, int64_t n_rows, int64_t n_classes,
+                 int32_t dim, float* loss, float* lse, hipStream_t s) {
+  const LossPlan plan = loss_plan(n_rows, n_classes);
+  void* ws = nullptr;
+  int rc = gbdt_internal::workspace(plan.bytes, s, &ws);
+  if (rc != GBDT_OK) return rc;
+  const bool direct = whole_chunks<T>(h, ld_h, dim) && whole_chunks<T>(c, ld_c, dim);
+  for (int64_t r = 0; r < n_rows; r += plan.rows) {
+    gbdt_softmax::ScoreArgs<T> g = {};
+    g.h = h + r * ld_h;
+    g.c = c;
+    g.labels = labels ? labels + r : nullptr;
+    g.parts = (gbdt_softmax::MaxSum*)ws;
+    g.picked = (float*)((char*)ws + plan.parts_bytes);
+    g.ld_h = ld_h;
+    g.ld_c = ld_c;
+    g.n_rows = (int32_t)std::min(plan.rows, n_rows - r);
+    g.n_classes = g.end = (int32_t)n_classes;
+    g.dim = dim;
+    rc = direct ? launch_scores<Shape<T, kScoreBM, kScoreBN, 2, 2, true>>(g, s)
+                : launch_scores<Shape<T, kScoreBM, kScoreBN, 2, 2, false>>(g, s);
+    if (rc != GBDT_OK) return rc;
+    gbdt_softmax::softmax_join_kernel<<<dim3((unsigned)ceil_div(g.n_rows, 16)), dim3(256), 0, s>>>(
+        g.parts, g.picked, g.labels, g.n_rows, g.n_classes, (int32_t)plan.tiles, loss ? loss + r : nullptr, lse + r);
+    LAUNCHED("softmax_join_kernel");
+  }
+  return GBDT_OK;
+}
+
+struct GradPlan {
+  int64_t width;   // classes a piece
+  int64_t pieces;
+  int64_t dh_splits, dh_split, dc_splits, dc_split;
+  size_t g_bytes, dh_bytes, dc_bytes;
+};
+// Splits of a summed axis of `k`: as many as fill the compute units, each 8 steps long at least.
+void split_axis(int64_t tiles, int64_t k, int64_t step, int64_t units, int64_t* splits, int64_t* len) {
+  const int64_t want = std::max<int64_t>(1, std::min(units / std::max<int64_t>(tiles, 1), ceil_div(k, 8 * step)));
+  *len = std::max(step, round_up(ceil_div(k, want), step));
+  *splits = std::max<int64_t>(1, ceil_div(k, *len));
+}
+GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, int64_t units) {
+  GradPlan p;
+  const int64_t rows = std::max<int64_t>(n_rows, 1);
+  const int64_t all = round_up(n_classes, kPieceAlign);
+  p.width = std::min(all, std::max(kPieceAlign, kPieceBytes / (rows * e) / kPieceAlign * kPieceAlign));
+  p.pieces = ceil_div(n_classes, p.width);
+  p.width = round_up(ceil_div(n_classes, p.pieces), kPieceAlign);
+  p.pieces = ceil_div(n_classes, p.width);
+  const int64_t step = gbdt_tile::kStepBytes / e;
+  const int64_t cols = ceil_div(dim, 128);
+  split_axis(ceil_div(rows, 128) * cols, p.width, step, units, &p.dh_splits, &p.dh_split);
+  split_axis(ceil_div(p.width, 128) * cols, n_rows, step, units, &p.dc_splits, &p.dc_split);
+  p.g_bytes = pad256((size_t)(rows * p.width * e));
+  p.dh_bytes = p.dh_splits > 1 || p.pieces > 1 ? pad256((size_t)(p.dh_splits * rows * dim) * 4) : 0;
+  p.dc_bytes = p.dc_splits > 1 ? pad256((size_t)(p.dc_splits * p.width * dim) * 4) : 0;
+  return p;
+}
+
+template <class S, typename T>
+int launch_piece(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
+  static_assert(kPieceAlign % S::BN == 0, "G's rows hold whole tiles");
+  unsigned blocks = 0;
+  const int rc = score_grid<S>(g, &blocks);
+  if (rc != GBDT_OK || blocks == 0) return rc;
+  gbdt_softmax::softmax_piece_kernel<S><<<dim3(blocks), dim3(S::NT), 0, s>>>(g);
+  LAUNCHED("softmax_piece_kernel");
+  return GBDT_OK;
+}
+
+template <class S, bool TO_ROWS, typename T>
+int launch_product(gbdt_softmax::PieceArgs<T>& g, hipStream_t s) {
+  g.row_tiles = (uint32_t)ceil_div(g.rows, S::BM);
+  g.col_tiles = (uint32_t)ceil_div(g.cols, S::BN);
+  g.group = 8;
+  const int64_t blocks = (int64_t)g.row_tiles * g.col_tiles * g.splits;
+  if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
+  if (blocks == 0) return GBDT_OK;
+  gbdt_softmax::piece_product_kernel<S, TO_ROWS><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+  LAUNCHED("piece_product_kernel");
+  return GBDT_OK;
+}
+
+template <typename T>
+int join_product(const gbdt_softmax::PieceArgs<T>& g, hipStream_t s) {
+  const int64_t n = ceil_div((int64_t)g.rows * g.cols, 256);
+  if (n == 0) return GBDT_OK;
+  gbdt_softmax::piece_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(n, 16384)), dim3(256), 0, s>>>(g);
+  LAUNCHED("piece_join_kernel");
+  return GBDT_OK;
+}
+
+template <typename T>
+int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32_t* labels, const float* lse, const float* weight,
+                 float scale, int64_t n_rows, int64_t n_classes, int32_t dim, T* dh, int64_t ld_dh, T* dc, int64_t ld_dc,
+                 hipStream_t s) {
+  const GradPlan plan = grad_plan(n_rows, n_classes, dim, sizeof(T), gbdt_internal::cu_count());
+  void* ws = nullptr;
+  int rc = gbdt_internal::workspace(plan.g_bytes + plan.dh_bytes + plan.dc_bytes, s, &ws);
+  if (rc != GBDT_OK) return rc;
+  T* piece = (T*)ws;
+  float* dh_sums = plan.dh_bytes ? (float*)((char*)ws + plan.g_bytes) : nullptr;
+  float* dc_sums = plan.dc_bytes ? (float*)((char*)ws + plan.g_bytes + plan.dh_bytes) : nullptr;
+  const bool direct = whole_chunks<T>(h, ld_h, dim) && whole_chunks<T>(c, ld_c, dim);
+  gbdt_softmax::PieceArgs<T> to_h = {}, to_c = {};
+  for (int64_t begin = 0; begin < n_classes; begin += plan.width) {
+    const int64_t end = std::min(n_classes, begin + plan.width);
+    gbdt_softmax::ScoreArgs<T> g = {};
+    g.h = h;
+    g.c = c;
+    g.labels = labels;
+    g.lse = lse;
+    g.weight = weight;
+    g.g = piece;
+    g.ld_h = ld_h;
+    g.ld_c = ld_c;
+    g.ld_g = plan.width;
+    g.n_rows = (int32_t)n_rows;
+    g.n_classes = (int32_t)n_classes;
+    g.dim = dim;
+    g.begin = (int32_t)begin;
+    g.end = (int32_t)end;
+    rc = direct ? launch_piece<Shape<T, 128, 128, 2, 2, true>>(g, s) : launch_piece<Shape<T, 128, 128, 2, 2, false>>(g, s);
+    if (rc != GBDT_OK) return rc;
+    if (dc) {
+      to_c.a = piece;
+      to_c.b = h;
+      to_c.out = dc + begin * ld_dc;
+      to_c.sums = dc_sums;
+      to_c.labels = labels;
+      to_c.ld_a = plan.width;
+      to_c.ld_b = ld_h;
+      to_c.ld_out = ld_dc;
+      to_c.scale = scale;
+      to_c.rows = (int32_t)(end - begin);
+      to_c.cols = dim;
+      to_c.k = to_c.b_rows = (int32_t)n_rows;
+      to_c.n_classes = (int32_t)n_classes;
+      to_c.k_split = (int32_t)plan.dc_split;
+      to_c.splits = (uint32_t)plan.dc_splits;
+      rc = direct ? launch_product<Shape<T, 128, 128, 2, 2, true>, false>(to_c, s)
+                  : launch_product<Shape<T, 128, 128, 2, 2, false>, false>(to_c, s);
+      if (rc != GBDT_OK) return rc;
+      if (dc_sums) {
+        gbdt_softmax::PieceArgs<T> j = to_c;
+        j.labels = nullptr;  // a class always has its gradient
+        if ((rc = join_product(j, s)) != GBDT_OK) return rc;
+      }
+    }
+    if (dh && n_rows > 0) {
+      to_h.a = piece;
+      to_h.b = c + begin * ld_c;
+      to_h.out = dh;
+      to_h.sums = dh_sums;
+      to_h.labels = labels;
+      to_h.ld_a = plan.width;
+      to_h.ld_b = ld_c;
+      to_h.ld_out = ld_dh;
+      to_h.scale = scale;
+      to_h.rows = (int32_t)n_rows;
+      to_h.cols = dim;
+      to_h.k = (int32_t)round_up(end - begin, kChunk<T>);
+      to_h.b_rows = (int32_t)(end - begin);
+      to_h.n_classes = (int32_t)n_classes;
+      to_h.k_split = (int32_t)plan.dh_split;
+      to_h.splits = (uint32_t)plan.dh_splits;
+      to_h.add = begin > 0;
+      rc = direct ? launch_product<Shape<T, 128, 128, 2, 2, true>, true>(to_h, s)
+                  : launch_product<Shape<T, 128, 128, 2, 2, false>, true>(to_h, s);
+      if (rc != GBDT_OK) return rc;
+    }
+  }
+  if (dh && n_rows > 0 && dh_sums) return join_product(to_h, s);
+  return GBDT_OK;
+}
+
+template <class S, typename T>
+int launch_stats(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
+  unsigned blocks = 0;
+  const int rc = score_grid<S>(g, &blocks);
+  if (rc != GBDT_OK || blocks == 0) return rc;
+  gbdt_softmax::softmax_stats_kernel<S><<<dim3(blocks), dim3(S::NT), 0, s>>>(g);
+  LAUNCHED("softmax_stats_kernel");
+  return GBDT_OK;
+}
+
+template <typename T>
+int softmax_stats(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
+  const bool direct = whole_chunks<T>(g.h, g.ld_h, g.dim) && whole_chunks<T>(g.c, g.ld_c, g.dim);
+  if (g.end - g.begin <= 16)
+    return direct ? launch_stats<Shape<T, 128, 16, 4, 1, true>>(g, s) : launch_stats<Shape<T, 128, 16, 4, 1, false>>(g, s);
+  return direct ? launch_stats<Shape<T, 128, 128, 2, 2, true>>(g, s) : launch_stats<Shape<T, 128, 128, 2, 2, false>>(g, s);
+}
+
+template <typename T>
+int leaf_product_call(const void* x, int64_t ld_x, const void* weight, const void* bias, const int32_t* row_idx,
+                      const int64_t* leaf_offsets, int64_t n_positions, int32_t n_leaves, int64_t n_rows, int32_t d_in, int32_t d_out,
+                      void* y_out, int64_t ld_y, hipStream_t s) {
+  gbdt_leaf::LeafArgs<T> g = {};
+  g.x = (const T*)x;
+  g.w = (const T*)weight;
+  g.bias = (const T*)bias;
+  g.y = (T*)y_out;
+  g.row_idx = row_idx;
+  g.offsets = leaf_offsets;
+  g.ld_x = ld_x;
+  g.ld_y = ld_y;
+  g.n_positions = (int32_t)n_positions;
+  g.n_leaves = n_leaves;
+  g.n_rows = (int32_t)n_rows;
+  g.d_in = d_in;
+  g.d_out = d_out;
+  return leaf_product(g, s);
+}
+
+template <typename T>
+int leaf_product_grad_call(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* weight, const int32_t* row_idx,
+                           const int64_t* leaf_offsets, int64_t n_positions, int32_t n_leaves, int64_t n_rows, int32_t d_in,
+                           int32_t d_out, void* dx_out, int64_t ld_dx, void* dweight_out, void* dbias_out, hipStream_t s) {
+  gbdt_leaf::LeafArgs<T> g = {};
+  g.x = (const T*)x;
+  g.dy = (const T*)dy;
+  g.w = (const T*)weight;
+  g.dx = (T*)dx_out;
+  g.dw = (T*)dweight_out;
+  g.dbias = (T*)dbias_out;
+  g.row_idx = row_idx;
+  g.offsets = leaf_offsets;
+  g.ld_x = ld_x;
+  g.ld_dy = ld_dy;
+  g.ld_dx = ld_dx;
+  g.n_positions = (int32_t)n_positions;
+  g.n_leaves = n_leaves;
+  g.n_rows = (int32_t)n_rows;
+  g.d_in = d_in;
+  g.d_out = d_out;
+  return leaf_product_grad(g, s);
+}
+
+template <typename T>
+int softmax_stats_call(const void* h, int64_t ld_h, const void* c, int64_t ld_c, const int32_t* labels, const float* lse,
+                       int64_t n_rows, int64_t n_classes, int32_t dim, int64_t class_begin, int64_t class_end, float* grad_out,
+                       float* hess_out, int64_t ld_out, hipStream_t s) {
+  gbdt_softmax::ScoreArgs<T> g = {};
+  g.h = (const T*)h;
+  g.c = (const T*)c;
+  g.labels = labels;
+  g.lse = lse;
+  g.grad = grad_out;
+  g.hess = hess_out;
+  g.ld_h = ld_h;
+  g.ld_c = ld_c;
+  g.ld_out = ld_out;
+  g.n_rows = (int32_t)n_rows;
+  g.n_classes = (int32_t)n_classes;
+  g.dim = dim;
+  g.begin = (int32_t)class_begin;
+  g.end = (int32_t)class_end;
+  return softmax_stats(g, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const void* bias, const int32_t* row_idx,
+                      const int64_t* leaf_offsets, int64_t n_positions, int32_t n_leaves, int64_t n_rows, int32_t d_in,
+                      int32_t d_out, int32_t dtype, void* y_out, int64_t ld_y, void* stream) {
+  int rc = leaf_check(n_positions, n_leaves, n_rows, d_in, d_out, row_idx, leaf_offsets, dtype);
+  if (rc != GBDT_OK) return rc;
+  if (ld_x < d_in || ld_y < d_out || !weight || off_element(x, dtype) || off_element(weight, dtype) || off_element(bias, dtype) ||
+      off_element(y_out, dtype))
+    return GBDT_EINVAL;
+  if (n_positions == 0 || n_rows == 0) return GBDT_OK;
+  if (!x || !y_out) return GBDT_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  rc = gbdt_internal::row_ids_checked(row_idx, n_positions, n_rows, s);
+  if (rc != GBDT_OK) return rc;
+  return dtype == GBDT_F32 ? leaf_product_call<float>(x, ld_x, weight, bias, row_idx, leaf_offsets, n_positions, n_leaves, n_rows,
+                                                      d_in, d_out, y_out, ld_y, s)
+                           : leaf_product_call<bf16>(x, ld_x, weight, bias, row_idx, leaf_offsets, n_positions, n_leaves, n_rows,
+                                                     d_in, d_out, y_out, ld_y, s);
+}
+
+size_t gbdt_leaf_product_grad_workspace_bytes(int64_t n_positions, int32_t d_in, int32_t d_out) {
+  if (n_positions < 0 || n_positions >= kMaxRows || d_in <= 0 || d_out <= 0 || d_in >= kMaxWidth || d_out >= kMaxWidth) return 0;
+  return gbdt_internal::workspace_head_bytes() + leaf_partial_bytes(n_positions, d_in, d_out, gbdt_internal::cu_count());
+}
+
+int gbdt_leaf_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* weight, const int32_t* row_idx,
+                           const int64_t* leaf_offsets, int64_t n_positions, int32_t n_leaves, int64_t n_rows, int32_t d_in,
+                           int32_t d_out, int32_t dtype, void* dx_out, int64_t ld_dx, void* dweight_out, void* dbias_out,
+                           void* stream) {
+  int rc = leaf_check(n_positions, n_leaves, n_rows, d_in, d_out, row_idx, leaf_offsets, dtype);
+  if (rc != GBDT_OK) return rc;
+  if (ld_dy < d_out || (dweight_out && ld_x < d_in) || (dx_out && (ld_dx < d_in || !weight))) return GBDT_EINVAL;
+  if (off_element(dy, dtype) || off_element(x, dtype) || off_element(weight, dtype) || off_element(dx_out, dtype) ||
+      off_element(dweight_out, dtype) || off_element(dbias_out, dtype))
+    return GBDT_EINVAL;
+  if (n_rows == 0) n_positions = 0;
+  if (n_positions > 0 && (!dy || (dweight_out && !x))) return GBDT_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  rc = gbdt_internal::row_ids_checked(row_idx, n_positions, n_rows, s);
+  if (rc != GBDT_OK) return rc;
+  return dtype == GBDT_F32 ? leaf_product_grad_call<float>(dy, ld_dy, x, ld_x, weight, row_idx, leaf_offsets, n_positions, n_leaves,
+                                                           n_rows, d_in, d_out, dx_out, ld_dx, dweight_out, dbias_out, s)
+                           : leaf_product_grad_call<bf16>(dy, ld_dy, x, ld_x, weight, row_idx, leaf_offsets, n_positions, n_leaves,
+                                                          n_rows, d_in, d_out, dx_out, ld_dx, dweight_out, dbias_out, s);
+}
+
+size_t gbdt_softmax_workspace_bytes(int64_t n_rows, int64_t n_classes, int32_t dim, int32_t dtype) {
+  if (n_rows < 0 || n_classes <= 0 || dim <= 0 || n_rows >= kMaxRows || n_classes >= kMaxRows || dim >= kMaxWidth ||
+      (dtype != GBDT_F32 && dtype != GBDT_BF16))
+    return 0;
+  const GradPlan p = grad_plan(n_rows, n_classes, dim, dtype == GBDT_F32 ? 4 : 2, gbdt_internal::cu_count());
+  const size_t grad = p.g_bytes + p.dh_bytes + p.dc_bytes, loss = loss_plan(n_rows, n_classes).bytes;
+  return gbdt_internal::workspace_head_bytes() + std::max(grad, loss);
+}
+
+int gbdt_softmax_loss(const void* h, int64_t ld_h, const void* classes, int64_t ld_c, const int32_t* labels, int64_t n_rows,
+                      int64_t n_classes, int32_t dim, int32_t dtype, float* loss_out, float* lse_out, void* stream) {
+  const int rc = softmax_check(h, ld_h, classes, ld_c, n_rows, n_classes, dim, dtype);
+  if (rc != GBDT_OK) return rc;
+  if ((labels == nullptr) != (loss_out == nullptr)) return GBDT_EINVAL;
+  if (n_rows == 0) return GBDT_OK;
+  if (!lse_out) return GBDT_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  return dtype == GBDT_F32 ? softmax_loss((const float*)h, ld_h, (const float*)classes, ld_c, labels, n_rows, n_classes, dim, loss_out,
+                                          lse_out, s)
+                           : softmax_loss((const bf16*)h, ld_h, (const bf16*)classes, ld_c, labels, n_rows, n_classes, dim, loss_out,
+                                          lse_out, s);
+}
+
+int gbdt_softmax_grad(const void* h, int64_t ld_h, const void* classes, int64_t ld_c, const int32_t* labels, const float* lse,
+                      const float* row_weight, float scale, int64_t n_rows, int64_t n_classes, int32_t dim, int32_t dtype, void* dh_out,
+                      int64_t ld_dh, void* dclasses_out, int64_t ld_dc, void* stream) {
+  const int rc = softmax_check(h, ld_h, classes, ld_c, n_rows, n_classes, dim, dtype);
+  if (rc != GBDT_OK) return rc;
+  if ((dh_out && ld_dh < dim) || (dclasses_out && ld_dc < dim) || off_element(dh_out, dtype) || off_element(dclasses_out, dtype))
+    return GBDT_EINVAL;
+  if (n_rows > 0 && (!labels || !lse)) return GBDT_EINVAL;
+  if (!dh_out && !dclasses_out) return GBDT_OK;
+  hipStream_t s = (hipStream_t)stream;
+  return dtype == GBDT_F32 ? softmax_grad((const float*)h, ld_h, (const float*)classes, ld_c, labels, lse, row_weight, scale, n_rows,
+                                          n_classes, dim, (float*)dh_out, ld_dh, (float*)dclasses_out, ld_dc, s)
+                           : softmax_grad((const bf16*)h, ld_h, (const bf16*)classes, ld_c, labels, lse, row_weight, scale, n_rows,
+                                          n_classes, dim, (bf16*)dh_out, ld_dh, (bf16*)dclasses_out, ld_dc, s);
+}
+
+int gbdt_softmax_stats(const void* h, int64_t ld_h, const void* classes, int64_t ld_c, const int32_t* labels, const float* lse,
+                       int64_t n_rows, int64_t n_classes, int32_t dim, int32_t dtype, int64_t class_begin, int64_t class_end,
+                       float* grad_out, float* hess_out, int64_t ld_out, void* stream) {
+  const int rc = softmax_check(h, ld_h, classes, ld_c, n_rows, n_classes, dim, dtype);
+  if (rc != GBDT_OK) return rc;
+  if (class_begin < 0 || class_end < class_begin || class_end > n_classes || ld_out < n_rows) return GBDT_EINVAL;
+  if (n_rows == 0 || class_begin == class_end) return GBDT_OK;
+  if (!lse || !grad_out || !hess_out) return GBDT_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  return dtype == GBDT_F32 ? softmax_stats_call<float>(h, ld_h, classes, ld_c, labels, lse, n_rows, n_classes, dim, class_begin,
+                                                       class_end, grad_out, hess_out, ld_out, s)
+                           : softmax_stats_call<bf16>(h, ld_h, classes, ld_c, labels, lse, n_rows, n_classes, dim, class_begin,
+                                                      class_end, grad_out, hess_out, ld_out, s);
+}
+
+}  // extern "C"

@@ -1,0 +1,335 @@
+// Softmax cross entropy over many classes, without the n_rows x n_classes scores ever being stored.
+//
+//   s_v = <h_d, c_v>      lse_d = log sum_v exp s_v      loss_d = lse_d - s_{y_d}
+//   G_dv = w_d (exp(s_v - lse_d) - [v = y_d])      dh = scale G C      dC = scale G^T H
+//
+// softmax_scores_kernel multiplies a tile of rows by a tile of classes and keeps, per row, the tile's maximum and the sum of
+// exponentials beneath it; softmax_join_kernel joins the tiles of a row, in order.  The gradient takes the classes in pieces:
+// softmax_piece_kernel recomputes a piece's scores and stores G of that piece alone, in the operands' type, from which two
+// products follow (piece_product_kernel): the piece's rows of dC, and the piece's share of dh, kept in f32 until the last.
+// Recomputing costs a quarter of the operations; storing the scores instead would cost n_rows x n_classes x 4 bytes out and
+// in, since a score rounded to 16 bits is off by up to 2^-8 of itself, and its exponential by as much as that times the score.
+// G lies in [-w, w]: rounded to bf16 each element is off by 2^-8 of itself at most, independently, as the results are.
+// scale (1 / n_rows, as a rule) multiplies f32 sums, so it takes no part in that rounding.
+//
+// A row whose label is outside [0, n_classes) is ignored: loss, lse, G, gradient and hessian are zeros whatever h holds there
+// (its row of H is read as zeros where it would meet a zero of G).
+#pragma once
+
+#include "leaf_product_kernels.h"
+
+namespace gbdt_softmax {
+
+using namespace gbdt_tile;
+using gbdt_leaf::PlainRows;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp_diff(float s, float base) { return __builtin_amdgcn_exp2f((s - base) * kLog2e); }
+// What a running maximum is subtracted as: exponentials beneath an infinite one are 0 or infinite, not inf - inf.
+__device__ __forceinline__ float base_of(float m) { return __builtin_isinf(m) ? 0.0f : m; }
+
+struct MaxSum {
+  float m, s;
+};
+__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
+  // a NaN in either sum or maximum stays in the sum
+  const float m = fmaxf(a.m, b.m), base = base_of(m);
+  return {m, a.s * exp_diff(a.m, base) + b.s * exp_diff(b.m, base)};
+}
+
+template <typename T>
+struct ScoreArgs {
+  const T* h;  // [n_rows][dim]
+  const T* c;  // [n_classes][dim]
+  const int32_t* labels;  // [n_rows] or null
+  const float* lse;       // [n_rows]
+  const float* weight;    // [n_rows] or null
+  MaxSum* parts;          // [col_tiles][n_rows]
+  float* picked;          // [n_rows]: the label's score
+  T* g;                   // [n_rows][ld_g]: G of the classes begin .. end, zeros behind
+  float* grad;            // [end - begin][ld_out]
+  float* hess;
+  int64_t ld_h, ld_c, ld_g, ld_out;
+  int32_t n_rows, n_classes, dim, begin, end;
+  uint32_t row_tiles, col_tiles, group;
+};
+
+// A tile's place: `group` row tiles side by side go through all column tiles before the next ones do, so that what runs at
+// the same time on an XCD shares both operands in its L2.
+template <typename Args>
+__device__ __forceinline__ void tile_place(const Args& g, uint32_t* row, uint32_t* col) {
+  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
+  const uint32_t span = g.group * g.col_tiles;
+  const uint32_t first = t / span * g.group;
+  const uint32_t rows = g.row_tiles - first < g.group ? g.row_tiles - first : g.group;
+  *row = first + t % span % rows;
+  *col = t % span / rows;
+}
+
+template <class S, bool N_INNER, typename T>
+__device__ __forceinline__ void scores_tile(char* lds, const ScoreArgs<T>& g, int row0, int col0, f32x4 (&acc)[S::TM][S::TN]) {
+  const PlainRows<T> rows_a = {g.h, g.ld_h, g.n_rows};
+  const PlainRows<T> rows_b = {g.c, g.ld_c, g.end};
+  RowOperand<T, S::BM, S::NT, S::DIRECT> a;
+  RowOperand<T, S::BN, S::NT, S::DIRECT> b;
+  a.init(rows_a, row0, 0, 0, g.dim);
+  b.init(rows_b, col0, 0, 0, g.dim);
+  tile_product<S, N_INNER>(lds, a, b, rows_a, rows_b, 0, g.dim, acc, Nothing{});
+}
+
+template <class S>
+__global__ void __launch_bounds__(S::NT) softmax_scores_kernel(const ScoreArgs<typename S::T> g) {
+  __shared__ __align__(16) char lds[S::kLdsBytes];
+  uint32_t tr, tc;
+  tile_place(g, &tr, &tc);
+  const int row0 = (int)tr * S::BM, col0 = (int)tc * S::BN;
+  f32x4 acc[S::TM][S::TN];
+  scores_tile<S, true>(lds, g, row0, col0, acc);
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int m0 = (w / S::WN) * (S::TM * 16), n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+  MaxSum* row_parts = (MaxSum*)lds;  // [WN][BM]
+  __syncthreads();                   // the stages have been read
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int m = m0 + 16 * i + (l & 15);
+    const int d = row0 + m;
+    const int y = g.labels && d < g.n_rows ? g.labels[d] : -1;
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int n = n0 + 16 * j + r;
+        if (n < g.end) {
+          top = fmaxf(top, acc[i][j][r]);
+          if (n == y) g.picked[d] = acc[i][j][r];
+        }
+      }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float base = base_of(top);
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (n0 + 16 * j + r < g.end) sum += exp_diff(acc[i][j][r], base);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (l < 16) row_parts[(w % S::WN) * S::BM + m] = {top, sum};
+  }
+  __syncthreads();
+  for (int m = threadIdx.x; m < S::BM; m += S::NT) {
+    if (row0 + m >= g.n_rows) break;
+    MaxSum p = row_parts[m];
+#pragma unroll
+    for (int k = 1; k < S::WN; ++k) p = join(p, row_parts[k * S::BM + m]);
+    g.parts[(int64_t)tc * g.n_rows + row0 + m] = p;
+  }
+}
+
+// Joins a row's tiles: 16 lanes a row, each every 16th tile in order, then pairwise.
+__global__ void __launch_bounds__(256) softmax_join_kernel(const MaxSum* parts, const float* picked, const int32_t* labels, int32_t n_rows,
+                                                           int32_t n_classes, int32_t tiles, float* loss, float* lse) {
+  const int d0 = blockIdx.x * 16;
+  const int i = threadIdx.x & 15, q = threadIdx.x >> 4;  // row of the block, turn
+  __shared__ MaxSum all[16][17];
+  const int d = d0 + i;
+  MaxSum p = {-__builtin_inff(), 0.0f};
+  if (d < n_rows)
+    for (int t = q; t < tiles; t += 16) p = join(p, parts[(int64_t)t * n_rows + d]);
+  all[q][i] = p;
+  __syncthreads();
+  for (int k = 8; k > 0; k >>= 1) {
+    if (q < k) all[q][i] = join(all[q][i], all[q + k][i]);
+    __syncthreads();
+  }
+  if (q != 0 || d >= n_rows) return;
+  p = all[0][i];
+  const float z = base_of(p.m) + kLn2 * __builtin_amdgcn_logf(p.s);
+  const bool use = labels == nullptr || (uint32_t)labels[d] < (uint32_t)n_classes;
+  lse[d] = use ? z : 0.0f;
+  if (loss) loss[d] = use ? z - picked[d] : 0.0f;
+}
+
+template <class S>
+__global__ void __launch_bounds__(S::NT) softmax_piece_kernel(const ScoreArgs<typename S::T> g) {
+  typedef typename S::T T;
+  __shared__ __align__(16) char lds[S::kLdsBytes];
+  uint32_t tr, tc;
+  tile_place(g, &tr, &tc);
+  const int row0 = (int)tr * S::BM, col0 = g.begin + (int)tc * S::BN;
+  f32x4 acc[S::TM][S::TN];
+  scores_tile<S, true>(lds, g, row0, col0, acc);
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int m0 = (w / S::WN) * (S::TM * 16), n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int d = row0 + m0 + 16 * i + (l & 15);
+    if (d >= g.n_rows) continue;
+    const int y = g.labels[d];
+    const bool use = (uint32_t)y < (uint32_t)g.n_classes;
+    const float lse = g.lse[d];
+    const float weight = g.weight ? g.weight[d] : 1.0f;
+    T* to = g.g + (int64_t)d * g.ld_g - g.begin;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      const int n = n0 + 16 * j;
+      f32x4 v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float p = exp_diff(acc[i][j][r], lse);
+        v[r] = use && n + r < g.end ? weight * (n + r == y ? p - 1.0f : p) : 0.0f;
+      }
+      store4(to + n, v, 4);
+    }
+  }
+}
+
+template <class S>
+__global__ void __launch_bounds__(S::NT) softmax_stats_kernel(const ScoreArgs<typename S::T> g) {
+  __shared__ __align__(16) char lds[S::kLdsBytes];
+  uint32_t tr, tc;
+  tile_place(g, &tr, &tc);
+  const int row0 = (int)tr * S::BM, col0 = g.begin + (int)tc * S::BN;
+  f32x4 acc[S::TM][S::TN];
+  scores_tile<S, false>(lds, g, row0, col0, acc);
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int d0 = row0 + (w / S::WN) * (S::TM * 16) + 4 * (l >> 4), n0 = col0 + (w % S::WN) * (S::TN * 16) + (l & 15);
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int d = d0 + 16 * i;
+    if (d >= g.n_rows) continue;
+    float lse[4];
+    int y[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const bool in = d + r < g.n_rows;
+      lse[r] = in ? g.lse[d + r] : 0.0f;
+      y[r] = in && g.labels ? g.labels[d + r] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      const int n = n0 + 16 * j;
+      if (n >= g.end) continue;
+      f32x4 grad, hess;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const bool use = g.labels == nullptr || (uint32_t)y[r] < (uint32_t)g.n_classes;
+        const float p = use ? exp_diff(acc[i][j][r], lse[r]) : 0.0f;
+        grad[r] = n == y[r] ? p - 1.0f : p;
+        hess[r] = p * (1.0f - p);
+      }
+      const int64_t at = (int64_t)(n - g.begin) * g.ld_out + d;
+      store4(g.grad + at, grad, g.n_rows - d);
+      store4(g.hess + at, hess, g.n_rows - d);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- the products with G
+
+template <typename T>
+struct PieceArgs {
+  const T* a;  // G of the piece
+  const T* b;  // C of the piece (dh) or H (dC)
+  T* out;      // the result, if it is written here
+  float* sums; // [splits][rows][cols] f32, otherwise
+  const int32_t* labels;
+  int64_t ld_a, ld_b, ld_out;
+  float scale;
+  int32_t rows, cols, k, n_classes;  // of the result; the summed axis
+  int32_t k_split;                   // of the summed axis a workgroup takes, whole steps
+  int32_t b_rows;                    // rows of b: k may pass them by the zeros behind G's classes
+  int32_t add;                       // sums hold earlier pieces' shares
+  uint32_t row_tiles, col_tiles, splits, group;
+};
+
+// Rows of H whose label counts.
+template <typename T>
+struct CountedRows {
+  const T* base;
+  int64_t ld;
+  const int32_t* labels;
+  int32_t n, n_classes;
+  __device__ __forceinline__ const T* operator()(int r) const {
+    return r < n && (uint32_t)labels[r] < (uint32_t)n_classes ? base + (int64_t)r * ld : nullptr;
+  }
+};
+
+// TO_ROWS: dh (the result's rows are G's rows, k = classes); otherwise dC (its rows are classes, k = G's rows).
+template <class S, bool TO_ROWS>
+__global__ void __launch_bounds__(S::NT) piece_product_kernel(const PieceArgs<typename S::T> g) {
+  typedef typename S::T T;
+  __shared__ __align__(16) char lds[S::kLdsBytes];
+  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
+  const uint32_t tiles = g.row_tiles * g.col_tiles;
+  const uint32_t split = t / tiles, u = t % tiles;
+  const uint32_t span = g.group * g.col_tiles, first = u / span * g.group;
+  const uint32_t in = g.row_tiles - first < g.group ? g.row_tiles - first : g.group;
+  const int row0 = (int)(first + u % span % in) * S::BM, col0 = (int)(u % span / in) * S::BN;
+  const int k0 = (int)split * g.k_split;
+  const int k1 = g.k - k0 < g.k_split ? g.k : k0 + g.k_split;
+  f32x4 acc[S::TM][S::TN];
+  ColumnOperand<T, S::BN, S::NT, S::DIRECT> b;
+  if constexpr (TO_ROWS) {
+    const PlainRows<T> rows_a = {g.a, g.ld_a, g.rows};
+    const PlainRows<T> rows_b = {g.b, g.ld_b, g.b_rows};
+    RowOperand<T, S::BM, S::NT, S::DIRECT> a;
+    a.init(rows_a, row0, 0, k0, k1);
+    b.init(rows_b, col0, g.cols, k0, k1);
+    tile_product<S, true>(lds, a, b, rows_a, rows_b, k0, k1, acc, Nothing{});
+  } else {
+    const PlainRows<T> rows_a = {g.a, g.ld_a, g.k};
+    const CountedRows<T> rows_b = {g.b, g.ld_b, g.labels, g.b_rows, g.n_classes};
+    ColumnOperand<T, S::BM, S::NT, S::DIRECT> a;
+    a.init(rows_a, row0, (g.rows + kChunk<T> - 1) / kChunk<T> * kChunk<T>, k0, k1);  // G is zero up to ld_a
+    b.init(rows_b, col0, g.cols, k0, k1);
+    tile_product<S, true>(lds, a, b, rows_a, rows_b, k0, k1, acc, Nothing{});
+  }
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int m0 = row0 + (w / S::WN) * (S::TM * 16), n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+  float* sums = g.sums ? g.sums + (int64_t)split * g.rows * g.cols : nullptr;
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int m = m0 + 16 * i + (l & 15);
+    if (m >= g.rows) continue;
+    const bool use = !TO_ROWS || (uint32_t)g.labels[m] < (uint32_t)g.n_classes;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      const int n = n0 + 16 * j;
+      if (n >= g.cols) continue;
+      f32x4 v = acc[i][j];
+      if (sums) {
+        float* to = sums + (int64_t)m * g.cols + n;
+        if (g.add) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r < g.cols) v[r] += to[r];
+        }
+        store4(to, v, g.cols - n);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = use ? g.scale * v[r] : 0.0f;
+        store4(g.out + (int64_t)m * g.ld_out + n, v, g.cols - n);
+      }
+    }
+  }
+}
+
+// out = scale * sums over the splits, in order; rows that do not count (labels given) are zeros.
+template <typename T>
+__global__ void __launch_bounds__(256) piece_join_kernel(const PieceArgs<T> g) {
+  const int64_t n = (int64_t)g.rows * g.cols;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
+    const int64_t m = e / g.cols;
+    float s = 0.0f;
+    for (uint32_t k = 0; k < g.splits; ++k) s += g.sums[(int64_t)k * n + e];
+    const bool use = g.labels == nullptr || (uint32_t)g.labels[m] < (uint32_t)g.n_classes;
+    g.out[m * g.ld_out + (e - m * g.cols)] = (T)(use ? g.scale * s : 0.0f);
+  }
+}
+
+}  // namespace gbdt_softmax
