@@ -57,28 +57,40 @@ __device__ __forceinline__ int find_leaf(const int64_t* offsets, int n_leaves, i
   return lo;
 }
 
-// Rows of a matrix by position in the list.
+// Rows of a matrix by position in the list; `end` is the matrix's, one past its last value.
 template <typename T>
 struct ListRows {
+  static constexpr bool kEven = false;  // not a constant distance apart
   const T* base;
+  const T* end;
   int64_t ld;
   const int32_t* row_idx;
-  int32_t end, n_rows;
-  __device__ __forceinline__ const T* operator()(int p) const {
-    if (p >= end) return nullptr;
-    const int d = row_idx ? row_idx[p] : p;
+  int32_t stop, n_rows;
+  __device__ __forceinline__ int fetch(int p) const { return p < stop ? (row_idx ? row_idx[p] : p) : -1; }
+  __device__ __forceinline__ const T* at(int, int d) const {
     return (uint32_t)d < (uint32_t)n_rows ? base + (int64_t)d * ld : nullptr;
   }
 };
+template <typename T>
+__device__ __forceinline__ ListRows<T> list_rows(const T* base, int64_t ld, int cols, const LeafArgs<T>& g, int stop) {
+  return {base, base + (int64_t)(g.n_rows - 1) * ld + cols, ld, g.row_idx, stop, g.n_rows};
+}
 
 // Rows of a matrix in order.
 template <typename T>
 struct PlainRows {
+  static constexpr bool kEven = true;
   const T* base;
+  const T* end;
   int64_t ld;
   int32_t n;
-  __device__ __forceinline__ const T* operator()(int r) const { return r < n ? base + (int64_t)r * ld : nullptr; }
+  __device__ __forceinline__ int fetch(int) const { return 0; }
+  __device__ __forceinline__ const T* at(int r, int) const { return r < n ? base + (int64_t)r * ld : nullptr; }
 };
+template <typename T>
+__device__ __forceinline__ PlainRows<T> plain_rows(const T* base, int64_t ld, int n, int cols) {
+  return {base, base + (int64_t)(n - 1) * ld + cols, ld, n};
+}
 
 // Writes the tile's values (N_INNER) to the rows of the list, adding bias if there is one.
 template <class S, typename T>
@@ -109,7 +121,7 @@ __device__ __forceinline__ void scatter_rows(const f32x4 (&acc)[S::TM][S::TN], c
 
 // y: rows of x times the leaf's rows of w, both with k = input along memory.
 template <class S>
-__global__ void __launch_bounds__(S::NT) leaf_product_kernel(const LeafArgs<typename S::T> g) {
+__global__ void __launch_bounds__(S::NT, 2) leaf_product_kernel(const LeafArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
   const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
@@ -119,10 +131,10 @@ __global__ void __launch_bounds__(S::NT) leaf_product_kernel(const LeafArgs<type
   const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
   const int p0 = begin + (tile - (begin / S::BM + leaf)) * S::BM;
   if (p0 >= end || p0 < begin) return;
-  const ListRows<T> rows_a = {g.x, g.ld_x, g.row_idx, end, g.n_rows};
-  const PlainRows<T> rows_b = {g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out};
-  RowOperand<T, S::BM, S::NT, S::DIRECT> a;
-  RowOperand<T, S::BN, S::NT, S::DIRECT> b;
+  const ListRows<T> rows_a = list_rows(g.x, g.ld_x, g.d_in, g, end);
+  const PlainRows<T> rows_b = plain_rows(g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out, g.d_in);
+  typename S::RowsA a;
+  typename S::RowsB b;
   a.init(rows_a, p0, 0, 0, g.d_in);
   b.init(rows_b, col0, 0, 0, g.d_in);
   f32x4 acc[S::TM][S::TN];
@@ -133,7 +145,7 @@ __global__ void __launch_bounds__(S::NT) leaf_product_kernel(const LeafArgs<type
 
 // dx: rows of dy (k = output along memory) times w, whose rows are k.
 template <class S>
-__global__ void __launch_bounds__(S::NT) leaf_grad_input_kernel(const LeafArgs<typename S::T> g) {
+__global__ void __launch_bounds__(S::NT, 2) leaf_grad_input_kernel(const LeafArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
   const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
@@ -143,10 +155,10 @@ __global__ void __launch_bounds__(S::NT) leaf_grad_input_kernel(const LeafArgs<t
   const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
   const int p0 = begin + (tile - (begin / S::BM + leaf)) * S::BM;
   if (p0 >= end || p0 < begin) return;
-  const ListRows<T> rows_a = {g.dy, g.ld_dy, g.row_idx, end, g.n_rows};
-  const PlainRows<T> rows_b = {g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out};
-  RowOperand<T, S::BM, S::NT, S::DIRECT> a;
-  ColumnOperand<T, S::BN, S::NT, S::DIRECT> b;
+  const ListRows<T> rows_a = list_rows(g.dy, g.ld_dy, g.d_out, g, end);
+  const PlainRows<T> rows_b = plain_rows(g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out, g.d_in);
+  typename S::RowsA a;
+  typename S::ColumnsB b;
   a.init(rows_a, p0, 0, 0, g.d_out);
   b.init(rows_b, col0, g.d_in, 0, g.d_out);
   f32x4 acc[S::TM][S::TN];
@@ -159,14 +171,13 @@ template <class S>
 struct RowSums {
   f32x4 (&sum)[S::TM];
   bool on;
-  template <class FA, class FB>
-  __device__ __forceinline__ void operator()(const FA& fa, const FB&) const {
+  template <class F>
+  __device__ __forceinline__ void operator()(int i, const F& rows) const {
     if (!on) return;
-    typename Traits<typename S::T>::Frag ones;
+    F ones;
 #pragma unroll
-    for (int i = 0; i < kChunk<typename S::T>; ++i) ones[i] = (typename S::T)1.0f;
-#pragma unroll
-    for (int i = 0; i < S::TM; ++i) sum[i] = mma(ones, fa[i], sum[i]);
+    for (int k = 0; k < kChunk<typename S::T>; ++k) ones[k] = (typename S::T)1.0f;
+    sum[i] = mma(ones, rows, sum[i]);
   }
 };
 
@@ -176,7 +187,7 @@ struct RowSums {
 // the pieces between two cuts only the first can have begun before (slot 2 b) and only the last can end behind (2 b + 1).
 // leaf_grad_join_kernel adds a leaf's slots in order, so the sums do not depend on which workgroup ran first.
 template <class S>
-__global__ void __launch_bounds__(S::NT) leaf_grad_weight_kernel(const LeafArgs<typename S::T> g) {
+__global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
   const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
@@ -190,10 +201,10 @@ __global__ void __launch_bounds__(S::NT) leaf_grad_weight_kernel(const LeafArgs<
   const int64_t b0 = block * g.cut, b1 = b0 + g.cut;
   const int p0 = begin > b0 ? begin : (int)(b0 < end ? b0 : end), p1 = end < b1 ? end : (int)b1;
   if (p0 >= p1 && (end > begin || block != begin / g.cut)) return;  // only an empty leaf's one piece is empty: zeros
-  const ListRows<T> rows_a = {g.dy, g.ld_dy, g.row_idx, p1, g.n_rows};
-  const ListRows<T> rows_b = {g.x, g.ld_x, g.row_idx, p1, g.n_rows};
-  ColumnOperand<T, S::BM, S::NT, S::DIRECT> a;
-  ColumnOperand<T, S::BN, S::NT, S::DIRECT> b;
+  const ListRows<T> rows_a = list_rows(g.dy, g.ld_dy, g.d_out, g, p1);
+  const ListRows<T> rows_b = list_rows(g.x, g.ld_x, g.d_in, g, p1);
+  typename S::ColumnsA a;
+  typename S::ColumnsB b;
   a.init(rows_a, row0, g.d_out, p0, p1);
   b.init(rows_b, col0, g.d_in, p0, p1);
   f32x4 acc[S::TM][S::TN];

@@ -7,6 +7,7 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/gbdt_hist.h"
 #include "library_state.h"
@@ -19,7 +20,6 @@ namespace {
 using gbdt_internal::hip_failed;
 using gbdt_tile::bf16;
 using gbdt_tile::kChunk;
-using gbdt_tile::kStep;
 using gbdt_tile::Shape;
 
 #define LAUNCHED(what)                                    \
@@ -144,7 +144,6 @@ int leaf_product_grad(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
 
 // ---------------------------------------------------------------- softmax
 
-constexpr int kScoreBM = 128, kScoreBN = 128;
 constexpr int64_t kPieceAlign = 256;                    // classes: whole tiles of every shape
 constexpr int64_t kPieceBytes = (int64_t)256 << 20;     // G of a piece, as long as it is kPieceAlign classes wide at least
 constexpr int64_t kPartsBytes = (int64_t)256 << 20;     // maxima and sums of a launch's tiles
@@ -156,6 +155,15 @@ int softmax_check(const void* h, int64_t ld_h, const void* c, int64_t ld_c, int6
   if (off_element(h, dtype) || off_element(c, dtype)) return GBDT_EINVAL;
   if (n_rows >= kMaxRows || n_classes >= kMaxRows || dim >= kMaxWidth) return GBDT_EUNSUPPORTED;
   return GBDT_OK;
+}
+
+// Tiles of 256 x 256 by eight wavefronts, one workgroup a compute unit (f32: as any other; its products are 16 times slower
+// and its loads never the bound).
+template <typename T>
+using Wide = typename std::conditional<sizeof(T) == 2, Shape<T, 256, 256, 2, 4, true, true>, Shape<T, 128, 128, 2, 2, true>>::type;
+template <typename T>
+bool wide_tiles(int64_t rows, int64_t cols) {
+  return sizeof(T) == 2 && ceil_div(rows, 256) * ceil_div(cols, 256) >= 256;
 }
 
 // Row tiles that go through the classes together: 2 MiB of rows, half of an XCD's L2.
@@ -181,7 +189,7 @@ struct LossPlan {
 };
 LossPlan loss_plan(int64_t n_rows, int64_t n_classes) {
   LossPlan p;
-  p.tiles = ceil_div(n_classes, kScoreBN);
+  p.tiles = ceil_div(n_classes, gbdt_softmax::kPartClasses);
   p.rows = std::min(n_rows, std::max<int64_t>(4096, kPartsBytes / (8 * p.tiles) / 4096 * 4096));
   p.parts_bytes = pad256((size_t)(p.rows * p.tiles) * 8);
   p.bytes = p.parts_bytes + pad256((size_t)p.rows * 4);
@@ -190,7 +198,6 @@ LossPlan loss_plan(int64_t n_rows, int64_t n_classes) {
 
 template <class S, typename T>
 int launch_scores(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
-  static_assert(S::BN == kScoreBN, "loss_plan counts these");
   unsigned blocks = 0;
   const int rc = score_grid<S>(g, &blocks);
   if (rc != GBDT_OK) return rc;
@@ -219,8 +226,9 @@ int softmax_loss(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
     g.n_rows = (int32_t)std::min(plan.rows, n_rows - r);
     g.n_classes = g.end = (int32_t)n_classes;
     g.dim = dim;
-    rc = direct ? launch_scores<Shape<T, kScoreBM, kScoreBN, 2, 2, true>>(g, s)
-                : launch_scores<Shape<T, kScoreBM, kScoreBN, 2, 2, false>>(g, s);
+    rc = direct && wide_tiles<T>(g.n_rows, n_classes) ? launch_scores<Wide<T>>(g, s)
+         : direct                                     ? launch_scores<Shape<T, 128, 128, 2, 2, true>>(g, s)
+                                                      : launch_scores<Shape<T, 128, 128, 2, 2, false>>(g, s);
     if (rc != GBDT_OK) return rc;
     gbdt_softmax::softmax_join_kernel<<<dim3((unsigned)ceil_div(g.n_rows, 16)), dim3(256), 0, s>>>(
         g.parts, g.picked, g.labels, g.n_rows, g.n_classes, (int32_t)plan.tiles, loss ? loss + r : nullptr, lse + r);
@@ -233,7 +241,8 @@ struct GradPlan {
   int64_t width;   // classes a piece
   int64_t pieces;
   int64_t dh_splits, dh_split, dc_splits, dc_split;
-  size_t g_bytes, dh_bytes, dc_bytes;
+  size_t g_bytes, dh_bytes, dc_bytes, h_bytes, c_bytes;
+  size_t bytes() const { return g_bytes + dh_bytes + dc_bytes + h_bytes + c_bytes; }
 };
 // Splits of a summed axis of `k`: as many as fill the compute units, each 8 steps long at least.
 void split_axis(int64_t tiles, int64_t k, int64_t step, int64_t units, int64_t* splits, int64_t* len) {
@@ -241,7 +250,7 @@ void split_axis(int64_t tiles, int64_t k, int64_t step, int64_t units, int64_t* 
   *len = std::max(step, round_up(ceil_div(k, want), step));
   *splits = std::max<int64_t>(1, ceil_div(k, *len));
 }
-GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, int64_t units) {
+GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, bool c_whole, int64_t units) {
   GradPlan p;
   const int64_t rows = std::max<int64_t>(n_rows, 1);
   const int64_t all = round_up(n_classes, kPieceAlign);
@@ -249,14 +258,30 @@ GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, in
   p.pieces = ceil_div(n_classes, p.width);
   p.width = round_up(ceil_div(n_classes, p.pieces), kPieceAlign);
   p.pieces = ceil_div(n_classes, p.width);
-  const int64_t step = gbdt_tile::kStepBytes / e;
+  const int64_t step = 128 / e;
   const int64_t cols = ceil_div(dim, 128);
   split_axis(ceil_div(rows, 128) * cols, p.width, step, units, &p.dh_splits, &p.dh_split);
+  const int64_t wide = ceil_div(rows, 256) * ceil_div(dim, 256);
+  if (e == 2 && wide < units && wide * ceil_div(p.width, 16 * step) >= units)
+    split_axis(wide, p.width, step, units, &p.dh_splits, &p.dh_split);
   split_axis(ceil_div(p.width, 128) * cols, n_rows, step, units, &p.dc_splits, &p.dc_split);
   p.g_bytes = pad256((size_t)(rows * p.width * e));
   p.dh_bytes = p.dh_splits > 1 || p.pieces > 1 ? pad256((size_t)(p.dh_splits * rows * dim) * 4) : 0;
   p.dc_bytes = p.dc_splits > 1 ? pad256((size_t)(p.dc_splits * p.width * dim) * 4) : 0;
+  const int64_t row_bytes = round_up(dim * e, 16);
+  p.h_bytes = pad256((size_t)(rows * row_bytes));
+  p.c_bytes = c_whole ? 0 : pad256((size_t)(n_classes * row_bytes));
   return p;
+}
+
+template <typename T>
+int whole_rows(const T* from, int64_t ld, T* to, int64_t rows, int32_t cols, const int32_t* labels, int64_t n_classes, hipStream_t s) {
+  const int64_t blocks = ceil_div(rows * ceil_div(cols, kChunk<T>), 256);
+  if (blocks == 0) return GBDT_OK;
+  gbdt_softmax::whole_rows_kernel<T><<<dim3((unsigned)std::min<int64_t>(blocks, 16384)), dim3(256), 0, s>>>(
+      from, ld, to, (int32_t)rows, cols, labels, (int32_t)n_classes);
+  LAUNCHED("whole_rows_kernel");
+  return GBDT_OK;
 }
 
 template <class S, typename T>
@@ -296,14 +321,30 @@ template <typename T>
 int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32_t* labels, const float* lse, const float* weight,
                  float scale, int64_t n_rows, int64_t n_classes, int32_t dim, T* dh, int64_t ld_dh, T* dc, int64_t ld_dc,
                  hipStream_t s) {
-  const GradPlan plan = grad_plan(n_rows, n_classes, dim, sizeof(T), gbdt_internal::cu_count());
+  const bool c_whole = whole_chunks<T>(c, ld_c, dim);
+  const GradPlan plan = grad_plan(n_rows, n_classes, dim, sizeof(T), c_whole, gbdt_internal::cu_count());
   void* ws = nullptr;
-  int rc = gbdt_internal::workspace(plan.g_bytes + plan.dh_bytes + plan.dc_bytes, s, &ws);
+  int rc = gbdt_internal::workspace(plan.bytes(), s, &ws);
   if (rc != GBDT_OK) return rc;
-  T* piece = (T*)ws;
-  float* dh_sums = plan.dh_bytes ? (float*)((char*)ws + plan.g_bytes) : nullptr;
-  float* dc_sums = plan.dc_bytes ? (float*)((char*)ws + plan.g_bytes + plan.dh_bytes) : nullptr;
-  const bool direct = whole_chunks<T>(h, ld_h, dim) && whole_chunks<T>(c, ld_c, dim);
+  char* at = (char*)ws;
+  T* piece = (T*)at;
+  at += plan.g_bytes;
+  float* dh_sums = plan.dh_bytes ? (float*)at : nullptr;
+  at += plan.dh_bytes;
+  float* dc_sums = plan.dc_bytes ? (float*)at : nullptr;
+  at += plan.dc_bytes;
+  // Both matrices are of whole chunks from here on; whole_dim is the length of their rows.
+  const int32_t whole_dim = (int32_t)round_up(dim, kChunk<T>);
+  if ((rc = whole_rows<T>(h, ld_h, (T*)at, n_rows, dim, labels, n_classes, s)) != GBDT_OK) return rc;
+  h = (const T*)at;
+  ld_h = whole_dim;
+  at += plan.h_bytes;
+  if (!c_whole) {
+    if ((rc = whole_rows<T>(c, ld_c, (T*)at, n_classes, dim, nullptr, n_classes, s)) != GBDT_OK) return rc;
+    c = (const T*)at;
+    ld_c = whole_dim;
+  }
+  typedef Shape<T, 128, 128, 2, 2, true> Small;
   gbdt_softmax::PieceArgs<T> to_h = {}, to_c = {};
   for (int64_t begin = 0; begin < n_classes; begin += plan.width) {
     const int64_t end = std::min(n_classes, begin + plan.width);
@@ -319,17 +360,16 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
     g.ld_g = plan.width;
     g.n_rows = (int32_t)n_rows;
     g.n_classes = (int32_t)n_classes;
-    g.dim = dim;
+    g.dim = whole_dim;
     g.begin = (int32_t)begin;
     g.end = (int32_t)end;
-    rc = direct ? launch_piece<Shape<T, 128, 128, 2, 2, true>>(g, s) : launch_piece<Shape<T, 128, 128, 2, 2, false>>(g, s);
+    rc = wide_tiles<T>(n_rows, end - begin) ? launch_piece<Wide<T>>(g, s) : launch_piece<Small>(g, s);
     if (rc != GBDT_OK) return rc;
     if (dc) {
       to_c.a = piece;
       to_c.b = h;
       to_c.out = dc + begin * ld_dc;
       to_c.sums = dc_sums;
-      to_c.labels = labels;
       to_c.ld_a = plan.width;
       to_c.ld_b = ld_h;
       to_c.ld_out = ld_dc;
@@ -337,17 +377,13 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
       to_c.rows = (int32_t)(end - begin);
       to_c.cols = dim;
       to_c.k = to_c.b_rows = (int32_t)n_rows;
+      to_c.b_cols = whole_dim;
       to_c.n_classes = (int32_t)n_classes;
       to_c.k_split = (int32_t)plan.dc_split;
       to_c.splits = (uint32_t)plan.dc_splits;
-      rc = direct ? launch_product<Shape<T, 128, 128, 2, 2, true>, false>(to_c, s)
-                  : launch_product<Shape<T, 128, 128, 2, 2, false>, false>(to_c, s);
+      rc = wide_tiles<T>(to_c.rows, dim) ? launch_product<Wide<T>, false>(to_c, s) : launch_product<Small, false>(to_c, s);
       if (rc != GBDT_OK) return rc;
-      if (dc_sums) {
-        gbdt_softmax::PieceArgs<T> j = to_c;
-        j.labels = nullptr;  // a class always has its gradient
-        if ((rc = join_product(j, s)) != GBDT_OK) return rc;
-      }
+      if (dc_sums && (rc = join_product(to_c, s)) != GBDT_OK) return rc;
     }
     if (dh && n_rows > 0) {
       to_h.a = piece;
@@ -363,12 +399,12 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
       to_h.cols = dim;
       to_h.k = (int32_t)round_up(end - begin, kChunk<T>);
       to_h.b_rows = (int32_t)(end - begin);
+      to_h.b_cols = whole_dim;
       to_h.n_classes = (int32_t)n_classes;
       to_h.k_split = (int32_t)plan.dh_split;
       to_h.splits = (uint32_t)plan.dh_splits;
       to_h.add = begin > 0;
-      rc = direct ? launch_product<Shape<T, 128, 128, 2, 2, true>, true>(to_h, s)
-                  : launch_product<Shape<T, 128, 128, 2, 2, false>, true>(to_h, s);
+      rc = wide_tiles<T>(n_rows * plan.dh_splits, dim) ? launch_product<Wide<T>, true>(to_h, s) : launch_product<Small, true>(to_h, s);
       if (rc != GBDT_OK) return rc;
     }
   }
@@ -514,8 +550,8 @@ size_t gbdt_softmax_workspace_bytes(int64_t n_rows, int64_t n_classes, int32_t d
   if (n_rows < 0 || n_classes <= 0 || dim <= 0 || n_rows >= kMaxRows || n_classes >= kMaxRows || dim >= kMaxWidth ||
       (dtype != GBDT_F32 && dtype != GBDT_BF16))
     return 0;
-  const GradPlan p = grad_plan(n_rows, n_classes, dim, dtype == GBDT_F32 ? 4 : 2, gbdt_internal::cu_count());
-  const size_t grad = p.g_bytes + p.dh_bytes + p.dc_bytes, loss = loss_plan(n_rows, n_classes).bytes;
+  const GradPlan p = grad_plan(n_rows, n_classes, dim, dtype == GBDT_F32 ? 4 : 2, false, gbdt_internal::cu_count());
+  const size_t grad = p.bytes(), loss = loss_plan(n_rows, n_classes).bytes;
   return gbdt_internal::workspace_head_bytes() + std::max(grad, loss);
 }
 

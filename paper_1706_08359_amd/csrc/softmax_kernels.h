@@ -13,7 +13,7 @@
 // scale (1 / n_rows, as a rule) multiplies f32 sums, so it takes no part in that rounding.
 //
 // A row whose label is outside [0, n_classes) is ignored: loss, lse, G, gradient and hessian are zeros whatever h holds there
-// (its row of H is read as zeros where it would meet a zero of G).
+// (its row of H is zeros in the copy that meets G).
 #pragma once
 
 #include "leaf_product_kernels.h"
@@ -22,13 +22,18 @@ namespace gbdt_softmax {
 
 using namespace gbdt_tile;
 using gbdt_leaf::PlainRows;
+using gbdt_leaf::plain_rows;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// The difference is taken first: it is exact where a score is close to its row's lse, however large both are, which
+// s log2 e - lse log2 e is not.
 __device__ __forceinline__ float exp_diff(float s, float base) { return __builtin_amdgcn_exp2f((s - base) * kLog2e); }
 // What a running maximum is subtracted as: exponentials beneath an infinite one are 0 or infinite, not inf - inf.
 __device__ __forceinline__ float base_of(float m) { return __builtin_isinf(m) ? 0.0f : m; }
+
+constexpr int kPartClasses = 128;  // of a maximum and a sum, whatever the tile
 
 struct MaxSum {
   float m, s;
@@ -46,7 +51,7 @@ struct ScoreArgs {
   const int32_t* labels;  // [n_rows] or null
   const float* lse;       // [n_rows]
   const float* weight;    // [n_rows] or null
-  MaxSum* parts;          // [col_tiles][n_rows]
+  MaxSum* parts;          // [ceil(n_classes / kPartClasses)][n_rows]
   float* picked;          // [n_rows]: the label's score
   T* g;                   // [n_rows][ld_g]: G of the classes begin .. end, zeros behind
   float* grad;            // [end - begin][ld_out]
@@ -70,17 +75,17 @@ __device__ __forceinline__ void tile_place(const Args& g, uint32_t* row, uint32_
 
 template <class S, bool N_INNER, typename T>
 __device__ __forceinline__ void scores_tile(char* lds, const ScoreArgs<T>& g, int row0, int col0, f32x4 (&acc)[S::TM][S::TN]) {
-  const PlainRows<T> rows_a = {g.h, g.ld_h, g.n_rows};
-  const PlainRows<T> rows_b = {g.c, g.ld_c, g.end};
-  RowOperand<T, S::BM, S::NT, S::DIRECT> a;
-  RowOperand<T, S::BN, S::NT, S::DIRECT> b;
+  const PlainRows<T> rows_a = plain_rows(g.h, g.ld_h, g.n_rows, g.dim);
+  const PlainRows<T> rows_b = plain_rows(g.c, g.ld_c, g.end, g.dim);
+  typename S::RowsA a;
+  typename S::RowsB b;
   a.init(rows_a, row0, 0, 0, g.dim);
   b.init(rows_b, col0, 0, 0, g.dim);
   tile_product<S, N_INNER>(lds, a, b, rows_a, rows_b, 0, g.dim, acc, Nothing{});
 }
 
 template <class S>
-__global__ void __launch_bounds__(S::NT) softmax_scores_kernel(const ScoreArgs<typename S::T> g) {
+__global__ void __launch_bounds__(S::NT, 2) softmax_scores_kernel(const ScoreArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
   uint32_t tr, tc;
   tile_place(g, &tr, &tc);
@@ -96,17 +101,26 @@ __global__ void __launch_bounds__(S::NT) softmax_scores_kernel(const ScoreArgs<t
     const int m = m0 + 16 * i + (l & 15);
     const int d = row0 + m;
     const int y = g.labels && d < g.n_rows ? g.labels[d] : -1;
+    if (col0 + S::BN > g.end) {  // classes past the last add nothing to either
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[i][j][r] = n0 + 16 * j + r < g.end ? acc[i][j][r] : -__builtin_inff();
+    }
+    const int rel = y - n0;  // rarely here
+    if (rel >= 0 && rel < 16 * S::TN && (rel & 15) < 4 && y < g.end) {
+      float picked = 0.0f;
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) picked = rel == 16 * j + r ? acc[i][j][r] : picked;
+      g.picked[d] = picked;
+    }
     float top = -__builtin_inff();
 #pragma unroll
     for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int n = n0 + 16 * j + r;
-        if (n < g.end) {
-          top = fmaxf(top, acc[i][j][r]);
-          if (n == y) g.picked[d] = acc[i][j][r];
-        }
-      }
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r]);
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     const float base = base_of(top);
@@ -114,23 +128,25 @@ __global__ void __launch_bounds__(S::NT) softmax_scores_kernel(const ScoreArgs<t
 #pragma unroll
     for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (n0 + 16 * j + r < g.end) sum += exp_diff(acc[i][j][r], base);
+      for (int r = 0; r < 4; ++r) sum += exp_diff(acc[i][j][r], base);
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     if (l < 16) row_parts[(w % S::WN) * S::BM + m] = {top, sum};
   }
   __syncthreads();
-  for (int m = threadIdx.x; m < S::BM; m += S::NT) {
-    if (row0 + m >= g.n_rows) break;
-    MaxSum p = row_parts[m];
+  constexpr int waves = kPartClasses / (S::TN * 16);  // of a part
+  static_assert(S::BN % kPartClasses == 0 && waves >= 1, "tiles of whole parts");
+  for (int e = threadIdx.x; e < S::BM * (S::BN / kPartClasses); e += S::NT) {
+    const int m = e % S::BM, q = e / S::BM;
+    if (row0 + m >= g.n_rows || col0 + q * kPartClasses >= g.end) continue;
+    MaxSum p = row_parts[q * waves * S::BM + m];
 #pragma unroll
-    for (int k = 1; k < S::WN; ++k) p = join(p, row_parts[k * S::BM + m]);
-    g.parts[(int64_t)tc * g.n_rows + row0 + m] = p;
+    for (int k = 1; k < waves; ++k) p = join(p, row_parts[(q * waves + k) * S::BM + m]);
+    g.parts[((int64_t)tc * (S::BN / kPartClasses) + q) * g.n_rows + row0 + m] = p;
   }
 }
 
-// Joins a row's tiles: 16 lanes a row, each every 16th tile in order, then pairwise.
+// Joins a row's parts: 16 lanes a row, each every 16th part in order, then pairwise.
 __global__ void __launch_bounds__(256) softmax_join_kernel(const MaxSum* parts, const float* picked, const int32_t* labels, int32_t n_rows,
                                                            int32_t n_classes, int32_t tiles, float* loss, float* lse) {
   const int d0 = blockIdx.x * 16;
@@ -155,7 +171,7 @@ __global__ void __launch_bounds__(256) softmax_join_kernel(const MaxSum* parts, 
 }
 
 template <class S>
-__global__ void __launch_bounds__(S::NT) softmax_piece_kernel(const ScoreArgs<typename S::T> g) {
+__global__ void __launch_bounds__(S::NT, 2) softmax_piece_kernel(const ScoreArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
   uint32_t tr, tc;
@@ -174,22 +190,31 @@ __global__ void __launch_bounds__(S::NT) softmax_piece_kernel(const ScoreArgs<ty
     const float lse = g.lse[d];
     const float weight = g.weight ? g.weight[d] : 1.0f;
     T* to = g.g + (int64_t)d * g.ld_g - g.begin;
+    f32x4 v[S::TN];
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j) {
-      const int n = n0 + 16 * j;
-      f32x4 v;
+    for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float p = exp_diff(acc[i][j][r], lse);
-        v[r] = use && n + r < g.end ? weight * (n + r == y ? p - 1.0f : p) : 0.0f;
-      }
-      store4(to + n, v, 4);
+      for (int r = 0; r < 4; ++r) v[j][r] = weight * exp_diff(acc[i][j][r], lse);
+    const int rel = y - n0;  // rarely here
+    if (rel >= 0 && rel < 16 * S::TN && (rel & 15) < 4) {
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[j][r] -= rel == 16 * j + r ? weight : 0.0f;
     }
+    if (!use || col0 + S::BN > g.end) {
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[j][r] = use && n0 + 16 * j + r < g.end ? v[j][r] : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) store4(to + n0 + 16 * j, v[j], 4);
   }
 }
 
 template <class S>
-__global__ void __launch_bounds__(S::NT) softmax_stats_kernel(const ScoreArgs<typename S::T> g) {
+__global__ void __launch_bounds__(S::NT, 2) softmax_stats_kernel(const ScoreArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
   uint32_t tr, tc;
   tile_place(g, &tr, &tc);
@@ -218,7 +243,8 @@ __global__ void __launch_bounds__(S::NT) softmax_stats_kernel(const ScoreArgs<ty
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const bool use = g.labels == nullptr || (uint32_t)y[r] < (uint32_t)g.n_classes;
-        const float p = use ? exp_diff(acc[i][j][r], lse[r]) : 0.0f;
+        const float e = exp_diff(acc[i][j][r], lse[r]);
+        const float p = use ? e : 0.0f;
         grad[r] = n == y[r] ? p - 1.0f : p;
         hess[r] = p * (1.0f - p);
       }
@@ -226,6 +252,29 @@ __global__ void __launch_bounds__(S::NT) softmax_stats_kernel(const ScoreArgs<ty
       store4(g.grad + at, grad, g.n_rows - d);
       store4(g.hess + at, hess, g.n_rows - d);
     }
+  }
+}
+
+// A copy whose rows are whole 16-byte chunks, filled up with zeros; rows whose label does not count (labels given) are all
+// zeros.  What meets G must be so: G is zero in a row that does not count, but h there may be anything, and 0 x NaN is not 0.
+template <typename T>
+__global__ void __launch_bounds__(256) whole_rows_kernel(const T* from, int64_t ld, T* to, int32_t rows, int32_t cols, const int32_t* labels,
+                                                         int32_t n_classes) {
+  const uint32_t per = (uint32_t)(cols + kChunk<T> - 1) / kChunk<T>;
+  const uint64_t n = (uint64_t)rows * per;
+  for (uint64_t e = (uint64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (uint64_t)gridDim.x * 256) {
+    const uint32_t r = (uint32_t)(e / per), c = (uint32_t)(e - (uint64_t)r * per) * kChunk<T>;
+    u32x4 v = {0, 0, 0, 0};
+    if (labels == nullptr || (uint32_t)labels[r] < (uint32_t)n_classes) {
+      const T* p = from + (int64_t)r * ld + c;
+      const int valid = cols - (int)c;
+      if (valid >= kChunk<T>) {
+        __builtin_memcpy(&v, p, 16);
+      } else {
+        v = last_chunk<T>(p, valid);
+      }
+    }
+    *(u32x4*)(to + e * kChunk<T>) = v;
   }
 }
 
@@ -242,26 +291,14 @@ struct PieceArgs {
   float scale;
   int32_t rows, cols, k, n_classes;  // of the result; the summed axis
   int32_t k_split;                   // of the summed axis a workgroup takes, whole steps
-  int32_t b_rows;                    // rows of b: k may pass them by the zeros behind G's classes
+  int32_t b_rows, b_cols;            // of b: k may pass its rows by the zeros behind G's classes; whole chunks of columns
   int32_t add;                       // sums hold earlier pieces' shares
   uint32_t row_tiles, col_tiles, splits, group;
 };
 
-// Rows of H whose label counts.
-template <typename T>
-struct CountedRows {
-  const T* base;
-  int64_t ld;
-  const int32_t* labels;
-  int32_t n, n_classes;
-  __device__ __forceinline__ const T* operator()(int r) const {
-    return r < n && (uint32_t)labels[r] < (uint32_t)n_classes ? base + (int64_t)r * ld : nullptr;
-  }
-};
-
 // TO_ROWS: dh (the result's rows are G's rows, k = classes); otherwise dC (its rows are classes, k = G's rows).
 template <class S, bool TO_ROWS>
-__global__ void __launch_bounds__(S::NT) piece_product_kernel(const PieceArgs<typename S::T> g) {
+__global__ void __launch_bounds__(S::NT, 2) piece_product_kernel(const PieceArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
   const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
@@ -273,20 +310,20 @@ __global__ void __launch_bounds__(S::NT) piece_product_kernel(const PieceArgs<ty
   const int k0 = (int)split * g.k_split;
   const int k1 = g.k - k0 < g.k_split ? g.k : k0 + g.k_split;
   f32x4 acc[S::TM][S::TN];
-  ColumnOperand<T, S::BN, S::NT, S::DIRECT> b;
+  typename S::ColumnsB b;
   if constexpr (TO_ROWS) {
-    const PlainRows<T> rows_a = {g.a, g.ld_a, g.rows};
-    const PlainRows<T> rows_b = {g.b, g.ld_b, g.b_rows};
-    RowOperand<T, S::BM, S::NT, S::DIRECT> a;
+    const PlainRows<T> rows_a = plain_rows(g.a, g.ld_a, g.rows, (int)g.ld_a);
+    const PlainRows<T> rows_b = plain_rows(g.b, g.ld_b, g.b_rows, g.cols);
+    typename S::RowsA a;
     a.init(rows_a, row0, 0, k0, k1);
-    b.init(rows_b, col0, g.cols, k0, k1);
+    b.init(rows_b, col0, g.b_cols, k0, k1 < g.b_rows ? k1 : g.b_rows);
     tile_product<S, true>(lds, a, b, rows_a, rows_b, k0, k1, acc, Nothing{});
   } else {
-    const PlainRows<T> rows_a = {g.a, g.ld_a, g.k};
-    const CountedRows<T> rows_b = {g.b, g.ld_b, g.labels, g.b_rows, g.n_classes};
-    ColumnOperand<T, S::BM, S::NT, S::DIRECT> a;
+    const PlainRows<T> rows_a = plain_rows(g.a, g.ld_a, g.k, (int)g.ld_a);
+    const PlainRows<T> rows_b = plain_rows(g.b, g.ld_b, g.b_rows, g.cols);
+    typename S::ColumnsA a;
     a.init(rows_a, row0, (g.rows + kChunk<T> - 1) / kChunk<T> * kChunk<T>, k0, k1);  // G is zero up to ld_a
-    b.init(rows_b, col0, g.cols, k0, k1);
+    b.init(rows_b, col0, g.b_cols, k0, k1);
     tile_product<S, true>(lds, a, b, rows_a, rows_b, k0, k1, acc, Nothing{});
   }
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;

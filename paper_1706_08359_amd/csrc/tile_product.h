@@ -8,13 +8,20 @@
 // column's four), 32-bit values by single-word reads.  So none of the products of a linear layer (values, gradient of the
 // input, gradient of the weights) needs a transposed copy of anything.
 //
-// A step takes 128 bytes of k (64 bf16, 32 f32): R x 128 bytes of an operand of R rows, in chunks of 16 bytes.  Chunk s of
-// the stage (thread s mod NT) lies at byte 16 s.  Within a row operand's row the chunks are permuted by the row's low
-// three bits, within a column operand's row by bits of k, so that the lanes of one fragment read spread over the banks.
-// Rows are found through functors that return a row's address or null; null rows and values past a limit are zeros.
-// There are two stages: the next step's chunks travel while the present one is multiplied.
-//   DIRECT: chunks go from memory to the stage without registers (every row 16-byte aligned, limits whole chunks).
-//   otherwise: through registers, by unaligned 16-byte loads, and value by value where a limit cuts a chunk.
+// A step takes KB = 128 or 64 bytes of k: R x KB bytes of an operand of R rows, in chunks of 16 bytes.  Chunk s of the stage
+// (thread s mod NT) lies at byte 16 s.  Within a row operand's row the chunks are permuted by bits of the row, within a
+// column operand's row by bits of k, so that the lanes of one fragment read spread over the banks.
+// Rows are found through functors: fetch(r) reads what the row's place hangs on (its id in a list, its label), at(r, that)
+// is its address or null.  Null rows and values past a limit are zeros.  A column operand fetches a step ahead, so that the
+// address of a gathered row does not wait for its id.
+// There are several stages: the next steps' chunks travel while the present one is multiplied.
+//   DIRECT: chunks go from memory to the stage without registers (every row 16-byte aligned, limits whole chunks).  A lane
+//   whose chunk is all zeros writes them itself; a row or column past its limit is any other, because what it yields is
+//   past the result's limit as well and is not stored.
+//   otherwise: through registers, by 16-byte loads of any alignment.  A chunk that a limit cuts is read whole, into the next
+//   row, and masked on its way to the stage; only where that would pass the matrix's end is it read value by value, behind
+//   the other loads (a branch among them made every load wait for the one before: 63 leaves of 50,021 x 137 f32, gradient of
+//   weights of 33 outputs, 159 us so).
 // Products of bf16 values are exact in f32 and sums are f32 throughout; f32 operands use the f32 matrix instruction.
 #pragma once
 
@@ -30,7 +37,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStepBytes = 128;  // of k, per staged row
 
 template <typename T> struct Traits;
 template <> struct Traits<bf16> {
@@ -40,29 +46,44 @@ template <> struct Traits<float> {
   typedef f32x4 Frag;
 };
 template <typename T> constexpr int kChunk = 16 / (int)sizeof(T);       // values a chunk
-template <typename T> constexpr int kStep = kStepBytes / (int)sizeof(T);  // k a step
 
-// 16 zero bytes in device memory: what a masked lane of a DIRECT load reads.
+// 16 zero bytes in device memory: what a lane without a chunk loads.
 static __device__ __align__(16) const uint32_t zero_chunk[4] = {0, 0, 0, 0};
 
+// The first `valid` values of a chunk, zeros behind.
 template <typename T>
-__device__ __forceinline__ u32x4 load_chunk(const T* p, int valid) {
-  u32x4 v = {0, 0, 0, 0};
-  if (p == nullptr || valid <= 0) return v;
-  if (valid >= kChunk<T>) {
-    __builtin_memcpy(&v, p, 16);  // any alignment
-    return v;
+__device__ __forceinline__ u32x4 first_values(u32x4 v, int valid) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(T) == 4) {
+      v[i] = i < valid ? v[i] : 0;
+    } else {
+      v[i] = 2 * i + 1 < valid ? v[i] : 2 * i < valid ? v[i] & 0xffffu : 0;
+    }
   }
+  return v;
+}
+
+// A chunk that begins less than 16 bytes before the matrix ends.
+template <typename T>
+__device__ __forceinline__ u32x4 last_chunk(const T* p, int valid) {
   T part[kChunk<T>];
 #pragma unroll
   for (int i = 0; i < kChunk<T>; ++i) part[i] = i < valid ? p[i] : (T)0.0f;
+  u32x4 v;
   __builtin_memcpy(&v, part, 16);
   return v;
 }
 
-__device__ __forceinline__ void direct_chunk(const void* src, char* lds_wave_base) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                   (__attribute__((address_space(3))) void*)lds_wave_base, 16, 0, 0);
+// 16 bytes from each lane's `src` to lane-consecutive places from `lds_wave_base` on (the same in all lanes).  Written as a
+// statement of its own, without results: the compiler, which would wait for every such load before the next turned read of
+// local memory, counts none of them, and arrived() below does.
+__device__ __forceinline__ void direct_chunk(const void* src, const char* lds_wave_base) {
+  const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)lds_wave_base);
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // m0 is a reserved register: nothing is kept in it
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(src) : "memory", "m0");
+#pragma clang diagnostic pop
 }
 
 // How the 16-byte chunks of a column operand's row k are permuted (R columns a row).
@@ -75,84 +96,147 @@ __device__ __forceinline__ int column_swizzle(int k) {
 
 // ---------------------------------------------------------------- operands
 
-// Rows are m or n, k along memory.  rows(r): address of row r (k = 0), or null.
-template <typename T, int R, int NT, bool DIRECT>
+// Rows are m or n, k along memory.
+template <typename T, int R, int NT, bool DIRECT, int KB>
 struct RowOperand {
-  static constexpr int kSlots = R * 8;
+  static constexpr int kStep = KB / (int)sizeof(T);
+  static constexpr int kRowChunks = KB / 16;
+  static constexpr int kSlots = R * kRowChunks;
   static constexpr int kPer = (kSlots + NT - 1) / NT;
-  static constexpr int kBytes = R * kStepBytes;
-  static constexpr bool kColumns = false;
-  static constexpr int kRows = R;
-  const T* row[kPer];
+  static constexpr int kBytes = R * KB;
+  static constexpr int kReads = 1;  // a fragment
+  const T* row[kPer];  // DIRECT: of the chunk that is loaded next
+  const T* end;
   u32x4 reg[DIRECT ? 1 : kPer];
   int k_of, k_end;
+
+  // How the chunks of row r are permuted: rows of 128 bytes by three of its bits, two rows of 64 bytes alike.
+  __device__ __forceinline__ static int swizzle(int r) { return KB == 128 ? r & 7 : (r >> 1) & 3; }
+  static_assert(KB == 128 || KB == 64, "");
+  static_assert(NT / kRowChunks % 8 == 0, "a thread's chunks lie in the same place of their rows");
 
   template <class Rows>
   __device__ __forceinline__ void init(const Rows& rows, int r0, int /*limit*/, int k0, int k1) {
     const int t = threadIdx.x;
-    k_of = k0 + ((t & 7) ^ ((t >> 3) & 7)) * kChunk<T>;
+    k_of = k0 + (t % kRowChunks ^ swizzle(t / kRowChunks)) * kChunk<T>;
     k_end = k1;
+    end = rows.end;
+    int id[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) id[i] = i * NT + t < kSlots ? rows.fetch(r0 + (i * NT + t) / kRowChunks) : -1;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int s = i * NT + t;
-      row[i] = s < kSlots ? rows(r0 + (s >> 3)) : nullptr;
+      row[i] = i * NT + t < kSlots ? rows.at(r0 + (i * NT + t) / kRowChunks, id[i]) : nullptr;
+      if (DIRECT) row[i] = (row[i] != nullptr ? row[i] : rows.base) + k_of;
     }
+  }
+  // DIRECT: the i'th of a step's chunks (WHOLE: of a step that no limit cuts); after the last, `advance`.
+  template <bool WHOLE, class Rows>
+  __device__ __forceinline__ void load_one(const Rows&, char* stage, int i) {
+    const int t = threadIdx.x;
+    if (kSlots % NT != 0 && i * NT + t >= kSlots) return;
+    if (WHOLE || k_of < k_end) {
+      direct_chunk(row[i], stage + (i * NT + (t & ~63)) * 16);
+    } else {
+      *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
+    }
+    row[i] += kStep;
+  }
+  template <class Rows>
+  __device__ __forceinline__ void advance(const Rows&) {
+    k_of += kStep;
   }
   template <class Rows>
   __device__ __forceinline__ void load(const Rows&, char* stage) {
     const int t = threadIdx.x;
+    if constexpr (DIRECT) {
+      if (k_of < k_end) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (kSlots % NT != 0 && i * NT + t >= kSlots) break;
-      if constexpr (DIRECT) {
-        const void* p = row[i] != nullptr && k_of < k_end ? (const void*)(row[i] + k_of) : (const void*)zero_chunk;
-        direct_chunk(p, stage + (i * NT + (t & ~63)) * 16);
+        for (int i = 0; i < kPer; ++i) {
+          if (kSlots % NT != 0 && i * NT + t >= kSlots) break;
+          direct_chunk(row[i], stage + (i * NT + (t & ~63)) * 16);
+          row[i] += kStep;
+        }
       } else {
-        reg[i] = load_chunk<T>(row[i] == nullptr ? nullptr : row[i] + k_of, k_end - k_of);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          if (kSlots % NT != 0 && i * NT + t >= kSlots) break;
+          *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
+        }
+      }
+    } else {
+      bool cut = false;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const bool any = row[i] != nullptr && k_of < k_end;
+        const bool fits = any && row[i] + k_of + kChunk<T> <= end;
+        const void* p = fits ? (const void*)(row[i] + k_of) : (const void*)zero_chunk;
+        __builtin_memcpy(&reg[i], p, 16);
+        cut |= any && !fits;
+      }
+      if (cut) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (row[i] != nullptr && k_of < k_end && row[i] + k_of + kChunk<T> > end) reg[i] = last_chunk<T>(row[i] + k_of, k_end - k_of);
       }
     }
-    k_of += kStep<T>;
+    k_of += kStep;
   }
   __device__ __forceinline__ void store(char* stage) {
     if constexpr (!DIRECT) {
       const int t = threadIdx.x;
+      const int valid = k_end - (k_of - kStep);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         if (kSlots % NT != 0 && i * NT + t >= kSlots) break;
-        *(u32x4*)(stage + (i * NT + t) * 16) = reg[i];
+        *(u32x4*)(stage + (i * NT + t) * 16) = valid < kChunk<T> ? first_values<T>(reg[i], valid) : reg[i];
       }
     }
   }
-  // Values of rows r0 .. r0 + 15 for the part'th half of the step: lane l holds row l mod 16; k as both operands order it.
-  __device__ __forceinline__ static typename Traits<T>::Frag frag(const char* stage, int r0, int part) {
-    const int l = threadIdx.x & 63;
-    const int r = r0 + (l & 15);
-    const int c = ((l >> 4) + 4 * part) ^ (r & 7);
-    return *(const typename Traits<T>::Frag*)(stage + r * kStepBytes + c * 16);
+  // Where a wavefront whose rows begin at r0 (a multiple of 16) reads: lane l holds row l mod 16 of a block of 16 and 16 bytes
+  // of k.  Blocks lie a constant distance apart, since the permutation hangs on a row's low three bits alone.
+  template <int BLOCKS>
+  struct Lanes {
+    int at[KB / 64];
+    __device__ __forceinline__ explicit Lanes(int r0) {
+      const int l = threadIdx.x & 63;
+#pragma unroll
+      for (int part = 0; part < KB / 64; ++part) at[part] = (r0 + (l & 15)) * KB + (((l >> 4) + 4 * part) ^ swizzle(l & 15)) * 16;
+    }
+  };
+  // The block'th 16 rows for the part'th half of the step; k as both operands order it.
+  template <int BLOCKS>
+  __device__ __forceinline__ static typename Traits<T>::Frag frag(const char* stage, const Lanes<BLOCKS>& lanes, int block, int part) {
+    return *(const typename Traits<T>::Frag*)(stage + lanes.at[part] + block * 16 * KB);
   }
 };
 
-// Rows are k, m or n along memory.  rows(k): address of row k (column 0), or null.
-template <typename T, int R, int NT, bool DIRECT>
+// Rows are k, m or n along memory.
+template <typename T, int R, int NT, bool DIRECT, int KB>
 struct ColumnOperand {
-  static constexpr int kSlots = R * 8;
+  static constexpr int kStep = KB / (int)sizeof(T);
+  static constexpr int kSlots = R * (KB / 16);
   static constexpr int kPer = (kSlots + NT - 1) / NT;
-  static constexpr int kBytes = R * kStepBytes;
+  static constexpr int kBytes = R * KB;
   static constexpr int kChunks = R / kChunk<T>;  // a row
-  static constexpr bool kColumns = true;
-  static constexpr int kRows = R;
-  const T* row[kPer];  // of the step that is loaded next
+  static constexpr int kReads = sizeof(T) == 2 ? 2 : 4;
+  static_assert(kSlots % NT == 0, "every thread has as many chunks");
+  int id[kPer];  // of the step that is loaded next
+  const T* here[DIRECT ? kPer : 1];  // DIRECT and rows a constant distance apart: the chunk that is loaded next
   u32x4 reg[DIRECT ? 1 : kPer];
   int k_at, k_end, c0, lim;
 
+  __device__ __forceinline__ static int slot_k(int i) { return (i * NT + (int)threadIdx.x) / kChunks; }
+  __device__ __forceinline__ int slot_column(int i) const {
+    const int s = i * NT + (int)threadIdx.x;
+    return c0 + ((s % kChunks) ^ column_swizzle<T, R>(s / kChunks)) * kChunk<T>;
+  }
   template <class Rows>
-  __device__ __forceinline__ void find(const Rows& rows) {
-    const int t = threadIdx.x;
+  __device__ __forceinline__ void fetch(const Rows& rows) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int s = i * NT + t;
-      const int k = k_at + s / kChunks;
-      row[i] = s < kSlots && k < k_end ? rows(k) : nullptr;
+      const int k = k_at + slot_k(i);
+      id[i] = k < k_end ? rows.fetch(k) : -1;
     }
   }
   template <class Rows>
@@ -161,58 +245,125 @@ struct ColumnOperand {
     k_end = k1;
     c0 = col0;
     lim = limit;
-    find(rows);
+    fetch(rows);
+    if constexpr (DIRECT && Rows::kEven) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) here[i] = rows.base + (int64_t)(k_at + slot_k(i)) * rows.ld + direct_column(i);
+    }
+  }
+  // Any column that exists stands in for one past the limit.
+  __device__ __forceinline__ int direct_column(int i) const {
+    const int c = slot_column(i);
+    return c < lim ? c : lim - kChunk<T>;
+  }
+  // DIRECT: the i'th of a step's chunks (WHOLE: of a step that no limit cuts); after the last, `advance`.
+  template <bool WHOLE, class Rows>
+  __device__ __forceinline__ void load_one(const Rows& rows, char* stage, int i) {
+    static_assert(DIRECT && Rows::kEven, "");
+    const int t = threadIdx.x;
+    if (WHOLE || k_at + slot_k(i) < k_end) {
+      direct_chunk(here[i], stage + (i * NT + (t & ~63)) * 16);
+    } else {
+      *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
+    }
+    here[i] += (int64_t)kStep * rows.ld;
+  }
+  template <class Rows>
+  __device__ __forceinline__ void advance(const Rows&) {
+    k_at += kStep;
   }
   template <class Rows>
   __device__ __forceinline__ void load(const Rows& rows, char* stage) {
     const int t = threadIdx.x;
+    if constexpr (DIRECT) {
+      if (Rows::kEven && k_at + kStep <= k_end) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int s = i * NT + t;
-      if (kSlots % NT != 0 && s >= kSlots) break;
-      const int c = c0 + ((s % kChunks) ^ column_swizzle<T, R>(s / kChunks)) * kChunk<T>;
-      if constexpr (DIRECT) {
-        const void* p = row[i] != nullptr && c < lim ? (const void*)(row[i] + c) : (const void*)zero_chunk;
-        direct_chunk(p, stage + (i * NT + (t & ~63)) * 16);
+        for (int i = 0; i < kPer; ++i) {
+          direct_chunk(here[i], stage + (i * NT + (t & ~63)) * 16);
+          here[i] += (int64_t)kStep * rows.ld;
+        }
       } else {
-        reg[i] = load_chunk<T>(row[i] == nullptr ? nullptr : row[i] + c, lim - c);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const int k = k_at + slot_k(i);
+          const T* row = k < k_end ? rows.at(k, id[i]) : nullptr;
+          if (row != nullptr) {
+            direct_chunk(row + direct_column(i), stage + (i * NT + (t & ~63)) * 16);
+          } else {
+            *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
+          }
+        }
+      }
+    } else {
+      const T* p[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int k = k_at + slot_k(i), c = slot_column(i);
+        const T* row = k < k_end && c < lim ? rows.at(k, id[i]) : nullptr;
+        p[i] = row != nullptr ? row + c : nullptr;
+      }
+      bool cut = false;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const bool fits = p[i] != nullptr && p[i] + kChunk<T> <= rows.end;
+        const void* q = fits ? (const void*)p[i] : (const void*)zero_chunk;
+        __builtin_memcpy(&reg[i], q, 16);
+        cut |= p[i] != nullptr && !fits;
+      }
+      if (cut) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+          if (p[i] != nullptr && p[i] + kChunk<T> > rows.end) reg[i] = last_chunk<T>(p[i], lim - slot_column(i));
       }
     }
-    k_at += kStep<T>;
-    find(rows);
+    k_at += kStep;
+    fetch(rows);
   }
   __device__ __forceinline__ void store(char* stage) {
     if constexpr (!DIRECT) {
       const int t = threadIdx.x;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        if (kSlots % NT != 0 && i * NT + t >= kSlots) break;
-        *(u32x4*)(stage + (i * NT + t) * 16) = reg[i];
+        const int valid = lim - slot_column(i);
+        *(u32x4*)(stage + (i * NT + t) * 16) = valid < kChunk<T> ? first_values<T>(reg[i], valid) : reg[i];
       }
     }
   }
-  __device__ __forceinline__ static typename Traits<T>::Frag frag(const char* stage, int r0, int part) {
-    const int l = threadIdx.x & 63;
-    constexpr int row_bytes = R * (int)sizeof(T);
+  // Here the permutation reaches the bits that tell blocks apart, and an offset a block is kept; it hangs on neither the
+  // half nor the reads of a fragment.
+  static constexpr int kRowBytes = R * (int)sizeof(T);
+  template <int BLOCKS>
+  struct Lanes {
+    int at[BLOCKS];
+    __device__ __forceinline__ explicit Lanes(int r0) {
+      const int l = threadIdx.x & 63, j = l & 15;
+#pragma unroll
+      for (int i = 0; i < BLOCKS; ++i) {
+        if (sizeof(T) == 2) {
+          // lane j of a group of 16 addresses row j / 4, values 4 (j mod 4) .. + 3, and receives column j of the four rows
+          const int k = (l >> 4) * 8 + (j >> 2), c = (r0 + 16 * i) / 8 + ((j & 3) >> 1);
+          at[i] = k * kRowBytes + (c ^ column_swizzle<T, R>(k)) * 16 + (j & 1) * 8;
+        } else {
+          const int k = (l >> 4) * 4, c = (r0 + 16 * i + j) / 4;
+          at[i] = k * kRowBytes + (c ^ column_swizzle<T, R>(k)) * 16 + (j & 3) * 4;
+        }
+      }
+    }
+  };
+  template <int BLOCKS>
+  __device__ __forceinline__ static typename Traits<T>::Frag frag(const char* stage, const Lanes<BLOCKS>& lanes, int block, int part) {
     typename Traits<T>::Frag f;
+    const char* a = stage + lanes.at[block];
     if constexpr (sizeof(T) == 2) {
-      // lane j of a group of 16 addresses row j / 4, values 4 (j mod 4) .. + 3, and receives column j of the four rows
-      const int j = l & 15;
-      const int c = r0 / 8 + ((j & 3) >> 1);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int k = part * 32 + (l >> 4) * 8 + h * 4 + (j >> 2);
-        const char* a = stage + k * row_bytes + (c ^ column_swizzle<T, R>(k)) * 16 + (j & 1) * 8;
-        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)a);
+        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(a + (part * 32 + h * 4) * kRowBytes));
         __builtin_memcpy((char*)&f + h * 8, &v, 8);
       }
     } else {
-      const int c = (r0 + (l & 15)) / 4, w = l & 3;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int k = part * 16 + (l >> 4) * 4 + i;
-        f[i] = *(const float*)(stage + k * row_bytes + (c ^ column_swizzle<T, R>(k)) * 16 + w * 4);
-      }
+      for (int i = 0; i < 4; ++i) f[i] = *(const float*)(a + (part * 16 + i) * kRowBytes);
     }
     return f;
   }
@@ -232,16 +383,59 @@ __device__ __forceinline__ f32x4 mma(f32x4 rows, f32x4 cols, f32x4 acc) {
 // BM x BN values by WM x WN wavefronts.  A lane's four values of the 16 x 16 block (i, j) of its wavefront:
 //   N_INNER: m = 16 i + lane mod 16, n = 16 j + 4 (lane / 16) + 0..3   (rows of an output along n)
 //   else:    n = 16 j + lane mod 16, m = 16 i + 4 (lane / 16) + 0..3   (columns of an output along m)
-template <typename T_, int BM_, int BN_, int WM_, int WN_, bool DIRECT_>
+// DEEP (DIRECT only): steps of 64 bytes of k and four stages instead of 128 bytes and two.
+template <typename T_, int BM_, int BN_, int WM_, int WN_, bool DIRECT_, bool DEEP_ = false>
 struct Shape {
   typedef T_ T;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NT = WM_ * WN_ * 64;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
-  static constexpr bool DIRECT = DIRECT_;
-  static constexpr int kStageBytes = (BM + BN) * kStepBytes;
-  static constexpr int kLdsBytes = 2 * kStageBytes;
+  static constexpr bool DIRECT = DIRECT_, DEEP = DEEP_;
+  static constexpr int KB = DEEP ? 64 : 128, kStep = KB / (int)sizeof(T), kStages = DEEP ? 4 : 2;
+  static constexpr int kStageBytes = (BM + BN) * KB;
+  static constexpr int kLdsBytes = kStages * kStageBytes;
   static_assert(TM >= 1 && TN >= 1 && BM % (WM * 16) == 0 && BN % (WN * 16) == 0, "whole 16 x 16 blocks");
+  static_assert(DIRECT || !DEEP, "");
+  typedef RowOperand<T, BM, NT, DIRECT, KB> RowsA;
+  typedef RowOperand<T, BN, NT, DIRECT, KB> RowsB;
+  typedef ColumnOperand<T, BM, NT, DIRECT, KB> ColumnsA;
+  typedef ColumnOperand<T, BN, NT, DIRECT, KB> ColumnsB;
 };
+
+// All chunks that this wavefront has asked for, but for the LATER last ones, have arrived and its reads are done; then
+// everyone's.
+template <int LATER>
+__device__ __forceinline__ void arrived() {
+  static_assert(LATER < 64, "the counter's six bits");
+  // (the builtin, not an asm statement: the compiler then knows that nothing is outstanding, scalar loads among it, and
+  // waits for single reads afterwards, where it would wait for all)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((LATER & 15) | 7 << 4 | (LATER >> 4) << 14);  // vmcnt(LATER) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Nothing is moved across: reads and products stay in the order they are written in.  (Left to itself the compiler reads
+// just before it multiplies, and waits.)
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+template <int I>
+struct Int {
+  static constexpr int value = I;
+};
+template <int I, int END, class F>
+__device__ __forceinline__ void for_blocks(const F& f) {
+  if constexpr (I < END) {
+    f(Int<I>{});
+    for_blocks<I + 1, END>(f);
+  }
+}
+
+// The second half's column fragments that are read before a row block: all of them in the first half, evenly.
+template <class S>
+constexpr int columns_before(int block) {
+  return block >= S::TM ? S::TN : (block * S::TN + S::TM - 1) / S::TM;
+}
 
 template <class S, bool N_INNER, class A, class B, class RowsA, class RowsB, class Also>
 __device__ __forceinline__ void tile_product(char* lds, A& a, B& b, const RowsA& rows_a, const RowsB& rows_b, int k0, int k1,
@@ -253,54 +447,187 @@ __device__ __forceinline__ void tile_product(char* lds, A& a, B& b, const RowsA&
   for (int i = 0; i < S::TM; ++i)
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int steps = (k1 - k0 + kStep<typename S::T> - 1) / kStep<typename S::T>;
+  const int steps = (k1 - k0 + S::kStep - 1) / S::kStep;
   if (steps <= 0) return;
 
-  auto multiply = [&](const char* stage) {
+  const typename A::template Lanes<S::TM> lanes_a(m0);
+  const typename B::template Lanes<S::TN> lanes_b(n0);
+  // A step is TM row blocks of 16 x (16 TN) for each 64 bytes of k.  The fragment of a block's rows is read two blocks ahead,
+  // those of its columns a turn of TM blocks ahead: 2 TN + 4 fragments are held, where two whole turns would be 2 (TN + TM)
+  // and take more registers than 256 x 256 tiles leave.
+  static_assert(S::TM == 2 || S::TM % 4 == 0, "four fragments in turn, two blocks ahead");
+  Frag fa[4], fb[2][S::TN];
+  auto read_rows = [&](const char* stage, int part, int i, int slot) { fa[slot & 3] = A::frag(stage, lanes_a, i, part); };
+  auto read_columns = [&](const char* stage, int part, int j, int turn) {
+    fb[turn][j] = B::frag(stage + A::kBytes, lanes_b, j, part);
+  };
+  auto multiply = [&](int i, int slot, int turn) {
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-      Frag fa[S::TM], fb[S::TN];
-#pragma unroll
-      for (int i = 0; i < S::TM; ++i) fa[i] = A::frag(stage, m0 + 16 * i, part);
-#pragma unroll
-      for (int j = 0; j < S::TN; ++j) fb[j] = B::frag(stage + A::kBytes, n0 + 16 * j, part);
-#pragma unroll
-      for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-        for (int j = 0; j < S::TN; ++j)
-          acc[i][j] = N_INNER ? mma(fb[j], fa[i], acc[i][j]) : mma(fa[i], fb[j], acc[i][j]);
-      also(fa, fb);
-    }
+    for (int j = 0; j < S::TN; ++j)
+      acc[i][j] = N_INNER ? mma(fb[turn][j], fa[slot & 3], acc[i][j]) : mma(fa[slot & 3], fb[turn][j], acc[i][j]);
+    also(i, fa[slot & 3]);
   };
 
-  a.load(rows_a, lds);
-  b.load(rows_b, lds + A::kBytes);
-  if constexpr (!S::DIRECT) {
-    a.store(lds);
-    b.store(lds + A::kBytes);
-  }
-  for (int s = 0; s < steps; ++s) {
-    char* here = lds + (s & 1) * S::kStageBytes;
-    char* next = lds + ((s + 1) & 1) * S::kStageBytes;
-    if constexpr (S::DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wavefront's chunks have arrived
-    __syncthreads();  // everyone's have, and everyone has read the other stage
-    if (s + 1 < steps) {
-      a.load(rows_a, next);
-      b.load(rows_b, next + A::kBytes);
+  if constexpr (S::DEEP) {
+    // A turn is a step.  Its stage is given up two blocks before the turn ends, when all of it has been read; the step four
+    // turns ahead goes there, a chunk at a time between the next turn's blocks: eight wavefronts that ask for all their chunks
+    // at once wait for the address units before they can go on to multiply.  (With two stages of twice the length a chunk
+    // would have to be on its way before the next turn.)  Turns go in pairs, so that the fragments' places are known to the
+    // compiler; an odd number is filled up with zeros.
+    constexpr int per = A::kPer + B::kPer;
+    const int full = ((a.k_end < b.k_end ? a.k_end : b.k_end) - k0) / S::kStep;  // steps whose every chunk is loaded
+    const int turns = (steps + 1) / 2 * 2;
+    auto load_one = [&](auto whole, int step, int i) {
+      char* to = lds + (step & 3) * S::kStageBytes;
+      if (i < A::kPer) {
+        a.template load_one<decltype(whole)::value>(rows_a, to, i);
+      } else {
+        b.template load_one<decltype(whole)::value>(rows_b, to + A::kBytes, i - A::kPer);
+      }
+    };
+    auto load = [&](int step) {
+#pragma unroll
+      for (int i = 0; i < per; ++i) load_one(Int<0>{}, step, i);
+      a.advance(rows_a);
+      b.advance(rows_b);
+    };
+    auto first_reads = [&](const char* stage, int turn) {
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) read_columns(stage, 0, j, turn);
+      read_rows(stage, 0, 0, 0);
+      in_order();
+      read_rows(stage, 0, 1, 1);
+    };
+    // WHOLE: the step that is loaded in this turn has no limit in it.
+    auto one_turn = [&](auto whole, auto which, int at_turn) {
+      constexpr int turn = decltype(which)::value;
+      const char* here = lds + (at_turn & 3) * S::kStageBytes;
+      const char* next = lds + ((at_turn + 1) & 3) * S::kStageBytes;
+      const bool more = decltype(whole)::value || at_turn + 3 < turns;
+      for_blocks<0, S::TM - 2>([&](auto at) {
+        constexpr int i = decltype(at)::value;
+        read_rows(here, 0, i + 2, i + 2);
+        in_order();
+        multiply(i, i, turn);
+        in_order();
+        if (more) {
+#pragma unroll
+          for (int k = i * per / (S::TM - 2); k < (i + 1) * per / (S::TM - 2); ++k) load_one(whole, at_turn + 3, k);
+        }
+        in_order();
+      });
+      if (more) {
+        a.advance(rows_a);
+        b.advance(rows_b);
+      }
+      // The next step is there; the two behind it may be on their way.
+      if (decltype(whole)::value) {
+        arrived<2 * per>();
+      } else {
+        arrived<0>();
+      }
+      first_reads(next, 1 - turn);  // (of whatever is there after the last step)
+      in_order();
+      multiply(S::TM - 2, S::TM - 2, turn);
+      multiply(S::TM - 1, S::TM - 1, turn);
+      in_order();
+    };
+    load(0);
+    load(1);
+    if (turns > 2) load(2);
+    if (full > 2) {
+      arrived<2 * per>();
+    } else {
+      arrived<0>();
     }
-    multiply(here);
-    if constexpr (!S::DIRECT) {
-      if (s + 1 < steps) {
-        a.store(next);
-        b.store(next + A::kBytes);
+    first_reads(lds, 0);
+    int s = 0;
+    for (; s + 4 < full; s += 2) {
+      one_turn(Int<1>{}, Int<0>{}, s);
+      one_turn(Int<1>{}, Int<1>{}, s + 1);
+    }
+    for (; s < turns; s += 2) {
+      one_turn(Int<0>{}, Int<0>{}, s);
+      one_turn(Int<0>{}, Int<1>{}, s + 1);
+    }
+  } else {
+    // Two turns a step.
+    auto first_reads = [&](const char* stage) {
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) read_columns(stage, 0, j, 0);
+      read_rows(stage, 0, 0, 0);
+      in_order();
+      read_rows(stage, 0, 1, 1);
+    };
+    // All blocks but the last two, whose fragments have been read by then.
+    constexpr int blocks = 2 * S::TM;
+    auto most_blocks = [&](const char* stage) {
+      for_blocks<0, blocks - 2>([&](auto at) {
+        constexpr int block = decltype(at)::value;
+        constexpr int columns = columns_before<S>(block + 1) - columns_before<S>(block);
+        read_rows(stage, (block + 2) / S::TM, (block + 2) % S::TM, block + 2);
+#pragma unroll
+        for (int j = 0; j < columns; ++j) read_columns(stage, 1, columns_before<S>(block) + j, 1);
+        in_order();
+        multiply(block % S::TM, block, block / S::TM);
+        in_order();
+      });
+    };
+    a.load(rows_a, lds);
+    b.load(rows_b, lds + A::kBytes);
+    if constexpr (S::DIRECT) {
+      // A stage is given up two blocks before its step ends, when all of it has been read, and the step after the next goes
+      // there: one barrier a step is enough, and the last two blocks cover the first reads of the next stage.
+      arrived<0>();
+      if (steps > 1) {
+        a.load(rows_a, lds + S::kStageBytes);
+        b.load(rows_b, lds + S::kStageBytes + A::kBytes);
+      }
+      first_reads(lds);
+      for (int s = 0; s < steps; ++s) {
+        char* here = lds + (s & 1) * S::kStageBytes;
+        char* next = lds + ((s + 1) & 1) * S::kStageBytes;
+        most_blocks(here);
+        arrived<0>();
+        first_reads(next);  // (of whatever is there after the last step)
+        in_order();
+        multiply(S::TM - 2, blocks - 2, 1);
+        in_order();
+        if (s + 2 < steps) {
+          a.load(rows_a, here);
+          b.load(rows_b, here + A::kBytes);
+        }
+        in_order();
+        multiply(S::TM - 1, blocks - 1, 1);
+        in_order();
+      }
+    } else {
+      a.store(lds);
+      b.store(lds + A::kBytes);
+      for (int s = 0; s < steps; ++s) {
+        char* here = lds + (s & 1) * S::kStageBytes;
+        char* next = lds + ((s + 1) & 1) * S::kStageBytes;
+        __syncthreads();  // everyone has written this stage and read the other
+        if (s + 1 < steps) {
+          a.load(rows_a, next);
+          b.load(rows_b, next + A::kBytes);
+        }
+        first_reads(here);
+        most_blocks(here);
+        multiply(S::TM - 2, blocks - 2, 1);
+        multiply(S::TM - 1, blocks - 1, 1);
+        if (s + 1 < steps) {
+          a.store(next);
+          b.store(next + A::kBytes);
+        }
       }
     }
   }
 }
 
 struct Nothing {
-  template <class FA, class FB>
-  __device__ __forceinline__ void operator()(const FA&, const FB&) const {}
+  template <class F>
+  __device__ __forceinline__ void operator()(int, const F&) const {}
 };
 
 // ---------------------------------------------------------------- results
