@@ -178,7 +178,9 @@ int score_grid(gbdt_softmax::ScoreArgs<T>& g, unsigned* blocks) {
   g.group = group_of(S::BM, g.dim, sizeof(T));
   const int64_t n = (int64_t)g.row_tiles * g.col_tiles;
   if (n > kMaxBlocks || (int64_t)g.group * g.col_tiles > kMaxBlocks) return GBDT_EUNSUPPORTED;
-  *blocks = (unsigned)n;
+  // One workgroup a compute unit goes through the tiles where there is no room for two; else one a tile.
+  const int64_t units = std::max(8, gbdt_internal::cu_count() / 8 * 8);
+  *blocks = (unsigned)(S::DEEP ? std::min(n, units) : n);
   return GBDT_OK;
 }
 

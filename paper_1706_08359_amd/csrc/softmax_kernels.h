@@ -64,8 +64,8 @@ struct ScoreArgs {
 // A tile's place: `group` row tiles side by side go through all column tiles before the next ones do, so that what runs at
 // the same time on an XCD shares both operands in its L2.
 template <typename Args>
-__device__ __forceinline__ void tile_place(const Args& g, uint32_t* row, uint32_t* col) {
-  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
+__device__ __forceinline__ void tile_place(const Args& g, uint32_t tile, uint32_t* row, uint32_t* col) {
+  const uint32_t t = xcd_tile(tile, g.row_tiles * g.col_tiles);
   const uint32_t span = g.group * g.col_tiles;
   const uint32_t first = t / span * g.group;
   const uint32_t rows = g.row_tiles - first < g.group ? g.row_tiles - first : g.group;
@@ -73,77 +73,115 @@ __device__ __forceinline__ void tile_place(const Args& g, uint32_t* row, uint32_
   *col = t % span / rows;
 }
 
-template <class S, bool N_INNER, typename T>
-__device__ __forceinline__ void scores_tile(char* lds, const ScoreArgs<T>& g, int row0, int col0, f32x4 (&acc)[S::TM][S::TN]) {
+// The scores of one tile after another (the grid is a multiple of 8, or one workgroup a tile: a workgroup's tiles are its
+// XCD's), each handed to `use` with what `fetch` read for its rows and its first row and class.  The next tile's first steps
+// are on their way while `use` works; `fetch` comes before them, since loads are waited for in order.
+template <class S, bool N_INNER, typename T, class Fetch, class Use>
+__device__ __forceinline__ void for_score_tiles(char* lds, const ScoreArgs<T>& g, const Fetch& fetch, const Use& use) {
   const PlainRows<T> rows_a = plain_rows(g.h, g.ld_h, g.n_rows, g.dim);
   const PlainRows<T> rows_b = plain_rows(g.c, g.ld_c, g.end, g.dim);
   typename S::RowsA a;
   typename S::RowsB b;
-  a.init(rows_a, row0, 0, 0, g.dim);
-  b.init(rows_b, col0, 0, 0, g.dim);
-  tile_product<S, N_INNER>(lds, a, b, rows_a, rows_b, 0, g.dim, acc, Nothing{});
+  const uint32_t tiles = g.row_tiles * g.col_tiles;
+  int row0, col0;
+  auto begin = [&](uint32_t tile) {
+    uint32_t tr, tc;
+    tile_place(g, tile, &tr, &tc);
+    row0 = (int)tr * S::BM;
+    col0 = g.begin + (int)tc * S::BN;
+    a.init(rows_a, row0, 0, 0, g.dim);
+    b.init(rows_b, col0, 0, 0, g.dim);
+    tile_begin<S>(lds, a, b, rows_a, rows_b, 0, g.dim);
+  };
+  uint32_t tile = blockIdx.x;
+  begin(tile);
+  for (;;) {
+    f32x4 acc[S::TM][S::TN];
+    tile_run<S, N_INNER>(lds, a, b, rows_a, rows_b, 0, g.dim, acc, Nothing{});
+    const int row = row0, col = col0;
+    const auto of_rows = fetch(row);
+    const uint32_t next = tile + gridDim.x;
+    if (next < tiles) begin(next);
+    use(acc, of_rows, row, col);
+    if (next >= tiles) return;
+    tile = next;
+  }
 }
+
+// What an epilogue needs of the rows of its lane's blocks; all of it is asked for at once (one at a time, block by block, it
+// cost more than everything else behind the products).  Rows past the last stand for an ignored one.
+template <class S>
+struct OfRows {
+  int y[S::TM];
+  float lse[S::TM], weight[S::TM];
+};
 
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) softmax_scores_kernel(const ScoreArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  uint32_t tr, tc;
-  tile_place(g, &tr, &tc);
-  const int row0 = (int)tr * S::BM, col0 = (int)tc * S::BN;
-  f32x4 acc[S::TM][S::TN];
-  scores_tile<S, true>(lds, g, row0, col0, acc);
+  // [128 classes: their wavefronts' lane groups][row]: the maximum and the sum of a lane's 4 TN values of a row
+  __shared__ MaxSum lane_parts[S::WN * 4 * S::BM];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int m0 = (w / S::WN) * (S::TM * 16), n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
-  MaxSum* row_parts = (MaxSum*)lds;  // [WN][BM]
-  __syncthreads();                   // the stages have been read
+  const int m0 = (w / S::WN) * (S::TM * 16) + (l & 15), wave_n = (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+  MaxSum* mine = lane_parts + (w % S::WN * 4 + (l >> 4)) * S::BM;
+  auto fetch = [&](int row0) {
+    OfRows<S> f;
 #pragma unroll
-  for (int i = 0; i < S::TM; ++i) {
-    const int m = m0 + 16 * i + (l & 15);
-    const int d = row0 + m;
-    const int y = g.labels && d < g.n_rows ? g.labels[d] : -1;
+    for (int i = 0; i < S::TM; ++i) {
+      const int d = row0 + m0 + 16 * i;
+      f.y[i] = g.labels ? g.labels[d < g.n_rows ? d : g.n_rows - 1] : -1;
+    }
+    return f;
+  };
+  for_score_tiles<S, true>(lds, g, fetch, [&](f32x4(&acc)[S::TM][S::TN], const OfRows<S>& f, int row0, int col0) {
+    const int n0 = col0 + wave_n;
     if (col0 + S::BN > g.end) {  // classes past the last add nothing to either
 #pragma unroll
+      for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[i][j][r] = n0 + 16 * j + r < g.end ? acc[i][j][r] : -__builtin_inff();
+    }
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+      float top = acc[i][0][0];
+#pragma unroll
       for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[i][j][r] = n0 + 16 * j + r < g.end ? acc[i][j][r] : -__builtin_inff();
-    }
-    const int rel = y - n0;  // rarely here
-    if (rel >= 0 && rel < 16 * S::TN && (rel & 15) < 4 && y < g.end) {
-      float picked = 0.0f;
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r]);
+      const float base = base_of(top);
+      float sum = 0.0f;
 #pragma unroll
       for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) picked = rel == 16 * j + r ? acc[i][j][r] : picked;
-      g.picked[d] = picked;
+        for (int r = 0; r < 4; ++r) sum += exp_diff(acc[i][j][r], base);
+      mine[m0 + 16 * i] = {top, sum};
     }
-    float top = -__builtin_inff();
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j)
+    for (int i = 0; i < S::TM; ++i) {
+      const int rel = f.y[i] - n0, d = row0 + m0 + 16 * i;  // rarely here
+      if (rel >= 0 && rel < 16 * S::TN && (rel & 15) < 4 && f.y[i] < g.end && d < g.n_rows) {
+        float picked = 0.0f;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) top = fmaxf(top, acc[i][j][r]);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float base = base_of(top);
-    float sum = 0.0f;
+        for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j)
+          for (int r = 0; r < 4; ++r) picked = rel == 16 * j + r ? acc[i][j][r] : picked;
+        g.picked[d] = picked;
+      }
+    }
+    __syncthreads();  // (the next tile's steps, with their barriers, come before these places are written again)
+    constexpr int lanes = 4 * kPartClasses / (S::TN * 16);  // of a row in a part
+    static_assert(S::BN % kPartClasses == 0 && lanes >= 4, "tiles of whole parts");
+    for (int e = threadIdx.x; e < S::BM * (S::BN / kPartClasses); e += S::NT) {
+      const int m = e % S::BM, q = e / S::BM;
+      if (row0 + m >= g.n_rows || col0 + q * kPartClasses >= g.end) continue;
+      MaxSum p = lane_parts[q * lanes * S::BM + m];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sum += exp_diff(acc[i][j][r], base);
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (l < 16) row_parts[(w % S::WN) * S::BM + m] = {top, sum};
-  }
-  __syncthreads();
-  constexpr int waves = kPartClasses / (S::TN * 16);  // of a part
-  static_assert(S::BN % kPartClasses == 0 && waves >= 1, "tiles of whole parts");
-  for (int e = threadIdx.x; e < S::BM * (S::BN / kPartClasses); e += S::NT) {
-    const int m = e % S::BM, q = e / S::BM;
-    if (row0 + m >= g.n_rows || col0 + q * kPartClasses >= g.end) continue;
-    MaxSum p = row_parts[q * waves * S::BM + m];
-#pragma unroll
-    for (int k = 1; k < waves; ++k) p = join(p, row_parts[(q * waves + k) * S::BM + m]);
-    g.parts[((int64_t)tc * (S::BN / kPartClasses) + q) * g.n_rows + row0 + m] = p;
-  }
+      for (int k = 1; k < lanes; ++k) p = join(p, lane_parts[(q * lanes + k) * S::BM + m]);
+      g.parts[((int64_t)(col0 / kPartClasses) + q) * g.n_rows + row0 + m] = p;
+    }
+  });
 }
 
 // Joins a row's parts: 16 lanes a row, each every 16th part in order, then pairwise.
@@ -174,85 +212,99 @@ template <class S>
 __global__ void __launch_bounds__(S::NT, 2) softmax_piece_kernel(const ScoreArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  uint32_t tr, tc;
-  tile_place(g, &tr, &tc);
-  const int row0 = (int)tr * S::BM, col0 = g.begin + (int)tc * S::BN;
-  f32x4 acc[S::TM][S::TN];
-  scores_tile<S, true>(lds, g, row0, col0, acc);
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int m0 = (w / S::WN) * (S::TM * 16), n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+  const int m0 = (w / S::WN) * (S::TM * 16) + (l & 15), wave_n = (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+  auto fetch = [&](int row0) {
+    OfRows<S> f;
 #pragma unroll
-  for (int i = 0; i < S::TM; ++i) {
-    const int d = row0 + m0 + 16 * i + (l & 15);
-    if (d >= g.n_rows) continue;
-    const int y = g.labels[d];
-    const bool use = (uint32_t)y < (uint32_t)g.n_classes;
-    const float lse = g.lse[d];
-    const float weight = g.weight ? g.weight[d] : 1.0f;
-    T* to = g.g + (int64_t)d * g.ld_g - g.begin;
-    f32x4 v[S::TN];
+    for (int i = 0; i < S::TM; ++i) {
+      const int d = row0 + m0 + 16 * i, at = d < g.n_rows ? d : g.n_rows - 1;
+      f.y[i] = g.labels[at];
+      f.lse[i] = g.lse[at];
+      f.weight[i] = g.weight ? g.weight[at] : 1.0f;
+    }
+    return f;
+  };
+  for_score_tiles<S, true>(lds, g, fetch, [&](f32x4(&acc)[S::TM][S::TN], const OfRows<S>& f, int row0, int col0) {
+    const int n0 = col0 + wave_n;
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[j][r] = weight * exp_diff(acc[i][j][r], lse);
-    const int rel = y - n0;  // rarely here
-    if (rel >= 0 && rel < 16 * S::TN && (rel & 15) < 4) {
+    for (int i = 0; i < S::TM; ++i) {
+      const int d = row0 + m0 + 16 * i;
+      const int y = f.y[i];
+      const bool use = (uint32_t)y < (uint32_t)g.n_classes;
+      f32x4 v[S::TN];
 #pragma unroll
       for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[j][r] -= rel == 16 * j + r ? weight : 0.0f;
+        for (int r = 0; r < 4; ++r) v[j][r] = f.weight[i] * exp_diff(acc[i][j][r], f.lse[i]);
+      const int rel = y - n0;  // rarely here
+      if (rel >= 0 && rel < 16 * S::TN && (rel & 15) < 4) {
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[j][r] -= rel == 16 * j + r ? f.weight[i] : 0.0f;
+      }
+      if (!use || col0 + S::BN > g.end) {
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[j][r] = use && n0 + 16 * j + r < g.end ? v[j][r] : 0.0f;
+      }
+      if (d < g.n_rows) {
+        T* to = g.g + (int64_t)d * g.ld_g - g.begin + n0;
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) store4(to + 16 * j, v[j], 4);
+      }
     }
-    if (!use || col0 + S::BN > g.end) {
-#pragma unroll
-      for (int j = 0; j < S::TN; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[j][r] = use && n0 + 16 * j + r < g.end ? v[j][r] : 0.0f;
-    }
-#pragma unroll
-    for (int j = 0; j < S::TN; ++j) store4(to + n0 + 16 * j, v[j], 4);
-  }
+  });
 }
 
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) softmax_stats_kernel(const ScoreArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  uint32_t tr, tc;
-  tile_place(g, &tr, &tc);
-  const int row0 = (int)tr * S::BM, col0 = g.begin + (int)tc * S::BN;
-  f32x4 acc[S::TM][S::TN];
-  scores_tile<S, false>(lds, g, row0, col0, acc);
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int d0 = row0 + (w / S::WN) * (S::TM * 16) + 4 * (l >> 4), n0 = col0 + (w % S::WN) * (S::TN * 16) + (l & 15);
+  const int m0 = (w / S::WN) * (S::TM * 16) + 4 * (l >> 4), wave_n = (w % S::WN) * (S::TN * 16) + (l & 15);
+  struct OfFourRows {
+    float lse[S::TM][4];
+    int y[S::TM][4];
+  };
+  auto fetch = [&](int row0) {
+    OfFourRows f;
 #pragma unroll
-  for (int i = 0; i < S::TM; ++i) {
-    const int d = d0 + 16 * i;
-    if (d >= g.n_rows) continue;
-    float lse[4];
-    int y[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const bool in = d + r < g.n_rows;
-      lse[r] = in ? g.lse[d + r] : 0.0f;
-      y[r] = in && g.labels ? g.labels[d + r] : -1;
-    }
-#pragma unroll
-    for (int j = 0; j < S::TN; ++j) {
-      const int n = n0 + 16 * j;
-      if (n >= g.end) continue;
-      f32x4 grad, hess;
+    for (int i = 0; i < S::TM; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const bool use = g.labels == nullptr || (uint32_t)y[r] < (uint32_t)g.n_classes;
-        const float e = exp_diff(acc[i][j][r], lse[r]);
-        const float p = use ? e : 0.0f;
-        grad[r] = n == y[r] ? p - 1.0f : p;
-        hess[r] = p * (1.0f - p);
+        const int d = row0 + m0 + 16 * i + r, at = d < g.n_rows ? d : g.n_rows - 1;
+        f.lse[i][r] = g.lse[at];
+        f.y[i][r] = g.labels ? g.labels[at] : -1;
       }
-      const int64_t at = (int64_t)(n - g.begin) * g.ld_out + d;
-      store4(g.grad + at, grad, g.n_rows - d);
-      store4(g.hess + at, hess, g.n_rows - d);
+    return f;
+  };
+  for_score_tiles<S, false>(lds, g, fetch, [&](f32x4(&acc)[S::TM][S::TN], const OfFourRows& f, int row0, int col0) {
+    const int n0 = col0 + wave_n;
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+      const int d = row0 + m0 + 16 * i;
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) {
+        const int n = n0 + 16 * j;
+        f32x4 grad, hess;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool use = g.labels == nullptr || (uint32_t)f.y[i][r] < (uint32_t)g.n_classes;
+          const float e = exp_diff(acc[i][j][r], f.lse[i][r]);
+          const float p = use ? e : 0.0f;
+          grad[r] = n == f.y[i][r] ? p - 1.0f : p;
+          hess[r] = p * (1.0f - p);
+        }
+        if (d < g.n_rows && n < g.end) {
+          const int64_t at = (int64_t)(n - g.begin) * g.ld_out + d;
+          store4(g.grad + at, grad, g.n_rows - d);
+          store4(g.hess + at, hess, g.n_rows - d);
+        }
+      }
     }
-  }
+  });
 }
 
 // A copy whose rows are whole 16-byte chunks, filled up with zeros; rows whose label does not count (labels given) are all

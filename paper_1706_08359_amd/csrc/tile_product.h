@@ -75,11 +75,16 @@ __device__ __forceinline__ u32x4 last_chunk(const T* p, int valid) {
   return v;
 }
 
-// 16 bytes from each lane's `src` to lane-consecutive places from `lds_wave_base` on (the same in all lanes).  Written as a
+// The byte of local memory where a wavefront's first chunk of a stage goes, for scalar registers.
+__device__ __forceinline__ uint32_t wave_place(const char* stage) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)stage +
+         __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024u;
+}
+
+// 16 bytes from each lane's `src` to lane-consecutive places from byte `to` of local memory on (the same in all lanes).  Written as a
 // statement of its own, without results: the compiler, which would wait for every such load before the next turned read of
 // local memory, counts none of them, and arrived() below does.
-__device__ __forceinline__ void direct_chunk(const void* src, const char* lds_wave_base) {
-  const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)lds_wave_base);
+__device__ __forceinline__ void direct_chunk(const void* src, uint32_t to) {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"  // m0 is a reserved register: nothing is kept in it
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(src) : "memory", "m0");
@@ -136,7 +141,7 @@ struct RowOperand {
     const int t = threadIdx.x;
     if (kSlots % NT != 0 && i * NT + t >= kSlots) return;
     if (WHOLE || k_of < k_end) {
-      direct_chunk(row[i], stage + (i * NT + (t & ~63)) * 16);
+      direct_chunk(row[i], wave_place(stage) + i * NT * 16);
     } else {
       *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
     }
@@ -154,7 +159,7 @@ struct RowOperand {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
           if (kSlots % NT != 0 && i * NT + t >= kSlots) break;
-          direct_chunk(row[i], stage + (i * NT + (t & ~63)) * 16);
+          direct_chunk(row[i], wave_place(stage) + i * NT * 16);
           row[i] += kStep;
         }
       } else {
@@ -262,7 +267,7 @@ struct ColumnOperand {
     static_assert(DIRECT && Rows::kEven, "");
     const int t = threadIdx.x;
     if (WHOLE || k_at + slot_k(i) < k_end) {
-      direct_chunk(here[i], stage + (i * NT + (t & ~63)) * 16);
+      direct_chunk(here[i], wave_place(stage) + i * NT * 16);
     } else {
       *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
     }
@@ -279,7 +284,7 @@ struct ColumnOperand {
       if (Rows::kEven && k_at + kStep <= k_end) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          direct_chunk(here[i], stage + (i * NT + (t & ~63)) * 16);
+          direct_chunk(here[i], wave_place(stage) + i * NT * 16);
           here[i] += (int64_t)kStep * rows.ld;
         }
       } else {
@@ -288,7 +293,7 @@ struct ColumnOperand {
           const int k = k_at + slot_k(i);
           const T* row = k < k_end ? rows.at(k, id[i]) : nullptr;
           if (row != nullptr) {
-            direct_chunk(row + direct_column(i), stage + (i * NT + (t & ~63)) * 16);
+            direct_chunk(row + direct_column(i), wave_place(stage) + i * NT * 16);
           } else {
             *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
           }
@@ -437,9 +442,26 @@ constexpr int columns_before(int block) {
   return block >= S::TM ? S::TN : (block * S::TN + S::TM - 1) / S::TM;
 }
 
+// Asks for a tile's first steps.  tile_run must follow; a kernel may do something else with the tile before, if it leaves
+// the stages alone: load the next tile's first steps and then store this one's results.
+template <class S, class A, class B, class RowsA, class RowsB>
+__device__ __forceinline__ void tile_begin(char* lds, A& a, B& b, const RowsA& rows_a, const RowsB& rows_b, int k0, int k1) {
+  const int steps = (k1 - k0 + S::kStep - 1) / S::kStep;
+  if (steps <= 0) return;
+  // (DEEP: an even number of steps, the last of them zeros if need be)
+  constexpr int first = S::DEEP ? 3 : 1;
+  for_blocks<0, first>([&](auto at) {
+    constexpr int i = decltype(at)::value;
+    if (i < 2 || steps > 2) {
+      a.load(rows_a, lds + i * S::kStageBytes);
+      b.load(rows_b, lds + i * S::kStageBytes + A::kBytes);
+    }
+  });
+}
+
 template <class S, bool N_INNER, class A, class B, class RowsA, class RowsB, class Also>
-__device__ __forceinline__ void tile_product(char* lds, A& a, B& b, const RowsA& rows_a, const RowsB& rows_b, int k0, int k1,
-                                             f32x4 (&acc)[S::TM][S::TN], const Also& also) {
+__device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& rows_a, const RowsB& rows_b, int k0, int k1,
+                                         f32x4 (&acc)[S::TM][S::TN], const Also& also) {
   typedef typename Traits<typename S::T>::Frag Frag;
   const int w = threadIdx.x >> 6;
   const int m0 = (w / S::WN) * (S::TM * 16), n0 = (w % S::WN) * (S::TN * 16);
@@ -485,12 +507,6 @@ __device__ __forceinline__ void tile_product(char* lds, A& a, B& b, const RowsA&
         b.template load_one<decltype(whole)::value>(rows_b, to + A::kBytes, i - A::kPer);
       }
     };
-    auto load = [&](int step) {
-#pragma unroll
-      for (int i = 0; i < per; ++i) load_one(Int<0>{}, step, i);
-      a.advance(rows_a);
-      b.advance(rows_b);
-    };
     auto first_reads = [&](const char* stage, int turn) {
 #pragma unroll
       for (int j = 0; j < S::TN; ++j) read_columns(stage, 0, j, turn);
@@ -532,9 +548,6 @@ __device__ __forceinline__ void tile_product(char* lds, A& a, B& b, const RowsA&
       multiply(S::TM - 1, S::TM - 1, turn);
       in_order();
     };
-    load(0);
-    load(1);
-    if (turns > 2) load(2);
     if (full > 2) {
       arrived<2 * per>();
     } else {
@@ -573,8 +586,6 @@ __device__ __forceinline__ void tile_product(char* lds, A& a, B& b, const RowsA&
         in_order();
       });
     };
-    a.load(rows_a, lds);
-    b.load(rows_b, lds + A::kBytes);
     if constexpr (S::DIRECT) {
       // A stage is given up two blocks before its step ends, when all of it has been read, and the step after the next goes
       // there: one barrier a step is enough, and the last two blocks cover the first reads of the next stage.
@@ -623,6 +634,13 @@ __device__ __forceinline__ void tile_product(char* lds, A& a, B& b, const RowsA&
       }
     }
   }
+}
+
+template <class S, bool N_INNER, class A, class B, class RowsA, class RowsB, class Also>
+__device__ __forceinline__ void tile_product(char* lds, A& a, B& b, const RowsA& rows_a, const RowsB& rows_b, int k0, int k1,
+                                             f32x4 (&acc)[S::TM][S::TN], const Also& also) {
+  tile_begin<S>(lds, a, b, rows_a, rows_b, k0, k1);
+  tile_run<S, N_INNER>(lds, a, b, rows_a, rows_b, k0, k1, acc, also);
 }
 
 struct Nothing {
