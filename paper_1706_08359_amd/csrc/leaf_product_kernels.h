@@ -30,7 +30,7 @@ struct LeafArgs {
   int64_t ld_x, ld_dy, ld_y, ld_dx;
   int32_t n_positions, n_leaves, n_rows, d_in, d_out;
   int32_t cut;        // gradient of the weights: positions between cuts
-  uint32_t col_tiles, row_tiles;
+  uint32_t col_tiles, row_tiles, cols_per;  // cols_per: column tiles that a workgroup goes through
 };
 
 // An offset as the kernels take it: inside the list, whatever the array holds.
@@ -76,6 +76,19 @@ __device__ __forceinline__ ListRows<T> list_rows(const T* base, int64_t ld, int 
   return {base, base + (int64_t)(g.n_rows - 1) * ld + cols, ld, g.row_idx, stop, g.n_rows};
 }
 
+// The same from a copy of a part of the list in local memory, -1 where there is no row.
+template <typename T>
+struct CopiedRows {
+  static constexpr bool kEven = false;
+  const T* base;
+  const T* end;
+  int64_t ld;
+  const int* ids;
+  int32_t first;  // the position of ids[0]
+  __device__ __forceinline__ int fetch(int p) const { return ids[p - first]; }
+  __device__ __forceinline__ const T* at(int, int d) const { return d >= 0 ? base + (int64_t)d * ld : nullptr; }
+};
+
 // Rows of a matrix in order.
 template <typename T>
 struct PlainRows {
@@ -92,78 +105,79 @@ __device__ __forceinline__ PlainRows<T> plain_rows(const T* base, int64_t ld, in
   return {base, base + (int64_t)(n - 1) * ld + cols, ld, n};
 }
 
-// Writes the tile's values (N_INNER) to the rows of the list, adding bias if there is one.
+// Writes a tile's values (N_INNER) to the rows of the list, adding bias if there is one.  rows: of this lane's blocks, null
+// for none.
 template <class S, typename T>
-__device__ __forceinline__ void scatter_rows(const f32x4 (&acc)[S::TM][S::TN], const T* bias, T* out, int64_t ld, const int32_t* row_idx,
-                                             int p0, int p1, int n_rows, int col0, int cols) {
+__device__ __forceinline__ void store_rows(const f32x4 (&acc)[S::TM][S::TN], const T* bias, T* const (&rows)[S::TM], int col0, int cols) {
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int m0 = (w / S::WN) * (S::TM * 16), n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+  const int n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j) {
+    const int n = n0 + 16 * j;
+    if (n >= cols) continue;
+    f32x4 add = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (bias) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) add[r] = (float)bias[n + r < cols ? n + r : n];
+    }
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+      if (rows[i]) store4(rows[i] + n, acc[i][j] + add, cols - n);
+  }
+}
+
+// The rows of one tile of positions times a matrix of the leaf, g.cols_per column tiles one after another; the next one's
+// first steps are on their way while one's values are stored.  B: the matrix' orientation, K its length along k.
+template <class S, class B, typename T>
+__device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& g, const T* in, int64_t ld_in, int k, const T* bias_all,
+                                                  T* out, int64_t ld_out, int cols) {
+  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
+  const uint32_t turns = (g.col_tiles + g.cols_per - 1) / g.cols_per;
+  const int tile = (int)(t / turns), col_first = (int)(t % turns * g.cols_per) * S::BN;
+  const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, S::BM, tile);
+  if (leaf < 0) return;
+  const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
+  const int p0 = begin + (tile - (begin / S::BM + leaf)) * S::BM;
+  if (p0 >= end || p0 < begin) return;
+  const int col_last = cols < col_first + (int)g.cols_per * S::BN ? cols : col_first + (int)g.cols_per * S::BN;
+  const ListRows<T> rows_a = list_rows(in, ld_in, k, g, end);
+  const PlainRows<T> rows_b = plain_rows(g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out, g.d_in);
+  T* rows[S::TM];  // of the output
+  const int m0 = p0 + (threadIdx.x >> 6) / S::WN * (S::TM * 16) + (threadIdx.x & 15);
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
-    const int p = p0 + m0 + 16 * i + (l & 15);
-    if (p >= p1) continue;
-    const int d = row_idx ? row_idx[p] : p;
-    if ((uint32_t)d >= (uint32_t)n_rows) continue;
-    T* to = out + (int64_t)d * ld;
-#pragma unroll
-    for (int j = 0; j < S::TN; ++j) {
-      const int n = n0 + 16 * j;
-      f32x4 v = acc[i][j];
-      if (bias) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (n + r < cols) v[r] += (float)bias[n + r];
-      }
-      if (n < cols) store4(to + n, v, cols - n);
-    }
+    const int p = m0 + 16 * i, d = p < end ? (g.row_idx ? g.row_idx[p] : p) : -1;
+    rows[i] = (uint32_t)d < (uint32_t)g.n_rows ? out + (int64_t)d * ld_out : nullptr;
+  }
+  typename S::RowsA a;
+  B b;
+  auto begin_columns = [&](int col) {
+    a.init(rows_a, p0, 0, 0, k);
+    b.init(rows_b, col, cols, 0, k);
+    tile_begin<S>(lds, a, b, rows_a, rows_b, 0, k);
+  };
+  begin_columns(col_first);
+  for (int col = col_first; col < col_last; col += S::BN) {
+    f32x4 acc[S::TM][S::TN];
+    zeros<S>(acc);
+    tile_run<S, true>(lds, a, b, rows_a, rows_b, 0, k, acc, Nothing{});
+    if (col + S::BN < col_last) begin_columns(col + S::BN);
+    store_rows<S>(acc, bias_all ? bias_all + (int64_t)leaf * cols : nullptr, rows, col, cols);
   }
 }
 
 // y: rows of x times the leaf's rows of w, both with k = input along memory.
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_product_kernel(const LeafArgs<typename S::T> g) {
-  typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
-  const int tile = (int)(t / g.col_tiles), col0 = (int)(t % g.col_tiles) * S::BN;
-  const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, S::BM, tile);
-  if (leaf < 0) return;
-  const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
-  const int p0 = begin + (tile - (begin / S::BM + leaf)) * S::BM;
-  if (p0 >= end || p0 < begin) return;
-  const ListRows<T> rows_a = list_rows(g.x, g.ld_x, g.d_in, g, end);
-  const PlainRows<T> rows_b = plain_rows(g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out, g.d_in);
-  typename S::RowsA a;
-  typename S::RowsB b;
-  a.init(rows_a, p0, 0, 0, g.d_in);
-  b.init(rows_b, col0, 0, 0, g.d_in);
-  f32x4 acc[S::TM][S::TN];
-  tile_product<S, true>(lds, a, b, rows_a, rows_b, 0, g.d_in, acc, Nothing{});
-  scatter_rows<S>(acc, g.bias ? g.bias + (int64_t)leaf * g.d_out : nullptr, g.y, g.ld_y, g.row_idx, p0,
-                  end < p0 + S::BM ? end : p0 + S::BM, g.n_rows, col0, g.d_out);
+  leaf_rows_product<S, typename S::RowsB>(lds, g, g.x, g.ld_x, g.d_in, g.bias, g.y, g.ld_y, g.d_out);
 }
 
 // dx: rows of dy (k = output along memory) times w, whose rows are k.
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_input_kernel(const LeafArgs<typename S::T> g) {
-  typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
-  const int tile = (int)(t / g.col_tiles), col0 = (int)(t % g.col_tiles) * S::BN;
-  const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, S::BM, tile);
-  if (leaf < 0) return;
-  const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
-  const int p0 = begin + (tile - (begin / S::BM + leaf)) * S::BM;
-  if (p0 >= end || p0 < begin) return;
-  const ListRows<T> rows_a = list_rows(g.dy, g.ld_dy, g.d_out, g, end);
-  const PlainRows<T> rows_b = plain_rows(g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out, g.d_in);
-  typename S::RowsA a;
-  typename S::ColumnsB b;
-  a.init(rows_a, p0, 0, 0, g.d_out);
-  b.init(rows_b, col0, g.d_in, 0, g.d_out);
-  f32x4 acc[S::TM][S::TN];
-  tile_product<S, true>(lds, a, b, rows_a, rows_b, 0, g.d_out, acc, Nothing{});
-  scatter_rows<S>(acc, (const T*)nullptr, g.dx, g.ld_dx, g.row_idx, p0, end < p0 + S::BM ? end : p0 + S::BM, g.n_rows, col0, g.d_in);
+  leaf_rows_product<S, typename S::ColumnsB>(lds, g, g.dy, g.ld_dy, g.d_out, (const typename S::T*)nullptr, g.dx, g.ld_dx, g.d_in);
 }
 
 // Sums over k of operand a's rows, by a product with ones: every n of the block holds the sum for its m.
@@ -186,11 +200,16 @@ struct RowSums {
 // offsets[l] / cut + l on (as above).  A leaf of one piece writes its result; the pieces of others leave f32 sums in slots: of
 // the pieces between two cuts only the first can have begun before (slot 2 b) and only the last can end behind (2 b + 1).
 // leaf_grad_join_kernel adds a leaf's slots in order, so the sums do not depend on which workgroup ran first.
+// The list's ids are copied to local memory first, kCopiedIds at a time: loads are waited for in order, so a row's address
+// that waits for an id on its way from memory waits for all chunks asked for before as well, and steps do not overlap.
+constexpr int kCopiedIds = 4096;
+
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
   const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
+  __shared__ int ids[kCopiedIds];
   const uint32_t tiles = g.col_tiles * g.row_tiles;
   const int piece = (int)(t / tiles), r = (int)(t % tiles);
   const int row0 = r / (int)g.col_tiles * S::BM, col0 = r % (int)g.col_tiles * S::BN;
@@ -201,19 +220,30 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   const int64_t b0 = block * g.cut, b1 = b0 + g.cut;
   const int p0 = begin > b0 ? begin : (int)(b0 < end ? b0 : end), p1 = end < b1 ? end : (int)b1;
   if (p0 >= p1 && (end > begin || block != begin / g.cut)) return;  // only an empty leaf's one piece is empty: zeros
-  const ListRows<T> rows_a = list_rows(g.dy, g.ld_dy, g.d_out, g, p1);
-  const ListRows<T> rows_b = list_rows(g.x, g.ld_x, g.d_in, g, p1);
   typename S::ColumnsA a;
   typename S::ColumnsB b;
-  a.init(rows_a, row0, g.d_out, p0, p1);
-  b.init(rows_b, col0, g.d_in, p0, p1);
   f32x4 acc[S::TM][S::TN];
+  zeros<S>(acc);
   f32x4 sum[S::TM];
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) sum[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
   const bool sums = g.dbias != nullptr && col0 == 0 && w % S::WN == 0;
-  tile_product<S, true>(lds, a, b, rows_a, rows_b, p0, p1, acc, RowSums<S>{sum, sums});
+  for (int c0 = p0; c0 < p1; c0 += kCopiedIds) {
+    const int c1 = p1 - c0 < kCopiedIds ? p1 : c0 + kCopiedIds;
+    __syncthreads();  // the part before has been used
+    for (int p = c0 + (int)threadIdx.x; p < c1; p += S::NT) {
+      const int d = g.row_idx ? g.row_idx[p] : p;
+      ids[p - c0] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
+    }
+    __syncthreads();
+    const CopiedRows<T> rows_a = {g.dy, g.dy + (int64_t)(g.n_rows - 1) * g.ld_dy + g.d_out, g.ld_dy, ids, c0};
+    const CopiedRows<T> rows_b = {g.x, g.x + (int64_t)(g.n_rows - 1) * g.ld_x + g.d_in, g.ld_x, ids, c0};
+    a.init(rows_a, row0, g.d_out, c0, c1);
+    b.init(rows_b, col0, g.d_in, c0, c1);
+    tile_begin<S>(lds, a, b, rows_a, rows_b, c0, c1);
+    tile_run<S, true>(lds, a, b, rows_a, rows_b, c0, c1, acc, RowSums<S>{sum, sums});
+  }
 
   const bool whole = begin >= b0 && end <= b1;
   const int64_t slot = 2 * block + (begin < b0 ? 0 : 1);

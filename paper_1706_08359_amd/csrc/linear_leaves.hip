@@ -58,12 +58,33 @@ int leaf_check(int64_t n_positions, int32_t n_leaves, int64_t n_rows, int32_t d_
 // A pointer that no element can lie at.
 bool off_element(const void* p, int32_t dtype) { return ((uintptr_t)p & (dtype == GBDT_F32 ? 3 : 1)) != 0; }
 
+// The tile of most calls, of whole chunks or not.  bf16: 128 x 128 by four wavefronts, two workgroups a compute unit.  f32: 64
+// x 64, since its matrix instructions, 16 times slower, are the bound at any tile, and smaller tiles waste less of them.
+template <typename T>
+using Square = typename std::conditional<sizeof(T) == 2, Shape<T, 128, 128, 2, 2, true, true>, Shape<T, 64, 64, 2, 2, true>>::type;
+template <typename T>
+using SquareAny = typename std::conditional<sizeof(T) == 2, Shape<T, 128, 128, 2, 2, false>, Shape<T, 64, 64, 2, 2, false>>::type;
+
+// Workgroups of the products over rows: the column tiles of a row tile are spread over as many as it takes to have eight a
+// compute unit, and no more, since a workgroup's first tile waits for its leaf and its rows.
+template <class S, typename T>
+int leaf_rows_grid(gbdt_leaf::LeafArgs<T>& g, int64_t cols, unsigned* blocks) {
+  const int64_t row_tiles = (int64_t)g.n_positions / S::BM + g.n_leaves;
+  const int64_t col_tiles = ceil_div(cols, S::BN);
+  g.col_tiles = (uint32_t)col_tiles;
+  g.cols_per = (uint32_t)std::max<int64_t>(1, std::min(col_tiles, (int64_t)g.n_positions / S::BM * col_tiles / (8 * gbdt_internal::cu_count())));
+  const int64_t n = row_tiles * ceil_div(col_tiles, g.cols_per);
+  if (n > kMaxBlocks) return GBDT_EUNSUPPORTED;
+  *blocks = (unsigned)n;
+  return GBDT_OK;
+}
+
 template <class S, typename T>
 int launch_leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  g.col_tiles = (uint32_t)ceil_div(g.d_out, S::BN);
-  const int64_t blocks = ((int64_t)g.n_positions / S::BM + g.n_leaves) * g.col_tiles;
-  if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
-  gbdt_leaf::leaf_product_kernel<S><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+  unsigned blocks = 0;
+  const int rc = leaf_rows_grid<S>(g, g.d_out, &blocks);
+  if (rc != GBDT_OK) return rc;
+  gbdt_leaf::leaf_product_kernel<S><<<dim3(blocks), dim3(S::NT), 0, s>>>(g);
   LAUNCHED("leaf_product_kernel");
   return GBDT_OK;
 }
@@ -73,35 +94,42 @@ int leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   const bool direct = whole_chunks<T>(g.x, g.ld_x, g.d_in) && whole_chunks<T>(g.w, g.d_in, g.d_in);
   if (g.d_out <= 16)
     return direct ? launch_leaf_product<Shape<T, 128, 16, 4, 1, true>>(g, s) : launch_leaf_product<Shape<T, 128, 16, 4, 1, false>>(g, s);
-  return direct ? launch_leaf_product<Shape<T, 128, 128, 2, 2, true>>(g, s) : launch_leaf_product<Shape<T, 128, 128, 2, 2, false>>(g, s);
+  if (direct && sizeof(T) == 2) {
+    // One pass over x: as many of its bytes on the way as local memory holds.
+    if (g.d_out <= 64) return launch_leaf_product<Shape<T, 128, 64, 4, 1, true>>(g, s);
+    return launch_leaf_product<Shape<T, 256, 128, 4, 2, true, false, 3>>(g, s);
+  }
+  return direct ? launch_leaf_product<Square<T>>(g, s) : launch_leaf_product<SquareAny<T>>(g, s);
 }
 
 template <class S, typename T>
 int launch_leaf_grad_input(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  g.col_tiles = (uint32_t)ceil_div(g.d_in, S::BN);
-  const int64_t blocks = ((int64_t)g.n_positions / S::BM + g.n_leaves) * g.col_tiles;
-  if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
-  gbdt_leaf::leaf_grad_input_kernel<S><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+  unsigned blocks = 0;
+  const int rc = leaf_rows_grid<S>(g, g.d_in, &blocks);
+  if (rc != GBDT_OK) return rc;
+  gbdt_leaf::leaf_grad_input_kernel<S><<<dim3(blocks), dim3(S::NT), 0, s>>>(g);
   LAUNCHED("leaf_grad_input_kernel");
   return GBDT_OK;
 }
 
-constexpr int kGradBM = 128, kGradBN = 128;  // the weights' gradient: outputs x inputs a tile
+// Tile of the weights' gradient: outputs x inputs.
+int64_t grad_bm(int64_t e, int64_t d_out) { return e == 4 || d_out <= 64 ? 64 : 128; }
+int64_t grad_bn(int64_t e) { return e == 4 ? 64 : 128; }
+int64_t leaf_tiles(int64_t e, int64_t d_in, int64_t d_out) { return ceil_div(d_out, grad_bm(e, d_out)) * ceil_div(d_in, grad_bn(e)); }
 
-// Positions between cuts: twice as many whole pieces of work as compute units, from 512 positions on.  Then the sums that
+// Positions between cuts: twice as many whole pieces of work as compute units, from 256 positions on.  Then the sums that
 // pieces leave behind are at most 2 x 2 x units tiles of f32 (64 MiB on 256 units) whatever the sizes are.
 int64_t leaf_cut(int64_t n_positions, int64_t tiles, int64_t units) {
-  return std::max<int64_t>(512, round_up(ceil_div(n_positions * tiles, 2 * units), 64));
+  return std::max<int64_t>(256, round_up(ceil_div(n_positions * tiles, 2 * units), 64));
 }
-int64_t leaf_tiles(int64_t d_in, int64_t d_out) { return ceil_div(d_out, kGradBM) * ceil_div(d_in, kGradBN); }
-size_t leaf_partial_bytes(int64_t n_positions, int64_t d_in, int64_t d_out, int64_t units) {
-  const int64_t blocks = ceil_div(n_positions, leaf_cut(n_positions, leaf_tiles(d_in, d_out), units));
+size_t leaf_partial_bytes(int64_t n_positions, int64_t e, int64_t d_in, int64_t d_out, int64_t units) {
+  const int64_t blocks = ceil_div(n_positions, leaf_cut(n_positions, leaf_tiles(e, d_in, d_out), units));
   return blocks < 2 ? 0 : pad256((size_t)(2 * blocks * (d_in + 1) * d_out) * sizeof(float));
 }
 
 template <class S, typename T>
 int launch_leaf_grad_weight(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  static_assert(S::BM == kGradBM && S::BN == kGradBN, "leaf_tiles counts these");
+  if (S::BM != grad_bm(sizeof(T), g.d_out) || S::BN != grad_bn(sizeof(T))) return GBDT_EUNSUPPORTED;  // (leaf_tiles counts these)
   g.col_tiles = (uint32_t)(g.dw ? ceil_div(g.d_in, S::BN) : 1);
   g.row_tiles = (uint32_t)ceil_div(g.d_out, S::BM);
   const int64_t blocks = ((int64_t)g.n_positions / g.cut + g.n_leaves) * g.col_tiles * g.row_tiles;
@@ -115,14 +143,13 @@ template <typename T>
 int leaf_product_grad(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   if (g.dx && g.n_positions > 0) {
     const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.w, g.d_in, g.d_in);
-    const int rc = direct ? launch_leaf_grad_input<Shape<T, 128, 128, 2, 2, true>>(g, s)
-                          : launch_leaf_grad_input<Shape<T, 128, 128, 2, 2, false>>(g, s);
+    const int rc = direct ? launch_leaf_grad_input<Square<T>>(g, s) : launch_leaf_grad_input<SquareAny<T>>(g, s);
     if (rc != GBDT_OK) return rc;
   }
   if (!g.dw && !g.dbias) return GBDT_OK;
   const int64_t units = gbdt_internal::cu_count();
-  g.cut = (int32_t)leaf_cut(g.n_positions, leaf_tiles(g.d_in, g.d_out), units);
-  const size_t bytes = leaf_partial_bytes(g.n_positions, g.d_in, g.d_out, units);
+  g.cut = (int32_t)leaf_cut(g.n_positions, leaf_tiles(sizeof(T), g.d_in, g.d_out), units);
+  const size_t bytes = leaf_partial_bytes(g.n_positions, sizeof(T), g.d_in, g.d_out, units);
   if (bytes) {
     void* ws = nullptr;
     const int rc = gbdt_internal::workspace(bytes, s, &ws);
@@ -130,8 +157,15 @@ int leaf_product_grad(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
     g.partial = (float*)ws;
   }
   const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.x, g.ld_x, g.d_in);
-  const int rc = direct ? launch_leaf_grad_weight<Shape<T, 128, 128, 2, 2, true>>(g, s)
-                        : launch_leaf_grad_weight<Shape<T, 128, 128, 2, 2, false>>(g, s);
+  int rc = GBDT_OK;
+  if constexpr (sizeof(T) == 2) {
+    if (g.d_out <= 64)
+      rc = direct ? launch_leaf_grad_weight<Shape<T, 64, 128, 1, 4, true, true>>(g, s) : launch_leaf_grad_weight<Shape<T, 64, 128, 1, 4, false>>(g, s);
+    else
+      rc = direct ? launch_leaf_grad_weight<Square<T>>(g, s) : launch_leaf_grad_weight<SquareAny<T>>(g, s);
+  } else {
+    rc = direct ? launch_leaf_grad_weight<Square<T>>(g, s) : launch_leaf_grad_weight<SquareAny<T>>(g, s);
+  }
   if (rc != GBDT_OK) return rc;
   const int64_t cuts = ceil_div(g.n_positions, g.cut) - 1;
   if (cuts > 0) {
@@ -160,7 +194,7 @@ int softmax_check(const void* h, int64_t ld_h, const void* c, int64_t ld_c, int6
 // Tiles of 256 x 256 by eight wavefronts, one workgroup a compute unit (f32: as any other; its products are 16 times slower
 // and its loads never the bound).
 template <typename T>
-using Wide = typename std::conditional<sizeof(T) == 2, Shape<T, 256, 256, 2, 4, true, true>, Shape<T, 128, 128, 2, 2, true>>::type;
+using Wide = typename std::conditional<sizeof(T) == 2, Shape<T, 256, 256, 2, 4, true, true>, Square<T>>::type;
 template <typename T>
 bool wide_tiles(int64_t rows, int64_t cols) {
   return sizeof(T) == 2 && ceil_div(rows, 256) * ceil_div(cols, 256) >= 256;
@@ -180,7 +214,7 @@ int score_grid(gbdt_softmax::ScoreArgs<T>& g, unsigned* blocks) {
   if (n > kMaxBlocks || (int64_t)g.group * g.col_tiles > kMaxBlocks) return GBDT_EUNSUPPORTED;
   // One workgroup a compute unit goes through the tiles where there is no room for two; else one a tile.
   const int64_t units = std::max(8, gbdt_internal::cu_count() / 8 * 8);
-  *blocks = (unsigned)(S::DEEP ? std::min(n, units) : n);
+  *blocks = (unsigned)(S::BM >= 256 ? std::min(n, units) : n);
   return GBDT_OK;
 }
 
@@ -189,9 +223,10 @@ struct LossPlan {
   int64_t tiles;
   size_t parts_bytes, bytes;
 };
+template <typename T>
 LossPlan loss_plan(int64_t n_rows, int64_t n_classes) {
   LossPlan p;
-  p.tiles = ceil_div(n_classes, gbdt_softmax::kPartClasses);
+  p.tiles = ceil_div(n_classes, gbdt_softmax::kPartClasses<T>);
   p.rows = std::min(n_rows, std::max<int64_t>(4096, kPartsBytes / (8 * p.tiles) / 4096 * 4096));
   p.parts_bytes = pad256((size_t)(p.rows * p.tiles) * 8);
   p.bytes = p.parts_bytes + pad256((size_t)p.rows * 4);
@@ -211,7 +246,7 @@ int launch_scores(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
 template <typename T>
 int softmax_loss(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32_t* labels, int64_t n_rows, int64_t n_classes,
                  int32_t dim, float* loss, float* lse, hipStream_t s) {
-  const LossPlan plan = loss_plan(n_rows, n_classes);
+  const LossPlan plan = loss_plan<T>(n_rows, n_classes);
   void* ws = nullptr;
   int rc = gbdt_internal::workspace(plan.bytes, s, &ws);
   if (rc != GBDT_OK) return rc;
@@ -229,8 +264,8 @@ int softmax_loss(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
     g.n_classes = g.end = (int32_t)n_classes;
     g.dim = dim;
     rc = direct && wide_tiles<T>(g.n_rows, n_classes) ? launch_scores<Wide<T>>(g, s)
-         : direct                                     ? launch_scores<Shape<T, 128, 128, 2, 2, true>>(g, s)
-                                                      : launch_scores<Shape<T, 128, 128, 2, 2, false>>(g, s);
+         : direct                                     ? launch_scores<Square<T>>(g, s)
+                                                      : launch_scores<SquareAny<T>>(g, s);
     if (rc != GBDT_OK) return rc;
     gbdt_softmax::softmax_join_kernel<<<dim3((unsigned)ceil_div(g.n_rows, 16)), dim3(256), 0, s>>>(
         g.parts, g.picked, g.labels, g.n_rows, g.n_classes, (int32_t)plan.tiles, loss ? loss + r : nullptr, lse + r);
@@ -246,9 +281,9 @@ struct GradPlan {
   size_t g_bytes, dh_bytes, dc_bytes, h_bytes, c_bytes;
   size_t bytes() const { return g_bytes + dh_bytes + dc_bytes + h_bytes + c_bytes; }
 };
-// Splits of a summed axis of `k`: as many as fill the compute units, each 8 steps long at least.
+// Splits of a summed axis of `k`: as many as give `units` workgroups work, each 4 steps long at least.
 void split_axis(int64_t tiles, int64_t k, int64_t step, int64_t units, int64_t* splits, int64_t* len) {
-  const int64_t want = std::max<int64_t>(1, std::min(units / std::max<int64_t>(tiles, 1), ceil_div(k, 8 * step)));
+  const int64_t want = std::max<int64_t>(1, std::min(units / std::max<int64_t>(tiles, 1), ceil_div(k, 4 * step)));
   *len = std::max(step, round_up(ceil_div(k, want), step));
   *splits = std::max<int64_t>(1, ceil_div(k, *len));
 }
@@ -261,12 +296,15 @@ GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, bo
   p.width = round_up(ceil_div(n_classes, p.pieces), kPieceAlign);
   p.pieces = ceil_div(n_classes, p.width);
   const int64_t step = 128 / e;
-  const int64_t cols = ceil_div(dim, 128);
-  split_axis(ceil_div(rows, 128) * cols, p.width, step, units, &p.dh_splits, &p.dh_split);
+  const int64_t tile = e == 2 ? 128 : 64;
+  const int64_t cols = ceil_div(dim, tile);
+  split_axis(ceil_div(rows, tile) * cols, p.width, step, 2 * units, &p.dh_splits, &p.dh_split);
   const int64_t wide = ceil_div(rows, 256) * ceil_div(dim, 256);
   if (e == 2 && wide < units && wide * ceil_div(p.width, 16 * step) >= units)
     split_axis(wide, p.width, step, units, &p.dh_splits, &p.dh_split);
-  split_axis(ceil_div(p.width, 128) * cols, n_rows, step, units, &p.dc_splits, &p.dc_split);
+  else if (e == 2 && wide >= units)
+    p.dh_splits = 1, p.dh_split = round_up(p.width, step);
+  split_axis(ceil_div(p.width, tile) * cols, n_rows, step, 2 * units, &p.dc_splits, &p.dc_split);
   p.g_bytes = pad256((size_t)(rows * p.width * e));
   p.dh_bytes = p.dh_splits > 1 || p.pieces > 1 ? pad256((size_t)(p.dh_splits * rows * dim) * 4) : 0;
   p.dc_bytes = p.dc_splits > 1 ? pad256((size_t)(p.dc_splits * p.width * dim) * 4) : 0;
@@ -346,7 +384,7 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
     c = (const T*)at;
     ld_c = whole_dim;
   }
-  typedef Shape<T, 128, 128, 2, 2, true> Small;
+  typedef Square<T> Small;
   gbdt_softmax::PieceArgs<T> to_h = {}, to_c = {};
   for (int64_t begin = 0; begin < n_classes; begin += plan.width) {
     const int64_t end = std::min(n_classes, begin + plan.width);
@@ -429,7 +467,7 @@ int softmax_stats(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
   const bool direct = whole_chunks<T>(g.h, g.ld_h, g.dim) && whole_chunks<T>(g.c, g.ld_c, g.dim);
   if (g.end - g.begin <= 16)
     return direct ? launch_stats<Shape<T, 128, 16, 4, 1, true>>(g, s) : launch_stats<Shape<T, 128, 16, 4, 1, false>>(g, s);
-  return direct ? launch_stats<Shape<T, 128, 128, 2, 2, true>>(g, s) : launch_stats<Shape<T, 128, 128, 2, 2, false>>(g, s);
+  return direct ? launch_stats<Square<T>>(g, s) : launch_stats<SquareAny<T>>(g, s);
 }
 
 template <typename T>
@@ -524,7 +562,8 @@ int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const voi
 
 size_t gbdt_leaf_product_grad_workspace_bytes(int64_t n_positions, int32_t d_in, int32_t d_out) {
   if (n_positions < 0 || n_positions >= kMaxRows || d_in <= 0 || d_out <= 0 || d_in >= kMaxWidth || d_out >= kMaxWidth) return 0;
-  return gbdt_internal::workspace_head_bytes() + leaf_partial_bytes(n_positions, d_in, d_out, gbdt_internal::cu_count());
+  const int64_t units = gbdt_internal::cu_count();
+  return gbdt_internal::workspace_head_bytes() + std::max(leaf_partial_bytes(n_positions, 2, d_in, d_out, units), leaf_partial_bytes(n_positions, 4, d_in, d_out, units));
 }
 
 int gbdt_leaf_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* weight, const int32_t* row_idx,
@@ -553,7 +592,7 @@ size_t gbdt_softmax_workspace_bytes(int64_t n_rows, int64_t n_classes, int32_t d
       (dtype != GBDT_F32 && dtype != GBDT_BF16))
     return 0;
   const GradPlan p = grad_plan(n_rows, n_classes, dim, dtype == GBDT_F32 ? 4 : 2, false, gbdt_internal::cu_count());
-  const size_t grad = p.bytes(), loss = loss_plan(n_rows, n_classes).bytes;
+  const size_t grad = p.bytes(), loss = (dtype == GBDT_F32 ? loss_plan<float>(n_rows, n_classes) : loss_plan<bf16>(n_rows, n_classes)).bytes;
   return gbdt_internal::workspace_head_bytes() + std::max(grad, loss);
 }
 

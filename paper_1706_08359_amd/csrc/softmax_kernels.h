@@ -33,7 +33,9 @@ __device__ __forceinline__ float exp_diff(float s, float base) { return __builti
 // What a running maximum is subtracted as: exponentials beneath an infinite one are 0 or infinite, not inf - inf.
 __device__ __forceinline__ float base_of(float m) { return __builtin_isinf(m) ? 0.0f : m; }
 
-constexpr int kPartClasses = 128;  // of a maximum and a sum, whatever the tile
+// Classes of a maximum and a sum, whatever the tile.
+template <typename T>
+constexpr int kPartClasses = sizeof(T) == 2 ? 128 : 64;
 
 struct MaxSum {
   float m, s;
@@ -51,7 +53,7 @@ struct ScoreArgs {
   const int32_t* labels;  // [n_rows] or null
   const float* lse;       // [n_rows]
   const float* weight;    // [n_rows] or null
-  MaxSum* parts;          // [ceil(n_classes / kPartClasses)][n_rows]
+  MaxSum* parts;          // [ceil(n_classes / kPartClasses<T>)][n_rows]
   float* picked;          // [n_rows]: the label's score
   T* g;                   // [n_rows][ld_g]: G of the classes begin .. end, zeros behind
   float* grad;            // [end - begin][ld_out]
@@ -97,6 +99,7 @@ __device__ __forceinline__ void for_score_tiles(char* lds, const ScoreArgs<T>& g
   begin(tile);
   for (;;) {
     f32x4 acc[S::TM][S::TN];
+    zeros<S>(acc);
     tile_run<S, N_INNER>(lds, a, b, rows_a, rows_b, 0, g.dim, acc, Nothing{});
     const int row = row0, col = col0;
     const auto of_rows = fetch(row);
@@ -119,7 +122,7 @@ struct OfRows {
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) softmax_scores_kernel(const ScoreArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  // [128 classes: their wavefronts' lane groups][row]: the maximum and the sum of a lane's 4 TN values of a row
+  // [a part's classes: their wavefronts' lane groups][row]: the maximum and the sum of a lane's 4 TN values of a row
   __shared__ MaxSum lane_parts[S::WN * 4 * S::BM];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int m0 = (w / S::WN) * (S::TM * 16) + (l & 15), wave_n = (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
@@ -171,15 +174,16 @@ __global__ void __launch_bounds__(S::NT, 2) softmax_scores_kernel(const ScoreArg
       }
     }
     __syncthreads();  // (the next tile's steps, with their barriers, come before these places are written again)
-    constexpr int lanes = 4 * kPartClasses / (S::TN * 16);  // of a row in a part
-    static_assert(S::BN % kPartClasses == 0 && lanes >= 4, "tiles of whole parts");
-    for (int e = threadIdx.x; e < S::BM * (S::BN / kPartClasses); e += S::NT) {
+    constexpr int part = kPartClasses<typename S::T>;
+    constexpr int lanes = 4 * part / (S::TN * 16);  // of a row in a part
+    static_assert(S::BN % part == 0 && lanes >= 4, "tiles of whole parts");
+    for (int e = threadIdx.x; e < S::BM * (S::BN / part); e += S::NT) {
       const int m = e % S::BM, q = e / S::BM;
-      if (row0 + m >= g.n_rows || col0 + q * kPartClasses >= g.end) continue;
+      if (row0 + m >= g.n_rows || col0 + q * part >= g.end) continue;
       MaxSum p = lane_parts[q * lanes * S::BM + m];
 #pragma unroll
       for (int k = 1; k < lanes; ++k) p = join(p, lane_parts[(q * lanes + k) * S::BM + m]);
-      g.parts[((int64_t)(col0 / kPartClasses) + q) * g.n_rows + row0 + m] = p;
+      g.parts[((int64_t)(col0 / part) + q) * g.n_rows + row0 + m] = p;
     }
   });
 }

@@ -238,6 +238,7 @@ struct ColumnOperand {
   }
   template <class Rows>
   __device__ __forceinline__ void fetch(const Rows& rows) {
+    if (DIRECT && Rows::kEven) return;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int k = k_at + slot_k(i);
@@ -256,7 +257,8 @@ struct ColumnOperand {
       for (int i = 0; i < kPer; ++i) here[i] = rows.base + (int64_t)(k_at + slot_k(i)) * rows.ld + direct_column(i);
     }
   }
-  // Any column that exists stands in for one past the limit.
+  // Any column that exists stands in for one past the limit.  (Rows that are none are zeros, loaded as such if rows come from
+  // a list: then every step has as many loads as any other.)
   __device__ __forceinline__ int direct_column(int i) const {
     const int c = slot_column(i);
     return c < lim ? c : lim - kChunk<T>;
@@ -264,39 +266,35 @@ struct ColumnOperand {
   // DIRECT: the i'th of a step's chunks (WHOLE: of a step that no limit cuts); after the last, `advance`.
   template <bool WHOLE, class Rows>
   __device__ __forceinline__ void load_one(const Rows& rows, char* stage, int i) {
-    static_assert(DIRECT && Rows::kEven, "");
+    static_assert(DIRECT, "");
     const int t = threadIdx.x;
-    if (WHOLE || k_at + slot_k(i) < k_end) {
-      direct_chunk(here[i], wave_place(stage) + i * NT * 16);
+    if constexpr (!Rows::kEven) {
+      const T* row = rows.at(k_at + slot_k(i), id[i]);
+      direct_chunk(row != nullptr ? (const void*)(row + direct_column(i)) : (const void*)zero_chunk, wave_place(stage) + i * NT * 16);
     } else {
-      *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
+      if (WHOLE || k_at + slot_k(i) < k_end) {
+        direct_chunk(here[i], wave_place(stage) + i * NT * 16);
+      } else {
+        *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
+      }
+      here[i] += (int64_t)kStep * rows.ld;
     }
-    here[i] += (int64_t)kStep * rows.ld;
   }
   template <class Rows>
-  __device__ __forceinline__ void advance(const Rows&) {
+  __device__ __forceinline__ void advance(const Rows& rows) {
     k_at += kStep;
+    fetch(rows);
   }
   template <class Rows>
   __device__ __forceinline__ void load(const Rows& rows, char* stage) {
     const int t = threadIdx.x;
     if constexpr (DIRECT) {
-      if (Rows::kEven && k_at + kStep <= k_end) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          direct_chunk(here[i], wave_place(stage) + i * NT * 16);
-          here[i] += (int64_t)kStep * rows.ld;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const int k = k_at + slot_k(i);
-          const T* row = k < k_end ? rows.at(k, id[i]) : nullptr;
-          if (row != nullptr) {
-            direct_chunk(row + direct_column(i), wave_place(stage) + i * NT * 16);
-          } else {
-            *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
-          }
+      for (int i = 0; i < kPer; ++i) {
+        if (Rows::kEven && k_at + kStep <= k_end) {
+          load_one<true>(rows, stage, i);
+        } else {
+          load_one<false>(rows, stage, i);
         }
       }
     } else {
@@ -388,18 +386,18 @@ __device__ __forceinline__ f32x4 mma(f32x4 rows, f32x4 cols, f32x4 acc) {
 // BM x BN values by WM x WN wavefronts.  A lane's four values of the 16 x 16 block (i, j) of its wavefront:
 //   N_INNER: m = 16 i + lane mod 16, n = 16 j + 4 (lane / 16) + 0..3   (rows of an output along n)
 //   else:    n = 16 j + lane mod 16, m = 16 i + 4 (lane / 16) + 0..3   (columns of an output along m)
-// DEEP (DIRECT only): steps of 64 bytes of k and four stages instead of 128 bytes and two.
-template <typename T_, int BM_, int BN_, int WM_, int WN_, bool DIRECT_, bool DEEP_ = false>
+// DEEP (DIRECT only): steps of 64 bytes of k and four stages instead of 128 bytes and STAGES (more than two: DIRECT only).
+template <typename T_, int BM_, int BN_, int WM_, int WN_, bool DIRECT_, bool DEEP_ = false, int STAGES_ = 2>
 struct Shape {
   typedef T_ T;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NT = WM_ * WN_ * 64;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
   static constexpr bool DIRECT = DIRECT_, DEEP = DEEP_;
-  static constexpr int KB = DEEP ? 64 : 128, kStep = KB / (int)sizeof(T), kStages = DEEP ? 4 : 2;
+  static constexpr int KB = DEEP ? 64 : 128, kStep = KB / (int)sizeof(T), kStages = DEEP ? 4 : STAGES_;
   static constexpr int kStageBytes = (BM + BN) * KB;
   static constexpr int kLdsBytes = kStages * kStageBytes;
   static_assert(TM >= 1 && TN >= 1 && BM % (WM * 16) == 0 && BN % (WN * 16) == 0, "whole 16 x 16 blocks");
-  static_assert(DIRECT || !DEEP, "");
+  static_assert(DIRECT || (!DEEP && kStages == 2), "");
   typedef RowOperand<T, BM, NT, DIRECT, KB> RowsA;
   typedef RowOperand<T, BN, NT, DIRECT, KB> RowsB;
   typedef ColumnOperand<T, BM, NT, DIRECT, KB> ColumnsA;
@@ -449,26 +447,30 @@ __device__ __forceinline__ void tile_begin(char* lds, A& a, B& b, const RowsA& r
   const int steps = (k1 - k0 + S::kStep - 1) / S::kStep;
   if (steps <= 0) return;
   // (DEEP: an even number of steps, the last of them zeros if need be)
-  constexpr int first = S::DEEP ? 3 : 1;
-  for_blocks<0, first>([&](auto at) {
+  for_blocks<0, S::kStages - 1>([&](auto at) {
     constexpr int i = decltype(at)::value;
-    if (i < 2 || steps > 2) {
+    if (i < steps || (S::DEEP && i == 1)) {
       a.load(rows_a, lds + i * S::kStageBytes);
       b.load(rows_b, lds + i * S::kStageBytes + A::kBytes);
     }
   });
 }
 
+template <class S>
+__device__ __forceinline__ void zeros(f32x4 (&acc)[S::TM][S::TN]) {
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+}
+
+// Adds the products of k0 <= k < k1 to acc.
 template <class S, bool N_INNER, class A, class B, class RowsA, class RowsB, class Also>
 __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& rows_a, const RowsB& rows_b, int k0, int k1,
                                          f32x4 (&acc)[S::TM][S::TN], const Also& also) {
   typedef typename Traits<typename S::T>::Frag Frag;
   const int w = threadIdx.x >> 6;
   const int m0 = (w / S::WN) * (S::TM * 16), n0 = (w % S::WN) * (S::TN * 16);
-#pragma unroll
-  for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-    for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const int steps = (k1 - k0 + S::kStep - 1) / S::kStep;
   if (steps <= 0) return;
 
@@ -587,30 +589,42 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
       });
     };
     if constexpr (S::DIRECT) {
-      // A stage is given up two blocks before its step ends, when all of it has been read, and the step after the next goes
+      // A stage is given up two blocks before its step ends, when all of it has been read, and the step kStages later goes
       // there: one barrier a step is enough, and the last two blocks cover the first reads of the next stage.
-      arrived<0>();
-      if (steps > 1) {
-        a.load(rows_a, lds + S::kStageBytes);
-        b.load(rows_b, lds + S::kStageBytes + A::kBytes);
+      constexpr int ns = S::kStages, per = A::kPer + B::kPer;
+      const int full = ((a.k_end < b.k_end ? a.k_end : b.k_end) - k0) / S::kStep;  // steps whose every chunk is loaded
+      // Step `next` is there; the kStages - 2 behind it may be on their way.
+      auto wait = [&](int next) {
+        if (ns > 2 && next + ns - 2 < full) {
+          arrived<(ns - 2) * per>();
+        } else {
+          arrived<0>();
+        }
+      };
+      wait(0);
+      char* here = lds;
+      char* free = lds + (ns - 1) * S::kStageBytes;
+      if (ns - 1 < steps) {
+        a.load(rows_a, free);
+        b.load(rows_b, free + A::kBytes);
       }
       first_reads(lds);
       for (int s = 0; s < steps; ++s) {
-        char* here = lds + (s & 1) * S::kStageBytes;
-        char* next = lds + ((s + 1) & 1) * S::kStageBytes;
+        char* next = here + S::kStageBytes == lds + ns * S::kStageBytes ? lds : here + S::kStageBytes;
         most_blocks(here);
-        arrived<0>();
+        wait(s + 1);
         first_reads(next);  // (of whatever is there after the last step)
         in_order();
         multiply(S::TM - 2, blocks - 2, 1);
         in_order();
-        if (s + 2 < steps) {
+        if (s + ns < steps) {
           a.load(rows_a, here);
           b.load(rows_b, here + A::kBytes);
         }
         in_order();
         multiply(S::TM - 1, blocks - 1, 1);
         in_order();
+        here = next;
       }
     } else {
       a.store(lds);
@@ -639,6 +653,7 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
 template <class S, bool N_INNER, class A, class B, class RowsA, class RowsB, class Also>
 __device__ __forceinline__ void tile_product(char* lds, A& a, B& b, const RowsA& rows_a, const RowsB& rows_b, int k0, int k1,
                                              f32x4 (&acc)[S::TM][S::TN], const Also& also) {
+  zeros<S>(acc);
   tile_begin<S>(lds, a, b, rows_a, rows_b, k0, k1);
   tile_run<S, N_INNER>(lds, a, b, rows_a, rows_b, k0, k1, acc, also);
 }
