@@ -468,7 +468,8 @@ typedef enum { GBDT_F32 = 0, GBDT_BF16 = 1 } gbdt_dtype;
  *                 outside [0, n_positions] are taken as its ends.  They are on the device so that a
  *                 caller that routes rows there need not wait for their numbers
  *   y_out         DEVICE [n_rows][d_out], by ROW ID; rows of no leaf are left as they are
- * n_rows and n_positions < 2^30, n_leaves, d_in and d_out < 2^24 (GBDT_EUNSUPPORTED beyond).
+ * n_rows and n_positions < 2^30, n_leaves, d_in and d_out < 2^24, ld_* < 2^28 (GBDT_EUNSUPPORTED
+ * beyond).
  */
 int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const void* bias,
                       const int32_t* row_idx, const int64_t* leaf_offsets, int64_t n_positions,
@@ -507,7 +508,7 @@ size_t gbdt_leaf_product_grad_workspace_bytes(int64_t n_positions, int32_t d_in,
  *            loss, lse, gradients and hessians are 0 and it takes no part in any sum, whatever
  *            its h holds.  NULL (loss_out NULL as well): every row counts and none has a label
  *   loss_out, lse_out   DEVICE float [n_rows]
- * n_rows and n_classes < 2^30, dim < 2^24 (GBDT_EUNSUPPORTED beyond).  An infinite or NaN score
+ * n_rows and n_classes < 2^30, dim < 2^24, ld_h and ld_c < 2^28 (GBDT_EUNSUPPORTED beyond).  An infinite or NaN score
  * goes where the formula takes it.
  */
 int gbdt_softmax_loss(const void* h, int64_t ld_h, const void* classes, int64_t ld_c,

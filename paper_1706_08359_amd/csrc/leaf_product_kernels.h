@@ -57,6 +57,12 @@ __device__ __forceinline__ int find_leaf(const int64_t* offsets, int n_leaves, i
   return lo;
 }
 
+// Row r >= 0: one 32 x 32 -> 64 bit product and sum (distances of rows are below 2^30 bytes).
+template <typename T>
+__device__ __forceinline__ const T* row_of(const T* base, int r, int64_t ld) {
+  return (const T*)((const char*)base + (uint64_t)(uint32_t)r * (uint32_t)(ld * (int64_t)sizeof(T)));
+}
+
 // Rows of a matrix by position in the list; `end` is the matrix's, one past its last value.
 template <typename T>
 struct ListRows {
@@ -68,7 +74,7 @@ struct ListRows {
   int32_t stop, n_rows;
   __device__ __forceinline__ int fetch(int p) const { return p < stop ? (row_idx ? row_idx[p] : p) : -1; }
   __device__ __forceinline__ const T* at(int, int d) const {
-    return (uint32_t)d < (uint32_t)n_rows ? base + (int64_t)d * ld : nullptr;
+    return (uint32_t)d < (uint32_t)n_rows ? row_of(base, d, ld) : nullptr;
   }
 };
 template <typename T>
@@ -83,10 +89,10 @@ struct CopiedRows {
   const T* base;
   const T* end;
   int64_t ld;
-  const int* ids;
+  const __attribute__((address_space(3))) int* ids;  // (said outright: a flat load would be waited for with all others)
   int32_t first;  // the position of ids[0]
   __device__ __forceinline__ int fetch(int p) const { return ids[p - first]; }
-  __device__ __forceinline__ const T* at(int, int d) const { return d >= 0 ? base + (int64_t)d * ld : nullptr; }
+  __device__ __forceinline__ const T* at(int, int d) const { return d >= 0 ? row_of(base, d, ld) : nullptr; }
 };
 
 // Rows of a matrix in order.
@@ -98,32 +104,11 @@ struct PlainRows {
   int64_t ld;
   int32_t n;
   __device__ __forceinline__ int fetch(int) const { return 0; }
-  __device__ __forceinline__ const T* at(int r, int) const { return r < n ? base + (int64_t)r * ld : nullptr; }
+  __device__ __forceinline__ const T* at(int r, int) const { return r < n ? row_of(base, r, ld) : nullptr; }
 };
 template <typename T>
 __device__ __forceinline__ PlainRows<T> plain_rows(const T* base, int64_t ld, int n, int cols) {
   return {base, base + (int64_t)(n - 1) * ld + cols, ld, n};
-}
-
-// Writes a tile's values (N_INNER) to the rows of the list, adding bias if there is one.  rows: of this lane's blocks, null
-// for none.
-template <class S, typename T>
-__device__ __forceinline__ void store_rows(const f32x4 (&acc)[S::TM][S::TN], const T* bias, T* const (&rows)[S::TM], int col0, int cols) {
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
-#pragma unroll
-  for (int j = 0; j < S::TN; ++j) {
-    const int n = n0 + 16 * j;
-    if (n >= cols) continue;
-    f32x4 add = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (bias) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) add[r] = (float)bias[n + r < cols ? n + r : n];
-    }
-#pragma unroll
-    for (int i = 0; i < S::TM; ++i)
-      if (rows[i]) store4(rows[i] + n, acc[i][j] + add, cols - n);
-  }
 }
 
 // The rows of one tile of positions times a matrix of the leaf, g.cols_per column tiles one after another; the next one's
@@ -142,12 +127,12 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& 
   const int col_last = cols < col_first + (int)g.cols_per * S::BN ? cols : col_first + (int)g.cols_per * S::BN;
   const ListRows<T> rows_a = list_rows(in, ld_in, k, g, end);
   const PlainRows<T> rows_b = plain_rows(g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out, g.d_in);
-  T* rows[S::TM];  // of the output
+  int ids[S::TM];  // rows of this lane's blocks, -1 for none
   const int m0 = p0 + (threadIdx.x >> 6) / S::WN * (S::TM * 16) + (threadIdx.x & 15);
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
     const int p = m0 + 16 * i, d = p < end ? (g.row_idx ? g.row_idx[p] : p) : -1;
-    rows[i] = (uint32_t)d < (uint32_t)g.n_rows ? out + (int64_t)d * ld_out : nullptr;
+    ids[i] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
   }
   typename S::RowsA a;
   B b;
@@ -162,7 +147,22 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& 
     zeros<S>(acc);
     tile_run<S, true>(lds, a, b, rows_a, rows_b, 0, k, acc, Nothing{});
     if (col + S::BN < col_last) begin_columns(col + S::BN);
-    store_rows<S>(acc, bias_all ? bias_all + (int64_t)leaf * cols : nullptr, rows, col, cols);
+    const int l = threadIdx.x & 63, wave_col = col + (int)(threadIdx.x >> 6) % S::WN * (S::TN * 16);
+    f32x4 add[S::TN];
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int n = wave_col + 16 * j + 4 * (l >> 4) + r;
+        add[j][r] = bias_all && n < cols ? (float)bias_all[(int64_t)leaf * cols + n] : 0.0f;
+      }
+    store_tile<S, T>(
+        lds + S::kLastStage, [&](int i, int j) { return acc[i][j] + add[j]; },
+        [&](int i, int r) {
+          const int d = __shfl(ids[i], r);
+          return d >= 0 ? out + (int64_t)d * ld_out : (T*)nullptr;
+        },
+        wave_col, cols);
   }
 }
 
@@ -203,16 +203,16 @@ struct RowSums {
 // The list's ids are copied to local memory first, kCopiedIds at a time: loads are waited for in order, so a row's address
 // that waits for an id on its way from memory waits for all chunks asked for before as well, and steps do not overlap.
 constexpr int kCopiedIds = 4096;
+constexpr int kShortPiece = 1024;  // positions
 
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
   __shared__ int ids[kCopiedIds];
-  const uint32_t tiles = g.col_tiles * g.row_tiles;
-  const int piece = (int)(t / tiles), r = (int)(t % tiles);
-  const int row0 = r / (int)g.col_tiles * S::BM, col0 = r % (int)g.col_tiles * S::BN;
+  // A piece's workgroups share its rows and so are one XCD's; pieces, which are of any length, go round.
+  const uint32_t tiles = g.col_tiles * g.row_tiles, at = blockIdx.x / 8;
+  const int piece = (int)(at / tiles * 8 + blockIdx.x % 8), r = (int)(at % tiles);
   const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, g.cut, piece);
   if (leaf < 0) return;
   const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
@@ -220,56 +220,87 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   const int64_t b0 = block * g.cut, b1 = b0 + g.cut;
   const int p0 = begin > b0 ? begin : (int)(b0 < end ? b0 : end), p1 = end < b1 ? end : (int)b1;
   if (p0 >= p1 && (end > begin || block != begin / g.cut)) return;  // only an empty leaf's one piece is empty: zeros
-  typename S::ColumnsA a;
-  typename S::ColumnsB b;
-  f32x4 acc[S::TM][S::TN];
-  zeros<S>(acc);
-  f32x4 sum[S::TM];
-#pragma unroll
-  for (int i = 0; i < S::TM; ++i) sum[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
-  const bool sums = g.dbias != nullptr && col0 == 0 && w % S::WN == 0;
-  for (int c0 = p0; c0 < p1; c0 += kCopiedIds) {
-    const int c1 = p1 - c0 < kCopiedIds ? p1 : c0 + kCopiedIds;
-    __syncthreads();  // the part before has been used
-    for (int p = c0 + (int)threadIdx.x; p < c1; p += S::NT) {
-      const int d = g.row_idx ? g.row_idx[p] : p;
-      ids[p - c0] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
-    }
-    __syncthreads();
-    const CopiedRows<T> rows_a = {g.dy, g.dy + (int64_t)(g.n_rows - 1) * g.ld_dy + g.d_out, g.ld_dy, ids, c0};
-    const CopiedRows<T> rows_b = {g.x, g.x + (int64_t)(g.n_rows - 1) * g.ld_x + g.d_in, g.ld_x, ids, c0};
-    a.init(rows_a, row0, g.d_out, c0, c1);
-    b.init(rows_b, col0, g.d_in, c0, c1);
-    tile_begin<S>(lds, a, b, rows_a, rows_b, c0, c1);
-    tile_run<S, true>(lds, a, b, rows_a, rows_b, c0, c1, acc, RowSums<S>{sum, sums});
-  }
-
+  // A short piece's column tiles are gone through cols_per at a time, one after another, by the first of its workgroups; the
+  // others leave.  (Not by every cols_per'th: workgroups go to an XCD's shader engines in turn as well.)
+  const int cols_per = p1 - p0 <= kShortPiece ? (int)g.cols_per : 1;
+  const int turns = ((int)g.col_tiles + cols_per - 1) / cols_per;
+  if (r >= turns * (int)g.row_tiles) return;
+  const int row0 = r / turns * S::BM, col_first = r % turns * cols_per * S::BN;
   const bool whole = begin >= b0 && end <= b1;
   const int64_t slot = 2 * block + (begin < b0 ? 0 : 1);
   float* part = g.partial + slot * ((int64_t)(g.d_in + 1) * g.d_out);
-  const int m0 = row0 + (w / S::WN) * (S::TM * 16), n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
+  const int all_cols = g.dw ? g.d_in : 1;  // (the outputs' sums alone come with the first tile)
+  const int col_last = all_cols < col_first + cols_per * S::BN ? all_cols : col_first + cols_per * S::BN;
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+  const int m0 = row0 + (w / S::WN) * (S::TM * 16);
+
+  typename S::ColumnsA a;
+  typename S::ColumnsB b;
+  CopiedRows<T> rows_a, rows_b;
+  int c0 = 0, c1 = 0, copied = -1;
+  // Positions from `from` on, of the column tile at `col`.
+  auto begin_part = [&](int from, int col) {
+    c0 = from;
+    c1 = p1 - c0 < kCopiedIds ? p1 : c0 + kCopiedIds;
+    if (copied != c0) {
+      __syncthreads();  // the part before has been used
+      for (int p = c0 + (int)threadIdx.x; p < c1; p += S::NT) {
+        const int d = g.row_idx ? g.row_idx[p] : p;
+        ids[p - c0] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
+      }
+      __syncthreads();
+      copied = c0;
+    }
+    rows_a = {g.dy, g.dy + (int64_t)(g.n_rows - 1) * g.ld_dy + g.d_out, g.ld_dy, (const __attribute__((address_space(3))) int*)ids, c0};
+    rows_b = {g.x, g.x + (int64_t)(g.n_rows - 1) * g.ld_x + g.d_in, g.ld_x, (const __attribute__((address_space(3))) int*)ids, c0};
+    a.init(rows_a, row0, g.d_out, c0, c1);
+    b.init(rows_b, col, g.d_in, c0, c1);
+    tile_begin<S>(lds, a, b, rows_a, rows_b, c0, c1);
+  };
+  begin_part(p0, col_first);
+  for (int col = col_first; col < col_last; col += S::BN) {
+    f32x4 acc[S::TM][S::TN];
+    zeros<S>(acc);
+    f32x4 sum[S::TM];
 #pragma unroll
-  for (int i = 0; i < S::TM; ++i) {
-    const int o = m0 + 16 * i + (l & 15);
-    if (o >= g.d_out) continue;
-    if (g.dw) {
+    for (int i = 0; i < S::TM; ++i) sum[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const bool sums = g.dbias != nullptr && col == 0 && w % S::WN == 0;
+    for (;;) {
+      tile_run<S, true>(lds, a, b, rows_a, rows_b, c0, c1, acc, RowSums<S>{sum, sums});
+      if (c1 >= p1) break;
+      begin_part(c1, col);
+    }
+    if (col + S::BN < col_last) begin_part(p0, col + S::BN);
+    const int wave_col = col + (w % S::WN) * (S::TN * 16);
+    if (g.dw && whole) {
+      store_tile<S, T>(
+          lds + S::kLastStage, [&](int i, int j) { return acc[i][j]; },
+          [&](int i, int r) {
+            const int o = m0 + 16 * i + r;
+            return o < g.d_out ? g.dw + ((int64_t)leaf * g.d_out + o) * g.d_in : (T*)nullptr;
+          },
+          wave_col, g.d_in);
+    } else if (g.dw) {
 #pragma unroll
-      for (int j = 0; j < S::TN; ++j) {
-        const int n = n0 + 16 * j;
-        if (n >= g.d_in) continue;
-        if (whole) {
-          store4(g.dw + ((int64_t)leaf * g.d_out + o) * g.d_in + n, acc[i][j], g.d_in - n);
-        } else {
-          store4(part + (int64_t)o * g.d_in + n, acc[i][j], g.d_in - n);
+      for (int i = 0; i < S::TM; ++i) {
+        const int o = m0 + 16 * i + (l & 15);
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+          const int n = wave_col + 16 * j + 4 * (l >> 4);
+          if (o < g.d_out && n < g.d_in) store4(part + (int64_t)o * g.d_in + n, acc[i][j], g.d_in - n);
         }
       }
     }
     if (sums && l < 16) {
-      if (whole) {
-        g.dbias[(int64_t)leaf * g.d_out + o] = (T)sum[i][0];
-      } else {
-        part[(int64_t)g.d_out * g.d_in + o] = sum[i][0];
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i) {
+        const int o = m0 + 16 * i + l;
+        if (o >= g.d_out) continue;
+        if (whole) {
+          g.dbias[(int64_t)leaf * g.d_out + o] = (T)sum[i][0];
+        } else {
+          part[(int64_t)g.d_out * g.d_in + o] = sum[i][0];
+        }
       }
     }
   }
@@ -280,15 +311,14 @@ template <typename T>
 __global__ void __launch_bounds__(256) leaf_grad_join_kernel(const LeafArgs<T> g) {
   const int64_t block = (int64_t)blockIdx.y + 1;
   const int64_t at = block * g.cut;
-  // the leaf that holds position at - 1 and position at
-  int lo = 0, hi = g.n_leaves;  // the largest leaf whose offset is < at
+  // the leaf that holds position at - 1 and position at: the last whose offset is < at
+  int lo = 0, hi = g.n_leaves;
   while (hi - lo > 1) {
-    const int mid = lo + (hi - lo) / 2;
-    if (offset_at(g.offsets, mid, g.n_positions) < at) {
-      lo = mid;
-    } else {
-      hi = mid;
-    }
+    const int step = (hi - lo + 63) / 64, i = lo + (int)(threadIdx.x & 63) * step;
+    const int n = __popcll(__ballot(i < hi && offset_at(g.offsets, i, g.n_positions) < at));
+    if (n == 0) return;
+    lo += (n - 1) * step;
+    hi = lo + step < hi ? lo + step : hi;
   }
   const int begin = offset_at(g.offsets, lo, g.n_positions), end = offset_at(g.offsets, lo + 1, g.n_positions);
   if (begin >= at || end <= at || begin < at - g.cut) return;

@@ -30,6 +30,7 @@ using gbdt_tile::Shape;
 
 constexpr int64_t kMaxRows = (int64_t)1 << 30;     // rows, positions, classes
 constexpr int64_t kMaxWidth = (int64_t)1 << 24;    // d_in, d_out, dim, leaves
+constexpr int64_t kMaxLd = (int64_t)1 << 28;       // distances of rows
 constexpr int64_t kMaxBlocks = ((int64_t)1 << 31) - 1;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -132,7 +133,11 @@ int launch_leaf_grad_weight(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   if (S::BM != grad_bm(sizeof(T), g.d_out) || S::BN != grad_bn(sizeof(T))) return GBDT_EUNSUPPORTED;  // (leaf_tiles counts these)
   g.col_tiles = (uint32_t)(g.dw ? ceil_div(g.d_in, S::BN) : 1);
   g.row_tiles = (uint32_t)ceil_div(g.d_out, S::BM);
-  const int64_t blocks = ((int64_t)g.n_positions / g.cut + g.n_leaves) * g.col_tiles * g.row_tiles;
+  // (as leaf_rows_grid: eight workgroups a unit, counting a piece a cut)
+  const int64_t pieces = (int64_t)g.n_positions / g.cut + g.n_leaves;
+  const int64_t tiles = pieces * g.col_tiles * g.row_tiles;
+  g.cols_per = (uint32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)g.col_tiles, tiles / (8 * gbdt_internal::cu_count()), 4}));
+  const int64_t blocks = round_up(pieces, 8) * g.col_tiles * g.row_tiles;
   if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
   gbdt_leaf::leaf_grad_weight_kernel<S><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
   LAUNCHED("leaf_grad_weight_kernel");
@@ -169,8 +174,10 @@ int leaf_product_grad(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   if (rc != GBDT_OK) return rc;
   const int64_t cuts = ceil_div(g.n_positions, g.cut) - 1;
   if (cuts > 0) {
+    // (few workgroups a cut: most find that no leaf crosses theirs first)
     const int64_t per = ceil_div((int64_t)(g.d_in + 1) * g.d_out, 256);
-    gbdt_leaf::leaf_grad_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(per, 2048), (unsigned)cuts), dim3(256), 0, s>>>(g);
+    const int64_t most = std::max<int64_t>(16, 4096 / cuts);
+    gbdt_leaf::leaf_grad_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(per, most), (unsigned)cuts), dim3(256), 0, s>>>(g);
     LAUNCHED("leaf_grad_join_kernel");
   }
   return GBDT_OK;
@@ -187,7 +194,7 @@ int softmax_check(const void* h, int64_t ld_h, const void* c, int64_t ld_c, int6
   if (n_rows < 0 || n_classes <= 0 || dim <= 0 || !c || (!h && n_rows > 0) || ld_h < dim || ld_c < dim) return GBDT_EINVAL;
   if (dtype != GBDT_F32 && dtype != GBDT_BF16) return GBDT_EINVAL;
   if (off_element(h, dtype) || off_element(c, dtype)) return GBDT_EINVAL;
-  if (n_rows >= kMaxRows || n_classes >= kMaxRows || dim >= kMaxWidth) return GBDT_EUNSUPPORTED;
+  if (n_rows >= kMaxRows || n_classes >= kMaxRows || dim >= kMaxWidth || ld_h >= kMaxLd || ld_c >= kMaxLd) return GBDT_EUNSUPPORTED;
   return GBDT_OK;
 }
 
@@ -549,6 +556,7 @@ int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const voi
   if (ld_x < d_in || ld_y < d_out || !weight || off_element(x, dtype) || off_element(weight, dtype) || off_element(bias, dtype) ||
       off_element(y_out, dtype))
     return GBDT_EINVAL;
+  if (ld_x >= kMaxLd || ld_y >= kMaxLd) return GBDT_EUNSUPPORTED;
   if (n_positions == 0 || n_rows == 0) return GBDT_OK;
   if (!x || !y_out) return GBDT_EINVAL;
   hipStream_t s = (hipStream_t)stream;
@@ -576,6 +584,7 @@ int gbdt_leaf_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t
   if (off_element(dy, dtype) || off_element(x, dtype) || off_element(weight, dtype) || off_element(dx_out, dtype) ||
       off_element(dweight_out, dtype) || off_element(dbias_out, dtype))
     return GBDT_EINVAL;
+  if (ld_dy >= kMaxLd || ld_x >= kMaxLd || ld_dx >= kMaxLd) return GBDT_EUNSUPPORTED;
   if (n_rows == 0) n_positions = 0;
   if (n_positions > 0 && (!dy || (dweight_out && !x))) return GBDT_EINVAL;
   hipStream_t s = (hipStream_t)stream;

@@ -233,33 +233,34 @@ __global__ void __launch_bounds__(S::NT, 2) softmax_piece_kernel(const ScoreArgs
     const int n0 = col0 + wave_n;
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) {
-      const int d = row0 + m0 + 16 * i;
       const int y = f.y[i];
       const bool use = (uint32_t)y < (uint32_t)g.n_classes;
-      f32x4 v[S::TN];
 #pragma unroll
       for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[j][r] = f.weight[i] * exp_diff(acc[i][j][r], f.lse[i]);
+        for (int r = 0; r < 4; ++r) acc[i][j][r] = f.weight[i] * exp_diff(acc[i][j][r], f.lse[i]);
       const int rel = y - n0;  // rarely here
       if (rel >= 0 && rel < 16 * S::TN && (rel & 15) < 4) {
 #pragma unroll
         for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) v[j][r] -= rel == 16 * j + r ? f.weight[i] : 0.0f;
+          for (int r = 0; r < 4; ++r) acc[i][j][r] -= rel == 16 * j + r ? f.weight[i] : 0.0f;
       }
       if (!use || col0 + S::BN > g.end) {
 #pragma unroll
         for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) v[j][r] = use && n0 + 16 * j + r < g.end ? v[j][r] : 0.0f;
-      }
-      if (d < g.n_rows) {
-        T* to = g.g + (int64_t)d * g.ld_g - g.begin + n0;
-#pragma unroll
-        for (int j = 0; j < S::TN; ++j) store4(to + 16 * j, v[j], 4);
+          for (int r = 0; r < 4; ++r) acc[i][j][r] = use && n0 + 16 * j + r < g.end ? acc[i][j][r] : 0.0f;
       }
     }
+    const int wave_row = row0 + (w / S::WN) * (S::TM * 16);
+    store_tile<S, T>(
+        lds + S::kLastStage, [&](int i, int j) { return acc[i][j]; },
+        [&](int i, int r) {
+          const int d = wave_row + 16 * i + r;
+          return d < g.n_rows ? g.g + (int64_t)d * g.ld_g - g.begin : (T*)nullptr;
+        },
+        n0 - 4 * (l >> 4), g.begin + (int)g.ld_g);
   });
 }
 
@@ -352,6 +353,11 @@ struct PieceArgs {
   uint32_t row_tiles, col_tiles, splits, group;
 };
 
+template <typename T>
+__device__ __forceinline__ bool counts(const PieceArgs<T>& g, int row) {
+  return (uint32_t)g.labels[row] < (uint32_t)g.n_classes;
+}
+
 // TO_ROWS: dh (the result's rows are G's rows, k = classes); otherwise dC (its rows are classes, k = G's rows).
 template <class S, bool TO_ROWS>
 __global__ void __launch_bounds__(S::NT, 2) piece_product_kernel(const PieceArgs<typename S::T> g) {
@@ -383,31 +389,46 @@ __global__ void __launch_bounds__(S::NT, 2) piece_product_kernel(const PieceArgs
     tile_product<S, true>(lds, a, b, rows_a, rows_b, k0, k1, acc, Nothing{});
   }
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int m0 = row0 + (w / S::WN) * (S::TM * 16), n0 = col0 + (w % S::WN) * (S::TN * 16) + 4 * (l >> 4);
-  float* sums = g.sums ? g.sums + (int64_t)split * g.rows * g.cols : nullptr;
+  const int m0 = row0 + (w / S::WN) * (S::TM * 16), wave_col = col0 + (w % S::WN) * (S::TN * 16);
+  if (!g.sums) {
+    store_tile<S, T>(
+        lds + S::kLastStage, [&](int i, int j) { return g.scale * acc[i][j]; },
+        [&](int i, int r) {
+          const int m = m0 + 16 * i + r;
+          return m < g.rows && (!TO_ROWS || counts(g, m)) ? g.out + (int64_t)m * g.ld_out : (T*)nullptr;
+        },
+        wave_col, g.cols);
+    if (TO_ROWS) {  // rows that do not count are zeros, whatever C holds
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i) {
+        const int m = m0 + 16 * i + (l & 15);
+        if (m >= g.rows || counts(g, m)) continue;
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+          const int n = wave_col + 16 * j + 4 * (l >> 4);
+          if (n < g.cols) store4(g.out + (int64_t)m * g.ld_out + n, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, g.cols - n);
+        }
+      }
+    }
+    return;
+  }
+  float* sums = g.sums + (int64_t)split * g.rows * g.cols;
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
     const int m = m0 + 16 * i + (l & 15);
     if (m >= g.rows) continue;
-    const bool use = !TO_ROWS || (uint32_t)g.labels[m] < (uint32_t)g.n_classes;
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
-      const int n = n0 + 16 * j;
+      const int n = wave_col + 16 * j + 4 * (l >> 4);
       if (n >= g.cols) continue;
       f32x4 v = acc[i][j];
-      if (sums) {
-        float* to = sums + (int64_t)m * g.cols + n;
-        if (g.add) {
+      float* to = sums + (int64_t)m * g.cols + n;
+      if (g.add) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (n + r < g.cols) v[r] += to[r];
-        }
-        store4(to, v, g.cols - n);
-      } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = use ? g.scale * v[r] : 0.0f;
-        store4(g.out + (int64_t)m * g.ld_out + n, v, g.cols - n);
+        for (int r = 0; r < 4; ++r)
+          if (n + r < g.cols) v[r] += to[r];
       }
+      store4(to, v, g.cols - n);
     }
   }
 }
