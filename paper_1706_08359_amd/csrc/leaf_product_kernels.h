@@ -39,7 +39,8 @@ __device__ __forceinline__ int offset_at(const int64_t* offsets, int l, int n_po
   return o < 0 ? 0 : o > n_positions ? n_positions : (int)o;
 }
 
-// The largest leaf l with offset(l) / unit + l <= tile, by 64 probes at a time; -1 if there is none.
+// The largest leaf l with T(l) = offset(l) / unit + l <= tile (unit 0: with offset(l) <= tile), by 64 probes at a time; -1 if
+// there is none.
 __device__ __forceinline__ int find_leaf(const int64_t* offsets, int n_leaves, int n_positions, int unit, int tile) {
   const int lane = threadIdx.x & 63;
   int lo = 0, hi = n_leaves;
@@ -47,7 +48,11 @@ __device__ __forceinline__ int find_leaf(const int64_t* offsets, int n_leaves, i
   while (hi - lo > 1 || !any) {
     const int step = (hi - lo + 63) / 64;
     const int i = lo + lane * step;
-    const bool ok = i < hi && offset_at(offsets, i, n_positions) / unit + i <= tile;
+    bool ok = i < hi;
+    if (ok) {
+      const int o = offset_at(offsets, i, n_positions);
+      ok = (unit ? o / unit + i : o) <= tile;
+    }
     const int n = __popcll(__ballot(ok));
     if (n == 0) return -1;
     any = true;
@@ -180,6 +185,58 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_input_kernel(const LeafArg
   leaf_rows_product<S, typename S::ColumnsB>(lds, g, g.dy, g.ld_dy, g.d_out, (const typename S::T*)nullptr, g.dx, g.ld_dx, g.d_in);
 }
 
+// A few positions (a row or a few answered at once): a wavefront takes OUTPUTS outputs of one position, each lane a chunk of k
+// of every 64, and adds up across the lanes.  There is nothing to share between rows, so the leaf's matrix is read once a
+// position, by as many compute units as there are outputs; a tile of 128 rows on the matrix cores reads it by two workgroups.
+// The end of a row that is no whole chunk is read as the last whole chunk, whose values before it count for nothing.
+template <typename T, int OUTPUTS>
+__global__ void __launch_bounds__(64) leaf_product_few_kernel(const LeafArgs<T> g) {
+  const int p = (int)blockIdx.y, o0 = (int)blockIdx.x * OUTPUTS, l = threadIdx.x;
+  const int d = g.row_idx ? g.row_idx[p] : p;
+  // the last leaf that begins at or before p
+  const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, 0, p);
+  if (leaf < 0 || (uint32_t)d >= (uint32_t)g.n_rows || p >= offset_at(g.offsets, leaf + 1, g.n_positions)) return;
+  const T* x = row_of(g.x, d, g.ld_x);
+  const T* w = g.w + ((int64_t)leaf * g.d_out + o0) * g.d_in;
+  constexpr int n = kChunk<T>;
+  float sum[OUTPUTS];
+#pragma unroll
+  for (int i = 0; i < OUTPUTS; ++i) sum[i] = 0.0f;
+  if (g.d_in >= n) {
+#pragma unroll 2
+    for (int k = l * n; k < g.d_in; k += 64 * n) {
+      const int at = k + n <= g.d_in ? k : g.d_in - n, skip = k - at;
+      const u32x4 xc = load16(x + at);
+      u32x4 wc[OUTPUTS];
+#pragma unroll
+      for (int i = 0; i < OUTPUTS; ++i) wc[i] = load16(w + (o0 + i < g.d_out ? (int64_t)i * g.d_in : 0) + at);
+      T xv[n], wv[n];
+      __builtin_memcpy(xv, &xc, 16);
+#pragma unroll
+      for (int i = 0; i < OUTPUTS; ++i) {
+        __builtin_memcpy(wv, &wc[i], 16);
+#pragma unroll
+        for (int e = 0; e < n; ++e) sum[i] = e >= skip ? __builtin_fmaf((float)xv[e], (float)wv[e], sum[i]) : sum[i];
+      }
+    }
+  } else if (l < g.d_in) {
+#pragma unroll
+    for (int i = 0; i < OUTPUTS; ++i)
+      if (o0 + i < g.d_out) sum[i] = (float)x[l] * (float)w[(int64_t)i * g.d_in + l];
+  }
+#pragma unroll
+  for (int i = 0; i < OUTPUTS; ++i) {
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) sum[i] += __shfl_xor(sum[i], s);
+  }
+  if (l != 0) return;
+#pragma unroll
+  for (int i = 0; i < OUTPUTS; ++i) {
+    const int o = o0 + i;
+    if (o < g.d_out) g.y[(int64_t)d * g.ld_y + o] = (T)(g.bias ? sum[i] + (float)g.bias[(int64_t)leaf * g.d_out + o] : sum[i]);
+  }
+}
+
 // Sums over k of operand a's rows, by a product with ones: every n of the block holds the sum for its m.
 template <class S>
 struct RowSums {
@@ -264,7 +321,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
     f32x4 sum[S::TM];
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) sum[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const bool sums = g.dbias != nullptr && col == 0 && w % S::WN == 0;
+    const bool sums = __builtin_amdgcn_readfirstlane(g.dbias != nullptr && col == 0 && w % S::WN == 0);
     for (;;) {
       tile_run<S, true>(lds, a, b, rows_a, rows_b, c0, c1, acc, RowSums<S>{sum, sums});
       if (c1 >= p1) break;

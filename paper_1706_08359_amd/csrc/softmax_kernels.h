@@ -188,19 +188,21 @@ __global__ void __launch_bounds__(S::NT, 2) softmax_scores_kernel(const ScoreArg
   });
 }
 
-// Joins a row's parts: 16 lanes a row, each every 16th part in order, then pairwise.
+// Joins a row's parts: 256 / ROWS lanes a row, each every so manieth part in order, then pairwise.  16 rows a workgroup read
+// whole lines; one row a workgroup has 391 parts (50,000 classes) joined in 3 us where 16 lanes take 12.
+template <int ROWS>
 __global__ void __launch_bounds__(256) softmax_join_kernel(const MaxSum* parts, const float* picked, const int32_t* labels, int32_t n_rows,
                                                            int32_t n_classes, int32_t tiles, float* loss, float* lse) {
-  const int d0 = blockIdx.x * 16;
-  const int i = threadIdx.x & 15, q = threadIdx.x >> 4;  // row of the block, turn
-  __shared__ MaxSum all[16][17];
-  const int d = d0 + i;
+  constexpr int lanes = 256 / ROWS;
+  const int i = threadIdx.x % ROWS, q = threadIdx.x / ROWS;  // row of the workgroup, turn
+  __shared__ MaxSum all[lanes][ROWS + (ROWS > 1)];
+  const int d = blockIdx.x * ROWS + i;
   MaxSum p = {-__builtin_inff(), 0.0f};
   if (d < n_rows)
-    for (int t = q; t < tiles; t += 16) p = join(p, parts[(int64_t)t * n_rows + d]);
+    for (int t = q; t < tiles; t += lanes) p = join(p, parts[(int64_t)t * n_rows + d]);
   all[q][i] = p;
   __syncthreads();
-  for (int k = 8; k > 0; k >>= 1) {
+  for (int k = lanes / 2; k > 0; k >>= 1) {
     if (q < k) all[q][i] = join(all[q][i], all[q + k][i]);
     __syncthreads();
   }
