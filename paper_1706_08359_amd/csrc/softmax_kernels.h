@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(S::NT, 2) softmax_piece_kernel(const ScoreArgs
       }
     }
     const int wave_row = row0 + (w / S::WN) * (S::TM * 16);
-    store_tile<S, T>(
+    store_tile<S, T, S::TM, S::TN>(
         lds + S::kLastStage, [&](int i, int j) { return acc[i][j]; },
         [&](int i, int r) {
           const int d = wave_row + 16 * i + r;
@@ -289,28 +289,36 @@ __global__ void __launch_bounds__(S::NT, 2) softmax_stats_kernel(const ScoreArgs
   };
   for_score_tiles<S, false>(lds, g, fetch, [&](f32x4(&acc)[S::TM][S::TN], const OfFourRows& f, int row0, int col0) {
     const int n0 = col0 + wave_n;
+    // p in place of the scores
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i) {
-      const int d = row0 + m0 + 16 * i;
+    for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-      for (int j = 0; j < S::TN; ++j) {
-        const int n = n0 + 16 * j;
-        f32x4 grad, hess;
+      for (int r = 0; r < 4; ++r) {
+        const bool use = g.labels == nullptr || (uint32_t)f.y[i][r] < (uint32_t)g.n_classes;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const bool use = g.labels == nullptr || (uint32_t)f.y[i][r] < (uint32_t)g.n_classes;
+        for (int j = 0; j < S::TN; ++j) {
           const float e = exp_diff(acc[i][j][r], f.lse[i][r]);
-          const float p = use ? e : 0.0f;
-          grad[r] = n == f.y[i][r] ? p - 1.0f : p;
-          hess[r] = p * (1.0f - p);
-        }
-        if (d < g.n_rows && n < g.end) {
-          const int64_t at = (int64_t)(n - g.begin) * g.ld_out + d;
-          store4(g.grad + at, grad, g.n_rows - d);
-          store4(g.hess + at, hess, g.n_rows - d);
+          acc[i][j][r] = use ? e : 0.0f;
         }
       }
-    }
+    const int wave_row = row0 + (w / S::WN) * (S::TM * 16);
+    auto column = [&](float* out) {
+      return [&g, out, n0, l](int j, int c) {
+        const int n = n0 - (l & 15) + 16 * j + c;
+        return n < g.end ? out + (int64_t)(n - g.begin) * g.ld_out : (float*)nullptr;
+      };
+    };
+    store_tile<S, float, S::TN, S::TM>(
+        lds + S::kLastStage, [&](int j, int i) { return acc[i][j] * (1.0f - acc[i][j]); }, column(g.hess), wave_row, g.n_rows);
+    store_tile<S, float, S::TN, S::TM>(
+        lds + S::kLastStage,
+        [&](int j, int i) {
+          f32x4 v = acc[i][j];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = n0 + 16 * j == f.y[i][r] ? v[r] - 1.0f : v[r];
+          return v;
+        },
+        column(g.grad), wave_row, g.n_rows);
   });
 }
 
@@ -393,7 +401,7 @@ __global__ void __launch_bounds__(S::NT, 2) piece_product_kernel(const PieceArgs
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int m0 = row0 + (w / S::WN) * (S::TM * 16), wave_col = col0 + (w % S::WN) * (S::TN * 16);
   if (!g.sums) {
-    store_tile<S, T>(
+    store_tile<S, T, S::TM, S::TN>(
         lds + S::kLastStage, [&](int i, int j) { return g.scale * acc[i][j]; },
         [&](int i, int r) {
           const int m = m0 + 16 * i + r;

@@ -689,24 +689,25 @@ __device__ __forceinline__ void store4(T* p, f32x4 v, int valid) {
   }
 }
 
-// Stores a wavefront's tile (N_INNER) by whole 16-byte chunks of its rows: each block of 16 rows goes through a piece of local
+// Stores a wavefront's tile, ROWS blocks of 16 rows of INNER x 16 values (N_INNER: TM and TN; the other way round: TN and TM),
+// by whole 16-byte chunks of its rows: each block of 16 rows goes through a piece of local
 // memory of the wavefront's own, so that a store writes lines of 128 bytes at once.  (Straight from the registers a store
 // writes 32 bytes of each of 16 rows, and the next 96 of them come with the stores after it: 100,000 x 256 -> 2,000 bf16,
 // gradient of the input, 341 us so against 210 us without any stores.)
 //   value(i, j): the four values of the block; row(i, r): where row r of block i begins, or null; col0, cols: the wavefront's
 //   first column and the end of the rows.  scratch: of the workgroup, the last stage, which tile_begin does not touch.
-template <class S, typename O, class Value, class Row>
+template <class S, typename O, int ROWS, int INNER, class Value, class Row>
 __device__ __forceinline__ void store_tile(char* scratch, const Value& value, const Row& row, int col0, int cols) {
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  constexpr int row_bytes = S::TN * 16 * (int)sizeof(O);
+  constexpr int row_bytes = INNER * 16 * (int)sizeof(O);
   if constexpr (row_bytes >= 128) {
     constexpr int chunks = row_bytes / 16, at_once = 64 / chunks, n = 16 / (int)sizeof(O);
     static_assert(S::WM * S::WN * 16 * row_bytes <= S::kStageBytes, "a piece a wavefront");
     char* mine = scratch + w * (16 * row_bytes);
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
 #pragma unroll
-      for (int j = 0; j < S::TN; ++j) {
+      for (int j = 0; j < INNER; ++j) {
         const f32x4 v = value(i, j);
         const O t[4] = {(O)v[0], (O)v[1], (O)v[2], (O)v[3]};
         const int byte = (16 * j + 4 * (l >> 4)) * (int)sizeof(O), r = l & 15;
@@ -734,11 +735,11 @@ __device__ __forceinline__ void store_tile(char* scratch, const Value& value, co
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
       O* to = row(i, l & 15);
       if (to == nullptr) continue;
 #pragma unroll
-      for (int j = 0; j < S::TN; ++j) {
+      for (int j = 0; j < INNER; ++j) {
         const int at = col0 + 16 * j + 4 * (l >> 4);
         if (at < cols) store4(to + at, value(i, j), cols - at);
       }
