@@ -316,8 +316,8 @@ struct GradPlan {
   int64_t width;   // classes a piece
   int64_t pieces;
   int64_t dh_splits, dh_split, dc_splits, dc_split;
-  size_t g_bytes, dh_bytes, dc_bytes, h_bytes, c_bytes;
-  size_t bytes() const { return g_bytes + dh_bytes + dc_bytes + h_bytes + c_bytes; }
+  size_t g_bytes, dh_bytes, dc_bytes, h_bytes, c_bytes, rest_bytes;
+  size_t bytes() const { return g_bytes + dh_bytes + dc_bytes + h_bytes + c_bytes + rest_bytes; }
 };
 // Splits of a summed axis of `k`: as many as give `units` workgroups work, each 4 steps long at least.
 void split_axis(int64_t tiles, int64_t k, int64_t step, int64_t units, int64_t* splits, int64_t* len) {
@@ -348,6 +348,7 @@ GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, bo
   p.dc_bytes = p.dc_splits > 1 ? pad256((size_t)(p.dc_splits * p.width * dim) * 4) : 0;
   const int64_t row_bytes = round_up(dim * e, 16);
   p.h_bytes = pad256((size_t)(rows * row_bytes));
+  p.rest_bytes = e == 2 ? pad256((size_t)rows * 4) : 0;
   p.c_bytes = c_whole ? 0 : pad256((size_t)(n_classes * row_bytes));
   return p;
 }
@@ -388,7 +389,7 @@ int launch_product(gbdt_softmax::PieceArgs<T>& g, hipStream_t s) {
 
 template <typename T>
 int join_product(const gbdt_softmax::PieceArgs<T>& g, hipStream_t s) {
-  const int64_t n = ceil_div((int64_t)g.rows * g.cols, 256);
+  const int64_t n = ceil_div((int64_t)g.rows * ceil_div(g.cols, 4), 256);
   if (n == 0) return GBDT_OK;
   gbdt_softmax::piece_join_kernel<T><<<dim3((unsigned)std::min<int64_t>(n, 16384)), dim3(256), 0, s>>>(g);
   LAUNCHED("piece_join_kernel");
@@ -411,6 +412,8 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
   at += plan.dh_bytes;
   float* dc_sums = plan.dc_bytes ? (float*)at : nullptr;
   at += plan.dc_bytes;
+  float* rest = plan.rest_bytes ? (float*)at : nullptr;
+  at += plan.rest_bytes;
   // Both matrices are of whole chunks from here on; whole_dim is the length of their rows.
   const int32_t whole_dim = (int32_t)round_up(dim, kChunk<T>);
   if ((rc = whole_rows<T>(h, ld_h, (T*)at, n_rows, dim, labels, n_classes, s)) != GBDT_OK) return rc;
@@ -433,6 +436,7 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
     g.lse = lse;
     g.weight = weight;
     g.g = piece;
+    g.rest = rest;
     g.ld_h = ld_h;
     g.ld_c = ld_c;
     g.ld_g = plan.width;
@@ -448,6 +452,9 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
       to_c.b = h;
       to_c.out = dc + begin * ld_dc;
       to_c.sums = dc_sums;
+      to_c.labels = labels;
+      to_c.rest = rest;
+      to_c.class0 = (int32_t)begin;
       to_c.ld_a = plan.width;
       to_c.ld_b = ld_h;
       to_c.ld_out = ld_dc;
@@ -461,7 +468,11 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
       to_c.splits = (uint32_t)plan.dc_splits;
       rc = wide_tiles<T>(to_c.rows, dim) ? launch_product<Wide<T>, false>(to_c, s) : launch_product<Small, false>(to_c, s);
       if (rc != GBDT_OK) return rc;
-      if (dc_sums && (rc = join_product(to_c, s)) != GBDT_OK) return rc;
+      if (dc_sums) {
+        gbdt_softmax::PieceArgs<T> sums = to_c;
+        sums.labels = nullptr;
+        if ((rc = join_product(sums, s)) != GBDT_OK) return rc;
+      }
     }
     if (dh && n_rows > 0) {
       to_h.a = piece;
@@ -469,6 +480,9 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
       to_h.out = dh;
       to_h.sums = dh_sums;
       to_h.labels = labels;
+      to_h.rest = rest;
+      to_h.c = c;
+      to_h.ld_c = ld_c;
       to_h.ld_a = plan.width;
       to_h.ld_b = ld_c;
       to_h.ld_out = ld_dh;

@@ -116,6 +116,7 @@ struct RowOperand {
   static constexpr int kRowChunks = KB / 16;
   static constexpr int kSlots = R * kRowChunks;
   static constexpr int kPer = (kSlots + NT - 1) / NT;
+  static constexpr int kLoads = kPer;  // of device memory, a step
   static constexpr int kBytes = R * KB;
   static constexpr int kReads = 1;  // a fragment
   const T* row[kPer];  // DIRECT: of the chunk that is loaded next
@@ -230,6 +231,7 @@ struct ColumnOperand {
   static constexpr int kStep = KB / (int)sizeof(T);
   static constexpr int kSlots = R * (KB / 16);
   static constexpr int kPer = (kSlots + NT - 1) / NT;
+  static constexpr int kLoads = kPer;  // of device memory, a step
   static constexpr int kBytes = R * KB;
   static constexpr int kChunks = R / kChunk<T>;  // a row
   static constexpr int kReads = sizeof(T) == 2 ? 2 : 4;
@@ -381,6 +383,42 @@ struct ColumnOperand {
   }
 };
 
+// A column operand (bf16) whose row k has one value that is not zero, as rows.fetch(k) tells: its column in the upper half of
+// the word and its bits in the lower, -1 for none.  Made in the stage, not loaded.
+template <int R, int NT, int KB>
+struct OneHotOperand : ColumnOperand<bf16, R, NT, true, KB> {
+  typedef ColumnOperand<bf16, R, NT, true, KB> Base;
+  static constexpr int kLoads = 0;
+  template <class Rows>
+  __device__ __forceinline__ void init(const Rows&, int k0, int k1) {
+    this->k_at = k0;
+    this->k_end = k1;
+    this->c0 = 0;
+    this->lim = R;
+  }
+  template <bool WHOLE, class Rows>
+  __device__ __forceinline__ void load_one(const Rows& rows, char* stage, int i) {
+    const int k = this->k_at + Base::slot_k(i), c = this->slot_column(i);
+    const int entry = k < this->k_end ? rows.fetch(k) : -1;
+    const int at = (entry >> 16) - c;
+    u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (at == e) v[e / 2] = ((uint32_t)entry & 0xffffu) << (e % 2 * 16);
+    *(u32x4*)(stage + (i * NT + (int)threadIdx.x) * 16) = v;
+  }
+  template <class Rows>
+  __device__ __forceinline__ void advance(const Rows&) {
+    this->k_at += Base::kStep;
+  }
+  template <class Rows>
+  __device__ __forceinline__ void load(const Rows& rows, char* stage) {
+#pragma unroll
+    for (int i = 0; i < Base::kPer; ++i) load_one<false>(rows, stage, i);
+    advance(rows);
+  }
+};
+
 __device__ __forceinline__ f32x4 mma(bf16x8 rows, bf16x8 cols, f32x4 acc) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(rows, cols, acc, 0, 0, 0);
 }
@@ -508,7 +546,7 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
     // at once wait for the address units before they can go on to multiply.  (With two stages of twice the length a chunk
     // would have to be on its way before the next turn.)  Turns go in pairs, so that the fragments' places are known to the
     // compiler; an odd number is filled up with zeros.
-    constexpr int per = A::kPer + B::kPer;
+    constexpr int per = A::kPer + B::kPer, loads = A::kLoads + B::kLoads;
     const int full = ((a.k_end < b.k_end ? a.k_end : b.k_end) - k0) / S::kStep;  // steps whose every chunk is loaded
     const int turns = (steps + 1) / 2 * 2;
     auto load_one = [&](auto whole, int step, int i) {
@@ -550,7 +588,7 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
       }
       // The next step is there; the two behind it may be on their way.
       if (decltype(whole)::value) {
-        arrived<2 * per>();
+        arrived<2 * loads>();
       } else {
         arrived<0>();
       }
@@ -561,7 +599,7 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
       in_order();
     };
     if (full > 2) {
-      arrived<2 * per>();
+      arrived<2 * loads>();
     } else {
       arrived<0>();
     }
@@ -601,12 +639,12 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
     if constexpr (S::DIRECT) {
       // A stage is given up two blocks before its step ends, when all of it has been read, and the step kStages later goes
       // there: one barrier a step is enough, and the last two blocks cover the first reads of the next stage.
-      constexpr int ns = S::kStages, per = A::kPer + B::kPer;
+      constexpr int ns = S::kStages, loads = A::kLoads + B::kLoads;
       const int full = ((a.k_end < b.k_end ? a.k_end : b.k_end) - k0) / S::kStep;  // steps whose every chunk is loaded
       // Step `next` is there; the kStages - 2 behind it may be on their way.
       auto wait = [&](int next) {
         if (ns > 2 && next + ns - 2 < full) {
-          arrived<(ns - 2) * per>();
+          arrived<(ns - 2) * loads>();
         } else {
           arrived<0>();
         }

@@ -57,6 +57,10 @@ CASES = [
     (900, [513, 127, 260], 200, 264, 1),
     (2, [2], 2000, 3, 0),
     (64, [30, 34], 129, 1, 0),
+    (64, [10, 0, 54], 100, 70, 0),
+    (64, [3, 61], 5, 40, 1),
+    (2000, [700, 650, 650], 264, 200, 0),
+    (1200, [300, 800, 0, 100], 72, 48, 0),
 ]
 
 
@@ -100,6 +104,16 @@ def test_long_leaves_are_summed_in_parts(sizes, dtype):
         assert only[1] is None and torch.equal(only[2], got[2])
         only = B.gbdt_leaf_product_grad(dy, x, w, offs, row_idx=idx, want=("weight",))
         assert only[2] is None and torch.equal(only[1], got[1])
+
+
+def test_pieces_longer_than_a_copy_of_their_list():
+    """So much work a position that pieces are thousands of positions long."""
+    from paper_1706_08359_amd import binding as B
+    x, dy, w, b, offs, idx = make(70_100, [62_000, 0, 100, 8000], 2000, 200, "bf16", seed=4)
+    got = B.gbdt_leaf_product_grad(dy, x, w, offs, row_idx=idx, want=("weight", "bias"))
+    want, mags = ref.leaf_product_grad(dy, x, w, offs, idx, torch.zeros(70_100, 1, device="cuda").expand(70_100, 2000))
+    for i in (1, 2):
+        close(got[i], want[i], mags[i], 62_000, i)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -200,6 +200,30 @@ def test_several_pieces_of_classes_and_parts_of_rows(dtype):
     assert only[0] is None and torch.equal(only[1], first[1])
 
 
+def test_many_rows_of_few_classes_and_many_dimensions():
+    """More rows of a tile's classes in one workgroup's share than it lists at a time."""
+    from paper_1706_08359_amd import binding as B
+    h, c, y, w = make(8000, 10, 8192, "bf16", seed=9, scale=1.0)
+    _, lse = check_loss(B, h, c, y)
+    first = check_grad(B, h, c, y, w, 1.0 / 8000, lse)
+    again = B.gbdt_softmax_grad(h, c, y, lse, row_weight=w, scale=1.0 / 8000)
+    assert all(torch.equal(a, e) for a, e in zip(first, again))
+
+
+@pytest.mark.parametrize("n,v,dim", [(1, 3000, 64), (40, 2000, 512), (700, 5000, 256)])
+def test_bf16_gradients_are_as_exact_as_their_own_rounding(n, v, dim):
+    """Root mean square error below 1.25 times that of the exact results rounded to bf16: among many classes the label's
+    element outweighs its row and its column, and it must not be rounded before the product."""
+    from paper_1706_08359_amd import binding as B
+    h, c, y, w = make(n, v, dim, "bf16", seed=10, ignore=0.0)
+    _, lse = B.gbdt_softmax_loss(h, c, y)
+    got = B.gbdt_softmax_grad(h, c, y, lse, row_weight=w, scale=0.3)
+    want, _ = ref.softmax_grad(h, c, y, lse, w, 0.3)
+    for a, e in zip(got, want):
+        err = float((a.double() - e).norm())
+        assert err <= 1.25 * float((e.bfloat16().double() - e).norm()), (n, v, dim)
+
+
 def test_loss_takes_many_rows_in_turns():
     """More maxima and sums than one launch's scratch holds."""
     from paper_1706_08359_amd import binding as B
