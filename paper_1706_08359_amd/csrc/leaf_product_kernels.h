@@ -237,18 +237,19 @@ __global__ void __launch_bounds__(64) leaf_product_few_kernel(const LeafArgs<T> 
   }
 }
 
-// Sums over k of operand a's rows, by a product with ones: every n of the block holds the sum for its m.
+// Sums over k of operand a's rows: every lane those of its values, of its row of each block.  (One register a block; a product
+// with ones takes four.)
 template <class S>
 struct RowSums {
-  f32x4 (&sum)[S::TM];
+  float (&sum)[S::TM];
   bool on;
   template <class F>
   __device__ __forceinline__ void operator()(int i, const F& rows) const {
     if (!on) return;
-    F ones;
+    float s = (float)rows[0];
 #pragma unroll
-    for (int k = 0; k < kChunk<typename S::T>; ++k) ones[k] = (typename S::T)1.0f;
-    sum[i] = mma(ones, rows, sum[i]);
+    for (int k = 1; k < kChunk<typename S::T>; ++k) s += (float)rows[k];
+    sum[i] += s;
   }
 };
 
@@ -257,10 +258,32 @@ struct RowSums {
 // offsets[l] / cut + l on (as above).  A leaf of one piece writes its result; the pieces of others leave f32 sums in slots: of
 // the pieces between two cuts only the first can have begun before (slot 2 b) and only the last can end behind (2 b + 1).
 // leaf_grad_join_kernel adds a leaf's slots in order, so the sums do not depend on which workgroup ran first.
-// The list's ids are copied to local memory first, kCopiedIds at a time: loads are waited for in order, so a row's address
-// that waits for an id on its way from memory waits for all chunks asked for before as well, and steps do not overlap.
+// The list's ids are copied to local memory first: loads are waited for in order, so a row's address that waits for an id on
+// its way from memory waits for all chunks asked for before as well, and steps do not overlap.  A piece is no longer than that.
 constexpr int kCopiedIds = 4096;
 constexpr int kShortPiece = 1024;  // positions
+
+struct Piece {
+  int leaf, p0, p1;  // leaf < 0: none
+  bool whole;        // all of its leaf
+  int64_t slot;      // of its sums, if not
+};
+template <typename T>
+__device__ __forceinline__ Piece find_piece(const LeafArgs<T>& g, int piece) {
+  Piece r = {-1, 0, 0, false, 0};
+  const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, g.cut, piece);
+  if (leaf < 0) return r;
+  const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
+  const int64_t block = piece - leaf;
+  const int64_t b0 = block * g.cut, b1 = b0 + g.cut;
+  r.p0 = begin > b0 ? begin : (int)(b0 < end ? b0 : end);
+  r.p1 = end < b1 ? end : (int)b1;
+  if (r.p0 >= r.p1 && (end > begin || block != begin / g.cut)) return r;  // only an empty leaf's one piece is empty: zeros
+  r.leaf = leaf;
+  r.whole = begin >= b0 && end <= b1;
+  r.slot = 2 * block + (begin < b0 ? 0 : 1);
+  return r;
+}
 
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafArgs<typename S::T> g) {
@@ -270,64 +293,47 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   // A piece's workgroups share its rows and so are one XCD's; pieces, which are of any length, go round.
   const uint32_t tiles = g.col_tiles * g.row_tiles, at = blockIdx.x / 8;
   const int piece = (int)(at / tiles * 8 + blockIdx.x % 8), r = (int)(at % tiles);
-  const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, g.cut, piece);
+  const Piece at_piece = find_piece(g, piece);
+  const int leaf = at_piece.leaf, p0 = at_piece.p0, p1 = at_piece.p1;
   if (leaf < 0) return;
-  const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
-  const int64_t block = piece - leaf;
-  const int64_t b0 = block * g.cut, b1 = b0 + g.cut;
-  const int p0 = begin > b0 ? begin : (int)(b0 < end ? b0 : end), p1 = end < b1 ? end : (int)b1;
-  if (p0 >= p1 && (end > begin || block != begin / g.cut)) return;  // only an empty leaf's one piece is empty: zeros
   // A short piece's column tiles are gone through cols_per at a time, one after another, by the first of its workgroups; the
   // others leave.  (Not by every cols_per'th: workgroups go to an XCD's shader engines in turn as well.)
   const int cols_per = p1 - p0 <= kShortPiece ? (int)g.cols_per : 1;
   const int turns = ((int)g.col_tiles + cols_per - 1) / cols_per;
   if (r >= turns * (int)g.row_tiles) return;
   const int row0 = r / turns * S::BM, col_first = r % turns * cols_per * S::BN;
-  const bool whole = begin >= b0 && end <= b1;
-  const int64_t slot = 2 * block + (begin < b0 ? 0 : 1);
-  float* part = g.partial + slot * ((int64_t)(g.d_in + 1) * g.d_out);
+  const bool whole = at_piece.whole;
+  float* part = g.partial + at_piece.slot * ((int64_t)(g.d_in + 1) * g.d_out);
   const int all_cols = g.dw ? g.d_in : 1;  // (the outputs' sums alone come with the first tile)
   const int col_last = all_cols < col_first + cols_per * S::BN ? all_cols : col_first + cols_per * S::BN;
   const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
   const int m0 = row0 + (w / S::WN) * (S::TM * 16);
 
+  for (int p = p0 + (int)threadIdx.x; p < p1; p += S::NT) {
+    const int d = g.row_idx ? g.row_idx[p] : p;
+    ids[p - p0] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
+  }
+  __syncthreads();
+  const auto listed = (const __attribute__((address_space(3))) int*)ids;
+  const CopiedRows<T> rows_a = {g.dy, g.dy + (int64_t)(g.n_rows - 1) * g.ld_dy + g.d_out, g.ld_dy, listed, p0};
+  const CopiedRows<T> rows_b = {g.x, g.x + (int64_t)(g.n_rows - 1) * g.ld_x + g.d_in, g.ld_x, listed, p0};
   typename S::ColumnsA a;
   typename S::ColumnsB b;
-  CopiedRows<T> rows_a, rows_b;
-  int c0 = 0, c1 = 0, copied = -1;
-  // Positions from `from` on, of the column tile at `col`.
-  auto begin_part = [&](int from, int col) {
-    c0 = from;
-    c1 = p1 - c0 < kCopiedIds ? p1 : c0 + kCopiedIds;
-    if (copied != c0) {
-      __syncthreads();  // the part before has been used
-      for (int p = c0 + (int)threadIdx.x; p < c1; p += S::NT) {
-        const int d = g.row_idx ? g.row_idx[p] : p;
-        ids[p - c0] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
-      }
-      __syncthreads();
-      copied = c0;
-    }
-    rows_a = {g.dy, g.dy + (int64_t)(g.n_rows - 1) * g.ld_dy + g.d_out, g.ld_dy, (const __attribute__((address_space(3))) int*)ids, c0};
-    rows_b = {g.x, g.x + (int64_t)(g.n_rows - 1) * g.ld_x + g.d_in, g.ld_x, (const __attribute__((address_space(3))) int*)ids, c0};
-    a.init(rows_a, row0, g.d_out, c0, c1);
-    b.init(rows_b, col, g.d_in, c0, c1);
-    tile_begin<S>(lds, a, b, rows_a, rows_b, c0, c1);
+  auto begin_columns = [&](int col) {
+    a.init(rows_a, row0, g.d_out, p0, p1);
+    b.init(rows_b, col, g.d_in, p0, p1);
+    tile_begin<S>(lds, a, b, rows_a, rows_b, p0, p1);
   };
-  begin_part(p0, col_first);
+  begin_columns(col_first);
   for (int col = col_first; col < col_last; col += S::BN) {
     f32x4 acc[S::TM][S::TN];
     zeros<S>(acc);
-    f32x4 sum[S::TM];
+    float sum[S::TM];
 #pragma unroll
-    for (int i = 0; i < S::TM; ++i) sum[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < S::TM; ++i) sum[i] = 0.0f;
     const bool sums = __builtin_amdgcn_readfirstlane(g.dbias != nullptr && col == 0 && w % S::WN == 0);
-    for (;;) {
-      tile_run<S, true>(lds, a, b, rows_a, rows_b, c0, c1, acc, RowSums<S>{sum, sums});
-      if (c1 >= p1) break;
-      begin_part(c1, col);
-    }
-    if (col + S::BN < col_last) begin_part(p0, col + S::BN);
+    tile_run<S, true>(lds, a, b, rows_a, rows_b, p0, p1, acc, RowSums<S>{sum, sums});
+    if (col + S::BN < col_last) begin_columns(col + S::BN);
     const int wave_col = col + (w % S::WN) * (S::TN * 16);
     if (g.dw && whole) {
       store_tile<S, T, S::TM, S::TN>(
@@ -348,15 +354,17 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
         }
       }
     }
-    if (sums && l < 16) {
+    if (sums) {
 #pragma unroll
       for (int i = 0; i < S::TM; ++i) {
-        const int o = m0 + 16 * i + l;
-        if (o >= g.d_out) continue;
+        const int o = m0 + 16 * i + (l & 15);
+        float all = sum[i] + __shfl_xor(sum[i], 16);
+        all += __shfl_xor(all, 32);
+        if (l >= 16 || o >= g.d_out) continue;
         if (whole) {
-          g.dbias[(int64_t)leaf * g.d_out + o] = (T)sum[i][0];
+          g.dbias[(int64_t)leaf * g.d_out + o] = (T)all;
         } else {
-          part[(int64_t)g.d_out * g.d_in + o] = sum[i][0];
+          part[(int64_t)g.d_out * g.d_in + o] = all;
         }
       }
     }

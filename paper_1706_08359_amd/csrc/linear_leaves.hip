@@ -146,30 +146,34 @@ int launch_leaf_grad_input(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   return GBDT_OK;
 }
 
-// Tile of the weights' gradient: outputs x inputs.
-int64_t grad_bm(int64_t e, int64_t d_out) { return e == 4 || d_out <= 64 ? 64 : 128; }
-int64_t grad_bn(int64_t e) { return e == 4 ? 64 : 128; }
-int64_t leaf_tiles(int64_t e, int64_t d_in, int64_t d_out) { return ceil_div(d_out, grad_bm(e, d_out)) * ceil_div(d_in, grad_bn(e)); }
-
-// Positions between cuts: twice as many whole pieces of work as compute units, from 256 positions on.  Then the sums that
-// pieces leave behind are at most 2 x 2 x units tiles of f32 (64 MiB on 256 units) whatever the sizes are.
-int64_t leaf_cut(int64_t n_positions, int64_t tiles, int64_t units) {
-  return std::max<int64_t>(256, round_up(ceil_div(n_positions * tiles, 2 * units), 64));
-}
-size_t leaf_partial_bytes(int64_t n_positions, int64_t e, int64_t d_in, int64_t d_out, int64_t units) {
-  const int64_t blocks = ceil_div(n_positions, leaf_cut(n_positions, leaf_tiles(e, d_in, d_out), units));
-  return blocks < 2 ? 0 : pad256((size_t)(2 * blocks * (d_in + 1) * d_out) * sizeof(float));
+// How the weights' gradient is taken: tiles of bm outputs x bn inputs, and the positions between cuts, two pieces of whole
+// tiles a compute unit, from 256 positions on and at most as many as a workgroup lists.  The sums that pieces leave behind are
+// then at most 4 x units tiles of f32 (64 MiB on 256 units), or two matrices for every 4,096 positions.  (Tiles of 256 x 256,
+// one workgroup a unit, took as long: 100,000 x 2,000 x 256, leaves of 392 rows on average, 330 us against 350.)
+struct LeafGradPlan {
+  int64_t bm, bn, tiles, cut;
+  size_t bytes;
+};
+LeafGradPlan leaf_grad_plan(int64_t e, int64_t n_positions, int64_t d_in, int64_t d_out, int64_t units) {
+  LeafGradPlan p;
+  p.bm = e == 4 || d_out <= 64 ? 64 : 128;
+  p.bn = e == 4 ? 64 : 128;
+  p.tiles = ceil_div(d_out, p.bm) * ceil_div(d_in, p.bn);
+  const int64_t fill = round_up(ceil_div(n_positions * p.tiles, 2 * units), 64);
+  p.cut = std::min<int64_t>(gbdt_leaf::kCopiedIds, std::max<int64_t>(256, fill));
+  const int64_t blocks = ceil_div(n_positions, p.cut);
+  p.bytes = blocks < 2 ? 0 : pad256((size_t)(2 * blocks * (d_in + 1) * d_out) * sizeof(float));
+  return p;
 }
 
 template <class S, typename T>
 int launch_leaf_grad_weight(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  if (S::BM != grad_bm(sizeof(T), g.d_out) || S::BN != grad_bn(sizeof(T))) return GBDT_EUNSUPPORTED;  // (leaf_tiles counts these)
   g.col_tiles = (uint32_t)(g.dw ? ceil_div(g.d_in, S::BN) : 1);
   g.row_tiles = (uint32_t)ceil_div(g.d_out, S::BM);
-  // (as leaf_rows_grid: eight workgroups a unit, counting a piece a cut)
+  // (as leaf_rows_grid, counting a piece a cut)
   const int64_t pieces = (int64_t)g.n_positions / g.cut + g.n_leaves;
-  const int64_t tiles = pieces * g.col_tiles * g.row_tiles;
-  g.cols_per = (uint32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)g.col_tiles, tiles / (8 * gbdt_internal::cu_count()), 4}));
+  const int64_t tiles = pieces * g.col_tiles * g.row_tiles, most = 8 * gbdt_internal::cu_count();
+  g.cols_per = (uint32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)g.col_tiles, tiles / most, 4}));
   const int64_t blocks = round_up(pieces, 8) * g.col_tiles * g.row_tiles;
   if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
   gbdt_leaf::leaf_grad_weight_kernel<S><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
@@ -187,19 +191,18 @@ int leaf_product_grad(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
     if (rc != GBDT_OK) return rc;
   }
   if (!g.dw && !g.dbias) return GBDT_OK;
-  const int64_t units = gbdt_internal::cu_count();
-  g.cut = (int32_t)leaf_cut(g.n_positions, leaf_tiles(sizeof(T), g.d_in, g.d_out), units);
-  const size_t bytes = leaf_partial_bytes(g.n_positions, sizeof(T), g.d_in, g.d_out, units);
-  if (bytes) {
+  const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.x, g.ld_x, g.d_in);
+  const LeafGradPlan plan = leaf_grad_plan(sizeof(T), g.n_positions, g.d_in, g.d_out, gbdt_internal::cu_count());
+  g.cut = (int32_t)plan.cut;
+  if (plan.bytes) {
     void* ws = nullptr;
-    const int rc = gbdt_internal::workspace(bytes, s, &ws);
+    const int rc = gbdt_internal::workspace(plan.bytes, s, &ws);
     if (rc != GBDT_OK) return rc;
     g.partial = (float*)ws;
   }
-  const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.x, g.ld_x, g.d_in);
   int rc = GBDT_OK;
   if constexpr (sizeof(T) == 2) {
-    if (g.d_out <= 64)
+    if (plan.bm == 64)
       rc = direct ? launch_leaf_grad_weight<Shape<T, 64, 128, 1, 4, true, true>>(g, s) : launch_leaf_grad_weight<Shape<T, 64, 128, 1, 4, false>>(g, s);
     else
       rc = direct ? launch_leaf_grad_weight<Square<T>>(g, s) : launch_leaf_grad_weight<SquareAny<T>>(g, s);
@@ -616,7 +619,9 @@ int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const voi
 size_t gbdt_leaf_product_grad_workspace_bytes(int64_t n_positions, int32_t d_in, int32_t d_out) {
   if (n_positions < 0 || n_positions >= kMaxRows || d_in <= 0 || d_out <= 0 || d_in >= kMaxWidth || d_out >= kMaxWidth) return 0;
   const int64_t units = gbdt_internal::cu_count();
-  return gbdt_internal::workspace_head_bytes() + std::max(leaf_partial_bytes(n_positions, 2, d_in, d_out, units), leaf_partial_bytes(n_positions, 4, d_in, d_out, units));
+  size_t most = 0;
+  for (int64_t e : {2, 4}) most = std::max(most, leaf_grad_plan(e, n_positions, d_in, d_out, units).bytes);
+  return gbdt_internal::workspace_head_bytes() + most;
 }
 
 int gbdt_leaf_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* weight, const int32_t* row_idx,

@@ -531,20 +531,28 @@ __global__ void __launch_bounds__(S::NT, 2) piece_product_kernel(const PieceArgs
   float* sums = g.sums + (int64_t)split * g.rows * g.cols;
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
-    const int m = m0 + 16 * i + (l & 15);
+    const int m = m0 + 16 * i + (l & 15), n0 = wave_col + 4 * (l >> 4);
     if (m >= g.rows) continue;
+    float* to = sums + (int64_t)m * g.cols + n0;
+    if (g.add && n0 + 16 * (S::TN - 1) + 4 <= g.cols) {  // all of a row's loads, then its stores
+      f32x4 v[S::TN];
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) __builtin_memcpy(&v[j], to + 16 * j, 16);
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) store4(to + 16 * j, v[j] + acc[i][j], 4);
+      continue;
+    }
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
-      const int n = wave_col + 16 * j + 4 * (l >> 4);
+      const int n = n0 + 16 * j;
       if (n >= g.cols) continue;
       f32x4 v = acc[i][j];
-      float* to = sums + (int64_t)m * g.cols + n;
       if (g.add) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (n + r < g.cols) v[r] += to[r];
+          if (n + r < g.cols) v[r] += to[16 * j + r];
       }
-      store4(to, v, g.cols - n);
+      store4(to + 16 * j, v, g.cols - n);
     }
   }
 }
