@@ -482,8 +482,8 @@ int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const voi
  *   dweight_out[l]   = sum over leaf l of dy[d] x[d]^T   DEVICE [n_leaves][d_out][d_in], zeros for an empty leaf
  *   dbias_out[l]     = sum over leaf l of dy[d]    DEVICE [n_leaves][d_out], zeros for an empty leaf
  * weight is read for dx only, x for dweight only.  Long leaves are summed in parts, whose f32
- * sums lie in the library's scratch and are added in the order of the list: the same call gives
- * the same bits.  gbdt_leaf_product_grad_workspace_bytes: the size of a registered workspace
+ * sums lie in the library's scratch (two matrices for every 4,096 positions at most, for short lists
+ * more often) and are added in the order of the list: the same call gives the same bits.  gbdt_leaf_product_grad_workspace_bytes: the size of a registered workspace
  * (gbdt_set_workspace) that suffices (0 on invalid arguments).
  */
 int gbdt_leaf_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
@@ -522,8 +522,8 @@ int gbdt_softmax_loss(const void* h, int64_t ld_h, const void* classes, int64_t 
  *   lse           DEVICE float [n_rows], as gbdt_softmax_loss left it
  *   row_weight    DEVICE float [n_rows] or NULL (all 1)
  * The classes are taken in pieces, whose row_weight * (p - [v = y]) lies in the library's scratch
- * in the element type (about 256 MiB, or 256 classes for all rows if that is more), beside f32 sums
- * of dh.  gbdt_softmax_workspace_bytes: the size of a registered workspace that suffices for
+ * in the element type (at most 512 MiB, or 256 classes for all rows if that is more), beside f32 sums
+ * of dh and copies of h and, if its rows are no whole chunks, of classes.  gbdt_softmax_workspace_bytes: the size of a registered workspace that suffices for
  * this call and gbdt_softmax_loss (0 on invalid arguments).  The same call gives the same bits.
  */
 int gbdt_softmax_grad(const void* h, int64_t ld_h, const void* classes, int64_t ld_c,

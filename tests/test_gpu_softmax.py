@@ -200,6 +200,14 @@ def test_several_pieces_of_classes_and_parts_of_rows(dtype):
     assert only[0] is None and torch.equal(only[1], first[1])
 
 
+@pytest.mark.parametrize("n,dtype", [(300_000, "bf16"), (160_000, "f32")])
+def test_pieces_of_a_few_hundred_classes(n, dtype):
+    from paper_1706_08359_amd import binding as B
+    h, c, y, w = make(n, 1300, 8, dtype, seed=11)
+    _, lse = B.gbdt_softmax_loss(h, c, y)
+    check_grad(B, h, c, y, w, 1.0 / n, lse)
+
+
 def test_many_rows_of_few_classes_and_many_dimensions():
     """More rows of a tile's classes in one workgroup's share than it lists at a time."""
     from paper_1706_08359_amd import binding as B
