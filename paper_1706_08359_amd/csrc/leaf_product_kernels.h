@@ -117,8 +117,9 @@ __device__ __forceinline__ PlainRows<T> plain_rows(const T* base, int64_t ld, in
 }
 
 // The rows of one tile of positions times a matrix of the leaf, g.cols_per column tiles one after another; the next one's
-// first steps are on their way while one's values are stored.  B: the matrix' orientation, K its length along k.
-template <class S, class B, typename T>
+// first steps are on their way while one's values are stored.  B: the matrix' orientation, k its length along k.
+// GROUPS > 1: as many times the tile's threads take a part of k each, all of as many steps, and the first adds up.
+template <class S, class B, int GROUPS, typename T>
 __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& g, const T* in, int64_t ld_in, int k, const T* bias_all,
                                                   T* out, int64_t ld_out, int cols) {
   const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
@@ -132,27 +133,48 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& 
   const int col_last = cols < col_first + (int)g.cols_per * S::BN ? cols : col_first + (int)g.cols_per * S::BN;
   const ListRows<T> rows_a = list_rows(in, ld_in, k, g, end);
   const PlainRows<T> rows_b = plain_rows(g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out, g.d_in);
+  const int w = thread_of<S::NT>() >> 6;
   int ids[S::TM];  // rows of this lane's blocks, -1 for none
-  const int m0 = p0 + (threadIdx.x >> 6) / S::WN * (S::TM * 16) + (threadIdx.x & 15);
+  const int m0 = p0 + w / S::WN * (S::TM * 16) + (threadIdx.x & 15);
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
     const int p = m0 + 16 * i, d = p < end ? (g.row_idx ? g.row_idx[p] : p) : -1;
     ids[i] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
   }
+  const int group = GROUPS > 1 ? (int)threadIdx.x / S::NT : 0;
+  lds += group * S::kLdsBytes;
+  const int part = GROUPS > 1 ? ((k + GROUPS - 1) / GROUPS + S::kStep - 1) / S::kStep * S::kStep : k;
+  const int k0 = group * part, k1 = k < k0 + part ? k : k0 + part;  // (steps past the end are zeros)
   typename S::RowsA a;
   B b;
   auto begin_columns = [&](int col) {
-    a.init(rows_a, p0, 0, 0, k);
-    b.init(rows_b, col, cols, 0, k);
-    tile_begin<S>(lds, a, b, rows_a, rows_b, 0, k);
+    a.init(rows_a, p0, 0, k0, k1);
+    b.init(rows_b, col, cols, k0, k1);
+    tile_begin<S>(lds, a, b, rows_a, rows_b, k0, k0 + part);
   };
   begin_columns(col_first);
   for (int col = col_first; col < col_last; col += S::BN) {
     f32x4 acc[S::TM][S::TN];
     zeros<S>(acc);
-    tile_run<S, true>(lds, a, b, rows_a, rows_b, 0, k, acc, Nothing{});
-    if (col + S::BN < col_last) begin_columns(col + S::BN);
-    const int l = threadIdx.x & 63, wave_col = col + (int)(threadIdx.x >> 6) % S::WN * (S::TN * 16);
+    tile_run<S, true>(lds, a, b, rows_a, rows_b, k0, k0 + part, acc, Nothing{});
+    if constexpr (GROUPS > 1) {
+      constexpr int values = S::TM * S::TN;
+      static_assert(values * S::NT * 16 <= S::kLdsBytes, "a group's sums take its stages' place");
+      f32x4* sums = (f32x4*)lds;
+      __syncthreads();  // (the last reads of the stages)
+#pragma unroll
+      for (int v = 0; v < values; ++v) sums[v * S::NT + thread_of<S::NT>()] = acc[v / S::TN][v % S::TN];
+      __syncthreads();
+      if (group > 0) return;
+#pragma unroll
+      for (int other = 1; other < GROUPS; ++other)
+#pragma unroll
+        for (int v = 0; v < values; ++v)
+          acc[v / S::TN][v % S::TN] += ((const f32x4*)(lds + other * S::kLdsBytes))[v * S::NT + thread_of<S::NT>()];
+    } else if (col + S::BN < col_last) {
+      begin_columns(col + S::BN);
+    }
+    const int l = threadIdx.x & 63, wave_col = col + w % S::WN * (S::TN * 16);
     f32x4 add[S::TN];
 #pragma unroll
     for (int j = 0; j < S::TN; ++j)
@@ -175,14 +197,21 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& 
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_product_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::RowsB>(lds, g, g.x, g.ld_x, g.d_in, g.bias, g.y, g.ld_y, g.d_out);
+  leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, g.bias, g.y, g.ld_y, g.d_out);
+}
+
+// The same where there are too few tiles for the compute units: a tile's k is split among GROUPS times the threads.
+template <class S, int GROUPS>
+__global__ void __launch_bounds__(S::NT* GROUPS) leaf_product_split_kernel(const LeafArgs<typename S::T> g) {
+  __shared__ __align__(16) char lds[S::kLdsBytes * GROUPS];
+  leaf_rows_product<S, typename S::RowsB, GROUPS>(lds, g, g.x, g.ld_x, g.d_in, g.bias, g.y, g.ld_y, g.d_out);
 }
 
 // dx: rows of dy (k = output along memory) times w, whose rows are k.
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_input_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::ColumnsB>(lds, g, g.dy, g.ld_dy, g.d_out, (const typename S::T*)nullptr, g.dx, g.ld_dx, g.d_in);
+  leaf_rows_product<S, typename S::ColumnsB, 1>(lds, g, g.dy, g.ld_dy, g.d_out, (const typename S::T*)nullptr, g.dx, g.ld_dx, g.d_in);
 }
 
 // A few positions (a row or a few answered at once): a wavefront takes OUTPUTS outputs of one position, each lane a chunk of k

@@ -100,11 +100,16 @@ int launch_leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   return GBDT_OK;
 }
 
-// Leaves long enough for tiles of 256 rows, and columns for more than one of 128.  (100,000 x 256 -> 2,000, gradient of the
-// input, leaves of 392 rows on average: 277 us against 318 us in tiles of 128.)
+// Leaves long enough for tiles of 256 rows, columns for more than one of 128, and such tiles for all compute units.  (100,000 x
+// 256 -> 2,000, gradient of the input, leaves of 392 rows on average: 277 us against 318 us in tiles of 128.  2,000 x 2,000 ->
+// 256 in one leaf, 8 tiles: 42 us against 12 in small ones.)
+template <typename T>
+bool long_leaves(const gbdt_leaf::LeafArgs<T>& g, int64_t cols, int64_t bn) {
+  return sizeof(T) == 2 && g.n_positions >= 192 * (int64_t)g.n_leaves && g.n_positions / 256 * ceil_div(cols, bn) >= gbdt_internal::cu_count();
+}
 template <typename T>
 bool wide_leaves(const gbdt_leaf::LeafArgs<T>& g, int64_t cols) {
-  return sizeof(T) == 2 && g.n_positions >= 192 * (int64_t)g.n_leaves && cols > 128;
+  return cols > 128 && long_leaves(g, cols, 256);
 }
 
 constexpr int64_t kFewPositions = 64;
@@ -121,17 +126,46 @@ int leaf_product_few(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   return GBDT_OK;
 }
 
+template <class S, int GROUPS, typename T>
+int launch_leaf_product_split(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
+  unsigned blocks = 0;
+  const int rc = leaf_rows_grid<S>(g, g.d_out, &blocks);
+  if (rc != GBDT_OK) return rc;
+  gbdt_leaf::leaf_product_split_kernel<S, GROUPS><<<dim3(blocks), dim3(S::NT * GROUPS), 0, s>>>(g);
+  LAUNCHED("leaf_product_split_kernel");
+  return GBDT_OK;
+}
+
+// No more tiles of 64 x 64 than compute units (f32: than half of them), and steps enough to split.  bf16: four groups of threads
+// a tile of 64 x 64 (500 x 2,000 -> 64 in one leaf: 10.6 us against 16.9 in tiles of 128 x 128).  f32, where a unit's matrix
+// instructions are the bound: eight a tile of 32 x 16, which spreads over eight times the units (the same: 10.8 us against 43
+// in tiles of 64 x 64; 2,000 x 700 -> 256 in 31 leaves, 252 tiles: 34 against 19).
+template <typename T>
+bool few_tiles(const gbdt_leaf::LeafArgs<T>& g) {
+  const int64_t tiles = (ceil_div(g.n_positions, 64) + std::min<int64_t>(g.n_leaves, g.n_positions)) * ceil_div(g.d_out, 64);
+  return tiles <= gbdt_internal::cu_count() / (sizeof(T) == 2 ? 1 : 2) && (int64_t)g.d_in * (int64_t)sizeof(T) >= 8 * 128;
+}
+
 template <typename T>
 int leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   if (g.n_positions <= kFewPositions) return leaf_product_few(g, s);
   const bool direct = whole_chunks<T>(g.x, g.ld_x, g.d_in) && whole_chunks<T>(g.w, g.d_in, g.d_in);
+  if (few_tiles(g)) {
+    if constexpr (sizeof(T) == 2) {
+      return direct ? launch_leaf_product_split<Shape<T, 64, 64, 2, 2, true>, 4>(g, s)
+                    : launch_leaf_product_split<Shape<T, 64, 64, 2, 2, false>, 4>(g, s);
+    } else {
+      return direct ? launch_leaf_product_split<Shape<T, 32, 16, 1, 1, true>, 8>(g, s)
+                    : launch_leaf_product_split<Shape<T, 32, 16, 1, 1, false>, 8>(g, s);
+    }
+  }
   if (g.d_out <= 16)
     return direct ? launch_leaf_product<Shape<T, 128, 16, 4, 1, true>>(g, s) : launch_leaf_product<Shape<T, 128, 16, 4, 1, false>>(g, s);
   if (direct && sizeof(T) == 2) {
     // One pass over x: as many of its bytes on the way as local memory holds.
     if (g.d_out <= 64) return launch_leaf_product<Shape<T, 128, 64, 4, 1, true>>(g, s);
     if (wide_leaves(g, g.d_out)) return launch_leaf_product<Wide<T>>(g, s);
-    return launch_leaf_product<Shape<T, 256, 128, 4, 2, true, false, 3>>(g, s);
+    if (long_leaves(g, g.d_out, 128)) return launch_leaf_product<Shape<T, 256, 128, 4, 2, true, false, 3>>(g, s);
   }
   return direct ? launch_leaf_product<Square<T>>(g, s) : launch_leaf_product<SquareAny<T>>(g, s);
 }

@@ -82,10 +82,17 @@ __device__ __forceinline__ u32x4 last_chunk(const T* p, int valid) {
   return v;
 }
 
+// The thread's number among the NT of its tile; a workgroup may hold several tiles' threads.
+template <int NT>
+__device__ __forceinline__ int thread_of() {
+  return (int)threadIdx.x % NT;
+}
+
 // The byte of local memory where a wavefront's first chunk of a stage goes, for scalar registers.
+template <int NT>
 __device__ __forceinline__ uint32_t wave_place(const char* stage) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)stage +
-         __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024u;
+         __builtin_amdgcn_readfirstlane(thread_of<NT>() >> 6) * 1024u;
 }
 
 // 16 bytes from each lane's `src` to lane-consecutive places from byte `place` of local memory on (the same in all lanes).  Written as a
@@ -131,7 +138,7 @@ struct RowOperand {
 
   template <class Rows>
   __device__ __forceinline__ void init(const Rows& rows, int r0, int /*limit*/, int k0, int k1) {
-    const int t = threadIdx.x;
+    const int t = thread_of<NT>();
     k_of = k0 + (t % kRowChunks ^ swizzle(t / kRowChunks)) * kChunk<T>;
     k_end = k1;
     end = rows.end;
@@ -147,10 +154,10 @@ struct RowOperand {
   // DIRECT: the i'th of a step's chunks (WHOLE: of a step that no limit cuts); after the last, `advance`.
   template <bool WHOLE, class Rows>
   __device__ __forceinline__ void load_one(const Rows&, char* stage, int i) {
-    const int t = threadIdx.x;
+    const int t = thread_of<NT>();
     if (kSlots % NT != 0 && i * NT + t >= kSlots) return;
     if (WHOLE || k_of < k_end) {
-      direct_chunk(row[i], wave_place(stage) + i * NT * 16);
+      direct_chunk(row[i], wave_place<NT>(stage) + i * NT * 16);
     } else {
       *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
     }
@@ -162,13 +169,13 @@ struct RowOperand {
   }
   template <class Rows>
   __device__ __forceinline__ void load(const Rows&, char* stage) {
-    const int t = threadIdx.x;
+    const int t = thread_of<NT>();
     if constexpr (DIRECT) {
       if (k_of < k_end) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
           if (kSlots % NT != 0 && i * NT + t >= kSlots) break;
-          direct_chunk(row[i], wave_place(stage) + i * NT * 16);
+          direct_chunk(row[i], wave_place<NT>(stage) + i * NT * 16);
           row[i] += kStep;
         }
       } else {
@@ -198,7 +205,7 @@ struct RowOperand {
   }
   __device__ __forceinline__ void store(char* stage) {
     if constexpr (!DIRECT) {
-      const int t = threadIdx.x;
+      const int t = thread_of<NT>();
       const int valid = k_end - (k_of - kStep);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
@@ -241,10 +248,10 @@ struct ColumnOperand {
   u32x4 reg[DIRECT ? 1 : kPer];
   int k_at, k_end, c0, lim;
 
-  __device__ __forceinline__ static int slot_k(int i) { return (i * NT + (int)threadIdx.x) / kChunks; }
+  __device__ __forceinline__ static int slot_k(int i) { return (i * NT + thread_of<NT>()) / kChunks; }
   // (the same for all of a thread's chunks where as many rows lie between them as the permutation repeats after)
   __device__ __forceinline__ int slot_column(int i) const {
-    const int s = (NT / kChunks % 16 == 0 ? 0 : i) * NT + (int)threadIdx.x;
+    const int s = (NT / kChunks % 16 == 0 ? 0 : i) * NT + thread_of<NT>();
     return c0 + ((s % kChunks) ^ column_swizzle<T, R>(s / kChunks)) * kChunk<T>;
   }
   template <class Rows>
@@ -278,13 +285,13 @@ struct ColumnOperand {
   template <bool WHOLE, class Rows>
   __device__ __forceinline__ void load_one(const Rows& rows, char* stage, int i) {
     static_assert(DIRECT, "");
-    const int t = threadIdx.x;
+    const int t = thread_of<NT>();
     if constexpr (!Rows::kEven) {
       const T* row = rows.at(k_at + slot_k(i), id[i]);
-      direct_chunk(row != nullptr ? (const void*)(row + direct_column(i)) : (const void*)zero_chunk, wave_place(stage) + i * NT * 16);
+      direct_chunk(row != nullptr ? (const void*)(row + direct_column(i)) : (const void*)zero_chunk, wave_place<NT>(stage) + i * NT * 16);
     } else {
       if (WHOLE || k_at + slot_k(i) < k_end) {
-        direct_chunk(here[i], wave_place(stage) + i * NT * 16);
+        direct_chunk(here[i], wave_place<NT>(stage) + i * NT * 16);
       } else {
         *(u32x4*)(stage + (i * NT + t) * 16) = u32x4{0, 0, 0, 0};
       }
@@ -298,7 +305,7 @@ struct ColumnOperand {
   }
   template <class Rows>
   __device__ __forceinline__ void load(const Rows& rows, char* stage) {
-    const int t = threadIdx.x;
+    const int t = thread_of<NT>();
     if constexpr (DIRECT) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
@@ -335,7 +342,7 @@ struct ColumnOperand {
   }
   __device__ __forceinline__ void store(char* stage) {
     if constexpr (!DIRECT) {
-      const int t = threadIdx.x;
+      const int t = thread_of<NT>();
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int valid = lim - slot_column(i);
@@ -405,7 +412,7 @@ struct OneHotOperand : ColumnOperand<bf16, R, NT, true, KB> {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (at == e) v[e / 2] = ((uint32_t)entry & 0xffffu) << (e % 2 * 16);
-    *(u32x4*)(stage + (i * NT + (int)threadIdx.x) * 16) = v;
+    *(u32x4*)(stage + (i * NT + thread_of<NT>()) * 16) = v;
   }
   template <class Rows>
   __device__ __forceinline__ void advance(const Rows&) {
@@ -517,7 +524,7 @@ template <class S, bool N_INNER, class A, class B, class RowsA, class RowsB, cla
 __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& rows_a, const RowsB& rows_b, int k0, int k1,
                                          f32x4 (&acc)[S::TM][S::TN], const Also& also) {
   typedef typename Traits<typename S::T>::Frag Frag;
-  const int w = threadIdx.x >> 6;
+  const int w = thread_of<S::NT>() >> 6;
   const int m0 = (w / S::WN) * (S::TM * 16), n0 = (w % S::WN) * (S::TN * 16);
   const int steps = (k1 - k0 + S::kStep - 1) / S::kStep;
   if (steps <= 0) return;
@@ -736,7 +743,7 @@ __device__ __forceinline__ void store4(T* p, f32x4 v, int valid) {
 //   first column and the end of the rows.  scratch: of the workgroup, the last stage, which tile_begin does not touch.
 template <class S, typename O, int ROWS, int INNER, class Value, class Row>
 __device__ __forceinline__ void store_tile(char* scratch, const Value& value, const Row& row, int col0, int cols) {
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int l = threadIdx.x & 63, w = thread_of<S::NT>() >> 6;
   constexpr int row_bytes = INNER * 16 * (int)sizeof(O);
   if constexpr (row_bytes >= 128) {
     constexpr int chunks = row_bytes / 16, at_once = 64 / chunks, n = 16 / (int)sizeof(O);

@@ -61,6 +61,12 @@ CASES = [
     (64, [3, 61], 5, 40, 1),
     (2000, [700, 650, 650], 264, 200, 0),
     (1200, [300, 800, 0, 100], 72, 48, 0),
+    (200, [130, 0, 70], 2000, 33, 0),
+    (70, [70], 513, 65, 0),
+    (150, [100, 50], 1999, 7, 3),
+    (90, [90], 5000, 17, 8),
+    (33_500, [20_000, 0, 13_400], 264, 264, 8),
+    (66_500, [66_000, 100, 0, 400], 72, 96, 0),
 ]
 
 
