@@ -557,8 +557,12 @@ template <typename T>
 int softmax_stats(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
   const bool direct = whole_chunks<T>(g.h, g.ld_h, g.dim) && whole_chunks<T>(g.c, g.ld_c, g.dim);
   if (g.end - g.begin <= 16)
-    return direct ? launch_stats<Shape<T, 128, 16, 4, 1, true>>(g, s) : launch_stats<Shape<T, 128, 16, 4, 1, false>>(g, s);
-  return direct ? launch_stats<Square<T>>(g, s) : launch_stats<SquareAny<T>>(g, s);
+    return direct ? launch_stats<Shape<T, 128, 16, 4, 1, true, false, 2, true>>(g, s) : launch_stats<Shape<T, 128, 16, 4, 1, false, false, 2, true>>(g, s);
+  if constexpr (sizeof(T) == 2) {
+    return direct ? launch_stats<Shape<T, 128, 128, 2, 2, true, true, 2, true>>(g, s) : launch_stats<Shape<T, 64, 64, 2, 2, false, false, 2, true>>(g, s);
+  } else {
+    return direct ? launch_stats<Square<T>>(g, s) : launch_stats<SquareAny<T>>(g, s);
+  }
 }
 
 template <typename T>

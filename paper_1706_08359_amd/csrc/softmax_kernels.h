@@ -34,6 +34,13 @@ constexpr float kLn2 = 0.6931471805599453f;
 // The difference is taken first: it is exact where a score is close to its row's lse, however large both are, which
 // s log2 e - lse log2 e is not.
 __device__ __forceinline__ float exp_diff(float s, float base) { return __builtin_amdgcn_exp2f((s - base) * kLog2e); }
+// The same without the rounding of the product: exp2(t + r) = exp2(t) (1 + r ln 2) up to r^2, where t + r is the product exactly.
+// (Three more operations; for results in f32 whose kernel waits for memory.)
+__device__ __forceinline__ float exp_diff_close(float s, float base) {
+  const float x = s - base, t = x * kLog2e, r = __builtin_fmaf(x, kLog2e, -t), e = __builtin_amdgcn_exp2f(t);
+  const float more = __builtin_fmaf(e, r * kLn2, e);
+  return __builtin_isfinite(t) ? more : e;
+}
 // What a running maximum is subtracted as: exponentials beneath an infinite one are 0 or infinite, not inf - inf.
 __device__ __forceinline__ float base_of(float m) { return __builtin_isinf(m) ? 0.0f : m; }
 
@@ -310,7 +317,7 @@ __global__ void __launch_bounds__(S::NT, 2) softmax_stats_kernel(const ScoreArgs
         const bool use = g.labels == nullptr || (uint32_t)f.y[i][r] < (uint32_t)g.n_classes;
 #pragma unroll
         for (int j = 0; j < S::TN; ++j) {
-          const float e = exp_diff(acc[i][j][r], f.lse[i][r]);
+          const float e = exp_diff_close(acc[i][j][r], f.lse[i][r]);
           acc[i][j][r] = use ? e : 0.0f;
         }
       }

@@ -441,12 +441,13 @@ __device__ __forceinline__ f32x4 mma(f32x4 rows, f32x4 cols, f32x4 acc) {
 //   N_INNER: m = 16 i + lane mod 16, n = 16 j + 4 (lane / 16) + 0..3   (rows of an output along n)
 //   else:    n = 16 j + lane mod 16, m = 16 i + 4 (lane / 16) + 0..3   (columns of an output along m)
 // DEEP (DIRECT only): steps of 64 bytes of k and four stages instead of 128 bytes and STAGES (more than two: DIRECT only).
-template <typename T_, int BM_, int BN_, int WM_, int WN_, bool DIRECT_, bool DEEP_ = false, int STAGES_ = 2>
+// PARTS: sums are taken in parts of 128 k (see tile_run); f32 operands' always are.
+template <typename T_, int BM_, int BN_, int WM_, int WN_, bool DIRECT_, bool DEEP_ = false, int STAGES_ = 2, bool PARTS_ = false>
 struct Shape {
   typedef T_ T;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NT = WM_ * WN_ * 64;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
-  static constexpr bool DIRECT = DIRECT_, DEEP = DEEP_;
+  static constexpr bool DIRECT = DIRECT_, DEEP = DEEP_, PARTS = PARTS_ || sizeof(T_) == 4;
   static constexpr int KB = DEEP ? 64 : 128, kStep = KB / (int)sizeof(T), kStages = DEEP ? 4 : STAGES_;
   static constexpr int kStageBytes = (BM + BN) * KB;
   static constexpr int kLdsBytes = kStages * kStageBytes;
@@ -540,12 +541,34 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
   auto read_columns = [&](const char* stage, int part, int j, int turn) {
     fb[turn][j] = B::frag(stage + A::kBytes, lanes_b, j, part);
   };
+  // f32 operands: products are added four k at a time, so a sum over 1,024 is a chain of 256 roundings; every 128 k
+  // what has come together is added to the rest instead, which leaves two chains of 32 and 8.  (Scores of 1,024 dimensions:
+  // three times the error of a product summed in parts without it.)  bf16 ones are added 32 k at a time, and only what ends in
+  // f32, the columns of statistics, is worth the registers.
+  constexpr bool kParts = S::PARTS;
+  f32x4 part_sum[kParts ? S::TM : 1][kParts ? S::TN : 1];
   auto multiply = [&](int i, int slot, int turn) {
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j)
-      acc[i][j] = N_INNER ? mma(fb[turn][j], fa[slot & 3], acc[i][j]) : mma(fa[slot & 3], fb[turn][j], acc[i][j]);
+    for (int j = 0; j < S::TN; ++j) {
+      f32x4& to = kParts ? part_sum[kParts ? i : 0][kParts ? j : 0] : acc[i][j];
+      to = N_INNER ? mma(fb[turn][j], fa[slot & 3], to) : mma(fa[slot & 3], fb[turn][j], to);
+    }
     also(i, fa[slot & 3]);
   };
+  auto add_part = [&](bool now) {
+    if constexpr (kParts) {
+      if (!now) return;
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+          acc[i][j] += part_sum[i][j];
+          part_sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
+  };
+  if constexpr (kParts) zeros<S>(part_sum);
+  constexpr int part_steps = 128 / S::kStep;  // (f32: 4; bf16: 2, or 4 of half the length)
 
   if constexpr (S::DEEP) {
     // A turn is a step.  Its stage is given up two blocks before the turn ends, when all of it has been read; the step four
@@ -603,6 +626,7 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
       in_order();
       multiply(S::TM - 2, S::TM - 2, turn);
       multiply(S::TM - 1, S::TM - 1, turn);
+      add_part(at_turn % part_steps == part_steps - 1 || at_turn + 1 == turns);
       in_order();
     };
     if (full > 2) {
@@ -678,6 +702,7 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
         }
         in_order();
         multiply(S::TM - 1, blocks - 1, 1);
+        add_part(s % part_steps == part_steps - 1 || s + 1 == steps);
         in_order();
         here = next;
       }
@@ -696,6 +721,7 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
         most_blocks(here);
         multiply(S::TM - 2, blocks - 2, 1);
         multiply(S::TM - 1, blocks - 1, 1);
+        add_part(s % part_steps == part_steps - 1 || s + 1 == steps);
         if (s + 1 < steps) {
           a.store(next);
           b.store(next + A::kBytes);
