@@ -2,7 +2,8 @@
  * gbdt_hist.h -- C ABI of libgbdt_hist: feature-histogram construction for the
  * leaves of a histogram-based gradient-boosted decision tree, the sibling
  * histogram by subtraction, the best-split gain scan and the row partition that
- * follows a split, on one AMD gfx950 (MI355X) GPU.  Method: "GPU-acceleration for Large-scale Tree Boosting"
+ * follows a split, and the products of trees with linear leaves and of a softmax
+ * over many classes, on one AMD gfx950 (MI355X) GPU.  Method of the former: "GPU-acceleration for Large-scale Tree Boosting"
  * (arXiv 1706.08359), Sec. 3.3 / Alg. 1 (what a feature histogram is), Sec. 4
  * (building many of them at once on a GPU), App. C.4 (4-bit bins).
  *
@@ -29,7 +30,8 @@
  *  - The library keeps one scratch workspace per process (partial histograms,
  *    split candidates, partition flags) and a few process-wide counters in device
  *    memory.  Calls that use them (gbdt_hist_build[_batch], gbdt_best_split[_batch],
- *    gbdt_partition_rows[_batch], the tree growers) must be issued on ONE stream at a
+ *    gbdt_partition_rows[_batch], the tree growers, gbdt_leaf_product_grad,
+ *    gbdt_softmax_loss, gbdt_softmax_grad) must be issued on ONE stream at a
  *    time: two such calls in flight on different streams, or from two threads, race.
  *    When the library owns the scratch it grows it on demand: a call that needs more
  *    allocates a larger buffer (hipMalloc) and keeps the old one until gbdt_reset; it never
@@ -483,7 +485,8 @@ int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const voi
  *   dbias_out[l]     = sum over leaf l of dy[d]    DEVICE [n_leaves][d_out], zeros for an empty leaf
  * weight is read for dx only, x for dweight only.  Long leaves are summed in parts, whose f32
  * sums lie in the library's scratch (two matrices for every 4,096 positions at most, for short lists
- * more often) and are added in the order of the list: the same call gives the same bits.  gbdt_leaf_product_grad_workspace_bytes: the size of a registered workspace
+ * more often) and are added in the order of the list: the same call gives the same bits.
+ * gbdt_leaf_product_grad_workspace_bytes: the size of a registered workspace
  * (gbdt_set_workspace) that suffices (0 on invalid arguments).
  */
 int gbdt_leaf_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
@@ -523,8 +526,9 @@ int gbdt_softmax_loss(const void* h, int64_t ld_h, const void* classes, int64_t 
  *   row_weight    DEVICE float [n_rows] or NULL (all 1)
  * The classes are taken in pieces, whose row_weight * (p - [v = y]) lies in the library's scratch
  * in the element type (at most 512 MiB, or 256 classes for all rows if that is more), beside f32 sums
- * of dh and copies of h and, if its rows are no whole chunks, of classes.  gbdt_softmax_workspace_bytes: the size of a registered workspace that suffices for
- * this call and gbdt_softmax_loss (0 on invalid arguments).  The same call gives the same bits.
+ * of dh and copies of h and, if its rows are no whole chunks, of classes.
+ * gbdt_softmax_workspace_bytes: the size of a registered workspace that suffices for this
+ * call and gbdt_softmax_loss (0 on invalid arguments).  The same call gives the same bits.
  */
 int gbdt_softmax_grad(const void* h, int64_t ld_h, const void* classes, int64_t ld_c,
                       const int32_t* labels, const float* lse, const float* row_weight, float scale,

@@ -70,6 +70,9 @@ using SquareAny = typename std::conditional<sizeof(T) == 2, Shape<T, 128, 128, 2
 // and its loads never the bound).
 template <typename T>
 using Wide = typename std::conditional<sizeof(T) == 2, Shape<T, 256, 256, 2, 4, true, true>, Square<T>>::type;
+// Taken where there is one for every unit.  (Softmax's loss, 4,096 x 32,768 x 512: 136 us against 156 in tiles of 128, 8,192 x
+// 65,536 x 1,024: 884 against 1,066, 4,096 x 4,096 x 512, a tile a unit: 23 against 29; 2,048 x 4,096 x 1,024, a tile for
+// every other unit: 31 against 26.)
 template <typename T>
 bool wide_tiles(int64_t rows, int64_t cols) {
   return sizeof(T) == 2 && ceil_div(rows, 256) * ceil_div(cols, 256) >= 256;
@@ -112,11 +115,21 @@ bool wide_leaves(const gbdt_leaf::LeafArgs<T>& g, int64_t cols) {
   return cols > 128 && long_leaves(g, cols, 256);
 }
 
-constexpr int64_t kFewPositions = 64;
+// So few answers that a wavefront for every few of them takes less than tiles, whose rows are mostly empty then: 64 positions,
+// or up to 2,048 with 16,384 outputs altogether; twice that (f32: four times) where leaves have fewer than four positions on
+// average, since each has a tile of its own.  (255 leaves, 2,000 -> 256: 64 positions in 12.5 us against 34 in tiles, f32 19.5
+// against 111; 128 in 18 against 36; 512 in 44 against 39.  One leaf, 700 -> 256: 128 in 9.1 against 9.4, 256 in 14.5 against
+// 9.3.  700 -> 1, 2,048 positions: 4.9 against 8.7; 28 -> 1, 4,096: 5.1 against 4.6.)
+template <typename T>
+bool few_answers(const gbdt_leaf::LeafArgs<T>& g) {
+  const int64_t most = 16384 * (g.n_positions >= 4 * (int64_t)g.n_leaves ? 1 : sizeof(T) == 2 ? 2 : 4);
+  return g.n_positions <= 64 || (g.n_positions <= 2048 && (int64_t)g.n_positions * g.d_out <= most);
+}
 
 template <typename T>
 int leaf_product_few(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  // one output a wavefront where that leaves compute units without work, four otherwise
+  // One output a wavefront where that leaves compute units without work, four otherwise.  (700 -> 256, one position: 4.1 us
+  // against 4.9; 64 positions: 10.5 against 7.3.)
   if ((int64_t)g.n_positions * g.d_out <= 1024) {
     gbdt_leaf::leaf_product_few_kernel<T, 1><<<dim3(g.d_out, g.n_positions), dim3(64), 0, s>>>(g);
   } else {
@@ -148,7 +161,7 @@ bool few_tiles(const gbdt_leaf::LeafArgs<T>& g) {
 
 template <typename T>
 int leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  if (g.n_positions <= kFewPositions) return leaf_product_few(g, s);
+  if (few_answers(g)) return leaf_product_few(g, s);
   const bool direct = whole_chunks<T>(g.x, g.ld_x, g.d_in) && whole_chunks<T>(g.w, g.d_in, g.d_in);
   if (few_tiles(g)) {
     if constexpr (sizeof(T) == 2) {
@@ -159,10 +172,11 @@ int leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
                     : launch_leaf_product_split<Shape<T, 32, 16, 1, 1, false>, 8>(g, s);
     }
   }
+  // (100,000 x 700 -> 1: 36 us against 53 in the tiles below, f32 69 against 102; 10,000 x 28 -> 1: 5.4 against 8.6.)
   if (g.d_out <= 16)
     return direct ? launch_leaf_product<Shape<T, 128, 16, 4, 1, true>>(g, s) : launch_leaf_product<Shape<T, 128, 16, 4, 1, false>>(g, s);
   if (direct && sizeof(T) == 2) {
-    // One pass over x: as many of its bytes on the way as local memory holds.
+    // (1,024 positions in 255 leaves, 2,000 -> 64: 25 us against 29 in tiles of 128 x 128; 400,000: 425 against 428.)
     if (g.d_out <= 64) return launch_leaf_product<Shape<T, 128, 64, 4, 1, true>>(g, s);
     if (wide_leaves(g, g.d_out)) return launch_leaf_product<Wide<T>>(g, s);
     if (long_leaves(g, g.d_out, 128)) return launch_leaf_product<Shape<T, 256, 128, 4, 2, true, false, 3>>(g, s);
@@ -183,7 +197,8 @@ int launch_leaf_grad_input(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
 // How the weights' gradient is taken: tiles of bm outputs x bn inputs, and the positions between cuts, two pieces of whole
 // tiles a compute unit, from 256 positions on and at most as many as a workgroup lists.  The sums that pieces leave behind are
 // then at most 4 x units tiles of f32 (64 MiB on 256 units), or two matrices for every 4,096 positions.  (Tiles of 256 x 256,
-// one workgroup a unit, took as long: 100,000 x 2,000 x 256, leaves of 392 rows on average, 330 us against 350.)
+// one workgroup a unit, took as long: 100,000 x 2,000 x 256, leaves of 392 rows on average, 330 us against 350.  64 outputs a
+// tile where there are no more: 100,000 x 700 -> 32, all gradients, 155 us against 173 with 128.)
 struct LeafGradPlan {
   int64_t bm, bn, tiles, cut;
   size_t bytes;
@@ -272,7 +287,8 @@ int softmax_check(const void* h, int64_t ld_h, const void* c, int64_t ld_c, int6
   return GBDT_OK;
 }
 
-// Row tiles that go through the classes together: 2 MiB of rows, half of an XCD's L2.
+// Row tiles that go through the classes together: 2 MiB of rows, half of an XCD's L2.  (Loss, 8,192 x 65,536 x 1,024: 888 us
+// against 936 one at a time; 1,500 x 10,000 x 512: 25 against 32.)
 uint32_t group_of(int64_t tile_rows, int64_t dim, int64_t bytes) {
   return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(64, ((int64_t)2 << 20) / (tile_rows * dim * bytes)));
 }
@@ -339,6 +355,8 @@ int softmax_loss(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
          : direct                                     ? launch_scores<Square<T>>(g, s)
                                                       : launch_scores<SquareAny<T>>(g, s);
     if (rc != GBDT_OK) return rc;
+    // (Whole call, 256 rows x 50,000 classes x 64: 13.5 us against 20 with 16 rows a workgroup; 4,096 x 1,000 x 64: 11.5
+    // against 8.3.)
     if (g.n_rows <= 256) {
       gbdt_softmax::softmax_join_kernel<1><<<dim3((unsigned)g.n_rows), dim3(256), 0, s>>>(
           g.parts, g.picked, g.labels, g.n_rows, g.n_classes, (int32_t)plan.tiles, loss ? loss + r : nullptr, lse + r);
@@ -358,7 +376,8 @@ struct GradPlan {
   size_t g_bytes, dh_bytes, dc_bytes, h_bytes, c_bytes, rest_bytes;
   size_t bytes() const { return g_bytes + dh_bytes + dc_bytes + h_bytes + c_bytes + rest_bytes; }
 };
-// Splits of a summed axis of `k`: as many as give `units` workgroups work, each 4 steps long at least.
+// Splits of a summed axis of `k`: as many as give `units` workgroups work, each 4 steps long at least.  (Loss and gradients, 64
+// x 32,768 x 512: 91 us against 285 unsplit; 4,096 x 1,000 x 512: 79 against 107.)
 void split_axis(int64_t tiles, int64_t k, int64_t step, int64_t units, int64_t* splits, int64_t* len) {
   const int64_t want = std::max<int64_t>(1, std::min(units / std::max<int64_t>(tiles, 1), ceil_div(k, 4 * step)));
   *len = std::max(step, round_up(ceil_div(k, want), step));
@@ -376,6 +395,8 @@ GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, bo
   const int64_t tile = e == 2 ? 128 : 64;
   const int64_t cols = ceil_div(dim, tile);
   split_axis(ceil_div(rows, tile) * cols, p.width, step, 2 * units, &p.dh_splits, &p.dh_split);
+  // Large tiles of dh even if it takes splits to have one for every unit, of 16 steps at least.  (4,096 x 32,768 x 512: 615 us
+  // against 633 with small ones.)
   const int64_t wide = ceil_div(rows, 256) * ceil_div(dim, 256);
   if (e == 2 && wide < units && wide * ceil_div(p.width, 16 * step) >= units)
     split_axis(wide, p.width, step, units, &p.dh_splits, &p.dh_split);
@@ -556,6 +577,7 @@ int launch_stats(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
 template <typename T>
 int softmax_stats(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
   const bool direct = whole_chunks<T>(g.h, g.ld_h, g.dim) && whole_chunks<T>(g.c, g.ld_c, g.dim);
+  // (16 of 1,000 classes, 400,000 x 64: 21 us against 55 in tiles of 128 x 128, f32 31 against 52 in 64 x 64.)
   if (g.end - g.begin <= 16)
     return direct ? launch_stats<Shape<T, 128, 16, 4, 1, true, false, 2, true>>(g, s) : launch_stats<Shape<T, 128, 16, 4, 1, false, false, 2, true>>(g, s);
   if constexpr (sizeof(T) == 2) {
