@@ -193,7 +193,10 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& 
   }
 }
 
-// y: rows of x times the leaf's rows of w, both with k = input along memory.
+// y: rows of x times the leaf's rows of w, both with k = input along memory.  Bound by reading x once: d_out products a value
+// are fewer than the matrix cores do in the time of its read.  Hence tiles that hold all outputs where they can, and as many
+// bytes on the way as local memory holds.  (400,000 x 2,000 -> 128 in 255 leaves, bf16: 466 us, 3.9 TB/s; 10,000 x 28 -> 1, f32:
+// 5.4 us, a chain of the search for the leaf, a row's id, its values, the store.)
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_product_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
@@ -207,7 +210,9 @@ __global__ void __launch_bounds__(S::NT* GROUPS) leaf_product_split_kernel(const
   leaf_rows_product<S, typename S::RowsB, GROUPS>(lds, g, g.x, g.ld_x, g.d_in, g.bias, g.y, g.ld_y, g.d_out);
 }
 
-// dx: rows of dy (k = output along memory) times w, whose rows are k.
+// dx: rows of dy (k = output along memory) times w, whose rows are k.  Bound by its stores, d_in values a row, which a tile's
+// short sum (d_out) leaves little time to hide: the next columns' first steps fly beneath them.  (100,000 x 256 -> 2,000 in 255
+// leaves, bf16: 290 us, 2.5 TB/s with the matrices read once; 50,021 x 33 -> 137 in 63, f32, rows of no whole chunks: 26 us.)
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_input_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
@@ -218,6 +223,8 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_input_kernel(const LeafArg
 // of every 64, and adds up across the lanes.  There is nothing to share between rows, so the leaf's matrix is read once a
 // position, by as many compute units as there are outputs; a tile of 128 rows on the matrix cores reads it by two workgroups.
 // The end of a row that is no whole chunk is read as the last whole chunk, whose values before it count for nothing.
+// Bound by a chain of four round trips (offsets, row id, values, store) for a row, by re-reading matrices from L2 for many: 700
+// -> 256 bf16, 255 leaves: 4.0 us for a row, 7.3 for 64.
 template <typename T, int OUTPUTS>
 __global__ void __launch_bounds__(64) leaf_product_few_kernel(const LeafArgs<T> g) {
   const int p = (int)blockIdx.y, o0 = (int)blockIdx.x * OUTPUTS, l = threadIdx.x;
@@ -287,6 +294,8 @@ struct RowSums {
 // offsets[l] / cut + l on (as above).  A leaf of one piece writes its result; the pieces of others leave f32 sums in slots: of
 // the pieces between two cuts only the first can have begun before (slot 2 b) and only the last can end behind (2 b + 1).
 // leaf_grad_join_kernel adds a leaf's slots in order, so the sums do not depend on which workgroup ran first.
+// Bound by the rows' loads, which no tile shares with another leaf's, and by what short and unequal leaves leave unused:
+// 100,000 x 2,000 x 256 in 255 leaves, bf16: 343 us, 2.1 TB/s, 300 TFLOP/s; 50,021 x 137 x 33 in 63, f32: 30 us.
 // The list's ids are copied to local memory first: loads are waited for in order, so a row's address that waits for an id on
 // its way from memory waits for all chunks asked for before as well, and steps do not overlap.  A piece is no longer than that.
 constexpr int kCopiedIds = 4096;
@@ -401,6 +410,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
 }
 
 // One row of workgroups for each cut but the first position: the cut's leaf, if it crosses a cut here for the first time.
+// Bound by the slots' bytes: 43 us after the 343 of the sums above, most of it the few longest leaves' slots in turn.
 template <typename T>
 __global__ void __launch_bounds__(256) leaf_grad_join_kernel(const LeafArgs<T> g) {
   const int64_t block = (int64_t)blockIdx.y + 1;

@@ -23,6 +23,9 @@
 //   the other loads (a branch among them made every load wait for the one before: 63 leaves of 50,021 x 137 f32, gradient of
 //   weights of 33 outputs, 159 us so).
 // Products of bf16 values are exact in f32 and sums are f32 throughout; f32 operands use the f32 matrix instruction.
+// Measured in the kernels that use it: 256 x 256 tiles of bf16 1.2 PFLOP/s with a long k (dC of 65,536 classes x 1,024 over 8,192
+// rows), where a large library product reached 1.2 to 1.6 on the same card; f32, whose matrix instructions are the bound, 58 to
+// 63 TFLOP/s where rows of 137 values end inside tiles of 64, of 153.
 #pragma once
 
 #include <hip/hip_runtime.h>
