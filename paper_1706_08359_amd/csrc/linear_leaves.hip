@@ -240,7 +240,10 @@ int leaf_product_grad(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
     if (rc != GBDT_OK) return rc;
   }
   if (!g.dw && !g.dbias) return GBDT_OK;
-  const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.x, g.ld_x, g.d_in);
+  // The outputs' sums alone do not read x, which may be null: the other operand is dy's first columns.
+  const bool dy_whole = whole_chunks<T>(g.dy, g.ld_dy, g.d_out);
+  if (!g.dw) g.x = g.dy, g.ld_x = g.ld_dy, g.d_in = dy_whole ? kChunk<T> : 1;
+  const bool direct = dy_whole && whole_chunks<T>(g.x, g.ld_x, g.d_in);
   const LeafGradPlan plan = leaf_grad_plan(sizeof(T), g.n_positions, g.d_in, g.d_out, gbdt_internal::cu_count());
   g.cut = (int32_t)plan.cut;
   if (plan.bytes) {
@@ -682,7 +685,10 @@ size_t gbdt_leaf_product_grad_workspace_bytes(int64_t n_positions, int32_t d_in,
   if (n_positions < 0 || n_positions >= kMaxRows || d_in <= 0 || d_out <= 0 || d_in >= kMaxWidth || d_out >= kMaxWidth) return 0;
   const int64_t units = gbdt_internal::cu_count();
   size_t most = 0;
-  for (int64_t e : {2, 4}) most = std::max(most, leaf_grad_plan(e, n_positions, d_in, d_out, units).bytes);
+  for (int64_t e : {2, 4}) {  // with the weights' gradient and without
+    most = std::max(most, leaf_grad_plan(e, n_positions, d_in, d_out, units).bytes);
+    most = std::max(most, leaf_grad_plan(e, n_positions, 16 / e, d_out, units).bytes);
+  }
   return gbdt_internal::workspace_head_bytes() + most;
 }
 

@@ -112,6 +112,28 @@ def test_long_leaves_are_summed_in_parts(sizes, dtype):
         assert only[2] is None and torch.equal(only[1], got[1])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d_in, d_out", [(40, 24), (13, 3), (8192, 1024)])
+def test_outputs_sums_alone_need_no_inputs(d_in, d_out, dtype):
+    """x and weight null, in a workspace of the size that is said to suffice."""
+    from paper_1706_08359_amd import binding as B
+    sizes = [700, 0, 1, 2000]
+    x, dy, w, b, offs, idx = make(2710, sizes, 1, d_out, dtype, seed=6)
+    want, mags = ref.leaf_product_grad(dy, x, w, offs, idx, torch.zeros_like(x))
+    got = torch.full((len(sizes), d_out), 7.0, dtype=DT[dtype], device="cuda")
+    ws = torch.empty(B.gbdt_leaf_product_grad_workspace_bytes(2701, d_in, d_out), dtype=torch.uint8, device="cuda")
+    B.gbdt_set_workspace(ws)
+    try:
+        rc = B.load().gbdt_leaf_product_grad(dy.data_ptr(), d_out, None, 0, None, idx.data_ptr(), offs.data_ptr(), 2701, len(sizes),
+                                             2710, d_in, d_out, B.DTYPES[DT[dtype]], None, 0, None, got.data_ptr(),
+                                             torch.cuda.current_stream().cuda_stream)
+        assert rc == 0
+        torch.cuda.synchronize()
+    finally:
+        B.gbdt_set_workspace(None)
+    close(got, want[2], mags[2], max(sizes), "db")
+
+
 def test_pieces_longer_than_a_copy_of_their_list():
     """So much work a position that pieces are thousands of positions long."""
     from paper_1706_08359_amd import binding as B
