@@ -527,6 +527,10 @@ int gbdt_softmax_loss(const void* h, int64_t ld_h, const void* classes, int64_t 
  * The classes are taken in pieces, whose row_weight * (p - [v = y]) lies in the library's scratch
  * in the element type (at most 512 MiB, or 256 classes for all rows if that is more), beside f32 sums
  * of dh and copies of h and, if its rows are no whole chunks, of classes.
+ * bf16: with up to 128 classes row_weight * (p - [v = y]) meets h and classes as two values that hold 16 bits of it, and
+ * the results are as far off as rounding exact ones.  With more it is rounded to bf16, off by 2^-8 of each element, but for the
+ * label's, which keeps what rounding took: root mean square 1.00 to 1.05 times the error of rounding exact results where a
+ * row's probability is spread over many classes, up to 1.26 times where a few share it, more where sums cancel.
  * gbdt_softmax_workspace_bytes: the size of a registered workspace that suffices for this
  * call and gbdt_softmax_loss (0 on invalid arguments).  The same call gives the same bits.
  */

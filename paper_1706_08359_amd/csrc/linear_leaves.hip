@@ -373,6 +373,7 @@ int softmax_loss(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
 }
 
 struct GradPlan {
+  bool pair;       // G as two values: one piece, tiles of kPairClasses
   int64_t width;   // classes a piece
   int64_t pieces;
   int64_t dh_splits, dh_split, dc_splits, dc_split;
@@ -388,6 +389,7 @@ void split_axis(int64_t tiles, int64_t k, int64_t step, int64_t units, int64_t* 
 }
 GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, bool c_whole, int64_t units) {
   GradPlan p;
+  p.pair = e == 2 && n_classes <= gbdt_softmax::kPairClasses;
   const int64_t rows = std::max<int64_t>(n_rows, 1);
   const int64_t all = round_up(n_classes, kPieceAlign);
   p.width = std::min(all, std::max(kPieceAlign, kPieceBytes / (rows * e) / kPieceAlign * kPieceAlign));
@@ -401,9 +403,9 @@ GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, bo
   // Large tiles of dh even if it takes splits to have one for every unit, of 16 steps at least.  (4,096 x 32,768 x 512: 615 us
   // against 633 with small ones.)
   const int64_t wide = ceil_div(rows, 256) * ceil_div(dim, 256);
-  if (e == 2 && wide < units && wide * ceil_div(p.width, 16 * step) >= units)
+  if (e == 2 && !p.pair && wide < units && wide * ceil_div(p.width, 16 * step) >= units)
     split_axis(wide, p.width, step, units, &p.dh_splits, &p.dh_split);
-  else if (e == 2 && wide >= units)
+  else if (e == 2 && !p.pair && wide >= units)
     p.dh_splits = 1, p.dh_split = round_up(p.width, step);
   split_axis(ceil_div(p.width, tile) * cols, n_rows, step, 2 * units, &p.dc_splits, &p.dc_split);
   p.g_bytes = pad256((size_t)(rows * p.width * e));
@@ -411,7 +413,7 @@ GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, bo
   p.dc_bytes = p.dc_splits > 1 ? pad256((size_t)(p.dc_splits * p.width * dim) * 4) : 0;
   const int64_t row_bytes = round_up(dim * e, 16);
   p.h_bytes = pad256((size_t)(rows * row_bytes));
-  p.rest_bytes = e == 2 ? pad256((size_t)rows * 4) : 0;
+  p.rest_bytes = e == 2 && !p.pair ? pad256((size_t)rows * 4) : 0;
   p.c_bytes = c_whole ? 0 : pad256((size_t)(n_classes * row_bytes));
   return p;
 }
@@ -426,18 +428,18 @@ int whole_rows(const T* from, int64_t ld, T* to, int64_t rows, int32_t cols, con
   return GBDT_OK;
 }
 
-template <class S, typename T>
+template <class S, bool PAIR, typename T>
 int launch_piece(gbdt_softmax::ScoreArgs<T>& g, hipStream_t s) {
-  static_assert(kPieceAlign % S::BN == 0, "G's rows hold whole tiles");
+  static_assert(kPieceAlign % S::BN == 0 && kPieceAlign >= 2 * gbdt_softmax::kPairClasses, "G's rows hold whole tiles");
   unsigned blocks = 0;
   const int rc = score_grid<S>(g, &blocks);
   if (rc != GBDT_OK || blocks == 0) return rc;
-  gbdt_softmax::softmax_piece_kernel<S><<<dim3(blocks), dim3(S::NT), 0, s>>>(g);
+  gbdt_softmax::softmax_piece_kernel<S, PAIR><<<dim3(blocks), dim3(S::NT), 0, s>>>(g);
   LAUNCHED("softmax_piece_kernel");
   return GBDT_OK;
 }
 
-template <class S, bool TO_ROWS, typename T>
+template <class S, bool TO_ROWS, bool PAIR, typename T>
 int launch_product(gbdt_softmax::PieceArgs<T>& g, hipStream_t s) {
   g.row_tiles = (uint32_t)ceil_div(g.rows, S::BM);
   g.col_tiles = (uint32_t)ceil_div(g.cols, S::BN);
@@ -445,9 +447,26 @@ int launch_product(gbdt_softmax::PieceArgs<T>& g, hipStream_t s) {
   const int64_t blocks = (int64_t)g.row_tiles * g.col_tiles * g.splits;
   if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
   if (blocks == 0) return GBDT_OK;
-  gbdt_softmax::piece_product_kernel<S, TO_ROWS><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+  gbdt_softmax::piece_product_kernel<S, TO_ROWS, PAIR><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
   LAUNCHED("piece_product_kernel");
   return GBDT_OK;
+}
+
+// The tile by the size of the result; PAIR is of bf16 alone and takes small ones, for its summed axis or its result is short.
+template <bool TO_ROWS, typename T>
+int product(gbdt_softmax::PieceArgs<T>& g, bool pair, bool wide, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (pair) return launch_product<Square<T>, TO_ROWS, true>(g, s);
+  }
+  return wide ? launch_product<Wide<T>, TO_ROWS, false>(g, s) : launch_product<Square<T>, TO_ROWS, false>(g, s);
+}
+
+template <typename T>
+int piece_of_g(gbdt_softmax::ScoreArgs<T>& g, bool pair, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (pair) return launch_piece<Square<T>, true>(g, s);
+  }
+  return wide_tiles<T>(g.n_rows, g.end - g.begin) ? launch_piece<Wide<T>, false>(g, s) : launch_piece<Square<T>, false>(g, s);
 }
 
 template <typename T>
@@ -488,7 +507,6 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
     c = (const T*)at;
     ld_c = whole_dim;
   }
-  typedef Square<T> Small;
   gbdt_softmax::PieceArgs<T> to_h = {}, to_c = {};
   for (int64_t begin = 0; begin < n_classes; begin += plan.width) {
     const int64_t end = std::min(n_classes, begin + plan.width);
@@ -508,8 +526,7 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
     g.dim = whole_dim;
     g.begin = (int32_t)begin;
     g.end = (int32_t)end;
-    rc = wide_tiles<T>(n_rows, end - begin) ? launch_piece<Wide<T>>(g, s) : launch_piece<Small>(g, s);
-    if (rc != GBDT_OK) return rc;
+    if ((rc = piece_of_g(g, plan.pair, s)) != GBDT_OK) return rc;
     if (dc) {
       to_c.a = piece;
       to_c.b = h;
@@ -529,8 +546,7 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
       to_c.n_classes = (int32_t)n_classes;
       to_c.k_split = (int32_t)plan.dc_split;
       to_c.splits = (uint32_t)plan.dc_splits;
-      rc = wide_tiles<T>(to_c.rows, dim) ? launch_product<Wide<T>, false>(to_c, s) : launch_product<Small, false>(to_c, s);
-      if (rc != GBDT_OK) return rc;
+      if ((rc = product<false>(to_c, plan.pair, wide_tiles<T>(to_c.rows, dim), s)) != GBDT_OK) return rc;
       if (dc_sums) {
         gbdt_softmax::PieceArgs<T> sums = to_c;
         sums.labels = nullptr;
@@ -559,8 +575,7 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
       to_h.k_split = (int32_t)plan.dh_split;
       to_h.splits = (uint32_t)plan.dh_splits;
       to_h.add = begin > 0;
-      rc = wide_tiles<T>(n_rows * plan.dh_splits, dim) ? launch_product<Wide<T>, true>(to_h, s) : launch_product<Small, true>(to_h, s);
-      if (rc != GBDT_OK) return rc;
+      if ((rc = product<true>(to_h, plan.pair, wide_tiles<T>(n_rows * plan.dh_splits, dim), s)) != GBDT_OK) return rc;
     }
   }
   if (dh && n_rows > 0 && dh_sums) return join_product(to_h, s);

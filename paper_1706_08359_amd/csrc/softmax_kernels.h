@@ -14,6 +14,11 @@
 // be as large as the result's.  What it loses is kept in f32, a number a row, and added to both products: to dh as that
 // number times the label's row of C, to dC as further rows of G with that one element (label_rest).  (4,096 x 32,768 x 512:
 // error of both results 0.0024 of their size without, 0.0017 with it, as much as rounding exact results.)
+// Among few classes no element stands out like that.  Up to kPairClasses G goes into the products as the sum of two bf16 values,
+// the rounded one and what rounding took, off by 2^-16 of an element at most; its row is padded for both, and the second
+// product of so short an axis is cheap.  (4,000 rows x 2 to 128 classes x 64, labels drawn from the softmax: error 1.04 to 1.26 times that of
+// rounding exact results without, 1.00 with it.)  With more classes it is 1.00 to 1.05 times as large where a row's
+// probability is spread, up to 1.26 where a few classes share it; the second products would take half as long again as the whole.
 // scale (1 / n_rows, as a rule) multiplies f32 sums, so it takes no part in that rounding.
 //
 // A row whose label is outside [0, n_classes) is ignored: loss, lse, G, gradient and hessian are zeros whatever h holds there
@@ -48,6 +53,9 @@ __device__ __forceinline__ float base_of(float m) { return __builtin_isinf(m) ? 
 template <typename T>
 constexpr int kPartClasses = sizeof(T) == 2 ? 128 : 64;
 
+// Classes up to which bf16 G is kept as two values; the second ones lie this far behind the first.
+constexpr int kPairClasses = 128;
+
 struct MaxSum {
   float m, s;
 };
@@ -67,7 +75,7 @@ struct ScoreArgs {
   MaxSum* parts;          // [ceil(n_classes / kPartClasses<T>)][n_rows]
   float* picked;          // [n_rows]: the label's score
   float* rest;            // [n_rows]: what rounding took from the label's element of G, or null
-  T* g;                   // [n_rows][ld_g]: G of the classes begin .. end, zeros behind
+  T* g;                   // [n_rows][ld_g]: G of the classes begin .. end, zeros behind; PAIR: kPairClasses, and as many rests
   float* grad;            // [end - begin][ld_out]
   float* hess;
   int64_t ld_h, ld_c, ld_g, ld_out;
@@ -232,7 +240,8 @@ __global__ void __launch_bounds__(256) softmax_join_kernel(const MaxSum* parts, 
 
 // The scores again, and G of a piece, stored in whole lines.  Bound by the same, and by the stores of G (for every `dim` products
 // one exponential and one stored value): 8,192 x 65,536 x 1,024 bf16 in two pieces, 594 us each, 0.93 PFLOP/s and 0.9 TB/s of G.
-template <class S>
+// PAIR: one tile holds all classes, and what rounding takes from them is stored behind them.
+template <class S, bool PAIR>
 __global__ void __launch_bounds__(S::NT, 2) softmax_piece_kernel(const ScoreArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
@@ -282,13 +291,28 @@ __global__ void __launch_bounds__(S::NT, 2) softmax_piece_kernel(const ScoreArgs
       }
     }
     const int wave_row = row0 + (w / S::WN) * (S::TM * 16);
-    store_tile<S, T, S::TM, S::TN>(
-        lds + S::kLastStage, [&](int i, int j) { return acc[i][j]; },
-        [&](int i, int r) {
-          const int d = wave_row + 16 * i + r;
-          return d < g.n_rows ? g.g + (int64_t)d * g.ld_g - g.begin : (T*)nullptr;
-        },
-        n0 - 4 * (l >> 4), g.begin + (int)g.ld_g);
+    auto row = [&](int i, int r) {
+      const int d = wave_row + 16 * i + r;
+      return d < g.n_rows ? g.g + (int64_t)d * g.ld_g - g.begin : (T*)nullptr;
+    };
+    const int wave_col = n0 - 4 * (l >> 4), cols = PAIR ? kPairClasses : g.begin + (int)g.ld_g;
+    store_tile<S, T, S::TM, S::TN>(lds + S::kLastStage, [&](int i, int j) { return acc[i][j]; }, row, wave_col, cols);
+    if constexpr (PAIR) {
+      static_assert(S::BN == kPairClasses, "one tile of all classes");
+      store_tile<S, T, S::TM, S::TN>(
+          lds + S::kLastStage,
+          [&](int i, int j) {
+            f32x4 v = acc[i][j];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] -= (float)(T)v[r];
+            return v;
+          },
+          [&](int i, int r) {
+            T* to = row(i, r);
+            return to != nullptr ? to + kPairClasses : to;
+          },
+          wave_col, cols);
+    }
   });
 }
 
@@ -477,7 +501,8 @@ __device__ __forceinline__ void label_rest(char* lds, const PieceArgs<typename S
 // TO_ROWS: dh (the result's rows are G's rows, k = classes); otherwise dC (its rows are classes, k = G's rows).
 // Bound by the matrix cores and what feeds them: 8,192 x 65,536 x 1,024 bf16, a product in two pieces, dC 900 us, 1.22 PFLOP/s, dh
 // 915, 1.20; 1,537 x 10,007 x 137 f32: 72 and 76 us, 58 TFLOP/s (137 columns take three tiles of 64).
-template <class S, bool TO_ROWS>
+// PAIR: what rounding took from G, which lies behind it, is multiplied as well.
+template <class S, bool TO_ROWS, bool PAIR>
 __global__ void __launch_bounds__(S::NT, 2) piece_product_kernel(const PieceArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
@@ -498,6 +523,13 @@ __global__ void __launch_bounds__(S::NT, 2) piece_product_kernel(const PieceArgs
     a.init(rows_a, row0, 0, k0, k1);
     b.init(rows_b, col0, g.b_cols, k0, k1 < g.b_rows ? k1 : g.b_rows);
     tile_product<S, true>(lds, a, b, rows_a, rows_b, k0, k1, acc, Nothing{});
+    if constexpr (PAIR) {
+      const PlainRows<T> rests = plain_rows(g.a + kPairClasses, g.ld_a, g.rows, kPairClasses);
+      a.init(rests, row0, 0, k0, k1);
+      b.init(rows_b, col0, g.b_cols, k0, k1 < g.b_rows ? k1 : g.b_rows);
+      tile_begin<S>(lds, a, b, rests, rows_b, k0, k1);
+      tile_run<S, true>(lds, a, b, rests, rows_b, k0, k1, acc, Nothing{});
+    }
   } else {
     const PlainRows<T> rows_a = plain_rows(g.a, g.ld_a, g.k, (int)g.ld_a);
     const PlainRows<T> rows_b = plain_rows(g.b, g.ld_b, g.b_rows, g.cols);
@@ -505,12 +537,18 @@ __global__ void __launch_bounds__(S::NT, 2) piece_product_kernel(const PieceArgs
     a.init(rows_a, row0, (g.rows + kChunk<T> - 1) / kChunk<T> * kChunk<T>, k0, k1);  // G is zero up to ld_a
     b.init(rows_b, col0, g.b_cols, k0, k1);
     tile_product<S, true>(lds, a, b, rows_a, rows_b, k0, k1, acc, Nothing{});
-    if constexpr (sizeof(T) == 2) label_rest<S>(lds, g, row0, col0, k0, k1, acc);
+    if constexpr (PAIR) {
+      const PlainRows<T> rests = plain_rows(g.a + kPairClasses, g.ld_a, g.k, kPairClasses);
+      a.init(rests, row0, (g.rows + kChunk<T> - 1) / kChunk<T> * kChunk<T>, k0, k1);
+      b.init(rows_b, col0, g.b_cols, k0, k1);
+      tile_begin<S>(lds, a, b, rests, rows_b, k0, k1);
+      tile_run<S, true>(lds, a, b, rests, rows_b, k0, k1, acc, Nothing{});
+    } else if constexpr (sizeof(T) == 2) label_rest<S>(lds, g, row0, col0, k0, k1, acc);
   }
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int m0 = row0 + (w / S::WN) * (S::TM * 16), wave_col = col0 + (w % S::WN) * (S::TN * 16);
   if (!g.sums) {
-    if constexpr (TO_ROWS && sizeof(T) == 2) {
+    if constexpr (TO_ROWS && sizeof(T) == 2 && !PAIR) {
 #pragma unroll
       for (int i = 0; i < S::TM; ++i) {
         const int m = m0 + 16 * i + (l & 15);
