@@ -24,7 +24,7 @@
  *    violating them is undefined behaviour.  Debugging aid: with the environment
  *    variable GBDT_HIST_CHECK_INPUTS=1 every call that takes a row list first counts
  *    its out-of-range entries on the device, waits for the stream, and returns
- *    GBDT_EINVAL if there are any.
+ *    GBDT_EINVAL if there are any (not the leaf products, which pass over them).
  *  - Bins are 0-based: a binned value b satisfies 0 <= b < n_bins (the paper
  *    writes 1..k).  2 <= n_bins <= 256.
  *  - The library keeps one scratch workspace per process (partial histograms,

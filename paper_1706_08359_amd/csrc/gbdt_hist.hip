@@ -1285,7 +1285,6 @@ namespace gbdt_internal {
 int workspace(size_t bytes, hipStream_t s, void** out) { return get_workspace(bytes, s, out); }
 size_t workspace_head_bytes() { return kWsHeadBytes; }
 int hip_failed(hipError_t e, const char* what) { return hip_fail(e, what); }
-int row_ids_checked(const int32_t* idx, int64_t n, int64_t n_rows, hipStream_t s) { return check_row_ids(idx, n, n_rows, s); }
 int cu_count() { return device_cu_count(); }
 
 }  // namespace gbdt_internal

@@ -1,5 +1,5 @@
-// What the translation units of the library share: the scratch workspace, the text of the last HIP error, the optional
-// check of row lists, the number of compute units.  Defined in gbdt_hist.hip; not exported.
+// What the translation units of the library share: the scratch workspace, the text of the last HIP error,
+// the number of compute units.  Defined in gbdt_hist.hip; not exported.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -11,7 +11,6 @@ namespace gbdt_internal __attribute__((visibility("hidden"))) {
 int workspace(size_t bytes, hipStream_t s, void** out);  // at least `bytes`, as every call's scratch
 size_t workspace_head_bytes();                           // what a registered workspace needs besides
 int hip_failed(hipError_t e, const char* what);          // keeps the text, returns GBDT_EHIP
-int row_ids_checked(const int32_t* idx, int64_t n, int64_t n_rows, hipStream_t s);
 int cu_count();
 
 }  // namespace gbdt_internal

@@ -679,7 +679,7 @@ extern "C" {
 int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const void* bias, const int32_t* row_idx,
                       const int64_t* leaf_offsets, int64_t n_positions, int32_t n_leaves, int64_t n_rows, int32_t d_in,
                       int32_t d_out, int32_t dtype, void* y_out, int64_t ld_y, void* stream) {
-  int rc = leaf_check(n_positions, n_leaves, n_rows, d_in, d_out, row_idx, leaf_offsets, dtype);
+  const int rc = leaf_check(n_positions, n_leaves, n_rows, d_in, d_out, row_idx, leaf_offsets, dtype);
   if (rc != GBDT_OK) return rc;
   if (ld_x < d_in || ld_y < d_out || !weight || off_element(x, dtype) || off_element(weight, dtype) || off_element(bias, dtype) ||
       off_element(y_out, dtype))
@@ -688,8 +688,6 @@ int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const voi
   if (n_positions == 0 || n_rows == 0) return GBDT_OK;
   if (!x || !y_out) return GBDT_EINVAL;
   hipStream_t s = (hipStream_t)stream;
-  rc = gbdt_internal::row_ids_checked(row_idx, n_positions, n_rows, s);
-  if (rc != GBDT_OK) return rc;
   return dtype == GBDT_F32 ? leaf_product_call<float>(x, ld_x, weight, bias, row_idx, leaf_offsets, n_positions, n_leaves, n_rows,
                                                       d_in, d_out, y_out, ld_y, s)
                            : leaf_product_call<bf16>(x, ld_x, weight, bias, row_idx, leaf_offsets, n_positions, n_leaves, n_rows,
@@ -711,7 +709,7 @@ int gbdt_leaf_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t
                            const int64_t* leaf_offsets, int64_t n_positions, int32_t n_leaves, int64_t n_rows, int32_t d_in,
                            int32_t d_out, int32_t dtype, void* dx_out, int64_t ld_dx, void* dweight_out, void* dbias_out,
                            void* stream) {
-  int rc = leaf_check(n_positions, n_leaves, n_rows, d_in, d_out, row_idx, leaf_offsets, dtype);
+  const int rc = leaf_check(n_positions, n_leaves, n_rows, d_in, d_out, row_idx, leaf_offsets, dtype);
   if (rc != GBDT_OK) return rc;
   if (ld_dy < d_out || (dweight_out && ld_x < d_in) || (dx_out && (ld_dx < d_in || !weight))) return GBDT_EINVAL;
   if (off_element(dy, dtype) || off_element(x, dtype) || off_element(weight, dtype) || off_element(dx_out, dtype) ||
@@ -721,8 +719,6 @@ int gbdt_leaf_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t
   if (n_rows == 0) n_positions = 0;
   if (n_positions > 0 && (!dy || (dweight_out && !x))) return GBDT_EINVAL;
   hipStream_t s = (hipStream_t)stream;
-  rc = gbdt_internal::row_ids_checked(row_idx, n_positions, n_rows, s);
-  if (rc != GBDT_OK) return rc;
   return dtype == GBDT_F32 ? leaf_product_grad_call<float>(dy, ld_dy, x, ld_x, weight, row_idx, leaf_offsets, n_positions, n_leaves,
                                                            n_rows, d_in, d_out, dx_out, ld_dx, dweight_out, dbias_out, s)
                            : leaf_product_grad_call<bf16>(dy, ld_dy, x, ld_x, weight, row_idx, leaf_offsets, n_positions, n_leaves,
