@@ -484,8 +484,8 @@ int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const voi
  *   dweight_out[l]   = sum over leaf l of dy[d] x[d]^T   DEVICE [n_leaves][d_out][d_in], zeros for an empty leaf
  *   dbias_out[l]     = sum over leaf l of dy[d]    DEVICE [n_leaves][d_out], zeros for an empty leaf
  * weight is read for dx only, x for dweight only.  Long leaves are summed in parts, whose f32
- * sums lie in the library's scratch (two matrices for every 4,096 positions at most, for short lists
- * more often) and are added in the order of the list: the same call gives the same bits.
+ * sums lie in the library's scratch (512 MiB at most) and are added in the order of the list: the
+ * same call gives the same bits.
  * gbdt_leaf_product_grad_workspace_bytes: the size of a registered workspace
  * (gbdt_set_workspace) that suffices (0 on invalid arguments).
  */

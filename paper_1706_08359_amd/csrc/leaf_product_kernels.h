@@ -296,10 +296,11 @@ struct RowSums {
 // leaf_grad_join_kernel adds a leaf's slots in order, so the sums do not depend on which workgroup ran first.
 // Bound by the rows' loads, which no tile shares with another leaf's, and by what short and unequal leaves leave unused:
 // 100,000 x 2,000 x 256 in 255 leaves, bf16: 343 us, 2.1 TB/s, 300 TFLOP/s; 50,021 x 137 x 33 in 63, f32: 30 us.
-// The list's ids are copied to local memory first: loads are waited for in order, so a row's address that waits for an id on
-// its way from memory waits for all chunks asked for before as well, and steps do not overlap.  A piece is no longer than that.
+// The list's ids are copied to local memory first, kCopiedIds at a time: loads are waited for in order, so a row's address that
+// waits for an id on its way from memory waits for all chunks asked for before as well, and steps do not overlap.
 constexpr int kCopiedIds = 4096;
 constexpr int kShortPiece = 1024;  // positions
+static_assert(kShortPiece <= kCopiedIds, "a piece of several column tiles a workgroup is copied at once");
 
 struct Piece {
   int leaf, p0, p1;  // leaf < 0: none
@@ -347,21 +348,27 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
   const int m0 = row0 + (w / S::WN) * (S::TM * 16);
 
-  for (int p = p0 + (int)threadIdx.x; p < p1; p += S::NT) {
-    const int d = g.row_idx ? g.row_idx[p] : p;
-    ids[p - p0] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
-  }
-  __syncthreads();
   const auto listed = (const __attribute__((address_space(3))) int*)ids;
-  const CopiedRows<T> rows_a = {g.dy, g.dy + (int64_t)(g.n_rows - 1) * g.ld_dy + g.d_out, g.ld_dy, listed, p0};
-  const CopiedRows<T> rows_b = {g.x, g.x + (int64_t)(g.n_rows - 1) * g.ld_x + g.d_in, g.ld_x, listed, p0};
+  CopiedRows<T> rows_a = {g.dy, g.dy + (int64_t)(g.n_rows - 1) * g.ld_dy + g.d_out, g.ld_dy, listed, p0};
+  CopiedRows<T> rows_b = {g.x, g.x + (int64_t)(g.n_rows - 1) * g.ld_x + g.d_in, g.ld_x, listed, p0};
   typename S::ColumnsA a;
   typename S::ColumnsB b;
-  auto begin_columns = [&](int col) {
-    a.init(rows_a, row0, g.d_out, p0, p1);
-    b.init(rows_b, col, g.d_in, p0, p1);
-    tile_begin<S>(lds, a, b, rows_a, rows_b, p0, p1);
+  int c0 = p0, c1 = p0;  // the positions copied
+  auto copy_ids = [&](int from) {
+    c0 = rows_a.first = rows_b.first = from;
+    c1 = p1 - from < kCopiedIds ? p1 : from + kCopiedIds;
+    for (int p = c0 + (int)threadIdx.x; p < c1; p += S::NT) {
+      const int d = g.row_idx ? g.row_idx[p] : p;
+      ids[p - c0] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
+    }
+    __syncthreads();
   };
+  auto begin_columns = [&](int col) {
+    a.init(rows_a, row0, g.d_out, c0, c1);
+    b.init(rows_b, col, g.d_in, c0, c1);
+    tile_begin<S>(lds, a, b, rows_a, rows_b, c0, c1);
+  };
+  copy_ids(p0);
   begin_columns(col_first);
   for (int col = col_first; col < col_last; col += S::BN) {
     f32x4 acc[S::TM][S::TN];
@@ -370,7 +377,13 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) sum[i] = 0.0f;
     const bool sums = __builtin_amdgcn_readfirstlane(g.dbias != nullptr && col == 0 && w % S::WN == 0);
-    tile_run<S, true>(lds, a, b, rows_a, rows_b, p0, p1, acc, RowSums<S>{sum, sums});
+    for (;;) {
+      tile_run<S, true>(lds, a, b, rows_a, rows_b, c0, c1, acc, RowSums<S>{sum, sums});
+      if (c1 >= p1) break;
+      __syncthreads();  // everyone has read the last of these ids
+      copy_ids(c1);
+      begin_columns(col);
+    }
     if (col + S::BN < col_last) begin_columns(col + S::BN);
     const int wave_col = col + (w % S::WN) * (S::TN * 16);
     if (g.dw && whole) {

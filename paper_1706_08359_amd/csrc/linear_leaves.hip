@@ -194,11 +194,14 @@ int launch_leaf_grad_input(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   return GBDT_OK;
 }
 
-// How the weights' gradient is taken: tiles of bm outputs x bn inputs, and the positions between cuts, two pieces of whole
-// tiles a compute unit, from 256 positions on and at most as many as a workgroup lists.  The sums that pieces leave behind are
-// then at most 4 x units tiles of f32 (64 MiB on 256 units), or two matrices for every 4,096 positions.  (Tiles of 256 x 256,
+// How the weights' gradient is taken: tiles of bm outputs x bn inputs, and the positions between cuts: two pieces of whole
+// tiles a compute unit, from 256 positions on and up to as many as a workgroup lists at once, which evens out unequal leaves; more
+// where the sums that pieces leave behind would pass kSlotBytes.  (Two pieces a unit whatever their length, 64 MiB of sums: dW and
+// db of 400,000 x 2,000 x 256 in 255 leaves 946 us against 1,046, but f32 100,000 x 2,000 x 256 in 31 leaves 2,248 against 1,447.  Tiles of 256 x 256,
 // one workgroup a unit, took as long: 100,000 x 2,000 x 256, leaves of 392 rows on average, 330 us against 350.  64 outputs a
 // tile where there are no more: 100,000 x 700 -> 32, all gradients, 155 us against 173 with 128.)
+constexpr int64_t kSlotBytes = (int64_t)512 << 20;
+constexpr int64_t kMaxCuts = 65535;  // (of a launch's second dimension)
 struct LeafGradPlan {
   int64_t bm, bn, tiles, cut;
   size_t bytes;
@@ -208,10 +211,13 @@ LeafGradPlan leaf_grad_plan(int64_t e, int64_t n_positions, int64_t d_in, int64_
   p.bm = e == 4 || d_out <= 64 ? 64 : 128;
   p.bn = e == 4 ? 64 : 128;
   p.tiles = ceil_div(d_out, p.bm) * ceil_div(d_in, p.bn);
-  const int64_t fill = round_up(ceil_div(n_positions * p.tiles, 2 * units), 64);
+  const int64_t fill = p.tiles >= 2 * units ? n_positions : ceil_div(n_positions * p.tiles, 2 * units);
+  const int64_t slots = 2 * (d_in + 1) * d_out * (int64_t)sizeof(float);  // of a cut
+  const int64_t most = std::max<int64_t>(1, std::min(kMaxCuts, kSlotBytes / slots));
   p.cut = std::min<int64_t>(gbdt_leaf::kCopiedIds, std::max<int64_t>(256, fill));
+  p.cut = round_up(std::max(p.cut, ceil_div(n_positions, most)), 64);
   const int64_t blocks = ceil_div(n_positions, p.cut);
-  p.bytes = blocks < 2 ? 0 : pad256((size_t)(2 * blocks * (d_in + 1) * d_out) * sizeof(float));
+  p.bytes = blocks < 2 ? 0 : pad256((size_t)(blocks * slots));
   return p;
 }
 

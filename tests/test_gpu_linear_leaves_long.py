@@ -1,0 +1,49 @@
+"""Gradients of the weights over lists whose parts are longer than what a workgroup lists at once, and over more positions than
+a launch has rows of workgroups for cuts of that length."""
+import pytest
+import torch
+
+from oracle import linear_leaves as ref
+from test_gpu_linear_leaves import close, make
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sizes", [[11_600, 0, 400], [100, 5900, 6000], [12_000]], ids=str)
+def test_parts_longer_than_a_listing(sizes, dtype):
+    """Matrices so large that only two cuts fit the scratch: 6,016 positions between them."""
+    from paper_1706_08359_amd import binding as B
+    d = 5000
+    need = B.gbdt_leaf_product_grad_workspace_bytes(12_000, d, d)
+    assert need < 520 << 20
+    x, dy, w, b, offs, idx = make(12_001, sizes, d, d, dtype, seed=len(sizes))
+    idx[4090:4100:3], idx[6010:6020:4], idx[::997] = -1, 12_001, -5
+    own = torch.empty(need, dtype=torch.uint8, device="cuda")
+    B.gbdt_set_workspace(own)
+    try:
+        got = B.gbdt_leaf_product_grad(dy, x, w, offs, row_idx=idx, want=("weight", "bias"))
+        again = B.gbdt_leaf_product_grad(dy, x, w, offs, row_idx=idx, want=("weight", "bias"))
+        torch.cuda.synchronize()
+    finally:
+        B.gbdt_set_workspace(None)
+    want, mags = ref.leaf_product_grad(dy, x, w, offs, idx, torch.zeros(12_001, 1, device="cuda").expand(12_001, d))
+    for i in (1, 2):
+        close(got[i], want[i], mags[i], max(sizes), i)
+        assert torch.equal(got[i], again[i])
+
+
+def test_more_positions_than_cuts_of_a_listing():
+    """270 million positions of one input and one output.  Zeros and ones, a sum of which is below 2^24: every f32 sum is exact."""
+    from paper_1706_08359_amd import binding as B
+    n = 270_000_000
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = (torch.rand(n, 1, generator=g, device="cuda") < 0.05).float()
+    dy = (torch.rand(n, 1, generator=g, device="cuda") < 0.05).float()
+    edges = [0, 5, 150_000_001, 150_000_001, n]
+    w = torch.zeros(4, 1, 1, device="cuda")
+    _, dw, db = B.gbdt_leaf_product_grad(dy, x, w, torch.tensor(edges, device="cuda"), want=("weight", "bias"))
+    for leaf in range(4):
+        a, e = edges[leaf], edges[leaf + 1]
+        assert int(dw[leaf, 0, 0]) == int((x[a:e] * dy[a:e]).double().sum())
+        assert int(db[leaf, 0]) == int(dy[a:e].double().sum()) < 1 << 24
