@@ -471,7 +471,8 @@ typedef enum { GBDT_F32 = 0, GBDT_BF16 = 1 } gbdt_dtype;
  *                 caller that routes rows there need not wait for their numbers
  *   y_out         DEVICE [n_rows][d_out], by ROW ID; rows of no leaf are left as they are
  * n_rows and n_positions < 2^30, n_leaves, d_in and d_out < 2^24, ld_* < 2^28 (GBDT_EUNSUPPORTED
- * beyond).
+ * beyond, and for gradients of the weights where a leaf's matrix has two million tiles or more, of 64 x
+ * 64 f32 or 128 x 128 bf16 values, 64 x 128 up to 64 outputs).
  */
 int gbdt_leaf_product(const void* x, int64_t ld_x, const void* weight, const void* bias,
                       const int32_t* row_idx, const int64_t* leaf_offsets, int64_t n_positions,

@@ -31,6 +31,7 @@ struct LeafArgs {
   int32_t n_positions, n_leaves, n_rows, d_in, d_out;
   int32_t cut;        // gradient of the weights: positions between cuts
   uint32_t col_tiles, row_tiles, cols_per;  // cols_per: column tiles that a workgroup goes through
+  uint32_t first;     // of this launch's workgroups (gradient of the weights: of its pieces), among all of the call
 };
 
 // An offset as the kernels take it: inside the list, whatever the array holds.
@@ -122,7 +123,7 @@ __device__ __forceinline__ PlainRows<T> plain_rows(const T* base, int64_t ld, in
 template <class S, class B, int GROUPS, typename T>
 __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& g, const T* in, int64_t ld_in, int k, const T* bias_all,
                                                   T* out, int64_t ld_out, int cols) {
-  const uint32_t t = xcd_tile(blockIdx.x, gridDim.x);
+  const uint32_t t = g.first + xcd_tile(blockIdx.x, gridDim.x);
   const uint32_t turns = (g.col_tiles + g.cols_per - 1) / g.cols_per;
   const int tile = (int)(t / turns), col_first = (int)(t % turns * g.cols_per) * S::BN;
   const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, S::BM, tile);
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   __shared__ int ids[kCopiedIds];
   // A piece's workgroups share its rows and so are one XCD's; pieces, which are of any length, go round.
   const uint32_t tiles = g.col_tiles * g.row_tiles, at = blockIdx.x / 8;
-  const int piece = (int)(at / tiles * 8 + blockIdx.x % 8), r = (int)(at % tiles);
+  const int piece = (int)(g.first + at / tiles * 8 + blockIdx.x % 8), r = (int)(at % tiles);
   const Piece at_piece = find_piece(g, piece);
   const int leaf = at_piece.leaf, p0 = at_piece.p0, p1 = at_piece.p1;
   if (leaf < 0) return;

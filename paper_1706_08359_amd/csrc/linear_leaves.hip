@@ -31,11 +31,14 @@ using gbdt_tile::Shape;
 constexpr int64_t kMaxRows = (int64_t)1 << 30;     // rows, positions, classes
 constexpr int64_t kMaxWidth = (int64_t)1 << 24;    // d_in, d_out, dim, leaves
 constexpr int64_t kMaxLd = (int64_t)1 << 28;       // distances of rows
-constexpr int64_t kMaxBlocks = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxTiles = ((int64_t)1 << 31) - 1;   // of a call
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 size_t pad256(size_t b) { return (b + 255) / 256 * 256; }
+
+// Workgroups of `threads` that one launch takes, a multiple of 8: it counts its threads in 32 bits.
+constexpr int64_t most_blocks(int threads) { return (((int64_t)1 << 32) - 1) / threads / 8 * 8; }
 
 // Rows of whole 16-byte chunks: every row 16-byte aligned and `cols` whole chunks.
 template <typename T>
@@ -80,27 +83,29 @@ bool wide_tiles(int64_t rows, int64_t cols) {
 
 // Workgroups of the products over rows: the column tiles of a row tile are spread over as many as it takes to have eight a
 // compute unit (four of the large ones), and no more, since a workgroup's first tile waits for its leaf and its rows.
-template <class S, typename T>
-int leaf_rows_grid(gbdt_leaf::LeafArgs<T>& g, int64_t cols, unsigned* blocks) {
+// `launch(blocks)` is called with g.first set, more than once where there are millions of leaves.
+template <class S, typename T, class Launch>
+int leaf_rows_launches(gbdt_leaf::LeafArgs<T>& g, int64_t cols, int threads, const Launch& launch) {
   const int64_t row_tiles = (int64_t)g.n_positions / S::BM + g.n_leaves;
   const int64_t col_tiles = ceil_div(cols, S::BN);
   const int64_t most = (S::BM >= 256 ? 4 : 8) * gbdt_internal::cu_count();  // one or two at a time on a unit
   g.col_tiles = (uint32_t)col_tiles;
   g.cols_per = (uint32_t)std::max<int64_t>(1, std::min(col_tiles, (int64_t)g.n_positions / S::BM * col_tiles / most));
   const int64_t n = row_tiles * ceil_div(col_tiles, g.cols_per);
-  if (n > kMaxBlocks) return GBDT_EUNSUPPORTED;
-  *blocks = (unsigned)n;
+  if (n > kMaxTiles) return GBDT_EUNSUPPORTED;
+  for (int64_t first = 0; first < n; first += most_blocks(threads)) {
+    g.first = (uint32_t)first;
+    launch(dim3((unsigned)std::min(n - first, most_blocks(threads))));
+    LAUNCHED("a product of the leaves");
+  }
   return GBDT_OK;
 }
 
 template <class S, typename T>
 int launch_leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  unsigned blocks = 0;
-  const int rc = leaf_rows_grid<S>(g, g.d_out, &blocks);
-  if (rc != GBDT_OK) return rc;
-  gbdt_leaf::leaf_product_kernel<S><<<dim3(blocks), dim3(S::NT), 0, s>>>(g);
-  LAUNCHED("leaf_product_kernel");
-  return GBDT_OK;
+  return leaf_rows_launches<S>(g, g.d_out, S::NT, [&](dim3 blocks) {
+    gbdt_leaf::leaf_product_kernel<S><<<blocks, dim3(S::NT), 0, s>>>(g);
+  });
 }
 
 // Leaves long enough for tiles of 256 rows, columns for more than one of 128, and such tiles for all compute units.  (100,000 x
@@ -141,12 +146,9 @@ int leaf_product_few(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
 
 template <class S, int GROUPS, typename T>
 int launch_leaf_product_split(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  unsigned blocks = 0;
-  const int rc = leaf_rows_grid<S>(g, g.d_out, &blocks);
-  if (rc != GBDT_OK) return rc;
-  gbdt_leaf::leaf_product_split_kernel<S, GROUPS><<<dim3(blocks), dim3(S::NT * GROUPS), 0, s>>>(g);
-  LAUNCHED("leaf_product_split_kernel");
-  return GBDT_OK;
+  return leaf_rows_launches<S>(g, g.d_out, S::NT * GROUPS, [&](dim3 blocks) {
+    gbdt_leaf::leaf_product_split_kernel<S, GROUPS><<<blocks, dim3(S::NT * GROUPS), 0, s>>>(g);
+  });
 }
 
 // No more tiles of 64 x 64 than compute units (f32: than half of them), and steps enough to split.  bf16: four groups of threads
@@ -186,12 +188,9 @@ int leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
 
 template <class S, typename T>
 int launch_leaf_grad_input(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  unsigned blocks = 0;
-  const int rc = leaf_rows_grid<S>(g, g.d_in, &blocks);
-  if (rc != GBDT_OK) return rc;
-  gbdt_leaf::leaf_grad_input_kernel<S><<<dim3(blocks), dim3(S::NT), 0, s>>>(g);
-  LAUNCHED("leaf_grad_input_kernel");
-  return GBDT_OK;
+  return leaf_rows_launches<S>(g, g.d_in, S::NT, [&](dim3 blocks) {
+    gbdt_leaf::leaf_grad_input_kernel<S><<<blocks, dim3(S::NT), 0, s>>>(g);
+  });
 }
 
 // How the weights' gradient is taken: tiles of bm outputs x bn inputs, and the positions between cuts: two pieces of whole
@@ -201,6 +200,7 @@ int launch_leaf_grad_input(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
 // one workgroup a unit, took as long: 100,000 x 2,000 x 256, leaves of 392 rows on average, 330 us against 350.  64 outputs a
 // tile where there are no more: 100,000 x 700 -> 32, all gradients, 155 us against 173 with 128.)
 constexpr int64_t kSlotBytes = (int64_t)512 << 20;
+constexpr int kGradThreads = 256;  // of a workgroup
 constexpr int64_t kMaxCuts = 65535;  // (of a launch's second dimension)
 struct LeafGradPlan {
   int64_t bm, bn, tiles, cut;
@@ -225,40 +225,49 @@ template <class S, typename T>
 int launch_leaf_grad_weight(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   g.col_tiles = (uint32_t)(g.dw ? ceil_div(g.d_in, S::BN) : 1);
   g.row_tiles = (uint32_t)ceil_div(g.d_out, S::BM);
-  // (as leaf_rows_grid, counting a piece a cut)
+  // (as leaf_rows_launches, counting a piece a cut)
   const int64_t pieces = (int64_t)g.n_positions / g.cut + g.n_leaves;
   const int64_t tiles = pieces * g.col_tiles * g.row_tiles, most = 8 * gbdt_internal::cu_count();
   g.cols_per = (uint32_t)std::max<int64_t>(1, std::min<int64_t>({(int64_t)g.col_tiles, tiles / most, 4}));
-  const int64_t blocks = round_up(pieces, 8) * g.col_tiles * g.row_tiles;
-  if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
-  gbdt_leaf::leaf_grad_weight_kernel<S><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
-  LAUNCHED("leaf_grad_weight_kernel");
+  const int64_t a_piece = (int64_t)g.col_tiles * g.row_tiles;
+  static_assert(S::NT <= kGradThreads, "eight pieces at least are a launch");
+  const int64_t at_once = most_blocks(S::NT) / a_piece / 8 * 8;
+  for (int64_t first = 0; first < pieces; first += at_once) {
+    g.first = (uint32_t)first;
+    const int64_t blocks = round_up(std::min(pieces - first, at_once), 8) * a_piece;
+    gbdt_leaf::leaf_grad_weight_kernel<S><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+    LAUNCHED("leaf_grad_weight_kernel");
+  }
   return GBDT_OK;
 }
 
 template <typename T>
+int leaf_grad_input(gbdt_leaf::LeafArgs<T> g, hipStream_t s) {
+  const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.w, g.d_in, g.d_in);
+  return direct && wide_leaves(g, g.d_in) ? launch_leaf_grad_input<Wide<T>>(g, s)
+         : direct                        ? launch_leaf_grad_input<Square<T>>(g, s)
+                                         : launch_leaf_grad_input<SquareAny<T>>(g, s);
+}
+
+template <typename T>
 int leaf_product_grad(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  if (g.dx && g.n_positions > 0) {
-    const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.w, g.d_in, g.d_in);
-    const int rc = direct && wide_leaves(g, g.d_in) ? launch_leaf_grad_input<Wide<T>>(g, s)
-                   : direct                        ? launch_leaf_grad_input<Square<T>>(g, s)
-                                                   : launch_leaf_grad_input<SquareAny<T>>(g, s);
-    if (rc != GBDT_OK) return rc;
-  }
-  if (!g.dw && !g.dbias) return GBDT_OK;
+  const bool inputs = g.dx && g.n_positions > 0;
+  if (!g.dw && !g.dbias) return inputs ? leaf_grad_input(g, s) : GBDT_OK;
+  const gbdt_leaf::LeafArgs<T> of_inputs = g;
   // The outputs' sums alone do not read x, which may be null: the other operand is dy's first columns.
   const bool dy_whole = whole_chunks<T>(g.dy, g.ld_dy, g.d_out);
   if (!g.dw) g.x = g.dy, g.ld_x = g.ld_dy, g.d_in = dy_whole ? kChunk<T> : 1;
   const bool direct = dy_whole && whole_chunks<T>(g.x, g.ld_x, g.d_in);
   const LeafGradPlan plan = leaf_grad_plan(sizeof(T), g.n_positions, g.d_in, g.d_out, gbdt_internal::cu_count());
+  if (plan.tiles > most_blocks(kGradThreads) / 8) return GBDT_EUNSUPPORTED;
   g.cut = (int32_t)plan.cut;
+  int rc = GBDT_OK;
   if (plan.bytes) {
     void* ws = nullptr;
-    const int rc = gbdt_internal::workspace(plan.bytes, s, &ws);
-    if (rc != GBDT_OK) return rc;
+    if ((rc = gbdt_internal::workspace(plan.bytes, s, &ws)) != GBDT_OK) return rc;
     g.partial = (float*)ws;
   }
-  int rc = GBDT_OK;
+  if (inputs && (rc = leaf_grad_input(of_inputs, s)) != GBDT_OK) return rc;
   if constexpr (sizeof(T) == 2) {
     if (plan.bm == 64)
       rc = direct ? launch_leaf_grad_weight<Shape<T, 64, 128, 1, 4, true, true>>(g, s) : launch_leaf_grad_weight<Shape<T, 64, 128, 1, 4, false>>(g, s);
@@ -308,10 +317,10 @@ int score_grid(gbdt_softmax::ScoreArgs<T>& g, unsigned* blocks) {
   g.col_tiles = (uint32_t)ceil_div(g.end - g.begin, S::BN);
   g.group = group_of(S::BM, g.dim, sizeof(T));
   const int64_t n = (int64_t)g.row_tiles * g.col_tiles;
-  if (n > kMaxBlocks || (int64_t)g.group * g.col_tiles > kMaxBlocks) return GBDT_EUNSUPPORTED;
-  // One workgroup a compute unit goes through the tiles where there is no room for two; else one a tile.
+  if (n > kMaxTiles || (int64_t)g.group * g.col_tiles > kMaxTiles) return GBDT_EUNSUPPORTED;
+  // One workgroup a compute unit goes through the tiles where there is no room for two; else one a tile, as far as a launch goes.
   const int64_t units = std::max(8, gbdt_internal::cu_count() / 8 * 8);
-  *blocks = (unsigned)(S::BM >= 256 ? std::min(n, units) : n);
+  *blocks = (unsigned)std::min(n, S::BM >= 256 ? units : most_blocks(S::NT));
   return GBDT_OK;
 }
 
@@ -451,7 +460,7 @@ int launch_product(gbdt_softmax::PieceArgs<T>& g, hipStream_t s) {
   g.col_tiles = (uint32_t)ceil_div(g.cols, S::BN);
   g.group = 8;
   const int64_t blocks = (int64_t)g.row_tiles * g.col_tiles * g.splits;
-  if (blocks > kMaxBlocks) return GBDT_EUNSUPPORTED;
+  if (blocks > most_blocks(S::NT)) return GBDT_EUNSUPPORTED;  // (operands and G of so many tiles fit no card)
   if (blocks == 0) return GBDT_OK;
   gbdt_softmax::piece_product_kernel<S, TO_ROWS, PAIR><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
   LAUNCHED("piece_product_kernel");

@@ -10,3 +10,10 @@ MIB = 1 << 20
                                           ((1 << 30) - 1, 1, 1), (1_000_000, 5000, 5000), (100_000, (1 << 24) - 1, 3)])
 def test_sums_of_long_leaves_take_512_mib_at_most(n, d_in, d_out):
     assert 0 < B.gbdt_leaf_product_grad_workspace_bytes(n, d_in, d_out) <= 513 * MIB
+
+
+def test_matrices_of_too_many_tiles_are_refused():
+    """f32, 9 x 262,144 tiles of 64 x 64; refused before anything is enqueued, the gradient of the input too."""
+    big = (1 << 24) - 1
+    for dx in (None, 4096):
+        assert B.load().gbdt_leaf_product_grad(4096, 513, 4096, big, 4096, None, 4096, 1, 1, 1, big, 513, 0, dx, big, 4096, None, None) == -2
