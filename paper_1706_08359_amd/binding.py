@@ -187,6 +187,17 @@ def _stream(stream) -> int:
     return int(stream)
 
 
+def _made(make, shape, dtype, device, stream):
+    """make(shape) for an output of a call on `stream`: allocated, and cleared by torch.zeros, there and not on the current
+    stream, whose work the call does not wait for."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device) if int(stream) else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=device)
+
+
 def _dev(t: torch.Tensor, dtype, name: str) -> int:
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name}: expected a contiguous CUDA tensor of dtype {dtype}")
@@ -749,7 +760,7 @@ def gbdt_leaf_product(x, weight, leaf_offsets, row_idx=None, bias=None, y_out=No
     b_p = None if bias is None else _dense(bias, x.dtype, (n_leaves, d_out), "bias")
     idx_p, off_p, n_positions = _leaf_lists(leaf_offsets, row_idx, n_leaves, n_rows)
     if y_out is None:
-        y_out = torch.zeros((n_rows, d_out), dtype=x.dtype, device=x.device)
+        y_out = _made(torch.zeros, (n_rows, d_out), x.dtype, x.device, stream)
     y_p, ld_y = _mat(y_out, x.dtype, n_rows, d_out, "y_out")
     _check(load().gbdt_leaf_product(x_p, ld_x, w_p, b_p, idx_p, off_p, n_positions, n_leaves, n_rows, d_in, d_out, code,
                                     y_p, ld_y, _stream(stream)), "gbdt_leaf_product")
@@ -775,15 +786,15 @@ def gbdt_leaf_product_grad(dy, x, weight, leaf_offsets, row_idx=None, dx_out=Non
     ld_dx = d_in
     if "x" in want:
         if dx_out is None:
-            dx_out = torch.zeros((n_rows, d_in), dtype=x.dtype, device=x.device)
+            dx_out = _made(torch.zeros, (n_rows, d_in), x.dtype, x.device, stream)
         dx_p, ld_dx = _mat(dx_out, x.dtype, n_rows, d_in, "dx_out")
     if "weight" in want:
         if dweight_out is None:
-            dweight_out = torch.empty((n_leaves, d_out, d_in), dtype=x.dtype, device=x.device)
+            dweight_out = _made(torch.empty, (n_leaves, d_out, d_in), x.dtype, x.device, stream)
         dw_p = _dense(dweight_out, x.dtype, (n_leaves, d_out, d_in), "dweight_out")
     if "bias" in want:
         if dbias_out is None:
-            dbias_out = torch.empty((n_leaves, d_out), dtype=x.dtype, device=x.device)
+            dbias_out = _made(torch.empty, (n_leaves, d_out), x.dtype, x.device, stream)
         db_p = _dense(dbias_out, x.dtype, (n_leaves, d_out), "dbias_out")
     _check(load().gbdt_leaf_product_grad(dy_p, ld_dy, x_p, ld_x, w_p, idx_p, off_p, n_positions, n_leaves, n_rows, d_in,
                                          d_out, code, dx_p, ld_dx, dw_p, db_p, _stream(stream)),
@@ -812,9 +823,9 @@ def gbdt_softmax_loss(h, classes, labels=None, loss_out=None, lse_out=None, stre
     (loss, lse), float32 [n_rows]; loss is None without labels."""
     code, n_rows, n_classes, dim, h_p, ld_h, c_p, ld_c, y_p = _softmax_operands(h, classes, labels)
     if labels is not None and loss_out is None:
-        loss_out = torch.empty(n_rows, dtype=torch.float32, device=h.device)
+        loss_out = _made(torch.empty, (n_rows,), torch.float32, h.device, stream)
     if lse_out is None:
-        lse_out = torch.empty(n_rows, dtype=torch.float32, device=h.device)
+        lse_out = _made(torch.empty, (n_rows,), torch.float32, h.device, stream)
     loss_p = None if loss_out is None else _dense(loss_out, torch.float32, (n_rows,), "loss_out")
     _check(load().gbdt_softmax_loss(h_p, ld_h, c_p, ld_c, y_p, n_rows, n_classes, dim, code, loss_p,
                                     _dense(lse_out, torch.float32, (n_rows,), "lse_out"), _stream(stream)),
@@ -836,11 +847,11 @@ def gbdt_softmax_grad(h, classes, labels, lse, row_weight=None, scale=1.0, dh_ou
     ld_dh = ld_dc = dim
     if "h" in want:
         if dh_out is None:
-            dh_out = torch.empty((n_rows, dim), dtype=h.dtype, device=h.device)
+            dh_out = _made(torch.empty, (n_rows, dim), h.dtype, h.device, stream)
         dh_p, ld_dh = _mat(dh_out, h.dtype, n_rows, dim, "dh_out")
     if "classes" in want:
         if dclasses_out is None:
-            dclasses_out = torch.empty((n_classes, dim), dtype=h.dtype, device=h.device)
+            dclasses_out = _made(torch.empty, (n_classes, dim), h.dtype, h.device, stream)
         dc_p, ld_dc = _mat(dclasses_out, h.dtype, n_classes, dim, "dclasses_out")
     _check(load().gbdt_softmax_grad(h_p, ld_h, c_p, ld_c, y_p, _dense(lse, torch.float32, (n_rows,), "lse"), w_p,
                                     float(scale), n_rows, n_classes, dim, code, dh_p, ld_dh, dc_p, ld_dc,
@@ -856,9 +867,9 @@ def gbdt_softmax_stats(h, classes, labels, lse, class_begin, class_end, grad_out
     if class_begin < 0 or count < 0 or class_end > n_classes:
         raise GbdtError("class_begin, class_end: outside the classes")
     if grad_out is None:
-        grad_out = torch.empty((count, n_rows), dtype=torch.float32, device=h.device)
+        grad_out = _made(torch.empty, (count, n_rows), torch.float32, h.device, stream)
     if hess_out is None:
-        hess_out = torch.empty((count, n_rows), dtype=torch.float32, device=h.device)
+        hess_out = _made(torch.empty, (count, n_rows), torch.float32, h.device, stream)
     g_p, ld_g = _mat(grad_out, torch.float32, count, n_rows, "grad_out")
     k_p, ld_k = _mat(hess_out, torch.float32, count, n_rows, "hess_out")
     if ld_g != ld_k:
