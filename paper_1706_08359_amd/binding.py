@@ -716,7 +716,7 @@ def _mat(t: torch.Tensor, dtype, rows, cols: int, name: str):
     if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.shape == (rows, cols):
         first, inner = t.stride()
         if inner == 1 and first >= cols:
-            return t.data_ptr(), first
+            return t.data_ptr(), first if rows > 1 else cols
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[1] == cols
             and (rows is None or t.shape[0] == rows)):
         raise TypeError(f"{name}: expected a CUDA tensor of dtype {dtype} and shape [{'n' if rows is None else rows}, {cols}]")
