@@ -513,7 +513,8 @@ size_t gbdt_leaf_product_grad_workspace_bytes(int64_t n_positions, int32_t d_in,
  *            its h holds.  NULL (loss_out NULL as well): every row counts and none has a label
  *   loss_out, lse_out   DEVICE float [n_rows]
  * n_rows and n_classes < 2^30, dim < 2^24, ld_h and ld_c < 2^28 (GBDT_EUNSUPPORTED beyond).  An infinite or NaN score
- * goes where the formula takes it.
+ * goes where the formula takes it.  Scratch: a maximum and a sum for every row and 128 classes (f32: 64), of so many rows at a
+ * time as take 256 MiB, or of 256.
  */
 int gbdt_softmax_loss(const void* h, int64_t ld_h, const void* classes, int64_t ld_c,
                       const int32_t* labels, int64_t n_rows, int64_t n_classes, int32_t dim,

@@ -294,7 +294,7 @@ constexpr int64_t kPieceAlign = 256;                    // classes: whole tiles 
 // G of a piece, as long as it is kPieceAlign classes wide at least.  8,192 x 65,536 x 1,024 bf16, loss and gradients: 4.07 ms at
 // 128 MiB, 3.95 at 256, 3.85 at 512, 3.95 in one piece of 1 GiB.
 constexpr int64_t kPieceBytes = (int64_t)512 << 20;
-constexpr int64_t kPartsBytes = (int64_t)256 << 20;     // maxima and sums of a launch's tiles
+constexpr int64_t kPartsBytes = (int64_t)256 << 20;     // maxima and sums of a launch's tiles, of 256 rows at least
 
 int softmax_check(const void* h, int64_t ld_h, const void* c, int64_t ld_c, int64_t n_rows, int64_t n_classes, int32_t dim,
                   int32_t dtype) {
@@ -333,7 +333,8 @@ template <typename T>
 LossPlan loss_plan(int64_t n_rows, int64_t n_classes) {
   LossPlan p;
   p.tiles = ceil_div(n_classes, gbdt_softmax::kPartClasses<T>);
-  p.rows = std::min(n_rows, std::max<int64_t>(4096, kPartsBytes / (8 * p.tiles) / 4096 * 4096));
+  const int64_t fit = kPartsBytes / (8 * p.tiles), whole = fit >= 4096 ? 4096 : 256;
+  p.rows = std::min(n_rows, std::max<int64_t>(256, fit / whole * whole));
   p.parts_bytes = pad256((size_t)(p.rows * p.tiles) * 8);
   p.bytes = p.parts_bytes + pad256((size_t)p.rows * 4);
   return p;
