@@ -50,7 +50,9 @@ def route(nodes: np.ndarray, bins: torch.Tensor, leaves: np.ndarray):
 
 class Model:
     """x: [n_rows, n_features] float32 or bfloat16, the values the leaves are linear in; bins: uint8 of the same rows, what
-    the trees split on; labels: int32 (outside [0, n_classes): the row is left out of the training)."""
+    the trees split on; labels: int32 (outside [0, n_classes): the row is left out of the training).
+    What is added to tree after tree, the rows' embeddings and the classes, is kept in 32 bits; `embed` and `classes` are
+    rounded to x's type, as the products take them."""
 
     def __init__(self, x, bins, n_bins, labels, n_classes, dim, seed=0):
         gen = torch.Generator(device=x.device)
@@ -58,10 +60,26 @@ class Model:
         self.x, self.bins, self.n_bins, self.labels = x, bins, n_bins, labels
         self.packed = B.gbdt_bins_pack(bins, n_bins)
         self.n_rows, self.n_classes = x.shape[0], n_classes
-        self.classes = (torch.randn(n_classes, dim, generator=gen, device=x.device) * dim ** -0.5).to(x.dtype)
-        self.embed = torch.zeros(self.n_rows, dim, dtype=x.dtype, device=x.device)
+        self._classes = (torch.randn(n_classes, dim, generator=gen, device=x.device) * dim ** -0.5).to(x.dtype).float()
+        self._embed = torch.zeros(self.n_rows, dim, device=x.device)
         self.counted = int(((labels >= 0) & (labels < n_classes)).sum())
         self.trees = []
+
+    @property
+    def classes(self):
+        return self._classes.to(self.x.dtype)
+
+    @classes.setter
+    def classes(self, value):
+        self._classes = value.float()
+
+    @property
+    def embed(self):
+        return self._embed.to(self.x.dtype)
+
+    @embed.setter
+    def embed(self, value):
+        self._embed = value.float()
 
     def loss(self):
         """(mean loss over the rows that count, lse)."""
@@ -70,44 +88,42 @@ class Model:
 
     def add_tree(self, max_leaves=31, steps=10, rate=1.0, lam=1.0, min_child_hess=1e-3, candidates=16):
         """Grows a tree, trains its leaves and the classes; returns the mean loss after the last step's gradient."""
-        _, lse = B.gbdt_softmax_loss(self.embed, self.classes, self.labels)
+        embed, classes = self.embed, self.classes
+        _, lse = B.gbdt_softmax_loss(embed, classes, self.labels)
         begin = (len(self.trees) * candidates) % max(1, self.n_classes - candidates + 1)
-        grad, hess = B.gbdt_softmax_stats(self.embed, self.classes, self.labels, lse, begin,
+        grad, hess = B.gbdt_softmax_stats(embed, classes, self.labels, lse, begin,
                                           min(self.n_classes, begin + candidates))
         k = int((grad.double() ** 2).sum(1).argmax())
         nodes, row_idx, _ = B.gbdt_grow_tree(self.packed, self.n_rows, self.bins.shape[1], self.n_bins, grad[k], hess[k],
                                              max_leaves, lam, min_child_hess)
         leaves, offsets = leaf_lists(nodes, self.x.device)
-        d_in, dim = self.x.shape[1], self.classes.shape[1]
-        # the gradient steps are taken in 32 bits, on copies of what the products read
+        d_in, dim, dtype = self.x.shape[1], classes.shape[1], self.x.dtype
+        # the gradient steps are taken in 32 bits; the products read copies
         weight = torch.zeros(len(leaves), dim, d_in, device=self.x.device)
         bias = torch.zeros(len(leaves), dim, device=self.x.device)
-        classes = self.classes.float()
-        base = self.embed
-        y = torch.empty_like(base)
+        y = torch.empty_like(embed)
         for _ in range(steps):
-            w, b, c = weight.to(base.dtype), bias.to(base.dtype), classes.to(base.dtype)
+            w, b, c = weight.to(dtype), bias.to(dtype), self.classes
             B.gbdt_leaf_product(self.x, w, offsets, row_idx=row_idx, bias=b, y_out=y)
-            h = base + y
+            h = (self._embed + y).to(dtype)
             loss, lse = B.gbdt_softmax_loss(h, c, self.labels)
             dh, dc = B.gbdt_softmax_grad(h, c, self.labels, lse, scale=1.0 / max(self.counted, 1))
             _, dw, db = B.gbdt_leaf_product_grad(dh, self.x, w, offsets, row_idx=row_idx, want=("weight", "bias"))
             weight -= rate * dw.float()
             bias -= rate * db.float()
-            classes -= rate * dc.float()
-        self.classes = classes.to(base.dtype)
-        w, b = weight.to(base.dtype), bias.to(base.dtype)
-        self.embed = base + B.gbdt_leaf_product(self.x, w, offsets, row_idx=row_idx, bias=b, y_out=y)
+            self._classes = self._classes - rate * dc.float()
+        w, b = weight.to(dtype), bias.to(dtype)
+        self._embed = self._embed + B.gbdt_leaf_product(self.x, w, offsets, row_idx=row_idx, bias=b, y_out=y)
         self.trees.append((nodes, leaves, w, b))
         return self.loss()[0]
 
     def embed_rows(self, x, bins):
         """Embeddings of other rows (one row is answered as well as many)."""
-        h = torch.zeros(x.shape[0], self.classes.shape[1], dtype=x.dtype, device=x.device)
+        h = torch.zeros(x.shape[0], self._classes.shape[1], device=x.device)
         for nodes, leaves, w, b in self.trees:
             row_idx, offsets = route(nodes, bins, leaves)
-            h = h + B.gbdt_leaf_product(x, w, offsets, row_idx=row_idx, bias=b)
-        return h
+            h += B.gbdt_leaf_product(x, w, offsets, row_idx=row_idx, bias=b)
+        return h.to(x.dtype)
 
     def probabilities(self, x, bins, class_begin=0, class_end=None):
         """[classes, rows]: the softmax of other rows for a range of classes."""
