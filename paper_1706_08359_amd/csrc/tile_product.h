@@ -128,7 +128,6 @@ struct RowOperand {
   static constexpr int kPer = (kSlots + NT - 1) / NT;
   static constexpr int kLoads = kPer;  // of device memory, a step
   static constexpr int kBytes = R * KB;
-  static constexpr int kReads = 1;  // a fragment
   const T* row[kPer];  // DIRECT: of the chunk that is loaded next
   const T* end;
   u32x4 reg[DIRECT ? 1 : kPer];
@@ -244,7 +243,6 @@ struct ColumnOperand {
   static constexpr int kLoads = kPer;  // of device memory, a step
   static constexpr int kBytes = R * KB;
   static constexpr int kChunks = R / kChunk<T>;  // a row
-  static constexpr int kReads = sizeof(T) == 2 ? 2 : 4;
   static_assert(kSlots % NT == 0, "every thread has as many chunks");
   int id[kPer];  // of the step that is loaded next
   const T* here[DIRECT ? kPer : 1];  // DIRECT and rows a constant distance apart: the chunk that is loaded next
