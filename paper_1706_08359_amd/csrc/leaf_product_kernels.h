@@ -119,7 +119,8 @@ __device__ __forceinline__ PlainRows<T> plain_rows(const T* base, int64_t ld, in
 
 // The rows of one tile of positions times a matrix of the leaf, g.cols_per column tiles one after another; the next one's
 // first steps are on their way while one's values are stored.  B: the matrix' orientation, k its length along k.
-// GROUPS > 1: as many times the tile's threads take a part of k each, all of as many steps, and the first adds up.
+// GROUPS > 1: as many times the tile's threads take a part of k each, all of as many steps, and the first adds up; one column
+// tile a workgroup then, since the other groups leave after it.
 template <class S, class B, int GROUPS, typename T>
 __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& g, const T* in, int64_t ld_in, int k, const T* bias_all,
                                                   T* out, int64_t ld_out, int cols) {

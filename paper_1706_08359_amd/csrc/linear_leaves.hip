@@ -91,6 +91,7 @@ int leaf_rows_launches(gbdt_leaf::LeafArgs<T>& g, int64_t cols, int threads, con
   const int64_t most = (S::BM >= 256 ? 4 : 8) * gbdt_internal::cu_count();  // one or two at a time on a unit
   g.col_tiles = (uint32_t)col_tiles;
   g.cols_per = (uint32_t)std::max<int64_t>(1, std::min(col_tiles, (int64_t)g.n_positions / S::BM * col_tiles / most));
+  if (threads > S::NT) g.cols_per = 1;  // several groups of threads a tile
   const int64_t n = row_tiles * ceil_div(col_tiles, g.cols_per);
   if (n > kMaxTiles) return GBDT_EUNSUPPORTED;
   for (int64_t first = 0; first < n; first += most_blocks(threads)) {
