@@ -121,15 +121,24 @@ bool wide_leaves(const gbdt_leaf::LeafArgs<T>& g, int64_t cols) {
   return cols > 128 && long_leaves(g, cols, 256);
 }
 
-// So few answers that a wavefront for every few of them takes less than tiles, whose rows are mostly empty then: 64 positions,
-// or up to 2,048 with 16,384 outputs altogether; twice that (f32: four times) where leaves have fewer than four positions on
-// average, since each has a tile of its own.  (255 leaves, 2,000 -> 256: 64 positions in 12.5 us against 34 in tiles, f32 19.5
-// against 111; 128 in 18 against 36; 512 in 44 against 39.  One leaf, 700 -> 256: 128 in 9.1 against 9.4, 256 in 14.5 against
-// 9.3.  700 -> 1, 2,048 positions: 4.9 against 8.7; 28 -> 1, 4,096: 5.1 against 4.6.)
+// So few answers that a wavefront for every few of them takes less than tiles, whose rows are mostly empty then: four
+// positions, or up to 2,048 with 16,384 outputs altogether (up to 64 of them twice that where rows are no whole chunks, which cost
+// tiles more).  Where leaves have fewer than four positions on average, each has a tile of its own, and it is 64 positions whatever
+// the outputs, or twice as many outputs (f32: four times).  (255 leaves, 2,000 -> 256: 64 positions in 12.5 us against 34 in
+// tiles, f32 19.5 against 111; 128 in 18 against 36; 512 in 44 against 39; 700 -> 10,000: 64 in 190 against 282.  One leaf, 700 ->
+// 256: 128 in 9.1 against 9.4, 256 in 14.5 against 9.3; 700 -> 10,000: 4 in 12 against 16, 16 in 34 against 16, 64 in 114 against
+// 17; 137 -> 1,000: 32 in 6.5 against 8.8.  700 -> 1, 2,048 positions: 4.9 against 8.7; 28 -> 1, 4,096: 5.1 against 4.6.)
 template <typename T>
-bool few_answers(const gbdt_leaf::LeafArgs<T>& g) {
-  const int64_t most = 16384 * (g.n_positions >= 4 * (int64_t)g.n_leaves ? 1 : sizeof(T) == 2 ? 2 : 4);
-  return g.n_positions <= 64 || (g.n_positions <= 2048 && (int64_t)g.n_positions * g.d_out <= most);
+bool few_answers(const gbdt_leaf::LeafArgs<T>& g, bool direct) {
+  const int64_t n = g.n_positions;
+  int64_t most = 16384;
+  if (n < 4 * (int64_t)g.n_leaves) {
+    if (n <= 64) return true;
+    most *= sizeof(T) == 2 ? 2 : 4;
+  } else if (n <= 64 && !direct) {
+    most *= 2;
+  }
+  return n <= 4 || (n <= 2048 && n * g.d_out <= most);
 }
 
 template <typename T>
@@ -164,8 +173,8 @@ bool few_tiles(const gbdt_leaf::LeafArgs<T>& g) {
 
 template <typename T>
 int leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  if (few_answers(g)) return leaf_product_few(g, s);
   const bool direct = whole_chunks<T>(g.x, g.ld_x, g.d_in) && whole_chunks<T>(g.w, g.d_in, g.d_in);
+  if (few_answers(g, direct)) return leaf_product_few(g, s);
   if (few_tiles(g)) {
     if constexpr (sizeof(T) == 2) {
       return direct ? launch_leaf_product_split<Shape<T, 64, 64, 2, 2, true>, 4>(g, s)
