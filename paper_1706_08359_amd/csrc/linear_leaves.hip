@@ -400,6 +400,7 @@ int softmax_loss(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
 
 struct GradPlan {
   bool pair;       // G as two values: one piece, tiles of kPairClasses
+  bool wide_dh;    // tiles of 256 x 256
   int64_t width;   // classes a piece
   int64_t pieces;
   int64_t dh_splits, dh_split, dc_splits, dc_split;
@@ -426,12 +427,14 @@ GradPlan grad_plan(int64_t n_rows, int64_t n_classes, int64_t dim, int64_t e, bo
   const int64_t tile = e == 2 ? 128 : 64;
   const int64_t cols = ceil_div(dim, tile);
   split_axis(ceil_div(rows, tile) * cols, p.width, step, 2 * units, &p.dh_splits, &p.dh_split);
-  // Large tiles of dh even if it takes splits to have one for every unit, of 16 steps at least.  (4,096 x 32,768 x 512: 615 us
-  // against 633 with small ones.)
+  // Large tiles of dh for more than 128 columns, even if it takes splits to have as many as there are units, of 16 steps at
+  // least.  (dh and its G, tiles of 128 x 128 against these: 3,000 x 50,000 x 1,024: 749 us against 602, 8,200 x 40,000 x 520: 1,143 against
+  // 974, 500 x 33,000 x 512: 87 and 86; 1,400 x 65,536 x 40: 109 against 120.)
   const int64_t wide = ceil_div(rows, 256) * ceil_div(dim, 256);
-  if (e == 2 && !p.pair && wide < units && wide * ceil_div(p.width, 16 * step) >= units)
+  p.wide_dh = e == 2 && !p.pair && dim > 128 && wide * ceil_div(p.width, 16 * step) >= units;
+  if (p.wide_dh && wide < units)
     split_axis(wide, p.width, step, units, &p.dh_splits, &p.dh_split);
-  else if (e == 2 && !p.pair && wide >= units)
+  else if (p.wide_dh)
     p.dh_splits = 1, p.dh_split = round_up(p.width, step);
   split_axis(ceil_div(p.width, tile) * cols, n_rows, step, 2 * units, &p.dc_splits, &p.dc_split);
   p.g_bytes = pad256((size_t)(rows * p.width * e));
@@ -601,7 +604,7 @@ int softmax_grad(const T* h, int64_t ld_h, const T* c, int64_t ld_c, const int32
       to_h.k_split = (int32_t)plan.dh_split;
       to_h.splits = (uint32_t)plan.dh_splits;
       to_h.add = begin > 0;
-      if ((rc = product<true>(to_h, plan.pair, wide_tiles<T>(n_rows * plan.dh_splits, dim), s)) != GBDT_OK) return rc;
+      if ((rc = product<true>(to_h, plan.pair, plan.wide_dh, s)) != GBDT_OK) return rc;
     }
   }
   if (dh && n_rows > 0 && dh_sums) return join_product(to_h, s);

@@ -33,8 +33,9 @@ def exactness(h, c, y, w, scale, lse, got):
     (1100, 33_000, 512, None),     # classes' gradient in tiles of 256 x 256, scores over 16 steps
     (4100, 33_000, 512, 0.5),      # the same with two thousand labels in its first tile
     (4090, 100_000, 505, None),    # two pieces, rows' gradient split eight ways in tiles of 256 x 256, copies of odd rows
-    (8200, 40_000, 520, None),     # two pieces and splits in smaller tiles, columns that end inside a tile
-    (1400, 194_174, 40, None),     # two pieces, the last split of the shorter one empty
+    (8200, 40_000, 520, None),     # two pieces and splits, columns that end inside a tile
+    (1400, 194_174, 40, None),     # two pieces and splits in tiles of 128 x 128
+    (1600, 170_150, 40, None),     # the same, the last split of the shorter piece empty
     (20_000, 200, 4096, 0.9),      # more labels of a tile of 128 classes than a list holds
 ])
 def test_large_bf16_gradients(n, v, dim, few):
