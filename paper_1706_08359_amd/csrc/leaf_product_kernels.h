@@ -300,6 +300,7 @@ struct RowSums {
 // 100,000 x 2,000 x 256 in 255 leaves, bf16: 343 us, 2.1 TB/s, 300 TFLOP/s; 50,021 x 137 x 33 in 63, f32: 30 us.
 // The list's ids are copied to local memory first, kCopiedIds at a time: loads are waited for in order, so a row's address that
 // waits for an id on its way from memory waits for all chunks asked for before as well, and steps do not overlap.
+// LONG: pieces may be longer than that.  (The loop over copies takes 38 registers more, and spills them without whole chunks.)
 constexpr int kCopiedIds = 4096;
 constexpr int kShortPiece = 1024;  // positions
 static_assert(kShortPiece <= kCopiedIds, "a piece of several column tiles a workgroup is copied at once");
@@ -326,7 +327,7 @@ __device__ __forceinline__ Piece find_piece(const LeafArgs<T>& g, int piece) {
   return r;
 }
 
-template <class S>
+template <class S, bool LONG>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
@@ -358,7 +359,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   int c0 = p0, c1 = p0;  // the positions copied
   auto copy_ids = [&](int from) {
     c0 = rows_a.first = rows_b.first = from;
-    c1 = p1 - from < kCopiedIds ? p1 : from + kCopiedIds;
+    c1 = !LONG || p1 - from < kCopiedIds ? p1 : from + kCopiedIds;
     for (int p = c0 + (int)threadIdx.x; p < c1; p += S::NT) {
       const int d = g.row_idx ? g.row_idx[p] : p;
       ids[p - c0] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
@@ -381,7 +382,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
     const bool sums = __builtin_amdgcn_readfirstlane(g.dbias != nullptr && col == 0 && w % S::WN == 0);
     for (;;) {
       tile_run<S, true>(lds, a, b, rows_a, rows_b, c0, c1, acc, RowSums<S>{sum, sums});
-      if (c1 >= p1) break;
+      if (!LONG || c1 >= p1) break;
       __syncthreads();  // everyone has read the last of these ids
       copy_ids(c1);
       begin_columns(col);

@@ -245,7 +245,11 @@ int launch_leaf_grad_weight(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
   for (int64_t first = 0; first < pieces; first += at_once) {
     g.first = (uint32_t)first;
     const int64_t blocks = round_up(std::min(pieces - first, at_once), 8) * a_piece;
-    gbdt_leaf::leaf_grad_weight_kernel<S><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+    if (g.cut > gbdt_leaf::kCopiedIds) {
+      gbdt_leaf::leaf_grad_weight_kernel<S, true><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+    } else {
+      gbdt_leaf::leaf_grad_weight_kernel<S, false><<<dim3((unsigned)blocks), dim3(S::NT), 0, s>>>(g);
+    }
     LAUNCHED("leaf_grad_weight_kernel");
   }
   return GBDT_OK;

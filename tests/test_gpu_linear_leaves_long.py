@@ -10,11 +10,11 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [5000, 4999])
 @pytest.mark.parametrize("sizes", [[11_600, 0, 400], [100, 5900, 6000], [12_000]], ids=str)
-def test_parts_longer_than_a_listing(sizes, dtype):
+def test_parts_longer_than_a_listing(sizes, d, dtype):
     """Matrices so large that only two cuts fit the scratch: 6,016 positions between them."""
     from paper_1706_08359_amd import binding as B
-    d = 5000
     need = B.gbdt_leaf_product_grad_workspace_bytes(12_000, d, d)
     assert need < 520 << 20
     x, dy, w, b, offs, idx = make(12_001, sizes, d, d, dtype, seed=len(sizes))

@@ -57,3 +57,14 @@ def test_both_sides_of_the_limit_agree(v):
     got = B.gbdt_softmax_grad(h, c, y, lse, row_weight=w, scale=0.1)
     for a, e in ((got[0][:, :48], few[0]), (got[1][:128, :48], few[1])):
         assert float((a.double() - e.double()).norm()) <= (0.0 if v == 128 else 4e-3) * float(e.double().norm())
+
+
+def test_no_rows_and_nothing_but_ignored_ones():
+    from paper_1706_08359_amd import binding as B
+    h, c, y, w = make(300, 30, 48, 2.0, 7, False)
+    dh, dc = B.gbdt_softmax_grad(h[:0], c, y[:0], torch.empty(0, device="cuda"))
+    assert dh.shape == (0, 48) and dc.shape == (30, 48) and not bool(dc.any())
+    y.fill_(30)
+    h[::2], w[::3] = float("nan"), float("inf")
+    dh, dc = B.gbdt_softmax_grad(h, c, y, torch.zeros(300, device="cuda"), row_weight=w)
+    assert not bool(dh.any()) and not bool(dc.any())
