@@ -731,10 +731,9 @@ size_t gbdt_leaf_product_grad_workspace_bytes(int64_t n_positions, int32_t d_in,
   if (n_positions < 0 || n_positions >= kMaxRows || d_in <= 0 || d_out <= 0 || d_in >= kMaxWidth || d_out >= kMaxWidth) return 0;
   const int64_t units = gbdt_internal::cu_count();
   size_t most = 0;
-  for (int64_t e : {2, 4}) {  // with the weights' gradient and without
-    most = std::max(most, leaf_grad_plan(e, n_positions, d_in, d_out, units).bytes);
-    most = std::max(most, leaf_grad_plan(e, n_positions, 16 / e, d_out, units).bytes);
-  }
+  for (int64_t e : {2, 4})
+    for (int64_t inputs : {(int64_t)d_in, 16 / e, (int64_t)1})  // with the weights' gradient and without
+      most = std::max(most, leaf_grad_plan(e, n_positions, inputs, d_out, units).bytes);
   return gbdt_internal::workspace_head_bytes() + most;
 }
 

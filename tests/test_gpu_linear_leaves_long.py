@@ -47,3 +47,23 @@ def test_more_positions_than_cuts_of_a_listing():
         a, e = edges[leaf], edges[leaf + 1]
         assert int(dw[leaf, 0, 0]) == int((x[a:e] * dy[a:e]).double().sum())
         assert int(db[leaf, 0]) == int(dy[a:e].double().sum()) < 1 << 24
+
+
+@pytest.mark.parametrize("d_out", [7_000_000, 7_000_001])
+def test_outputs_sums_alone_of_wide_rows_fit_the_stated_scratch(d_out):
+    """Sums of 7 million outputs: one matrix' sums would pass the scratch, so that the weights' gradient has one part; the outputs'
+    alone have two.  The list names one row, of ones, 4,160 times (sums do not mind)."""
+    from paper_1706_08359_amd import binding as B
+    n = 4160
+    dy = torch.ones(1, d_out, dtype=torch.bfloat16, device="cuda")
+    idx, offs = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.tensor([0, n], device="cuda")
+    got = torch.zeros(1, d_out, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(B.gbdt_leaf_product_grad_workspace_bytes(n, 8, d_out), dtype=torch.uint8, device="cuda")
+    B.gbdt_set_workspace(ws)
+    try:
+        rc = B.load().gbdt_leaf_product_grad(dy.data_ptr(), d_out, None, 0, None, idx.data_ptr(), offs.data_ptr(), n, 1, 1, 8, d_out,
+                                             1, None, 0, None, got.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+    finally:
+        B.gbdt_set_workspace(None)
+    assert rc == 0 and bool((got == n).all())
