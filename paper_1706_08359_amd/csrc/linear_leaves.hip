@@ -73,9 +73,9 @@ using SquareAny = typename std::conditional<sizeof(T) == 2, Shape<T, 128, 128, 2
 // and its loads never the bound).
 template <typename T>
 using Wide = typename std::conditional<sizeof(T) == 2, Shape<T, 256, 256, 2, 4, true, true>, Square<T>>::type;
-// Taken where there is one for every unit.  (Softmax's loss, 4,096 x 32,768 x 512: 136 us against 156 in tiles of 128, 8,192 x
-// 65,536 x 1,024: 884 against 1,066, 4,096 x 4,096 x 512, a tile a unit: 23 against 29; 2,048 x 4,096 x 1,024, a tile for
-// every other unit: 31 against 26.)
+// Taken where there is one for every unit.  (Softmax's loss, 4,096 x 32,768 x 512: 143 us against 159 in tiles of 128, 8,192 x
+// 65,536 x 1,024: 917 against 1,100, 8,192 x 32,768 x 128: 141 against 153, 4,096 x 4,096 x 512, a tile a unit: 22 against 27; 2,048 x
+// 4,096 x 1,024, a tile for every other unit: 30 against 25.)
 template <typename T>
 bool wide_tiles(int64_t rows, int64_t cols) {
   return sizeof(T) == 2 && ceil_div(rows, 256) * ceil_div(cols, 256) >= 256;

@@ -141,8 +141,9 @@ struct OfRows {
 
 // Bound by the matrix cores for many rows and by the read of c for few; a lane's values meet in its registers, lanes of a row
 // through local memory, once a tile.  The exponentials are the next cost, one for every `dim` products, so that 512
-// dimensions reach less of the rate than 1,024.  (8,192 x 65,536 x 1,024 bf16: loss in 884 us, 1.24 PFLOP/s; 4,096 x 32,768 x 512: 136,
-// 1.01; one row of 50,000 x 512: 14 us, 3.7 TB/s; 1,537 x 10,007 x 137 f32, no whole chunks: 67 us, 63 TFLOP/s.)
+// dimensions reach less of the rate than 1,024.  (8,192 x 65,536 x 1,024 bf16: 900 to 1,000 us, 1.1 to 1.2 PFLOP/s, the less the warmer
+// the card, matrix cores busy for 57 % of the cycles; 4,096 x 32,768 x 512: 136 to 146, 0.94 to 1.0, 43 %; one row of 50,000 x 512: 14
+// us, 3.7 TB/s; 1,537 x 10,007 x 137 f32, no whole chunks: 67 us, 63 TFLOP/s, 50 %.)
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) softmax_scores_kernel(const ScoreArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
@@ -239,7 +240,8 @@ __global__ void __launch_bounds__(256) softmax_join_kernel(const MaxSum* parts, 
 }
 
 // The scores again, and G of a piece, stored in whole lines.  Bound by the same, and by the stores of G (for every `dim` products
-// one exponential and one stored value): 8,192 x 65,536 x 1,024 bf16 in two pieces, 594 us each, 0.93 PFLOP/s and 0.9 TB/s of G.
+// one exponential and one stored value): 8,192 x 65,536 x 1,024 bf16 in two pieces, 587 us each, 0.94 PFLOP/s and 0.9 TB/s of G,
+// matrix cores busy for 44 % of the cycles.
 // PAIR: one tile holds all classes, and what rounding takes from them is stored behind them.
 template <class S, bool PAIR>
 __global__ void __launch_bounds__(S::NT, 2) softmax_piece_kernel(const ScoreArgs<typename S::T> g) {
@@ -318,7 +320,7 @@ __global__ void __launch_bounds__(S::NT, 2) softmax_piece_kernel(const ScoreArgs
 
 // Two columns of f32 a score are stored, which bounds it up to some hundred dimensions: accumulators are transposed on their way
 // out, so that a column's rows leave as whole lines.  (16 classes of 400,000 x 64 f32: 31 us, 5.0 TB/s of what it reads and
-// writes, some of it from the last-level cache; 1,023 of 10,000 x 256 bf16: 28 us, 3.1 TB/s.)
+// writes, some of it from the last-level cache; 1,023 of 10,000 x 256 bf16: 28 us, 3.1 TB/s; matrix cores busy for 14 and 6 %.)
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) softmax_stats_kernel(const ScoreArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
@@ -499,8 +501,9 @@ __device__ __forceinline__ void label_rest(char* lds, const PieceArgs<typename S
 }
 
 // TO_ROWS: dh (the result's rows are G's rows, k = classes); otherwise dC (its rows are classes, k = G's rows).
-// Bound by the matrix cores and what feeds them: 8,192 x 65,536 x 1,024 bf16, a product in two pieces, dC 900 us, 1.22 PFLOP/s, dh
-// 915, 1.20; 1,537 x 10,007 x 137 f32: 72 and 76 us, 58 TFLOP/s (137 columns take three tiles of 64).
+// Bound by the matrix cores and what feeds them: 8,192 x 65,536 x 1,024 bf16, a product in two pieces, dC 877 us, 1.25 PFLOP/s, matrix
+// cores busy for 63 % of the cycles, dh 948, 1.16, 57 %; 1,537 x 10,007 x 137 f32: 71 and 76 us, 59 and 56 TFLOP/s, 53 and 51 % (137
+// columns take three tiles of 64).
 // PAIR: what rounding took from G, which lies behind it, is multiplied as well.
 template <class S, bool TO_ROWS, bool PAIR>
 __global__ void __launch_bounds__(S::NT, 2) piece_product_kernel(const PieceArgs<typename S::T> g) {
