@@ -1,0 +1,468 @@
+"""Mixtures of linear leaves, as cases for a benchmark: rows that several leaves answer with weights.
+
+A tree sends a row to one leaf.  A learned router sends it to k of them: it scores the leaves (softmax or sigmoid),
+chooses the k largest, possibly with a bias a leaf that evens out how often it is chosen and within the best groups of
+leaves only, and weighs their answers (`route`; `route_train`: with the gradient of the scores).  The row's answer is
+the weighted sum of the chosen leaves' linear maps (`mixture`; `mixture_train`: with all gradients).  For answering,
+rows and matrices are held as 8-bit integers with a scale for each row and each output (`q8`): of one leaf a row, from
+stored codes, or of k, with rows quantized in the call.
+
+Row, leaf and feature counts are those of the workloads of synth.py (10,000 x 28, 400,000 x 2,000, 137 and 700
+features, 255 leaves) and generic sizes between them; `draw` covers the ranges.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def listed():
+    return [
+        # one new row and 255 leaves: latency
+        dict(name="route_one_row", op="route", rows=1, leaves=255, k=2, score="softmax", bias=False, groups=1, kept=1,
+             best=1, renorm=True, scale=1.0, dtype="f32"),
+        # all rows of the widest matrix, 255 scores each: rows of an odd length, one pass over 408 MB
+        dict(name="route_tall", op="route", rows=400_000, leaves=255, k=4, score="softmax", bias=False, groups=1,
+             kept=1, best=1, renorm=True, scale=1.0, dtype="f32"),
+        # a batch routed within the best four of eight groups, by sigmoid scores with a bias for balance
+        dict(name="route_groups", op="route", rows=16_384, leaves=256, k=8, score="sigmoid", bias=True, groups=8,
+             kept=4, best=2, renorm=True, scale=2.5, dtype="bf16"),
+        # a training batch: choice, weights and the gradient of all scores
+        dict(name="route_train", op="route_train", rows=65_536, leaves=64, k=4, score="softmax", bias=True, groups=1,
+             kept=1, best=1, renorm=False, scale=1.0, dtype="f32"),
+        # odd sizes, 16-bit scores
+        dict(name="route_train_odd", op="route_train", rows=10_007, leaves=137, k=3, score="sigmoid", bias=True,
+             groups=1, kept=1, best=1, renorm=True, scale=1.0, dtype="bf16"),
+        # one new row answered by four of 255 leaves with 700 features: four matrices are read
+        dict(name="mixture_one_row", op="mixture", rows=1, leaves=255, k=4, d_in=700, d_out=256, pad=0, skew=0.5,
+             dtype="bf16"),
+        # a small batch to answer: each of 64 matrices is read for about four rows
+        dict(name="mixture_serve", op="mixture", rows=64, leaves=64, k=4, d_in=1024, d_out=1024, pad=0, skew=0.5,
+             dtype="bf16"),
+        # a large batch, eight leaves a row: bound by the products
+        dict(name="mixture_large", op="mixture", rows=8192, leaves=64, k=8, d_in=1024, d_out=1024, pad=0, skew=0.5,
+             dtype="bf16"),
+        # 137 features in rows of a longer buffer, 33 outputs, unequal leaves, in 32 bits
+        dict(name="mixture_train_odd", op="mixture_train", rows=20_011, leaves=63, k=3, d_in=137, d_out=33, pad=6,
+             skew=1.5, dtype="f32"),
+        # an ordinary training step
+        dict(name="mixture_train", op="mixture_train", rows=8192, leaves=64, k=4, d_in=1024, d_out=1024, pad=0,
+             skew=0.5, dtype="bf16"),
+        # embeddings from the widest matrix, which the program holds in 8 bits: one leaf a row, one pass over 0.8 GB
+        dict(name="q8_wide", op="q8", rows=400_000, leaves=255, k=0, d_in=2000, d_out=128, skew=1.0, stored=True,
+             dtype="bf16"),
+        # a batch in 16 bits, quantized in the call, four leaves a row
+        dict(name="q8_mixture", op="q8", rows=8192, leaves=64, k=4, d_in=1024, d_out=1024, skew=0.5, stored=False,
+             dtype="bf16"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["route", "route_train", "mixture", "mixture_train", "q8"])
+    dtype = rng.choice(["bf16", "bf16", "f32"])
+    if op.startswith("route"):
+        leaves = rng.choice([8, 64, 255, 256, _log_int(rng, 2, 1024), _log_int(rng, 2, 1024)])
+        groups = kept = best = 1
+        if rng.random() < 0.3:
+            groups = rng.choice([2, 4, 8])
+            leaves = max(2, leaves // groups) * groups
+            kept, best = rng.randint(1, groups), rng.randint(1, 2)
+        k = min(rng.choice([1, 2, 4, 8, rng.randint(1, 16)]), leaves // groups * kept)
+        return dict(op=op, rows=min(_log_int(rng, 1, 400_000), 100_000_000 // leaves), leaves=leaves, k=k,
+                    score=rng.choice(["softmax", "sigmoid"]), bias=rng.random() < 0.5, groups=groups, kept=kept,
+                    best=best, renorm=k > 1 and rng.random() < 0.5, scale=rng.choice([1.0, 2.5]), dtype=dtype)
+    leaves = rng.choice([8, 64, 255, _log_int(rng, 2, 400)])
+    k = min(rng.choice([1, 2, 4, 8, rng.randint(1, 12)]), leaves)
+    d_in = rng.choice([28, 137, 700, 1024, 2000, _log_int(rng, 8, 2000), 64 * rng.randint(1, 31)])
+    d_out = rng.choice([64, 256, 1024, _log_int(rng, 1, 1024)])
+    # matrices, pairs of a row and a leaf, and products no larger than those of the largest listed cases
+    d_out = max(1, min(d_out, 64_000_000 // (leaves * d_in)))
+    if op == "q8":
+        k = rng.choice([0, k])
+        pairs = 60_000_000_000 // (d_in * d_out) if k == 0 else 60_000_000 // max(d_in, d_out)
+        rows = min(_log_int(rng, 1, 400_000), 800_000_000 // d_in, pairs // max(k, 1))
+        return dict(op=op, rows=max(1, rows), leaves=leaves, k=k, d_in=d_in, d_out=d_out,
+                    skew=rng.choice([0.0, 0.5, 1.5]), stored=rng.random() < 0.5, dtype=dtype)
+    pairs = min(30_000_000 // max(d_in, d_out), (30_000_000_000 if dtype == "bf16" else 6_000_000_000) // (d_in * d_out))
+    return dict(op=op, rows=max(1, min(_log_int(rng, 1, 400_000), pairs // k)), leaves=leaves, k=k, d_in=d_in,
+                d_out=d_out, pad=rng.choice([0, 0, 8, rng.randint(1, 9)]), skew=rng.choice([0.0, 0.5, 1.5]),
+                dtype=dtype)
+
+
+def _randn(gen, *shape, dtype, scale=1.0):
+    return torch.randn(*shape, generator=gen, device="cuda", dtype=torch.float32).mul_(scale).to(dtype)
+
+
+def _matrix(gen, rows, cols, pad, dtype):
+    """Normal values, [rows, cols] inside rows of cols + pad elements; drawn in blocks of rows."""
+    buf = torch.zeros(rows, cols + pad, device="cuda", dtype=dtype)
+    for a in range(0, rows, 50_000):
+        b = min(rows, a + 50_000)
+        buf[a:b, :cols] = torch.randn(b - a, cols, generator=gen, device="cuda", dtype=torch.float32)
+    return buf[:, :cols]
+
+
+def _plain_codes(x):
+    """(codes, scales) of rows: scale = largest magnitude / 127 in 32 bits, codes the nearest whole numbers to x / scale, ties to
+    even.  The quotient in 64 bits: next to a half, 32 round it to the half itself."""
+    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scales = torch.empty(x.shape[0], device=x.device)
+    step = max(1, 100_000_000 // x.shape[1])
+    for a in range(0, x.shape[0], step):
+        v = x[a:a + step].float()
+        s = v.abs().amax(1) / 127.0
+        q = torch.where(s[:, None] > 0, v.double() / s[:, None].double(), 0.0)
+        codes[a:a + step] = torch.round(q).to(torch.int8)
+        scales[a:a + step] = s
+    return codes, scales
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    dtype = DTYPES[case["dtype"]]
+    n, leaves, k = case["rows"], case["leaves"], case["k"]
+    state = dict(op=case["op"], k=k, leaves_n=leaves)
+    if case["op"].startswith("route"):
+        # scores of a router in training: some leaves are liked more than others; a few are closed to some rows
+        liked = torch.randn(leaves, generator=gen, device="cuda") * 0.5
+        logits = torch.empty(n, leaves, device="cuda", dtype=dtype)
+        for a in range(0, n, 100_000):
+            b = min(n, a + 100_000)
+            logits[a:b] = torch.randn(b - a, leaves, generator=gen, device="cuda") + liked
+        if leaves >= 8 * k:
+            shut = torch.randint(0, n, (n // 50,), generator=gen, device="cuda")
+            logits[shut, torch.randint(0, leaves, (n // 50,), generator=gen, device="cuda")] = float("-inf")
+        state.update(logits=logits, bias=None, score=case["score"], renorm=case["renorm"], scale=case["scale"],
+                     groups=case["groups"], kept=case["kept"], best=case["best"])
+        if case["bias"]:
+            state["bias"] = torch.randn(leaves, generator=gen, device="cuda") * (0.1 if case["score"] == "sigmoid" else 0.1 / leaves)
+        if case["op"] == "route_train":
+            state["dgates"] = torch.randn(n, k, generator=gen, device="cuda")
+        return state
+    d_in, d_out = case["d_in"], case["d_out"]
+    share = case["skew"] * torch.randn(leaves, generator=gen, device="cuda")
+    if k == 0:
+        # what a grown tree leaves behind: the rows of each leaf side by side, ascending inside a leaf
+        edges = torch.cumsum(torch.exp(share), 0) / torch.exp(share).sum()
+        leaf = torch.bucketize(torch.rand(n, generator=gen, device="cuda"), edges).clamp_(max=leaves - 1)
+        order = torch.sort(leaf, stable=True)[1]
+        offsets = torch.zeros(leaves + 1, dtype=torch.int64, device="cuda")
+        offsets[1:] = torch.cumsum(torch.bincount(leaf, minlength=leaves), 0)
+        state.update(rows=order.to(torch.int32), offsets=offsets, host_offsets=offsets.tolist())
+    else:
+        # what a router chose: k leaves a row, no leaf twice
+        chosen = torch.empty(n, k, dtype=torch.int32, device="cuda")
+        for a in range(0, n, 100_000):
+            b = min(n, a + 100_000)
+            noise = -torch.log(-torch.log(torch.rand(b - a, leaves, generator=gen, device="cuda").clamp_(1e-20, 1 - 1e-7)))
+            chosen[a:b] = torch.topk(noise + share, k, dim=1)[1].to(torch.int32)
+        gates = torch.rand(n, k, generator=gen, device="cuda") + 0.1
+        state.update(leaves=chosen, gates=gates / gates.sum(1, keepdim=True))
+    x = _matrix(gen, n, d_in, case.get("pad", 0), dtype)
+    weight = _randn(gen, leaves, d_out, d_in, dtype=dtype, scale=d_in ** -0.5)
+    if case["op"] == "q8":
+        # matrices are quantized once, when a model is loaded; rows too, if the program holds them so
+        w, ws = _plain_codes(weight.view(leaves * d_out, d_in))
+        state.update(w_codes=_padded(w).view(leaves, d_out, -1), w_scales=ws.view(leaves, d_out), d_in=d_in,
+                     bias=torch.randn(leaves, d_out, generator=gen, device="cuda"), dtype=dtype)
+        if case["stored"]:
+            codes, scales = _plain_codes(x)
+            state.update(codes=_padded(codes), scales=scales)
+        else:
+            state["x"] = x
+        return state
+    state.update(x=x, weight=weight, bias=_randn(gen, leaves, d_out, dtype=dtype))
+    if case["op"] == "mixture_train":
+        state["dy"] = _matrix(gen, n, d_out, case["pad"], dtype)
+    return state
+
+
+def _padded(codes):
+    """Rows of codes as the products take them: a multiple of 16 long, zeros behind."""
+    out = torch.zeros(codes.shape[0], (codes.shape[1] + 15) // 16 * 16, dtype=torch.int8, device=codes.device)
+    out[:, :codes.shape[1]] = codes
+    return out
+
+
+def run(state):
+    return (_run_own if own else _run_plain)(state)
+
+
+def _run_own(state):
+    from paper_1706_08359_amd import binding as B
+    op, k = state["op"], state["k"]
+    if op.startswith("route"):
+        how = dict(score=state["score"], renormalise=state["renorm"], scale=state["scale"])
+        leaves, gates = B.gbdt_route(state["logits"], k, choice_bias=state["bias"], n_groups=state["groups"],
+                                     groups_kept=state["kept"], group_best=state["best"], **how)
+        if op == "route":
+            return leaves, gates
+        return leaves, gates, B.gbdt_route_grad(state["logits"], leaves, state["dgates"], **how)
+    if op == "q8":
+        codes, scales = (state["codes"], state["scales"]) if "codes" in state else B.gbdt_rows_quantize(state["x"])
+        if k == 0:
+            return B.gbdt_leaf_product_q8(codes, scales, state["w_codes"], state["w_scales"], state["offsets"],
+                                          row_idx=state["rows"], bias=state["bias"], dtype=state["dtype"])
+        return B.gbdt_mixture_product_q8(codes, scales, state["w_codes"], state["w_scales"], state["leaves"],
+                                         state["gates"], bias=state["bias"], dtype=state["dtype"])
+    y = B.gbdt_mixture_product(state["x"], state["weight"], state["leaves"], state["gates"], bias=state["bias"])
+    if op == "mixture":
+        return y
+    return (y,) + tuple(B.gbdt_mixture_product_grad(state["dy"], state["x"], state["weight"], state["leaves"],
+                                                    state["gates"], bias=state["bias"]))
+
+
+def _plain_largest(values, k):
+    """Columns of the k largest values of each row, equal ones from the left; -1 where only minus infinity is left."""
+    values, columns = values.clone(), torch.arange(values.shape[1], device=values.device)
+    out = torch.empty(values.shape[0], k, dtype=torch.int64, device=values.device)
+    for j in range(k):
+        top = values.amax(1, keepdim=True)
+        first = torch.where(values == top, columns, values.shape[1]).amin(1)
+        out[:, j] = torch.where(top[:, 0] == float("-inf"), -1, first)
+        values.scatter_(1, first[:, None], float("-inf"))
+    return out
+
+
+def _plain_route(state):
+    # in 64 bits up to the choice: scores next to each other decide which leaf is taken
+    low = float("-inf")
+    logits = state["logits"].double()
+    value = logits
+    if state["bias"] is not None or state["best"] == 2:
+        if state["score"] == "softmax":
+            e = torch.exp(logits - logits.amax(1, keepdim=True))
+            value = e / e.sum(1, keepdim=True)
+        else:
+            value = 1.0 / (1.0 + torch.exp(-logits))
+        if state["bias"] is not None:
+            value = value + state["bias"].double()
+        value = torch.where(logits == low, low, value)
+    n, groups = logits.shape[0], state["groups"]
+    if groups > 1:
+        parts = value.view(n, groups, -1)
+        worth = parts.amax(2)
+        if state["best"] == 2:
+            first = _plain_largest(parts.reshape(n * groups, -1), 2).view(n, groups, 2)
+            two = torch.where(first >= 0, parts.gather(2, first.clamp(min=0)), 0.0).sum(2)
+            worth = torch.where(worth == low, low, two)
+        keep = torch.zeros(n, groups, dtype=torch.bool, device=logits.device)
+        picked = _plain_largest(worth, state["kept"])
+        for j in range(state["kept"]):
+            keep |= picked[:, j:j + 1] == torch.arange(groups, device=logits.device)
+        value = torch.where(keep[:, :, None], parts, low).view(n, -1)
+    leaves = _plain_largest(value, state["k"])
+    there = leaves >= 0
+    at = logits.gather(1, leaves.clamp(min=0)).float()
+    if state["score"] == "softmax":
+        top = logits.float().amax(1, keepdim=True)
+        score = torch.where(there, torch.exp(at - top), 0.0)
+        if not state["renorm"]:
+            score = score / torch.exp(logits.float() - top).sum(1, keepdim=True)
+    else:
+        score = torch.where(there, 1.0 / (1.0 + torch.exp(-at)), 0.0)
+    share = score / score.sum(1, keepdim=True)
+    return leaves, there, at, score, share, (share if state["renorm"] else score) * state["scale"]
+
+
+def _plain_pairs(leaves, n_leaves):
+    """The (row, slot) pairs of each leaf, as numbers row * k + slot."""
+    flat = leaves.reshape(-1).long()
+    order = torch.sort(flat, stable=True)[1]
+    ends = torch.cumsum(torch.bincount(flat, minlength=n_leaves), 0).tolist()
+    return [(leaf, order[a:b]) for leaf, (a, b) in enumerate(zip([0] + ends[:-1], ends)) if b > a]
+
+
+def _run_plain(state):
+    op, k = state["op"], state["k"]
+    if op.startswith("route"):
+        leaves, there, at, score, share, gates = _plain_route(state)
+        if op == "route":
+            return leaves.to(torch.int32), gates
+        dg = torch.where(there, state["dgates"], 0.0)
+        scale, logits = state["scale"], state["logits"].float()
+        dlogits = torch.zeros_like(logits)
+        if state["renorm"]:
+            inner = scale * (dg - (share * dg).sum(1, keepdim=True))
+            if state["score"] == "softmax":
+                each = share * inner
+            else:
+                each = share * (1.0 - score) * inner
+        elif state["score"] == "softmax":
+            e = torch.exp(logits - logits.amax(1, keepdim=True))
+            p = e / e.sum(1, keepdim=True)
+            dlogits = -scale * p * (score * dg).sum(1, keepdim=True)
+            each = scale * score * dg
+        else:
+            each = scale * score * (1.0 - score) * dg
+        dlogits.scatter_add_(1, leaves.clamp(min=0), torch.where(there, each, 0.0))
+        return leaves.to(torch.int32), gates, dlogits.to(state["logits"].dtype)
+    if op == "q8":
+        d_in = state["d_in"]
+        codes, scales = (state["codes"][:, :d_in], state["scales"]) if "codes" in state else _plain_codes(state["x"])
+        w, ws, bias = state["w_codes"], state["w_scales"], state["bias"]
+        if k == 0:
+            offs, rows = state["host_offsets"], state["rows"]
+            y = torch.zeros(codes.shape[0], w.shape[1], dtype=state["dtype"], device=codes.device)
+            for leaf in range(len(offs) - 1):
+                if offs[leaf + 1] > offs[leaf]:
+                    d = rows[offs[leaf]:offs[leaf + 1]]
+                    s = codes[d].float() @ w[leaf, :, :d_in].float().t()
+                    y[d] = (s * scales[d][:, None] * ws[leaf] + bias[leaf]).to(y.dtype)
+            return y
+        out = torch.zeros(codes.shape[0] * k, w.shape[1], device=codes.device)
+        for leaf, pairs in _plain_pairs(state["leaves"], state["leaves_n"]):
+            d = pairs // k
+            s = codes[d].float() @ w[leaf, :, :d_in].float().t()
+            out[pairs] = s * scales[d][:, None] * ws[leaf] + bias[leaf]
+        return (out.view(-1, k, w.shape[1]) * state["gates"][:, :, None]).sum(1).to(state["dtype"])
+    x, weight, bias, gates = state["x"], state["weight"], state["bias"], state["gates"]
+    n, (n_leaves, d_out, d_in) = x.shape[0], weight.shape
+    spans = _plain_pairs(state["leaves"], n_leaves)
+    z = torch.zeros(n * k, d_out, device=x.device)
+    for leaf, pairs in spans:
+        z[pairs] = x[pairs // k].float() @ weight[leaf].float().t() + bias[leaf].float()
+    z = z.view(n, k, d_out)
+    y = (z * gates[:, :, None]).sum(1).to(x.dtype)
+    if op == "mixture":
+        return y
+    dy = state["dy"]
+    dgates = (z * dy.float()[:, None, :]).sum(2)
+    u = torch.zeros(n * k, d_in, device=x.device)
+    dweight = torch.zeros_like(weight)
+    dbias = torch.zeros(n_leaves, d_out, dtype=weight.dtype, device=x.device)
+    flat = gates.reshape(-1)
+    for leaf, pairs in spans:
+        d = pairs // k
+        g = dy[d].float() * flat[pairs][:, None]
+        u[pairs] = g @ weight[leaf].float()
+        dweight[leaf] = (g.t() @ x[d].float()).to(dweight.dtype)
+        dbias[leaf] = g.sum(0).to(dbias.dtype)
+    return y, u.view(n, k, d_in).sum(1).to(x.dtype), dweight, dbias, dgates
+
+
+def _exact_route(case, state):
+    f64, low = torch.float64, -math.inf
+    n, k, groups = case["rows"], case["k"], case["groups"]
+    chosen = torch.empty(n, k, dtype=torch.int32, device="cuda")
+    gates = torch.zeros(n, k, dtype=f64, device="cuda")
+    dlogits = torch.zeros(n, case["leaves"], dtype=f64, device="cuda") if case["op"] == "route_train" else None
+    step = max(1, 30_000_000 // case["leaves"])
+    for a in range(0, n, step):
+        l = state["logits"][a:a + step].to(f64)
+        s = torch.softmax(l, 1) if case["score"] == "softmax" else torch.sigmoid(l)
+        c = l if state["bias"] is None and case["best"] == 1 else s if state["bias"] is None else s + state["bias"].to(f64)
+        c = c.masked_fill(torch.isneginf(l), low)
+        if groups > 1:
+            by_group = c.unflatten(1, (groups, -1))
+            best = torch.sort(by_group, dim=2, descending=True)[0][:, :, :case["best"]]
+            worth = best[:, :, 0] if case["best"] == 1 else torch.where(
+                torch.isneginf(best[:, :, 0]), best[:, :, 0], best.masked_fill(torch.isneginf(best), 0.0).sum(2))
+            kept = torch.sort(worth, dim=1, descending=True, stable=True)[1][:, :case["kept"]]
+            closed = torch.ones_like(worth, dtype=torch.bool).scatter_(1, kept, False)
+            c = by_group.masked_fill(closed[:, :, None], low).flatten(1)
+        top, e = torch.sort(c, dim=1, descending=True, stable=True)
+        top, e = top[:, :k], e[:, :k]
+        gone = torch.isneginf(top)
+        chosen[a:a + step] = e.masked_fill(gone, -1).to(torch.int32)
+        at = s.gather(1, e).masked_fill(gone, 0.0)
+        total = at.sum(1, keepdim=True)
+        gates[a:a + step] = case["scale"] * (at / total if case["renorm"] else at)
+        if dlogits is None:
+            continue
+        dg = state["dgates"][a:a + step].to(f64).masked_fill(gone, 0.0)
+        if case["renorm"]:
+            at = at / total
+            ds = at * (dg - (at * dg).sum(1, keepdim=True)) * (1.0 if case["score"] == "softmax" else 1.0 - s.gather(1, e))
+            dlogits[a:a + step].scatter_add_(1, e, case["scale"] * ds.masked_fill(gone, 0.0))
+        else:
+            ds = torch.zeros_like(s).scatter_add_(1, e, case["scale"] * dg)
+            within = (s * ds).sum(1, keepdim=True) if case["score"] == "softmax" else s * ds
+            dlogits[a:a + step] = s * (ds - within)
+    return (chosen, gates) if dlogits is None else (chosen, gates, dlogits)
+
+
+def exact(case, seed):
+    state = prepare(case, seed)
+    if case["op"].startswith("route"):
+        return _exact_route(case, state)
+    f64 = torch.float64
+    n, leaves, k, d_in, d_out = case["rows"], case["leaves"], case["k"], case["d_in"], case["d_out"]
+    bias = state["bias"].to(f64)
+    if case["op"] == "q8":
+        w = state["w_codes"][:, :, :d_in]
+        if case["stored"]:
+            codes, scales = state["codes"][:, :d_in], state["scales"]
+        else:
+            scales = torch.amax(torch.abs(state["x"].float()), 1) / 127.0
+            unit = torch.where(scales > 0, scales, torch.ones_like(scales)).to(f64)
+            codes = torch.round(state["x"].to(f64) / unit[:, None])
+
+        def answers(leaf, d):
+            s = torch.mm(codes.index_select(0, d).to(f64), w[leaf].to(f64).t().contiguous())
+            return s * scales[d].to(f64)[:, None] * state["w_scales"][leaf].to(f64)[None, :] + bias[leaf]
+    else:
+        x = state["x"]
+
+        def answers(leaf, d):
+            return torch.addmm(bias[leaf], x.index_select(0, d).to(f64), state["weight"][leaf].to(f64).t().contiguous())
+    y = torch.zeros(n, d_out, dtype=f64, device="cuda")
+    if k == 0:
+        offs = state["host_offsets"]
+        for leaf, (a, b) in enumerate(zip(offs[:-1], offs[1:])):
+            if b > a:
+                d = state["rows"][a:b].long()
+                y.index_copy_(0, d, answers(leaf, d))
+        return y
+    gates = state["gates"].to(f64)
+    train = case["op"] == "mixture_train"
+    if train:
+        dy = state["dy"].to(f64)
+        dx = torch.zeros(n, d_in, dtype=f64, device="cuda")
+        dw = torch.zeros(leaves, d_out, d_in, dtype=f64, device="cuda")
+        db = torch.zeros(leaves, d_out, dtype=f64, device="cuda")
+        dg = torch.zeros(n, k, dtype=f64, device="cuda")
+    for leaf in range(leaves):
+        d, j = torch.nonzero(state["leaves"] == leaf, as_tuple=True)
+        if d.numel() == 0:
+            continue
+        z, g = answers(leaf, d), gates[d, j][:, None]
+        y.index_add_(0, d, z * g)
+        if train:
+            of = dy.index_select(0, d)
+            dg[d, j] = (z * of).sum(1)
+            of = of * g
+            dx.index_add_(0, d, torch.mm(of, state["weight"][leaf].to(f64)))
+            dw[leaf] = torch.mm(of.t().contiguous(), state["x"].index_select(0, d).to(f64))
+            db[leaf] = of.sum(0)
+    return (y, dx, dw, db, dg) if train else y
+
+
+def work(case):
+    """Bytes and operations that a pass cannot do without: inputs once, outputs once, the products."""
+    e = 2 if case["dtype"] == "bf16" else 4
+    n, leaves, k = case["rows"], case["leaves"], case["k"]
+    if case["op"] == "route":
+        return {"bytes": e * n * leaves + 8 * n * k, "flops": 4.0 * n * leaves}
+    if case["op"] == "route_train":
+        return {"bytes": 2 * e * n * leaves + 12 * n * k, "flops": 8.0 * n * leaves}
+    d_in, d_out = case["d_in"], case["d_out"]
+    one, used = 2.0 * n * max(k, 1) * d_in * d_out, min(leaves, n * max(k, 1))
+    if case["op"] == "q8":
+        row = d_in + 4 if case["stored"] else e * d_in
+        lists = 4 * n if k == 0 else 8 * n * k
+        return {"bytes": n * (row + e * d_out) + used * d_out * (d_in + 8) + lists, "flops": one}
+    answer = e * (n * (d_in + d_out) + used * d_out * (d_in + 1)) + 8 * n * k
+    if case["op"] == "mixture":
+        return {"bytes": answer, "flops": one}
+    return {"bytes": answer + e * (n * (d_in + d_out) + leaves * d_out * (d_in + 1)) + 4 * n * k, "flops": 3 * one}
