@@ -212,9 +212,9 @@ def _run_own(state):
         codes, scales = (state["codes"], state["scales"]) if "codes" in state else B.gbdt_rows_quantize(state["x"])
         if k == 0:
             return B.gbdt_leaf_product_codes(codes, scales, state["w_codes"], state["w_scales"], state["offsets"],
-                                          row_idx=state["rows"], bias=state["bias"], dtype=state["dtype"])
+                                             row_idx=state["rows"], bias=state["bias"], dtype=state["dtype"])
         return B.gbdt_mixture_product_codes(codes, scales, state["w_codes"], state["w_scales"], state["leaves"],
-                                         state["gates"], bias=state["bias"], dtype=state["dtype"])
+                                            state["gates"], bias=state["bias"], dtype=state["dtype"])
     y = B.gbdt_mixture_product(state["x"], state["weight"], state["leaves"], state["gates"], bias=state["bias"])
     if op == "mixture":
         return y
