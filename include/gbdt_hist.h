@@ -31,7 +31,7 @@
  *    split candidates, partition flags) and a few process-wide counters in device
  *    memory.  Calls that use them (gbdt_hist_build[_batch], gbdt_best_split[_batch],
  *    gbdt_partition_rows[_batch], the tree growers, gbdt_leaf_product_grad,
- *    gbdt_softmax_loss, gbdt_softmax_grad) must be issued on ONE stream at a
+ *    gbdt_softmax_loss, gbdt_softmax_grad, gbdt_mixture_*) must be issued on ONE stream at a
  *    time: two such calls in flight on different streams, or from two threads, race.
  *    When the library owns the scratch it grows it on demand: a call that needs more
  *    allocates a larger buffer (hipMalloc) and keeps the old one until gbdt_reset; it never
@@ -554,6 +554,123 @@ int gbdt_softmax_stats(const void* h, int64_t ld_h, const void* classes, int64_t
                        const int32_t* labels, const float* lse, int64_t n_rows, int64_t n_classes,
                        int32_t dim, int32_t dtype, int64_t class_begin, int64_t class_end,
                        float* grad_out, float* hess_out, int64_t ld_out, void* stream);
+
+/*
+ * ---- Rows that several leaves answer --------------------------------------------------------
+ *
+ * A tree sends a row to one leaf.  A learned router scores all leaves and sends it to k of them, whose
+ * answers it weighs; a forest sends it to one leaf of each tree.  gbdt_route chooses, gbdt_mixture_product
+ * answers, and both have their gradients.
+ *
+ *   s = softmax(logits[d]) or sigmoid(logits[d])       c = s + choice_bias       g_j = scale * s_{e_j}
+ *
+ * The k leaves e_1 .. e_k with the largest choice values c are taken, largest first, of equal values
+ * the lowest leaf first; without a bias the order is that of the logits.  Choices are those of exact
+ * arithmetic to about 1e-15 of the scores.  A leaf whose logit is NaN or minus infinity, or whose c is, is never taken; where
+ * fewer than k are left the other slots have leaf -1 and weight 0.  (Softmax: infinite logits share
+ * all of the probability.)
+ * With n_groups > 1 the leaves fall into as many groups of neighbours of equal size, and only leaves of the groups_kept
+ * groups with the largest values are taken: a group's value is the sum of its group_best (1 or 2) largest c.
+ */
+typedef enum { GBDT_SOFTMAX = 0, GBDT_SIGMOID = 1 } gbdt_score;
+
+/*
+ *   logits       DEVICE [n_rows][n_leaves] of dtype, rows ld apart
+ *   choice_bias  DEVICE float [n_leaves] or NULL: has a part in the choice only (a trainer evens
+ *                out with it how often leaves are taken)
+ *   renormalise  not 0: the row's weights are divided by their sum, g_j = scale * s_{e_j} / sum_i s_{e_i}
+ *   leaves_out   DEVICE int32 [n_rows][k]
+ *   gates_out    DEVICE float [n_rows][k], the weights
+ * n_leaves <= 1024, k <= 32, n_groups <= 64, n_rows < 2^30 (GBDT_EUNSUPPORTED beyond); n_groups divides n_leaves and k leaves are
+ * in groups_kept groups; scale is finite.  Uses no scratch.
+ */
+int gbdt_route(const void* logits, int64_t ld, const float* choice_bias, int64_t n_rows, int32_t n_leaves,
+               int32_t dtype, int32_t score, int32_t n_groups, int32_t groups_kept, int32_t group_best,
+               int32_t k, int32_t renormalise, float scale, int32_t* leaves_out, float* gates_out,
+               void* stream);
+
+/*
+ * The logits' gradient by the weights' (the choice itself, and so choice_bias, has none):
+ *   leaves        as gbdt_route left them; slots with a leaf outside [0, n_leaves) are passed over
+ *   dgates        DEVICE float [n_rows][k]
+ *   dlogits_out   DEVICE [n_rows][n_leaves] of dtype, rows ld_out apart: every value is written
+ */
+int gbdt_route_grad(const void* logits, int64_t ld, const int32_t* leaves, const float* dgates,
+                    int64_t n_rows, int32_t n_leaves, int32_t dtype, int32_t score, int32_t k,
+                    int32_t renormalise, float scale, void* dlogits_out, int64_t ld_out, void* stream);
+
+/*
+ *   y[d] = sum_j gates[d][j] (W_l x[d] + b_l),  l = leaves[d][j]
+ *   x        DEVICE [n_rows][d_in]
+ *   weight   DEVICE [n_leaves][d_out][d_in], dense;  bias  DEVICE [n_leaves][d_out] or NULL
+ *   leaves   DEVICE int32 [n_rows][k]; a slot with a leaf outside [0, n_leaves) is passed over, whatever
+ *            its weight; a leaf may be named twice
+ *   gates    DEVICE float [n_rows][k]
+ *   y_out    DEVICE [n_rows][d_out]; zeros for a row without a leaf
+ * Element types, distances and limits as for gbdt_leaf_product; k <= 64, n_leaves <= 16384, n_rows * k < 2^30.  The slots' answers
+ * are kept in f32 in the library's scratch, of so many rows at a time as take 256 MiB or of 1,024, and
+ * added in their order: the same call gives the same bits, rounded once.
+ * gbdt_mixture_workspace_bytes: the size of a registered workspace that suffices for the three
+ * gbdt_mixture_* calls (0 on invalid arguments).
+ */
+int gbdt_mixture_product(const void* x, int64_t ld_x, const void* weight, const void* bias,
+                         const int32_t* leaves, const float* gates, int64_t n_rows, int32_t k,
+                         int32_t n_leaves, int32_t d_in, int32_t d_out, int32_t dtype, void* y_out,
+                         int64_t ld_y, void* stream);
+size_t gbdt_mixture_workspace_bytes(int64_t n_rows, int32_t k, int32_t n_leaves, int32_t d_in, int32_t d_out,
+                                    int32_t dtype);
+
+/*
+ * Its gradients, of which any may be NULL:
+ *   dx_out[d]        = sum_j gates[d][j] W_l^T dy[d]                    DEVICE [n_rows][d_in]
+ *   dweight_out[l]   = sum over the slots of leaf l of gates dy x^T     DEVICE [n_leaves][d_out][d_in]
+ *   dbias_out[l]     = sum over the slots of leaf l of gates dy         DEVICE [n_leaves][d_out]
+ *   dgates_out[d][j] = <dy[d], W_l x[d] + b_l>                          DEVICE float [n_rows][k], 0 for a slot passed over
+ * weight is read for dx and dgates, x for dweight and dgates, bias for dgates.  In dweight and dbias
+ * gates * dy is rounded to the element type before it is summed.
+ */
+int gbdt_mixture_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
+                              const void* weight, const void* bias, const int32_t* leaves,
+                              const float* gates, int64_t n_rows, int32_t k, int32_t n_leaves,
+                              int32_t d_in, int32_t d_out, int32_t dtype, void* dx_out, int64_t ld_dx,
+                              void* dweight_out, void* dbias_out, float* dgates_out, void* stream);
+
+/*
+ * ---- Leaf products in 8-bit integers ----------------------------------------------------------
+ *
+ * Rows of x, and rows of the leaves' matrices, as 8-bit codes with a scale each:
+ *
+ *   scale = max |x[d]| / 127 in f32       code = x / scale to the nearest whole number, ties to even
+ *
+ * A row with an infinity or a NaN has scale NaN (and codes 0), so what it is multiplied into is NaN; a
+ * row whose scale would be below 2^-126 has scale and codes 0.
+ *   x           DEVICE [n_rows][n_cols] of dtype, rows ld_x apart
+ *   codes_out   DEVICE int8 [n_rows][ld_codes], 16-byte aligned, ld_codes a multiple of 16 and at least n_cols; zeros from n_cols up to the
+ *               next multiple of 16, nothing written behind
+ *   scales_out  DEVICE float [n_rows]
+ */
+int gbdt_rows_quantize(const void* x, int64_t ld_x, int64_t n_rows, int32_t n_cols, int32_t dtype,
+                       int8_t* codes_out, int64_t ld_codes, float* scales_out, void* stream);
+
+/*
+ * gbdt_leaf_product and gbdt_mixture_product of codes: y[d] = (sum of the codes' products) scales[d] weight_scales[l][o] + bias[l][o].
+ * The sums are exact.  d_in <= 131072 (GBDT_EUNSUPPORTED beyond).
+ *   codes          DEVICE int8 [n_rows][ld_codes], scales  DEVICE float [n_rows], as gbdt_rows_quantize
+ *                  leaves them (zeros up to the next multiple of 16)
+ *   weight         DEVICE int8 [n_leaves][d_out][d_in rounded up to a multiple of 16], 16-byte aligned: the rows of the
+ *                  matrices, quantized;  weight_scales  DEVICE float [n_leaves][d_out]
+ *   bias           DEVICE float [n_leaves][d_out] or NULL
+ *   dtype          of y_out
+ *   other arguments as for gbdt_leaf_product (uses no scratch) and gbdt_mixture_product
+ */
+int gbdt_leaf_product_codes(const int8_t* codes, int64_t ld_codes, const float* scales, const int8_t* weight,
+                         const float* weight_scales, const float* bias, const int32_t* row_idx,
+                         const int64_t* leaf_offsets, int64_t n_positions, int32_t n_leaves, int64_t n_rows,
+                         int32_t d_in, int32_t d_out, int32_t dtype, void* y_out, int64_t ld_y, void* stream);
+int gbdt_mixture_product_codes(const int8_t* codes, int64_t ld_codes, const float* scales, const int8_t* weight,
+                            const float* weight_scales, const float* bias, const int32_t* leaves,
+                            const float* gates, int64_t n_rows, int32_t k, int32_t n_leaves, int32_t d_in,
+                            int32_t d_out, int32_t dtype, void* y_out, int64_t ld_y, void* stream);
 
 /*
  * Scratch workspace.  By default the library allocates device scratch itself

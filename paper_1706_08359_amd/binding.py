@@ -35,6 +35,8 @@ EXPORTS = [
     "gbdt_bins_fused_bytes", "gbdt_bins_fuse", "gbdt_bins_unfuse", "gbdt_debug_fusion_plan",
     "gbdt_leaf_product", "gbdt_leaf_product_grad", "gbdt_leaf_product_grad_workspace_bytes",
     "gbdt_softmax_loss", "gbdt_softmax_grad", "gbdt_softmax_stats", "gbdt_softmax_workspace_bytes",
+    "gbdt_route", "gbdt_route_grad", "gbdt_mixture_product", "gbdt_mixture_product_grad", "gbdt_mixture_workspace_bytes",
+    "gbdt_rows_quantize", "gbdt_leaf_product_codes", "gbdt_mixture_product_codes",
 ]
 
 # numpy views of the two C structs
@@ -165,6 +167,23 @@ def load():
                                        c.c_void_p, c.c_void_p, c.c_int64, c.c_void_p]
     lib.gbdt_softmax_workspace_bytes.restype = c.c_size_t
     lib.gbdt_softmax_workspace_bytes.argtypes = [c.c_int64, c.c_int64, c.c_int32, c.c_int32]
+    p, i32, i64, f32 = c.c_void_p, c.c_int32, c.c_int64, c.c_float
+    lib.gbdt_route.restype = c.c_int
+    lib.gbdt_route.argtypes = [p, i64, p, i64, i32, i32, i32, i32, i32, i32, i32, i32, f32, p, p, p]
+    lib.gbdt_route_grad.restype = c.c_int
+    lib.gbdt_route_grad.argtypes = [p, i64, p, p, i64, i32, i32, i32, i32, i32, f32, p, i64, p]
+    lib.gbdt_mixture_product.restype = c.c_int
+    lib.gbdt_mixture_product.argtypes = [p, i64, p, p, p, p, i64, i32, i32, i32, i32, i32, p, i64, p]
+    lib.gbdt_mixture_product_grad.restype = c.c_int
+    lib.gbdt_mixture_product_grad.argtypes = [p, i64, p, i64, p, p, p, p, i64, i32, i32, i32, i32, i32, p, i64, p, p, p, p]
+    lib.gbdt_mixture_workspace_bytes.restype = c.c_size_t
+    lib.gbdt_mixture_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
+    lib.gbdt_rows_quantize.restype = c.c_int
+    lib.gbdt_rows_quantize.argtypes = [p, i64, i64, i32, i32, p, i64, p, p]
+    lib.gbdt_leaf_product_codes.restype = c.c_int
+    lib.gbdt_leaf_product_codes.argtypes = [p, i64, p, p, p, p, p, p, i64, i32, i64, i32, i32, i32, p, i64, p]
+    lib.gbdt_mixture_product_codes.restype = c.c_int
+    lib.gbdt_mixture_product_codes.argtypes = [p, i64, p, p, p, p, p, p, i64, i32, i32, i32, i32, i32, p, i64, p]
     _lib = lib
     return lib
 
@@ -882,6 +901,211 @@ def gbdt_softmax_stats(h, classes, labels, lse, class_begin, class_end, grad_out
 
 def gbdt_softmax_workspace_bytes(n_rows: int, n_classes: int, dim: int, dtype=torch.float32) -> int:
     return int(load().gbdt_softmax_workspace_bytes(n_rows, n_classes, dim, DTYPES[dtype]))
+
+
+SCORES = {"softmax": 0, "sigmoid": 1}   # gbdt_score
+
+
+def _here(*tensors):
+    """All on the current device, whose stream and library the call takes."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise GbdtError(f"a tensor on {t.device}, the current device is cuda:{device}")
+
+
+def _score(score):
+    if score not in SCORES:
+        raise GbdtError("score: 'softmax' or 'sigmoid'")
+    return SCORES[score]
+
+
+def gbdt_route(logits, k, choice_bias=None, score="softmax", n_groups=1, groups_kept=1, group_best=1, renormalise=True, scale=1.0,
+               leaves_out=None, gates_out=None, stream=None):
+    """The k leaves that answer each row, and their weights.  logits: [n_rows, n_leaves] float32 or bfloat16; choice_bias: float32
+    [n_leaves].  Returns (leaves int32 [n_rows, k], gates float32 [n_rows, k]); a slot that no leaf is left for has leaf -1, weight
+    0."""
+    code = _element_type(logits, "logits")
+    if logits.dim() != 2:
+        raise TypeError("logits: expected [n_rows, n_leaves]")
+    n_rows, n_leaves = logits.shape
+    l_p, ld = _mat(logits, logits.dtype, n_rows, n_leaves, "logits")
+    b_p = None if choice_bias is None else _dense(choice_bias, torch.float32, (n_leaves,), "choice_bias")
+    if not 0 < k <= n_leaves:
+        raise GbdtError("k: between 1 and n_leaves")
+    if leaves_out is None:
+        leaves_out = _made(torch.empty, (n_rows, k), torch.int32, logits.device, stream)
+    if gates_out is None:
+        gates_out = _made(torch.empty, (n_rows, k), torch.float32, logits.device, stream)
+    _here(logits, choice_bias, leaves_out, gates_out)
+    _check(load().gbdt_route(l_p, ld, b_p, n_rows, n_leaves, code, _score(score), n_groups, groups_kept, group_best, k,
+                             1 if renormalise else 0, float(scale), _dense(leaves_out, torch.int32, (n_rows, k), "leaves_out"),
+                             _dense(gates_out, torch.float32, (n_rows, k), "gates_out"), _stream(stream)), "gbdt_route")
+    return leaves_out, gates_out
+
+
+def gbdt_route_grad(logits, leaves, dgates, score="softmax", renormalise=True, scale=1.0, dlogits_out=None, stream=None):
+    """Gradient of the logits by that of gbdt_route's weights, dgates float32 [n_rows, k]; leaves as gbdt_route returned them.  Returns
+    dlogits [n_rows, n_leaves] of the logits' type."""
+    code = _element_type(logits, "logits")
+    if logits.dim() != 2 or not isinstance(leaves, torch.Tensor) or leaves.dim() != 2:
+        raise TypeError("expected logits [n_rows, n_leaves] and leaves [n_rows, k]")
+    (n_rows, n_leaves), k = logits.shape, leaves.shape[1]
+    l_p, ld = _mat(logits, logits.dtype, n_rows, n_leaves, "logits")
+    e_p = _dense(leaves, torch.int32, (n_rows, k), "leaves")
+    g_p = _dense(dgates, torch.float32, (n_rows, k), "dgates")
+    if dlogits_out is None:
+        dlogits_out = _made(torch.empty, (n_rows, n_leaves), logits.dtype, logits.device, stream)
+    o_p, ld_out = _mat(dlogits_out, logits.dtype, n_rows, n_leaves, "dlogits_out")
+    _here(logits, leaves, dgates, dlogits_out)
+    _check(load().gbdt_route_grad(l_p, ld, e_p, g_p, n_rows, n_leaves, code, _score(score), k, 1 if renormalise else 0, float(scale),
+                                  o_p, ld_out, _stream(stream)), "gbdt_route_grad")
+    return dlogits_out
+
+
+def _slots(leaves, gates, n_rows):
+    """(k, addresses) of the leaves and weights of every row."""
+    if not isinstance(leaves, torch.Tensor) or leaves.dim() != 2 or leaves.shape[0] != n_rows:
+        raise TypeError("leaves: expected an int32 CUDA tensor [n_rows, k]")
+    k = leaves.shape[1]
+    return k, _dense(leaves, torch.int32, (n_rows, k), "leaves"), _dense(gates, torch.float32, (n_rows, k), "gates")
+
+
+def gbdt_mixture_product(x, weight, leaves, gates, bias=None, y_out=None, stream=None):
+    """y[d] = sum_j gates[d, j] (weight[l] x[d] + bias[l]), l = leaves[d, j].  x: [n_rows, d_in]; weight: [n_leaves, d_out, d_in];
+    bias: [n_leaves, d_out]; all float32 or all bfloat16.  leaves: int32 [n_rows, k], entries outside the leaves are passed over;
+    gates: float32 [n_rows, k].  Returns y_out [n_rows, d_out]."""
+    code = _element_type(x, "x")
+    if weight.dim() != 3 or x.dim() != 2:
+        raise TypeError("expected x [n_rows, d_in] and weight [n_leaves, d_out, d_in]")
+    n_rows, (n_leaves, d_out, d_in) = x.shape[0], weight.shape
+    x_p, ld_x = _mat(x, x.dtype, n_rows, d_in, "x")
+    w_p = _dev(weight, x.dtype, "weight")
+    b_p = None if bias is None else _dense(bias, x.dtype, (n_leaves, d_out), "bias")
+    k, e_p, g_p = _slots(leaves, gates, n_rows)
+    if y_out is None:
+        y_out = _made(torch.empty, (n_rows, d_out), x.dtype, x.device, stream)
+    y_p, ld_y = _mat(y_out, x.dtype, n_rows, d_out, "y_out")
+    _here(x, weight, leaves, gates, bias, y_out)
+    _check(load().gbdt_mixture_product(x_p, ld_x, w_p, b_p, e_p, g_p, n_rows, k, n_leaves, d_in, d_out, code, y_p, ld_y,
+                                       _stream(stream)), "gbdt_mixture_product")
+    return y_out
+
+
+def gbdt_mixture_product_grad(dy, x, weight, leaves, gates, bias=None, dx_out=None, dweight_out=None, dbias_out=None, dgates_out=None,
+                              want=("x", "weight", "bias", "gates"), stream=None):
+    """Gradients of gbdt_mixture_product by what `want` names.  dy: [n_rows, d_out]; bias as the product took it.  Returns
+    (dx [n_rows, d_in], dweight [n_leaves, d_out, d_in], dbias [n_leaves, d_out], dgates float32 [n_rows, k]), None for what is
+    not wanted."""
+    code = _element_type(x, "x")
+    if weight.dim() != 3 or x.dim() != 2:
+        raise TypeError("expected x [n_rows, d_in] and weight [n_leaves, d_out, d_in]")
+    if not set(want) <= {"x", "weight", "bias", "gates"}:
+        raise GbdtError("want: any of 'x', 'weight', 'bias', 'gates'")
+    n_rows, (n_leaves, d_out, d_in) = x.shape[0], weight.shape
+    x_p, ld_x = _mat(x, x.dtype, n_rows, d_in, "x")
+    dy_p, ld_dy = _mat(dy, x.dtype, n_rows, d_out, "dy")
+    w_p = _dev(weight, x.dtype, "weight")
+    b_p = None if bias is None else _dense(bias, x.dtype, (n_leaves, d_out), "bias")
+    k, e_p, g_p = _slots(leaves, gates, n_rows)
+    dx_p = dw_p = db_p = dg_p = None
+    ld_dx = d_in
+    if "x" in want:
+        if dx_out is None:
+            dx_out = _made(torch.empty, (n_rows, d_in), x.dtype, x.device, stream)
+        dx_p, ld_dx = _mat(dx_out, x.dtype, n_rows, d_in, "dx_out")
+    if "weight" in want:
+        if dweight_out is None:
+            dweight_out = _made(torch.empty, (n_leaves, d_out, d_in), x.dtype, x.device, stream)
+        dw_p = _dense(dweight_out, x.dtype, (n_leaves, d_out, d_in), "dweight_out")
+    if "bias" in want:
+        if dbias_out is None:
+            dbias_out = _made(torch.empty, (n_leaves, d_out), x.dtype, x.device, stream)
+        db_p = _dense(dbias_out, x.dtype, (n_leaves, d_out), "dbias_out")
+    if "gates" in want:
+        if dgates_out is None:
+            dgates_out = _made(torch.empty, (n_rows, k), torch.float32, x.device, stream)
+        dg_p = _dense(dgates_out, torch.float32, (n_rows, k), "dgates_out")
+    _here(dy, x, weight, leaves, gates, bias, dx_out, dweight_out, dbias_out, dgates_out)
+    _check(load().gbdt_mixture_product_grad(dy_p, ld_dy, x_p, ld_x, w_p, b_p, e_p, g_p, n_rows, k, n_leaves, d_in, d_out, code, dx_p,
+                                            ld_dx, dw_p, db_p, dg_p, _stream(stream)), "gbdt_mixture_product_grad")
+    return (dx_out if "x" in want else None, dweight_out if "weight" in want else None, dbias_out if "bias" in want else None,
+            dgates_out if "gates" in want else None)
+
+
+def gbdt_mixture_workspace_bytes(n_rows: int, k: int, n_leaves: int, d_in: int, d_out: int, dtype=torch.float32) -> int:
+    return int(load().gbdt_mixture_workspace_bytes(n_rows, k, n_leaves, d_in, d_out, DTYPES[dtype]))
+
+
+def code_columns(n_cols: int) -> int:
+    """The length of a row of codes: n_cols rounded up to a multiple of 16."""
+    return (n_cols + 15) // 16 * 16
+
+
+def gbdt_rows_quantize(x, codes_out=None, scales_out=None, stream=None):
+    """Rows as 8-bit codes with a scale each, x ~ codes * scale.  x: [n_rows, n_cols] float32 or bfloat16.  Returns (codes int8
+    [n_rows, code_columns(n_cols)], zeros behind n_cols; scales float32 [n_rows])."""
+    code = _element_type(x, "x")
+    if x.dim() != 2:
+        raise TypeError("x: expected [n_rows, n_cols]")
+    n_rows, n_cols = x.shape
+    x_p, ld_x = _mat(x, x.dtype, n_rows, n_cols, "x")
+    if codes_out is None:
+        codes_out = _made(torch.empty, (n_rows, code_columns(n_cols)), torch.int8, x.device, stream)
+    if scales_out is None:
+        scales_out = _made(torch.empty, (n_rows,), torch.float32, x.device, stream)
+    c_p, ld_c = _mat(codes_out, torch.int8, n_rows, code_columns(n_cols), "codes_out")
+    _here(x, codes_out, scales_out)
+    _check(load().gbdt_rows_quantize(x_p, ld_x, n_rows, n_cols, code, c_p, ld_c, _dense(scales_out, torch.float32, (n_rows,), "scales_out"),
+                                     _stream(stream)), "gbdt_rows_quantize")
+    return codes_out, scales_out
+
+
+def _codes(codes, scales, weight, weight_scales, bias, dtype):
+    """What the products of codes have in common."""
+    if dtype not in DTYPES:
+        raise TypeError("dtype: torch.float32 or torch.bfloat16")
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 3 or not isinstance(codes, torch.Tensor) or codes.dim() != 2:
+        raise TypeError("expected codes [n_rows, columns] and weight [n_leaves, d_out, columns]")
+    n_rows, (n_leaves, d_out, columns) = codes.shape[0], weight.shape
+    if columns % 16 != 0:
+        raise TypeError("weight: rows of codes are a multiple of 16 long")
+    c_p, ld_c = _mat(codes, torch.int8, n_rows, columns, "codes")
+    s_p = _dense(scales, torch.float32, (n_rows,), "scales")
+    w_p = _dev(weight, torch.int8, "weight")
+    ws_p = _dense(weight_scales, torch.float32, (n_leaves, d_out), "weight_scales")
+    b_p = None if bias is None else _dense(bias, torch.float32, (n_leaves, d_out), "bias")
+    return n_rows, n_leaves, d_out, columns, (c_p, ld_c, s_p, w_p, ws_p, b_p)
+
+
+def gbdt_leaf_product_codes(codes, scales, weight, weight_scales, leaf_offsets, row_idx=None, bias=None, dtype=torch.float32, y_out=None,
+                         stream=None):
+    """gbdt_leaf_product of 8-bit codes, as gbdt_rows_quantize makes them of the rows and of the rows of the matrices: codes int8
+    [n_rows, columns], scales float32 [n_rows], weight int8 [n_leaves, d_out, columns], weight_scales float32 [n_leaves, d_out], bias
+    float32 [n_leaves, d_out].  Returns y_out [n_rows, d_out] of dtype; rows of no leaf keep what y_out holds (zeros if it is
+    made here)."""
+    n_rows, n_leaves, d_out, columns, operands = _codes(codes, scales, weight, weight_scales, bias, dtype)
+    idx_p, off_p, n_positions = _leaf_lists(leaf_offsets, row_idx, n_leaves, n_rows)
+    if y_out is None:
+        y_out = _made(torch.zeros, (n_rows, d_out), dtype, codes.device, stream)
+    y_p, ld_y = _mat(y_out, dtype, n_rows, d_out, "y_out")
+    _here(codes, scales, weight, weight_scales, leaf_offsets, row_idx, bias, y_out)
+    _check(load().gbdt_leaf_product_codes(*operands, idx_p, off_p, n_positions, n_leaves, n_rows, columns, d_out, DTYPES[dtype], y_p, ld_y,
+                                       _stream(stream)), "gbdt_leaf_product_codes")
+    return y_out
+
+
+def gbdt_mixture_product_codes(codes, scales, weight, weight_scales, leaves, gates, bias=None, dtype=torch.float32, y_out=None, stream=None):
+    """gbdt_mixture_product of 8-bit codes (see gbdt_leaf_product_codes).  Returns y_out [n_rows, d_out] of dtype."""
+    n_rows, n_leaves, d_out, columns, operands = _codes(codes, scales, weight, weight_scales, bias, dtype)
+    k, e_p, g_p = _slots(leaves, gates, n_rows)
+    if y_out is None:
+        y_out = _made(torch.empty, (n_rows, d_out), dtype, codes.device, stream)
+    y_p, ld_y = _mat(y_out, dtype, n_rows, d_out, "y_out")
+    _here(codes, scales, weight, weight_scales, leaves, gates, bias, y_out)
+    _check(load().gbdt_mixture_product_codes(*operands, e_p, g_p, n_rows, k, n_leaves, columns, d_out, DTYPES[dtype], y_p, ld_y,
+                                          _stream(stream)), "gbdt_mixture_product_codes")
+    return y_out
 
 
 def gbdt_set_deterministic(enable: bool) -> None:

@@ -11,7 +11,7 @@ import sys
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(_HERE, "csrc", "gbdt_hist.hip")
-SRCS = [SRC, os.path.join(_HERE, "csrc", "linear_leaves.hip")]
+SRCS = [SRC, os.path.join(_HERE, "csrc", "linear_leaves.hip"), os.path.join(_HERE, "csrc", "routed_leaves.hip")]
 LIB = os.path.join(_HERE, "libgbdt_hist.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -8,6 +8,8 @@
 // lengths are, no sum over the leaves before a leaf is needed, and a tile finds its leaf by a search over T.
 #pragma once
 
+#include <type_traits>
+
 #include "tile_product.h"
 
 namespace gbdt_leaf {
@@ -31,6 +33,7 @@ struct LeafArgs {
   int32_t n_positions, n_leaves, n_rows, d_in, d_out;
   int32_t cut;        // gradient of the weights: positions between cuts
   uint32_t col_tiles, row_tiles, cols_per;  // cols_per: column tiles that a workgroup goes through
+  int32_t row_first;  // gradient of the weights from listed rows: the output that dy's first column belongs to
   uint32_t first;     // of this launch's workgroups (gradient of the weights: of its pieces), among all of the call
 };
 
@@ -117,13 +120,30 @@ __device__ __forceinline__ PlainRows<T> plain_rows(const T* base, int64_t ld, in
   return {base, base + (int64_t)(n - 1) * ld + cols, ld, n};
 }
 
+// Where the results of a product over rows go: value + the leaf's bias, to the row of y that the position names.
+template <typename T>
+struct ToRows {
+  typedef T Out;
+  static constexpr bool kScaled = false;
+  const T* bias;  // [n_leaves][cols] or null
+  T* out;
+  int64_t ld;
+  // The place of position p's results, -1 for none.
+  __device__ __forceinline__ int place(const LeafArgs<T>& g, int p) const {
+    const int d = g.row_idx ? g.row_idx[p] : p;
+    return (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
+  }
+  __device__ __forceinline__ float add(int64_t column) const { return bias ? (float)bias[column] : 0.0f; }
+};
+
 // The rows of one tile of positions times a matrix of the leaf, g.cols_per column tiles one after another; the next one's
 // first steps are on their way while one's values are stored.  B: the matrix' orientation, k its length along k.
+// To::kScaled: values are multiplied by a factor of their position and one of the leaf's column.
 // GROUPS > 1: as many times the tile's threads take a part of k each, all of as many steps, and the first adds up; one column
 // tile a workgroup then, since the other groups leave after it.
-template <class S, class B, int GROUPS, typename T>
-__device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& g, const T* in, int64_t ld_in, int k, const T* bias_all,
-                                                  T* out, int64_t ld_out, int cols) {
+template <class S, class B, int GROUPS, typename T, class G, class To>
+__device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T* in, int64_t ld_in, int k, const To& to, int cols) {
+  typedef typename S::Acc Acc;
   const uint32_t t = g.first + xcd_tile(blockIdx.x, gridDim.x);
   const uint32_t turns = (g.col_tiles + g.cols_per - 1) / g.cols_per;
   const int tile = (int)(t / turns), col_first = (int)(t % turns * g.cols_per) * S::BN;
@@ -136,12 +156,14 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& 
   const ListRows<T> rows_a = list_rows(in, ld_in, k, g, end);
   const PlainRows<T> rows_b = plain_rows(g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out, g.d_in);
   const int w = thread_of<S::NT>() >> 6;
-  int ids[S::TM];  // rows of this lane's blocks, -1 for none
+  int ids[S::TM];  // places of this lane's blocks, -1 for none
+  float factor[To::kScaled ? S::TM : 1];
   const int m0 = p0 + w / S::WN * (S::TM * 16) + (threadIdx.x & 15);
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
-    const int p = m0 + 16 * i, d = p < end ? (g.row_idx ? g.row_idx[p] : p) : -1;
-    ids[i] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
+    const int p = m0 + 16 * i;
+    ids[i] = p < end ? to.place(g, p) : -1;
+    if constexpr (To::kScaled) factor[i] = ids[i] >= 0 ? to.row_scale(g, p) : 0.0f;
   }
   const int group = GROUPS > 1 ? (int)threadIdx.x / S::NT : 0;
   lds += group * S::kLdsBytes;
@@ -156,13 +178,13 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& 
   };
   begin_columns(col_first);
   for (int col = col_first; col < col_last; col += S::BN) {
-    f32x4 acc[S::TM][S::TN];
+    Acc acc[S::TM][S::TN];
     zeros<S>(acc);
     tile_run<S, true>(lds, a, b, rows_a, rows_b, k0, k0 + part, acc, Nothing{});
     if constexpr (GROUPS > 1) {
       constexpr int values = S::TM * S::TN;
       static_assert(values * S::NT * 16 <= S::kLdsBytes, "a group's sums take its stages' place");
-      f32x4* sums = (f32x4*)lds;
+      Acc* sums = (Acc*)lds;
       __syncthreads();  // (the last reads of the stages)
 #pragma unroll
       for (int v = 0; v < values; ++v) sums[v * S::NT + thread_of<S::NT>()] = acc[v / S::TN][v % S::TN];
@@ -172,24 +194,35 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& 
       for (int other = 1; other < GROUPS; ++other)
 #pragma unroll
         for (int v = 0; v < values; ++v)
-          acc[v / S::TN][v % S::TN] += ((const f32x4*)(lds + other * S::kLdsBytes))[v * S::NT + thread_of<S::NT>()];
+          acc[v / S::TN][v % S::TN] += ((const Acc*)(lds + other * S::kLdsBytes))[v * S::NT + thread_of<S::NT>()];
     } else if (col + S::BN < col_last) {
       begin_columns(col + S::BN);
     }
     const int l = threadIdx.x & 63, wave_col = col + w % S::WN * (S::TN * 16);
-    f32x4 add[S::TN];
+    f32x4 add[S::TN], scale[To::kScaled ? S::TN : 1];
 #pragma unroll
     for (int j = 0; j < S::TN; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int n = wave_col + 16 * j + 4 * (l >> 4) + r;
-        add[j][r] = bias_all && n < cols ? (float)bias_all[(int64_t)leaf * cols + n] : 0.0f;
+        add[j][r] = n < cols ? to.add((int64_t)leaf * cols + n) : 0.0f;
+        if constexpr (To::kScaled) scale[j][r] = n < cols ? to.column_scale((int64_t)leaf * cols + n) : 0.0f;
       }
-    store_tile<S, T, S::TM, S::TN>(
-        lds + S::kLastStage, [&](int i, int j) { return acc[i][j] + add[j]; },
+    store_tile<S, typename To::Out, S::TM, S::TN>(
+        lds + S::kLastStage,
+        [&](int i, int j) {
+          if constexpr (To::kScaled) {
+            f32x4 v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = __builtin_fmaf((float)acc[i][j][r] * factor[i], scale[j][r], add[j][r]);
+            return v;
+          } else {
+            return acc[i][j] + add[j];
+          }
+        },
         [&](int i, int r) {
           const int d = __shfl(ids[i], r);
-          return d >= 0 ? out + (int64_t)d * ld_out : (T*)nullptr;
+          return d >= 0 ? to.out + (int64_t)d * to.ld : (typename To::Out*)nullptr;
         },
         wave_col, cols);
   }
@@ -202,14 +235,14 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const LeafArgs<T>& 
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_product_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, g.bias, g.y, g.ld_y, g.d_out);
+  leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, ToRows<typename S::T>{g.bias, g.y, g.ld_y}, g.d_out);
 }
 
 // The same where there are too few tiles for the compute units: a tile's k is split among GROUPS times the threads.
 template <class S, int GROUPS>
 __global__ void __launch_bounds__(S::NT* GROUPS) leaf_product_split_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes * GROUPS];
-  leaf_rows_product<S, typename S::RowsB, GROUPS>(lds, g, g.x, g.ld_x, g.d_in, g.bias, g.y, g.ld_y, g.d_out);
+  leaf_rows_product<S, typename S::RowsB, GROUPS>(lds, g, g.x, g.ld_x, g.d_in, ToRows<typename S::T>{g.bias, g.y, g.ld_y}, g.d_out);
 }
 
 // dx: rows of dy (k = output along memory) times w, whose rows are k.  Bound by its stores, d_in values a row, which a tile's
@@ -218,7 +251,7 @@ __global__ void __launch_bounds__(S::NT* GROUPS) leaf_product_split_kernel(const
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_input_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::ColumnsB, 1>(lds, g, g.dy, g.ld_dy, g.d_out, (const typename S::T*)nullptr, g.dx, g.ld_dx, g.d_in);
+  leaf_rows_product<S, typename S::ColumnsB, 1>(lds, g, g.dy, g.ld_dy, g.d_out, ToRows<typename S::T>{nullptr, g.dx, g.ld_dx}, g.d_in);
 }
 
 // A few positions (a row or a few answered at once): a wavefront takes OUTPUTS outputs of one position, each lane a chunk of k
@@ -327,7 +360,8 @@ __device__ __forceinline__ Piece find_piece(const LeafArgs<T>& g, int piece) {
   return r;
 }
 
-template <class S, bool LONG>
+// LISTED: dy holds a row for every position, in the list's order, of ld_dy values from output row_first on, zeros behind the outputs.
+template <class S, bool LONG, bool LISTED>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafArgs<typename S::T> g) {
   typedef typename S::T T;
   __shared__ __align__(16) char lds[S::kLdsBytes];
@@ -343,7 +377,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   const int cols_per = p1 - p0 <= kShortPiece ? (int)g.cols_per : 1;
   const int turns = ((int)g.col_tiles + cols_per - 1) / cols_per;
   if (r >= turns * (int)g.row_tiles) return;
-  const int row0 = r / turns * S::BM, col_first = r % turns * cols_per * S::BN;
+  const int row0 = (LISTED ? g.row_first : 0) + r / turns * S::BM, col_first = r % turns * cols_per * S::BN;
   const bool whole = at_piece.whole;
   float* part = g.partial + at_piece.slot * ((int64_t)(g.d_in + 1) * g.d_out);
   const int all_cols = g.dw ? g.d_in : 1;  // (the outputs' sums alone come with the first tile)
@@ -352,13 +386,21 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   const int m0 = row0 + (w / S::WN) * (S::TM * 16);
 
   const auto listed = (const __attribute__((address_space(3))) int*)ids;
-  CopiedRows<T> rows_a = {g.dy, g.dy + (int64_t)(g.n_rows - 1) * g.ld_dy + g.d_out, g.ld_dy, listed, p0};
+  typedef typename std::conditional<LISTED, PlainRows<T>, CopiedRows<T>>::type RowsOfDy;
+  RowsOfDy rows_a;
+  if constexpr (LISTED) {
+    rows_a = plain_rows(g.dy - g.row_first, g.ld_dy, g.n_positions, g.row_first + (int)g.ld_dy);
+  } else {
+    rows_a = {g.dy, g.dy + (int64_t)(g.n_rows - 1) * g.ld_dy + g.d_out, g.ld_dy, listed, p0};
+  }
+  const int dy_cols = LISTED ? g.row_first + (int)g.ld_dy : g.d_out;
   CopiedRows<T> rows_b = {g.x, g.x + (int64_t)(g.n_rows - 1) * g.ld_x + g.d_in, g.ld_x, listed, p0};
   typename S::ColumnsA a;
   typename S::ColumnsB b;
   int c0 = p0, c1 = p0;  // the positions copied
   auto copy_ids = [&](int from) {
-    c0 = rows_a.first = rows_b.first = from;
+    c0 = rows_b.first = from;
+    if constexpr (!LISTED) rows_a.first = from;
     c1 = !LONG || p1 - from < kCopiedIds ? p1 : from + kCopiedIds;
     for (int p = c0 + (int)threadIdx.x; p < c1; p += S::NT) {
       const int d = g.row_idx ? g.row_idx[p] : p;
@@ -367,7 +409,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
     __syncthreads();
   };
   auto begin_columns = [&](int col) {
-    a.init(rows_a, row0, g.d_out, c0, c1);
+    a.init(rows_a, row0, dy_cols, c0, c1);
     b.init(rows_b, col, g.d_in, c0, c1);
     tile_begin<S>(lds, a, b, rows_a, rows_b, c0, c1);
   };
@@ -427,7 +469,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
 
 // One row of workgroups for each cut but the first position: the cut's leaf, if it crosses a cut here for the first time.
 // Bound by the slots' bytes: 43 us after the 343 of the sums above, most of it the few longest leaves' slots in turn.
-template <typename T>
+template <typename T, bool LISTED>
 __global__ void __launch_bounds__(256) leaf_grad_join_kernel(const LeafArgs<T> g) {
   const int64_t block = (int64_t)blockIdx.y + 1;
   const int64_t at = block * g.cut;

@@ -1,0 +1,554 @@
+// A learned router: which k of the leaves answer a row, and with what weights; and the lists of rows by leaf that follow.
+//
+// Scores s are the softmax of a row's logits, or their sigmoids.  The k leaves of the largest choice values c = s + bias are
+// taken, those of equal values from the lowest index; without a bias the order of s is that of the logits, which are compared
+// themselves.  A row is LANES lanes' work, PER neighbouring columns each: a pick is a maximum over the lanes and the first lane
+// that holds it.
+//
+// c decides between neighbours, so its roundings must not.  Values are taken in f32 with a bound of their error; a row that has two
+// values closer than that among its first k + 1, or at the border of its groups, is taken again in 64 bits (with the other rows of
+// its wavefront, whose choice 64 bits confirm).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+namespace gbdt_router {
+
+constexpr int kMaxLeaves = 1024, kMaxChosen = 32, kMaxGroups = 64;
+constexpr int kThreads = 256;
+
+struct RouteArgs {
+  const void* logits;   // [n_rows][n_leaves]
+  const float* bias;    // [n_leaves] or null
+  int32_t* leaves;      // [n_rows][k]
+  float* gates;         // [n_rows][k]
+  const float* dgates;  // gradient: [n_rows][k]
+  void* dlogits;        // gradient: [n_rows][n_leaves]
+  int64_t ld, ld_out;
+  int32_t n_rows, n_leaves, k;
+  int32_t n_groups, groups_kept, group_best, group_size;
+  int32_t sigmoid, renormalise;
+  float scale;
+};
+
+// ---------------------------------------------------------------- lanes of a row
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+// op over the row's lanes, in all of them.  Within 16 lanes by moves of the vector unit: neighbours, pairs, the other half of
+// eight and of sixteen (mirrored: each half is uniform by then).
+template <int LANES, class Op>
+__device__ __forceinline__ float over_lanes(float v, const Op& op) {
+  v = op(v, dpp<0xB1>(v));                     // lanes 1 0 3 2
+  v = op(v, dpp<0x4E>(v));                     // lanes 2 3 0 1
+  if (LANES >= 8) v = op(v, dpp<0x141>(v));    // mirrored within 8
+  if (LANES >= 16) v = op(v, dpp<0x140>(v));   // mirrored within 16
+  if (LANES >= 32) v = op(v, __shfl_xor(v, 16));
+  if (LANES >= 64) v = op(v, __shfl_xor(v, 32));
+  return v;
+}
+template <int LANES, class Op>
+__device__ __forceinline__ double over_lanes(double v, const Op& op) {
+#pragma unroll
+  for (int m = 1; m < LANES; m <<= 1) v = op(v, __shfl_xor(v, m));
+  return v;
+}
+struct Max {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+  __device__ __forceinline__ double operator()(double a, double b) const { return fmax(a, b); }
+};
+struct Sum {
+  template <typename V>
+  __device__ __forceinline__ V operator()(V a, V b) const { return a + b; }
+};
+
+// Which of the row's lanes say yes: bit i is its lane i.
+template <int LANES>
+__device__ __forceinline__ uint64_t row_ballot(bool yes) {
+  const uint64_t all = __ballot(yes);
+  return LANES == 64 ? all : (all >> ((threadIdx.x & 63) / LANES * LANES)) & ((1ull << (LANES & 63)) - 1);
+}
+
+template <typename V>
+__device__ __forceinline__ V lowest() {
+  return -(V)INFINITY;
+}
+
+// The exponential of a value at or below 0; of a masked logit 0.  inf - inf counts as 0: the largest logit's is 1.
+__device__ __forceinline__ float exp_below(float l, float top) { return l == top ? 1.0f : expf(l - top); }
+__device__ __forceinline__ double exp_below(double l, double top) { return l == top ? 1.0 : exp(l - top); }
+
+__device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
+__device__ __forceinline__ double sigmoid(double l) { return 1.0 / (1.0 + exp(-l)); }
+
+// The largest of the row's values, and its first column, which is taken out; false if only masked ones are left.
+template <typename V, int LANES, int PER>
+__device__ __forceinline__ bool take_largest(V (&v)[PER], V* value, int* column) {
+  V mine = v[0];
+#pragma unroll
+  for (int i = 1; i < PER; ++i) mine = Max{}(mine, v[i]);
+  const V top = over_lanes<LANES>(mine, Max{});
+  const bool any = top > lowest<V>();
+  const uint64_t who = row_ballot<LANES>(mine == top);
+  const int lane = threadIdx.x & (LANES - 1), first = __ffsll((unsigned long long)who) - 1;
+  int at = PER;
+#pragma unroll
+  for (int i = PER - 1; i >= 0; --i) at = v[i] == top ? i : at;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (any && lane == first && i == at) v[i] = lowest<V>();
+  *value = top;
+  *column = first * PER + __shfl(at, first, LANES);
+  return any;
+}
+
+// Values of all but the best groups become masked.  worth: room for kMaxGroups values of this row.  True if a border is closer
+// than `tol` says (of single values).
+template <typename V, int LANES, int PER>
+__device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V tol, V* worth) {
+  const int lane = threadIdx.x & (LANES - 1);
+  int group[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) group[i] = (lane * PER + i) / g.group_size;
+  for (int q = 0; q < g.n_groups; ++q) {
+    V in[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) in[i] = group[i] == q ? v[i] : lowest<V>();
+    V sum = lowest<V>(), second;
+    int column;
+    if (take_largest<V, LANES, PER>(in, &sum, &column) && g.group_best == 2) {
+      if (take_largest<V, LANES, PER>(in, &second, &column)) sum += second;
+    }
+    if (lane == 0) worth[q] = sum;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  // lane i has the groups i, i + LANES, ..
+  constexpr int most = (kMaxGroups + LANES - 1) / LANES;
+  V mine[most];
+#pragma unroll
+  for (int t = 0; t < most; ++t) mine[t] = lane + t * LANES < g.n_groups ? worth[lane + t * LANES] : lowest<V>();
+  uint64_t kept = 0;
+  bool close = false;
+  V last = lowest<V>();
+  for (int r = 0; r <= g.groups_kept; ++r) {
+    V top = mine[0];
+#pragma unroll
+    for (int t = 1; t < most; ++t) top = Max{}(top, mine[t]);
+    top = over_lanes<LANES>(top, Max{});
+    if (r == g.groups_kept) {
+      close = top > lowest<V>() && !(last - top > 2 * tol + (V)0x1p-21 * fabs(last));
+      break;
+    }
+    int who = kMaxGroups;
+#pragma unroll
+    for (int t = most - 1; t >= 0; --t) {
+      const uint64_t w = row_ballot<LANES>(mine[t] == top);
+      if (w) who = t * LANES + __ffsll((unsigned long long)w) - 1;
+    }
+    if (top > lowest<V>()) {
+      kept |= 1ull << who;
+      last = top;
+#pragma unroll
+      for (int t = 0; t < most; ++t)
+        if (lane + t * LANES == who) mine[t] = lowest<V>();
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (!(group[i] < g.n_groups && kept >> group[i] & 1)) v[i] = lowest<V>();
+  return close;
+}
+
+// The k columns of the largest values, -1 where fewer are left, into picked.  True if two of the first k + 1 are closer than
+// their errors, tol of each and 2^-23 of its size.
+template <typename V, int LANES, int PER>
+__device__ __forceinline__ bool choose(const RouteArgs& g, V (&v)[PER], V tol, bool check, V* worth, int* picked) {
+  bool close = g.n_groups > 1 ? keep_groups<V, LANES, PER>(g, v, tol, worth) && check : false;
+  const int lane = threadIdx.x & (LANES - 1), more = check && g.k < g.n_leaves ? 1 : 0;
+  V before = lowest<V>();
+  for (int j = 0; j < g.k + more; ++j) {
+    V top;
+    int column;
+    const bool any = take_largest<V, LANES, PER>(v, &top, &column);
+    if (check && any && j > 0) close |= !(before - top > tol + (V)0x1p-22 * fabs(before));
+    before = top;
+    if (lane == 0 && j < g.k) picked[j] = any ? column : -1;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  return close;
+}
+
+// A lane's PER neighbouring logits; masked ones (NaN, minus infinity, past the end) are minus infinity.
+template <typename T, int PER>
+__device__ __forceinline__ void load_logits(const T* row, int column, int n, float (&l)[PER]) {
+  T t[PER];
+  if (row != nullptr && column + PER <= n) {
+    __builtin_memcpy(t, row + column, sizeof t);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) l[i] = (float)t[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) l[i] = row != nullptr && column + i < n ? (float)row[column + i] : -INFINITY;
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) l[i] = l[i] == l[i] ? l[i] : -INFINITY;
+}
+
+// A row's choice values; *tol: the error of a value in f32 beside 2^-23 of its size.  (Sigmoid: its exponential to 2 ulp and two
+// roundings, of at most 1.  Softmax: the sum of the exponentials, PER + 6 roundings and 2 ulp of each, all of the largest score.)
+template <typename V, int LANES, int PER>
+__device__ __forceinline__ void choice_values(const RouteArgs& g, const float (&l)[PER], float top, V (&v)[PER], V* tol) {
+  const int lane = threadIdx.x & (LANES - 1);
+  V inverse = 1;
+  if (!g.sigmoid) {
+    V sum = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      v[i] = l[i] > -INFINITY ? exp_below((V)l[i], (V)top) : (V)0;
+      sum += v[i];
+    }
+    inverse = 1 / over_lanes<LANES>(sum, Sum{});
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = lane * PER + i;
+    V c = g.sigmoid ? sigmoid((V)l[i]) : v[i] * inverse;
+    if (g.bias != nullptr && e < g.n_leaves) c += (V)g.bias[e];
+    v[i] = l[i] > -INFINITY && c == c ? c : lowest<V>();
+  }
+  *tol = g.sigmoid ? (V)0x1p-20 : (V)0x1p-18 * inverse;
+}
+
+// exp(l - c) / (1 + exp(l)) for l < 0, its limit for the others (whose c is 0): the sigmoid over exp(c), which renormalised
+// weights leave out, so that they hold however small all scores are.
+__device__ __forceinline__ float sigmoid_over(float l, float c) { return l >= 0.0f ? sigmoid(l) : expf(l - c) / (1.0f + expf(l)); }
+
+// k slots of a row, lane i the slots i, i + LANES, ..; scores of the chosen, renormalised or not, without scale.
+template <int LANES>
+struct Slots {
+  static constexpr int kMost = (kMaxChosen + LANES - 1) / LANES;
+  int column[kMost];
+  float logit[kMost], score[kMost];
+  // f(column): the logit, minus infinity for a masked one
+  template <class F>
+  __device__ __forceinline__ void read(const RouteArgs& g, const int* picked, const F& f) {
+    const int lane = threadIdx.x & (LANES - 1);
+#pragma unroll
+    for (int t = 0; t < kMost; ++t) {
+      const int j = lane + t * LANES;
+      column[t] = j < g.k ? picked[j] : -1;
+      logit[t] = column[t] >= 0 ? f(column[t]) : -INFINITY;
+    }
+  }
+  // top, inverse: of all logits, for a softmax that is not renormalised
+  __device__ __forceinline__ void scores(const RouteArgs& g, float top, float inverse) {
+    if (!g.renormalise) {
+#pragma unroll
+      for (int t = 0; t < kMost; ++t)
+        score[t] = !(logit[t] > -INFINITY) ? 0.0f : g.sigmoid ? sigmoid(logit[t]) : exp_below(logit[t], top) * inverse;
+      return;
+    }
+    float best = logit[0];
+#pragma unroll
+    for (int t = 1; t < kMost; ++t) best = fmaxf(best, logit[t]);
+    best = over_lanes<LANES>(best, Max{});
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < kMost; ++t) {
+      score[t] = !(logit[t] > -INFINITY) ? 0.0f : g.sigmoid ? sigmoid_over(logit[t], fminf(best, 0.0f)) : exp_below(logit[t], best);
+      sum += score[t];
+    }
+    sum = over_lanes<LANES>(sum, Sum{});
+#pragma unroll
+    for (int t = 0; t < kMost; ++t) score[t] = sum > 0.0f ? score[t] / sum : 0.0f;
+  }
+};
+
+// Bound by reading the logits where rows are many; k picks of some twenty instructions each are the rest.
+template <typename T, int LANES, int PER>
+__global__ void __launch_bounds__(kThreads) route_kernel(const RouteArgs g) {
+  constexpr int rows = kThreads / LANES;
+  __shared__ double worth[rows][kMaxGroups];
+  __shared__ int picked_of[rows][kMaxChosen];
+  const int r = threadIdx.x / LANES, lane = threadIdx.x & (LANES - 1);
+  const int64_t d = (int64_t)blockIdx.x * rows + r;
+  const T* row = d < g.n_rows ? (const T*)g.logits + d * g.ld : nullptr;
+  int* picked = picked_of[r];
+  float l[PER];
+  load_logits<T, PER>(row, lane * PER, g.n_leaves, l);
+  float top = l[0];
+#pragma unroll
+  for (int i = 1; i < PER; ++i) top = fmaxf(top, l[i]);
+  top = over_lanes<LANES>(top, Max{});
+  float v[PER];
+  if (g.bias == nullptr && g.group_best == 1) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = l[i];
+    choose<float, LANES, PER>(g, v, 0.0f, false, (float*)worth[r], picked);
+  } else {
+    float tol;
+    choice_values<float, LANES, PER>(g, l, top, v, &tol);
+    if (__any(choose<float, LANES, PER>(g, v, tol, true, (float*)worth[r], picked))) {
+      double exact[PER], none;
+      choice_values<double, LANES, PER>(g, l, top, exact, &none);
+      choose<double, LANES, PER>(g, exact, none, false, worth[r], picked);
+    }
+  }
+  float inverse = 0.0f;
+  if (!g.sigmoid && !g.renormalise) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += l[i] > -INFINITY ? exp_below(l[i], top) : 0.0f;
+    inverse = 1.0f / over_lanes<LANES>(sum, Sum{});
+  }
+  Slots<LANES> s;
+  s.read(g, picked, [&](int e) { return (float)row[e]; });
+  s.scores(g, top, inverse);
+  if (row == nullptr) return;
+#pragma unroll
+  for (int t = 0; t < Slots<LANES>::kMost; ++t) {
+    const int j = lane + t * LANES;
+    if (j >= g.k) break;
+    g.leaves[d * g.k + j] = s.column[t];
+    g.gates[d * g.k + j] = g.scale * s.score[t];
+  }
+}
+
+// With s the score and r the share of a slot:
+//   softmax, renormalised   scale r (dg - sum r dg) at the slot's leaf
+//   softmax                 scale s ([chosen] dg - sum s dg) at every leaf
+//   sigmoid, renormalised   scale r (1 - s) (dg - sum r dg) at the slot's leaf
+//   sigmoid                 scale s (1 - s) dg at the slot's leaf
+// and zeros elsewhere.  Bound by writing the gradients and, for the second, reading the logits.
+template <typename T, int LANES, int PER>
+__global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteArgs g) {
+  constexpr int rows = kThreads / LANES;
+  __shared__ int picked_of[rows][kMaxChosen];
+  __shared__ float each_of[rows][kMaxChosen];
+  const int r = threadIdx.x / LANES, lane = threadIdx.x & (LANES - 1);
+  const int64_t d = (int64_t)blockIdx.x * rows + r;
+  const T* row = d < g.n_rows ? (const T*)g.logits + d * g.ld : nullptr;
+  int* picked = picked_of[r];
+  float* each = each_of[r];
+  for (int j = lane; j < g.k; j += LANES) {
+    const int e = row != nullptr ? g.leaves[d * g.k + j] : -1;
+    picked[j] = (uint32_t)e < (uint32_t)g.n_leaves ? e : -1;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  const bool all = !g.sigmoid && !g.renormalise;
+  float p[PER], top = 0.0f, inverse = 0.0f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) p[i] = 0.0f;
+  if (all) {
+    float l[PER];
+    load_logits<T, PER>(row, lane * PER, g.n_leaves, l);
+    top = l[0];
+#pragma unroll
+    for (int i = 1; i < PER; ++i) top = fmaxf(top, l[i]);
+    top = over_lanes<LANES>(top, Max{});
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      p[i] = l[i] > -INFINITY ? exp_below(l[i], top) : 0.0f;
+      sum += p[i];
+    }
+    sum = over_lanes<LANES>(sum, Sum{});
+    inverse = sum > 0.0f ? 1.0f / sum : 0.0f;
+  }
+  Slots<LANES> s;
+  s.read(g, picked, [&](int e) {
+    const float l = (float)row[e];
+    return l == l ? l : -INFINITY;
+  });
+  s.scores(g, top, inverse);
+  float dg[Slots<LANES>::kMost], inner = 0.0f;
+#pragma unroll
+  for (int t = 0; t < Slots<LANES>::kMost; ++t) {
+    dg[t] = s.logit[t] > -INFINITY ? g.dgates[d * g.k + lane + t * LANES] : 0.0f;
+    inner += s.score[t] * dg[t];
+  }
+  inner = over_lanes<LANES>(inner, Sum{});
+#pragma unroll
+  for (int t = 0; t < Slots<LANES>::kMost; ++t) {
+    const int j = lane + t * LANES;
+    if (j >= g.k) break;
+    float v = g.scale * s.score[t] * (g.renormalise ? dg[t] - inner : dg[t]);
+    if (g.sigmoid) v *= sigmoid(-s.logit[t]);
+    each[j] = s.logit[t] > -INFINITY ? v : 0.0f;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (row == nullptr) return;
+  float out[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) out[i] = all ? -g.scale * (p[i] * inverse) * inner : 0.0f;
+  for (int j = 0; j < g.k; ++j) {
+    const int at = picked[j] - lane * PER;
+    const float v = each[j];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) out[i] += at == i ? v : 0.0f;
+  }
+  T* to = (T*)g.dlogits + d * g.ld_out + lane * PER;
+  T t[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) t[i] = (T)out[i];
+  const int left = g.n_leaves - lane * PER;
+  if (left >= PER) {
+    __builtin_memcpy(to, t, sizeof t);
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (i < left) to[i] = t[i];
+  }
+}
+
+// ---------------------------------------------------------------- lists of rows by leaf
+
+// Pairs p = row * k + slot, grouped by leaf, ascending within one: what the products take.  Pairs whose leaf is none are in no
+// list.  A wavefront counts a run of neighbouring pairs in local memory, a table of its own for all leaves; sums over the runs give
+// each its places, and it goes through its pairs again.  No order hangs on which ran first.
+struct ListArgs {
+  const int32_t* leaves;   // [n_pairs]
+  int64_t* offsets;        // [n_leaves + 1]
+  int32_t* row;            // [n_pairs] of each position
+  int32_t* pair;           // [n_pairs]
+  int32_t* counts;         // [n_leaves][runs], then the first places within the leaf
+  int32_t* totals;         // [n_leaves]
+  int32_t n_pairs, n_leaves, k, run, runs;  // run: pairs, a multiple of 64
+};
+
+constexpr int kListWaves = 16;             // of the one workgroup that lists few pairs
+constexpr int kFewListLeaves = 1024;       // it takes that many leaves
+constexpr int kMaxListLeaves = 16384;
+
+// Adds the run's pairs to a table.
+__device__ __forceinline__ void count_run(const ListArgs& g, int first, int end, int* table) {
+  const int lane = threadIdx.x & 63;
+  for (int p = first + lane; p < end; p += 64) {
+    const int e = g.leaves[p];
+    if ((uint32_t)e < (uint32_t)g.n_leaves) __hip_atomic_fetch_add(&table[e], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  }
+}
+
+// Puts the run's pairs to the places that the table has for them, in order.
+__device__ __forceinline__ void place_run(const ListArgs& g, int first, int end, int* table) {
+  const int lane = threadIdx.x & 63, bits = 32 - __clz(g.n_leaves);
+  const uint64_t below = (1ull << lane) - 1;
+  for (int p0 = first; p0 < end; p0 += 64) {
+    const int p = p0 + lane;
+    int e = p < end ? g.leaves[p] : -1;
+    if ((uint32_t)e >= (uint32_t)g.n_leaves) e = -1;
+    uint64_t same = __ballot(e >= 0);
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t ones = __ballot(e >> b & 1);
+      same &= e >> b & 1 ? ones : ~ones;
+    }
+    if (e >= 0) {
+      const int at = table[e];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if ((same >> lane) == 1) table[e] = at + __popcll(same);  // the last of them
+      const int to = at + __popcll(same & below);
+      g.row[to] = p / g.k;
+      g.pair[to] = p;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
+// Sum over the lanes before this one; *all: over all lanes.
+__device__ __forceinline__ int before_lane(int v, int* all) {
+  const int lane = threadIdx.x & 63;
+  int sum = v;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int other = __shfl_up(sum, m);
+    if (lane >= m) sum += other;
+  }
+  *all = __shfl(sum, 63);
+  return sum - v;
+}
+
+__global__ void __launch_bounds__(kListWaves * 64) list_few_kernel(const ListArgs g) {
+  __shared__ int table[kListWaves][kFewListLeaves];
+  __shared__ int sums[kListWaves];
+  const int t = threadIdx.x, w = t >> 6;
+  for (int i = t & 63; i < g.n_leaves; i += 64) table[w][i] = 0;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  const int first = w * g.run < g.n_pairs ? w * g.run : g.n_pairs;
+  const int end = first + g.run < g.n_pairs ? first + g.run : g.n_pairs;
+  count_run(g, first, end, table[w]);
+  __syncthreads();
+  static_assert(kListWaves * 64 >= kFewListLeaves, "a thread a leaf");
+  int total = 0;
+  if (t < g.n_leaves)
+    for (int i = 0; i < kListWaves; ++i) {
+      const int n = table[i][t];
+      table[i][t] = total;
+      total += n;
+    }
+  int wave_total;
+  int at = before_lane(total, &wave_total);
+  if ((t & 63) == 0) sums[w] = wave_total;
+  __syncthreads();
+  for (int i = 0; i < w; ++i) at += sums[i];
+  if (t < g.n_leaves) {
+    g.offsets[t] = at;
+    if (t == g.n_leaves - 1) g.offsets[g.n_leaves] = at + total;
+    for (int i = 0; i < kListWaves; ++i) table[i][t] += at;
+  }
+  __syncthreads();
+  place_run(g, first, end, table[w]);
+}
+
+// Many pairs: a wavefront a workgroup and run.
+template <int LEAVES>
+__global__ void __launch_bounds__(64) list_count_kernel(const ListArgs g) {
+  __shared__ int table[LEAVES];
+  for (int i = threadIdx.x; i < g.n_leaves; i += 64) table[i] = 0;
+  __syncthreads();
+  const int first = (int)blockIdx.x * g.run, end = g.n_pairs - first < g.run ? g.n_pairs : first + g.run;
+  count_run(g, first, end, table);
+  __syncthreads();
+  for (int i = threadIdx.x; i < g.n_leaves; i += 64) g.counts[(int64_t)i * g.runs + blockIdx.x] = table[i];
+}
+
+// A leaf a workgroup: its counts become sums of those before.
+__global__ void __launch_bounds__(64) list_scan_kernel(const ListArgs g) {
+  int32_t* counts = g.counts + (int64_t)blockIdx.x * g.runs;
+  int base = 0;
+  for (int i0 = 0; i0 < g.runs; i0 += 64) {
+    const int i = i0 + threadIdx.x, n = i < g.runs ? counts[i] : 0;
+    int all;
+    const int at = before_lane(n, &all);
+    if (i < g.runs) counts[i] = base + at;
+    base += all;
+  }
+  if (threadIdx.x == 0) g.totals[blockIdx.x] = base;
+}
+
+template <int LEAVES>
+__global__ void __launch_bounds__(64) list_place_kernel(const ListArgs g) {
+  __shared__ int table[LEAVES];
+  int base = 0;
+  for (int i0 = 0; i0 < g.n_leaves; i0 += 64) {
+    const int i = i0 + threadIdx.x, n = i < g.n_leaves ? g.totals[i] : 0;
+    int all;
+    const int at = base + before_lane(n, &all);
+    if (i < g.n_leaves) {
+      table[i] = at + g.counts[(int64_t)i * g.runs + blockIdx.x];
+      if (blockIdx.x == 0) g.offsets[i] = at;
+    }
+    base += all;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) g.offsets[g.n_leaves] = base;
+  __syncthreads();
+  const int first = (int)blockIdx.x * g.run, end = g.n_pairs - first < g.run ? g.n_pairs : first + g.run;
+  place_run(g, first, end, table);
+}
+
+}  // namespace gbdt_router

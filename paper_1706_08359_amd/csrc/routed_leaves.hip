@@ -1,0 +1,682 @@
+// Rows routed to several linear leaves, and leaf products in 8-bit integers: host side of gbdt_route, gbdt_route_grad,
+// gbdt_mixture_product, gbdt_mixture_product_grad, gbdt_rows_quantize, gbdt_leaf_product_codes and gbdt_mixture_product_codes (checks,
+// choice of tile, scratch, launches).  The kernels are in route_kernels.h, routed_kernels.h and code_kernels.h.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "../../include/gbdt_hist.h"
+#include "library_state.h"
+
+#include "code_kernels.h"
+#include "product_host.h"
+#include "route_kernels.h"
+#include "routed_kernels.h"
+
+namespace {
+
+using namespace gbdt_host;
+using gbdt_code::CodeArgs;
+using gbdt_router::RouteArgs;
+using gbdt_routed::CombineArgs;
+using gbdt_routed::RoutedArgs;
+
+// ---------------------------------------------------------------- routing
+
+int route_check(const void* logits, int64_t ld, int64_t n_rows, int32_t n_leaves, int32_t dtype, int32_t score, int32_t k, float scale) {
+  if (n_rows < 0 || n_leaves <= 0 || k <= 0 || k > n_leaves || ld < n_leaves || !isfinite(scale)) return GBDT_EINVAL;
+  if (dtype != GBDT_F32 && dtype != GBDT_BF16) return GBDT_EINVAL;
+  if (score != GBDT_SOFTMAX && score != GBDT_SIGMOID) return GBDT_EINVAL;
+  if (off_element(logits, dtype)) return GBDT_EINVAL;
+  if (n_rows >= kMaxRows || ld >= kMaxLd || n_leaves > gbdt_router::kMaxLeaves || k > gbdt_router::kMaxChosen) return GBDT_EUNSUPPORTED;
+  return GBDT_OK;
+}
+
+template <typename T, int LANES, int PER>
+int launch_route(const RouteArgs& g, bool grad, hipStream_t s) {
+  const unsigned blocks = (unsigned)ceil_div(g.n_rows, gbdt_router::kThreads / LANES);
+  if (grad) {
+    gbdt_router::route_grad_kernel<T, LANES, PER><<<dim3(blocks), dim3(gbdt_router::kThreads), 0, s>>>(g);
+  } else {
+    gbdt_router::route_kernel<T, LANES, PER><<<dim3(blocks), dim3(gbdt_router::kThreads), 0, s>>>(g);
+  }
+  LAUNCHED("routing");
+  return GBDT_OK;
+}
+
+template <typename T>
+int route(const RouteArgs& g, bool grad, hipStream_t s) {
+  if (g.n_leaves <= 32) return launch_route<T, 8, 4>(g, grad, s);
+  if (g.n_leaves <= 64) return launch_route<T, 16, 4>(g, grad, s);
+  if (g.n_leaves <= 128) return launch_route<T, 32, 4>(g, grad, s);
+  if (g.n_leaves <= 256) return launch_route<T, 64, 4>(g, grad, s);
+  if (g.n_leaves <= 512) return launch_route<T, 64, 8>(g, grad, s);
+  return launch_route<T, 64, 16>(g, grad, s);
+}
+
+// ---------------------------------------------------------------- lists of pairs
+
+struct ListPlan {
+  int64_t pairs, run, runs;  // runs 0: one workgroup lists all
+  size_t table_bytes;        // of the counts: no less for more pairs
+  size_t offsets_bytes, row_bytes, count_bytes;
+  size_t bytes() const { return offsets_bytes + 2 * row_bytes + count_bytes; }
+};
+// One workgroup lists few pairs by itself, which is one launch instead of three.
+constexpr int64_t kFewPairs = 8192;
+ListPlan list_plan(int64_t pairs, int64_t n_leaves) {
+  ListPlan p;
+  p.pairs = pairs;
+  p.offsets_bytes = pad256((size_t)(n_leaves + 1) * 8);
+  p.row_bytes = pad256((size_t)pairs * 4);
+  p.table_bytes = p.count_bytes = 0;
+  if (pairs <= kFewPairs && n_leaves <= gbdt_router::kFewListLeaves) {
+    p.run = round_up(ceil_div(pairs, gbdt_router::kListWaves), 64);
+    p.runs = 0;
+  } else {
+    const int64_t most = std::min<int64_t>(2048, std::max<int64_t>(64, ((int64_t)8 << 20) / n_leaves));
+    p.run = std::max<int64_t>(256, round_up(ceil_div(pairs, most), 64));
+    p.runs = std::max<int64_t>(1, ceil_div(pairs, p.run));
+    p.table_bytes = pad256((size_t)(n_leaves * std::min(most, std::max<int64_t>(1, ceil_div(pairs, 256)))) * 4);
+    p.count_bytes = p.table_bytes + pad256((size_t)n_leaves * 4);
+  }
+  return p;
+}
+
+template <int LEAVES>
+int launch_lists(const gbdt_router::ListArgs& g, hipStream_t s) {
+  gbdt_router::list_count_kernel<LEAVES><<<dim3(g.runs), dim3(64), 0, s>>>(g);
+  LAUNCHED("list_count_kernel");
+  gbdt_router::list_scan_kernel<<<dim3(g.n_leaves), dim3(64), 0, s>>>(g);
+  LAUNCHED("list_scan_kernel");
+  gbdt_router::list_place_kernel<LEAVES><<<dim3(g.runs), dim3(64), 0, s>>>(g);
+  LAUNCHED("list_place_kernel");
+  return GBDT_OK;
+}
+
+// Lists the pairs of n_rows rows in scratch of plan.bytes(), and says where.
+int make_lists(const ListPlan& plan, const int32_t* leaves, int32_t n_leaves, int32_t k, char* scratch, const int64_t** offsets,
+               const int32_t** row, const int32_t** pair, hipStream_t s) {
+  gbdt_router::ListArgs g = {};
+  g.leaves = leaves;
+  g.offsets = (int64_t*)scratch;
+  g.row = (int32_t*)(scratch + plan.offsets_bytes);
+  g.pair = (int32_t*)(scratch + plan.offsets_bytes + plan.row_bytes);
+  g.counts = (int32_t*)(scratch + plan.offsets_bytes + 2 * plan.row_bytes);
+  g.totals = g.counts + plan.table_bytes / 4;
+  g.n_pairs = (int32_t)plan.pairs;
+  g.n_leaves = n_leaves;
+  g.k = k;
+  g.run = (int32_t)plan.run;
+  g.runs = (int32_t)plan.runs;
+  *offsets = g.offsets;
+  *row = g.row;
+  *pair = g.pair;
+  if (plan.runs == 0) {
+    gbdt_router::list_few_kernel<<<dim3(1), dim3(gbdt_router::kListWaves * 64), 0, s>>>(g);
+    LAUNCHED("list_few_kernel");
+    return GBDT_OK;
+  }
+  if (n_leaves <= 1024) return launch_lists<1024>(g, s);
+  if (n_leaves <= 4096) return launch_lists<4096>(g, s);
+  return launch_lists<gbdt_router::kMaxListLeaves>(g, s);
+}
+
+// ---------------------------------------------------------------- mixtures
+
+// Slots of so many rows at a time as take this, or of 1,024.
+constexpr int64_t kSlotsBytes = (int64_t)256 << 20;
+// Weighted gradients of so many outputs at a time as take this, or of a tile.
+constexpr int64_t kGatedBytes = (int64_t)256 << 20;
+constexpr int32_t kMaxSlots = 64;  // leaves a row
+
+struct SlotPlan {
+  int64_t rows, ld;  // rows at a time
+  ListPlan list;
+  size_t slots_bytes;
+  size_t bytes() const { return list.bytes() + slots_bytes; }
+};
+SlotPlan slot_plan(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t cols) {
+  SlotPlan p;
+  p.ld = round_up(cols, 4);
+  p.rows = std::min(n_rows, std::max<int64_t>(1024, kSlotsBytes / (k * p.ld * 4)));
+  p.list = list_plan(p.rows * k, n_leaves);
+  p.slots_bytes = pad256((size_t)(p.rows * k * p.ld) * 4);
+  return p;
+}
+
+struct WeightPlan {
+  ListPlan list;
+  int64_t piece;  // outputs at a time
+  int64_t ld;
+  LeafGradPlan sums;
+  size_t gated_bytes;
+  size_t bytes() const { return list.bytes() + gated_bytes + sums.bytes; }
+};
+WeightPlan weight_plan(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t d_in, int64_t d_out, int64_t e, int64_t units) {
+  WeightPlan p;
+  const int64_t pairs = n_rows * k;
+  p.list = list_plan(pairs, n_leaves);
+  p.sums = leaf_grad_plan(e, pairs, d_in, d_out, units);
+  p.piece = std::max(p.sums.bm, kGatedBytes / std::max<int64_t>(1, pairs * e) / p.sums.bm * p.sums.bm);
+  p.piece = std::min(p.piece, d_out);
+  p.ld = round_up(p.piece, 16 / e);
+  p.gated_bytes = pad256((size_t)(pairs * p.ld * e));
+  return p;
+}
+
+int mixture_check(int64_t n_rows, int32_t k, int32_t n_leaves, int32_t d_in, int32_t d_out, const void* leaves, const void* gates,
+                  int32_t dtype) {
+  if (n_rows < 0 || k <= 0 || n_leaves <= 0 || d_in <= 0 || d_out <= 0) return GBDT_EINVAL;
+  if (n_rows > 0 && (!leaves || !gates)) return GBDT_EINVAL;
+  if (((uintptr_t)leaves & 3) != 0 || ((uintptr_t)gates & 3) != 0) return GBDT_EINVAL;
+  if (dtype != GBDT_F32 && dtype != GBDT_BF16) return GBDT_EINVAL;
+  if (n_rows >= kMaxRows || k > kMaxSlots || n_rows * k >= kMaxRows || n_leaves > gbdt_router::kMaxListLeaves || d_in >= kMaxWidth ||
+      d_out >= kMaxWidth)
+    return GBDT_EUNSUPPORTED;
+  return GBDT_OK;
+}
+
+template <class S, typename T>
+int launch_routed_product(RoutedArgs<T>& g, hipStream_t s) {
+  return leaf_rows_launches<S>(g, g.d_out, S::NT, [&](dim3 blocks) {
+    gbdt_routed::routed_product_kernel<S><<<blocks, dim3(S::NT), 0, s>>>(g);
+  });
+}
+template <class S, typename T>
+int launch_routed_grad_input(RoutedArgs<T>& g, hipStream_t s) {
+  return leaf_rows_launches<S>(g, g.d_in, S::NT, [&](dim3 blocks) {
+    gbdt_routed::routed_grad_input_kernel<S><<<blocks, dim3(S::NT), 0, s>>>(g);
+  });
+}
+
+// Leaves of few positions: tiles of 32 rows, which waste less and leave room for more workgroups reading matrices.
+template <typename T>
+bool short_leaves(const gbdt_leaf::LeafArgs<T>& g) {
+  return g.n_positions <= 32 * (int64_t)g.n_leaves;
+}
+template <typename T>
+using Short = Shape<T, 32, 128, 1, 2, true>;
+
+template <typename T>
+int routed_product(RoutedArgs<T>& g, hipStream_t s) {
+  const bool direct = whole_chunks<T>(g.x, g.ld_x, g.d_in) && whole_chunks<T>(g.w, g.d_in, g.d_in);
+  if constexpr (sizeof(T) == 2) {
+    if (direct) {
+      if (short_leaves(g)) return launch_routed_product<Short<T>>(g, s);
+      if (g.d_out <= 64) return launch_routed_product<Shape<T, 128, 64, 4, 1, true>>(g, s);
+      if (wide_leaves(g, g.d_out)) return launch_routed_product<Wide<T>>(g, s);
+      if (long_leaves(g, g.d_out, 128)) return launch_routed_product<Shape<T, 256, 128, 4, 2, true, false, 3>>(g, s);
+    }
+  }
+  return direct ? launch_routed_product<Square<T>>(g, s) : launch_routed_product<SquareAny<T>>(g, s);
+}
+
+template <typename T>
+int routed_grad_input(RoutedArgs<T>& g, hipStream_t s) {
+  const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.w, g.d_in, g.d_in);
+  if constexpr (sizeof(T) == 2) {
+    if (direct && short_leaves(g)) return launch_routed_grad_input<Short<T>>(g, s);
+    if (direct && wide_leaves(g, g.d_in)) return launch_routed_grad_input<Wide<T>>(g, s);
+  }
+  return direct ? launch_routed_grad_input<Square<T>>(g, s) : launch_routed_grad_input<SquareAny<T>>(g, s);
+}
+
+template <typename O>
+int combine(const CombineArgs<O>& g, hipStream_t s) {
+  if (g.cols <= 64) {
+    gbdt_routed::combine_kernel<O, 16><<<dim3((unsigned)ceil_div(g.n_rows, 16)), dim3(256), 0, s>>>(g);
+  } else {
+    gbdt_routed::combine_kernel<O, 64><<<dim3((unsigned)ceil_div(g.n_rows, 4)), dim3(256), 0, s>>>(g);
+  }
+  LAUNCHED("combine_kernel");
+  return GBDT_OK;
+}
+
+// So few rows that a wavefront for every few outputs of a row takes less than lists, tiles and slots.
+bool few_rows(int64_t n_rows, int64_t k, int64_t d_out) { return n_rows <= 4 || (n_rows <= 2048 && n_rows * k * d_out <= 16384); }
+
+// Products of all rows, kept in slots and added up, so many rows at a time as the plan says.  products(g): to the slots.
+template <typename T, class G, typename O, class Products>
+int by_slots(const G& all, int64_t n_rows, int64_t cols, const CombineArgs<O>& to, const SlotPlan& plan, char* scratch,
+             const Products& products, hipStream_t s, const T* in, int64_t ld_in, bool grad) {
+  for (int64_t r = 0; r < n_rows; r += plan.rows) {
+    const int64_t n = std::min(plan.rows, n_rows - r);
+    G g = all;
+    g.leaves += r * g.k;
+    const ListPlan list = n == plan.rows ? plan.list : list_plan(n * g.k, g.n_leaves);
+    int rc = make_lists(list, g.leaves, g.n_leaves, g.k, scratch, &g.offsets, &g.row_idx, &g.pair_idx, s);
+    if (rc != GBDT_OK) return rc;
+    g.slots = (float*)(scratch + plan.list.bytes());
+    g.ld_slots = plan.ld;
+    g.n_rows = (int32_t)n;
+    g.n_positions = (int32_t)(n * g.k);
+    if ((rc = products(g, in + r * ld_in, r)) != GBDT_OK) return rc;
+    CombineArgs<O> c = to;
+    c.slots = g.slots;
+    c.leaves = g.leaves;
+    c.gates += r * g.k;
+    if (c.out) c.out += r * c.ld_out;
+    c.ld = plan.ld;
+    c.n_rows = (int32_t)n;
+    c.n_leaves = g.n_leaves;
+    c.k = g.k;
+    c.cols = (int32_t)cols;
+    if (!grad) {
+      if ((rc = combine(c, s)) != GBDT_OK) return rc;
+      continue;
+    }
+    c.x += r * c.ld_x;
+    c.dy += r * c.ld_dy;
+    if (c.dgates) c.dgates += r * g.k;
+    gbdt_routed::combine_grad_kernel<O><<<dim3((unsigned)ceil_div(n, 4)), dim3(256), 0, s>>>(c);
+    LAUNCHED("combine_grad_kernel");
+  }
+  return GBDT_OK;
+}
+
+template <typename T>
+int mixture_product(RoutedArgs<T>& g, int64_t n_rows, hipStream_t s) {
+  if (few_rows(n_rows, g.k, g.d_out)) {
+    if (n_rows * g.d_out <= 1024) {
+      gbdt_routed::routed_few_kernel<T, 1><<<dim3(g.d_out, (unsigned)n_rows), dim3(64), 0, s>>>(g);
+    } else {
+      gbdt_routed::routed_few_kernel<T, 2><<<dim3((unsigned)ceil_div(g.d_out, 2), (unsigned)n_rows), dim3(64), 0, s>>>(g);
+    }
+    LAUNCHED("routed_few_kernel");
+    return GBDT_OK;
+  }
+  const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out);
+  void* ws = nullptr;
+  const int rc = gbdt_internal::workspace(plan.bytes(), s, &ws);
+  if (rc != GBDT_OK) return rc;
+  CombineArgs<T> to = {};
+  to.gates = g.gates;
+  to.out = g.y;
+  to.ld_out = g.ld_y;
+  return by_slots<T>(g, n_rows, g.d_out, to, plan, (char*)ws,
+                     [&](RoutedArgs<T>& piece, const T* x, int64_t) {
+                       piece.x = x;
+                       return routed_product(piece, s);
+                     },
+                     s, g.x, g.ld_x, false);
+}
+
+template <typename T>
+int mixture_weights(RoutedArgs<T> g, int64_t n_rows, const WeightPlan& plan, char* scratch, hipStream_t s) {
+  g.n_rows = (int32_t)n_rows;
+  g.n_positions = (int32_t)(n_rows * g.k);
+  int rc = make_lists(plan.list, g.leaves, g.n_leaves, g.k, scratch, &g.offsets, &g.row_idx, &g.pair_idx, s);
+  if (rc != GBDT_OK) return rc;
+  T* gated = (T*)(scratch + plan.list.bytes());
+  if (!g.dw) g.x = gated, g.ld_x = plan.ld, g.d_in = kChunk<T>;  // the outputs' sums alone read no inputs
+  g.cut = (int32_t)plan.sums.cut;
+  g.partial = (float*)(scratch + plan.list.bytes() + plan.gated_bytes);
+  const bool direct = whole_chunks<T>(g.x, g.ld_x, g.d_in);
+  const RoutedArgs<T> whole = g;
+  for (int64_t first = 0; first < g.d_out; first += plan.piece) {
+    const int64_t cols = std::min(plan.piece, whole.d_out - first);
+    if (n_rows > 0) {
+      gbdt_routed::gated_rows_kernel<T><<<dim3((unsigned)ceil_div(g.n_positions, 4)), dim3(256), 0, s>>>(whole, gated, plan.ld, (int)first, (int)cols);
+      LAUNCHED("gated_rows_kernel");
+    }
+    g.dy = gated;
+    g.ld_dy = plan.ld;
+    g.row_first = (int32_t)first;
+    if constexpr (sizeof(T) == 2) {
+      if (plan.sums.bm == 64)
+        rc = direct ? launch_leaf_grad_weight<Shape<T, 64, 128, 1, 4, true, true>, true>(g, s, cols)
+                    : launch_leaf_grad_weight<Shape<T, 64, 128, 1, 4, false>, true>(g, s, cols);
+      else
+        rc = direct ? launch_leaf_grad_weight<Square<T>, true>(g, s, cols) : launch_leaf_grad_weight<SquareAny<T>, true>(g, s, cols);
+    } else {
+      rc = direct ? launch_leaf_grad_weight<Square<T>, true>(g, s, cols) : launch_leaf_grad_weight<SquareAny<T>, true>(g, s, cols);
+    }
+    if (rc != GBDT_OK) return rc;
+  }
+  return launch_leaf_grad_join<true>(g, s);
+}
+
+template <typename T>
+int mixture_product_grad(RoutedArgs<T>& g, int64_t n_rows, hipStream_t s) {
+  const bool weights = g.dw || g.dbias, rows = (g.dx || g.dgates) && n_rows > 0;
+  if (!weights && !rows) return GBDT_OK;
+  const SlotPlan slots = slot_plan(n_rows, g.k, g.n_leaves, g.d_in);
+  const WeightPlan sums = weight_plan(n_rows, g.k, g.n_leaves, g.dw ? g.d_in : kChunk<T>, g.d_out, sizeof(T), gbdt_internal::cu_count());
+  if (weights && sums.sums.tiles > most_blocks(kGradThreads) / 8) return GBDT_EUNSUPPORTED;
+  void* ws = nullptr;
+  int rc = gbdt_internal::workspace(std::max(rows ? slots.bytes() : 0, weights ? sums.bytes() : 0), s, &ws);
+  if (rc != GBDT_OK) return rc;
+  if (rows) {
+    CombineArgs<T> to = {};
+    to.gates = g.gates;
+    to.out = g.dx;
+    to.ld_out = g.ld_dx;
+    to.x = g.x;
+    to.dy = g.dy;
+    to.bias = g.bias;
+    to.dgates = g.dgates;
+    to.ld_x = g.ld_x;
+    to.ld_dy = g.ld_dy;
+    to.d_out = g.d_out;
+    rc = by_slots<T>(g, n_rows, g.d_in, to, slots, (char*)ws,
+                     [&](RoutedArgs<T>& piece, const T* dy, int64_t) {
+                       piece.dy = dy;
+                       return routed_grad_input(piece, s);
+                     },
+                     s, g.dy, g.ld_dy, true);
+    if (rc != GBDT_OK) return rc;
+  }
+  return weights ? mixture_weights(g, n_rows, sums, (char*)ws, s) : GBDT_OK;
+}
+
+template <typename T>
+int mixture_call(const void* x, int64_t ld_x, const void* weight, const void* bias, const int32_t* leaves, const float* gates, int64_t n_rows,
+                 int32_t k, int32_t n_leaves, int32_t d_in, int32_t d_out, void* y_out, int64_t ld_y, hipStream_t s) {
+  RoutedArgs<T> g = {};
+  g.x = (const T*)x;
+  g.w = (const T*)weight;
+  g.bias = (const T*)bias;
+  g.y = (T*)y_out;
+  g.leaves = leaves;
+  g.gates = gates;
+  g.ld_x = ld_x;
+  g.ld_y = ld_y;
+  g.n_leaves = n_leaves;
+  g.d_in = d_in;
+  g.d_out = d_out;
+  g.k = k;
+  return mixture_product(g, n_rows, s);
+}
+
+template <typename T>
+int mixture_grad_call(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* weight, const void* bias, const int32_t* leaves,
+                      const float* gates, int64_t n_rows, int32_t k, int32_t n_leaves, int32_t d_in, int32_t d_out, void* dx_out,
+                      int64_t ld_dx, void* dweight_out, void* dbias_out, float* dgates_out, hipStream_t s) {
+  RoutedArgs<T> g = {};
+  g.x = (const T*)x;
+  g.dy = (const T*)dy;
+  g.w = (const T*)weight;
+  g.bias = (const T*)bias;
+  g.dx = (T*)dx_out;
+  g.dw = (T*)dweight_out;
+  g.dbias = (T*)dbias_out;
+  g.dgates = dgates_out;
+  g.leaves = leaves;
+  g.gates = gates;
+  g.ld_x = ld_x;
+  g.ld_dy = ld_dy;
+  g.ld_dx = ld_dx;
+  g.n_leaves = n_leaves;
+  g.d_in = d_in;
+  g.d_out = d_out;
+  g.k = k;
+  return mixture_product_grad(g, n_rows, s);
+}
+
+// ---------------------------------------------------------------- 8-bit integers
+
+int code_check(const void* codes, int64_t ld_codes, const float* scales, const void* weight, const float* weight_scales, const float* bias,
+               int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype, const void* y_out, int64_t ld_y) {
+  const int64_t padded = round_up(d_in, 16);
+  if (ld_codes < padded || ld_codes % 16 != 0 || ((uintptr_t)codes & 15) != 0 || ((uintptr_t)weight & 15) != 0) return GBDT_EINVAL;
+  if (!weight || !weight_scales || ld_y < d_out || off_element(y_out, dtype)) return GBDT_EINVAL;
+  if (((uintptr_t)scales & 3) != 0 || ((uintptr_t)weight_scales & 3) != 0 || ((uintptr_t)bias & 3) != 0) return GBDT_EINVAL;
+  if (n_rows > 0 && (!codes || !scales || !y_out)) return GBDT_EINVAL;
+  if (padded > gbdt_code::kMaxWidth || ld_codes >= kMaxLd || ld_y >= kMaxLd) return GBDT_EUNSUPPORTED;
+  return GBDT_OK;
+}
+
+template <typename T, int CHUNKS>
+int launch_quantize(const gbdt_code::QuantizeArgs& g, hipStream_t s) {
+  gbdt_code::quantize_kernel<T, CHUNKS><<<dim3((unsigned)ceil_div(g.n_rows, 4)), dim3(256), 0, s>>>(g);
+  LAUNCHED("quantize_kernel");
+  return GBDT_OK;
+}
+template <typename T>
+int quantize(const gbdt_code::QuantizeArgs& g, hipStream_t s) {
+  if (g.padded <= 512) return launch_quantize<T, 1>(g, s);
+  if (g.padded <= 1024) return launch_quantize<T, 2>(g, s);
+  return launch_quantize<T, 4>(g, s);
+}
+
+template <class S, typename O, bool SLOTS>
+int launch_code_product(CodeArgs& g, hipStream_t s) {
+  return leaf_rows_launches<S>(g, g.d_out, S::NT, [&](dim3 blocks) {
+    gbdt_code::code_product_kernel<S, O, SLOTS><<<blocks, dim3(S::NT), 0, s>>>(g);
+  });
+}
+
+template <typename O, bool SLOTS>
+int code_tiles(CodeArgs& g, hipStream_t s) {
+  if (short_leaves(g)) return launch_code_product<Short<int8_t>, O, SLOTS>(g, s);
+  if (g.d_out <= 64) return launch_code_product<Shape<int8_t, 128, 64, 4, 1, true>, O, SLOTS>(g, s);
+  if (wide_leaves(g, g.d_out)) return launch_code_product<Shape<int8_t, 256, 256, 2, 4, true, true>, O, SLOTS>(g, s);
+  if (long_leaves(g, g.d_out, 128)) return launch_code_product<Shape<int8_t, 256, 128, 4, 2, true, false, 3>, O, SLOTS>(g, s);
+  return launch_code_product<Shape<int8_t, 128, 128, 2, 2, true, true>, O, SLOTS>(g, s);
+}
+
+template <typename O, bool LISTED>
+int code_few(const CodeArgs& g, int64_t rows, hipStream_t s) {
+  if (rows * g.d_out <= 1024) {
+    gbdt_code::code_few_kernel<O, 1, LISTED><<<dim3(g.d_out, (unsigned)rows), dim3(64), 0, s>>>(g);
+  } else {
+    gbdt_code::code_few_kernel<O, 2, LISTED><<<dim3((unsigned)ceil_div(g.d_out, 2), (unsigned)rows), dim3(64), 0, s>>>(g);
+  }
+  LAUNCHED("code_few_kernel");
+  return GBDT_OK;
+}
+
+template <typename O>
+int leaf_codes(CodeArgs& g, hipStream_t s) {
+  if (few_rows(g.n_positions, 1, g.d_out)) return code_few<O, true>(g, g.n_positions, s);
+  return code_tiles<O, false>(g, s);
+}
+
+template <typename O>
+int mixture_codes(CodeArgs& g, int64_t n_rows, hipStream_t s) {
+  if (few_rows(n_rows, g.k, g.d_out)) return code_few<O, false>(g, n_rows, s);
+  const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out);
+  void* ws = nullptr;
+  const int rc = gbdt_internal::workspace(plan.bytes(), s, &ws);
+  if (rc != GBDT_OK) return rc;
+  CombineArgs<O> to = {};
+  to.gates = g.gates;
+  to.out = (O*)g.out;
+  to.ld_out = g.ld_out;
+  return by_slots<int8_t>(g, n_rows, g.d_out, to, plan, (char*)ws,
+                          [&](CodeArgs& piece, const int8_t* x, int64_t r) {
+                            piece.x = x;
+                            piece.row_scales += r;
+                            return code_tiles<float, true>(piece, s);
+                          },
+                          s, g.x, g.ld_x, false);
+}
+
+}  // namespace
+
+using namespace gbdt_host;
+
+extern "C" {
+
+int gbdt_route(const void* logits, int64_t ld, const float* choice_bias, int64_t n_rows, int32_t n_leaves, int32_t dtype, int32_t score,
+               int32_t n_groups, int32_t groups_kept, int32_t group_best, int32_t k, int32_t renormalise, float scale, int32_t* leaves_out,
+               float* gates_out, void* stream) {
+  const int rc = route_check(logits, ld, n_rows, n_leaves, dtype, score, k, scale);
+  if (n_groups <= 0 || groups_kept <= 0 || groups_kept > n_groups || (group_best != 1 && group_best != 2)) return GBDT_EINVAL;
+  if (rc != GBDT_OK) return rc;
+  if (n_leaves % n_groups != 0 || (int64_t)k > (int64_t)n_leaves / n_groups * groups_kept) return GBDT_EINVAL;
+  if (((uintptr_t)choice_bias & 3) != 0 || ((uintptr_t)leaves_out & 3) != 0 || ((uintptr_t)gates_out & 3) != 0) return GBDT_EINVAL;
+  if (n_groups > gbdt_router::kMaxGroups) return GBDT_EUNSUPPORTED;
+  if (n_rows == 0) return GBDT_OK;
+  if (!logits || !leaves_out || !gates_out) return GBDT_EINVAL;
+  RouteArgs g = {};
+  g.logits = logits;
+  g.bias = choice_bias;
+  g.leaves = leaves_out;
+  g.gates = gates_out;
+  g.ld = ld;
+  g.n_rows = (int32_t)n_rows;
+  g.n_leaves = n_leaves;
+  g.k = k;
+  g.n_groups = n_groups;
+  g.groups_kept = groups_kept;
+  g.group_best = n_groups > 1 ? group_best : 1;
+  g.group_size = n_leaves / n_groups;
+  g.sigmoid = score == GBDT_SIGMOID;
+  g.renormalise = renormalise != 0;
+  g.scale = scale;
+  hipStream_t s = (hipStream_t)stream;
+  return dtype == GBDT_F32 ? route<float>(g, false, s) : route<bf16>(g, false, s);
+}
+
+int gbdt_route_grad(const void* logits, int64_t ld, const int32_t* leaves, const float* dgates, int64_t n_rows, int32_t n_leaves,
+                    int32_t dtype, int32_t score, int32_t k, int32_t renormalise, float scale, void* dlogits_out, int64_t ld_out,
+                    void* stream) {
+  const int rc = route_check(logits, ld, n_rows, n_leaves, dtype, score, k, scale);
+  if (rc != GBDT_OK) return rc;
+  if (ld_out < n_leaves || off_element(dlogits_out, dtype) || ((uintptr_t)leaves & 3) != 0 || ((uintptr_t)dgates & 3) != 0) return GBDT_EINVAL;
+  if (ld_out >= kMaxLd) return GBDT_EUNSUPPORTED;
+  if (n_rows == 0) return GBDT_OK;
+  if (!logits || !leaves || !dgates || !dlogits_out) return GBDT_EINVAL;
+  RouteArgs g = {};
+  g.logits = logits;
+  g.leaves = const_cast<int32_t*>(leaves);
+  g.dgates = dgates;
+  g.dlogits = dlogits_out;
+  g.ld = ld;
+  g.ld_out = ld_out;
+  g.n_rows = (int32_t)n_rows;
+  g.n_leaves = n_leaves;
+  g.k = k;
+  g.sigmoid = score == GBDT_SIGMOID;
+  g.renormalise = renormalise != 0;
+  g.scale = scale;
+  hipStream_t s = (hipStream_t)stream;
+  return dtype == GBDT_F32 ? route<float>(g, true, s) : route<bf16>(g, true, s);
+}
+
+size_t gbdt_mixture_workspace_bytes(int64_t n_rows, int32_t k, int32_t n_leaves, int32_t d_in, int32_t d_out, int32_t dtype) {
+  if (n_rows < 0 || k <= 0 || n_leaves <= 0 || d_in <= 0 || d_out <= 0 || (dtype != GBDT_F32 && dtype != GBDT_BF16)) return 0;
+  if (mixture_check(n_rows, k, n_leaves, d_in, d_out, (const void*)4, (const void*)4, dtype) != GBDT_OK) return 0;
+  const int64_t e = dtype == GBDT_F32 ? 4 : 2, units = gbdt_internal::cu_count();
+  size_t most = 0;
+  for (int64_t cols : {d_in, d_out}) most = std::max(most, slot_plan(n_rows, k, n_leaves, cols).bytes());
+  for (int64_t inputs : {(int64_t)d_in, 16 / e}) most = std::max(most, weight_plan(n_rows, k, n_leaves, inputs, d_out, e, units).bytes());
+  return gbdt_internal::workspace_head_bytes() + most;
+}
+
+int gbdt_mixture_product(const void* x, int64_t ld_x, const void* weight, const void* bias, const int32_t* leaves, const float* gates,
+                         int64_t n_rows, int32_t k, int32_t n_leaves, int32_t d_in, int32_t d_out, int32_t dtype, void* y_out, int64_t ld_y,
+                         void* stream) {
+  const int rc = mixture_check(n_rows, k, n_leaves, d_in, d_out, leaves, gates, dtype);
+  if (rc != GBDT_OK) return rc;
+  if (ld_x < d_in || ld_y < d_out || !weight || off_element(x, dtype) || off_element(weight, dtype) || off_element(bias, dtype) ||
+      off_element(y_out, dtype))
+    return GBDT_EINVAL;
+  if (ld_x >= kMaxLd || ld_y >= kMaxLd) return GBDT_EUNSUPPORTED;
+  if (n_rows == 0) return GBDT_OK;
+  if (!x || !y_out) return GBDT_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  return dtype == GBDT_F32
+             ? mixture_call<float>(x, ld_x, weight, bias, leaves, gates, n_rows, k, n_leaves, d_in, d_out, y_out, ld_y, s)
+             : mixture_call<bf16>(x, ld_x, weight, bias, leaves, gates, n_rows, k, n_leaves, d_in, d_out, y_out, ld_y, s);
+}
+
+int gbdt_mixture_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, const void* weight, const void* bias,
+                              const int32_t* leaves, const float* gates, int64_t n_rows, int32_t k, int32_t n_leaves, int32_t d_in,
+                              int32_t d_out, int32_t dtype, void* dx_out, int64_t ld_dx, void* dweight_out, void* dbias_out,
+                              float* dgates_out, void* stream) {
+  const int rc = mixture_check(n_rows, k, n_leaves, d_in, d_out, leaves, gates, dtype);
+  if (rc != GBDT_OK) return rc;
+  const bool reads_x = dweight_out || dgates_out, reads_w = dx_out || dgates_out;
+  if (ld_dy < d_out || (reads_x && ld_x < d_in) || (dx_out && ld_dx < d_in) || (reads_w && !weight)) return GBDT_EINVAL;
+  if (off_element(dy, dtype) || off_element(x, dtype) || off_element(weight, dtype) || off_element(bias, dtype) ||
+      off_element(dx_out, dtype) || off_element(dweight_out, dtype) || off_element(dbias_out, dtype) || ((uintptr_t)dgates_out & 3) != 0)
+    return GBDT_EINVAL;
+  if (ld_dy >= kMaxLd || ld_x >= kMaxLd || ld_dx >= kMaxLd) return GBDT_EUNSUPPORTED;
+  if (n_rows > 0 && (!dy || (reads_x && !x))) return GBDT_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  return dtype == GBDT_F32 ? mixture_grad_call<float>(dy, ld_dy, x, ld_x, weight, bias, leaves, gates, n_rows, k, n_leaves, d_in, d_out,
+                                                      dx_out, ld_dx, dweight_out, dbias_out, dgates_out, s)
+                           : mixture_grad_call<bf16>(dy, ld_dy, x, ld_x, weight, bias, leaves, gates, n_rows, k, n_leaves, d_in, d_out,
+                                                     dx_out, ld_dx, dweight_out, dbias_out, dgates_out, s);
+}
+
+int gbdt_rows_quantize(const void* x, int64_t ld_x, int64_t n_rows, int32_t n_cols, int32_t dtype, int8_t* codes_out, int64_t ld_codes,
+                       float* scales_out, void* stream) {
+  if (n_rows < 0 || n_cols <= 0 || ld_x < n_cols || (dtype != GBDT_F32 && dtype != GBDT_BF16)) return GBDT_EINVAL;
+  const int64_t padded = round_up(n_cols, 16);
+  if (ld_codes < padded || ld_codes % 16 != 0 || ((uintptr_t)codes_out & 15) != 0 || ((uintptr_t)scales_out & 3) != 0 || off_element(x, dtype))
+    return GBDT_EINVAL;
+  if (n_rows >= kMaxRows || n_cols >= kMaxWidth || ld_x >= kMaxLd || ld_codes >= kMaxLd) return GBDT_EUNSUPPORTED;
+  if (n_rows == 0) return GBDT_OK;
+  if (!x || !codes_out || !scales_out) return GBDT_EINVAL;
+  const gbdt_code::QuantizeArgs g = {x, codes_out, scales_out, ld_x, ld_codes, n_rows, n_cols, (int32_t)padded};
+  hipStream_t s = (hipStream_t)stream;
+  return dtype == GBDT_F32 ? quantize<float>(g, s) : quantize<bf16>(g, s);
+}
+
+int gbdt_leaf_product_codes(const int8_t* codes, int64_t ld_codes, const float* scales, const int8_t* weight, const float* weight_scales,
+                         const float* bias, const int32_t* row_idx, const int64_t* leaf_offsets, int64_t n_positions, int32_t n_leaves,
+                         int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype, void* y_out, int64_t ld_y, void* stream) {
+  if (n_positions < 0 || n_leaves <= 0 || n_rows < 0 || d_in <= 0 || d_out <= 0 || !leaf_offsets) return GBDT_EINVAL;
+  if (((uintptr_t)leaf_offsets & 7) != 0 || ((uintptr_t)row_idx & 3) != 0) return GBDT_EINVAL;
+  if (dtype != GBDT_F32 && dtype != GBDT_BF16) return GBDT_EINVAL;
+  if (!row_idx && n_positions > n_rows) return GBDT_EINVAL;
+  if (n_positions >= kMaxRows || n_rows >= kMaxRows || n_leaves >= kMaxWidth || d_in >= kMaxWidth || d_out >= kMaxWidth)
+    return GBDT_EUNSUPPORTED;
+  if (n_rows == 0) n_positions = 0;
+  const int rc = code_check(codes, ld_codes, scales, weight, weight_scales, bias, n_positions, d_in, d_out, dtype, y_out, ld_y);
+  if (rc != GBDT_OK || n_positions == 0) return rc;
+  CodeArgs g = {};
+  g.x = codes;
+  g.w = weight;
+  g.row_idx = row_idx;
+  g.offsets = leaf_offsets;
+  g.row_scales = scales;
+  g.col_scales = weight_scales;
+  g.add = bias;
+  g.out = y_out;
+  g.ld_x = ld_codes;
+  g.ld_out = ld_y;
+  g.n_positions = (int32_t)n_positions;
+  g.n_leaves = n_leaves;
+  g.n_rows = (int32_t)n_rows;
+  g.d_in = (int32_t)round_up(d_in, 16);
+  g.d_out = d_out;
+  hipStream_t s = (hipStream_t)stream;
+  return dtype == GBDT_F32 ? leaf_codes<float>(g, s) : leaf_codes<bf16>(g, s);
+}
+
+int gbdt_mixture_product_codes(const int8_t* codes, int64_t ld_codes, const float* scales, const int8_t* weight, const float* weight_scales,
+                            const float* bias, const int32_t* leaves, const float* gates, int64_t n_rows, int32_t k, int32_t n_leaves,
+                            int32_t d_in, int32_t d_out, int32_t dtype, void* y_out, int64_t ld_y, void* stream) {
+  int rc = mixture_check(n_rows, k, n_leaves, d_in, d_out, leaves, gates, dtype);
+  if (rc != GBDT_OK) return rc;
+  rc = code_check(codes, ld_codes, scales, weight, weight_scales, bias, n_rows, d_in, d_out, dtype, y_out, ld_y);
+  if (rc != GBDT_OK || n_rows == 0) return rc;
+  CodeArgs g = {};
+  g.x = codes;
+  g.w = weight;
+  g.leaves = leaves;
+  g.gates = gates;
+  g.row_scales = scales;
+  g.col_scales = weight_scales;
+  g.add = bias;
+  g.out = y_out;
+  g.ld_x = ld_codes;
+  g.ld_out = ld_y;
+  g.n_leaves = n_leaves;
+  g.d_in = (int32_t)round_up(d_in, 16);
+  g.d_out = d_out;
+  g.k = k;
+  hipStream_t s = (hipStream_t)stream;
+  return dtype == GBDT_F32 ? mixture_codes<float>(g, n_rows, s) : mixture_codes<bf16>(g, n_rows, s);
+}
+
+}  // extern "C"

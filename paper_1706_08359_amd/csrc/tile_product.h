@@ -22,7 +22,8 @@
 //   row, and masked on its way to the stage; only where that would pass the matrix's end is it read value by value, behind
 //   the other loads (a branch among them made every load wait for the one before: 63 leaves of 50,021 x 137 f32, gradient of
 //   weights of 33 outputs, 159 us so).
-// Products of bf16 values are exact in f32 and sums are f32 throughout; f32 operands use the f32 matrix instruction.
+// Products of bf16 values are exact in f32 and sums are f32 throughout; f32 operands use the f32 matrix instruction; products of
+// 8-bit integers and their sums are exact in 32 bits (row operands and DIRECT only: rows of codes are whole chunks).
 // Measured in the kernels that use it: 256 x 256 tiles of bf16 1.2 PFLOP/s with a long k (dC of 65,536 classes x 1,024 over 8,192
 // rows), where a large library product reached 1.2 to 1.6 on the same card; f32, whose matrix instructions are the bound, 58 to
 // 63 TFLOP/s where rows of 137 values end inside tiles of 64, of 153.  Reads of the stages meet no bank
@@ -40,14 +41,21 @@ typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
-
+// A fragment is 16 bytes of k; Acc holds four sums.
 template <typename T> struct Traits;
 template <> struct Traits<bf16> {
   typedef bf16x8 Frag;
+  typedef f32x4 Acc;
 };
 template <> struct Traits<float> {
   typedef f32x4 Frag;
+  typedef f32x4 Acc;
+};
+template <> struct Traits<int8_t> {
+  typedef i32x4 Frag;
+  typedef i32x4 Acc;
 };
 template <typename T> constexpr int kChunk = 16 / (int)sizeof(T);       // values a chunk
 
@@ -437,6 +445,11 @@ __device__ __forceinline__ f32x4 mma(f32x4 rows, f32x4 cols, f32x4 acc) {
   return acc;
 }
 
+// 16 codes each: exact sums in 32 bits.
+__device__ __forceinline__ i32x4 mma(i32x4 rows, i32x4 cols, i32x4 acc) {
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(rows, cols, acc, 0, 0, 0);
+}
+
 // ---------------------------------------------------------------- the tile
 
 // BM x BN values by WM x WN wavefronts.  A lane's four values of the 16 x 16 block (i, j) of its wavefront:
@@ -447,6 +460,7 @@ __device__ __forceinline__ f32x4 mma(f32x4 rows, f32x4 cols, f32x4 acc) {
 template <typename T_, int BM_, int BN_, int WM_, int WN_, bool DIRECT_, bool DEEP_ = false, int STAGES_ = 2, bool PARTS_ = false>
 struct Shape {
   typedef T_ T;
+  typedef typename Traits<T_>::Acc Acc;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NT = WM_ * WN_ * 64;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
   static constexpr bool DIRECT = DIRECT_, DEEP = DEEP_, PARTS = PARTS_ || sizeof(T_) == 4;
@@ -456,6 +470,7 @@ struct Shape {
   static constexpr int kLastStage = (kStages - 1) * kStageBytes;
   static_assert(TM >= 1 && TN >= 1 && BM % (WM * 16) == 0 && BN % (WN * 16) == 0, "whole 16 x 16 blocks");
   static_assert(DIRECT || (!DEEP && kStages == 2), "");
+  static_assert(!DEEP || TM >= 4, "a turn's chunks are asked for between its row blocks, but for the last two");
   typedef RowOperand<T, BM, NT, DIRECT, KB> RowsA;
   typedef RowOperand<T, BN, NT, DIRECT, KB> RowsB;
   typedef ColumnOperand<T, BM, NT, DIRECT, KB> ColumnsA;
@@ -515,18 +530,20 @@ __device__ __forceinline__ void tile_begin(char* lds, A& a, B& b, const RowsA& r
 }
 
 template <class S>
-__device__ __forceinline__ void zeros(f32x4 (&acc)[S::TM][S::TN]) {
+__device__ __forceinline__ void zeros(typename S::Acc (&acc)[S::TM][S::TN]) {
 #pragma unroll
   for (int i = 0; i < S::TM; ++i)
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < S::TN; ++j) acc[i][j] = typename S::Acc{0, 0, 0, 0};
 }
 
 // Adds the products of k0 <= k < k1 to acc.
 template <class S, bool N_INNER, class A, class B, class RowsA, class RowsB, class Also>
 __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& rows_a, const RowsB& rows_b, int k0, int k1,
-                                         f32x4 (&acc)[S::TM][S::TN], const Also& also) {
+                                         typename S::Acc (&acc)[S::TM][S::TN], const Also& also) {
   typedef typename Traits<typename S::T>::Frag Frag;
+  // (with more stages than two a wait counts loads, and every wavefront must have asked for as many)
+  static_assert(S::kStages == 2 || (A::kSlots % S::NT == 0 && B::kSlots % S::NT == 0), "every thread has as many chunks");
   const int w = thread_of<S::NT>() >> 6;
   const int m0 = (w / S::WN) * (S::TM * 16), n0 = (w % S::WN) * (S::TN * 16);
   const int steps = (k1 - k0 + S::kStep - 1) / S::kStep;
@@ -548,11 +565,11 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
   // three times the error of a product summed in parts without it.)  bf16 ones are added 32 k at a time, and only what ends in
   // f32, the columns of statistics, is worth the registers.
   constexpr bool kParts = S::PARTS;
-  f32x4 part_sum[kParts ? S::TM : 1][kParts ? S::TN : 1];
+  typename S::Acc part_sum[kParts ? S::TM : 1][kParts ? S::TN : 1];
   auto multiply = [&](int i, int slot, int turn) {
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) {
-      f32x4& to = kParts ? part_sum[kParts ? i : 0][kParts ? j : 0] : acc[i][j];
+      typename S::Acc& to = kParts ? part_sum[kParts ? i : 0][kParts ? j : 0] : acc[i][j];
       to = N_INNER ? mma(fb[turn][j], fa[slot & 3], to) : mma(fa[slot & 3], fb[turn][j], to);
     }
     also(i, fa[slot & 3]);
@@ -565,7 +582,7 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
 #pragma unroll
         for (int j = 0; j < S::TN; ++j) {
           acc[i][j] += part_sum[i][j];
-          part_sum[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          part_sum[i][j] = typename S::Acc{0, 0, 0, 0};
         }
     }
   };
@@ -736,7 +753,7 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
 
 template <class S, bool N_INNER, class A, class B, class RowsA, class RowsB, class Also>
 __device__ __forceinline__ void tile_product(char* lds, A& a, B& b, const RowsA& rows_a, const RowsB& rows_b, int k0, int k1,
-                                             f32x4 (&acc)[S::TM][S::TN], const Also& also) {
+                                             typename S::Acc (&acc)[S::TM][S::TN], const Also& also) {
   zeros<S>(acc);
   tile_begin<S>(lds, a, b, rows_a, rows_b, k0, k1);
   tile_run<S, N_INNER>(lds, a, b, rows_a, rows_b, k0, k1, acc, also);
