@@ -109,31 +109,48 @@ __global__ void __launch_bounds__(256) quantize_kernel(const QuantizeArgs g) {
 
 // ---------------------------------------------------------------- products
 
-// To rows of y, or (SLOTS) to the pairs' slots.
-template <typename O, bool SLOTS>
+// Where the results go: to the row of y (kRow), weighed to the row of y (kGatedRow: k = 1), or to the pair's slot.
+enum class Place { kRow, kGatedRow, kSlot };
+
+template <typename O, Place WHERE>
 struct ToScaled {
-  typedef O Out;
-  static constexpr bool kScaled = true;
-  O* out;
+  typedef typename std::conditional<WHERE == Place::kSlot, typename SlotOf<O>::Type, O>::type Out;
+  static constexpr bool kScaled = true, kHalves = WHERE == Place::kSlot && sizeof(Out) == 2;
+  static constexpr bool kFinished = kHalves || WHERE == Place::kGatedRow;
+  Out* out;
   int64_t ld;
   const float* row_scales;
   const float* col_scales;
   const float* bias;
   __device__ __forceinline__ int row(const CodeArgs& g, int p) const { return g.row_idx ? g.row_idx[p] : p; }
   __device__ __forceinline__ int place(const CodeArgs& g, int p) const {
-    if (SLOTS) return g.pair_idx[p];
+    if (WHERE != Place::kRow) return g.pair_idx[p];
     const int d = row(g, p);
     return (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
   }
   __device__ __forceinline__ float row_scale(const CodeArgs& g, int p) const { return row_scales[row(g, p)]; }
   __device__ __forceinline__ float column_scale(int64_t column) const { return col_scales[column]; }
   __device__ __forceinline__ float add(int64_t column) const { return bias ? bias[column] : 0.0f; }
+  template <int TN>
+  __device__ __forceinline__ void finish(const CodeArgs& g, int, int pair, int col, int cols, f32x4 (&v)[TN]) const {
+    if constexpr (WHERE == Place::kGatedRow) {
+      const float gate = pair >= 0 ? g.gates[pair] : 0.0f;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) v[j] *= gate;
+    } else {
+      static_assert(TN * 16 == block_columns<int8_t>, "a wavefront's columns");
+      const float unit = to_units<TN>(v);
+      if ((threadIdx.x & 63) < 16 && pair >= 0 && col < cols) g.units[(int64_t)pair * g.blocks + col / (TN * 16)] = unit;
+    }
+  }
 };
 
-template <class S, typename O, bool SLOTS>
+template <class S, typename O, Place WHERE>
 __global__ void __launch_bounds__(S::NT, 2) code_product_kernel(const CodeArgs g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  const ToScaled<O, SLOTS> to = {SLOTS ? (O*)g.slots : (O*)g.out, SLOTS ? g.ld_slots : g.ld_out, g.row_scales, g.col_scales, g.add};
+  typedef ToScaled<O, WHERE> To;
+  const bool slot = WHERE == Place::kSlot;
+  const To to = {(typename To::Out*)(slot ? g.slots : g.out), slot ? g.ld_slots : g.ld_out, g.row_scales, g.col_scales, g.add};
   leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, to, g.d_out);
 }
 

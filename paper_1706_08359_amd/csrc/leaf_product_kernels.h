@@ -124,7 +124,7 @@ __device__ __forceinline__ PlainRows<T> plain_rows(const T* base, int64_t ld, in
 template <typename T>
 struct ToRows {
   typedef T Out;
-  static constexpr bool kScaled = false;
+  static constexpr bool kScaled = false, kFinished = false;
   const T* bias;  // [n_leaves][cols] or null
   T* out;
   int64_t ld;
@@ -139,6 +139,7 @@ struct ToRows {
 // The rows of one tile of positions times a matrix of the leaf, g.cols_per column tiles one after another; the next one's
 // first steps are on their way while one's values are stored.  B: the matrix' orientation, k its length along k.
 // To::kScaled: values are multiplied by a factor of their position and one of the leaf's column.
+// To::kFinished: a row's values of this wavefront's columns go through to.finish before they are stored.
 // GROUPS > 1: as many times the tile's threads take a part of k each, all of as many steps, and the first adds up; one column
 // tile a workgroup then, since the other groups leave after it.
 template <class S, class B, int GROUPS, typename T, class G, class To>
@@ -208,21 +209,39 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T
         add[j][r] = n < cols ? to.add((int64_t)leaf * cols + n) : 0.0f;
         if constexpr (To::kScaled) scale[j][r] = n < cols ? to.column_scale((int64_t)leaf * cols + n) : 0.0f;
       }
+    auto value = [&](int i, int j) {
+      if constexpr (To::kScaled) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = __builtin_fmaf((float)acc[i][j][r] * factor[i], scale[j][r], add[j][r]);
+        return v;
+      } else {
+        return acc[i][j] + add[j];
+      }
+    };
+    if constexpr (To::kFinished) {
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i) {
+        f32x4 v[S::TN];
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) v[j] = value(i, j);
+        to.template finish<S::TN>(g, m0 + 16 * i, ids[i], wave_col, cols, v);
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) acc[i][j] = __builtin_bit_cast(Acc, v[j]);
+      }
+    }
     store_tile<S, typename To::Out, S::TM, S::TN>(
         lds + S::kLastStage,
         [&](int i, int j) {
-          if constexpr (To::kScaled) {
-            f32x4 v;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = __builtin_fmaf((float)acc[i][j][r] * factor[i], scale[j][r], add[j][r]);
-            return v;
+          if constexpr (To::kFinished) {
+            return __builtin_bit_cast(f32x4, acc[i][j]);
           } else {
-            return acc[i][j] + add[j];
+            return value(i, j);
           }
         },
         [&](int i, int r) {
           const int d = __shfl(ids[i], r);
-          return d >= 0 ? to.out + (int64_t)d * to.ld : (typename To::Out*)nullptr;
+          return d >= 0 && to.out != nullptr ? to.out + (int64_t)d * to.ld : (typename To::Out*)nullptr;
         },
         wave_col, cols);
   }

@@ -1,9 +1,12 @@
 // Rows that several leaves answer with weights: y[d] = sum_j g[d][j] (W_l x[d] + b_l), l = leaves[d][j], and its gradients.
 //
 // A pair p = d * k + j is a row and one of its leaves.  Lists of pairs by leaf (route_kernels.h) make each product that of
-// leaf_product_kernels.h, whose results go to a slot of f32 values for every pair; a second kernel weighs and adds up a row's slots
-// in order.  So nothing is added from several workgroups to one place, the same call gives the same bits, and the result is rounded
-// once.
+// leaf_product_kernels.h, whose results go to a slot for every pair; a second kernel weighs and adds up a row's slots in order.  So
+// nothing is added from several workgroups to one place, the same call gives the same bits, and sums are f32.
+//
+// Slots of f32 results hold f32; those of bf16 results hold 11 bits, as fp16 values with a power of two for every pair and 64
+// columns: half the bytes, and an eighth of the error that rounding the result has anyway (8,192 rows x 8 leaves, 1,024 -> 1,024: products
+// 202 us with f32 slots, their sums 85).
 #pragma once
 
 #include "leaf_product_kernels.h"
@@ -12,62 +15,56 @@ namespace gbdt_routed {
 
 using namespace gbdt_leaf;
 
+typedef _Float16 f16;
+
 template <typename T>
 struct RoutedArgs : LeafArgs<T> {
   const int32_t* pair_idx;  // of the list's positions
   const int32_t* leaves;    // [n_rows][k]
   const float* gates;       // [n_rows][k]
-  float* slots;             // [n_rows * k][ld_slots]
   float* dgates;            // [n_rows][k] or null
-  int64_t ld_slots;         // a multiple of 4
-  int32_t k;
+  void* slots;              // [n_rows * k][ld_slots] or null
+  float* units;             // fp16 slots: [n_rows * k][blocks], the powers of two
+  float* dots;              // gradient: [n_rows * k][blocks], parts of <u, x>, or null
+  int64_t ld_slots;         // a multiple of 16 bytes
+  int32_t k, blocks;        // blocks of block_columns columns
 };
+
+// What results of type O are kept in until a row's are added up, and the columns of a wavefront in the tiles that make them.
+template <typename O> struct SlotOf;
+template <> struct SlotOf<bf16> { typedef f16 Type; };
+template <> struct SlotOf<float> { typedef float Type; };
+template <typename T> constexpr int block_columns = sizeof(T) == 4 ? 32 : 64;  // T: the operands'
 
 // ---------------------------------------------------------------- products to slots
 
-template <typename T>
-struct ToSlots {
-  typedef float Out;
-  static constexpr bool kScaled = false;
-  const T* bias;
-  float* out;
-  int64_t ld;
-  __device__ __forceinline__ int place(const RoutedArgs<T>& g, int p) const { return g.pair_idx[p]; }
-  __device__ __forceinline__ float add(int64_t column) const { return bias ? (float)bias[column] : 0.0f; }
-};
-
-template <class S>
-__global__ void __launch_bounds__(S::NT, 2) routed_product_kernel(const RoutedArgs<typename S::T> g) {
-  __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, ToSlots<typename S::T>{g.bias, g.slots, g.ld_slots}, g.d_out);
+__device__ __forceinline__ float over_groups(float v, bool max) {  // over the four groups of 16 lanes
+#pragma unroll
+  for (int m = 16; m < 64; m <<= 1) {
+    const float other = __shfl_xor(v, m);
+    v = max ? fmaxf(v, other) : v + other;
+  }
+  return v;
 }
 
-template <class S>
-__global__ void __launch_bounds__(S::NT, 2) routed_grad_input_kernel(const RoutedArgs<typename S::T> g) {
-  __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::ColumnsB, 1>(lds, g, g.dy, g.ld_dy, g.d_out, ToSlots<typename S::T>{nullptr, g.slots, g.ld_slots}, g.d_in);
+// Divides a row's values (4 TN of them a lane, 16 TN in all) by a power of two that brings the largest finite one to 2^14 .. 2^15, and
+// returns that power.  Infinities and NaN stay what they are, in their places.
+template <int TN>
+__device__ __forceinline__ float to_units(f32x4 (&v)[TN]) {
+  float most = 0.0f;
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(v[j][r]) < INFINITY ? fabsf(v[j][r]) : 0.0f);
+  most = over_groups(most, true);
+  const int e = (int)(__float_as_uint(most) >> 23), exponent = e < 15 ? 15 : e;
+  const float by = __uint_as_float((uint32_t)(268 - exponent) << 23);
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[j][r] *= by;
+  return __uint_as_float((uint32_t)(exponent - 14) << 23);
 }
-
-// ---------------------------------------------------------------- sums of slots
-
-template <typename O>
-struct CombineArgs {
-  const float* slots;     // [n_rows * k][ld]
-  const int32_t* leaves;  // [n_rows][k]; a slot whose leaf is none holds anything
-  const float* gates;     // [n_rows][k]
-  O* out;                 // [n_rows][cols] or null
-  int64_t ld, ld_out;
-  int32_t n_rows, n_leaves, k, cols;
-  // gradient
-  const O* x;             // [n_rows][cols]
-  const O* dy;            // [n_rows][d_out]
-  const O* bias;          // [n_leaves][d_out] or null
-  float* dgates;          // [n_rows][k]
-  int64_t ld_x, ld_dy;
-  int32_t d_out;
-};
-
-__device__ __forceinline__ f32x4 load4(const float* p) { return *(const f32x4*)p; }
 
 // Up to four values of any alignment, zeros behind.
 template <typename T>
@@ -86,97 +83,204 @@ __device__ __forceinline__ f32x4 load4_any(const T* p, int valid) {
   return v;
 }
 
-__device__ __forceinline__ void add_scaled(f32x4& sum, float by, f32x4 v) {
+// To the pairs' slots, of type H.  DOTS: each row's values also meet x's, and their sums over the wavefront's columns are left in
+// dots: dg[d][j] = <dy, W x + b> = <W^T dy, x> + <dy, b>, so the gates' gradient needs the answers of neither pass, only f32 values
+// that are in registers here.
+template <typename T, typename H, bool DOTS>
+struct ToSlots {
+  typedef H Out;
+  static constexpr bool kScaled = false, kHalves = sizeof(H) == 2, kFinished = kHalves || DOTS;
+  const T* bias;
+  H* out;
+  int64_t ld;
+  __device__ __forceinline__ int place(const RoutedArgs<T>& g, int p) const { return g.pair_idx[p]; }
+  __device__ __forceinline__ float add(int64_t column) const { return bias ? (float)bias[column] : 0.0f; }
+  template <int TN>
+  __device__ __forceinline__ void finish(const RoutedArgs<T>& g, int p, int pair, int col, int cols, f32x4 (&v)[TN]) const {
+    static_assert(TN * 16 == block_columns<T>, "a wavefront's columns");
+    const int l = threadIdx.x & 63;
+    const int64_t block = (int64_t)pair * g.blocks + col / (TN * 16);
+    if constexpr (DOTS) {
+      float dot = 0.0f;
+      if (pair >= 0) {
+        const T* x = row_of(g.x, g.row_idx[p], g.ld_x);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(by, v[i], sum[i]);
+        for (int j = 0; j < TN; ++j) {
+          const int n = col + 16 * j + 4 * (l >> 4);
+          const f32x4 xs = n < cols ? load4_any(x + n, cols - n) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int r = 0; r < 4; ++r) dot = n + r < cols ? __builtin_fmaf(v[j][r], xs[r], dot) : dot;
+        }
+      }
+      dot = over_groups(dot, false);
+      if (l < 16 && pair >= 0 && col < cols) g.dots[block] = dot;
+    }
+    if constexpr (kHalves) {
+      const float unit = to_units<TN>(v);
+      if (l < 16 && pair >= 0 && col < cols) g.units[block] = unit;
+    }
+  }
+};
+
+// k = 1: a row's only answer, weighed, is the result.
+template <typename T>
+struct ToGatedRows {
+  typedef T Out;
+  static constexpr bool kScaled = false, kFinished = true;
+  const T* bias;
+  T* out;
+  int64_t ld;
+  __device__ __forceinline__ int place(const RoutedArgs<T>& g, int p) const { return g.pair_idx[p]; }
+  __device__ __forceinline__ float add(int64_t column) const { return bias ? (float)bias[column] : 0.0f; }
+  template <int TN>
+  __device__ __forceinline__ void finish(const RoutedArgs<T>& g, int, int pair, int, int, f32x4 (&v)[TN]) const {
+    const float gate = pair >= 0 ? g.gates[pair] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) v[j] *= gate;
+  }
+};
+
+// What a product over pairs leaves: slots; answers to rows of one leaf each; slots and dots of the gradient; dots alone come of that
+// with null slots.
+enum class Leaves { kSlots, kRows };
+
+template <class S, Leaves WHAT>
+__global__ void __launch_bounds__(S::NT, 2) routed_product_kernel(const RoutedArgs<typename S::T> g) {
+  typedef typename S::T T;
+  typedef typename SlotOf<T>::Type H;
+  __shared__ __align__(16) char lds[S::kLdsBytes];
+  if constexpr (WHAT == Leaves::kRows) {
+    leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, ToGatedRows<T>{g.bias, g.y, g.ld_y}, g.d_out);
+  } else {
+    leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, ToSlots<T, H, false>{g.bias, (H*)g.slots, g.ld_slots}, g.d_out);
+  }
 }
 
-// The weighted sum of a row's slots for four columns.
+template <class S, bool DOTS>
+__global__ void __launch_bounds__(S::NT, 2) routed_grad_input_kernel(const RoutedArgs<typename S::T> g) {
+  typedef typename S::T T;
+  typedef typename SlotOf<T>::Type H;
+  __shared__ __align__(16) char lds[S::kLdsBytes];
+  leaf_rows_product<S, typename S::ColumnsB, 1>(lds, g, g.dy, g.ld_dy, g.d_out, ToSlots<T, H, DOTS>{nullptr, (H*)g.slots, g.ld_slots}, g.d_in);
+}
+
+// ---------------------------------------------------------------- sums of slots
+
 template <typename O>
-__device__ __forceinline__ f32x4 weighted_sum(const CombineArgs<O>& g, int64_t d, int c) {
-  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-  const int64_t p0 = d * g.k;
-#pragma unroll 4
-  for (int j = 0; j < g.k; ++j)
-    if ((uint32_t)g.leaves[p0 + j] < (uint32_t)g.n_leaves) add_scaled(sum, g.gates[p0 + j], load4(g.slots + (p0 + j) * g.ld + c));
-  return sum;
-}
+struct CombineArgs {
+  const void* slots;      // [n_rows * k][ld]; a slot whose leaf is none holds anything
+  const float* units;     // [n_rows * k][blocks]
+  const int32_t* leaves;  // [n_rows][k]
+  const float* gates;     // [n_rows][k]
+  O* out;                 // [n_rows][cols] or null
+  int64_t ld, ld_out;
+  int32_t n_rows, n_leaves, k, cols, blocks;
+  // gradient of the gates
+  const float* dots;      // [n_rows * k][blocks]
+  const O* dy;            // [n_rows][d_out]
+  const O* bias;          // [n_leaves][d_out] or null
+  float* dgates;          // [n_rows][k] or null
+  int64_t ld_dy;
+  int32_t d_out;
+};
 
-// LANES lanes a row, four columns each at a time.
-template <typename O, int LANES>
-__global__ void __launch_bounds__(256) combine_kernel(const CombineArgs<O> g) {
-  const int64_t d = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (d >= g.n_rows) return;
-  for (int c = (int)(threadIdx.x & (LANES - 1)) * 4; c < g.cols; c += LANES * 4)
-    store4(g.out + d * g.ld_out + c, weighted_sum(g, d, c), g.cols - c);
-}
+template <int N>
+struct Values {
+  float v[N];
+};
 
-// dx[d] = sum_j g u_j and dg[d][j] = <u_j, x[d]> + <b_l, dy[d]>, u_j = W_l^T dy[d] in the row's slots: <W_l x, dy> is <x, W_l^T dy>, so
-// the answers need not be kept.  A wavefront a row; up to kAtOnce slots are read once for both.
-constexpr int kAtOnce = 8;
-__device__ __forceinline__ float wave_sum(float v) {
+// N = 16 bytes of a pair's values.
+template <typename H>
+__device__ __forceinline__ Values<16 / (int)sizeof(H)> chunk_of(const void* p) {
+  constexpr int n = 16 / (int)sizeof(H);
+  const u32x4 c = load16(p);
+  H h[n];
+  __builtin_memcpy(h, &c, 16);
+  Values<n> r;
 #pragma unroll
-  for (int s = 32; s > 0; s >>= 1) v += __shfl_xor(v, s);
+  for (int i = 0; i < n; ++i) r.v[i] = (float)h[i];
+  return r;
+}
+
+template <int LANES>
+__device__ __forceinline__ float over_row(float v) {
+#pragma unroll
+  for (int s = LANES / 2; s > 0; s >>= 1) v += __shfl_xor(v, s);
   return v;
 }
-template <typename O>
-__global__ void __launch_bounds__(256) combine_grad_kernel(const CombineArgs<O> g) {
-  const int64_t d = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int l = threadIdx.x & 63;
+
+// out[d] = sum_j g[d][j] slot_j, LANES lanes a row, 16 bytes of a slot each at a time, eight slots on their way; dgates[d][j] =
+// the sum of the pair's dots and <bias, dy>.  Bound by reading the slots.
+template <typename O, int LANES>
+__global__ void __launch_bounds__(256) combine_kernel(const CombineArgs<O> g) {
+  typedef typename SlotOf<O>::Type H;
+  constexpr int n = 16 / (int)sizeof(H), at_once = 8;
+  const int64_t d = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   if (d >= g.n_rows) return;
+  const int l = threadIdx.x & (LANES - 1);
   const int64_t p0 = d * g.k;
-  if (g.dgates != nullptr) {
-    const bool fused = g.k <= kAtOnce && g.out != nullptr;
-    for (int j0 = 0; j0 < g.k; j0 += kAtOnce) {
-      int leaf[kAtOnce];
-      float gate[kAtOnce], dot[kAtOnce];
+  if (g.out != nullptr) {
+    for (int c = l * n; c < g.cols; c += LANES * n) {
+      float sum[n];
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const int e = j0 + i < g.k ? g.leaves[p0 + j0 + i] : -1;
-        leaf[i] = (uint32_t)e < (uint32_t)g.n_leaves ? e : -1;
-        gate[i] = leaf[i] >= 0 ? g.gates[p0 + j0 + i] : 0.0f;
-        dot[i] = 0.0f;
-      }
-      for (int c = l * 4; c < g.cols; c += 256) {
-        const f32x4 x = load4_any(g.x + d * g.ld_x + c, g.cols - c);
-        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-        f32x4 u[kAtOnce];
+      for (int e = 0; e < n; ++e) sum[e] = 0.0f;
+      for (int j0 = 0; j0 < g.k; j0 += at_once) {
+        const void* from[at_once];
+        float gate[at_once];
+        Values<n> v[at_once];
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i)
-          if (leaf[i] >= 0) u[i] = load4(g.slots + (p0 + j0 + i) * g.ld + c);
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-          if (leaf[i] < 0) continue;
-          const int valid = g.cols - c;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) dot[i] = e < valid ? __builtin_fmaf(u[i][e], x[e], dot[i]) : dot[i];
-          add_scaled(sum, gate[i], u[i]);
+        for (int i = 0; i < at_once; ++i) {
+          const int64_t p = p0 + (j0 + i < g.k ? j0 + i : 0);
+          const bool there = j0 + i < g.k && (uint32_t)g.leaves[p] < (uint32_t)g.n_leaves;
+          from[i] = there ? (const void*)((const H*)g.slots + p * g.ld + c) : (const void*)zero_chunk;
+          gate[i] = there ? g.gates[p] : 0.0f;
+          if constexpr (sizeof(H) == 2) gate[i] = there ? gate[i] * g.units[p * g.blocks + c / 64] : 0.0f;
         }
-        if (fused) store4(g.out + d * g.ld_out + c, sum, g.cols - c);
+#pragma unroll
+        for (int i = 0; i < at_once; ++i) v[i] = chunk_of<H>(from[i]);
+#pragma unroll
+        for (int i = 0; i < at_once; ++i)
+#pragma unroll
+          for (int e = 0; e < n; ++e) sum[e] = __builtin_fmaf(gate[i], v[i].v[e], sum[e]);
       }
-      if (g.bias != nullptr) {
-        for (int c = l * 4; c < g.d_out; c += 256) {
-          const f32x4 dy = load4_any(g.dy + d * g.ld_dy + c, g.d_out - c);
+      O* to = g.out + d * g.ld_out + c;
+      O t[n];
 #pragma unroll
-          for (int i = 0; i < kAtOnce; ++i) {
-            if (leaf[i] < 0) continue;
-            const f32x4 b = load4_any(g.bias + (int64_t)leaf[i] * g.d_out + c, g.d_out - c);
+      for (int e = 0; e < n; ++e) t[e] = (O)sum[e];
+      if (c + n <= g.cols) {
+        __builtin_memcpy(to, t, sizeof t);
+      } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) dot[i] = __builtin_fmaf(b[e], dy[e], dot[i]);
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        if (j0 + i >= g.k) break;
-        const float all = wave_sum(dot[i]);
-        if (l == 0) g.dgates[p0 + j0 + i] = leaf[i] >= 0 ? all : 0.0f;
+        for (int e = 0; e < n; ++e)
+          if (c + e < g.cols) to[e] = t[e];
       }
     }
-    if (fused) return;
   }
-  if (g.out != nullptr)
-    for (int c = l * 4; c < g.cols; c += 256) store4(g.out + d * g.ld_out + c, weighted_sum(g, d, c), g.cols - c);
+  if (g.dgates == nullptr) return;
+  for (int j = 0; j < g.k; ++j) {
+    const int leaf = g.leaves[p0 + j];
+    const bool there = (uint32_t)leaf < (uint32_t)g.n_leaves;
+    float dot = 0.0f;
+    if (there) {
+      for (int b = l; b < g.blocks; b += LANES) dot += g.dots[(p0 + j) * g.blocks + b];
+      if (g.bias != nullptr)
+        for (int c = l * 4; c < g.d_out; c += LANES * 4) {
+          const f32x4 b = load4_any(g.bias + (int64_t)leaf * g.d_out + c, g.d_out - c), dy = load4_any(g.dy + d * g.ld_dy + c, g.d_out - c);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dot = __builtin_fmaf(b[e], dy[e], dot);
+        }
+    }
+    dot = over_row<LANES>(dot);
+    if (l == 0) g.dgates[p0 + j] = there ? dot : 0.0f;
+  }
+}
+
+// Zeros for the rows that no leaf answers, where answers go to rows directly (k = 1).
+template <typename O>
+__global__ void __launch_bounds__(256) clear_rows_kernel(const int32_t* leaves, int32_t n_leaves, int32_t n_rows, int32_t cols, O* out, int64_t ld) {
+  const int64_t d = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (d >= n_rows || (uint32_t)leaves[d] < (uint32_t)n_leaves) return;
+  for (int c = 0; c < cols; ++c) out[d * ld + c] = (O)0.0f;
 }
 
 // ---------------------------------------------------------------- gradients of the weights
@@ -262,7 +366,7 @@ __global__ void __launch_bounds__(64) routed_few_kernel(const RoutedArgs<T> g) {
       if (leaf[j] < 0) continue;
 #pragma unroll
       for (int i = 0; i < OUTPUTS; ++i) {
-        const float all = wave_sum(sum[j][i]);
+        const float all = over_row<64>(sum[j][i]);
         const float b = g.bias && o0 + i < g.d_out ? (float)g.bias[(int64_t)leaf[j] * g.d_out + o0 + i] : 0.0f;
         y[i] = __builtin_fmaf(gate[j], all + b, y[i]);
       }

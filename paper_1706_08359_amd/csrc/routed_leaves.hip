@@ -98,14 +98,22 @@ int launch_lists(const gbdt_router::ListArgs& g, hipStream_t s) {
   return GBDT_OK;
 }
 
-// Lists the pairs of n_rows rows in scratch of plan.bytes(), and says where.
+// Where a list lies in scratch of plan.bytes().
+void list_places(const ListPlan& plan, char* scratch, const int64_t** offsets, const int32_t** row, const int32_t** pair) {
+  *offsets = (int64_t*)scratch;
+  *row = (int32_t*)(scratch + plan.offsets_bytes);
+  *pair = (int32_t*)(scratch + plan.offsets_bytes + plan.row_bytes);
+}
+
+// Lists the pairs of the rows that `leaves` begins with, and says where.
 int make_lists(const ListPlan& plan, const int32_t* leaves, int32_t n_leaves, int32_t k, char* scratch, const int64_t** offsets,
                const int32_t** row, const int32_t** pair, hipStream_t s) {
+  list_places(plan, scratch, offsets, row, pair);
   gbdt_router::ListArgs g = {};
   g.leaves = leaves;
-  g.offsets = (int64_t*)scratch;
-  g.row = (int32_t*)(scratch + plan.offsets_bytes);
-  g.pair = (int32_t*)(scratch + plan.offsets_bytes + plan.row_bytes);
+  g.offsets = const_cast<int64_t*>(*offsets);
+  g.row = const_cast<int32_t*>(*row);
+  g.pair = const_cast<int32_t*>(*pair);
   g.counts = (int32_t*)(scratch + plan.offsets_bytes + 2 * plan.row_bytes);
   g.totals = g.counts + plan.table_bytes / 4;
   g.n_pairs = (int32_t)plan.pairs;
@@ -113,9 +121,6 @@ int make_lists(const ListPlan& plan, const int32_t* leaves, int32_t n_leaves, in
   g.k = k;
   g.run = (int32_t)plan.run;
   g.runs = (int32_t)plan.runs;
-  *offsets = g.offsets;
-  *row = g.row;
-  *pair = g.pair;
   if (plan.runs == 0) {
     gbdt_router::list_few_kernel<<<dim3(1), dim3(gbdt_router::kListWaves * 64), 0, s>>>(g);
     LAUNCHED("list_few_kernel");
@@ -134,18 +139,22 @@ constexpr int64_t kSlotsBytes = (int64_t)256 << 20;
 constexpr int64_t kGatedBytes = (int64_t)256 << 20;
 constexpr int32_t kMaxSlots = 64;  // leaves a row
 
+// e: bytes of a slot's value; block: columns that share a power of two or a part of a dot product.
 struct SlotPlan {
-  int64_t rows, ld;  // rows at a time
+  int64_t rows, ld, blocks;  // rows at a time
   ListPlan list;
-  size_t slots_bytes;
-  size_t bytes() const { return list.bytes() + slots_bytes; }
+  size_t slots_bytes, units_bytes, dots_bytes;
+  size_t bytes() const { return list.bytes() + slots_bytes + units_bytes + dots_bytes; }
 };
-SlotPlan slot_plan(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t cols) {
+SlotPlan slot_plan(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t cols, int64_t e, int64_t block, bool dots) {
   SlotPlan p;
-  p.ld = round_up(cols, 4);
-  p.rows = std::min(n_rows, std::max<int64_t>(1024, kSlotsBytes / (k * p.ld * 4)));
+  p.ld = round_up(cols, 16 / e);
+  p.blocks = ceil_div(cols, block);
+  p.rows = std::min(n_rows, std::max<int64_t>(1024, kSlotsBytes / (k * p.ld * e)));
   p.list = list_plan(p.rows * k, n_leaves);
-  p.slots_bytes = pad256((size_t)(p.rows * k * p.ld) * 4);
+  p.slots_bytes = pad256((size_t)(p.rows * k * p.ld * e));
+  p.units_bytes = e == 2 ? pad256((size_t)(p.rows * k * p.blocks) * 4) : 0;
+  p.dots_bytes = dots ? pad256((size_t)(p.rows * k * p.blocks) * 4) : 0;
   return p;
 }
 
@@ -181,19 +190,6 @@ int mixture_check(int64_t n_rows, int32_t k, int32_t n_leaves, int32_t d_in, int
   return GBDT_OK;
 }
 
-template <class S, typename T>
-int launch_routed_product(RoutedArgs<T>& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_out, S::NT, [&](dim3 blocks) {
-    gbdt_routed::routed_product_kernel<S><<<blocks, dim3(S::NT), 0, s>>>(g);
-  });
-}
-template <class S, typename T>
-int launch_routed_grad_input(RoutedArgs<T>& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_in, S::NT, [&](dim3 blocks) {
-    gbdt_routed::routed_grad_input_kernel<S><<<blocks, dim3(S::NT), 0, s>>>(g);
-  });
-}
-
 // Leaves of few positions: tiles of 32 rows, which waste less and leave room for more workgroups reading matrices.
 template <typename T>
 bool short_leaves(const gbdt_leaf::LeafArgs<T>& g) {
@@ -202,18 +198,36 @@ bool short_leaves(const gbdt_leaf::LeafArgs<T>& g) {
 template <typename T>
 using Short = Shape<T, 32, 128, 1, 2, true>;
 
-template <typename T>
+template <class S, gbdt_routed::Leaves WHAT, typename T>
+int launch_routed_product(RoutedArgs<T>& g, hipStream_t s) {
+  return leaf_rows_launches<S>(g, g.d_out, S::NT, [&](dim3 blocks) {
+    gbdt_routed::routed_product_kernel<S, WHAT><<<blocks, dim3(S::NT), 0, s>>>(g);
+  });
+}
+
+template <gbdt_routed::Leaves WHAT, typename T>
 int routed_product(RoutedArgs<T>& g, hipStream_t s) {
   const bool direct = whole_chunks<T>(g.x, g.ld_x, g.d_in) && whole_chunks<T>(g.w, g.d_in, g.d_in);
   if constexpr (sizeof(T) == 2) {
     if (direct) {
-      if (short_leaves(g)) return launch_routed_product<Short<T>>(g, s);
-      if (g.d_out <= 64) return launch_routed_product<Shape<T, 128, 64, 4, 1, true>>(g, s);
-      if (wide_leaves(g, g.d_out)) return launch_routed_product<Wide<T>>(g, s);
-      if (long_leaves(g, g.d_out, 128)) return launch_routed_product<Shape<T, 256, 128, 4, 2, true, false, 3>>(g, s);
+      if (short_leaves(g)) return launch_routed_product<Short<T>, WHAT>(g, s);
+      if (g.d_out <= 64) return launch_routed_product<Shape<T, 128, 64, 4, 1, true>, WHAT>(g, s);
+      if (wide_leaves(g, g.d_out)) return launch_routed_product<Wide<T>, WHAT>(g, s);
+      if (long_leaves(g, g.d_out, 128)) return launch_routed_product<Shape<T, 256, 128, 4, 2, true, false, 3>, WHAT>(g, s);
     }
   }
-  return direct ? launch_routed_product<Square<T>>(g, s) : launch_routed_product<SquareAny<T>>(g, s);
+  return direct ? launch_routed_product<Square<T>, WHAT>(g, s) : launch_routed_product<SquareAny<T>, WHAT>(g, s);
+}
+
+template <class S, typename T>
+int launch_routed_grad_input(RoutedArgs<T>& g, hipStream_t s) {
+  return leaf_rows_launches<S>(g, g.d_in, S::NT, [&](dim3 blocks) {
+    if (g.dots) {
+      gbdt_routed::routed_grad_input_kernel<S, true><<<blocks, dim3(S::NT), 0, s>>>(g);
+    } else {
+      gbdt_routed::routed_grad_input_kernel<S, false><<<blocks, dim3(S::NT), 0, s>>>(g);
+    }
+  });
 }
 
 template <typename T>
@@ -228,7 +242,7 @@ int routed_grad_input(RoutedArgs<T>& g, hipStream_t s) {
 
 template <typename O>
 int combine(const CombineArgs<O>& g, hipStream_t s) {
-  if (g.cols <= 64) {
+  if (g.cols <= 256 / (int)sizeof(O)) {
     gbdt_routed::combine_kernel<O, 16><<<dim3((unsigned)ceil_div(g.n_rows, 16)), dim3(256), 0, s>>>(g);
   } else {
     gbdt_routed::combine_kernel<O, 64><<<dim3((unsigned)ceil_div(g.n_rows, 4)), dim3(256), 0, s>>>(g);
@@ -240,41 +254,49 @@ int combine(const CombineArgs<O>& g, hipStream_t s) {
 // So few rows that a wavefront for every few outputs of a row takes less than lists, tiles and slots.
 bool few_rows(int64_t n_rows, int64_t k, int64_t d_out) { return n_rows <= 4 || (n_rows <= 2048 && n_rows * k * d_out <= 16384); }
 
-// Products of all rows, kept in slots and added up, so many rows at a time as the plan says.  products(g): to the slots.
-template <typename T, class G, typename O, class Products>
-int by_slots(const G& all, int64_t n_rows, int64_t cols, const CombineArgs<O>& to, const SlotPlan& plan, char* scratch,
-             const Products& products, hipStream_t s, const T* in, int64_t ld_in, bool grad) {
+// Products of all rows, kept in slots and added up, so many rows at a time as the plan says.  products(g, r): of the rows from r on,
+// to the slots.  Where answers go to rows directly (`direct`), the plan's list is all that is used of the scratch.
+template <class G, typename O, class Products>
+int by_slots(const G& all, int64_t n_rows, int64_t cols, const CombineArgs<O>& to, const SlotPlan& plan, char* scratch, bool direct,
+             const Products& products, hipStream_t s) {
   for (int64_t r = 0; r < n_rows; r += plan.rows) {
     const int64_t n = std::min(plan.rows, n_rows - r);
     G g = all;
     g.leaves += r * g.k;
+    g.gates += r * g.k;
     const ListPlan list = n == plan.rows ? plan.list : list_plan(n * g.k, g.n_leaves);
     int rc = make_lists(list, g.leaves, g.n_leaves, g.k, scratch, &g.offsets, &g.row_idx, &g.pair_idx, s);
     if (rc != GBDT_OK) return rc;
-    g.slots = (float*)(scratch + plan.list.bytes());
+    char* at = scratch + plan.list.bytes();
+    g.slots = direct || !to.out ? nullptr : at;
+    g.units = (float*)(at + plan.slots_bytes);
+    g.dots = to.dgates ? (float*)(at + plan.slots_bytes + plan.units_bytes) : nullptr;
     g.ld_slots = plan.ld;
+    g.blocks = (int32_t)plan.blocks;
     g.n_rows = (int32_t)n;
     g.n_positions = (int32_t)(n * g.k);
-    if ((rc = products(g, in + r * ld_in, r)) != GBDT_OK) return rc;
+    if ((rc = products(g, r)) != GBDT_OK) return rc;
+    if (direct) {
+      gbdt_routed::clear_rows_kernel<O><<<dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, s>>>(g.leaves, g.n_leaves, (int32_t)n, (int32_t)cols,
+                                                                                              to.out + r * to.ld_out, to.ld_out);
+      LAUNCHED("clear_rows_kernel");
+      continue;
+    }
     CombineArgs<O> c = to;
     c.slots = g.slots;
+    c.units = g.units;
+    c.dots = g.dots;
     c.leaves = g.leaves;
-    c.gates += r * g.k;
+    c.gates = g.gates;
     if (c.out) c.out += r * c.ld_out;
+    if (c.dgates) c.dgates += r * g.k, c.dy += r * c.ld_dy;
     c.ld = plan.ld;
+    c.blocks = g.blocks;
     c.n_rows = (int32_t)n;
     c.n_leaves = g.n_leaves;
     c.k = g.k;
     c.cols = (int32_t)cols;
-    if (!grad) {
-      if ((rc = combine(c, s)) != GBDT_OK) return rc;
-      continue;
-    }
-    c.x += r * c.ld_x;
-    c.dy += r * c.ld_dy;
-    if (c.dgates) c.dgates += r * g.k;
-    gbdt_routed::combine_grad_kernel<O><<<dim3((unsigned)ceil_div(n, 4)), dim3(256), 0, s>>>(c);
-    LAUNCHED("combine_grad_kernel");
+    if ((rc = combine(c, s)) != GBDT_OK) return rc;
   }
   return GBDT_OK;
 }
@@ -290,28 +312,30 @@ int mixture_product(RoutedArgs<T>& g, int64_t n_rows, hipStream_t s) {
     LAUNCHED("routed_few_kernel");
     return GBDT_OK;
   }
-  const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out);
+  const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out, sizeof(T), gbdt_routed::block_columns<T>, false);
   void* ws = nullptr;
   const int rc = gbdt_internal::workspace(plan.bytes(), s, &ws);
   if (rc != GBDT_OK) return rc;
   CombineArgs<T> to = {};
-  to.gates = g.gates;
   to.out = g.y;
   to.ld_out = g.ld_y;
-  return by_slots<T>(g, n_rows, g.d_out, to, plan, (char*)ws,
-                     [&](RoutedArgs<T>& piece, const T* x, int64_t) {
-                       piece.x = x;
-                       return routed_product(piece, s);
-                     },
-                     s, g.x, g.ld_x, false);
+  const bool direct = g.k == 1;
+  return by_slots(g, n_rows, g.d_out, to, plan, (char*)ws, direct,
+                  [&](RoutedArgs<T>& piece, int64_t r) {
+                    piece.x = g.x + r * g.ld_x;
+                    piece.y = g.y + r * g.ld_y;
+                    return direct ? routed_product<gbdt_routed::Leaves::kRows>(piece, s) : routed_product<gbdt_routed::Leaves::kSlots>(piece, s);
+                  },
+                  s);
 }
 
 template <typename T>
-int mixture_weights(RoutedArgs<T> g, int64_t n_rows, const WeightPlan& plan, char* scratch, hipStream_t s) {
+int mixture_weights(RoutedArgs<T> g, int64_t n_rows, const WeightPlan& plan, char* scratch, bool listed, hipStream_t s) {
   g.n_rows = (int32_t)n_rows;
   g.n_positions = (int32_t)(n_rows * g.k);
-  int rc = make_lists(plan.list, g.leaves, g.n_leaves, g.k, scratch, &g.offsets, &g.row_idx, &g.pair_idx, s);
-  if (rc != GBDT_OK) return rc;
+  list_places(plan.list, scratch, &g.offsets, &g.row_idx, &g.pair_idx);
+  int rc = GBDT_OK;
+  if (!listed && (rc = make_lists(plan.list, g.leaves, g.n_leaves, g.k, scratch, &g.offsets, &g.row_idx, &g.pair_idx, s)) != GBDT_OK) return rc;
   T* gated = (T*)(scratch + plan.list.bytes());
   if (!g.dw) g.x = gated, g.ld_x = plan.ld, g.d_in = kChunk<T>;  // the outputs' sums alone read no inputs
   g.cut = (int32_t)plan.sums.cut;
@@ -345,7 +369,7 @@ template <typename T>
 int mixture_product_grad(RoutedArgs<T>& g, int64_t n_rows, hipStream_t s) {
   const bool weights = g.dw || g.dbias, rows = (g.dx || g.dgates) && n_rows > 0;
   if (!weights && !rows) return GBDT_OK;
-  const SlotPlan slots = slot_plan(n_rows, g.k, g.n_leaves, g.d_in);
+  const SlotPlan slots = slot_plan(n_rows, g.k, g.n_leaves, g.d_in, sizeof(T), gbdt_routed::block_columns<T>, true);
   const WeightPlan sums = weight_plan(n_rows, g.k, g.n_leaves, g.dw ? g.d_in : kChunk<T>, g.d_out, sizeof(T), gbdt_internal::cu_count());
   if (weights && sums.sums.tiles > most_blocks(kGradThreads) / 8) return GBDT_EUNSUPPORTED;
   void* ws = nullptr;
@@ -353,25 +377,24 @@ int mixture_product_grad(RoutedArgs<T>& g, int64_t n_rows, hipStream_t s) {
   if (rc != GBDT_OK) return rc;
   if (rows) {
     CombineArgs<T> to = {};
-    to.gates = g.gates;
     to.out = g.dx;
     to.ld_out = g.ld_dx;
-    to.x = g.x;
     to.dy = g.dy;
     to.bias = g.bias;
     to.dgates = g.dgates;
-    to.ld_x = g.ld_x;
     to.ld_dy = g.ld_dy;
     to.d_out = g.d_out;
-    rc = by_slots<T>(g, n_rows, g.d_in, to, slots, (char*)ws,
-                     [&](RoutedArgs<T>& piece, const T* dy, int64_t) {
-                       piece.dy = dy;
-                       return routed_grad_input(piece, s);
-                     },
-                     s, g.dy, g.ld_dy, true);
+    rc = by_slots(g, n_rows, g.d_in, to, slots, (char*)ws, false,
+                  [&](RoutedArgs<T>& piece, int64_t r) {
+                    piece.dy = g.dy + r * g.ld_dy;
+                    if (g.dgates) piece.x = g.x + r * g.ld_x;
+                    return routed_grad_input(piece, s);
+                  },
+                  s);
     if (rc != GBDT_OK) return rc;
   }
-  return weights ? mixture_weights(g, n_rows, sums, (char*)ws, s) : GBDT_OK;
+  // (rows that were all taken at once have left the whole list in its place)
+  return weights ? mixture_weights(g, n_rows, sums, (char*)ws, rows && slots.rows == n_rows, s) : GBDT_OK;
 }
 
 template <typename T>
@@ -444,20 +467,22 @@ int quantize(const gbdt_code::QuantizeArgs& g, hipStream_t s) {
   return launch_quantize<T, 4>(g, s);
 }
 
-template <class S, typename O, bool SLOTS>
+using gbdt_code::Place;
+
+template <class S, typename O, Place WHERE>
 int launch_code_product(CodeArgs& g, hipStream_t s) {
   return leaf_rows_launches<S>(g, g.d_out, S::NT, [&](dim3 blocks) {
-    gbdt_code::code_product_kernel<S, O, SLOTS><<<blocks, dim3(S::NT), 0, s>>>(g);
+    gbdt_code::code_product_kernel<S, O, WHERE><<<blocks, dim3(S::NT), 0, s>>>(g);
   });
 }
 
-template <typename O, bool SLOTS>
+template <typename O, Place WHERE>
 int code_tiles(CodeArgs& g, hipStream_t s) {
-  if (short_leaves(g)) return launch_code_product<Short<int8_t>, O, SLOTS>(g, s);
-  if (g.d_out <= 64) return launch_code_product<Shape<int8_t, 128, 64, 4, 1, true>, O, SLOTS>(g, s);
-  if (wide_leaves(g, g.d_out)) return launch_code_product<Shape<int8_t, 256, 256, 2, 4, true, true>, O, SLOTS>(g, s);
-  if (long_leaves(g, g.d_out, 128)) return launch_code_product<Shape<int8_t, 256, 128, 4, 2, true, false, 3>, O, SLOTS>(g, s);
-  return launch_code_product<Shape<int8_t, 128, 128, 2, 2, true, true>, O, SLOTS>(g, s);
+  if (short_leaves(g)) return launch_code_product<Short<int8_t>, O, WHERE>(g, s);
+  if (g.d_out <= 64) return launch_code_product<Shape<int8_t, 128, 64, 4, 1, true>, O, WHERE>(g, s);
+  if (wide_leaves(g, g.d_out)) return launch_code_product<Shape<int8_t, 256, 256, 2, 4, true, true>, O, WHERE>(g, s);
+  if (long_leaves(g, g.d_out, 128)) return launch_code_product<Shape<int8_t, 256, 128, 4, 2, true, false, 3>, O, WHERE>(g, s);
+  return launch_code_product<Shape<int8_t, 128, 128, 2, 2, true, true>, O, WHERE>(g, s);
 }
 
 template <typename O, bool LISTED>
@@ -474,27 +499,28 @@ int code_few(const CodeArgs& g, int64_t rows, hipStream_t s) {
 template <typename O>
 int leaf_codes(CodeArgs& g, hipStream_t s) {
   if (few_rows(g.n_positions, 1, g.d_out)) return code_few<O, true>(g, g.n_positions, s);
-  return code_tiles<O, false>(g, s);
+  return code_tiles<O, Place::kRow>(g, s);
 }
 
 template <typename O>
 int mixture_codes(CodeArgs& g, int64_t n_rows, hipStream_t s) {
   if (few_rows(n_rows, g.k, g.d_out)) return code_few<O, false>(g, n_rows, s);
-  const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out);
+  const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out, sizeof(O), gbdt_routed::block_columns<int8_t>, false);
   void* ws = nullptr;
   const int rc = gbdt_internal::workspace(plan.bytes(), s, &ws);
   if (rc != GBDT_OK) return rc;
   CombineArgs<O> to = {};
-  to.gates = g.gates;
   to.out = (O*)g.out;
   to.ld_out = g.ld_out;
-  return by_slots<int8_t>(g, n_rows, g.d_out, to, plan, (char*)ws,
-                          [&](CodeArgs& piece, const int8_t* x, int64_t r) {
-                            piece.x = x;
-                            piece.row_scales += r;
-                            return code_tiles<float, true>(piece, s);
-                          },
-                          s, g.x, g.ld_x, false);
+  const bool direct = g.k == 1;
+  return by_slots(g, n_rows, g.d_out, to, plan, (char*)ws, direct,
+                  [&](CodeArgs& piece, int64_t r) {
+                    piece.x = g.x + r * g.ld_x;
+                    piece.row_scales = g.row_scales + r;
+                    piece.out = (O*)g.out + r * g.ld_out;
+                    return direct ? code_tiles<O, Place::kGatedRow>(piece, s) : code_tiles<O, Place::kSlot>(piece, s);
+                  },
+                  s);
 }
 
 }  // namespace
@@ -565,7 +591,8 @@ size_t gbdt_mixture_workspace_bytes(int64_t n_rows, int32_t k, int32_t n_leaves,
   if (mixture_check(n_rows, k, n_leaves, d_in, d_out, (const void*)4, (const void*)4, dtype) != GBDT_OK) return 0;
   const int64_t e = dtype == GBDT_F32 ? 4 : 2, units = gbdt_internal::cu_count();
   size_t most = 0;
-  for (int64_t cols : {d_in, d_out}) most = std::max(most, slot_plan(n_rows, k, n_leaves, cols).bytes());
+  const int64_t block = dtype == GBDT_F32 ? 32 : 64;  // (a product of codes takes no more)
+  for (int64_t cols : {d_in, d_out}) most = std::max(most, slot_plan(n_rows, k, n_leaves, cols, e, block, true).bytes());
   for (int64_t inputs : {(int64_t)d_in, 16 / e}) most = std::max(most, weight_plan(n_rows, k, n_leaves, inputs, d_out, e, units).bytes());
   return gbdt_internal::workspace_head_bytes() + most;
 }

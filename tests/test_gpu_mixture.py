@@ -1,7 +1,9 @@
 """Rows that several leaves answer, on the GPU, against the definition in 64 bits.
 
 u = 2^-24, half = half a step of the element type.  y: sums of d_in + 1 terms in f32, weighed and added up over k slots, rounded once:
-(d_in + k + 3) u of the terms' magnitudes and half of the result.  dx the same with d_out.  dweight, dbias: gates * dy is rounded to
+(d_in + k + 3) u of the terms' magnitudes and half of the result; bf16 with k > 1: the terms of the last sum are held with 11 bits,
+half a step of which is 2^-11 of each (and 2^-25 of the unit of the least, which is at most 2^-14 of the largest of the row's: 2^-39
+of that).  dx the same with d_out.  dweight, dbias: gates * dy is rounded to
 the type (half of each term, after u of the product), summed over up to n positions: half + (n + 2) u of the magnitudes, and the
 result's half.  dgates: a sum of d_out inside one of d_in + d_out: (d_in + 2 d_out + 4) u of the magnitudes."""
 import math
@@ -39,10 +41,17 @@ def made(n, k, n_leaves, d_in, d_out, dtype, seed, pad=0, skew=1.0, outside=0.05
     return x, dy, w, b, leaves, gates
 
 
+def held(x, k, mag):
+    """What the roundings of a row's terms add, for bf16."""
+    if x.dtype == torch.float32 or k == 1:
+        return 0.0
+    return 2.0 ** -11 * mag + 2.0 ** -39 * mag.amax(1, keepdim=True)
+
+
 def check_y(y, x, w, b, leaves, gates, what=""):
     want, mag = ref.mixture(x, w, b, leaves, gates)
     half = torch.finfo(x.dtype).eps / 2
-    bad = (y.double() - want).abs() > (w.shape[2] + leaves.shape[1] + 3) * U * mag + half * want.abs()
+    bad = (y.double() - want).abs() > (w.shape[2] + leaves.shape[1] + 3) * U * mag + half * want.abs() + held(x, leaves.shape[1], mag)
     assert not bool(bad.any()), (what, int(bad.sum()), torch.nonzero(bad)[:3].tolist())
 
 
@@ -56,7 +65,7 @@ def check_grad(got, dy, x, w, b, leaves, gates):
     for name, a, e, m, t, h in zip(("dx", "dweight", "dbias", "dgates"), got, want, mag, tols, halves):
         if a is None:
             continue
-        bad = (a.double() - e).abs() > t * m + h * e.abs()
+        bad = (a.double() - e).abs() > t * m + h * e.abs() + (held(x, max(k, 2), m) if name == "dx" else 0.0)
         assert not bool(bad.any()) and not bool(torch.isnan(a).any()), (name, int(bad.sum()), torch.nonzero(bad)[:3].tolist())
 
 
@@ -180,3 +189,27 @@ def test_gradients_against_differences():
         want = float((grad.double() * step).sum())
         grad_tol = float((grad.double().abs() * step.abs()).sum()) * U * 2 + 72 * 2 * U * t0 / (19 * U)
         assert abs((l1 - l0) - want) <= t1 + t0 + grad_tol, name
+
+
+def test_infinities_and_sizes_within_a_row_of_terms():
+    """bf16 terms share a power of two by 64 columns: an infinity or a NaN among them leaves the others as they are, and columns of very
+    different size keep their own digits."""
+    n, k = 300, 3
+    x, dy, w, b, leaves, gates = made(n, k, 4, 64, 128, "bf16", seed=21, outside=0.0)
+    size = 2.0 ** torch.randint(-60, 60, (128,), generator=torch.Generator().manual_seed(1)).float().cuda()
+    w = (w.float() * size[:, None]).to(torch.bfloat16)
+    b = (b.float() * size).to(torch.bfloat16)
+    w[1, 3], b[2, 70] = math.inf, math.nan
+    y = B.gbdt_mixture_product(x, w, leaves, gates, bias=b)
+    hit3 = (leaves == 1).any(1)
+    hit70 = (leaves == 2).any(1)
+    assert torch.equal(~torch.isfinite(y[:, 3]), hit3) and torch.equal(torch.isnan(y[:, 70]), hit70)
+    clean_w, clean_b = w.clone(), b.clone()
+    clean_w[1, 3], clean_b[2, 70] = 0.0, 0.0
+    want, mag = ref.mixture(x, clean_w, clean_b, leaves, gates)
+    block = mag.view(n, 2, 64).amax(2, keepdim=True).expand(n, 2, 64).reshape(n, 128)
+    tol = (64 + 3 + 3) * U * mag + 2.0 ** -8 * want.abs() + 2.0 ** -11 * mag + 2.0 ** -39 * block
+    ok = (y.double() - want).abs() <= tol
+    ok[:, 3] |= hit3
+    ok[:, 70] |= hit70
+    assert bool(ok.all())
