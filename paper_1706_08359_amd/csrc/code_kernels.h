@@ -116,7 +116,7 @@ template <typename O, Place WHERE>
 struct ToScaled {
   typedef typename std::conditional<WHERE == Place::kSlot, typename SlotOf<O>::Type, O>::type Out;
   static constexpr bool kScaled = true, kHalves = WHERE == Place::kSlot && sizeof(Out) == 2;
-  static constexpr bool kFinished = kHalves || WHERE == Place::kGatedRow;
+  static constexpr bool kFinished = kHalves || WHERE == Place::kGatedRow, kDots = false;
   Out* out;
   int64_t ld;
   const float* row_scales;
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(S::NT, 2) code_product_kernel(const CodeArgs g
   typedef ToScaled<O, WHERE> To;
   const bool slot = WHERE == Place::kSlot;
   const To to = {(typename To::Out*)(slot ? g.slots : g.out), slot ? g.ld_slots : g.ld_out, g.row_scales, g.col_scales, g.add};
-  leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, to, g.d_out);
+  leaf_rows_product<S, typename S::RowsB, 1, S::BM < 256>(lds, g, g.x, g.ld_x, g.d_in, to, g.d_out);
 }
 
 // A few rows: OUTPUTS outputs of one row a wavefront, sums of four products an instruction.  LISTED: one leaf a row, by position in

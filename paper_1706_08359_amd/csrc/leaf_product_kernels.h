@@ -124,7 +124,7 @@ __device__ __forceinline__ PlainRows<T> plain_rows(const T* base, int64_t ld, in
 template <typename T>
 struct ToRows {
   typedef T Out;
-  static constexpr bool kScaled = false, kFinished = false;
+  static constexpr bool kScaled = false, kFinished = false, kDots = false;
   const T* bias;  // [n_leaves][cols] or null
   T* out;
   int64_t ld;
@@ -139,10 +139,12 @@ struct ToRows {
 // The rows of one tile of positions times a matrix of the leaf, g.cols_per column tiles one after another; the next one's
 // first steps are on their way while one's values are stored.  B: the matrix' orientation, k its length along k.
 // To::kScaled: values are multiplied by a factor of their position and one of the leaf's column.
-// To::kFinished: a row's values of this wavefront's columns go through to.finish before they are stored.
+// To::kFinished: a row's values of this wavefront's columns go through to.finish before they are stored, which is given the position's
+// row if To::kDots.
 // GROUPS > 1: as many times the tile's threads take a part of k each, all of as many steps, and the first adds up; one column
 // tile a workgroup then, since the other groups leave after it.
-template <class S, class B, int GROUPS, typename T, class G, class To>
+// MANY: a workgroup may have several column tiles (without it the next one's state takes no registers).
+template <class S, class B, int GROUPS, bool MANY, typename T, class G, class To>
 __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T* in, int64_t ld_in, int k, const To& to, int cols) {
   typedef typename S::Acc Acc;
   const uint32_t t = g.first + xcd_tile(blockIdx.x, gridDim.x);
@@ -159,12 +161,14 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T
   const int w = thread_of<S::NT>() >> 6;
   int ids[S::TM];  // places of this lane's blocks, -1 for none
   float factor[To::kScaled ? S::TM : 1];
+  int row_of_id[To::kDots ? S::TM : 1];
   const int m0 = p0 + w / S::WN * (S::TM * 16) + (threadIdx.x & 15);
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
     const int p = m0 + 16 * i;
     ids[i] = p < end ? to.place(g, p) : -1;
     if constexpr (To::kScaled) factor[i] = ids[i] >= 0 ? to.row_scale(g, p) : 0.0f;
+    if constexpr (To::kDots) row_of_id[i] = ids[i] >= 0 ? g.row_idx[p] : 0;
   }
   const int group = GROUPS > 1 ? (int)threadIdx.x / S::NT : 0;
   lds += group * S::kLdsBytes;
@@ -178,7 +182,7 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T
     tile_begin<S>(lds, a, b, rows_a, rows_b, k0, k0 + part);
   };
   begin_columns(col_first);
-  for (int col = col_first; col < col_last; col += S::BN) {
+  for (int col = col_first; col < col_last; col = MANY ? col + S::BN : col_last) {
     Acc acc[S::TM][S::TN];
     zeros<S>(acc);
     tile_run<S, true>(lds, a, b, rows_a, rows_b, k0, k0 + part, acc, Nothing{});
@@ -196,7 +200,7 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T
 #pragma unroll
         for (int v = 0; v < values; ++v)
           acc[v / S::TN][v % S::TN] += ((const Acc*)(lds + other * S::kLdsBytes))[v * S::NT + thread_of<S::NT>()];
-    } else if (col + S::BN < col_last) {
+    } else if (MANY && col + S::BN < col_last) {
       begin_columns(col + S::BN);
     }
     const int l = threadIdx.x & 63, wave_col = col + w % S::WN * (S::TN * 16);
@@ -225,7 +229,7 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T
         f32x4 v[S::TN];
 #pragma unroll
         for (int j = 0; j < S::TN; ++j) v[j] = value(i, j);
-        to.template finish<S::TN>(g, m0 + 16 * i, ids[i], wave_col, cols, v);
+        to.template finish<S::TN>(g, row_of_id[To::kDots ? i : 0], ids[i], wave_col, cols, v);
 #pragma unroll
         for (int j = 0; j < S::TN; ++j) acc[i][j] = __builtin_bit_cast(Acc, v[j]);
       }
@@ -254,14 +258,14 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_product_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, ToRows<typename S::T>{g.bias, g.y, g.ld_y}, g.d_out);
+  leaf_rows_product<S, typename S::RowsB, 1, true>(lds, g, g.x, g.ld_x, g.d_in, ToRows<typename S::T>{g.bias, g.y, g.ld_y}, g.d_out);
 }
 
 // The same where there are too few tiles for the compute units: a tile's k is split among GROUPS times the threads.
 template <class S, int GROUPS>
 __global__ void __launch_bounds__(S::NT* GROUPS) leaf_product_split_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes * GROUPS];
-  leaf_rows_product<S, typename S::RowsB, GROUPS>(lds, g, g.x, g.ld_x, g.d_in, ToRows<typename S::T>{g.bias, g.y, g.ld_y}, g.d_out);
+  leaf_rows_product<S, typename S::RowsB, GROUPS, false>(lds, g, g.x, g.ld_x, g.d_in, ToRows<typename S::T>{g.bias, g.y, g.ld_y}, g.d_out);
 }
 
 // dx: rows of dy (k = output along memory) times w, whose rows are k.  Bound by its stores, d_in values a row, which a tile's
@@ -270,7 +274,7 @@ __global__ void __launch_bounds__(S::NT* GROUPS) leaf_product_split_kernel(const
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_input_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::ColumnsB, 1>(lds, g, g.dy, g.ld_dy, g.d_out, ToRows<typename S::T>{nullptr, g.dx, g.ld_dx}, g.d_in);
+  leaf_rows_product<S, typename S::ColumnsB, 1, true>(lds, g, g.dy, g.ld_dy, g.d_out, ToRows<typename S::T>{nullptr, g.dx, g.ld_dx}, g.d_in);
 }
 
 // A few positions (a row or a few answered at once): a wavefront takes OUTPUTS outputs of one position, each lane a chunk of k
@@ -362,12 +366,26 @@ struct Piece {
   bool whole;        // all of its leaf
   int64_t slot;      // of its sums, if not
 };
-template <typename T>
+// FROM_LEAF: pieces are cut from their leaf's first position on, so that a leaf no longer than a cut is whole: where leaves are many
+// that is most of them, and no sums are left behind.  Slots then go by the block of positions that a piece begins in: of those that
+// begin in one, at most one is its leaf's last (slot 2 b) and one is not (2 b + 1), since that one is a whole cut long.
+template <bool FROM_LEAF, typename T>
 __device__ __forceinline__ Piece find_piece(const LeafArgs<T>& g, int piece) {
   Piece r = {-1, 0, 0, false, 0};
   const int leaf = find_leaf(g.offsets, g.n_leaves, g.n_positions, g.cut, piece);
   if (leaf < 0) return r;
   const int begin = offset_at(g.offsets, leaf, g.n_positions), end = offset_at(g.offsets, leaf + 1, g.n_positions);
+  if constexpr (FROM_LEAF) {
+    const int first = begin / g.cut, nth = piece - (first + leaf);
+    const int64_t p0 = (int64_t)begin + (int64_t)nth * g.cut;
+    if (p0 >= end && nth > 0) return r;  // an empty leaf has one piece: zeros
+    r.leaf = leaf;
+    r.p0 = (int)(p0 < end ? p0 : end);
+    r.p1 = p0 + g.cut < end ? (int)p0 + g.cut : end;
+    r.whole = end - begin <= g.cut;
+    r.slot = 2 * (p0 / g.cut) + (r.p1 == end ? 0 : 1);
+    return r;
+  }
   const int64_t block = piece - leaf;
   const int64_t b0 = block * g.cut, b1 = b0 + g.cut;
   r.p0 = begin > b0 ? begin : (int)(b0 < end ? b0 : end);
@@ -388,7 +406,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   // A piece's workgroups share its rows and so are one XCD's; pieces, which are of any length, go round.
   const uint32_t tiles = g.col_tiles * g.row_tiles, at = blockIdx.x / 8;
   const int piece = (int)(g.first + at / tiles * 8 + blockIdx.x % 8), r = (int)(at % tiles);
-  const Piece at_piece = find_piece(g, piece);
+  const Piece at_piece = find_piece<LISTED>(g, piece);
   const int leaf = at_piece.leaf, p0 = at_piece.p0, p1 = at_piece.p1;
   if (leaf < 0) return;
   // A short piece's column tiles are gone through cols_per at a time, one after another, by the first of its workgroups; the
@@ -503,7 +521,11 @@ __global__ void __launch_bounds__(256) leaf_grad_join_kernel(const LeafArgs<T> g
   }
   const int begin = offset_at(g.offsets, lo, g.n_positions), end = offset_at(g.offsets, lo + 1, g.n_positions);
   if (begin >= at || end <= at || begin < at - g.cut) return;
-  const int64_t last = ((int64_t)end - 1) / g.cut;
+  int64_t last = ((int64_t)end - 1) / g.cut;  // block of the last piece
+  if constexpr (LISTED) {
+    if (end - begin <= g.cut) return;
+    last = begin / g.cut + (end - begin - 1) / g.cut;
+  }
   const int64_t per = (int64_t)(g.d_in + 1) * g.d_out, n_w = (int64_t)g.d_in * g.d_out;
   for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < per; e += (int64_t)gridDim.x * 256) {
     if (e < n_w ? g.dw == nullptr : g.dbias == nullptr) continue;
@@ -511,7 +533,11 @@ __global__ void __launch_bounds__(256) leaf_grad_join_kernel(const LeafArgs<T> g
     for (int64_t b = block; b <= last; b += 8) {  // (eight at a time on their way, added in order)
       float v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = b + k <= last ? g.partial[2 * (b + k) * per + e] : 0.0f;
+      for (int k = 0; k < 8; ++k) {
+        // (cut from the leaf: every piece but the last is one that is not the last of those that begin in its block)
+        const int64_t slot = LISTED && b + k < last ? 2 * (b + k) + 1 : 2 * (b + k);
+        v[k] = b + k <= last ? g.partial[slot * per + e] : 0.0f;
+      }
 #pragma unroll
       for (int k = 0; k < 8; ++k) s = b + k <= last ? s + v[k] : s;
     }

@@ -34,7 +34,7 @@ int leaf_check(int64_t n_positions, int32_t n_leaves, int64_t n_rows, int32_t d_
 
 template <class S, typename T>
 int launch_leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_out, S::NT, [&](dim3 blocks) {
+  return leaf_rows_launches<S>(g, g.d_out, S::NT, true, [&](dim3 blocks) {
     gbdt_leaf::leaf_product_kernel<S><<<blocks, dim3(S::NT), 0, s>>>(g);
   });
 }
@@ -74,7 +74,7 @@ int leaf_product_few(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
 
 template <class S, int GROUPS, typename T>
 int launch_leaf_product_split(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_out, S::NT * GROUPS, [&](dim3 blocks) {
+  return leaf_rows_launches<S>(g, g.d_out, S::NT * GROUPS, false, [&](dim3 blocks) {
     gbdt_leaf::leaf_product_split_kernel<S, GROUPS><<<blocks, dim3(S::NT * GROUPS), 0, s>>>(g);
   });
 }
@@ -116,7 +116,7 @@ int leaf_product(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
 
 template <class S, typename T>
 int launch_leaf_grad_input(gbdt_leaf::LeafArgs<T>& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_in, S::NT, [&](dim3 blocks) {
+  return leaf_rows_launches<S>(g, g.d_in, S::NT, true, [&](dim3 blocks) {
     gbdt_leaf::leaf_grad_input_kernel<S><<<blocks, dim3(S::NT), 0, s>>>(g);
   });
 }

@@ -69,15 +69,15 @@ bool wide_tiles(int64_t rows, int64_t cols) {
 
 // Workgroups of the products over rows: the column tiles of a row tile are spread over as many as it takes to have eight a
 // compute unit (four of the large ones), and no more, since a workgroup's first tile waits for its leaf and its rows.
-// `launch(blocks)` is called with g.first set, more than once where there are millions of leaves.
+// `launch(blocks)` is called with g.first set, more than once where there are millions of leaves.  many: the kernel takes more than one
+// column tile.
 template <class S, typename T, class Launch>
-int leaf_rows_launches(gbdt_leaf::LeafArgs<T>& g, int64_t cols, int threads, const Launch& launch) {
+int leaf_rows_launches(gbdt_leaf::LeafArgs<T>& g, int64_t cols, int threads, bool many, const Launch& launch) {
   const int64_t row_tiles = (int64_t)g.n_positions / S::BM + g.n_leaves;
   const int64_t col_tiles = ceil_div(cols, S::BN);
   const int64_t most = (S::BM >= 256 ? 4 : 8) * gbdt_internal::cu_count();  // one or two at a time on a unit
   g.col_tiles = (uint32_t)col_tiles;
-  g.cols_per = (uint32_t)std::max<int64_t>(1, std::min(col_tiles, (int64_t)g.n_positions / S::BM * col_tiles / most));
-  if (threads > S::NT) g.cols_per = 1;  // several groups of threads a tile
+  g.cols_per = many ? (uint32_t)std::max<int64_t>(1, std::min(col_tiles, (int64_t)g.n_positions / S::BM * col_tiles / most)) : 1;
   const int64_t n = row_tiles * ceil_div(col_tiles, g.cols_per);
   if (n > kMaxTiles) return GBDT_EUNSUPPORTED;
   for (int64_t first = 0; first < n; first += most_blocks(threads)) {

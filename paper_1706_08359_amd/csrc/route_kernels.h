@@ -3,11 +3,10 @@
 // Scores s are the softmax of a row's logits, or their sigmoids.  The k leaves of the largest choice values c = s + bias are
 // taken, those of equal values from the lowest index; without a bias the order of s is that of the logits, which are compared
 // themselves.  A row is LANES lanes' work, PER neighbouring columns each: a pick is a maximum over the lanes and the first lane
-// that holds it.
+// that holds it.  Sixteen lanes where 16 columns each hold a row: the maximum then takes four moves of the vector unit for four rows.
 //
 // c decides between neighbours, so its roundings must not.  Values are taken in f32 with a bound of their error; a row that has two
-// values closer than that among its first k + 1, or at the border of its groups, is taken again in 64 bits (with the other rows of
-// its wavefront, whose choice 64 bits confirm).
+// values closer than that among its first k + 1, or at the border of its groups, is taken again in 64 bits, by the whole wavefront.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -41,15 +40,21 @@ __device__ __forceinline__ float dpp(float v) {
 }
 
 // op over the row's lanes, in all of them.  Within 16 lanes by moves of the vector unit: neighbours, pairs, the other half of
-// eight and of sixteen (mirrored: each half is uniform by then).
+// eight and of sixteen (mirrored: each half is uniform by then); then by exchanges of rows of 16 and of halves.
 template <int LANES, class Op>
 __device__ __forceinline__ float over_lanes(float v, const Op& op) {
   v = op(v, dpp<0xB1>(v));                     // lanes 1 0 3 2
-  v = op(v, dpp<0x4E>(v));                     // lanes 2 3 0 1
+  if (LANES >= 4) v = op(v, dpp<0x4E>(v));     // lanes 2 3 0 1
   if (LANES >= 8) v = op(v, dpp<0x141>(v));    // mirrored within 8
   if (LANES >= 16) v = op(v, dpp<0x140>(v));   // mirrored within 16
-  if (LANES >= 32) v = op(v, __shfl_xor(v, 16));
-  if (LANES >= 64) v = op(v, __shfl_xor(v, 32));
+  if (LANES >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  if (LANES >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
   return v;
 }
 template <int LANES, class Op>
@@ -96,23 +101,59 @@ __device__ __forceinline__ bool take_largest(V (&v)[PER], V* value, int* column)
   const bool any = top > lowest<V>();
   const uint64_t who = row_ballot<LANES>(mine == top);
   const int lane = threadIdx.x & (LANES - 1), first = __ffsll((unsigned long long)who) - 1;
-  int at = PER;
+  bool looking = any && lane == first;
+  int at = 0;
 #pragma unroll
-  for (int i = PER - 1; i >= 0; --i) at = v[i] == top ? i : at;
-#pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (any && lane == first && i == at) v[i] = lowest<V>();
+  for (int i = 0; i < PER; ++i) {
+    const bool here = looking && v[i] == top;
+    at = here ? i : at;
+    v[i] = here ? lowest<V>() : v[i];
+    looking = looking && !here;
+  }
   *value = top;
   *column = first * PER + __shfl(at, first, LANES);
   return any;
 }
 
-// Values of all but the best groups become masked.  worth: room for kMaxGroups values of this row.  True if a border is closer
-// than `tol` says (of single values).
+// Values of all but the best groups become masked.  True if the border is closer than `tol` says (of single values).
 template <typename V, int LANES, int PER>
-__device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V tol, V* worth) {
+__device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V tol) {
   const int lane = threadIdx.x & (LANES - 1);
+  const int lanes = g.group_size / PER;
+  if (lanes >= 1 && lanes * PER == g.group_size && (lanes & (lanes - 1)) == 0) {
+    // a group is `lanes` neighbouring lanes: the two largest of all groups at once
+    V one = lowest<V>(), two = lowest<V>();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      two = Max{}(two, v[i] < one ? v[i] : one);
+      one = Max{}(one, v[i]);
+    }
+    for (int m = 1; m < lanes; m <<= 1) {
+      const V other = __shfl_xor(one, m), next = __shfl_xor(two, m);
+      const V lower = other < one ? other : one;
+      two = Max{}(Max{}(two, next), lower);
+      one = Max{}(one, other);
+    }
+    const V worth = g.group_best == 2 && two > lowest<V>() ? one + two : one;
+    const int mine = lane / lanes;
+    int before = 0;  // groups that come before this lane's
+    for (int q = 0; q < g.n_groups; ++q) {
+      const V other = __shfl(worth, q * lanes, LANES);
+      before += other > worth || (other == worth && q < mine) ? 1 : 0;
+    }
+    const bool group = mine < g.n_groups, kept = group && before < g.groups_kept && worth > lowest<V>();
+    const V least = -over_lanes<LANES>(kept ? -worth : lowest<V>(), Max{});
+    const V next = over_lanes<LANES>(group && !kept ? worth : lowest<V>(), Max{});
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = kept ? v[i] : lowest<V>();
+    return next > lowest<V>() && !(least - next > 2 * tol + (V)0x1p-21 * fabs(least));
+  }
+  // groups of any size, one after another; lane q mod LANES keeps group q's value
+  constexpr int most = (kMaxGroups + LANES - 1) / LANES;
+  V mine[most];
   int group[PER];
+#pragma unroll
+  for (int t = 0; t < most; ++t) mine[t] = lowest<V>();
 #pragma unroll
   for (int i = 0; i < PER; ++i) group[i] = (lane * PER + i) / g.group_size;
   for (int q = 0; q < g.n_groups; ++q) {
@@ -124,14 +165,9 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V t
     if (take_largest<V, LANES, PER>(in, &sum, &column) && g.group_best == 2) {
       if (take_largest<V, LANES, PER>(in, &second, &column)) sum += second;
     }
-    if (lane == 0) worth[q] = sum;
-  }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  // lane i has the groups i, i + LANES, ..
-  constexpr int most = (kMaxGroups + LANES - 1) / LANES;
-  V mine[most];
 #pragma unroll
-  for (int t = 0; t < most; ++t) mine[t] = lane + t * LANES < g.n_groups ? worth[lane + t * LANES] : lowest<V>();
+    for (int t = 0; t < most; ++t) mine[t] = lane + t * LANES == q ? sum : mine[t];
+  }
   uint64_t kept = 0;
   bool close = false;
   V last = lowest<V>();
@@ -158,29 +194,36 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V t
         if (lane + t * LANES == who) mine[t] = lowest<V>();
     }
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
   for (int i = 0; i < PER; ++i)
     if (!(group[i] < g.n_groups && kept >> group[i] & 1)) v[i] = lowest<V>();
   return close;
 }
 
-// The k columns of the largest values, -1 where fewer are left, into picked.  True if two of the first k + 1 are closer than
-// their errors, tol of each and 2^-23 of its size.
+// Slots of a row's k chosen leaves: lane i has the slots i, i + LANES, ..
+template <int LANES>
+constexpr int kSlotsOf = (kMaxChosen + LANES - 1) / LANES;
+
+// The k columns of the largest values, -1 where fewer are left.  True if two of the first k + 1 are closer than their errors, tol of
+// each and 2^-23 of its size.
 template <typename V, int LANES, int PER>
-__device__ __forceinline__ bool choose(const RouteArgs& g, V (&v)[PER], V tol, bool check, V* worth, int* picked) {
-  bool close = g.n_groups > 1 ? keep_groups<V, LANES, PER>(g, v, tol, worth) && check : false;
+__device__ __forceinline__ bool choose(const RouteArgs& g, V (&v)[PER], V tol, bool check, int (&picked)[kSlotsOf<LANES>]) {
+  bool close = false;
+  if (g.n_groups > 1) close = keep_groups<V, LANES, PER>(g, v, tol) && check;
   const int lane = threadIdx.x & (LANES - 1), more = check && g.k < g.n_leaves ? 1 : 0;
   V before = lowest<V>();
+#pragma unroll
+  for (int t = 0; t < kSlotsOf<LANES>; ++t) picked[t] = -1;
   for (int j = 0; j < g.k + more; ++j) {
     V top;
     int column;
     const bool any = take_largest<V, LANES, PER>(v, &top, &column);
     if (check && any && j > 0) close |= !(before - top > tol + (V)0x1p-22 * fabs(before));
     before = top;
-    if (lane == 0 && j < g.k) picked[j] = any ? column : -1;
+#pragma unroll
+    for (int t = 0; t < kSlotsOf<LANES>; ++t)
+      if (lane + t * LANES == j) picked[t] = any ? column : -1;
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   return close;
 }
 
@@ -232,17 +275,16 @@ __device__ __forceinline__ float sigmoid_over(float l, float c) { return l >= 0.
 // k slots of a row, lane i the slots i, i + LANES, ..; scores of the chosen, renormalised or not, without scale.
 template <int LANES>
 struct Slots {
-  static constexpr int kMost = (kMaxChosen + LANES - 1) / LANES;
+  static constexpr int kMost = kSlotsOf<LANES>;
   int column[kMost];
   float logit[kMost], score[kMost];
   // f(column): the logit, minus infinity for a masked one
   template <class F>
-  __device__ __forceinline__ void read(const RouteArgs& g, const int* picked, const F& f) {
+  __device__ __forceinline__ void read(const RouteArgs& g, const int (&picked)[kMost], const F& f) {
     const int lane = threadIdx.x & (LANES - 1);
 #pragma unroll
     for (int t = 0; t < kMost; ++t) {
-      const int j = lane + t * LANES;
-      column[t] = j < g.k ? picked[j] : -1;
+      column[t] = lane + t * LANES < g.k ? picked[t] : -1;
       logit[t] = column[t] >= 0 ? f(column[t]) : -INFINITY;
     }
   }
@@ -271,41 +313,58 @@ struct Slots {
 };
 
 // Bound by reading the logits where rows are many; k picks of some twenty instructions each are the rest.
-template <typename T, int LANES, int PER>
+// VALUES: leaves are chosen by their values, not by the logits themselves.
+template <typename T, int LANES, int PER, bool VALUES>
 __global__ void __launch_bounds__(kThreads) route_kernel(const RouteArgs g) {
   constexpr int rows = kThreads / LANES;
-  __shared__ double worth[rows][kMaxGroups];
-  __shared__ int picked_of[rows][kMaxChosen];
   const int r = threadIdx.x / LANES, lane = threadIdx.x & (LANES - 1);
   const int64_t d = (int64_t)blockIdx.x * rows + r;
   const T* row = d < g.n_rows ? (const T*)g.logits + d * g.ld : nullptr;
-  int* picked = picked_of[r];
-  float l[PER];
-  load_logits<T, PER>(row, lane * PER, g.n_leaves, l);
-  float top = l[0];
+  int picked[kSlotsOf<LANES>];
+  float top, inverse = 0.0f;
+  {
+    float l[PER];
+    load_logits<T, PER>(row, lane * PER, g.n_leaves, l);
+    top = l[0];
 #pragma unroll
-  for (int i = 1; i < PER; ++i) top = fmaxf(top, l[i]);
-  top = over_lanes<LANES>(top, Max{});
-  float v[PER];
-  if (g.bias == nullptr && g.group_best == 1) {
+    for (int i = 1; i < PER; ++i) top = fmaxf(top, l[i]);
+    top = over_lanes<LANES>(top, Max{});
+    if (!g.sigmoid && !g.renormalise) {
+      float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) v[i] = l[i];
-    choose<float, LANES, PER>(g, v, 0.0f, false, (float*)worth[r], picked);
-  } else {
-    float tol;
-    choice_values<float, LANES, PER>(g, l, top, v, &tol);
-    if (__any(choose<float, LANES, PER>(g, v, tol, true, (float*)worth[r], picked))) {
-      double exact[PER], none;
-      choice_values<double, LANES, PER>(g, l, top, exact, &none);
-      choose<double, LANES, PER>(g, exact, none, false, worth[r], picked);
+      for (int i = 0; i < PER; ++i) sum += l[i] > -INFINITY ? exp_below(l[i], top) : 0.0f;
+      inverse = 1.0f / over_lanes<LANES>(sum, Sum{});
     }
-  }
-  float inverse = 0.0f;
-  if (!g.sigmoid && !g.renormalise) {
-    float sum = 0.0f;
+    if constexpr (!VALUES) {
+      choose<float, LANES, PER>(g, l, 0.0f, false, picked);
+    } else {
+      float v[PER], tol;
+      choice_values<float, LANES, PER>(g, l, top, v, &tol);
+      const bool close = choose<float, LANES, PER>(g, v, tol, true, picked);
+      // rows to be taken again, all 64 lanes a row
+      constexpr int wide = (LANES * PER + 63) / 64;
+      uint64_t again = __ballot(close && lane == 0);
+      while (again) {
+        const int from = __ffsll((unsigned long long)again) - 1;
+        again &= again - 1;
+        const int64_t other = (int64_t)blockIdx.x * rows + ((threadIdx.x & ~63) + from) / LANES;
+        float logits[wide], most;
+        load_logits<T, wide>((const T*)g.logits + other * g.ld, (threadIdx.x & 63) * wide, g.n_leaves, logits);
+        most = logits[0];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += l[i] > -INFINITY ? exp_below(l[i], top) : 0.0f;
-    inverse = 1.0f / over_lanes<LANES>(sum, Sum{});
+        for (int i = 1; i < wide; ++i) most = fmaxf(most, logits[i]);
+        most = over_lanes<64>(most, Max{});
+        double exact[wide], none;
+        choice_values<double, 64, wide>(g, logits, most, exact, &none);
+        int chosen[kSlotsOf<64>];
+        choose<double, 64, wide>(g, exact, none, false, chosen);
+#pragma unroll
+        for (int t = 0; t < kSlotsOf<LANES>; ++t) {
+          const int e = __shfl(chosen[0], lane + t * LANES);
+          if ((int)(threadIdx.x & 63) / LANES == from / LANES) picked[t] = e;
+        }
+      }
+    }
   }
   Slots<LANES> s;
   s.read(g, picked, [&](int e) { return (float)row[e]; });
@@ -329,18 +388,15 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteArgs g) {
 template <typename T, int LANES, int PER>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteArgs g) {
   constexpr int rows = kThreads / LANES;
-  __shared__ int picked_of[rows][kMaxChosen];
-  __shared__ float each_of[rows][kMaxChosen];
   const int r = threadIdx.x / LANES, lane = threadIdx.x & (LANES - 1);
   const int64_t d = (int64_t)blockIdx.x * rows + r;
   const T* row = d < g.n_rows ? (const T*)g.logits + d * g.ld : nullptr;
-  int* picked = picked_of[r];
-  float* each = each_of[r];
-  for (int j = lane; j < g.k; j += LANES) {
-    const int e = row != nullptr ? g.leaves[d * g.k + j] : -1;
-    picked[j] = (uint32_t)e < (uint32_t)g.n_leaves ? e : -1;
+  int picked[kSlotsOf<LANES>];
+#pragma unroll
+  for (int t = 0; t < kSlotsOf<LANES>; ++t) {
+    const int j = lane + t * LANES, e = row != nullptr && j < g.k ? g.leaves[d * g.k + j] : -1;
+    picked[t] = (uint32_t)e < (uint32_t)g.n_leaves ? e : -1;
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   const bool all = !g.sigmoid && !g.renormalise;
   float p[PER], top = 0.0f, inverse = 0.0f;
 #pragma unroll
@@ -374,25 +430,25 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteArgs g)
     inner += s.score[t] * dg[t];
   }
   inner = over_lanes<LANES>(inner, Sum{});
+  float each[Slots<LANES>::kMost];
 #pragma unroll
   for (int t = 0; t < Slots<LANES>::kMost; ++t) {
-    const int j = lane + t * LANES;
-    if (j >= g.k) break;
     float v = g.scale * s.score[t] * (g.renormalise ? dg[t] - inner : dg[t]);
     if (g.sigmoid) v *= sigmoid(-s.logit[t]);
-    each[j] = s.logit[t] > -INFINITY ? v : 0.0f;
+    each[t] = s.logit[t] > -INFINITY ? v : 0.0f;
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  if (row == nullptr) return;
   float out[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) out[i] = all ? -g.scale * (p[i] * inverse) * inner : 0.0f;
-  for (int j = 0; j < g.k; ++j) {
-    const int at = picked[j] - lane * PER;
-    const float v = each[j];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) out[i] += at == i ? v : 0.0f;
-  }
+  for (int t = 0; t < Slots<LANES>::kMost; ++t)
+    for (int j = 0; j < LANES && j + t * LANES < g.k; ++j) {
+      const int at = __shfl(s.column[t], j, LANES) - lane * PER;
+      const float v = __shfl(each[t], j, LANES);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) out[i] += at == i ? v : 0.0f;
+    }
+  if (row == nullptr) return;
   T* to = (T*)g.dlogits + d * g.ld_out + lane * PER;
   T t[PER];
 #pragma unroll

@@ -89,21 +89,21 @@ __device__ __forceinline__ f32x4 load4_any(const T* p, int valid) {
 template <typename T, typename H, bool DOTS>
 struct ToSlots {
   typedef H Out;
-  static constexpr bool kScaled = false, kHalves = sizeof(H) == 2, kFinished = kHalves || DOTS;
+  static constexpr bool kScaled = false, kHalves = sizeof(H) == 2, kFinished = kHalves || DOTS, kDots = DOTS;
   const T* bias;
   H* out;
   int64_t ld;
   __device__ __forceinline__ int place(const RoutedArgs<T>& g, int p) const { return g.pair_idx[p]; }
   __device__ __forceinline__ float add(int64_t column) const { return bias ? (float)bias[column] : 0.0f; }
   template <int TN>
-  __device__ __forceinline__ void finish(const RoutedArgs<T>& g, int p, int pair, int col, int cols, f32x4 (&v)[TN]) const {
+  __device__ __forceinline__ void finish(const RoutedArgs<T>& g, int row, int pair, int col, int cols, f32x4 (&v)[TN]) const {
     static_assert(TN * 16 == block_columns<T>, "a wavefront's columns");
     const int l = threadIdx.x & 63;
     const int64_t block = (int64_t)pair * g.blocks + col / (TN * 16);
     if constexpr (DOTS) {
       float dot = 0.0f;
       if (pair >= 0) {
-        const T* x = row_of(g.x, g.row_idx[p], g.ld_x);
+        const T* x = row_of(g.x, row, g.ld_x);
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
           const int n = col + 16 * j + 4 * (l >> 4);
@@ -126,7 +126,7 @@ struct ToSlots {
 template <typename T>
 struct ToGatedRows {
   typedef T Out;
-  static constexpr bool kScaled = false, kFinished = true;
+  static constexpr bool kScaled = false, kFinished = true, kDots = false;
   const T* bias;
   T* out;
   int64_t ld;
@@ -150,9 +150,9 @@ __global__ void __launch_bounds__(S::NT, 2) routed_product_kernel(const RoutedAr
   typedef typename SlotOf<T>::Type H;
   __shared__ __align__(16) char lds[S::kLdsBytes];
   if constexpr (WHAT == Leaves::kRows) {
-    leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, ToGatedRows<T>{g.bias, g.y, g.ld_y}, g.d_out);
+    leaf_rows_product<S, typename S::RowsB, 1, S::BM < 256>(lds, g, g.x, g.ld_x, g.d_in, ToGatedRows<T>{g.bias, g.y, g.ld_y}, g.d_out);
   } else {
-    leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, ToSlots<T, H, false>{g.bias, (H*)g.slots, g.ld_slots}, g.d_out);
+    leaf_rows_product<S, typename S::RowsB, 1, S::BM < 256>(lds, g, g.x, g.ld_x, g.d_in, ToSlots<T, H, false>{g.bias, (H*)g.slots, g.ld_slots}, g.d_out);
   }
 }
 
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(S::NT, 2) routed_grad_input_kernel(const Route
   typedef typename S::T T;
   typedef typename SlotOf<T>::Type H;
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::ColumnsB, 1>(lds, g, g.dy, g.ld_dy, g.d_out, ToSlots<T, H, DOTS>{nullptr, (H*)g.slots, g.ld_slots}, g.d_in);
+  leaf_rows_product<S, typename S::ColumnsB, 1, S::BM < 256>(lds, g, g.dy, g.ld_dy, g.d_out, ToSlots<T, H, DOTS>{nullptr, (H*)g.slots, g.ld_slots}, g.d_in);
 }
 
 // ---------------------------------------------------------------- sums of slots
@@ -257,21 +257,49 @@ __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs<O> g) {
     }
   }
   if (g.dgates == nullptr) return;
-  for (int j = 0; j < g.k; ++j) {
-    const int leaf = g.leaves[p0 + j];
-    const bool there = (uint32_t)leaf < (uint32_t)g.n_leaves;
-    float dot = 0.0f;
-    if (there) {
-      for (int b = l; b < g.blocks; b += LANES) dot += g.dots[(p0 + j) * g.blocks + b];
-      if (g.bias != nullptr)
-        for (int c = l * 4; c < g.d_out; c += LANES * 4) {
-          const f32x4 b = load4_any(g.bias + (int64_t)leaf * g.d_out + c, g.d_out - c), dy = load4_any(g.dy + d * g.ld_dy + c, g.d_out - c);
+  constexpr int pairs = 4, m = kChunk<O>;  // four pairs of a row at a time
+  const O* dy = g.dy + d * g.ld_dy;
+  for (int j0 = 0; j0 < g.k; j0 += pairs) {
+    int leaf[pairs];
+    float dot[pairs];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) dot = __builtin_fmaf(b[e], dy[e], dot);
-        }
+    for (int i = 0; i < pairs; ++i) {
+      const int e = j0 + i < g.k ? g.leaves[p0 + j0 + i] : -1;
+      leaf[i] = (uint32_t)e < (uint32_t)g.n_leaves ? e : -1;
+      dot[i] = 0.0f;
     }
-    dot = over_row<LANES>(dot);
-    if (l == 0) g.dgates[p0 + j] = there ? dot : 0.0f;
+    for (int b = l; b < g.blocks; b += LANES) {
+#pragma unroll
+      for (int i = 0; i < pairs; ++i)
+        if (leaf[i] >= 0) dot[i] += g.dots[(p0 + j0 + i) * g.blocks + b];
+    }
+    if (g.bias != nullptr) {
+      for (int c = l * m; c < g.d_out; c += LANES * m) {
+        O y[m], w[pairs][m];
+        if (c + m <= g.d_out) {
+          __builtin_memcpy(y, dy + c, sizeof y);
+#pragma unroll
+          for (int i = 0; i < pairs; ++i) __builtin_memcpy(w[i], g.bias + (int64_t)(leaf[i] < 0 ? 0 : leaf[i]) * g.d_out + c, sizeof y);
+        } else {
+#pragma unroll
+          for (int e = 0; e < m; ++e) {
+            y[e] = c + e < g.d_out ? dy[c + e] : (O)0.0f;
+#pragma unroll
+            for (int i = 0; i < pairs; ++i)
+              w[i][e] = c + e < g.d_out ? g.bias[(int64_t)(leaf[i] < 0 ? 0 : leaf[i]) * g.d_out + c + e] : (O)0.0f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < pairs; ++i)
+#pragma unroll
+          for (int e = 0; e < m; ++e) dot[i] = __builtin_fmaf((float)w[i][e], (float)y[e], dot[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < pairs; ++i) {
+      const float all = over_row<LANES>(dot[i]);
+      if (l == 0 && j0 + i < g.k) g.dgates[p0 + j0 + i] = leaf[i] >= 0 ? all : 0.0f;
+    }
   }
 }
 

@@ -38,11 +38,13 @@ int route_check(const void* logits, int64_t ld, int64_t n_rows, int32_t n_leaves
 
 template <typename T, int LANES, int PER>
 int launch_route(const RouteArgs& g, bool grad, hipStream_t s) {
-  const unsigned blocks = (unsigned)ceil_div(g.n_rows, gbdt_router::kThreads / LANES);
+  const dim3 blocks((unsigned)ceil_div(g.n_rows, gbdt_router::kThreads / LANES)), threads(gbdt_router::kThreads);
   if (grad) {
-    gbdt_router::route_grad_kernel<T, LANES, PER><<<dim3(blocks), dim3(gbdt_router::kThreads), 0, s>>>(g);
+    gbdt_router::route_grad_kernel<T, LANES, PER><<<blocks, threads, 0, s>>>(g);
+  } else if (g.bias == nullptr && g.group_best == 1) {
+    gbdt_router::route_kernel<T, LANES, PER, false><<<blocks, threads, 0, s>>>(g);
   } else {
-    gbdt_router::route_kernel<T, LANES, PER><<<dim3(blocks), dim3(gbdt_router::kThreads), 0, s>>>(g);
+    gbdt_router::route_kernel<T, LANES, PER, true><<<blocks, threads, 0, s>>>(g);
   }
   LAUNCHED("routing");
   return GBDT_OK;
@@ -50,11 +52,10 @@ int launch_route(const RouteArgs& g, bool grad, hipStream_t s) {
 
 template <typename T>
 int route(const RouteArgs& g, bool grad, hipStream_t s) {
-  if (g.n_leaves <= 32) return launch_route<T, 8, 4>(g, grad, s);
   if (g.n_leaves <= 64) return launch_route<T, 16, 4>(g, grad, s);
-  if (g.n_leaves <= 128) return launch_route<T, 32, 4>(g, grad, s);
-  if (g.n_leaves <= 256) return launch_route<T, 64, 4>(g, grad, s);
-  if (g.n_leaves <= 512) return launch_route<T, 64, 8>(g, grad, s);
+  if (g.n_leaves <= 128) return launch_route<T, 16, 8>(g, grad, s);
+  if (g.n_leaves <= 256) return launch_route<T, 16, 16>(g, grad, s);
+  if (g.n_leaves <= 512) return launch_route<T, 32, 16>(g, grad, s);
   return launch_route<T, 64, 16>(g, grad, s);
 }
 
@@ -200,7 +201,7 @@ using Short = Shape<T, 32, 128, 1, 2, true>;
 
 template <class S, gbdt_routed::Leaves WHAT, typename T>
 int launch_routed_product(RoutedArgs<T>& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_out, S::NT, [&](dim3 blocks) {
+  return leaf_rows_launches<S>(g, g.d_out, S::NT, S::BM < 256, [&](dim3 blocks) {
     gbdt_routed::routed_product_kernel<S, WHAT><<<blocks, dim3(S::NT), 0, s>>>(g);
   });
 }
@@ -221,7 +222,7 @@ int routed_product(RoutedArgs<T>& g, hipStream_t s) {
 
 template <class S, typename T>
 int launch_routed_grad_input(RoutedArgs<T>& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_in, S::NT, [&](dim3 blocks) {
+  return leaf_rows_launches<S>(g, g.d_in, S::NT, S::BM < 256, [&](dim3 blocks) {
     if (g.dots) {
       gbdt_routed::routed_grad_input_kernel<S, true><<<blocks, dim3(S::NT), 0, s>>>(g);
     } else {
@@ -471,7 +472,7 @@ using gbdt_code::Place;
 
 template <class S, typename O, Place WHERE>
 int launch_code_product(CodeArgs& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_out, S::NT, [&](dim3 blocks) {
+  return leaf_rows_launches<S>(g, g.d_out, S::NT, S::BM < 256, [&](dim3 blocks) {
     gbdt_code::code_product_kernel<S, O, WHERE><<<blocks, dim3(S::NT), 0, s>>>(g);
   });
 }
