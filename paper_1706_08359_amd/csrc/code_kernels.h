@@ -131,8 +131,9 @@ struct ToScaled {
   __device__ __forceinline__ float row_scale(const CodeArgs& g, int p) const { return row_scales[row(g, p)]; }
   __device__ __forceinline__ float column_scale(int64_t column) const { return col_scales[column]; }
   __device__ __forceinline__ float add(int64_t column) const { return bias ? bias[column] : 0.0f; }
+  struct Beside {};
   template <int TN>
-  __device__ __forceinline__ void finish(const CodeArgs& g, int, int pair, int col, int cols, f32x4 (&v)[TN]) const {
+  __device__ __forceinline__ void finish(const CodeArgs& g, int pair, int col, int cols, const Beside (&)[TN], f32x4 (&v)[TN]) const {
     if constexpr (WHERE == Place::kGatedRow) {
       const float gate = pair >= 0 ? g.gates[pair] : 0.0f;
 #pragma unroll
@@ -151,7 +152,7 @@ __global__ void __launch_bounds__(S::NT, 2) code_product_kernel(const CodeArgs g
   typedef ToScaled<O, WHERE> To;
   const bool slot = WHERE == Place::kSlot;
   const To to = {(typename To::Out*)(slot ? g.slots : g.out), slot ? g.ld_slots : g.ld_out, g.row_scales, g.col_scales, g.add};
-  leaf_rows_product<S, typename S::RowsB, 1, S::BM < 256>(lds, g, g.x, g.ld_x, g.d_in, to, g.d_out);
+  rows_product<S, typename S::RowsB>(lds, g, g.x, g.ld_x, g.d_in, to, g.d_out);
 }
 
 // A few rows: OUTPUTS outputs of one row a wavefront, sums of four products an instruction.  LISTED: one leaf a row, by position in

@@ -136,15 +136,117 @@ struct ToRows {
   __device__ __forceinline__ float add(int64_t column) const { return bias ? (float)bias[column] : 0.0f; }
 };
 
+// Where a row of a tile goes, and what it is multiplied by (To::kScaled) or which row it is (To::kDots).
+struct RowPlace {
+  int id;  // -1 for none
+  union {
+    float factor;
+    int row;
+  };
+};
+template <class G, class To>
+__device__ __forceinline__ RowPlace place_of(const G& g, const To& to, int p, int end) {
+  static_assert(!(To::kScaled && To::kDots), "");
+  RowPlace r;
+  r.id = p < end ? to.place(g, p) : -1;
+  r.row = 0;
+  if constexpr (To::kScaled) r.factor = r.id >= 0 ? to.row_scale(g, p) : 0.0f;
+  if constexpr (To::kDots) r.row = r.id >= 0 ? g.row_idx[p] : 0;
+  return r;
+}
+
+// Those of a lane's rows of its blocks, kept in registers.
+template <class S>
+struct Places {
+  RowPlace at[S::TM];
+  template <class G, class To>
+  __device__ __forceinline__ void fetch(const G& g, const To& to, int p0, int end) {
+    const int m0 = p0 + (thread_of<S::NT>() >> 6) / S::WN * (S::TM * 16) + (threadIdx.x & 15);
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) at[i] = place_of(g, to, m0 + 16 * i, end);
+  }
+  __device__ __forceinline__ RowPlace operator()(int i) const { return at[i]; }
+};
+
+// Of a whole tile, kept in local memory.
+template <class S>
+struct TilePlaces {
+  const RowPlace* of;  // [BM]
+  __device__ __forceinline__ RowPlace operator()(int i) const {
+    return of[(thread_of<S::NT>() >> 6) / S::WN * (S::TM * 16) + (threadIdx.x & 15) + 16 * i];
+  }
+};
+
+// A tile's results to their rows, through the last stage.
+template <class S, class G, class To, class Where>
+__device__ __forceinline__ void store_rows(char* lds, const G& g, const To& to, typename S::Acc (&acc)[S::TM][S::TN], const Where& places,
+                                           int leaf, int col, int cols) {
+  typedef typename S::Acc Acc;
+  const int w = thread_of<S::NT>() >> 6;
+  const int l = threadIdx.x & 63, wave_col = col + w % S::WN * (S::TN * 16);
+  f32x4 add[S::TN], scale[To::kScaled ? S::TN : 1];
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int n = wave_col + 16 * j + 4 * (l >> 4) + r;
+      add[j][r] = n < cols ? to.add((int64_t)leaf * cols + n) : 0.0f;
+      if constexpr (To::kScaled) scale[j][r] = n < cols ? to.column_scale((int64_t)leaf * cols + n) : 0.0f;
+    }
+  auto value = [&](int i, int j) {
+    if constexpr (To::kScaled) {
+      f32x4 v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = __builtin_fmaf((float)acc[i][j][r] * places(i).factor, scale[j][r], add[j][r]);
+      return v;
+    } else {
+      return acc[i][j] + add[j];
+    }
+  };
+  if constexpr (To::kFinished) {
+    constexpr int at_once = To::kDots ? 2 : 1;  // rows whose x is on its way together
+#pragma unroll
+    for (int i0 = 0; i0 < S::TM; i0 += at_once) {
+      typename To::Beside x[at_once][S::TN];
+      if constexpr (To::kDots) {
+#pragma unroll
+        for (int i = 0; i < at_once; ++i) to.template beside<S::TN>(g, places(i0 + i).row, wave_col, cols, x[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < at_once; ++i) {
+        f32x4 v[S::TN];
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) v[j] = value(i0 + i, j);
+        to.template finish<S::TN>(g, places(i0 + i).id, wave_col, cols, x[i], v);
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) acc[i0 + i][j] = __builtin_bit_cast(Acc, v[j]);
+      }
+    }
+  }
+  store_tile<S, typename To::Out, S::TM, S::TN>(
+      lds + S::kLastStage,
+      [&](int i, int j) {
+        if constexpr (To::kFinished) {
+          return __builtin_bit_cast(f32x4, acc[i][j]);
+        } else {
+          return value(i, j);
+        }
+      },
+      [&](int i, int r) {
+        const int d = __shfl(places(i).id, r);
+        return d >= 0 && to.out != nullptr ? to.out + (int64_t)d * to.ld : (typename To::Out*)nullptr;
+      },
+      wave_col, cols);
+}
+
 // The rows of one tile of positions times a matrix of the leaf, g.cols_per column tiles one after another; the next one's
 // first steps are on their way while one's values are stored.  B: the matrix' orientation, k its length along k.
 // To::kScaled: values are multiplied by a factor of their position and one of the leaf's column.
-// To::kFinished: a row's values of this wavefront's columns go through to.finish before they are stored, which is given the position's
-// row if To::kDots.
+// To::kFinished: a row's values of this wavefront's columns go through to.finish before they are stored; To::kDots: beside what
+// to.beside reads of the position's row.
 // GROUPS > 1: as many times the tile's threads take a part of k each, all of as many steps, and the first adds up; one column
 // tile a workgroup then, since the other groups leave after it.
-// MANY: a workgroup may have several column tiles (without it the next one's state takes no registers).
-template <class S, class B, int GROUPS, bool MANY, typename T, class G, class To>
+template <class S, class B, int GROUPS, typename T, class G, class To>
 __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T* in, int64_t ld_in, int k, const To& to, int cols) {
   typedef typename S::Acc Acc;
   const uint32_t t = g.first + xcd_tile(blockIdx.x, gridDim.x);
@@ -158,18 +260,8 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T
   const int col_last = cols < col_first + (int)g.cols_per * S::BN ? cols : col_first + (int)g.cols_per * S::BN;
   const ListRows<T> rows_a = list_rows(in, ld_in, k, g, end);
   const PlainRows<T> rows_b = plain_rows(g.w + (int64_t)leaf * g.d_out * g.d_in, g.d_in, g.d_out, g.d_in);
-  const int w = thread_of<S::NT>() >> 6;
-  int ids[S::TM];  // places of this lane's blocks, -1 for none
-  float factor[To::kScaled ? S::TM : 1];
-  int row_of_id[To::kDots ? S::TM : 1];
-  const int m0 = p0 + w / S::WN * (S::TM * 16) + (threadIdx.x & 15);
-#pragma unroll
-  for (int i = 0; i < S::TM; ++i) {
-    const int p = m0 + 16 * i;
-    ids[i] = p < end ? to.place(g, p) : -1;
-    if constexpr (To::kScaled) factor[i] = ids[i] >= 0 ? to.row_scale(g, p) : 0.0f;
-    if constexpr (To::kDots) row_of_id[i] = ids[i] >= 0 ? g.row_idx[p] : 0;
-  }
+  Places<S> places;
+  places.fetch(g, to, p0, end);
   const int group = GROUPS > 1 ? (int)threadIdx.x / S::NT : 0;
   lds += group * S::kLdsBytes;
   const int part = GROUPS > 1 ? ((k + GROUPS - 1) / GROUPS + S::kStep - 1) / S::kStep * S::kStep : k;
@@ -182,7 +274,7 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T
     tile_begin<S>(lds, a, b, rows_a, rows_b, k0, k0 + part);
   };
   begin_columns(col_first);
-  for (int col = col_first; col < col_last; col = MANY ? col + S::BN : col_last) {
+  for (int col = col_first; col < col_last; col += S::BN) {
     Acc acc[S::TM][S::TN];
     zeros<S>(acc);
     tile_run<S, true>(lds, a, b, rows_a, rows_b, k0, k0 + part, acc, Nothing{});
@@ -200,54 +292,116 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T
 #pragma unroll
         for (int v = 0; v < values; ++v)
           acc[v / S::TN][v % S::TN] += ((const Acc*)(lds + other * S::kLdsBytes))[v * S::NT + thread_of<S::NT>()];
-    } else if (MANY && col + S::BN < col_last) {
+    } else if (col + S::BN < col_last) {
       begin_columns(col + S::BN);
     }
-    const int l = threadIdx.x & 63, wave_col = col + w % S::WN * (S::TN * 16);
-    f32x4 add[S::TN], scale[To::kScaled ? S::TN : 1];
+    store_rows<S>(lds, g, to, acc, places, leaf, col, cols);
+  }
+}
+
+// The same by workgroups that stay: as many as there are places for, each goes through tiles of rows and columns, and the next
+// one's ids are on their way while one is multiplied, its first steps while one's values are stored.  (Where a compute unit holds one
+// workgroup, nothing else hides a tile's beginning and end.)  The tiles of an XCD are neighbours.  first: room for the leaves' first tiles
+// and positions, and for rows' places.
+constexpr int kStayLeaves = 1024;
+template <class S>
+struct StayTable {
+  int tile[kStayLeaves + 1], begin[kStayLeaves + 1];
+  RowPlace rows[3][S::BM];  // of three tiles in turn: what is written while one is multiplied is read no more by a wavefront behind
+};
+template <class S, class B, typename T, class G, class To>
+__device__ __forceinline__ void leaf_rows_stay(char* lds, StayTable<S>& first, const G& g, const T* in, int64_t ld_in, int k, const To& to, int cols) {
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    int base = 0;
+    for (int l0 = 0; l0 <= g.n_leaves; l0 += 64) {
+      const int l = l0 + lane;
+      const int begin = offset_at(g.offsets, l < g.n_leaves ? l : g.n_leaves, g.n_positions);
+      const int end = offset_at(g.offsets, l + 1 < g.n_leaves ? l + 1 : g.n_leaves, g.n_positions);
+      const int n = l < g.n_leaves && end > begin ? (end - begin + S::BM - 1) / S::BM : 0;
+      int sum = n;
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int n = wave_col + 16 * j + 4 * (l >> 4) + r;
-        add[j][r] = n < cols ? to.add((int64_t)leaf * cols + n) : 0.0f;
-        if constexpr (To::kScaled) scale[j][r] = n < cols ? to.column_scale((int64_t)leaf * cols + n) : 0.0f;
+      for (int m = 1; m < 64; m <<= 1) {
+        const int other = __shfl_up(sum, m);
+        if (lane >= m) sum += other;
       }
-    auto value = [&](int i, int j) {
-      if constexpr (To::kScaled) {
-        f32x4 v;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = __builtin_fmaf((float)acc[i][j][r] * factor[i], scale[j][r], add[j][r]);
-        return v;
-      } else {
-        return acc[i][j] + add[j];
-      }
-    };
-    if constexpr (To::kFinished) {
-#pragma unroll
-      for (int i = 0; i < S::TM; ++i) {
-        f32x4 v[S::TN];
-#pragma unroll
-        for (int j = 0; j < S::TN; ++j) v[j] = value(i, j);
-        to.template finish<S::TN>(g, row_of_id[To::kDots ? i : 0], ids[i], wave_col, cols, v);
-#pragma unroll
-        for (int j = 0; j < S::TN; ++j) acc[i][j] = __builtin_bit_cast(Acc, v[j]);
-      }
+      if (l <= g.n_leaves) first.tile[l] = base + sum - n, first.begin[l] = begin;
+      base += __shfl(sum, 63);
     }
-    store_tile<S, typename To::Out, S::TM, S::TN>(
-        lds + S::kLastStage,
-        [&](int i, int j) {
-          if constexpr (To::kFinished) {
-            return __builtin_bit_cast(f32x4, acc[i][j]);
-          } else {
-            return value(i, j);
-          }
-        },
-        [&](int i, int r) {
-          const int d = __shfl(ids[i], r);
-          return d >= 0 && to.out != nullptr ? to.out + (int64_t)d * to.ld : (typename To::Out*)nullptr;
-        },
-        wave_col, cols);
+  }
+  __syncthreads();
+  const int64_t tiles = (int64_t)first.tile[g.n_leaves] * g.col_tiles;
+  const int xcd = blockIdx.x % 8;
+  const int64_t last = tiles * (xcd + 1) / 8, step = gridDim.x / 8;
+  int64_t t = tiles * xcd / 8 + blockIdx.x / 8;
+  struct At {
+    int leaf, p0, end, col;
+  };
+  auto locate = [&](int64_t tile) {
+    const int row_tile = (int)((uint32_t)tile / g.col_tiles);  // (fewer than 2^31)
+    int lo = 0, hi = g.n_leaves;  // the last leaf whose first tile is no later (leaves without rows have the next one's)
+    while (hi - lo > 1) {
+      const int stride = (hi - lo + 63) / 64, i = lo + (int)(threadIdx.x & 63) * stride;
+      const int n = __popcll(__ballot(i < hi && first.tile[i] <= row_tile));
+      lo += (n - 1) * stride;
+      hi = lo + stride < hi ? lo + stride : hi;
+    }
+    At at;
+    at.leaf = __builtin_amdgcn_readfirstlane(lo);
+    at.p0 = first.begin[at.leaf] + (row_tile - first.tile[at.leaf]) * S::BM;
+    at.end = first.begin[at.leaf + 1];
+    at.col = (int)((uint32_t)tile - (uint32_t)row_tile * g.col_tiles) * S::BN;
+    return at;
+  };
+  typename S::RowsA a;
+  B b;
+  typename S::RowsA::Ids ids;
+  auto fetch = [&](const At& at, int turn) {
+    S::RowsA::fetch(list_rows(in, ld_in, k, g, at.end), at.p0, ids);
+    if ((int)threadIdx.x < S::BM) first.rows[turn][threadIdx.x] = place_of(g, to, at.p0 + (int)threadIdx.x, at.end);
+  };
+  auto rows_a = [&](const At& at) { return list_rows(in, ld_in, k, g, at.end); };
+  auto rows_b = [&](const At& at) { return plain_rows(g.w + (int64_t)at.leaf * g.d_out * g.d_in, g.d_in, g.d_out, g.d_in); };
+  auto begin = [&](const At& at) {
+    a.init(rows_a(at), at.p0, 0, 0, k, ids);
+    b.init(rows_b(at), at.col, cols, 0, k);
+    tile_begin<S>(lds, a, b, rows_a(at), rows_b(at), 0, k);
+  };
+  if (t >= last) return;
+  static_assert(S::NT >= S::BM, "a thread a row");
+  At at = locate(t);
+  fetch(at, 0);
+  begin(at);
+  for (int turn = 0;;) {
+    t += step;
+    const bool more = t < last;
+    At next = at;
+    const int next_turn = turn == 2 ? 0 : turn + 1;
+    if (more) {
+      next = locate(t);
+      fetch(next, next_turn);
+    }
+    typename S::Acc acc[S::TM][S::TN];
+    zeros<S>(acc);
+    tile_run<S, true>(lds, a, b, rows_a(at), rows_b(at), 0, k, acc, Nothing{});
+    if (more) begin(next);
+    store_rows<S>(lds, g, to, acc, TilePlaces<S>{first.rows[turn]}, at.leaf, at.col, cols);
+    if (!more) return;
+    at = next;
+    turn = next_turn;
+  }
+}
+
+// By workgroups that stay, in tiles so large that a compute unit holds one; by others in smaller ones.
+template <class S>
+constexpr bool kStays = S::BM >= 256;
+template <class S, class B, typename T, class G, class To>
+__device__ __forceinline__ void rows_product(char* lds, const G& g, const T* in, int64_t ld_in, int k, const To& to, int cols) {
+  if constexpr (kStays<S>) {
+    __shared__ StayTable<S> first;
+    leaf_rows_stay<S, B>(lds, first, g, in, ld_in, k, to, cols);
+  } else {
+    leaf_rows_product<S, B, 1>(lds, g, in, ld_in, k, to, cols);
   }
 }
 
@@ -258,14 +412,14 @@ __device__ __forceinline__ void leaf_rows_product(char* lds, const G& g, const T
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_product_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::RowsB, 1, true>(lds, g, g.x, g.ld_x, g.d_in, ToRows<typename S::T>{g.bias, g.y, g.ld_y}, g.d_out);
+  leaf_rows_product<S, typename S::RowsB, 1>(lds, g, g.x, g.ld_x, g.d_in, ToRows<typename S::T>{g.bias, g.y, g.ld_y}, g.d_out);
 }
 
 // The same where there are too few tiles for the compute units: a tile's k is split among GROUPS times the threads.
 template <class S, int GROUPS>
 __global__ void __launch_bounds__(S::NT* GROUPS) leaf_product_split_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes * GROUPS];
-  leaf_rows_product<S, typename S::RowsB, GROUPS, false>(lds, g, g.x, g.ld_x, g.d_in, ToRows<typename S::T>{g.bias, g.y, g.ld_y}, g.d_out);
+  leaf_rows_product<S, typename S::RowsB, GROUPS>(lds, g, g.x, g.ld_x, g.d_in, ToRows<typename S::T>{g.bias, g.y, g.ld_y}, g.d_out);
 }
 
 // dx: rows of dy (k = output along memory) times w, whose rows are k.  Bound by its stores, d_in values a row, which a tile's
@@ -274,7 +428,7 @@ __global__ void __launch_bounds__(S::NT* GROUPS) leaf_product_split_kernel(const
 template <class S>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_input_kernel(const LeafArgs<typename S::T> g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::ColumnsB, 1, true>(lds, g, g.dy, g.ld_dy, g.d_out, ToRows<typename S::T>{nullptr, g.dx, g.ld_dx}, g.d_in);
+  leaf_rows_product<S, typename S::ColumnsB, 1>(lds, g, g.dy, g.ld_dy, g.d_out, ToRows<typename S::T>{nullptr, g.dx, g.ld_dx}, g.d_in);
 }
 
 // A few positions (a row or a few answered at once): a wavefront takes OUTPUTS outputs of one position, each lane a chunk of k

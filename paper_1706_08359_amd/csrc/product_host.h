@@ -88,6 +88,18 @@ int leaf_rows_launches(gbdt_leaf::LeafArgs<T>& g, int64_t cols, int threads, boo
   return GBDT_OK;
 }
 
+// The same by workgroups that stay (gbdt_leaf::rows_product): one a compute unit.
+template <class S, typename T, class Launch>
+int rows_launches(gbdt_leaf::LeafArgs<T>& g, int64_t cols, const Launch& launch) {
+  if constexpr (!gbdt_leaf::kStays<S>) return leaf_rows_launches<S>(g, cols, S::NT, true, launch);
+  const int64_t col_tiles = ceil_div(cols, S::BN), n = ((int64_t)g.n_positions / S::BM + g.n_leaves) * col_tiles;
+  if (n > kMaxTiles || g.n_leaves > gbdt_leaf::kStayLeaves) return GBDT_EUNSUPPORTED;
+  g.col_tiles = (uint32_t)col_tiles;
+  launch(dim3((unsigned)std::min(round_up(n, 8), std::max<int64_t>(8, gbdt_internal::cu_count() / 8 * 8))));
+  LAUNCHED("a product of the leaves");
+  return GBDT_OK;
+}
+
 // Leaves long enough for tiles of 256 rows, columns for more than one of 128, and such tiles for all compute units.  (100,000 x
 // 256 -> 2,000, gradient of the input, leaves of 392 rows on average: 277 us against 318 us in tiles of 128.  2,000 x 2,000 ->
 // 256 in one leaf, 8 tiles: 42 us against 12 in small ones.)

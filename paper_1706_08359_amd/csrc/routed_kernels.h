@@ -95,22 +95,36 @@ struct ToSlots {
   int64_t ld;
   __device__ __forceinline__ int place(const RoutedArgs<T>& g, int p) const { return g.pair_idx[p]; }
   __device__ __forceinline__ float add(int64_t column) const { return bias ? (float)bias[column] : 0.0f; }
+  struct Beside {
+    T x[4];
+  };
+  // x's values at this lane's columns, zeros past the last.
   template <int TN>
-  __device__ __forceinline__ void finish(const RoutedArgs<T>& g, int row, int pair, int col, int cols, f32x4 (&v)[TN]) const {
+  __device__ __forceinline__ void beside(const RoutedArgs<T>& g, int row, int col, int cols, Beside (&to)[TN]) const {
+    const T* x = row_of(g.x, row, g.ld_x);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int n = col + 16 * j + 4 * (int)((threadIdx.x & 63) >> 4);
+      if (n + 4 <= cols) {
+        __builtin_memcpy(to[j].x, x + n, sizeof to[j].x);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) to[j].x[r] = n + r < cols ? x[n + r] : (T)0.0f;
+      }
+    }
+  }
+  template <int TN>
+  __device__ __forceinline__ void finish(const RoutedArgs<T>& g, int pair, int col, int cols, const Beside (&x)[TN], f32x4 (&v)[TN]) const {
     static_assert(TN * 16 == block_columns<T>, "a wavefront's columns");
     const int l = threadIdx.x & 63;
     const int64_t block = (int64_t)pair * g.blocks + col / (TN * 16);
     if constexpr (DOTS) {
       float dot = 0.0f;
-      if (pair >= 0) {
-        const T* x = row_of(g.x, row, g.ld_x);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const int n = col + 16 * j + 4 * (l >> 4);
-          const f32x4 xs = n < cols ? load4_any(x + n, cols - n) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int j = 0; j < TN; ++j) {
+        const int n = col + 16 * j + 4 * (l >> 4);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) dot = n + r < cols ? __builtin_fmaf(v[j][r], xs[r], dot) : dot;
-        }
+        for (int r = 0; r < 4; ++r) dot = n + r < cols ? __builtin_fmaf(v[j][r], (float)x[j].x[r], dot) : dot;
       }
       dot = over_groups(dot, false);
       if (l < 16 && pair >= 0 && col < cols) g.dots[block] = dot;
@@ -132,8 +146,9 @@ struct ToGatedRows {
   int64_t ld;
   __device__ __forceinline__ int place(const RoutedArgs<T>& g, int p) const { return g.pair_idx[p]; }
   __device__ __forceinline__ float add(int64_t column) const { return bias ? (float)bias[column] : 0.0f; }
+  struct Beside {};
   template <int TN>
-  __device__ __forceinline__ void finish(const RoutedArgs<T>& g, int, int pair, int, int, f32x4 (&v)[TN]) const {
+  __device__ __forceinline__ void finish(const RoutedArgs<T>& g, int pair, int, int, const Beside (&)[TN], f32x4 (&v)[TN]) const {
     const float gate = pair >= 0 ? g.gates[pair] : 0.0f;
 #pragma unroll
     for (int j = 0; j < TN; ++j) v[j] *= gate;
@@ -150,9 +165,9 @@ __global__ void __launch_bounds__(S::NT, 2) routed_product_kernel(const RoutedAr
   typedef typename SlotOf<T>::Type H;
   __shared__ __align__(16) char lds[S::kLdsBytes];
   if constexpr (WHAT == Leaves::kRows) {
-    leaf_rows_product<S, typename S::RowsB, 1, S::BM < 256>(lds, g, g.x, g.ld_x, g.d_in, ToGatedRows<T>{g.bias, g.y, g.ld_y}, g.d_out);
+    rows_product<S, typename S::RowsB>(lds, g, g.x, g.ld_x, g.d_in, ToGatedRows<T>{g.bias, g.y, g.ld_y}, g.d_out);
   } else {
-    leaf_rows_product<S, typename S::RowsB, 1, S::BM < 256>(lds, g, g.x, g.ld_x, g.d_in, ToSlots<T, H, false>{g.bias, (H*)g.slots, g.ld_slots}, g.d_out);
+    rows_product<S, typename S::RowsB>(lds, g, g.x, g.ld_x, g.d_in, ToSlots<T, H, false>{g.bias, (H*)g.slots, g.ld_slots}, g.d_out);
   }
 }
 
@@ -161,7 +176,7 @@ __global__ void __launch_bounds__(S::NT, 2) routed_grad_input_kernel(const Route
   typedef typename S::T T;
   typedef typename SlotOf<T>::Type H;
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  leaf_rows_product<S, typename S::ColumnsB, 1, S::BM < 256>(lds, g, g.dy, g.ld_dy, g.d_out, ToSlots<T, H, DOTS>{nullptr, (H*)g.slots, g.ld_slots}, g.d_in);
+  rows_product<S, typename S::ColumnsB>(lds, g, g.dy, g.ld_dy, g.d_out, ToSlots<T, H, DOTS>{nullptr, (H*)g.slots, g.ld_slots}, g.d_in);
 }
 
 // ---------------------------------------------------------------- sums of slots

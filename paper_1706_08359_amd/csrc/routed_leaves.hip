@@ -199,9 +199,15 @@ bool short_leaves(const gbdt_leaf::LeafArgs<T>& g) {
 template <typename T>
 using Short = Shape<T, 32, 128, 1, 2, true>;
 
+// Tiles of 256 rows need long leaves, and no more of them than a workgroup that stays has room for.
+template <typename T>
+bool long_leaves_of(const gbdt_leaf::LeafArgs<T>& g, int64_t cols, int64_t bn) {
+  return g.n_leaves <= gbdt_leaf::kStayLeaves && (bn < 256 || cols > 128) && long_leaves(g, cols, bn);
+}
+
 template <class S, gbdt_routed::Leaves WHAT, typename T>
 int launch_routed_product(RoutedArgs<T>& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_out, S::NT, S::BM < 256, [&](dim3 blocks) {
+  return rows_launches<S>(g, g.d_out, [&](dim3 blocks) {
     gbdt_routed::routed_product_kernel<S, WHAT><<<blocks, dim3(S::NT), 0, s>>>(g);
   });
 }
@@ -213,8 +219,8 @@ int routed_product(RoutedArgs<T>& g, hipStream_t s) {
     if (direct) {
       if (short_leaves(g)) return launch_routed_product<Short<T>, WHAT>(g, s);
       if (g.d_out <= 64) return launch_routed_product<Shape<T, 128, 64, 4, 1, true>, WHAT>(g, s);
-      if (wide_leaves(g, g.d_out)) return launch_routed_product<Wide<T>, WHAT>(g, s);
-      if (long_leaves(g, g.d_out, 128)) return launch_routed_product<Shape<T, 256, 128, 4, 2, true, false, 3>, WHAT>(g, s);
+      if (long_leaves_of(g, g.d_out, 256)) return launch_routed_product<Wide<T>, WHAT>(g, s);
+      if (long_leaves_of(g, g.d_out, 128)) return launch_routed_product<Shape<T, 256, 128, 4, 2, true, false, 3>, WHAT>(g, s);
     }
   }
   return direct ? launch_routed_product<Square<T>, WHAT>(g, s) : launch_routed_product<SquareAny<T>, WHAT>(g, s);
@@ -222,7 +228,7 @@ int routed_product(RoutedArgs<T>& g, hipStream_t s) {
 
 template <class S, typename T>
 int launch_routed_grad_input(RoutedArgs<T>& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_in, S::NT, S::BM < 256, [&](dim3 blocks) {
+  return rows_launches<S>(g, g.d_in, [&](dim3 blocks) {
     if (g.dots) {
       gbdt_routed::routed_grad_input_kernel<S, true><<<blocks, dim3(S::NT), 0, s>>>(g);
     } else {
@@ -236,7 +242,7 @@ int routed_grad_input(RoutedArgs<T>& g, hipStream_t s) {
   const bool direct = whole_chunks<T>(g.dy, g.ld_dy, g.d_out) && whole_chunks<T>(g.w, g.d_in, g.d_in);
   if constexpr (sizeof(T) == 2) {
     if (direct && short_leaves(g)) return launch_routed_grad_input<Short<T>>(g, s);
-    if (direct && wide_leaves(g, g.d_in)) return launch_routed_grad_input<Wide<T>>(g, s);
+    if (direct && long_leaves_of(g, g.d_in, 256)) return launch_routed_grad_input<Wide<T>>(g, s);
   }
   return direct ? launch_routed_grad_input<Square<T>>(g, s) : launch_routed_grad_input<SquareAny<T>>(g, s);
 }
@@ -472,7 +478,7 @@ using gbdt_code::Place;
 
 template <class S, typename O, Place WHERE>
 int launch_code_product(CodeArgs& g, hipStream_t s) {
-  return leaf_rows_launches<S>(g, g.d_out, S::NT, S::BM < 256, [&](dim3 blocks) {
+  return rows_launches<S>(g, g.d_out, [&](dim3 blocks) {
     gbdt_code::code_product_kernel<S, O, WHERE><<<blocks, dim3(S::NT), 0, s>>>(g);
   });
 }
@@ -481,8 +487,8 @@ template <typename O, Place WHERE>
 int code_tiles(CodeArgs& g, hipStream_t s) {
   if (short_leaves(g)) return launch_code_product<Short<int8_t>, O, WHERE>(g, s);
   if (g.d_out <= 64) return launch_code_product<Shape<int8_t, 128, 64, 4, 1, true>, O, WHERE>(g, s);
-  if (wide_leaves(g, g.d_out)) return launch_code_product<Shape<int8_t, 256, 256, 2, 4, true, true>, O, WHERE>(g, s);
-  if (long_leaves(g, g.d_out, 128)) return launch_code_product<Shape<int8_t, 256, 128, 4, 2, true, false, 3>, O, WHERE>(g, s);
+  if (long_leaves_of(g, g.d_out, 256)) return launch_code_product<Shape<int8_t, 256, 256, 2, 4, true, true>, O, WHERE>(g, s);
+  if (long_leaves_of(g, g.d_out, 128)) return launch_code_product<Shape<int8_t, 256, 128, 4, 2, true, false, 3>, O, WHERE>(g, s);
   return launch_code_product<Shape<int8_t, 128, 128, 2, 2, true, true>, O, WHERE>(g, s);
 }
 

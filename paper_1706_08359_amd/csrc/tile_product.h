@@ -147,18 +147,31 @@ struct RowOperand {
   static_assert(KB == 128 || KB == 64, "");
   static_assert(NT / kRowChunks % 8 == 0, "a thread's chunks lie in the same place of their rows");
 
+  // What init needs of the rows' ids: it may be asked for long before.
+  struct Ids {
+    int id[kPer];
+  };
   template <class Rows>
-  __device__ __forceinline__ void init(const Rows& rows, int r0, int /*limit*/, int k0, int k1) {
+  __device__ __forceinline__ static void fetch(const Rows& rows, int r0, Ids& ids) {
+    const int t = thread_of<NT>();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) ids.id[i] = i * NT + t < kSlots ? rows.fetch(r0 + (i * NT + t) / kRowChunks) : -1;
+  }
+  template <class Rows>
+  __device__ __forceinline__ void init(const Rows& rows, int r0, int limit, int k0, int k1) {
+    Ids ids;
+    fetch(rows, r0, ids);
+    init(rows, r0, limit, k0, k1, ids);
+  }
+  template <class Rows>
+  __device__ __forceinline__ void init(const Rows& rows, int r0, int /*limit*/, int k0, int k1, const Ids& ids) {
     const int t = thread_of<NT>();
     k_of = k0 + (t % kRowChunks ^ swizzle(t / kRowChunks)) * kChunk<T>;
     k_end = k1;
     end = rows.end;
-    int id[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) id[i] = i * NT + t < kSlots ? rows.fetch(r0 + (i * NT + t) / kRowChunks) : -1;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      row[i] = i * NT + t < kSlots ? rows.at(r0 + (i * NT + t) / kRowChunks, id[i]) : nullptr;
+      row[i] = i * NT + t < kSlots ? rows.at(r0 + (i * NT + t) / kRowChunks, ids.id[i]) : nullptr;
       if (DIRECT) row[i] = (row[i] != nullptr ? row[i] : rows.base) + k_of;
     }
   }
