@@ -908,10 +908,26 @@ SCORES = {"softmax": 0, "sigmoid": 1}   # gbdt_score
 
 def _here(*tensors):
     """All on the current device, whose stream and library the call takes."""
-    device = torch.cuda.current_device()
+    device = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.device.index != device:
+        if t is not None and t.get_device() != device:
             raise GbdtError(f"a tensor on {t.device}, the current device is cuda:{device}")
+
+
+def _out(t, shape, dtype, device, stream, name, make=torch.empty):
+    """(tensor, address) of a dense output: the caller's, or one made here, whose shape needs no checks."""
+    if t is not None:
+        return t, _dense(t, dtype, shape, name)
+    t = _made(make, shape, dtype, device, stream)
+    return t, t.data_ptr()
+
+
+def _out_rows(t, shape, dtype, device, stream, name, make=torch.empty):
+    """(tensor, address, distance of rows) of an output whose rows may lie apart."""
+    if t is not None:
+        return (t,) + _mat(t, dtype, shape[0], shape[1], name)
+    t = _made(make, shape, dtype, device, stream)
+    return t, t.data_ptr(), shape[1]
 
 
 def _score(score):
@@ -933,14 +949,12 @@ def gbdt_route(logits, k, choice_bias=None, score="softmax", n_groups=1, groups_
     b_p = None if choice_bias is None else _dense(choice_bias, torch.float32, (n_leaves,), "choice_bias")
     if not 0 < k <= n_leaves:
         raise GbdtError("k: between 1 and n_leaves")
-    if leaves_out is None:
-        leaves_out = _made(torch.empty, (n_rows, k), torch.int32, logits.device, stream)
-    if gates_out is None:
-        gates_out = _made(torch.empty, (n_rows, k), torch.float32, logits.device, stream)
+    device = logits.device
+    leaves_out, e_p = _out(leaves_out, (n_rows, k), torch.int32, device, stream, "leaves_out")
+    gates_out, g_p = _out(gates_out, (n_rows, k), torch.float32, device, stream, "gates_out")
     _here(logits, choice_bias, leaves_out, gates_out)
     _check(load().gbdt_route(l_p, ld, b_p, n_rows, n_leaves, code, _score(score), n_groups, groups_kept, group_best, k,
-                             1 if renormalise else 0, float(scale), _dense(leaves_out, torch.int32, (n_rows, k), "leaves_out"),
-                             _dense(gates_out, torch.float32, (n_rows, k), "gates_out"), _stream(stream)), "gbdt_route")
+                             1 if renormalise else 0, scale, e_p, g_p, _stream(stream)), "gbdt_route")
     return leaves_out, gates_out
 
 
@@ -954,11 +968,9 @@ def gbdt_route_grad(logits, leaves, dgates, score="softmax", renormalise=True, s
     l_p, ld = _mat(logits, logits.dtype, n_rows, n_leaves, "logits")
     e_p = _dense(leaves, torch.int32, (n_rows, k), "leaves")
     g_p = _dense(dgates, torch.float32, (n_rows, k), "dgates")
-    if dlogits_out is None:
-        dlogits_out = _made(torch.empty, (n_rows, n_leaves), logits.dtype, logits.device, stream)
-    o_p, ld_out = _mat(dlogits_out, logits.dtype, n_rows, n_leaves, "dlogits_out")
+    dlogits_out, o_p, ld_out = _out_rows(dlogits_out, (n_rows, n_leaves), logits.dtype, logits.device, stream, "dlogits_out")
     _here(logits, leaves, dgates, dlogits_out)
-    _check(load().gbdt_route_grad(l_p, ld, e_p, g_p, n_rows, n_leaves, code, _score(score), k, 1 if renormalise else 0, float(scale),
+    _check(load().gbdt_route_grad(l_p, ld, e_p, g_p, n_rows, n_leaves, code, _score(score), k, 1 if renormalise else 0, scale,
                                   o_p, ld_out, _stream(stream)), "gbdt_route_grad")
     return dlogits_out
 
@@ -983,9 +995,7 @@ def gbdt_mixture_product(x, weight, leaves, gates, bias=None, y_out=None, stream
     w_p = _dev(weight, x.dtype, "weight")
     b_p = None if bias is None else _dense(bias, x.dtype, (n_leaves, d_out), "bias")
     k, e_p, g_p = _slots(leaves, gates, n_rows)
-    if y_out is None:
-        y_out = _made(torch.empty, (n_rows, d_out), x.dtype, x.device, stream)
-    y_p, ld_y = _mat(y_out, x.dtype, n_rows, d_out, "y_out")
+    y_out, y_p, ld_y = _out_rows(y_out, (n_rows, d_out), x.dtype, x.device, stream, "y_out")
     _here(x, weight, leaves, gates, bias, y_out)
     _check(load().gbdt_mixture_product(x_p, ld_x, w_p, b_p, e_p, g_p, n_rows, k, n_leaves, d_in, d_out, code, y_p, ld_y,
                                        _stream(stream)), "gbdt_mixture_product")
@@ -1010,22 +1020,15 @@ def gbdt_mixture_product_grad(dy, x, weight, leaves, gates, bias=None, dx_out=No
     k, e_p, g_p = _slots(leaves, gates, n_rows)
     dx_p = dw_p = db_p = dg_p = None
     ld_dx = d_in
+    dtype, device = x.dtype, x.device
     if "x" in want:
-        if dx_out is None:
-            dx_out = _made(torch.empty, (n_rows, d_in), x.dtype, x.device, stream)
-        dx_p, ld_dx = _mat(dx_out, x.dtype, n_rows, d_in, "dx_out")
+        dx_out, dx_p, ld_dx = _out_rows(dx_out, (n_rows, d_in), dtype, device, stream, "dx_out")
     if "weight" in want:
-        if dweight_out is None:
-            dweight_out = _made(torch.empty, (n_leaves, d_out, d_in), x.dtype, x.device, stream)
-        dw_p = _dense(dweight_out, x.dtype, (n_leaves, d_out, d_in), "dweight_out")
+        dweight_out, dw_p = _out(dweight_out, (n_leaves, d_out, d_in), dtype, device, stream, "dweight_out")
     if "bias" in want:
-        if dbias_out is None:
-            dbias_out = _made(torch.empty, (n_leaves, d_out), x.dtype, x.device, stream)
-        db_p = _dense(dbias_out, x.dtype, (n_leaves, d_out), "dbias_out")
+        dbias_out, db_p = _out(dbias_out, (n_leaves, d_out), dtype, device, stream, "dbias_out")
     if "gates" in want:
-        if dgates_out is None:
-            dgates_out = _made(torch.empty, (n_rows, k), torch.float32, x.device, stream)
-        dg_p = _dense(dgates_out, torch.float32, (n_rows, k), "dgates_out")
+        dgates_out, dg_p = _out(dgates_out, (n_rows, k), torch.float32, device, stream, "dgates_out")
     _here(dy, x, weight, leaves, gates, bias, dx_out, dweight_out, dbias_out, dgates_out)
     _check(load().gbdt_mixture_product_grad(dy_p, ld_dy, x_p, ld_x, w_p, b_p, e_p, g_p, n_rows, k, n_leaves, d_in, d_out, code, dx_p,
                                             ld_dx, dw_p, db_p, dg_p, _stream(stream)), "gbdt_mixture_product_grad")
@@ -1050,14 +1053,10 @@ def gbdt_rows_quantize(x, codes_out=None, scales_out=None, stream=None):
         raise TypeError("x: expected [n_rows, n_cols]")
     n_rows, n_cols = x.shape
     x_p, ld_x = _mat(x, x.dtype, n_rows, n_cols, "x")
-    if codes_out is None:
-        codes_out = _made(torch.empty, (n_rows, code_columns(n_cols)), torch.int8, x.device, stream)
-    if scales_out is None:
-        scales_out = _made(torch.empty, (n_rows,), torch.float32, x.device, stream)
-    c_p, ld_c = _mat(codes_out, torch.int8, n_rows, code_columns(n_cols), "codes_out")
+    codes_out, c_p, ld_c = _out_rows(codes_out, (n_rows, code_columns(n_cols)), torch.int8, x.device, stream, "codes_out")
+    scales_out, s_p = _out(scales_out, (n_rows,), torch.float32, x.device, stream, "scales_out")
     _here(x, codes_out, scales_out)
-    _check(load().gbdt_rows_quantize(x_p, ld_x, n_rows, n_cols, code, c_p, ld_c, _dense(scales_out, torch.float32, (n_rows,), "scales_out"),
-                                     _stream(stream)), "gbdt_rows_quantize")
+    _check(load().gbdt_rows_quantize(x_p, ld_x, n_rows, n_cols, code, c_p, ld_c, s_p, _stream(stream)), "gbdt_rows_quantize")
     return codes_out, scales_out
 
 
@@ -1086,9 +1085,7 @@ def gbdt_leaf_product_codes(codes, scales, weight, weight_scales, leaf_offsets, 
     made here)."""
     n_rows, n_leaves, d_out, columns, operands = _codes(codes, scales, weight, weight_scales, bias, dtype)
     idx_p, off_p, n_positions = _leaf_lists(leaf_offsets, row_idx, n_leaves, n_rows)
-    if y_out is None:
-        y_out = _made(torch.zeros, (n_rows, d_out), dtype, codes.device, stream)
-    y_p, ld_y = _mat(y_out, dtype, n_rows, d_out, "y_out")
+    y_out, y_p, ld_y = _out_rows(y_out, (n_rows, d_out), dtype, codes.device, stream, "y_out", torch.zeros)
     _here(codes, scales, weight, weight_scales, leaf_offsets, row_idx, bias, y_out)
     _check(load().gbdt_leaf_product_codes(*operands, idx_p, off_p, n_positions, n_leaves, n_rows, columns, d_out, DTYPES[dtype], y_p, ld_y,
                                        _stream(stream)), "gbdt_leaf_product_codes")
@@ -1099,9 +1096,7 @@ def gbdt_mixture_product_codes(codes, scales, weight, weight_scales, leaves, gat
     """gbdt_mixture_product of 8-bit codes (see gbdt_leaf_product_codes).  Returns y_out [n_rows, d_out] of dtype."""
     n_rows, n_leaves, d_out, columns, operands = _codes(codes, scales, weight, weight_scales, bias, dtype)
     k, e_p, g_p = _slots(leaves, gates, n_rows)
-    if y_out is None:
-        y_out = _made(torch.empty, (n_rows, d_out), dtype, codes.device, stream)
-    y_p, ld_y = _mat(y_out, dtype, n_rows, d_out, "y_out")
+    y_out, y_p, ld_y = _out_rows(y_out, (n_rows, d_out), dtype, codes.device, stream, "y_out")
     _here(codes, scales, weight, weight_scales, leaves, gates, bias, y_out)
     _check(load().gbdt_mixture_product_codes(*operands, e_p, g_p, n_rows, k, n_leaves, columns, d_out, DTYPES[dtype], y_p, ld_y,
                                           _stream(stream)), "gbdt_mixture_product_codes")

@@ -57,10 +57,21 @@ __device__ __forceinline__ float over_lanes(float v, const Op& op) {
   }
   return v;
 }
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t bits = (uint64_t)__double_as_longlong(v);
+  const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, CTRL, 0xf, 0xf, true);
+  const uint32_t high = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(bits >> 32), CTRL, 0xf, 0xf, true);
+  return __longlong_as_double((long long)((uint64_t)high << 32 | low));
+}
 template <int LANES, class Op>
 __device__ __forceinline__ double over_lanes(double v, const Op& op) {
+  v = op(v, dpp<0xB1>(v));
+  if (LANES >= 4) v = op(v, dpp<0x4E>(v));
+  if (LANES >= 8) v = op(v, dpp<0x141>(v));
+  if (LANES >= 16) v = op(v, dpp<0x140>(v));
 #pragma unroll
-  for (int m = 1; m < LANES; m <<= 1) v = op(v, __shfl_xor(v, m));
+  for (int m = 16; m < LANES; m <<= 1) v = op(v, __shfl_xor(v, m));
   return v;
 }
 struct Max {
@@ -482,12 +493,26 @@ constexpr int kListWaves = 16;             // of the one workgroup that lists fe
 constexpr int kFewListLeaves = 1024;       // it takes that many leaves
 constexpr int kMaxListLeaves = 16384;
 
+// The leaves of kAhead x 64 pairs at once (-1: none), since each load would be waited for otherwise.
+constexpr int kAhead = 8;
+__device__ __forceinline__ void load_leaves(const ListArgs& g, int first, int end, int (&e)[kAhead]) {
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    const int p = first + i * 64 + (int)(threadIdx.x & 63);
+    e[i] = p < end ? g.leaves[p] : -1;
+  }
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) e[i] = (uint32_t)e[i] < (uint32_t)g.n_leaves ? e[i] : -1;
+}
+
 // Adds the run's pairs to a table.
 __device__ __forceinline__ void count_run(const ListArgs& g, int first, int end, int* table) {
-  const int lane = threadIdx.x & 63;
-  for (int p = first + lane; p < end; p += 64) {
-    const int e = g.leaves[p];
-    if ((uint32_t)e < (uint32_t)g.n_leaves) __hip_atomic_fetch_add(&table[e], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  for (int p = first; p < end; p += 64 * kAhead) {
+    int e[kAhead];
+    load_leaves(g, p, end, e);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (e[i] >= 0) __hip_atomic_fetch_add(&table[e[i]], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
   }
 }
 
@@ -495,24 +520,32 @@ __device__ __forceinline__ void count_run(const ListArgs& g, int first, int end,
 __device__ __forceinline__ void place_run(const ListArgs& g, int first, int end, int* table) {
   const int lane = threadIdx.x & 63, bits = 32 - __clz(g.n_leaves);
   const uint64_t below = (1ull << lane) - 1;
-  for (int p0 = first; p0 < end; p0 += 64) {
-    const int p = p0 + lane;
-    int e = p < end ? g.leaves[p] : -1;
-    if ((uint32_t)e >= (uint32_t)g.n_leaves) e = -1;
-    uint64_t same = __ballot(e >= 0);
-    for (int b = 0; b < bits; ++b) {
-      const uint64_t ones = __ballot(e >> b & 1);
-      same &= e >> b & 1 ? ones : ~ones;
-    }
-    if (e >= 0) {
-      const int at = table[e];
+  int next[kAhead];
+  load_leaves(g, first, end, next);
+  for (int p0 = first; p0 < end; p0 += 64 * kAhead) {
+    int leaves[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) leaves[i] = next[i];
+    if (p0 + 64 * kAhead < end) load_leaves(g, p0 + 64 * kAhead, end, next);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (p0 + i * 64 >= end) break;
+      const int p = p0 + i * 64 + lane, e = leaves[i];
+      uint64_t same = __ballot(e >= 0);
+      for (int b = 0; b < bits; ++b) {
+        const uint64_t ones = __ballot(e >> b & 1);
+        same &= e >> b & 1 ? ones : ~ones;
+      }
+      if (e >= 0) {
+        const int at = table[e];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if ((same >> lane) == 1) table[e] = at + __popcll(same);  // the last of them
+        const int to = at + __popcll(same & below);
+        g.row[to] = p / g.k;
+        g.pair[to] = p;
+      }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      if ((same >> lane) == 1) table[e] = at + __popcll(same);  // the last of them
-      const int to = at + __popcll(same & below);
-      g.row[to] = p / g.k;
-      g.pair[to] = p;
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 

@@ -199,24 +199,6 @@ struct CombineArgs {
   int32_t d_out;
 };
 
-template <int N>
-struct Values {
-  float v[N];
-};
-
-// N = 16 bytes of a pair's values.
-template <typename H>
-__device__ __forceinline__ Values<16 / (int)sizeof(H)> chunk_of(const void* p) {
-  constexpr int n = 16 / (int)sizeof(H);
-  const u32x4 c = load16(p);
-  H h[n];
-  __builtin_memcpy(h, &c, 16);
-  Values<n> r;
-#pragma unroll
-  for (int i = 0; i < n; ++i) r.v[i] = (float)h[i];
-  return r;
-}
-
 template <int LANES>
 __device__ __forceinline__ float over_row(float v) {
 #pragma unroll
@@ -224,39 +206,108 @@ __device__ __forceinline__ float over_row(float v) {
   return v;
 }
 
+// (said to be device memory, as load16 says)
+__device__ __forceinline__ float load_float(const float* p) { return *(const __attribute__((address_space(1))) float*)p; }
+
+// Eight of a row's slots: whether there is a leaf, and its weight.
+constexpr int kSlotsAtOnce = 8;
+struct SlotGates {
+  int leaf[kSlotsAtOnce];  // -1 for none
+  float gate[kSlotsAtOnce];
+  template <typename O>
+  __device__ __forceinline__ void load(const CombineArgs<O>& g, int64_t p0, int j0) {
+#pragma unroll
+    for (int i = 0; i < kSlotsAtOnce; ++i) {  // (loads without a branch, which would be waited for one by one)
+      const int64_t p = p0 + (j0 + i < g.k ? j0 + i : g.k - 1);
+      leaf[i] = g.leaves[p];
+      gate[i] = g.gates[p];
+    }
+#pragma unroll
+    for (int i = 0; i < kSlotsAtOnce; ++i)
+      if (j0 + i >= g.k || (uint32_t)leaf[i] >= (uint32_t)g.n_leaves) leaf[i] = -1;
+  }
+};
+
+// The gates' gradients of four slots of row d from slot j0 on.
+template <typename O, int LANES>
+__device__ __forceinline__ void gate_gradients(const CombineArgs<O>& g, int64_t d, int j0, const int* leaf) {
+  constexpr int pairs = kSlotsAtOnce / 2, m = kChunk<O>;
+  const int l = threadIdx.x & (LANES - 1);
+  const int64_t p0 = d * g.k + j0;
+  const O* dy = g.dy + d * g.ld_dy;
+  float dot[pairs];
+#pragma unroll
+  for (int i = 0; i < pairs; ++i) dot[i] = 0.0f;
+  for (int b = l; b < g.blocks; b += LANES) {
+#pragma unroll
+    for (int i = 0; i < pairs; ++i) dot[i] += load_float(leaf[i] >= 0 ? g.dots + (p0 + i) * g.blocks + b : (const float*)zero_chunk);
+  }
+  if (g.bias != nullptr) {
+    for (int c = l * m; c < g.d_out; c += LANES * m) {
+      O y[m], w[pairs][m];
+      if (c + m <= g.d_out) {
+        __builtin_memcpy(y, dy + c, sizeof y);
+#pragma unroll
+        for (int i = 0; i < pairs; ++i) __builtin_memcpy(w[i], g.bias + (int64_t)(leaf[i] < 0 ? 0 : leaf[i]) * g.d_out + c, sizeof y);
+      } else {
+#pragma unroll
+        for (int e = 0; e < m; ++e) {
+          y[e] = c + e < g.d_out ? dy[c + e] : (O)0.0f;
+#pragma unroll
+          for (int i = 0; i < pairs; ++i)
+            w[i][e] = c + e < g.d_out ? g.bias[(int64_t)(leaf[i] < 0 ? 0 : leaf[i]) * g.d_out + c + e] : (O)0.0f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < pairs; ++i)
+#pragma unroll
+        for (int e = 0; e < m; ++e) dot[i] = __builtin_fmaf((float)w[i][e], (float)y[e], dot[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < pairs; ++i) {
+    const float all = over_row<LANES>(dot[i]);
+    if (l == 0 && j0 + i < g.k) g.dgates[p0 + i] = leaf[i] >= 0 ? all : 0.0f;
+  }
+}
+
 // out[d] = sum_j g[d][j] slot_j, LANES lanes a row, 16 bytes of a slot each at a time, eight slots on their way; dgates[d][j] =
 // the sum of the pair's dots and <bias, dy>.  Bound by reading the slots.
-template <typename O, int LANES>
+template <typename O, int LANES, bool GATES>
 __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs<O> g) {
   typedef typename SlotOf<O>::Type H;
-  constexpr int n = 16 / (int)sizeof(H), at_once = 8;
+  constexpr int n = 16 / (int)sizeof(H);
   const int64_t d = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   if (d >= g.n_rows) return;
   const int l = threadIdx.x & (LANES - 1);
   const int64_t p0 = d * g.k;
+  const bool once = g.k <= kSlotsAtOnce;
+  SlotGates slots;
+  slots.load(g, p0, 0);
   if (g.out != nullptr) {
     for (int c = l * n; c < g.cols; c += LANES * n) {
       float sum[n];
 #pragma unroll
       for (int e = 0; e < n; ++e) sum[e] = 0.0f;
-      for (int j0 = 0; j0 < g.k; j0 += at_once) {
-        const void* from[at_once];
-        float gate[at_once];
-        Values<n> v[at_once];
+      for (int j0 = 0; j0 < g.k; j0 += kSlotsAtOnce) {
+        if (!once) slots.load(g, p0, j0);
+        float unit[kSlotsAtOnce];
+        u32x4 raw[kSlotsAtOnce];
 #pragma unroll
-        for (int i = 0; i < at_once; ++i) {
-          const int64_t p = p0 + (j0 + i < g.k ? j0 + i : 0);
-          const bool there = j0 + i < g.k && (uint32_t)g.leaves[p] < (uint32_t)g.n_leaves;
-          from[i] = there ? (const void*)((const H*)g.slots + p * g.ld + c) : (const void*)zero_chunk;
-          gate[i] = there ? g.gates[p] : 0.0f;
-          if constexpr (sizeof(H) == 2) gate[i] = there ? gate[i] * g.units[p * g.blocks + c / 64] : 0.0f;
+        for (int i = 0; i < kSlotsAtOnce; ++i) {
+          const int64_t p = p0 + j0 + i;
+          const bool there = slots.leaf[i] >= 0;
+          raw[i] = load16(there ? (const void*)((const H*)g.slots + p * g.ld + c) : (const void*)zero_chunk);
+          unit[i] = sizeof(H) == 4 ? 1.0f : load_float(there ? g.units + p * g.blocks + c / 64 : (const float*)zero_chunk);
         }
 #pragma unroll
-        for (int i = 0; i < at_once; ++i) v[i] = chunk_of<H>(from[i]);
+        for (int i = 0; i < kSlotsAtOnce; ++i) {
+          const float by = slots.leaf[i] < 0 ? 0.0f : sizeof(H) == 4 ? slots.gate[i] : slots.gate[i] * unit[i];
+          H v[n];
+          __builtin_memcpy(v, &raw[i], 16);
 #pragma unroll
-        for (int i = 0; i < at_once; ++i)
-#pragma unroll
-          for (int e = 0; e < n; ++e) sum[e] = __builtin_fmaf(gate[i], v[i].v[e], sum[e]);
+          for (int e = 0; e < n; ++e) sum[e] = __builtin_fmaf(by, (float)v[e], sum[e]);
+        }
       }
       O* to = g.out + d * g.ld_out + c;
       O t[n];
@@ -271,50 +322,11 @@ __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs<O> g) {
       }
     }
   }
-  if (g.dgates == nullptr) return;
-  constexpr int pairs = 4, m = kChunk<O>;  // four pairs of a row at a time
-  const O* dy = g.dy + d * g.ld_dy;
-  for (int j0 = 0; j0 < g.k; j0 += pairs) {
-    int leaf[pairs];
-    float dot[pairs];
-#pragma unroll
-    for (int i = 0; i < pairs; ++i) {
-      const int e = j0 + i < g.k ? g.leaves[p0 + j0 + i] : -1;
-      leaf[i] = (uint32_t)e < (uint32_t)g.n_leaves ? e : -1;
-      dot[i] = 0.0f;
-    }
-    for (int b = l; b < g.blocks; b += LANES) {
-#pragma unroll
-      for (int i = 0; i < pairs; ++i)
-        if (leaf[i] >= 0) dot[i] += g.dots[(p0 + j0 + i) * g.blocks + b];
-    }
-    if (g.bias != nullptr) {
-      for (int c = l * m; c < g.d_out; c += LANES * m) {
-        O y[m], w[pairs][m];
-        if (c + m <= g.d_out) {
-          __builtin_memcpy(y, dy + c, sizeof y);
-#pragma unroll
-          for (int i = 0; i < pairs; ++i) __builtin_memcpy(w[i], g.bias + (int64_t)(leaf[i] < 0 ? 0 : leaf[i]) * g.d_out + c, sizeof y);
-        } else {
-#pragma unroll
-          for (int e = 0; e < m; ++e) {
-            y[e] = c + e < g.d_out ? dy[c + e] : (O)0.0f;
-#pragma unroll
-            for (int i = 0; i < pairs; ++i)
-              w[i][e] = c + e < g.d_out ? g.bias[(int64_t)(leaf[i] < 0 ? 0 : leaf[i]) * g.d_out + c + e] : (O)0.0f;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < pairs; ++i)
-#pragma unroll
-          for (int e = 0; e < m; ++e) dot[i] = __builtin_fmaf((float)w[i][e], (float)y[e], dot[i]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < pairs; ++i) {
-      const float all = over_row<LANES>(dot[i]);
-      if (l == 0 && j0 + i < g.k) g.dgates[p0 + j0 + i] = leaf[i] >= 0 ? all : 0.0f;
-    }
+  if constexpr (!GATES) return;
+  for (int j0 = 0; j0 < g.k; j0 += kSlotsAtOnce) {
+    if (!once) slots.load(g, p0, j0);
+    gate_gradients<O, LANES>(g, d, j0, &slots.leaf[0]);
+    if (j0 + kSlotsAtOnce / 2 < g.k) gate_gradients<O, LANES>(g, d, j0 + kSlotsAtOnce / 2, &slots.leaf[kSlotsAtOnce / 2]);
   }
 }
 
