@@ -260,9 +260,10 @@ int launch_combine(const CombineArgs<O>& g, hipStream_t s) {
   LAUNCHED("combine_kernel");
   return GBDT_OK;
 }
+// (20,011 rows x 3 leaves, 137 -> 33, f32, a training step: 152 us with sixteen lanes a row of 137 values, 163 with 64.)
 template <typename O>
 int combine(const CombineArgs<O>& g, hipStream_t s) {
-  return g.cols <= 256 / (int)sizeof(O) ? launch_combine<O, 16>(g, s) : launch_combine<O, 64>(g, s);
+  return g.cols <= 256 ? launch_combine<O, 16>(g, s) : launch_combine<O, 64>(g, s);
 }
 
 // So few rows that a wavefront for every few outputs of a row takes less than lists, tiles and slots.
