@@ -640,7 +640,8 @@ int gbdt_mixture_product_grad(const void* dy, int64_t ld_dy, const void* x, int6
  *
  * Rows of x, and rows of the leaves' matrices, as 8-bit codes with a scale each:
  *
- *   scale = max |x[d]| / 127 in f32       code = x / scale to the nearest whole number, ties to even
+ *   scale = max |x[d]| * (1 / 127), both factors and the product in f32
+ *   code  = x / scale to the nearest whole number, ties to even
  *
  * A row with an infinity or a NaN has scale NaN (and codes 0), so what it is multiplied into is NaN; a
  * row whose scale would be below 2^-126 has scale and codes 0.

@@ -127,10 +127,10 @@ def mixture_grad(dy, x, weight, bias, leaves, gates):
 
 
 def quantize(x):
-    """(codes int8, scales float32): scale = max |x| / 127 rounded to 32 bits, codes round to even."""
+    """(codes int8, scales float32): scale = max |x| times the 32-bit 1 / 127, rounded to 32 bits; codes round to even."""
     most = x.float().abs().amax(1)
     finite = torch.isfinite(x.float()).all(1)
-    scales = (most.double() / 127.0).float()
+    scales = (most.double() * torch.tensor(1.0 / 127.0, dtype=torch.float32).double().item()).float()
     scales = torch.where(scales < 2.0 ** -126, 0.0, scales)
     unit = torch.where(finite & (scales > 0), scales, 1.0).double()
     codes = torch.where((finite & (scales > 0))[:, None], torch.round(x.double() / unit[:, None]), 0.0)

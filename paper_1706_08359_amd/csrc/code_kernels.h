@@ -1,6 +1,6 @@
 // Leaf products in 8-bit integers: rows and matrices as codes with a scale each, x ~ q s.
 //
-//   s = max |x| / 127 (f32)      q = x / s to the nearest whole number, ties to even
+//   s = max |x| * (1 / 127) (f32, both factors)      q = x / s to the nearest whole number, ties to even
 //   y[d] = (sum q_x q_w) s_d s_lo + b_lo       sums of codes exact in 32 bits
 //
 // Rows of codes are a multiple of 16 long, zeros behind, so every operand is whole chunks.
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(256) quantize_kernel(const QuantizeArgs g) {
   }
   // a row with an infinity or a NaN has no scale; one whose scale would be below the normal numbers is zeros
   const bool finite = most < 0x7f800000u;
-  float scale = finite ? __uint_as_float(most) / 127.0f : __uint_as_float(0x7fc00000u);
+  float scale = finite ? __uint_as_float(most) * (1.0f / 127.0f) : __uint_as_float(0x7fc00000u);
   if (finite && scale < 0x1p-126f) scale = 0.0f;
   const bool zero = !(scale > 0.0f);
   const float inverse = zero ? 0.0f : 1.0f / scale;

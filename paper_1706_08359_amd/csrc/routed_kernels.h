@@ -343,14 +343,14 @@ __global__ void __launch_bounds__(256) clear_rows_kernel(const int32_t* leaves, 
 // g dy of every position, in the list's order, rounded to the products' type: dW_l = sum (g dy) x^T then is the sum of
 // leaf_grad_weight_kernel.  (A value is off by half a step of its type; a sum of many such, of independent sign, by less than the
 // rounding of the result.)  Columns [first, first + cols) of dy, zeros up to ld.
-template <typename T>
+template <typename T, int LANES>
 __global__ void __launch_bounds__(256) gated_rows_kernel(const RoutedArgs<T> g, T* out, int64_t ld, int first, int cols) {
-  const int p = (int)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int p = (int)(blockIdx.x * (256 / LANES) + threadIdx.x / LANES);
   if (p >= offset_at(g.offsets, g.n_leaves, g.n_positions)) return;
   const float gate = g.gates[g.pair_idx[p]];
   const T* dy = row_of(g.dy, g.row_idx[p], g.ld_dy) + first;
   constexpr int n = kChunk<T>;
-  for (int c = (int)(threadIdx.x & 63) * n; c < ld; c += 64 * n) {
+  for (int c = (int)(threadIdx.x & (LANES - 1)) * n; c < ld; c += LANES * n) {
     T t[n];
     if (c + n <= cols) {
       __builtin_memcpy(t, dy + c, sizeof t);

@@ -141,6 +141,7 @@ constexpr int64_t kSlotsBytes = (int64_t)256 << 20;
 // Weighted gradients of so many outputs at a time as take this, or of a tile.
 constexpr int64_t kGatedBytes = (int64_t)256 << 20;
 constexpr int32_t kMaxSlots = 64;  // leaves a row
+constexpr int64_t kMaxGridRows = 65535;  // rows of a launch's second dimension
 
 // e: bytes of a slot's value; block: columns that share a power of two or a part of a dot product.
 struct SlotPlan {
@@ -266,8 +267,19 @@ int combine(const CombineArgs<O>& g, hipStream_t s) {
   return g.cols <= 256 ? launch_combine<O, 16>(g, s) : launch_combine<O, 64>(g, s);
 }
 
-// So few rows that a wavefront for every few outputs of a row takes less than lists, tiles and slots.
-bool few_rows(int64_t n_rows, int64_t k, int64_t d_out) { return n_rows <= 4 || (n_rows <= 2048 && n_rows * k * d_out <= 16384); }
+// So few rows that a wavefront for every few outputs of a row takes less than lists, tiles and slots.  It reads a matrix again for
+// every row that takes the leaf: pairs x outputs x inputs, of 64 chunks at least, at 3.8 million a us (f32 2.1, codes 9), after 4 us; the
+// other way is 13 us and each matrix that is taken once, 0.3 us a million values more (f32, whose tiles are mostly empty, 1.2; codes
+// 0.18).  (bf16, us, this way / the other, pairs of 64 matrices of 1,024 x 1,024: 64 22/27, 128 34/33, 256 64/33; of 255 of 700 x 256: 256
+// 16/29, 512 33/30; of 8 of 256 x 64: 512 8.0/13, 2,000 21/15.  f32: 128 70/108, 256 141/110; 512 48/68, 2,000 174/81; 2,000 17/17.  Codes: 128
+// 19/25, 256 30/25; 512 20/23, 2,000 62/25; 512 7.3/14, 2,000 18/15.)
+template <typename T>
+bool few_rows(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t d_in, int64_t d_out) {
+  const double products = (double)(n_rows * k) * (double)d_out * (double)std::max<int64_t>(d_in, 64 * kChunk<T>);
+  const double taken = (double)std::min(n_leaves, n_rows * k) * (double)d_in * (double)d_out;
+  const double room = sizeof(T) == 2 ? 34e6 + 1.2 * taken : sizeof(T) == 4 ? 23e6 + 2.5 * taken : 80e6 + 1.6 * taken;
+  return n_rows <= kMaxGridRows && (n_rows <= 4 || products <= room);
+}
 
 // Products of all rows, kept in slots and added up, so many rows at a time as the plan says.  products(g, r): of the rows from r on,
 // to the slots.  Where answers go to rows directly (`direct`), the plan's list is all that is used of the scratch.
@@ -318,7 +330,7 @@ int by_slots(const G& all, int64_t n_rows, int64_t cols, const CombineArgs<O>& t
 
 template <typename T>
 int mixture_product(RoutedArgs<T>& g, int64_t n_rows, hipStream_t s) {
-  if (few_rows(n_rows, g.k, g.d_out)) {
+  if (few_rows<T>(n_rows, g.k, g.n_leaves, g.d_in, g.d_out)) {
     if (n_rows * g.d_out <= 1024) {
       gbdt_routed::routed_few_kernel<T, 1><<<dim3(g.d_out, (unsigned)n_rows), dim3(64), 0, s>>>(g);
     } else {
@@ -360,7 +372,13 @@ int mixture_weights(RoutedArgs<T> g, int64_t n_rows, const WeightPlan& plan, cha
   for (int64_t first = 0; first < g.d_out; first += plan.piece) {
     const int64_t cols = std::min(plan.piece, whole.d_out - first);
     if (n_rows > 0) {
-      gbdt_routed::gated_rows_kernel<T><<<dim3((unsigned)ceil_div(g.n_positions, 4)), dim3(256), 0, s>>>(whole, gated, plan.ld, (int)first, (int)cols);
+      if (plan.ld * (int64_t)sizeof(T) <= 1024) {
+        gbdt_routed::gated_rows_kernel<T, 16><<<dim3((unsigned)ceil_div(g.n_positions, 16)), dim3(256), 0, s>>>(whole, gated, plan.ld, (int)first,
+                                                                                                             (int)cols);
+      } else {
+        gbdt_routed::gated_rows_kernel<T, 64><<<dim3((unsigned)ceil_div(g.n_positions, 4)), dim3(256), 0, s>>>(whole, gated, plan.ld, (int)first,
+                                                                                                            (int)cols);
+      }
       LAUNCHED("gated_rows_kernel");
     }
     g.dy = gated;
@@ -513,13 +531,14 @@ int code_few(const CodeArgs& g, int64_t rows, hipStream_t s) {
 
 template <typename O>
 int leaf_codes(CodeArgs& g, hipStream_t s) {
-  if (few_rows(g.n_positions, 1, g.d_out)) return code_few<O, true>(g, g.n_positions, s);
+  // (as few positions as gbdt_leaf_product answers so)
+  if (g.n_positions <= 4 || (g.n_positions <= 2048 && (int64_t)g.n_positions * g.d_out <= 16384)) return code_few<O, true>(g, g.n_positions, s);
   return code_tiles<O, Place::kRow>(g, s);
 }
 
 template <typename O>
 int mixture_codes(CodeArgs& g, int64_t n_rows, hipStream_t s) {
-  if (few_rows(n_rows, g.k, g.d_out)) return code_few<O, false>(g, n_rows, s);
+  if (few_rows<int8_t>(n_rows, g.k, g.n_leaves, g.d_in, g.d_out)) return code_few<O, false>(g, n_rows, s);
   const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out, sizeof(O), gbdt_routed::block_columns<int8_t>, false);
   void* ws = nullptr;
   const int rc = gbdt_internal::workspace(plan.bytes(), s, &ws);

@@ -40,8 +40,7 @@ def test_codes_next_to_a_half():
     g = torch.Generator().manual_seed(0)
     out = []
     for top in (127.0, 1.0, 3.14159, 1e-30, 2.7e37, 1.1754944e-36):
-        s = torch.tensor(top, dtype=torch.float32).double() / 127
-        s = s.float().double()
+        s = float(ref.quantize(torch.tensor([[top]]))[1])
         half = (torch.arange(0, 127).double() + 0.5) * s
         near = half.float()
         row = torch.cat([near, torch.nextafter(near, torch.tensor(math.inf)), torch.nextafter(near, torch.tensor(0.0)),

@@ -174,6 +174,7 @@ def test_the_oracles_mixture_against_automatic_differentiation():
 def test_the_oracles_codes():
     x = torch.tensor([[127.0, -127.0, 0.5, 1.5, 2.5, -0.5], [0.0] * 6, [math.inf, 1, 2, 3, 4, 5], [1e-40] * 6, [math.nan, 0, 0, 0, 0, 0]])
     codes, scales = ref.quantize(x)
+    # (127 / 127 is 1 with the 32-bit 1 / 127 too)
     assert codes[0].tolist() == [127, -127, 0, 2, 2, 0] and scales[0] == 1.0
     assert codes[1:].abs().sum() == 0 and scales[1] == 0 and scales[3] == 0
     assert torch.isnan(scales[2]) and torch.isnan(scales[4])
