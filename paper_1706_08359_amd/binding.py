@@ -918,7 +918,8 @@ def _out(t, shape, dtype, device, stream, name, make=torch.empty):
     """(tensor, address) of a dense output: the caller's, or one made here, whose shape needs no checks."""
     if t is not None:
         return t, _dense(t, dtype, shape, name)
-    t = _made(make, shape, dtype, device, stream)
+    # (sizes one by one: 1.3 us instead of 1.6, of the 9 that a call on a row waits for the host)
+    t = make(*shape, dtype=dtype, device=device) if stream is None else _made(make, shape, dtype, device, stream)
     return t, t.data_ptr()
 
 
@@ -926,7 +927,7 @@ def _out_rows(t, shape, dtype, device, stream, name, make=torch.empty):
     """(tensor, address, distance of rows) of an output whose rows may lie apart."""
     if t is not None:
         return (t,) + _mat(t, dtype, shape[0], shape[1], name)
-    t = _made(make, shape, dtype, device, stream)
+    t = make(*shape, dtype=dtype, device=device) if stream is None else _made(make, shape, dtype, device, stream)
     return t, t.data_ptr(), shape[1]
 
 

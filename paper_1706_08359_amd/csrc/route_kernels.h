@@ -74,7 +74,28 @@ __device__ __forceinline__ double over_lanes(double v, const Op& op) {
   for (int m = 16; m < LANES; m <<= 1) v = op(v, __shfl_xor(v, m));
   return v;
 }
+template <int CTRL>
+__device__ __forceinline__ int dpp(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);
+}
+template <int LANES, class Op>
+__device__ __forceinline__ int over_lanes(int v, const Op& op) {
+  v = op(v, dpp<0xB1>(v));
+  if (LANES >= 4) v = op(v, dpp<0x4E>(v));
+  if (LANES >= 8) v = op(v, dpp<0x141>(v));
+  if (LANES >= 16) v = op(v, dpp<0x140>(v));
+  if (LANES >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = op((int)r[0], (int)r[1]);
+  }
+  if (LANES >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    v = op((int)r[0], (int)r[1]);
+  }
+  return v;
+}
 struct Max {
+  __device__ __forceinline__ int operator()(int a, int b) const { return a > b ? a : b; }
   __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
   __device__ __forceinline__ double operator()(double a, double b) const { return fmax(a, b); }
 };
@@ -95,12 +116,32 @@ __device__ __forceinline__ V lowest() {
   return -(V)INFINITY;
 }
 
+// f32 values as whole numbers of the same order, equal where they are equal: a maximum of two is one instruction, where one of floats
+// is two or three that see to NaN.  And back.
+__device__ __forceinline__ int key_of(float v) {
+  const int bits = __float_as_int(v + 0.0f);  // (-0 becomes 0)
+  return bits ^ ((bits >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float value_of(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
+__device__ __forceinline__ double key_of(double v) { return v; }
+__device__ __forceinline__ double value_of(double v) { return v; }
+template <>
+__device__ __forceinline__ int lowest<int>() {
+  return (int)0x807fffff;  // of minus infinity
+}
+
 // The exponential of a value at or below 0; of a masked logit 0.  inf - inf counts as 0: the largest logit's is 1.
 __device__ __forceinline__ float exp_below(float l, float top) { return l == top ? 1.0f : expf(l - top); }
 __device__ __forceinline__ double exp_below(double l, double top) { return l == top ? 1.0 : exp(l - top); }
 
+// The same for choice values in f32, whose errors are allowed for: by the exponential instruction, off by |x| 2^-24 of its result.
+__device__ __forceinline__ float quick_below(float l, float top) { return l == top ? 1.0f : __expf(l - top); }
+__device__ __forceinline__ double quick_below(double l, double top) { return exp_below(l, top); }
+
 __device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
 __device__ __forceinline__ double sigmoid(double l) { return 1.0 / (1.0 + exp(-l)); }
+__device__ __forceinline__ float quick_sigmoid(float l) { return __builtin_amdgcn_rcpf(1.0f + __expf(-l)); }
+__device__ __forceinline__ double quick_sigmoid(double l) { return sigmoid(l); }
 
 // The largest of the row's values, and its first column, which is taken out; false if only masked ones are left.
 template <typename V, int LANES, int PER>
@@ -112,15 +153,12 @@ __device__ __forceinline__ bool take_largest(V (&v)[PER], V* value, int* column)
   const bool any = top > lowest<V>();
   const uint64_t who = row_ballot<LANES>(mine == top);
   const int lane = threadIdx.x & (LANES - 1), first = __ffsll((unsigned long long)who) - 1;
-  bool looking = any && lane == first;
   int at = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const bool here = looking && v[i] == top;
-    at = here ? i : at;
-    v[i] = here ? lowest<V>() : v[i];
-    looking = looking && !here;
-  }
+  for (int i = PER - 1; i >= 0; --i) at = v[i] == top ? i : at;
+  const int out = any && lane == first ? at : -1;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) v[i] = i == out ? lowest<V>() : v[i];
   *value = top;
   *column = first * PER + __shfl(at, first, LANES);
   return any;
@@ -222,15 +260,22 @@ __device__ __forceinline__ bool choose(const RouteArgs& g, V (&v)[PER], V tol, b
   bool close = false;
   if (g.n_groups > 1) close = keep_groups<V, LANES, PER>(g, v, tol) && check;
   const int lane = threadIdx.x & (LANES - 1), more = check && g.k < g.n_leaves ? 1 : 0;
+  typedef decltype(key_of(V())) Key;
+  Key keys[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) keys[i] = key_of(v[i]);
   V before = lowest<V>();
 #pragma unroll
   for (int t = 0; t < kSlotsOf<LANES>; ++t) picked[t] = -1;
   for (int j = 0; j < g.k + more; ++j) {
-    V top;
+    Key key;
     int column;
-    const bool any = take_largest<V, LANES, PER>(v, &top, &column);
-    if (check && any && j > 0) close |= !(before - top > tol + (V)0x1p-22 * fabs(before));
-    before = top;
+    const bool any = take_largest<Key, LANES, PER>(keys, &key, &column);
+    if (check) {
+      const V top = value_of(key);
+      if (any && j > 0) close |= !(before - top > tol + (V)0x1p-22 * fabs(before));
+      before = top;
+    }
 #pragma unroll
     for (int t = 0; t < kSlotsOf<LANES>; ++t)
       if (lane + t * LANES == j) picked[t] = any ? column : -1;
@@ -246,16 +291,22 @@ __device__ __forceinline__ void load_logits(const T* row, int column, int n, flo
     __builtin_memcpy(t, row + column, sizeof t);
 #pragma unroll
     for (int i = 0; i < PER; ++i) l[i] = (float)t[i];
+  } else if (row != nullptr) {  // (loads without a branch each, which would be waited for one by one)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) t[i] = row[column + i < n ? column + i : n - 1];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) l[i] = column + i < n ? (float)t[i] : -INFINITY;
   } else {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) l[i] = row != nullptr && column + i < n ? (float)row[column + i] : -INFINITY;
+    for (int i = 0; i < PER; ++i) l[i] = -INFINITY;
   }
 #pragma unroll
   for (int i = 0; i < PER; ++i) l[i] = l[i] == l[i] ? l[i] : -INFINITY;
 }
 
-// A row's choice values; *tol: the error of a value in f32 beside 2^-23 of its size.  (Sigmoid: its exponential to 2 ulp and two
-// roundings, of at most 1.  Softmax: the sum of the exponentials, PER + 6 roundings and 2 ulp of each, all of the largest score.)
+// A row's choice values; *tol: the error of a value in f32 beside 2^-23 of its size.  (Sigmoid: its
+// exponential's error, (|l| + 2) 2^-24, times s (1 - s), below 2^-24, and 2^-23 for the sum and the reciprocal, of at most 1.
+// Softmax, all of the largest score: x exp(-x) 2^-24, below 2^-25, of each and PER + 6 roundings and 2^-22 of the sum.)
 template <typename V, int LANES, int PER>
 __device__ __forceinline__ void choice_values(const RouteArgs& g, const float (&l)[PER], float top, V (&v)[PER], V* tol) {
   const int lane = threadIdx.x & (LANES - 1);
@@ -264,7 +315,7 @@ __device__ __forceinline__ void choice_values(const RouteArgs& g, const float (&
     V sum = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      v[i] = l[i] > -INFINITY ? exp_below((V)l[i], (V)top) : (V)0;
+      v[i] = l[i] > -INFINITY ? quick_below((V)l[i], (V)top) : (V)0;
       sum += v[i];
     }
     inverse = 1 / over_lanes<LANES>(sum, Sum{});
@@ -272,7 +323,7 @@ __device__ __forceinline__ void choice_values(const RouteArgs& g, const float (&
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int e = lane * PER + i;
-    V c = g.sigmoid ? sigmoid((V)l[i]) : v[i] * inverse;
+    V c = g.sigmoid ? quick_sigmoid((V)l[i]) : v[i] * inverse;
     if (g.bias != nullptr && e < g.n_leaves) c += (V)g.bias[e];
     v[i] = l[i] > -INFINITY && c == c ? c : lowest<V>();
   }
