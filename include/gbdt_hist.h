@@ -608,8 +608,9 @@ int gbdt_route_grad(const void* logits, int64_t ld, const int32_t* leaves, const
  *   gates    DEVICE float [n_rows][k]
  *   y_out    DEVICE [n_rows][d_out]; zeros for a row without a leaf
  * Element types, distances and limits as for gbdt_leaf_product; k <= 64, n_leaves <= 16384, n_rows * k < 2^30.  The slots' answers
- * are kept in f32 in the library's scratch, of so many rows at a time as take 256 MiB or of 1,024, and
- * added in their order: the same call gives the same bits, rounded once.
+ * are kept in the library's scratch, of so many rows at a time as take 256 MiB or of 1,024, and
+ * added in f32 in their order: the same call gives the same bits.  f32 answers are kept as they are, those of bf16 results with 11
+ * bits, an eighth of the error that rounding the result has.
  * gbdt_mixture_workspace_bytes: the size of a registered workspace that suffices for the three
  * gbdt_mixture_* calls (0 on invalid arguments).
  */
@@ -627,7 +628,9 @@ size_t gbdt_mixture_workspace_bytes(int64_t n_rows, int32_t k, int32_t n_leaves,
  *   dbias_out[l]     = sum over the slots of leaf l of gates dy         DEVICE [n_leaves][d_out]
  *   dgates_out[d][j] = <dy[d], W_l x[d] + b_l>                          DEVICE float [n_rows][k], 0 for a slot passed over
  * weight is read for dx and dgates, x for dweight and dgates, bias for dgates.  In dweight and dbias
- * gates * dy is rounded to the element type before it is summed.
+ * gates * dy is rounded to the element type before it is summed: bf16 results are off by 1.4 times the error of rounding exact
+ * ones, root mean square.  The slots' scratch as above; that of dweight holds gates * dy of so many outputs as take 256 MiB, or of 128
+ * (f32: 64), beside the sums of leaves that are long (as gbdt_leaf_product_grad).  The same call gives the same bits.
  */
 int gbdt_mixture_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
                               const void* weight, const void* bias, const int32_t* leaves,

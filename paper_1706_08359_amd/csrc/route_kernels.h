@@ -374,7 +374,9 @@ struct Slots {
   }
 };
 
-// Bound by reading the logits where rows are many; k picks of some twenty instructions each are the rest.
+// Bound by reading the logits where rows are many and k is small: 400,000 x 255 f32, four leaves each, 115 us, 3.7 TB/s.  A pick is some
+// 130 instructions for four rows of 256 columns: 16,384 x 256 bf16 in 8 groups, 8 leaves each by values, 23 us, 18 of it picks, 4 the few rows
+// that 64 bits decide, which end last; 65,536 x 64 f32, four leaves each by values, 14 us.
 // VALUES: leaves are chosen by their values, not by the logits themselves.
 template <typename T, int LANES, int PER, bool VALUES>
 __global__ void __launch_bounds__(kThreads) route_kernel(const RouteArgs g) {
@@ -446,7 +448,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteArgs g) {
 //   softmax                 scale s ([chosen] dg - sum s dg) at every leaf
 //   sigmoid, renormalised   scale r (1 - s) (dg - sum r dg) at the slot's leaf
 //   sigmoid                 scale s (1 - s) dg at the slot's leaf
-// and zeros elsewhere.  Bound by writing the gradients and, for the second, reading the logits.
+// and zeros elsewhere.  Bound by writing the gradients and, for the second, reading the logits: 65,536 x 64 f32, 11 us, 3.0 TB/s.
 template <typename T, int LANES, int PER>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteArgs g) {
   constexpr int rows = kThreads / LANES;
@@ -529,7 +531,8 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteArgs g)
 
 // Pairs p = row * k + slot, grouped by leaf, ascending within one: what the products take.  Pairs whose leaf is none are in no
 // list.  A wavefront counts a run of neighbouring pairs in local memory, a table of its own for all leaves; sums over the runs give
-// each its places, and it goes through its pairs again.  No order hangs on which ran first.
+// each its places, and it goes through its pairs again.  No order hangs on which ran first.  Three launches of 5 us each, whose lengths
+// are those of a launch and a chain of two or three round trips (65,536 pairs, 64 leaves); one of 3.5 us for 256 pairs.
 struct ListArgs {
   const int32_t* leaves;   // [n_pairs]
   int64_t* offsets;        // [n_leaves + 1]
