@@ -313,19 +313,30 @@ template <class S, class B, typename T, class G, class To>
 __device__ __forceinline__ void leaf_rows_stay(char* lds, StayTable<S>& first, const G& g, const T* in, int64_t ld_in, int k, const To& to, int cols) {
   if (threadIdx.x < 64) {
     const int lane = threadIdx.x;
-    int base = 0;
+    int least = 0, base = 0;  // (offsets that decrease are taken as the largest before them)
     for (int l0 = 0; l0 <= g.n_leaves; l0 += 64) {
       const int l = l0 + lane;
-      const int begin = offset_at(g.offsets, l < g.n_leaves ? l : g.n_leaves, g.n_positions);
-      const int end = offset_at(g.offsets, l + 1 < g.n_leaves ? l + 1 : g.n_leaves, g.n_positions);
-      const int n = l < g.n_leaves && end > begin ? (end - begin + S::BM - 1) / S::BM : 0;
+      int begin = offset_at(g.offsets, l < g.n_leaves ? l : g.n_leaves, g.n_positions);
+      begin = begin > least ? begin : least;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        const int other = __shfl_up(begin, m);
+        if (lane >= m && other > begin) begin = other;
+      }
+      if (l <= g.n_leaves) first.begin[l] = begin;
+      least = __shfl(begin, 63);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int l0 = 0; l0 <= g.n_leaves; l0 += 64) {
+      const int l = l0 + lane;
+      const int n = l < g.n_leaves ? (first.begin[l + 1] - first.begin[l] + S::BM - 1) / S::BM : 0;
       int sum = n;
 #pragma unroll
       for (int m = 1; m < 64; m <<= 1) {
         const int other = __shfl_up(sum, m);
         if (lane >= m) sum += other;
       }
-      if (l <= g.n_leaves) first.tile[l] = base + sum - n, first.begin[l] = begin;
+      if (l <= g.n_leaves) first.tile[l] = base + sum - n;
       base += __shfl(sum, 63);
     }
   }

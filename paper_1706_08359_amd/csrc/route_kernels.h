@@ -26,6 +26,7 @@ struct RouteArgs {
   const float* dgates;  // gradient: [n_rows][k]
   void* dlogits;        // gradient: [n_rows][n_leaves]
   int64_t ld, ld_out;
+  int64_t first;        // row of this launch's first
   int32_t n_rows, n_leaves, k;
   int32_t n_groups, groups_kept, group_best, group_size;
   int32_t sigmoid, renormalise;
@@ -382,7 +383,7 @@ template <typename T, int LANES, int PER, bool VALUES>
 __global__ void __launch_bounds__(kThreads) route_kernel(const RouteArgs g) {
   constexpr int rows = kThreads / LANES;
   const int r = threadIdx.x / LANES, lane = threadIdx.x & (LANES - 1);
-  const int64_t d = (int64_t)blockIdx.x * rows + r;
+  const int64_t d = g.first + (int64_t)blockIdx.x * rows + r;
   const T* row = d < g.n_rows ? (const T*)g.logits + d * g.ld : nullptr;
   int picked[kSlotsOf<LANES>];
   float top, inverse = 0.0f;
@@ -411,7 +412,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteArgs g) {
       while (again) {
         const int from = __ffsll((unsigned long long)again) - 1;
         again &= again - 1;
-        const int64_t other = (int64_t)blockIdx.x * rows + ((threadIdx.x & ~63) + from) / LANES;
+        const int64_t other = g.first + (int64_t)blockIdx.x * rows + ((threadIdx.x & ~63) + from) / LANES;
         float logits[wide], most;
         load_logits<T, wide>((const T*)g.logits + other * g.ld, (threadIdx.x & 63) * wide, g.n_leaves, logits);
         most = logits[0];
@@ -453,7 +454,7 @@ template <typename T, int LANES, int PER>
 __global__ void __launch_bounds__(kThreads) route_grad_kernel(const RouteArgs g) {
   constexpr int rows = kThreads / LANES;
   const int r = threadIdx.x / LANES, lane = threadIdx.x & (LANES - 1);
-  const int64_t d = (int64_t)blockIdx.x * rows + r;
+  const int64_t d = g.first + (int64_t)blockIdx.x * rows + r;
   const T* row = d < g.n_rows ? (const T*)g.logits + d * g.ld : nullptr;
   int picked[kSlotsOf<LANES>];
 #pragma unroll

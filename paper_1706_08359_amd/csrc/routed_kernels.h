@@ -351,10 +351,10 @@ __global__ void __launch_bounds__(256) clear_rows_kernel(const int32_t* leaves, 
 // leaf_grad_weight_kernel, 148 us for 32,768 positions of 64 leaves, 1,024 x 1,024, bf16 (460 TFLOP/s).  The matrix cores take bf16 only,
 // and two values for g dy would take them twice as long; one is off by half a step of each term, which adds as much to a result's error as
 // its own rounding: 2.4e-3 of bf16 results' size in all, 1.7e-3 without.  Bound by memory: the same case 22 us, 6 TB/s.
-//  Columns [first, first + cols) of dy, zeros up to ld.
+//  Columns [first, first + cols) of dy, zeros up to ld; positions from `from` on.
 template <typename T, int LANES>
-__global__ void __launch_bounds__(256) gated_rows_kernel(const RoutedArgs<T> g, T* out, int64_t ld, int first, int cols) {
-  const int p = (int)(blockIdx.x * (256 / LANES) + threadIdx.x / LANES);
+__global__ void __launch_bounds__(256) gated_rows_kernel(const RoutedArgs<T> g, T* out, int64_t ld, int first, int cols, int from) {
+  const int p = from + (int)(blockIdx.x * (256 / LANES) + threadIdx.x / LANES);
   if (p >= offset_at(g.offsets, g.n_leaves, g.n_positions)) return;
   const float gate = g.gates[g.pair_idx[p]];
   const T* dy = row_of(g.dy, g.row_idx[p], g.ld_dy) + first;

@@ -36,18 +36,29 @@ int route_check(const void* logits, int64_t ld, int64_t n_rows, int32_t n_leaves
   return GBDT_OK;
 }
 
-template <typename T, int LANES, int PER>
-int launch_route(const RouteArgs& g, bool grad, hipStream_t s) {
-  const dim3 blocks((unsigned)ceil_div(g.n_rows, gbdt_router::kThreads / LANES)), threads(gbdt_router::kThreads);
-  if (grad) {
-    gbdt_router::route_grad_kernel<T, LANES, PER><<<blocks, threads, 0, s>>>(g);
-  } else if (g.bias == nullptr && g.group_best == 1) {
-    gbdt_router::route_kernel<T, LANES, PER, false><<<blocks, threads, 0, s>>>(g);
-  } else {
-    gbdt_router::route_kernel<T, LANES, PER, true><<<blocks, threads, 0, s>>>(g);
+// launch(first, blocks) for `rows` rows, `per` of them a workgroup of 256 threads, as many at a time as a launch takes.
+template <class Launch>
+int row_launches(int64_t rows, int64_t per, const char* what, const Launch& launch) {
+  for (int64_t first = 0; first < rows; first += most_blocks(256) * per) {
+    launch(first, dim3((unsigned)std::min(ceil_div(rows - first, per), most_blocks(256))));
+    LAUNCHED(what);
   }
-  LAUNCHED("routing");
   return GBDT_OK;
+}
+
+template <typename T, int LANES, int PER>
+int launch_route(RouteArgs g, bool grad, hipStream_t s) {
+  static_assert(gbdt_router::kThreads == 256, "");
+  return row_launches(g.n_rows, 256 / LANES, "routing", [&](int64_t first, dim3 blocks) {
+    g.first = first;
+    if (grad) {
+      gbdt_router::route_grad_kernel<T, LANES, PER><<<blocks, dim3(256), 0, s>>>(g);
+    } else if (g.bias == nullptr && g.group_best == 1) {
+      gbdt_router::route_kernel<T, LANES, PER, false><<<blocks, dim3(256), 0, s>>>(g);
+    } else {
+      gbdt_router::route_kernel<T, LANES, PER, true><<<blocks, dim3(256), 0, s>>>(g);
+    }
+  });
 }
 
 // (400,000 rows x 255, four leaves each: 125 us by sixteen lanes a row, 148 by eight, 158 by 32, 219 by 64.  65,536 x 64 with a bias and
@@ -151,7 +162,12 @@ struct SlotPlan {
   size_t bytes() const { return list.bytes() + slots_bytes + units_bytes + dots_bytes; }
 };
 SlotPlan slot_plan(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t cols, int64_t e, int64_t block, bool dots) {
-  SlotPlan p;
+  SlotPlan p = {};
+  if (k == 1 && !dots) {  // answers go to their rows, all at once
+    p.rows = n_rows;
+    p.list = list_plan(n_rows, n_leaves);
+    return p;
+  }
   p.ld = round_up(cols, 16 / e);
   p.blocks = ceil_div(cols, block);
   p.rows = std::min(n_rows, std::max<int64_t>(1024, kSlotsBytes / (k * p.ld * e)));
@@ -372,14 +388,15 @@ int mixture_weights(RoutedArgs<T> g, int64_t n_rows, const WeightPlan& plan, cha
   for (int64_t first = 0; first < g.d_out; first += plan.piece) {
     const int64_t cols = std::min(plan.piece, whole.d_out - first);
     if (n_rows > 0) {
-      if (plan.ld * (int64_t)sizeof(T) <= 1024) {
-        gbdt_routed::gated_rows_kernel<T, 16><<<dim3((unsigned)ceil_div(g.n_positions, 16)), dim3(256), 0, s>>>(whole, gated, plan.ld, (int)first,
-                                                                                                             (int)cols);
-      } else {
-        gbdt_routed::gated_rows_kernel<T, 64><<<dim3((unsigned)ceil_div(g.n_positions, 4)), dim3(256), 0, s>>>(whole, gated, plan.ld, (int)first,
-                                                                                                            (int)cols);
-      }
-      LAUNCHED("gated_rows_kernel");
+      const bool narrow = plan.ld * (int64_t)sizeof(T) <= 1024;
+      rc = row_launches(g.n_positions, narrow ? 16 : 4, "gated_rows_kernel", [&](int64_t from, dim3 blocks) {
+        if (narrow) {
+          gbdt_routed::gated_rows_kernel<T, 16><<<blocks, dim3(256), 0, s>>>(whole, gated, plan.ld, (int)first, (int)cols, (int)from);
+        } else {
+          gbdt_routed::gated_rows_kernel<T, 64><<<blocks, dim3(256), 0, s>>>(whole, gated, plan.ld, (int)first, (int)cols, (int)from);
+        }
+      });
+      if (rc != GBDT_OK) return rc;
     }
     g.dy = gated;
     g.ld_dy = plan.ld;
@@ -488,10 +505,15 @@ int code_check(const void* codes, int64_t ld_codes, const float* scales, const v
 }
 
 template <typename T, int CHUNKS>
-int launch_quantize(const gbdt_code::QuantizeArgs& g, hipStream_t s) {
-  gbdt_code::quantize_kernel<T, CHUNKS><<<dim3((unsigned)ceil_div(g.n_rows, 4)), dim3(256), 0, s>>>(g);
-  LAUNCHED("quantize_kernel");
-  return GBDT_OK;
+int launch_quantize(const gbdt_code::QuantizeArgs& all, hipStream_t s) {
+  return row_launches(all.n_rows, 4, "quantize_kernel", [&](int64_t first, dim3 blocks) {
+    gbdt_code::QuantizeArgs g = all;
+    g.x = (const T*)all.x + first * all.ld_x;
+    g.codes += first * all.ld_codes;
+    g.scales += first;
+    g.n_rows -= first;
+    gbdt_code::quantize_kernel<T, CHUNKS><<<blocks, dim3(256), 0, s>>>(g);
+  });
 }
 template <typename T>
 int quantize(const gbdt_code::QuantizeArgs& g, hipStream_t s) {

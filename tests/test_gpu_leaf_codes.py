@@ -158,3 +158,13 @@ def test_a_row_without_a_scale():
     y = B.gbdt_mixture_product_codes(codes, scales, w, ws, leaves, torch.ones(300, 1).cuda(), bias=b)
     assert bool(torch.isnan(y[7]).all()) and bool((y[9] == 0).all())
     assert not bool(torch.isnan(y[torch.arange(300).cuda() != 7]).any())
+
+
+@pytest.mark.parametrize("n,d_out", [(70_000, 200), (60_000, 300), (300, 64)])
+def test_offsets_past_the_list_and_leaves_before_the_first(n, d_out):
+    """Offsets outside the list are its ends, positions before the first and from the last on belong to no leaf."""
+    codes, scales, w, ws, b, g = made(n, 4, 64, d_out, seed=n)
+    offs = torch.tensor([n // 10, n // 2, n // 2, n - n // 7, n + 50]).cuda()
+    y = B.gbdt_leaf_product_codes(codes, scales, w, ws, offs, bias=b, y_out=torch.full((n, d_out), 3.0).cuda())
+    want, mag = one_leaf.leaf_product(values(codes, scales), values(w, ws), b, offs, None, torch.full((n, d_out), 3.0).cuda())
+    assert close(y, want, mag, 4) and bool((y[:n // 10] == 3).all())

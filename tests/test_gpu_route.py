@@ -182,3 +182,20 @@ def test_rows_past_the_batch_are_left_alone_and_many_rows():
     assert bool((out[:, :3] == 5).all()) and bool((out[:, 36:] == 5).all())
     empty = torch.zeros(0, 33, dtype=torch.bfloat16).cuda()
     assert B.gbdt_route(empty, 4)[0].shape == (0, 4)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_types_lowest_value_as_a_mask(dtype):
+    """Leaves closed by the lowest finite value have no weight, and a row of nothing else is shared evenly."""
+    l, g = made(40, 70, dtype, seed=3)
+    low = torch.finfo(DTYPES[dtype]).min
+    l[:, 5:60] = low
+    l[7] = low
+    for score in ("softmax", "sigmoid"):
+        leaves, gates = B.gbdt_route(l, 20, score=score)
+        want, want_gates = ref.route(l, 20, score=score)
+        assert torch.equal(leaves, want)
+        assert float((gates.double() - want_gates).abs().max()) <= 1e-6 and bool(torch.isfinite(gates).all())
+        assert bool((gates[7] == gates[7, 0]).all()) and abs(float(gates[7].sum()) - 1.0) < 1e-5
+        d = B.gbdt_route_grad(l, leaves, torch.randn(40, 20, generator=g).cuda(), score=score)
+        assert bool(torch.isfinite(d).all())
