@@ -155,8 +155,7 @@ struct ToGatedRows {
   }
 };
 
-// What a product over pairs leaves: slots; answers to rows of one leaf each; slots and dots of the gradient; dots alone come of that
-// with null slots.
+// Where a product over pairs leaves its answers: in slots, or weighed in the rows of y (k = 1).
 enum class Leaves { kSlots, kRows };
 
 // Answers of all pairs.  Bound by the matrix cores and by what a tile's beginning and end leave them idle: 65,536 pairs, 1,024 -> 1,024 in

@@ -468,7 +468,7 @@ __device__ __forceinline__ i32x4 mma(i32x4 rows, i32x4 cols, i32x4 acc) {
 // BM x BN values by WM x WN wavefronts.  A lane's four values of the 16 x 16 block (i, j) of its wavefront:
 //   N_INNER: m = 16 i + lane mod 16, n = 16 j + 4 (lane / 16) + 0..3   (rows of an output along n)
 //   else:    n = 16 j + lane mod 16, m = 16 i + 4 (lane / 16) + 0..3   (columns of an output along m)
-// DEEP (DIRECT only): steps of 64 bytes of k instead of 128, and four stages, or three if STAGES says so (more than two: DIRECT only).
+// DEEP (DIRECT only): steps of 64 bytes of k and four stages instead of 128 bytes and STAGES (more than two: DIRECT only).
 // PARTS: sums are taken in parts of 128 k (see tile_run); f32 operands' always are.
 template <typename T_, int BM_, int BN_, int WM_, int WN_, bool DIRECT_, bool DEEP_ = false, int STAGES_ = 2, bool PARTS_ = false>
 struct Shape {
@@ -477,7 +477,7 @@ struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NT = WM_ * WN_ * 64;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
   static constexpr bool DIRECT = DIRECT_, DEEP = DEEP_, PARTS = PARTS_ || sizeof(T_) == 4;
-  static constexpr int KB = DEEP ? 64 : 128, kStep = KB / (int)sizeof(T), kStages = DEEP && STAGES_ != 3 ? 4 : STAGES_;
+  static constexpr int KB = DEEP ? 64 : 128, kStep = KB / (int)sizeof(T), kStages = DEEP ? 4 : STAGES_;
   static constexpr int kStageBytes = (BM + BN) * KB;
   static constexpr int kLdsBytes = kStages * kStageBytes;
   static constexpr int kLastStage = (kStages - 1) * kStageBytes;
@@ -603,37 +603,35 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
   constexpr int part_steps = 128 / S::kStep;  // (f32: 4; bf16: 2, or 4 of half the length)
 
   if constexpr (S::DEEP) {
-    // A turn is a step.  Its stage is given up two blocks before the turn ends, when all of it has been read; the step as many
-    // turns ahead as there are stages goes there, a chunk at a time between the next turn's blocks: eight wavefronts that ask for all their chunks
+    // A turn is a step.  Its stage is given up two blocks before the turn ends, when all of it has been read; the step four
+    // turns ahead goes there, a chunk at a time between the next turn's blocks: eight wavefronts that ask for all their chunks
     // at once wait for the address units before they can go on to multiply.  (With two stages of twice the length a chunk
     // would have to be on its way before the next turn.)  Turns go in pairs, so that the fragments' places are known to the
     // compiler; an odd number is filled up with zeros.
     constexpr int per = A::kPer + B::kPer, loads = A::kLoads + B::kLoads;
     const int full = ((a.k_end < b.k_end ? a.k_end : b.k_end) - k0) / S::kStep;  // steps whose every chunk is loaded
     const int turns = (steps + 1) / 2 * 2;
-    constexpr int ns = S::kStages;
-    auto stage = [&](int step) { return lds + (ns == 4 ? step & 3 : (int)((uint32_t)step % ns)) * S::kStageBytes; };
     auto load_one = [&](auto whole, int step, int i) {
-      char* to = stage(step);
+      char* to = lds + (step & 3) * S::kStageBytes;
       if (i < A::kPer) {
         a.template load_one<decltype(whole)::value>(rows_a, to, i);
       } else {
         b.template load_one<decltype(whole)::value>(rows_b, to + A::kBytes, i - A::kPer);
       }
     };
-    auto first_reads = [&](const char* of, int turn) {
+    auto first_reads = [&](const char* stage, int turn) {
 #pragma unroll
-      for (int j = 0; j < S::TN; ++j) read_columns(of, 0, j, turn);
-      read_rows(of, 0, 0, 0);
+      for (int j = 0; j < S::TN; ++j) read_columns(stage, 0, j, turn);
+      read_rows(stage, 0, 0, 0);
       in_order();
-      read_rows(of, 0, 1, 1);
+      read_rows(stage, 0, 1, 1);
     };
     // WHOLE: the step that is loaded in this turn has no limit in it.
     auto one_turn = [&](auto whole, auto which, int at_turn) {
       constexpr int turn = decltype(which)::value;
-      const char* here = stage(at_turn);
-      const char* next = stage(at_turn + 1);
-      const bool more = decltype(whole)::value || at_turn + ns - 1 < turns;
+      const char* here = lds + (at_turn & 3) * S::kStageBytes;
+      const char* next = lds + ((at_turn + 1) & 3) * S::kStageBytes;
+      const bool more = decltype(whole)::value || at_turn + 3 < turns;
       for_blocks<0, S::TM - 2>([&](auto at) {
         constexpr int i = decltype(at)::value;
         read_rows(here, 0, i + 2, i + 2);
@@ -642,7 +640,7 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
         in_order();
         if (more) {
 #pragma unroll
-          for (int k = i * per / (S::TM - 2); k < (i + 1) * per / (S::TM - 2); ++k) load_one(whole, at_turn + ns - 1, k);
+          for (int k = i * per / (S::TM - 2); k < (i + 1) * per / (S::TM - 2); ++k) load_one(whole, at_turn + 3, k);
         }
         in_order();
       });
@@ -650,9 +648,9 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
         a.advance(rows_a);
         b.advance(rows_b);
       }
-      // The next step is there; those behind it may be on their way.
+      // The next step is there; the two behind it may be on their way.
       if (decltype(whole)::value) {
-        arrived<(ns - 2) * loads>();
+        arrived<2 * loads>();
       } else {
         arrived<0>();
       }
@@ -663,14 +661,14 @@ __device__ __forceinline__ void tile_run(char* lds, A& a, B& b, const RowsA& row
       add_part(at_turn % part_steps == part_steps - 1 || at_turn + 1 == turns);
       in_order();
     };
-    if (full > ns - 2) {
-      arrived<(ns - 2) * loads>();
+    if (full > 2) {
+      arrived<2 * loads>();
     } else {
       arrived<0>();
     }
     first_reads(lds, 0);
     int s = 0;
-    for (; s + ns < full; s += 2) {
+    for (; s + 4 < full; s += 2) {
       one_turn(Int<1>{}, Int<0>{}, s);
       one_turn(Int<1>{}, Int<1>{}, s + 1);
     }

@@ -95,7 +95,7 @@ def close(y, want, mag, roundings, k=1):
 
 
 SIZES = [(1, 255, 700, 256), (3, 4, 1, 1), (9, 5, 28, 16), (40, 3, 137, 33), (64, 64, 128, 100), (500, 7, 64, 10), (1000, 31, 2000, 64),
-         (3000, 5, 200, 130), (20_000, 8, 144, 300), (70_000, 4, 40, 24), (60_000, 3, 272, 128), (40_000, 2, 128, 512)]
+         (3000, 5, 200, 130), (20_000, 8, 144, 300), (70_000, 4, 40, 24), (60_000, 3, 272, 128), (40_000, 2, 128, 512), (70_000, 5, 100, 120)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -120,7 +120,7 @@ def test_leaf_products(dtype, size):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("k", [1, 3, 9])
 @pytest.mark.parametrize("size", [(1, 255, 700, 256), (5, 4, 20, 3), (64, 64, 128, 96), (900, 13, 137, 33), (5000, 6, 256, 200),
-                                  (12_000, 5, 64, 600)], ids=str)
+                                  (12_000, 5, 64, 600), (30_000, 5, 64, 100), (70_000, 4, 48, 300)], ids=str)
 def test_mixtures(dtype, k, size):
     n, n_leaves, d_in, d_out = size
     codes, scales, w, ws, b, g = made(*size, seed=n + k)

@@ -72,7 +72,7 @@ def check_grad(got, dy, x, w, b, leaves, gates):
 SIZES = [  # n, k, leaves, d_in, d_out, pad
     (1, 1, 1, 1, 1, 0), (1, 4, 255, 700, 256, 0), (3, 2, 5, 137, 33, 0), (4, 9, 31, 64, 1000, 0), (5, 3, 4, 3, 2, 1), (64, 4, 64, 128, 96, 0),
     (200, 1, 7, 40, 24, 8), (333, 3, 13, 137, 33, 6), (1000, 2, 8, 256, 130, 0), (777, 8, 255, 72, 64, 0), (130, 64, 10, 16, 16, 0),
-    (2500, 2, 3, 64, 257, 7), (600, 5, 1, 512, 20, 0), (5000, 2, 1100, 24, 8, 0), (9000, 1, 2, 8, 300, 0), (700, 6, 40, 1000, 4, 0),
+    (2500, 2, 3, 64, 257, 7), (600, 5, 1, 512, 20, 0), (400, 2, 5000, 16, 8, 0), (5000, 2, 1100, 24, 8, 0), (9000, 1, 2, 8, 300, 0), (700, 6, 40, 1000, 4, 0),
 ]
 
 
@@ -89,7 +89,9 @@ def test_sizes(dtype, size):
 
 
 @pytest.mark.parametrize("dtype,size", [("bf16", (20_000, 4, 16, 256, 512)), ("bf16", (3000, 8, 64, 512, 300)), ("f32", (6000, 3, 20, 200, 130)),
-                                        ("bf16", (40_000, 2, 9, 64, 48)), ("bf16", (30_000, 2, 2, 128, 136)), ("f32", (40_000, 2, 3, 24, 20))],
+                                        ("bf16", (40_000, 2, 9, 64, 48)), ("bf16", (40_000, 2, 7, 64, 100)),
+                                        ("bf16", (70_000, 1, 4, 64, 300)), ("bf16", (70_000, 1, 4, 40, 100)), ("f32", (20_000, 1, 4, 40, 100)),
+                                        ("bf16", (30_000, 2, 2, 128, 136)), ("f32", (40_000, 2, 3, 24, 20))],
                          ids=str)
 def test_larger(dtype, size):
     """Tiles of every kind, lists by many wavefronts, leaves cut into pieces."""
@@ -104,6 +106,14 @@ def test_several_blocks_of_rows_and_pieces_of_outputs():
     check_y(B.gbdt_mixture_product(x, w, leaves, gates, bias=b), x, w, b, leaves, gates)
     x, dy, w, b, leaves, gates = made(20_000, 4, 6, 1024, 2000, "bf16", seed=3, outside=0.01)
     check_grad(B.gbdt_mixture_product_grad(dy, x, w, leaves, gates, bias=b), dy, x, w, b, leaves, gates)
+
+
+@pytest.mark.parametrize("dtype,d_in", [("bf16", 2000), ("bf16", 1999), ("f32", 1000)])
+def test_pieces_longer_than_a_listing(dtype, d_in):
+    """Sums of 1,500 x d_in matrices that would pass the scratch with short pieces: 120,000 positions of two leaves."""
+    x, dy, w, b, leaves, gates = made(40_000, 3, 2, d_in, 1500, dtype, seed=15, outside=0.01)
+    got = B.gbdt_mixture_product_grad(dy, x, w, leaves, gates, bias=b, want=("weight", "bias"))
+    check_grad(got, dy, x, w, b, leaves, gates)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
