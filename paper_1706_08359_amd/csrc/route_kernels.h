@@ -311,6 +311,10 @@ __device__ __forceinline__ void load_logits(const T* row, int column, int n, flo
 template <typename V, int LANES, int PER>
 __device__ __forceinline__ void choice_values(const RouteArgs& g, const float (&l)[PER], float top, V (&v)[PER], V* tol) {
   const int lane = threadIdx.x & (LANES - 1);
+  float bias[PER];  // (one that is NaN closes its leaf, as minus infinity does)
+#pragma unroll
+  for (int i = 0; i < PER; ++i) bias[i] = 0.0f;
+  if (g.bias != nullptr) load_logits<float, PER>(g.bias, lane * PER, g.n_leaves, bias);
   V inverse = 1;
   if (!g.sigmoid) {
     V sum = 0;
@@ -323,9 +327,7 @@ __device__ __forceinline__ void choice_values(const RouteArgs& g, const float (&
   }
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int e = lane * PER + i;
-    V c = g.sigmoid ? quick_sigmoid((V)l[i]) : v[i] * inverse;
-    if (g.bias != nullptr && e < g.n_leaves) c += (V)g.bias[e];
+    const V c = (g.sigmoid ? quick_sigmoid((V)l[i]) : v[i] * inverse) + (V)bias[i];
     v[i] = l[i] > -INFINITY && c == c ? c : lowest<V>();
   }
   *tol = g.sigmoid ? (V)0x1p-20 : (V)0x1p-18 * inverse;
@@ -376,11 +378,13 @@ struct Slots {
 };
 
 // Bound by reading the logits where rows are many and k is small: 400,000 x 255 f32, four leaves each, 115 us, 3.7 TB/s.  A pick is some
-// 130 instructions for four rows of 256 columns: 16,384 x 256 bf16 in 8 groups, 8 leaves each by values, 23 us, 18 of it picks, 4 the few rows
-// that 64 bits decide, which end last; 65,536 x 64 f32, four leaves each by values, 14 us.
+// 130 instructions for four rows of 256 columns: 16,384 x 256 bf16 in 8 groups, 8 leaves each by values, 18 us, 12 of it nine picks, 4 the few
+// rows that 64 bits decide, which end last; 65,536 x 64 f32, four leaves each by values, 14 us.
 // VALUES: leaves are chosen by their values, not by the logits themselves.
+// (At most 128 registers, which only the 64-bit path would pass: 100,000 x 700 f32, 16 leaves each by
+// values, 295 us against 381.)
 template <typename T, int LANES, int PER, bool VALUES>
-__global__ void __launch_bounds__(kThreads) route_kernel(const RouteArgs g) {
+__global__ void __launch_bounds__(kThreads, 4) route_kernel(const RouteArgs g) {
   constexpr int rows = kThreads / LANES;
   const int r = threadIdx.x / LANES, lane = threadIdx.x & (LANES - 1);
   const int64_t d = g.first + (int64_t)blockIdx.x * rows + r;

@@ -62,14 +62,17 @@ int launch_route(RouteArgs g, bool grad, hipStream_t s) {
 }
 
 // (400,000 rows x 255, four leaves each: 125 us by sixteen lanes a row, 148 by eight, 158 by 32, 219 by 64.  65,536 x 64 with a bias and
-// the gradient: 25.5 by eight, 27.1 by sixteen.)
+// the gradient: 25.5 by eight, 27.1 by sixteen.  100,000 x 285, 16 leaves each: 105 by sixteen, 142 by 32; x 700: 200 by 32, 268 by 64; x
+// 1,024: 232 by 32, 256 by 64.)
 template <typename T>
 int route(const RouteArgs& g, bool grad, hipStream_t s) {
   if (g.n_leaves <= 64) return launch_route<T, 8, 8>(g, grad, s);
   if (g.n_leaves <= 128) return launch_route<T, 16, 8>(g, grad, s);
   if (g.n_leaves <= 256) return launch_route<T, 16, 16>(g, grad, s);
+  if (g.n_leaves <= 384) return launch_route<T, 16, 24>(g, grad, s);
   if (g.n_leaves <= 512) return launch_route<T, 32, 16>(g, grad, s);
-  return launch_route<T, 64, 16>(g, grad, s);
+  if (g.n_leaves <= 768) return launch_route<T, 32, 24>(g, grad, s);
+  return launch_route<T, 32, 32>(g, grad, s);
 }
 
 // ---------------------------------------------------------------- lists of pairs
