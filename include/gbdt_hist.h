@@ -608,9 +608,8 @@ int gbdt_route_grad(const void* logits, int64_t ld, const int32_t* leaves, const
  *   gates    DEVICE float [n_rows][k]
  *   y_out    DEVICE [n_rows][d_out]; zeros for a row without a leaf
  * Element types, distances and limits as for gbdt_leaf_product; k <= 64, n_leaves <= 16384, n_rows * k < 2^30.  The slots' answers
- * are kept in the library's scratch, of so many rows at a time as take 256 MiB or of 1,024, and
- * added in f32 in their order: the same call gives the same bits.  f32 answers are kept as they are, those of bf16 results with 11
- * bits, an eighth of the error that rounding the result has.
+ * are kept in the library's scratch in f32, of so many rows at a time as take 256 MiB or of 1,024, and
+ * added in f32 in their order: the same call gives the same bits.
  * gbdt_mixture_workspace_bytes: the size of a registered workspace that suffices for the three
  * gbdt_mixture_* calls (0 on invalid arguments).
  */

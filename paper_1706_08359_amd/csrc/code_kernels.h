@@ -114,9 +114,8 @@ enum class Place { kRow, kGatedRow, kSlot };
 
 template <typename O, Place WHERE>
 struct ToScaled {
-  typedef typename std::conditional<WHERE == Place::kSlot, typename SlotOf<O>::Type, O>::type Out;
-  static constexpr bool kScaled = true, kHalves = WHERE == Place::kSlot && sizeof(Out) == 2;
-  static constexpr bool kFinished = kHalves || WHERE == Place::kGatedRow, kDots = false;
+  typedef typename std::conditional<WHERE == Place::kSlot, float, O>::type Out;
+  static constexpr bool kScaled = true, kFinished = WHERE == Place::kGatedRow, kDots = false;
   Out* out;
   int64_t ld;
   const float* row_scales;
@@ -133,16 +132,10 @@ struct ToScaled {
   __device__ __forceinline__ float add(int64_t column) const { return bias ? bias[column] : 0.0f; }
   struct Beside {};
   template <int TN>
-  __device__ __forceinline__ void finish(const CodeArgs& g, int pair, int col, int cols, const Beside (&)[TN], f32x4 (&v)[TN]) const {
-    if constexpr (WHERE == Place::kGatedRow) {
-      const float gate = pair >= 0 ? g.gates[pair] : 0.0f;
+  __device__ __forceinline__ void finish(const CodeArgs& g, int pair, int, int, const Beside (&)[TN], f32x4 (&v)[TN]) const {
+    const float gate = pair >= 0 ? g.gates[pair] : 0.0f;
 #pragma unroll
-      for (int j = 0; j < TN; ++j) v[j] *= gate;
-    } else {
-      static_assert(TN * 16 == block_columns<int8_t>, "a wavefront's columns");
-      const float unit = to_units<TN>(v);
-      if ((threadIdx.x & 63) < 16 && pair >= 0 && col < cols) g.units[(int64_t)pair * g.blocks + col / (TN * 16)] = unit;
-    }
+    for (int j = 0; j < TN; ++j) v[j] *= gate;
   }
 };
 
@@ -154,7 +147,7 @@ __global__ void __launch_bounds__(S::NT, 2) code_product_kernel(const CodeArgs g
   __shared__ __align__(16) char lds[S::kLdsBytes];
   typedef ToScaled<O, WHERE> To;
   const bool slot = WHERE == Place::kSlot;
-  const To to = {(typename To::Out*)(slot ? g.slots : g.out), slot ? g.ld_slots : g.ld_out, g.row_scales, g.col_scales, g.add};
+  const To to = {(typename To::Out*)(slot ? (void*)g.slots : g.out), slot ? g.ld_slots : g.ld_out, g.row_scales, g.col_scales, g.add};
   rows_product<S, typename S::RowsB>(lds, g, g.x, g.ld_x, g.d_in, to, g.d_out);
 }
 

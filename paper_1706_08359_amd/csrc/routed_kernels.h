@@ -4,9 +4,9 @@
 // leaf_product_kernels.h, whose results go to a slot for every pair; a second kernel weighs and adds up a row's slots in order.  So
 // nothing is added from several workgroups to one place, the same call gives the same bits, and sums are f32.
 //
-// Slots of f32 results hold f32; those of bf16 results hold 11 bits, as fp16 values with a power of two for every pair and 64
-// columns: half the bytes, and an eighth of the error that rounding the result has anyway (8,192 rows x 8 leaves, 1,024 -> 1,024: products
-// 202 us with f32 slots, their sums 85).
+// Slots hold f32, of bf16 results as well: a row's answers may cancel in their sum, and outputs beside each other may be of any size.
+// (Half the bytes, as fp16 values with a power of two that 64 columns share, lost outputs beside one 2^29 times as large or closed by the
+// type's lowest value.)
 #pragma once
 
 #include "leaf_product_kernels.h"
@@ -15,83 +15,38 @@ namespace gbdt_routed {
 
 using namespace gbdt_leaf;
 
-typedef _Float16 f16;
-
 template <typename T>
 struct RoutedArgs : LeafArgs<T> {
   const int32_t* pair_idx;  // of the list's positions
   const int32_t* leaves;    // [n_rows][k]
   const float* gates;       // [n_rows][k]
   float* dgates;            // [n_rows][k] or null
-  void* slots;              // [n_rows * k][ld_slots] or null
-  float* units;             // fp16 slots: [n_rows * k][blocks], the powers of two
+  float* slots;             // [n_rows * k][ld_slots] or null
   float* dots;              // gradient: [n_rows * k][blocks], parts of <u, x>, or null
   int64_t ld_slots;         // a multiple of 16 bytes
   int32_t k, blocks;        // blocks of block_columns columns
 };
 
-// What results of type O are kept in until a row's are added up, and the columns of a wavefront in the tiles that make them.
-template <typename O> struct SlotOf;
-template <> struct SlotOf<bf16> { typedef f16 Type; };
-template <> struct SlotOf<float> { typedef float Type; };
+// The columns of a wavefront in the tiles that make slots.
 template <typename T> constexpr int block_columns = sizeof(T) == 4 ? 32 : 64;  // T: the operands'
 
 // ---------------------------------------------------------------- products to slots
 
-__device__ __forceinline__ float over_groups(float v, bool max) {  // over the four groups of 16 lanes
+__device__ __forceinline__ float over_groups(float v) {  // over the four groups of 16 lanes
 #pragma unroll
-  for (int m = 16; m < 64; m <<= 1) {
-    const float other = __shfl_xor(v, m);
-    v = max ? fmaxf(v, other) : v + other;
-  }
+  for (int m = 16; m < 64; m <<= 1) v += __shfl_xor(v, m);
   return v;
 }
 
-// Divides a row's values (4 TN of them a lane, 16 TN in all) by a power of two that brings the largest finite one to 2^14 .. 2^15, and
-// returns that power.  Infinities and NaN stay what they are, in their places.
-template <int TN>
-__device__ __forceinline__ float to_units(f32x4 (&v)[TN]) {
-  float most = 0.0f;
-#pragma unroll
-  for (int j = 0; j < TN; ++j)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(v[j][r]) < INFINITY ? fabsf(v[j][r]) : 0.0f);
-  most = over_groups(most, true);
-  const int e = (int)(__float_as_uint(most) >> 23), exponent = e < 15 ? 15 : e;
-  const float by = __uint_as_float((uint32_t)(268 - exponent) << 23);
-#pragma unroll
-  for (int j = 0; j < TN; ++j)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v[j][r] *= by;
-  return __uint_as_float((uint32_t)(exponent - 14) << 23);
-}
-
-// Up to four values of any alignment, zeros behind.
-template <typename T>
-__device__ __forceinline__ f32x4 load4_any(const T* p, int valid) {
-  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (valid >= 4) {
-    T t[4];
-    __builtin_memcpy(t, p, sizeof t);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (float)t[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-      if (i < valid) v[i] = (float)p[i];
-  }
-  return v;
-}
-
-// To the pairs' slots, of type H.  DOTS: each row's values also meet x's, and their sums over the wavefront's columns are left in
+// To the pairs' slots.  DOTS: each row's values also meet x's, and their sums over the wavefront's columns are left in
 // dots: dg[d][j] = <dy, W x + b> = <W^T dy, x> + <dy, b>, so the gates' gradient needs the answers of neither pass, only f32 values
 // that are in registers here.
-template <typename T, typename H, bool DOTS>
+template <typename T, bool DOTS>
 struct ToSlots {
-  typedef H Out;
-  static constexpr bool kScaled = false, kHalves = sizeof(H) == 2, kFinished = kHalves || DOTS, kDots = DOTS;
+  typedef float Out;
+  static constexpr bool kScaled = false, kFinished = DOTS, kDots = DOTS;
   const T* bias;
-  H* out;
+  float* out;
   int64_t ld;
   __device__ __forceinline__ int place(const RoutedArgs<T>& g, int p) const { return g.pair_idx[p]; }
   __device__ __forceinline__ float add(int64_t column) const { return bias ? (float)bias[column] : 0.0f; }
@@ -117,22 +72,15 @@ struct ToSlots {
   __device__ __forceinline__ void finish(const RoutedArgs<T>& g, int pair, int col, int cols, const Beside (&x)[TN], f32x4 (&v)[TN]) const {
     static_assert(TN * 16 == block_columns<T>, "a wavefront's columns");
     const int l = threadIdx.x & 63;
-    const int64_t block = (int64_t)pair * g.blocks + col / (TN * 16);
-    if constexpr (DOTS) {
-      float dot = 0.0f;
+    float dot = 0.0f;
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int n = col + 16 * j + 4 * (l >> 4);
+    for (int j = 0; j < TN; ++j) {
+      const int n = col + 16 * j + 4 * (l >> 4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) dot = n + r < cols ? __builtin_fmaf(v[j][r], (float)x[j].x[r], dot) : dot;
-      }
-      dot = over_groups(dot, false);
-      if (l < 16 && pair >= 0 && col < cols) g.dots[block] = dot;
+      for (int r = 0; r < 4; ++r) dot = n + r < cols ? __builtin_fmaf(v[j][r], (float)x[j].x[r], dot) : dot;
     }
-    if constexpr (kHalves) {
-      const float unit = to_units<TN>(v);
-      if (l < 16 && pair >= 0 && col < cols) g.units[block] = unit;
-    }
+    dot = over_groups(dot);
+    if (l < 16 && pair >= 0 && col < cols) g.dots[(int64_t)pair * g.blocks + col / (TN * 16)] = dot;
   }
 };
 
@@ -165,12 +113,11 @@ enum class Leaves { kSlots, kRows };
 template <class S, Leaves WHAT>
 __global__ void __launch_bounds__(S::NT, 2) routed_product_kernel(const RoutedArgs<typename S::T> g) {
   typedef typename S::T T;
-  typedef typename SlotOf<T>::Type H;
   __shared__ __align__(16) char lds[S::kLdsBytes];
   if constexpr (WHAT == Leaves::kRows) {
     rows_product<S, typename S::RowsB>(lds, g, g.x, g.ld_x, g.d_in, ToGatedRows<T>{g.bias, g.y, g.ld_y}, g.d_out);
   } else {
-    rows_product<S, typename S::RowsB>(lds, g, g.x, g.ld_x, g.d_in, ToSlots<T, H, false>{g.bias, (H*)g.slots, g.ld_slots}, g.d_out);
+    rows_product<S, typename S::RowsB>(lds, g, g.x, g.ld_x, g.d_in, ToSlots<T, false>{g.bias, g.slots, g.ld_slots}, g.d_out);
   }
 }
 
@@ -179,17 +126,15 @@ __global__ void __launch_bounds__(S::NT, 2) routed_product_kernel(const RoutedAr
 template <class S, bool DOTS>
 __global__ void __launch_bounds__(S::NT, 2) routed_grad_input_kernel(const RoutedArgs<typename S::T> g) {
   typedef typename S::T T;
-  typedef typename SlotOf<T>::Type H;
   __shared__ __align__(16) char lds[S::kLdsBytes];
-  rows_product<S, typename S::ColumnsB>(lds, g, g.dy, g.ld_dy, g.d_out, ToSlots<T, H, DOTS>{nullptr, (H*)g.slots, g.ld_slots}, g.d_in);
+  rows_product<S, typename S::ColumnsB>(lds, g, g.dy, g.ld_dy, g.d_out, ToSlots<T, DOTS>{nullptr, g.slots, g.ld_slots}, g.d_in);
 }
 
 // ---------------------------------------------------------------- sums of slots
 
 template <typename O>
 struct CombineArgs {
-  const void* slots;      // [n_rows * k][ld]; a slot whose leaf is none holds anything
-  const float* units;     // [n_rows * k][blocks]
+  const float* slots;     // [n_rows * k][ld]; a slot whose leaf is none holds anything
   const int32_t* leaves;  // [n_rows][k]
   const float* gates;     // [n_rows][k]
   O* out;                 // [n_rows][cols] or null
@@ -281,8 +226,7 @@ __device__ __forceinline__ void gate_gradients(const CombineArgs<O>& g, int64_t 
 // are in the memory-side cache); x 4, 18 us, with the gates' gradients 28.
 template <typename O, int LANES, bool GATES>
 __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs<O> g) {
-  typedef typename SlotOf<O>::Type H;
-  constexpr int n = 16 / (int)sizeof(H);
+  constexpr int n = 4;
   const int64_t d = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   if (d >= g.n_rows) return;
   const int l = threadIdx.x & (LANES - 1);
@@ -297,22 +241,17 @@ __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs<O> g) {
       for (int e = 0; e < n; ++e) sum[e] = 0.0f;
       for (int j0 = 0; j0 < g.k; j0 += kSlotsAtOnce) {
         if (!once) slots.load(g, p0, j0);
-        float unit[kSlotsAtOnce];
         u32x4 raw[kSlotsAtOnce];
 #pragma unroll
-        for (int i = 0; i < kSlotsAtOnce; ++i) {
-          const int64_t p = p0 + j0 + i;
-          const bool there = slots.leaf[i] >= 0;
-          raw[i] = load16(there ? (const void*)((const H*)g.slots + p * g.ld + c) : (const void*)zero_chunk);
-          unit[i] = sizeof(H) == 4 ? 1.0f : load_float(there ? g.units + p * g.blocks + c / 64 : (const float*)zero_chunk);
-        }
+        for (int i = 0; i < kSlotsAtOnce; ++i)
+          raw[i] = load16(slots.leaf[i] >= 0 ? (const void*)(g.slots + (p0 + j0 + i) * g.ld + c) : (const void*)zero_chunk);
 #pragma unroll
         for (int i = 0; i < kSlotsAtOnce; ++i) {
-          const float by = slots.leaf[i] < 0 ? 0.0f : sizeof(H) == 4 ? slots.gate[i] : slots.gate[i] * unit[i];
-          H v[n];
+          const float by = slots.leaf[i] < 0 ? 0.0f : slots.gate[i];
+          float v[n];
           __builtin_memcpy(v, &raw[i], 16);
 #pragma unroll
-          for (int e = 0; e < n; ++e) sum[e] = __builtin_fmaf(by, (float)v[e], sum[e]);
+          for (int e = 0; e < n; ++e) sum[e] = __builtin_fmaf(by, v[e], sum[e]);
         }
       }
       O* to = g.out + d * g.ld_out + c;

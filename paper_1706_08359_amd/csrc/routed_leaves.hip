@@ -157,26 +157,25 @@ constexpr int64_t kGatedBytes = (int64_t)256 << 20;
 constexpr int32_t kMaxSlots = 64;  // leaves a row
 constexpr int64_t kMaxGridRows = 65535;  // rows of a launch's second dimension
 
-// e: bytes of a slot's value; block: columns that share a power of two or a part of a dot product.
+// block: columns of a part of a dot product.
 struct SlotPlan {
   int64_t rows, ld, blocks;  // rows at a time
   ListPlan list;
-  size_t slots_bytes, units_bytes, dots_bytes;
-  size_t bytes() const { return list.bytes() + slots_bytes + units_bytes + dots_bytes; }
+  size_t slots_bytes, dots_bytes;
+  size_t bytes() const { return list.bytes() + slots_bytes + dots_bytes; }
 };
-SlotPlan slot_plan(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t cols, int64_t e, int64_t block, bool dots) {
+SlotPlan slot_plan(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t cols, int64_t block, bool dots) {
   SlotPlan p = {};
   if (k == 1 && !dots) {  // answers go to their rows, all at once
     p.rows = n_rows;
     p.list = list_plan(n_rows, n_leaves);
     return p;
   }
-  p.ld = round_up(cols, 16 / e);
+  p.ld = round_up(cols, 4);
   p.blocks = ceil_div(cols, block);
-  p.rows = std::min(n_rows, std::max<int64_t>(1024, kSlotsBytes / (k * p.ld * e)));
+  p.rows = std::min(n_rows, std::max<int64_t>(1024, kSlotsBytes / (k * p.ld * 4)));
   p.list = list_plan(p.rows * k, n_leaves);
-  p.slots_bytes = pad256((size_t)(p.rows * k * p.ld * e));
-  p.units_bytes = e == 2 ? pad256((size_t)(p.rows * k * p.blocks) * 4) : 0;
+  p.slots_bytes = pad256((size_t)(p.rows * k * p.ld * 4));
   p.dots_bytes = dots ? pad256((size_t)(p.rows * k * p.blocks) * 4) : 0;
   return p;
 }
@@ -314,9 +313,8 @@ int by_slots(const G& all, int64_t n_rows, int64_t cols, const CombineArgs<O>& t
     int rc = make_lists(list, g.leaves, g.n_leaves, g.k, scratch, &g.offsets, &g.row_idx, &g.pair_idx, s);
     if (rc != GBDT_OK) return rc;
     char* at = scratch + plan.list.bytes();
-    g.slots = direct || !to.out ? nullptr : at;
-    g.units = (float*)(at + plan.slots_bytes);
-    g.dots = to.dgates ? (float*)(at + plan.slots_bytes + plan.units_bytes) : nullptr;
+    g.slots = direct || !to.out ? nullptr : (float*)at;
+    g.dots = to.dgates ? (float*)(at + plan.slots_bytes) : nullptr;
     g.ld_slots = plan.ld;
     g.blocks = (int32_t)plan.blocks;
     g.n_rows = (int32_t)n;
@@ -330,7 +328,6 @@ int by_slots(const G& all, int64_t n_rows, int64_t cols, const CombineArgs<O>& t
     }
     CombineArgs<O> c = to;
     c.slots = g.slots;
-    c.units = g.units;
     c.dots = g.dots;
     c.leaves = g.leaves;
     c.gates = g.gates;
@@ -358,7 +355,7 @@ int mixture_product(RoutedArgs<T>& g, int64_t n_rows, hipStream_t s) {
     LAUNCHED("routed_few_kernel");
     return GBDT_OK;
   }
-  const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out, sizeof(T), gbdt_routed::block_columns<T>, false);
+  const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out, gbdt_routed::block_columns<T>, false);
   void* ws = nullptr;
   const int rc = gbdt_internal::workspace(plan.bytes(), s, &ws);
   if (rc != GBDT_OK) return rc;
@@ -422,7 +419,7 @@ template <typename T>
 int mixture_product_grad(RoutedArgs<T>& g, int64_t n_rows, hipStream_t s) {
   const bool weights = g.dw || g.dbias, rows = (g.dx || g.dgates) && n_rows > 0;
   if (!weights && !rows) return GBDT_OK;
-  const SlotPlan slots = slot_plan(n_rows, g.k, g.n_leaves, g.d_in, sizeof(T), gbdt_routed::block_columns<T>, true);
+  const SlotPlan slots = slot_plan(n_rows, g.k, g.n_leaves, g.d_in, gbdt_routed::block_columns<T>, true);
   const WeightPlan sums = weight_plan(n_rows, g.k, g.n_leaves, g.dw ? g.d_in : kChunk<T>, g.d_out, sizeof(T), gbdt_internal::cu_count());
   if (weights && sums.sums.tiles > most_blocks(kGradThreads) / 8) return GBDT_EUNSUPPORTED;
   void* ws = nullptr;
@@ -564,7 +561,7 @@ int leaf_codes(CodeArgs& g, hipStream_t s) {
 template <typename O>
 int mixture_codes(CodeArgs& g, int64_t n_rows, hipStream_t s) {
   if (few_rows<int8_t>(n_rows, g.k, g.n_leaves, g.d_in, g.d_out)) return code_few<O, false>(g, n_rows, s);
-  const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out, sizeof(O), gbdt_routed::block_columns<int8_t>, false);
+  const SlotPlan plan = slot_plan(n_rows, g.k, g.n_leaves, g.d_out, gbdt_routed::block_columns<int8_t>, false);
   void* ws = nullptr;
   const int rc = gbdt_internal::workspace(plan.bytes(), s, &ws);
   if (rc != GBDT_OK) return rc;
@@ -651,7 +648,7 @@ size_t gbdt_mixture_workspace_bytes(int64_t n_rows, int32_t k, int32_t n_leaves,
   const int64_t e = dtype == GBDT_F32 ? 4 : 2, units = gbdt_internal::cu_count();
   size_t most = 0;
   const int64_t block = dtype == GBDT_F32 ? 32 : 64;  // (a product of codes takes no more)
-  for (int64_t cols : {d_in, d_out}) most = std::max(most, slot_plan(n_rows, k, n_leaves, cols, e, block, true).bytes());
+  for (int64_t cols : {d_in, d_out}) most = std::max(most, slot_plan(n_rows, k, n_leaves, cols, block, true).bytes());
   for (int64_t inputs : {(int64_t)d_in, 16 / e}) most = std::max(most, weight_plan(n_rows, k, n_leaves, inputs, d_out, e, units).bytes());
   return gbdt_internal::workspace_head_bytes() + most;
 }
