@@ -566,7 +566,7 @@ int gbdt_softmax_stats(const void* h, int64_t ld_h, const void* classes, int64_t
  *
  * The k leaves e_1 .. e_k with the largest choice values c are taken, largest first, of equal values
  * the lowest leaf first; without a bias the order is that of the logits.  Choices are those of exact
- * arithmetic to about 1e-15 of the scores.  A leaf whose logit is NaN or minus infinity, or whose c is, is never taken; where
+ * arithmetic to about 1e-15 of the scores and of the size of the c that decide.  A leaf whose logit is NaN or minus infinity, or whose c is, is never taken; where
  * fewer than k are left the other slots have leaf -1 and weight 0.  (Softmax: infinite logits share
  * all of the probability.)
  * With n_groups > 1 the leaves fall into as many groups of neighbours of equal size, and only leaves of the groups_kept

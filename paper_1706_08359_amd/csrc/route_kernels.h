@@ -165,7 +165,33 @@ __device__ __forceinline__ bool take_largest(V (&v)[PER], V* value, int* column)
   return any;
 }
 
-// Values of all but the best groups become masked.  True if the border is closer than `tol` says (of single values).
+// What a group's value may be off by, for a value that is one or one + two (two: lowest() if there is none): each is off by tol and by
+// 2^-23 of its own size, which may be any multiple of their sum's where they cancel.
+template <typename V>
+__device__ __forceinline__ V group_error(V one, V two, V tol) {
+  return tol + (V)0x1p-22 * (fabs(one) + (two > lowest<V>() ? fabs(two) : (V)0));
+}
+// The border between groups: `least` the least that the values of kept ones can be, `next` the most that the others' can.
+template <typename V>
+struct Border {
+  V least = (V)INFINITY, next = lowest<V>();
+  __device__ __forceinline__ void add(bool kept, V worth, V error) {
+    const bool any = error < (V)INFINITY;  // (values whose sum leaves the numbers are anywhere)
+    const V low = any ? worth - error : lowest<V>(), high = any ? worth + error : (V)INFINITY;
+    if (kept) {
+      least = low < least ? low : least;
+    } else {
+      next = high > next ? high : next;
+    }
+  }
+  template <int LANES>
+  __device__ __forceinline__ bool close() const {
+    const V low = -over_lanes<LANES>(-least, Max{}), high = over_lanes<LANES>(next, Max{});
+    return high > lowest<V>() && !(low > high);
+  }
+};
+
+// Values of all but the best groups become masked.  True if the border is closer than the values' errors say.
 template <typename V, int LANES, int PER>
 __device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V tol) {
   const int lane = threadIdx.x & (LANES - 1);
@@ -184,7 +210,8 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V t
       two = Max{}(Max{}(two, next), lower);
       one = Max{}(one, other);
     }
-    const V worth = g.group_best == 2 && two > lowest<V>() ? one + two : one;
+    if (g.group_best == 1) two = lowest<V>();
+    const V worth = two > lowest<V>() ? one + two : one;
     const int mine = lane / lanes;
     int before = 0;  // groups that come before this lane's
     for (int q = 0; q < g.n_groups; ++q) {
@@ -192,62 +219,61 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V t
       before += other > worth || (other == worth && q < mine) ? 1 : 0;
     }
     const bool group = mine < g.n_groups, kept = group && before < g.groups_kept && worth > lowest<V>();
-    const V least = -over_lanes<LANES>(kept ? -worth : lowest<V>(), Max{});
-    const V next = over_lanes<LANES>(group && !kept ? worth : lowest<V>(), Max{});
+    Border<V> border;
+    if (group && worth > lowest<V>()) border.add(kept, worth, group_error(one, two, tol));
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] = kept ? v[i] : lowest<V>();
-    return next > lowest<V>() && !(least - next > 2 * tol + (V)0x1p-21 * fabs(least));
+    return border.template close<LANES>();
   }
   // groups of any size, one after another; lane q mod LANES keeps group q's value
   constexpr int most = (kMaxGroups + LANES - 1) / LANES;
-  V mine[most];
+  V mine[most], left[most], error[most];  // values, those not yet taken, errors
   int group[PER];
 #pragma unroll
-  for (int t = 0; t < most; ++t) mine[t] = lowest<V>();
+  for (int t = 0; t < most; ++t) mine[t] = error[t] = lowest<V>();
 #pragma unroll
   for (int i = 0; i < PER; ++i) group[i] = (lane * PER + i) / g.group_size;
   for (int q = 0; q < g.n_groups; ++q) {
     V in[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) in[i] = group[i] == q ? v[i] : lowest<V>();
-    V sum = lowest<V>(), second;
+    V one = lowest<V>(), two = lowest<V>();
     int column;
-    if (take_largest<V, LANES, PER>(in, &sum, &column) && g.group_best == 2) {
-      if (take_largest<V, LANES, PER>(in, &second, &column)) sum += second;
-    }
+    if (take_largest<V, LANES, PER>(in, &one, &column) && g.group_best == 2) take_largest<V, LANES, PER>(in, &two, &column);
+    const V worth = two > lowest<V>() ? one + two : one, off = group_error(one, two, tol);
 #pragma unroll
-    for (int t = 0; t < most; ++t) mine[t] = lane + t * LANES == q ? sum : mine[t];
+    for (int t = 0; t < most; ++t)
+      if (lane + t * LANES == q) mine[t] = worth, error[t] = off;
   }
   uint64_t kept = 0;
-  bool close = false;
-  V last = lowest<V>();
-  for (int r = 0; r <= g.groups_kept; ++r) {
-    V top = mine[0];
 #pragma unroll
-    for (int t = 1; t < most; ++t) top = Max{}(top, mine[t]);
+  for (int t = 0; t < most; ++t) left[t] = mine[t];
+  for (int r = 0; r < g.groups_kept; ++r) {
+    V top = left[0];
+#pragma unroll
+    for (int t = 1; t < most; ++t) top = Max{}(top, left[t]);
     top = over_lanes<LANES>(top, Max{});
-    if (r == g.groups_kept) {
-      close = top > lowest<V>() && !(last - top > 2 * tol + (V)0x1p-21 * fabs(last));
-      break;
-    }
     int who = kMaxGroups;
 #pragma unroll
     for (int t = most - 1; t >= 0; --t) {
-      const uint64_t w = row_ballot<LANES>(mine[t] == top);
+      const uint64_t w = row_ballot<LANES>(left[t] == top);
       if (w) who = t * LANES + __ffsll((unsigned long long)w) - 1;
     }
     if (top > lowest<V>()) {
       kept |= 1ull << who;
-      last = top;
 #pragma unroll
       for (int t = 0; t < most; ++t)
-        if (lane + t * LANES == who) mine[t] = lowest<V>();
+        if (lane + t * LANES == who) left[t] = lowest<V>();
     }
   }
+  Border<V> border;
+#pragma unroll
+  for (int t = 0; t < most; ++t)
+    if (mine[t] > lowest<V>()) border.add(kept >> (lane + t * LANES) & 1, mine[t], error[t]);
 #pragma unroll
   for (int i = 0; i < PER; ++i)
     if (!(group[i] < g.n_groups && kept >> group[i] & 1)) v[i] = lowest<V>();
-  return close;
+  return border.template close<LANES>();
 }
 
 // Slots of a row's k chosen leaves: lane i has the slots i, i + LANES, ..

@@ -1,0 +1,52 @@
+"""Borders between groups that 32 bits cannot draw: pairs of choice values that nearly cancel.  Chosen leaves equal those of the
+definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from oracle import routed_leaves as ref
+from paper_1706_08359_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def nearly_tied(n, n_groups, group_size, score, size, seed):
+    """Logits, and biases that give each group two open leaves of opposite sign, about size, whose values add up to nearly the same
+    in all groups; the group's other leaves are closed by their logits."""
+    g = torch.Generator().manual_seed(seed)
+    row = torch.randn(1, n_groups * group_size, generator=g)
+    row.view(n_groups, group_size)[:, 2:] = -math.inf
+    s = ref.scores(row, score)[0].view(n_groups, group_size)
+    bias = torch.zeros(n_groups, group_size)
+    up = torch.rand(n_groups, generator=g) < 0.5
+    first = (size * (1 + 0.25 * torch.rand(n_groups, generator=g))) * torch.where(up, 1.0, -1.0)
+    bias[:, 0] = first
+    bias[:, 1] = (0.03 - s[:, 0] - s[:, 1] - first.double()).float()
+    l = row.repeat(n, 1)
+    l[1:] += torch.randn(n - 1, l.shape[1], generator=g) * size * 1e-7
+    return l, bias.view(-1)
+
+
+def group_values(l, bias, score, n_groups):
+    c = ref.scores(l, score)[0] + bias.double()
+    c = torch.where(l.double() == -math.inf, -math.inf, c).view(l.shape[0], n_groups, -1)
+    return torch.sort(c, 2, descending=True)[0][:, :, :2].sum(2)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("size", [17.0, 110.0, 1000.0])
+@pytest.mark.parametrize("n_groups,group_size,kept", [(32, 2, 6), (8, 8, 3), (16, 16, 5), (4, 16, 2), (12, 32, 4), (64, 16, 16)])
+def test_two_best_values_that_cancel(score, size, n_groups, group_size, kept):
+    l, bias = nearly_tied(400, n_groups, group_size, score, size, seed=n_groups)
+    worth = torch.sort(group_values(l, bias, score, n_groups), 1, descending=True)[0]
+    gap = worth[:, kept - 1] - worth[:, kept]
+    told = gap > 1e-11 * size   # what 64 bits tell apart
+    assert int(told.sum()) > 390 and float(gap.median()) < 1e-6 * size
+    how = dict(score=score, n_groups=n_groups, groups_kept=kept, group_best=2)
+    leaves, _ = B.gbdt_route(l.cuda(), 2 * kept, choice_bias=bias.cuda(), **how)
+    want, _ = ref.route(l, 2 * kept, choice_bias=bias, **how)
+    # (both leaves of a kept group are taken, so groups alone decide; the order of leaves of nearly equal values is another matter)
+    leaves, want = torch.sort(leaves.cpu(), 1)[0], torch.sort(want, 1)[0]
+    wrong = (leaves != want).any(1) & told
+    assert not bool(wrong.any()), int(wrong.sum())
