@@ -171,6 +171,14 @@ template <typename V>
 __device__ __forceinline__ V group_error(V one, V two, V tol) {
   return tol + (V)0x1p-22 * (fabs(one) + (two > lowest<V>() ? fabs(two) : (V)0));
 }
+// A group's value.  Two lowest values, as leaves are closed with, add up to minus infinity in f32, which is a group without a leaf: such a
+// one stays below all others, has an error without end, and 64 bits tell it from its like.
+template <typename V>
+__device__ __forceinline__ V group_value(V one, V two) {
+  if (!(two > lowest<V>())) return one;
+  const V sum = one + two;
+  return sum > lowest<V>() ? sum : -(V)__FLT_MAX__;
+}
 // The border between groups: `least` the least that the values of kept ones can be, `next` the most that the others' can.
 template <typename V>
 struct Border {
@@ -211,7 +219,7 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V t
       one = Max{}(one, other);
     }
     if (g.group_best == 1) two = lowest<V>();
-    const V worth = two > lowest<V>() ? one + two : one;
+    const V worth = group_value(one, two);
     const int mine = lane / lanes;
     int before = 0;  // groups that come before this lane's
     for (int q = 0; q < g.n_groups; ++q) {
@@ -240,7 +248,7 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V t
     V one = lowest<V>(), two = lowest<V>();
     int column;
     if (take_largest<V, LANES, PER>(in, &one, &column) && g.group_best == 2) take_largest<V, LANES, PER>(in, &two, &column);
-    const V worth = two > lowest<V>() ? one + two : one, off = group_error(one, two, tol);
+    const V worth = group_value(one, two), off = group_error(one, two, tol);
 #pragma unroll
     for (int t = 0; t < most; ++t)
       if (lane + t * LANES == q) mine[t] = worth, error[t] = off;

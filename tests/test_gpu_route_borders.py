@@ -1,5 +1,5 @@
-"""Borders between groups that 32 bits cannot draw: pairs of choice values that nearly cancel.  Chosen leaves equal those of the
-definition in 64 bits."""
+"""Borders between groups that 32 bits cannot draw: pairs of choice values that nearly cancel, leaves closed by a lowest value as their
+bias.  Chosen leaves equal those of the definition in 64 bits."""
 import math
 
 import pytest
@@ -50,3 +50,25 @@ def test_two_best_values_that_cancel(score, size, n_groups, group_size, kept):
     leaves, want = torch.sort(leaves.cpu(), 1)[0], torch.sort(want, 1)[0]
     wrong = (leaves != want).any(1) & told
     assert not bool(wrong.any()), int(wrong.sum())
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("low", [torch.finfo(torch.float32).min, torch.finfo(torch.bfloat16).min, -2e38], ids=str)
+@pytest.mark.parametrize("n_groups,group_size", [(8, 8), (8, 3), (8, 16), (16, 32), (6, 2)])
+def test_groups_closed_by_the_lowest_value(score, low, n_groups, group_size):
+    """Two groups are open, one has a single open leaf, the others are closed by a bias whose double leaves the 32-bit numbers: they
+    come after all others, the lowest first, and are taken where more groups are kept than are open."""
+    g = torch.Generator().manual_seed(group_size)
+    l = torch.randn(50, n_groups * group_size, generator=g)
+    bias = torch.full((n_groups, group_size), low)
+    bias[1], bias[n_groups - 1] = 0.1, 0.0
+    bias[3, 1] = 0.2
+    bias = bias.view(-1)
+    for kept in (2, 3, 4, n_groups):
+        how = dict(score=score, n_groups=n_groups, groups_kept=kept, group_best=2)
+        k = min(32, kept * group_size)
+        leaves, gates = B.gbdt_route(l.cuda(), k, choice_bias=bias.cuda(), **how)
+        want, want_gates = ref.route(l, k, choice_bias=bias, **how)
+        assert torch.equal(leaves.cpu(), want), kept
+        assert bool((leaves >= 0).all())
+        assert bool(((gates.cpu().double() - want_gates).abs() <= 1e-4 * want_gates.abs() + 1e-37).all())
