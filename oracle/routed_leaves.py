@@ -24,16 +24,16 @@ def route(logits, k, choice_bias=None, score="softmax", n_groups=1, groups_kept=
     """(leaves int32, gates float64)."""
     s, l = scores(logits, score)
     n, n_leaves = l.shape
-    plain = choice_bias is None and (group_best == 1 or n_groups == 1)
-    c = l.clone() if plain else s if choice_bias is None else s + choice_bias.double()
-    c = torch.where((l == LOW) | torch.isnan(c), torch.full_like(c, LOW), c)
+    c = l if choice_bias is None else s + choice_bias.double()  # what leaves are chosen by
+    v = s if choice_bias is None and group_best == 2 else c      # what groups are worth
+    c, v = (torch.where((l == LOW) | torch.isnan(c), torch.full_like(c, LOW), t) for t in (c, v))
     if n_groups > 1:
-        g = c.view(n, n_groups, -1)
+        g = v.view(n, n_groups, -1)
         best = torch.sort(g, dim=2, descending=True)[0][:, :, :group_best]
         worth = torch.where(best[:, :, 0] == LOW, best[:, :, 0], torch.where(best == LOW, 0.0, best).sum(2))
         order = torch.sort(worth, dim=1, descending=True, stable=True)[1][:, :groups_kept]
         keep = torch.zeros_like(worth, dtype=torch.bool).scatter_(1, order, True)
-        c = torch.where(keep[:, :, None], g, LOW).reshape(n, n_leaves)
+        c = torch.where(keep[:, :, None], c.view(n, n_groups, -1), LOW).reshape(n, n_leaves)
     top, at = torch.sort(c, dim=1, descending=True, stable=True)
     top, at = top[:, :k], at[:, :k]
     leaves = torch.where(top == LOW, -1, at).to(torch.int32)

@@ -288,12 +288,11 @@ __device__ __forceinline__ bool keep_groups(const RouteArgs& g, V (&v)[PER], V t
 template <int LANES>
 constexpr int kSlotsOf = (kMaxChosen + LANES - 1) / LANES;
 
-// The k columns of the largest values, -1 where fewer are left.  True if two of the first k + 1 are closer than their errors, tol of
+// The k columns of the largest values, -1 where fewer are left.  check: true if two of the first k + 1 are closer than their errors, tol of
 // each and 2^-23 of its size.
 template <typename V, int LANES, int PER>
 __device__ __forceinline__ bool choose(const RouteArgs& g, V (&v)[PER], V tol, bool check, int (&picked)[kSlotsOf<LANES>]) {
   bool close = false;
-  if (g.n_groups > 1) close = keep_groups<V, LANES, PER>(g, v, tol) && check;
   const int lane = threadIdx.x & (LANES - 1), more = check && g.k < g.n_leaves ? 1 : 0;
   typedef decltype(key_of(V())) Key;
   Key keys[PER];
@@ -367,6 +366,16 @@ __device__ __forceinline__ void choice_values(const RouteArgs& g, const float (&
   *tol = g.sigmoid ? (V)0x1p-20 : (V)0x1p-18 * inverse;
 }
 
+// Without a bias, leaves of the groups that their values keep go by their logits, as they do without groups: scores may be equal where
+// logits are not.  (Read again: few lanes have room for both.)
+template <typename T, typename V, int PER>
+__device__ __forceinline__ void logits_for_values(const T* row, int column, int n, V (&v)[PER]) {
+  float l[PER];
+  load_logits<T, PER>(row, column, n, l);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) v[i] = v[i] > lowest<V>() ? (V)l[i] : lowest<V>();
+}
+
 // exp(l - c) / (1 + exp(l)) for l < 0, its limit for the others (whose c is 0): the sigmoid over exp(c), which renormalised
 // weights leave out, so that they hold however small all scores are.
 __device__ __forceinline__ float sigmoid_over(float l, float c) { return l >= 0.0f ? sigmoid(l) : expf(l - c) / (1.0f + expf(l)); }
@@ -414,7 +423,7 @@ struct Slots {
 // Bound by reading the logits where rows are many and k is small: 400,000 x 255 f32, four leaves each, 115 us, 3.7 TB/s.  A pick is some
 // 130 instructions for four rows of 256 columns: 16,384 x 256 bf16 in 8 groups, 8 leaves each by values, 18 us, 12 of it nine picks, 4 the few
 // rows that 64 bits decide, which end last; 65,536 x 64 f32, four leaves each by values, 14 us.
-// VALUES: leaves are chosen by their values, not by the logits themselves.
+// VALUES: leaves (without a bias: their groups) are chosen by their values, not by the logits themselves.
 // (At most 128 registers, which only the 64-bit path would pass: 100,000 x 700 f32, 16 leaves each by
 // values, 295 us against 381.)
 template <typename T, int LANES, int PER, bool VALUES>
@@ -439,11 +448,15 @@ __global__ void __launch_bounds__(kThreads, 4) route_kernel(const RouteArgs g) {
       inverse = 1.0f / over_lanes<LANES>(sum, Sum{});
     }
     if constexpr (!VALUES) {
+      if (g.n_groups > 1) keep_groups<float, LANES, PER>(g, l, 0.0f);
       choose<float, LANES, PER>(g, l, 0.0f, false, picked);
     } else {
       float v[PER], tol;
       choice_values<float, LANES, PER>(g, l, top, v, &tol);
-      const bool close = choose<float, LANES, PER>(g, v, tol, true, picked);
+      bool close = g.n_groups > 1 && keep_groups<float, LANES, PER>(g, v, tol);
+      const bool by_values = g.bias != nullptr;
+      if (!by_values) logits_for_values<T, float, PER>(row, lane * PER, g.n_leaves, v);
+      close |= choose<float, LANES, PER>(g, v, tol, by_values, picked);
       // rows to be taken again, all 64 lanes a row
       constexpr int wide = (LANES * PER + 63) / 64;
       uint64_t again = __ballot(close && lane == 0);
@@ -460,6 +473,8 @@ __global__ void __launch_bounds__(kThreads, 4) route_kernel(const RouteArgs g) {
         double exact[wide], none;
         choice_values<double, 64, wide>(g, logits, most, exact, &none);
         int chosen[kSlotsOf<64>];
+        if (g.n_groups > 1) keep_groups<double, 64, wide>(g, exact, none);
+        if (!by_values) logits_for_values<T, double, wide>((const T*)g.logits + other * g.ld, (threadIdx.x & 63) * wide, g.n_leaves, exact);
         choose<double, 64, wide>(g, exact, none, false, chosen);
 #pragma unroll
         for (int t = 0; t < kSlotsOf<LANES>; ++t) {

@@ -1,5 +1,5 @@
 """Borders between groups that 32 bits cannot draw: pairs of choice values that nearly cancel, leaves closed by a lowest value as their
-bias.  Chosen leaves equal those of the definition in 64 bits."""
+bias, scores that are saturated.  Chosen leaves equal those of the definition in 64 bits."""
 import math
 
 import pytest
@@ -72,3 +72,26 @@ def test_groups_closed_by_the_lowest_value(score, low, n_groups, group_size):
         assert torch.equal(leaves.cpu(), want), kept
         assert bool((leaves >= 0).all())
         assert bool(((gates.cpu().double() - want_gates).abs() <= 1e-4 * want_gates.abs() + 1e-37).all())
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n_groups,group_size,kept", [(4, 4, 2), (8, 8, 3), (4, 64, 2), (3, 43, 1), (16, 32, 5)])
+def test_without_a_bias_the_order_is_that_of_the_logits(score, dtype, n_groups, group_size, kept):
+    """Sigmoids of logits from 37 on are all 1 in 64 bits, softmaxes of those 745 below the largest all 0: in the groups that their two
+    best scores keep, leaves are taken by their logits all the same."""
+    g = torch.Generator().manual_seed(group_size)
+    n = n_groups * group_size
+    l = (torch.randperm(n, generator=g)[None] * torch.ones(40, 1) * 0.5 + 38.0)
+    l[10:20] = torch.randperm(n, generator=g) * -900.0
+    l[20:30] = torch.randn(10, n, generator=g) * 30 + 40
+    l[30:] = torch.randn(10, n, generator=g) * 600
+    l = torch.where((l > 28) & (l < 38.5), l + 11, l).to(dtype)   # (between, sigmoids differ from 1 by a last place or two)
+    how = dict(score=score, n_groups=n_groups, groups_kept=kept, group_best=2)
+    k = min(32, kept * group_size)
+    leaves, gates = B.gbdt_route(l.cuda(), k, **how)
+    leaves = leaves.cpu().long()
+    took = l.double().gather(1, leaves)
+    assert bool((took[:, 1:] <= took[:, :-1]).all())
+    want, _ = ref.route(l, k, **how)
+    assert torch.equal(leaves, want.long())
