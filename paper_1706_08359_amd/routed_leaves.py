@@ -18,7 +18,7 @@ import torch
 from . import binding as B
 from . import linear_leaves as L
 
-MAX_LEAVES_A_ROW = 64   # of one call; a forest of more trees takes several
+MAX_LEAVES_A_ROW, MAX_LEAVES = 64, 16384   # of one call; a forest of more trees, or of more leaves in all, takes several
 
 
 class Codes:
@@ -36,11 +36,15 @@ class Codes:
 
     def answer_codes(self, codes, scales, leaves, gates, dtype=torch.float32):
         """The same of rows that are held as codes."""
-        y = None
-        for a in range(0, leaves.shape[1], MAX_LEAVES_A_ROW):
-            part = [t[:, a:a + MAX_LEAVES_A_ROW].contiguous() for t in (leaves, gates)]
-            z = B.gbdt_mixture_product_codes(codes, scales, self.weight, self.scales, *part, bias=self.bias, dtype=torch.float32)
-            y = z if y is None else y + z
+        y, n_leaves = None, self.weight.shape[0]
+        for first in range(0, max(1, n_leaves), MAX_LEAVES):
+            # (the others are outside this part's leaves, and passed over)
+            matrices = [t[first:first + MAX_LEAVES] for t in (self.weight, self.scales, self.bias)]
+            here = leaves - first if first else leaves
+            for a in range(0, max(1, leaves.shape[1]), MAX_LEAVES_A_ROW):
+                part = [t[:, a:a + MAX_LEAVES_A_ROW].contiguous() for t in (here, gates)]
+                z = B.gbdt_mixture_product_codes(codes, scales, *matrices[:2], *part, bias=matrices[2], dtype=torch.float32)
+                y = z if y is None else y + z
         return y.to(dtype)
 
 
