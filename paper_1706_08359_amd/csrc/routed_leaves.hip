@@ -296,7 +296,8 @@ bool few_rows(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t d_in, int64_t
   const double products = (double)(n_rows * k) * (double)d_out * (double)std::max<int64_t>(d_in, 64 * kChunk<T>);
   const double taken = (double)std::min(n_leaves, n_rows * k) * (double)d_in * (double)d_out;
   const double room = sizeof(T) == 2 ? 34e6 + 1.2 * taken : sizeof(T) == 4 ? 23e6 + 2.5 * taken : 80e6 + 1.6 * taken;
-  return n_rows <= kMaxGridRows && (n_rows <= 4 || products <= room);
+  // (four rows: 2^24 outputs at most, two a wavefront)
+  return n_rows <= 4 || (n_rows <= kMaxGridRows && products <= room && n_rows * ceil_div(d_out, 2) <= most_blocks(64));
 }
 
 // Products of all rows, kept in slots and added up, so many rows at a time as the plan says.  products(g, r): of the rows from r on,
