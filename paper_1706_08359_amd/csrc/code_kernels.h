@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(64) code_few_kernel(const CodeArgs g) {
 #pragma unroll
         for (int s = 32; s > 0; s >>= 1) all += __shfl_xor(all, s);
         const int64_t o = (int64_t)leaf[j] * g.d_out + (o0 + i < g.d_out ? o0 + i : o0);
-        y[i] = __builtin_fmaf(gate[j], __builtin_fmaf((float)all * row_scale, g.col_scales[o], g.add ? g.add[o] : 0.0f), y[i]);
+        y[i] = __builtin_fmaf(gate[j], scaled((float)all, row_scale, g.col_scales[o], g.add ? g.add[o] : 0.0f), y[i]);
       }
     }
   }

@@ -177,6 +177,13 @@ struct TilePlaces {
   }
 };
 
+// sum a b + add for scales a and b: times the smaller first, which neither overflows nor underflows (scales are 0 or normal numbers, a sum is
+// 0 or at least 1) unless the product of all three does.
+__device__ __forceinline__ float scaled(float sum, float a, float b, float add) {
+  const bool first = fabsf(a) < fabsf(b);  // (a NaN is one of the two either way)
+  return __builtin_fmaf(sum * (first ? a : b), first ? b : a, add);
+}
+
 // A tile's results to their rows, through the last stage.
 template <class S, class G, class To, class Where>
 __device__ __forceinline__ void store_rows(char* lds, const G& g, const To& to, typename S::Acc (&acc)[S::TM][S::TN], const Where& places,
@@ -197,7 +204,7 @@ __device__ __forceinline__ void store_rows(char* lds, const G& g, const To& to, 
     if constexpr (To::kScaled) {
       f32x4 v;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = __builtin_fmaf((float)acc[i][j][r] * places(i).factor, scale[j][r], add[j][r]);
+      for (int r = 0; r < 4; ++r) v[r] = scaled((float)acc[i][j][r], places(i).factor, scale[j][r], add[j][r]);
       return v;
     } else {
       return acc[i][j] + add[j];
