@@ -569,7 +569,8 @@ __device__ __forceinline__ Piece find_piece(const LeafArgs<T>& g, int piece) {
   return r;
 }
 
-// LISTED: dy holds a row for every position, in the list's order, of ld_dy values from output row_first on, zeros behind the outputs.
+// LISTED: dy holds a row for every position, in the list's order, of ld_dy values from output row_first on, zeros behind the outputs; of
+// 16-bit values dW alone.
 template <class S, bool LONG, bool LISTED>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafArgs<typename S::T> g) {
   typedef typename S::T T;
@@ -633,7 +634,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
     float sum[S::TM];
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) sum[i] = 0.0f;
-    const bool sums = __builtin_amdgcn_readfirstlane(g.dbias != nullptr && col == 0 && w % S::WN == 0);
+    const bool sums = (!LISTED || sizeof(T) == 4) && __builtin_amdgcn_readfirstlane(g.dbias != nullptr && col == 0 && w % S::WN == 0);
     for (;;) {
       tile_run<S, true>(lds, a, b, rows_a, rows_b, c0, c1, acc, RowSums<S>{sum, sums});
       if (!LONG || c1 >= p1) break;
