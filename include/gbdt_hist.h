@@ -626,9 +626,8 @@ size_t gbdt_mixture_workspace_bytes(int64_t n_rows, int32_t k, int32_t n_leaves,
  *   dweight_out[l]   = sum over the slots of leaf l of gates dy x^T     DEVICE [n_leaves][d_out][d_in]
  *   dbias_out[l]     = sum over the slots of leaf l of gates dy         DEVICE [n_leaves][d_out]
  *   dgates_out[d][j] = <dy[d], W_l x[d] + b_l>                          DEVICE float [n_rows][k], 0 for a slot passed over
- * weight is read for dx and dgates, x for dweight and dgates, bias for dgates.  All sums are f32.  In dweight gates * dy is rounded to
- * the element type before it is multiplied: bf16 results are off by up to half a step (2^-9) of the sum of the terms' magnitudes beside
- * their own rounding; where terms do not cancel that is 1.4 times the error of rounding exact ones, root mean square.
+ * weight is read for dx and dgates, x for dweight and dgates, bias for dgates.  All sums are f32.  In dweight bf16 gates * dy
+ * is held as the sum of two bf16 values: 2^-18 of a term's magnitude is left out.
  * The slots' scratch as above; that of dweight holds gates * dy of so many outputs as take 256 MiB, or of 128
  * (f32: 64), beside the sums of leaves that are long (as gbdt_leaf_product_grad).  The same call gives the same bits.
  */

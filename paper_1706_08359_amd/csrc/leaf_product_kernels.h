@@ -91,8 +91,8 @@ __device__ __forceinline__ ListRows<T> list_rows(const T* base, int64_t ld, int 
   return {base, base + (int64_t)(g.n_rows - 1) * ld + cols, ld, g.row_idx, stop, g.n_rows};
 }
 
-// The same from a copy of a part of the list in local memory, -1 where there is no row.
-template <typename T>
+// The same from a copy of a part of the list in local memory, -1 where there is no row.  EACH: so many k stand for a position.
+template <typename T, int EACH = 1>
 struct CopiedRows {
   static constexpr bool kEven = false;
   const T* base;
@@ -100,7 +100,7 @@ struct CopiedRows {
   int64_t ld;
   const __attribute__((address_space(3))) int* ids;  // (said outright: a flat load would be waited for with all others)
   int32_t first;  // the position of ids[0]
-  __device__ __forceinline__ int fetch(int p) const { return ids[p - first]; }
+  __device__ __forceinline__ int fetch(int k) const { return ids[k / EACH - first]; }
   __device__ __forceinline__ const T* at(int, int d) const { return d >= 0 ? row_of(base, d, ld) : nullptr; }
 };
 
@@ -570,7 +570,9 @@ __device__ __forceinline__ Piece find_piece(const LeafArgs<T>& g, int piece) {
 }
 
 // LISTED: dy holds a row for every position, in the list's order, of ld_dy values from output row_first on, zeros behind the outputs; of
-// 16-bit values dW alone.
+// 16-bit values two one after the other, whose sum is meant, and dW alone.  (k then counts rows of dy, from the copied list's first on.)
+template <typename T, bool LISTED>
+constexpr int kRowsEach = LISTED && sizeof(T) == 2 ? 2 : 1;
 template <class S, bool LONG, bool LISTED>
 __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafArgs<typename S::T> g) {
   typedef typename S::T T;
@@ -599,32 +601,38 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   const int m0 = row0 + (w / S::WN) * (S::TM * 16);
 
   const auto listed = (const __attribute__((address_space(3))) int*)ids;
+  constexpr int each = kRowsEach<T, LISTED>;
   typedef typename std::conditional<LISTED, PlainRows<T>, CopiedRows<T>>::type RowsOfDy;
   RowsOfDy rows_a;
-  if constexpr (LISTED) {
-    rows_a = plain_rows(g.dy - g.row_first, g.ld_dy, g.n_positions, g.row_first + (int)g.ld_dy);
-  } else {
+  if constexpr (!LISTED) {
     rows_a = {g.dy, g.dy + (int64_t)(g.n_rows - 1) * g.ld_dy + g.d_out, g.ld_dy, listed, p0};
   }
   const int dy_cols = LISTED ? g.row_first + (int)g.ld_dy : g.d_out;
-  CopiedRows<T> rows_b = {g.x, g.x + (int64_t)(g.n_rows - 1) * g.ld_x + g.d_in, g.ld_x, listed, p0};
+  CopiedRows<T, each> rows_b = {g.x, g.x + (int64_t)(g.n_rows - 1) * g.ld_x + g.d_in, g.ld_x, listed, p0};
   typename S::ColumnsA a;
   typename S::ColumnsB b;
   int c0 = p0, c1 = p0;  // the positions copied
   auto copy_ids = [&](int from) {
-    c0 = rows_b.first = from;
-    if constexpr (!LISTED) rows_a.first = from;
+    c0 = from;
     c1 = !LONG || p1 - from < kCopiedIds ? p1 : from + kCopiedIds;
+    rows_b.first = LISTED ? 0 : from;
+    if constexpr (LISTED) {
+      rows_a = plain_rows(g.dy + (int64_t)from * each * g.ld_dy - g.row_first, g.ld_dy, each * (c1 - from), dy_cols);
+    } else {
+      rows_a.first = from;
+    }
     for (int p = c0 + (int)threadIdx.x; p < c1; p += S::NT) {
       const int d = g.row_idx ? g.row_idx[p] : p;
       ids[p - c0] = (uint32_t)d < (uint32_t)g.n_rows ? d : -1;
     }
     __syncthreads();
   };
+  auto k0 = [&] { return LISTED ? 0 : c0; };
+  auto k1 = [&] { return LISTED ? each * (c1 - c0) : c1; };
   auto begin_columns = [&](int col) {
-    a.init(rows_a, row0, dy_cols, c0, c1);
-    b.init(rows_b, col, g.d_in, c0, c1);
-    tile_begin<S>(lds, a, b, rows_a, rows_b, c0, c1);
+    a.init(rows_a, row0, dy_cols, k0(), k1());
+    b.init(rows_b, col, g.d_in, k0(), k1());
+    tile_begin<S>(lds, a, b, rows_a, rows_b, k0(), k1());
   };
   copy_ids(p0);
   begin_columns(col_first);
@@ -636,7 +644,7 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
     for (int i = 0; i < S::TM; ++i) sum[i] = 0.0f;
     const bool sums = (!LISTED || sizeof(T) == 4) && __builtin_amdgcn_readfirstlane(g.dbias != nullptr && col == 0 && w % S::WN == 0);
     for (;;) {
-      tile_run<S, true>(lds, a, b, rows_a, rows_b, c0, c1, acc, RowSums<S>{sum, sums});
+      tile_run<S, true>(lds, a, b, rows_a, rows_b, k0(), k1(), acc, RowSums<S>{sum, sums});
       if (!LONG || c1 >= p1) break;
       __syncthreads();  // everyone has read the last of these ids
       copy_ids(c1);

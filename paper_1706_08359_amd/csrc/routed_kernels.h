@@ -285,10 +285,10 @@ __global__ void __launch_bounds__(256) clear_rows_kernel(const int32_t* leaves, 
 
 // ---------------------------------------------------------------- gradients of the weights
 
-// g dy of every position, in the list's order, rounded to the products' type: dW_l = sum (g dy) x^T then is the sum of
-// leaf_grad_weight_kernel, 148 us for 32,768 positions of 64 leaves, 1,024 x 1,024, bf16 (460 TFLOP/s).  The matrix cores take bf16 only,
-// and two values for g dy would take them twice as long; one is off by half a step of each term, which adds as much to a result's error as
-// its own rounding: 2.4e-3 of bf16 results' size in all, 1.7e-3 without.  Bound by memory: the same case 22 us, 6 TB/s.
+// g dy of every position, in the list's order: dW_l = sum (g dy) x^T then is the sum of leaf_grad_weight_kernel, 238 us for 32,768
+// positions of 64 leaves, 1,024 x 1,024, bf16.  The matrix cores take bf16 only, so g dy is the sum of two such values, 16 bits: 2^-18 of a term
+// is left out.  (One value, off by half a step of every term: 139 us, and 2.3e-3 of the results' size instead of the 1.7e-3 of their own rounding.)
+// Bound by memory: the same case 32 us, 6.3 TB/s.
 //  Columns [first, first + cols) of dy, zeros up to ld; positions from `from` on.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256) gated_rows_kernel(const RoutedArgs<T> g, T* out, int64_t ld, int first, int cols, int from) {
@@ -298,16 +298,23 @@ __global__ void __launch_bounds__(256) gated_rows_kernel(const RoutedArgs<T> g, 
   const T* dy = row_of(g.dy, g.row_idx[p], g.ld_dy) + first;
   constexpr int n = kChunk<T>;
   for (int c = (int)(threadIdx.x & (LANES - 1)) * n; c < ld; c += LANES * n) {
-    T t[n];
+    T t[n], rest[n];
     if (c + n <= cols) {
       __builtin_memcpy(t, dy + c, sizeof t);
-#pragma unroll
-      for (int e = 0; e < n; ++e) t[e] = (T)(gate * (float)t[e]);
     } else {
 #pragma unroll
-      for (int e = 0; e < n; ++e) t[e] = c + e < cols ? (T)(gate * (float)dy[c + e]) : (T)0.0f;
+      for (int e = 0; e < n; ++e) t[e] = c + e < cols ? dy[c + e] : (T)0.0f;
     }
-    __builtin_memcpy(out + (int64_t)p * ld + c, t, sizeof t);
+#pragma unroll
+    for (int e = 0; e < n; ++e) {
+      const float v = gate * (float)t[e];
+      t[e] = c + e < cols ? (T)v : (T)0.0f;
+      rest[e] = fabsf((float)t[e]) < INFINITY ? (T)(v - (float)t[e]) : (T)0.0f;
+    }
+    constexpr int each = kRowsEach<T, true>;
+    T* to = out + (int64_t)p * each * ld + c;
+    __builtin_memcpy(to, t, sizeof t);
+    if constexpr (each == 2) __builtin_memcpy(to + ld, rest, sizeof rest);
   }
 }
 

@@ -193,10 +193,11 @@ WeightPlan weight_plan(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t d_in
   const int64_t pairs = n_rows * k;
   p.list = list_plan(pairs, n_leaves);
   p.sums = leaf_grad_plan(e, pairs, d_in, d_out, units);
-  p.piece = std::max(p.sums.bm, kGatedBytes / std::max<int64_t>(1, pairs * e) / p.sums.bm * p.sums.bm);
+  const int64_t a_value = e == 2 ? 4 : e;  // (two of 16 bits, gbdt_leaf::kRowsEach)
+  p.piece = std::max(p.sums.bm, kGatedBytes / std::max<int64_t>(1, pairs * a_value) / p.sums.bm * p.sums.bm);
   p.piece = std::min(p.piece, d_out);
   p.ld = round_up(p.piece, 16 / e);
-  p.gated_bytes = pad256((size_t)(pairs * p.ld * e));
+  p.gated_bytes = pad256((size_t)(pairs * p.ld * a_value));
   return p;
 }
 
