@@ -627,9 +627,9 @@ size_t gbdt_mixture_workspace_bytes(int64_t n_rows, int32_t k, int32_t n_leaves,
  *   dbias_out[l]     = sum over the slots of leaf l of gates dy         DEVICE [n_leaves][d_out]
  *   dgates_out[d][j] = <dy[d], W_l x[d] + b_l>                          DEVICE float [n_rows][k], 0 for a slot passed over
  * weight is read for dx and dgates, x for dweight and dgates, bias for dgates.  All sums are f32.  In dweight bf16 gates * dy
- * is held as the sum of two bf16 values: 2^-18 of a term's magnitude is left out.
+ * is held as the sum of two bf16 values: 2^-17 of a term's magnitude is left out at most.
  * The slots' scratch as above; that of dweight holds gates * dy of so many outputs as take 256 MiB, or of 128
- * (f32: 64), beside the sums of leaves that are long (as gbdt_leaf_product_grad).  The same call gives the same bits.
+ * (64 in f32, and where 128 take more than 1 GiB), beside the sums of leaves that are long (as gbdt_leaf_product_grad).  The same call gives the same bits.
  */
 int gbdt_mixture_product_grad(const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
                               const void* weight, const void* bias, const int32_t* leaves,

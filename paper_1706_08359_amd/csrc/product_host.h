@@ -125,9 +125,10 @@ struct LeafGradPlan {
   int64_t bm, bn, tiles, cut;
   size_t bytes;
 };
-inline LeafGradPlan leaf_grad_plan(int64_t e, int64_t n_positions, int64_t d_in, int64_t d_out, int64_t units) {
+// few: tiles of 64 outputs whatever their number.
+inline LeafGradPlan leaf_grad_plan(int64_t e, int64_t n_positions, int64_t d_in, int64_t d_out, int64_t units, bool few = false) {
   LeafGradPlan p;
-  p.bm = e == 4 || d_out <= 64 ? 64 : 128;
+  p.bm = e == 4 || d_out <= 64 || few ? 64 : 128;
   p.bn = e == 4 ? 64 : 128;
   p.tiles = ceil_div(d_out, p.bm) * ceil_div(d_in, p.bn);
   const int64_t fill = p.tiles >= 2 * units ? n_positions : ceil_div(n_positions * p.tiles, 2 * units);

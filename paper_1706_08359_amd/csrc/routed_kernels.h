@@ -286,8 +286,8 @@ __global__ void __launch_bounds__(256) clear_rows_kernel(const int32_t* leaves, 
 // ---------------------------------------------------------------- gradients of the weights
 
 // g dy of every position, in the list's order: dW_l = sum (g dy) x^T then is the sum of leaf_grad_weight_kernel, 238 us for 32,768
-// positions of 64 leaves, 1,024 x 1,024, bf16.  The matrix cores take bf16 only, so g dy is the sum of two such values, 16 bits: 2^-18 of a term
-// is left out.  (One value, off by half a step of every term: 139 us, and 2.3e-3 of the results' size instead of the 1.7e-3 of their own rounding.)
+// positions of 64 leaves, 1,024 x 1,024, bf16.  The matrix cores take bf16 only, so g dy is the sum of two such values: 2^-17 of a term at
+// most is left out.  (One value, off by half a step of every term: 139 us, and 2.3e-3 of the results' size instead of the 1.7e-3 of their own rounding.)
 // Bound by memory: the same case 32 us, 6.3 TB/s.
 //  Columns [first, first + cols) of dy, zeros up to ld; positions from `from` on.
 template <typename T, int LANES>

@@ -152,8 +152,9 @@ int make_lists(const ListPlan& plan, const int32_t* leaves, int32_t n_leaves, in
 
 // Slots of so many rows at a time as take this, or of 1,024.
 constexpr int64_t kSlotsBytes = (int64_t)256 << 20;
-// Weighted gradients of so many outputs at a time as take this, or of a tile.
-constexpr int64_t kGatedBytes = (int64_t)256 << 20;
+// Weighted gradients of so many outputs at a time as take this, or of a tile, which is one of 64 outputs where 128 would take more than the
+// second number.
+constexpr int64_t kGatedBytes = (int64_t)256 << 20, kTileBytes = (int64_t)1 << 30;
 constexpr int32_t kMaxSlots = 64;  // leaves a row
 constexpr int64_t kMaxGridRows = 65535;  // rows of a launch's second dimension
 
@@ -192,8 +193,8 @@ WeightPlan weight_plan(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t d_in
   WeightPlan p;
   const int64_t pairs = n_rows * k;
   p.list = list_plan(pairs, n_leaves);
-  p.sums = leaf_grad_plan(e, pairs, d_in, d_out, units);
   const int64_t a_value = e == 2 ? 4 : e;  // (two of 16 bits, gbdt_leaf::kRowsEach)
+  p.sums = leaf_grad_plan(e, pairs, d_in, d_out, units, pairs * 128 * a_value > kTileBytes);
   p.piece = std::max(p.sums.bm, kGatedBytes / std::max<int64_t>(1, pairs * a_value) / p.sums.bm * p.sums.bm);
   p.piece = std::min(p.piece, d_out);
   p.ld = round_up(p.piece, 16 / e);
