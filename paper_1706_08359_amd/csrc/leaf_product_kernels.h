@@ -579,8 +579,9 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   __shared__ __align__(16) char lds[S::kLdsBytes];
   __shared__ int ids[kCopiedIds];
   // A piece's workgroups share its rows and so are one XCD's; pieces, which are of any length, go round.  LISTED: leaves that are whole
-  // are of more unequal length than cuts make pieces, and each is all XCDs' work, a part of the columns each (8,192 rows x 4 leaves, 1,024 x
-  // 1,024 x 64: 148 us against 171).
+  // are of more unequal length than cuts make pieces, and each is all XCDs' work, a part of the columns each (with one row of dy a position, 8,192
+  // rows x 4 leaves, 1,024 x 1,024 x 64: 148 us against 171), or of the outputs where dy has two (30,000 rows, one of 8 leaves, 1,024 ->
+  // 512, lists and weighted rows included: 131 us against 147 by columns).
   const uint32_t tiles = g.col_tiles * g.row_tiles, at = blockIdx.x / 8;
   const int piece = (int)(g.first + (LISTED ? blockIdx.x / tiles : at / tiles * 8 + blockIdx.x % 8));
   const int r = (int)(LISTED ? blockIdx.x % tiles : at % tiles);
@@ -592,7 +593,9 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   const int cols_per = p1 - p0 <= kShortPiece ? (int)g.cols_per : 1;
   const int turns = ((int)g.col_tiles + cols_per - 1) / cols_per;
   if (r >= turns * (int)g.row_tiles) return;
-  const int row0 = (LISTED ? g.row_first : 0) + r / turns * S::BM, col_first = r % turns * cols_per * S::BN;
+  constexpr int each = kRowsEach<T, LISTED>;
+  const int row_tile = each == 2 ? r % (int)g.row_tiles : r / turns, turn = each == 2 ? r / (int)g.row_tiles : r % turns;
+  const int row0 = (LISTED ? g.row_first : 0) + row_tile * S::BM, col_first = turn * cols_per * S::BN;
   const bool whole = at_piece.whole;
   float* part = g.partial + at_piece.slot * ((int64_t)(g.d_in + 1) * g.d_out);
   const int all_cols = g.dw ? g.d_in : 1;  // (the outputs' sums alone come with the first tile)
@@ -601,7 +604,6 @@ __global__ void __launch_bounds__(S::NT, 2) leaf_grad_weight_kernel(const LeafAr
   const int m0 = row0 + (w / S::WN) * (S::TM * 16);
 
   const auto listed = (const __attribute__((address_space(3))) int*)ids;
-  constexpr int each = kRowsEach<T, LISTED>;
   typedef typename std::conditional<LISTED, PlainRows<T>, CopiedRows<T>>::type RowsOfDy;
   RowsOfDy rows_a;
   if constexpr (!LISTED) {
