@@ -141,7 +141,7 @@ struct ToScaled {
 
 // Bound by the gathered rows of codes where outputs are few: 400,000 x 2,000 -> 128 in 255 leaves, 274 us, 3.6 TB/s of rows' lines and
 // matrices, waiting for half of the cycles (tiles of 128 x 128, two a unit, 307; with two stages instead of three 293); by the ends
-// of tiles where they are many: 32,768 pairs, 1,024 -> 1,024 in 64 leaves, 70 us, 980 TOP/s.
+// of tiles where they are many: 32,768 pairs, 1,024 -> 1,024 in 64 leaves, 72 us, 950 TOP/s.
 template <class S, typename O, Place WHERE>
 __global__ void __launch_bounds__(S::NT, 2) code_product_kernel(const CodeArgs g) {
   __shared__ __align__(16) char lds[S::kLdsBytes];

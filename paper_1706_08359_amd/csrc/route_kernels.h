@@ -338,9 +338,14 @@ __device__ __forceinline__ void load_logits(const T* row, int column, int n, flo
   for (int i = 0; i < PER; ++i) l[i] = l[i] == l[i] ? l[i] : -INFINITY;
 }
 
-// A row's choice values; *tol: the error of a value in f32 beside 2^-23 of its size.  (Sigmoid: its
-// exponential's error, (|l| + 2) 2^-24, times s (1 - s), below 2^-24, and 2^-23 for the sum and the reciprocal, of at most 1.
-// Softmax, all of the largest score: x exp(-x) 2^-24, below 2^-25, of each and PER + 6 roundings and 2^-22 of the sum.)
+// A row's choice values; *tol: the most that the difference of two may be off by in f32 beside 2^-23 of their sizes (the bias' sum).  In u = 2^-24,
+// for x = |l| or top - l:
+//   sigmoid   the exponential: its argument's roundings, 1.5 x u, and 2 u of the instruction, times s (1 - s): 0.9 u; 1 + it and the
+//             reciprocal, 3 u.  Twice that: 8 u, of 16.
+//   softmax   all divide by the same sum, so its error counts once, times a difference of scores, at most the largest score 1 / sum: 36
+//             additions and the reciprocal 37 u, the exponentials (2.5 x + 2) u each, on average over their own sizes 14 u, since a
+//             softmax of 1,024 has an average x below 4.5; the two scores' own, 2.5 x exp(-x) + 3, twice 4 u.  59 u of the largest score, of 64.
+// (A group's value is two of them, and allowed for as much again.)
 template <typename V, int LANES, int PER>
 __device__ __forceinline__ void choice_values(const RouteArgs& g, const float (&l)[PER], float top, V (&v)[PER], V* tol) {
   const int lane = threadIdx.x & (LANES - 1);
@@ -420,12 +425,13 @@ struct Slots {
   }
 };
 
-// Bound by reading the logits where rows are many and k is small: 400,000 x 255 f32, four leaves each, 115 us, 3.7 TB/s.  A pick is some
-// 130 instructions for four rows of 256 columns: 16,384 x 256 bf16 in 8 groups, 8 leaves each by values, 18 us, 12 of it nine picks, 4 the few
-// rows that 64 bits decide, which end last; 65,536 x 64 f32, four leaves each by values, 14 us.
+// Bound by reading the logits where rows are many and k is small: 400,000 x 255 f32, four leaves each, 107 us a call among others, 3.9 TB/s (115
+// by itself under a profiler).  A pick is some 130 instructions for four rows of 256 columns: 16,384 x 256 bf16 in 8 groups, 8 leaves each by
+// values, 17 to 19 us, 12 of it nine picks, 4 the few rows that 64 bits decide, which end last; 65,536 x 64 f32, four leaves each by values, 14 us.
 // VALUES: leaves (without a bias: their groups) are chosen by their values, not by the logits themselves.
-// (At most 128 registers, which only the 64-bit path would pass: 100,000 x 700 f32, 16 leaves each by
-// values, 295 us against 381.)
+// (At most 128 registers.  From 24 columns a lane on by values, more would be taken, most of them on the 64-bit path, and some are kept
+// in memory; even so, 100,000 rows f32, 16 leaves each by values: x 285 135 us against 149 with as many as it takes, x 512 187 against 258, x
+// 700 274 against 375, x 1,024 316 against 767.)
 template <typename T, int LANES, int PER, bool VALUES>
 __global__ void __launch_bounds__(kThreads, 4) route_kernel(const RouteArgs g) {
   constexpr int rows = kThreads / LANES;

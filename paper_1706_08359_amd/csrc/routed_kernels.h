@@ -107,8 +107,8 @@ struct ToGatedRows {
 enum class Leaves { kSlots, kRows };
 
 // Answers of all pairs.  Bound by the matrix cores and by what a tile's beginning and end leave them idle: 65,536 pairs, 1,024 -> 1,024 in
-// 64 leaves, bf16: 180 us, 760 TFLOP/s, matrix cores busy for 38 % of the cycles, compute units for 80 (leaves end inside tiles of
-// 256 rows, and 4.5 tiles a unit are five turns).  256 pairs of 64 leaves, tiles of 32 rows: 25 us, 5.1 TB/s of matrices, some of which
+// 64 leaves, bf16: 205 us, 670 TFLOP/s, matrix cores busy for 33 % of the cycles, compute units for 77 (leaves end inside tiles of
+// 256 rows, and 4.5 tiles a unit are five turns; 268 MB of answers are written beneath).  256 pairs of 64 leaves, tiles of 32 rows: 25 us, 5.1 TB/s of matrices, some of which
 // the memory-side cache holds.
 template <class S, Leaves WHAT>
 __global__ void __launch_bounds__(S::NT, 2) routed_product_kernel(const RoutedArgs<typename S::T> g) {
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(S::NT, 2) routed_product_kernel(const RoutedAr
 }
 
 // Gradients of the rows by every pair.  Bound as above, beside reading x once more for the gates' gradients: 32,768 pairs, 1,024 ->
-// 1,024 in 64 leaves, bf16: 130 us (111 the answers); 60,033 pairs, 33 -> 137 in 63 leaves, f32: 39 us, tiles of 64 half full of k.
+// 1,024 in 64 leaves, bf16: 141 us (114 the answers); 60,033 pairs, 33 -> 137 in 63 leaves, f32: 39 us, tiles of 64 half full of k.
 template <class S, bool DOTS>
 __global__ void __launch_bounds__(S::NT, 2) routed_grad_input_kernel(const RoutedArgs<typename S::T> g) {
   typedef typename S::T T;
@@ -222,8 +222,8 @@ __device__ __forceinline__ void gate_gradients(const CombineArgs<O>& g, int64_t 
 }
 
 // out[d] = sum_j g[d][j] slot_j, LANES lanes a row, 16 bytes of a slot each at a time, eight slots on their way; dgates[d][j] =
-// the sum of the pair's dots and <bias, dy>.  Bound by reading the slots: 8,192 rows x 8 slots of 1,024 fp16 values, 25 us, 6 TB/s (they
-// are in the memory-side cache); x 4, 18 us, with the gates' gradients 28.
+// the sum of the pair's dots and <bias, dy>.  Bound by reading the slots: 8,192 rows x 8 slots of 1,024 values, 49 us, 5.5 TB/s (the
+// memory-side cache has some); x 4, 28 us, with the gates' gradients 35.
 template <typename O, int LANES, bool GATES>
 __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs<O> g) {
   constexpr int n = 4;
@@ -285,9 +285,9 @@ __global__ void __launch_bounds__(256) clear_rows_kernel(const int32_t* leaves, 
 
 // ---------------------------------------------------------------- gradients of the weights
 
-// g dy of every position, in the list's order: dW_l = sum (g dy) x^T then is the sum of leaf_grad_weight_kernel, 238 us for 32,768
+// g dy of every position, in the list's order: dW_l = sum (g dy) x^T then is the sum of leaf_grad_weight_kernel, 225 to 245 us for 32,768
 // positions of 64 leaves, 1,024 x 1,024, bf16.  The matrix cores take bf16 only, so g dy is the sum of two such values: 2^-17 of a term at
-// most is left out.  (One value, off by half a step of every term: 139 us, and 2.3e-3 of the results' size instead of the 1.7e-3 of their own rounding.)
+// most is left out.  (One value, off by half a step of every term: 140 us, and 2.3e-3 of the results' size instead of the 1.7e-3 of their own rounding.)
 // Bound by memory: the same case 32 us, 6.3 TB/s.
 //  Columns [first, first + cols) of dy, zeros up to ld; positions from `from` on.
 template <typename T, int LANES>

@@ -61,9 +61,10 @@ int launch_route(RouteArgs g, bool grad, hipStream_t s) {
   });
 }
 
-// (400,000 rows x 255, four leaves each: 125 us by sixteen lanes a row, 148 by eight, 158 by 32, 219 by 64.  65,536 x 64 with a bias and
-// the gradient: 25.5 by eight, 27.1 by sixteen.  100,000 x 285, 16 leaves each: 105 by sixteen, 142 by 32; x 700: 200 by 32, 268 by 64; x
-// 1,024: 232 by 32, 256 by 64.)
+// (f32, calls among others.  By logits: 400,000 rows x 255, four leaves each: 107 us by sixteen lanes a row, 114 by eight, 139 by 32, 211 by 64;
+// 100,000 x 285, 16 leaves each: 100 by sixteen, 114 by 32; x 700: 190 by 32, 216 by 64; x 1,024: 224 by 32, 251 by 64.  By values: 65,536 x
+// 64 and the gradient: 22.6 by eight, 24.7 by sixteen; 100,000 x 285, 16 leaves each: 136 and 159; x 700: 269 and 320; x 1,024: 310 and 364; but
+// 400,000 x 200, eight leaves each: 242 by sixteen, 223 by eight.)
 template <typename T>
 int route(const RouteArgs& g, bool grad, hipStream_t s) {
   if (g.n_leaves <= 64) return launch_route<T, 8, 8>(g, grad, s);
@@ -281,7 +282,7 @@ int launch_combine(const CombineArgs<O>& g, hipStream_t s) {
   LAUNCHED("combine_kernel");
   return GBDT_OK;
 }
-// (20,011 rows x 3 leaves, 137 -> 33, f32, a training step: 152 us with sixteen lanes a row of 137 values, 163 with 64.)
+// (20,011 rows x 3 leaves, 137 -> 33, f32, a training step: 148 us with sixteen lanes a row of 137 values, 162 with 64.)
 template <typename O>
 int combine(const CombineArgs<O>& g, hipStream_t s) {
   return g.cols <= 256 ? launch_combine<O, 16>(g, s) : launch_combine<O, 64>(g, s);
@@ -290,9 +291,11 @@ int combine(const CombineArgs<O>& g, hipStream_t s) {
 // So few rows that a wavefront for every few outputs of a row takes less than lists, tiles and slots.  It reads a matrix again for
 // every row that takes the leaf: pairs x outputs x inputs, of 64 chunks at least, at 3.8 million a us (f32 2.1, codes 9), after 4 us; the
 // other way is 13 us and each matrix that is taken once, 0.3 us a million values more (f32, whose tiles are mostly empty, 1.2; codes
-// 0.18).  (bf16, us, this way / the other, pairs of 64 matrices of 1,024 x 1,024: 64 22/27, 128 34/33, 256 64/33; of 255 of 700 x 256: 256
-// 16/29, 512 33/30; of 8 of 256 x 64: 512 8.0/13, 2,000 21/15.  f32: 128 70/108, 256 141/110; 512 48/68, 2,000 174/81; 2,000 17/17.  Codes: 128
-// 19/25, 256 30/25; 512 20/23, 2,000 62/25; 512 7.3/14, 2,000 18/15.)
+// 0.18).  (us, this way / the other, k = 4.  bf16, pairs of 64 matrices of 1,024 x 1,024: 64 19/26, 128 35/30, 256 58/32; of 255 of 700 x
+// 256: 256 16/29, 512 25/29; of 8 of 256 x 64: 512 8.6/15, 2,000 16/16.  f32: 128 69/106, 256 138/107; 512 47/66, 2,000 170/80; 2,000 12/18.
+// Codes: 128 18/25, 256 32/25; 512 15/23, 2,000 43/26; 512 9.6/16, 2,000 13/17.  The kernels take four leaves at a time, and a k that is no multiple
+// of four costs this way more: k = 1 bf16 128 60/27, 512 56/26, 12/15; f32 83/102, 64/63; codes, the rule's worst, 30/22, 31/19,
+// 10/16.)
 template <typename T>
 bool few_rows(int64_t n_rows, int64_t k, int64_t n_leaves, int64_t d_in, int64_t d_out) {
   const double products = (double)(n_rows * k) * (double)d_out * (double)std::max<int64_t>(d_in, 64 * kChunk<T>);
