@@ -172,7 +172,7 @@ __device__ __forceinline__ V group_error(V one, V two, V tol) {
   return tol + (V)0x1p-22 * (fabs(one) + (two > lowest<V>() ? fabs(two) : (V)0));
 }
 // A group's value.  Two lowest values, as leaves are closed with, add up to minus infinity in f32, which is a group without a leaf: such a
-// one stays below all others, has an error without end, and 64 bits tell it from its like.
+// one has the lowest number, which its value is below, an error without end, and 64 bits tell it from its like.
 template <typename V>
 __device__ __forceinline__ V group_value(V one, V two) {
   if (!(two > lowest<V>())) return one;
@@ -184,8 +184,8 @@ template <typename V>
 struct Border {
   V least = (V)INFINITY, next = lowest<V>();
   __device__ __forceinline__ void add(bool kept, V worth, V error) {
-    const bool any = error < (V)INFINITY;  // (values whose sum leaves the numbers are anywhere)
-    const V low = any ? worth - error : lowest<V>(), high = any ? worth + error : (V)INFINITY;
+    const bool any = error < (V)INFINITY, closed = worth <= -(V)__FLT_MAX__;  // (values whose sum leaves the numbers otherwise are anywhere)
+    const V low = any ? worth - error : lowest<V>(), high = any ? worth + error : closed ? worth : (V)INFINITY;
     if (kept) {
       least = low < least ? low : least;
     } else {

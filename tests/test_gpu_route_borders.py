@@ -95,3 +95,21 @@ def test_without_a_bias_the_order_is_that_of_the_logits(score, dtype, n_groups, 
     assert bool((took[:, 1:] <= took[:, :-1]).all())
     want, _ = ref.route(l, k, **how)
     assert torch.equal(leaves, want.long())
+
+
+@pytest.mark.parametrize("n_groups,group_size", [(8, 8), (6, 2), (8, 32)])
+def test_values_of_opposite_sign_whose_sizes_leave_the_numbers(n_groups, group_size):
+    """3e38 and -3e38 add up to what their scores leave, and their sizes to more than f32 holds: 64 bits alone can tell the groups apart."""
+    g = torch.Generator().manual_seed(n_groups)
+    l = torch.randn(60, n_groups * group_size, generator=g)
+    l.view(60, n_groups, group_size)[:, :, 2:] = -math.inf
+    bias = torch.zeros(n_groups, group_size)
+    bias[:, 0] = 3e38 * (1 - 2.0 ** -10 * torch.rand(n_groups, generator=g))
+    bias[:, 1] = -bias[:, 0] * (1 + 2.0 ** -20 * torch.randint(-3, 4, (n_groups,), generator=g))
+    bias[n_groups - 1, :2] = torch.finfo(torch.float32).min
+    bias = bias.view(-1)
+    for kept in (1, 2, n_groups - 1, n_groups):
+        how = dict(score="sigmoid", n_groups=n_groups, groups_kept=kept, group_best=2)
+        leaves, _ = B.gbdt_route(l.cuda(), 2 * kept, choice_bias=bias.cuda(), **how)
+        want, _ = ref.route(l, 2 * kept, choice_bias=bias, **how)
+        assert torch.equal(leaves.cpu(), want), kept
